@@ -325,6 +325,113 @@ int thinfer_op_argmax(const void* logits, void* ids, int32_t rows, int32_t n, vo
 int thinfer_op_rmsnorm(const void* x, const void* gain, void* y, int32_t rows, int32_t n, float eps,
                        void* cuda_stream);
 
+/* ------------------------------------------------------------------------ *
+ * Per-head norm with rotation, and a key / value cache held in 4 bits on pages
+ * (no counterpart in the paper: later models of the family normalise queries
+ * and keys per head, and Section 3.4.1's per-request caches are what limits the
+ * number of requests a device holds).  Context-free: every pointer is device
+ * memory of the current device, every call only enqueues kernels on
+ * cuda_stream, allocates nothing and keeps nothing for the next call, and can
+ * be captured into a CUDA graph; a replayed graph follows the tables, lengths
+ * and positions it finds on the device at that time.  The text of a refusal is
+ * in thinfer_last_error(NULL).
+ * ------------------------------------------------------------------------ */
+
+/* turns[j] = base^(-2j/rotary_dim) / (2 pi), j < rotary_dim / 2: revolutions per position of each rotated pair, as
+ * thinfer_op_qk_norm_rope reads them.  host_out: host FP64 [rotary_dim / 2]; copy it to the device once.  Scaled
+ * frequencies are a matter of scaling these numbers. */
+int thinfer_rope_turns(float base, int32_t rotary_dim, double* host_out);
+
+/* RMSNorm of every query and key head over its head_dim values (FP32 inside), then the rotation of its first
+ * rotary_dim dimensions by 2 pi * position * turns[j], rounded to the storage type once:
+ *   x^ = x * gain / sqrt(mean(x^2) + eps),  (a, b) -> (a cos - b sin, b cos + a sin)
+ * halves 0: pairs are neighbours (2j, 2j+1), the framework's order; 1: pairs are (j, j + rotary_dim/2).
+ *   q FP16 [tokens][n_q_heads * head_dim], k FP16 [tokens][n_kv_heads * head_dim]; the strides count elements between
+ *   tokens, so that both may lie inside one fused projection output.  q_out / k_out: the same layout, may be q / k
+ *   themselves (same stride), must not overlap them otherwise.  q_gain, k_gain FP16 [head_dim].  turns FP64
+ *   [rotary_dim / 2].  positions int32 [tokens]; the outputs of a token with a negative position are left as they were.
+ * head_dim 64 or 128; rotary_dim a multiple of 16 up to head_dim (0: norm only); strides multiples of 8; pointers
+ * 16-byte aligned. */
+int thinfer_op_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out,
+                            int64_t q_out_stride, void* k_out, int64_t k_out_stride, const void* q_gain,
+                            const void* k_gain, const double* turns, const int32_t* positions, int32_t tokens,
+                            int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t rotary_dim, int32_t halves,
+                            float eps, void* cuda_stream);
+
+/* The cache.  A pool is [n_layers][n_pages][page] device bytes, 16-byte aligned; a page holds page_size (16, 32, 64 or
+ * 128) tokens of one layer, for every KV head one block of page_size * (head_dim + 8) bytes:
+ *   K codes  [page_size][head_dim/2]         byte i of a token: code 2i (low four bits), code 2i+1 (high four bits)
+ *   V codes  [page_size/2][head_dim/4][2][2] token pair, group of four dimensions, token of the pair, bytes as for K
+ *   K params [page_size][2], V params [page_size][2]: FP16 scale, offset of the token's row
+ * A row x (one token, one head, K or V) is stored with offset = min x, scale = (max x - min x) / 15 rounded to FP16,
+ * code = (x - offset) / scale rounded to nearest, ties to even, and is read as offset + scale * code.  A row with a NaN
+ * or an infinity (or whose range overflows the storage type) is read as NaN.
+ * table: int32 [n_rows][max_pages]; position p of row r lies on page table[r][p / page_size], slot p % page_size.  The
+ * same table serves all layers.  lens: int32 [n_rows], tokens of each row (negative: none).  A page is in use when a row names it
+ * among its first ceil(len / page_size) entries; several rows may name one page (fork).  Nothing else records who
+ * owns a page: a row is freed by setting its length to 0.  A row's length may be lowered (drafted tokens that were
+ * rejected), but not into a page that it shares with another row: what is appended there would change both.
+ * Pages out of range: appends there are dropped, reads and attention over them give NaN. */
+int thinfer_kv4_page_bytes(int32_t n_kv_heads, int32_t head_dim, int32_t page_size, size_t* bytes);
+
+/* Makes room for add[r] more tokens of every row (negative: none): rows in ascending order take the lowest free pages,
+ * their numbers are written into table, lens_out[r] = lens[r] + add[r].  A row whose pages, together with those asked
+ * for by the rows before it, exceed the free pages, or that would not fit max_pages, keeps its length and table;
+ * *refused (int32) counts those rows.  lens_out may be lens.  n_rows <= 4096, n_pages <= 262144. */
+int thinfer_op_kv4_reserve(int32_t* table, const int32_t* lens, const int32_t* add, int32_t* lens_out, int32_t* refused,
+                           int32_t n_rows, int32_t max_pages, int32_t n_pages, int32_t page_size, void* cuda_stream);
+
+/* Quantises tokens into one layer's pages: k, v FP16 [tokens][n_kv_heads * head_dim], strides in elements between
+ * tokens; token i goes to position positions[i] of row rows[i] (int32 [tokens]; a negative one skips the token), which
+ * have to be different places.  pool: the layer's [n_pages][page] bytes. */
+int thinfer_op_kv4_append(void* pool, int32_t n_pages, const int32_t* table, int32_t n_rows, int32_t max_pages,
+                          const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* rows,
+                          const int32_t* positions, int32_t tokens, int32_t n_kv_heads, int32_t head_dim,
+                          int32_t page_size, void* cuda_stream);
+
+/* Reads tokens of one layer back: FP16 values at k_out / v_out + i * token_stride + head * head_stride (elements) for
+ * token i = (rows[i], positions[i]); with head_stride = T * head_dim and token_stride = head_dim this is the layout
+ * thinfer_op_attention_prefill reads.  A token with a negative row or position is left as it was. */
+int thinfer_op_kv4_read(const void* pool, int32_t n_pages, const int32_t* table, int32_t n_rows, int32_t max_pages,
+                        void* k_out, void* v_out, int64_t token_stride, int64_t head_stride, const int32_t* rows,
+                        const int32_t* positions, int32_t tokens, int32_t n_kv_heads, int32_t head_dim,
+                        int32_t page_size, void* cuda_stream);
+
+/* Attention of the last `queries` tokens of every request over the cache of one layer (Eq. 6): request b is row b of
+ * table with lens[b] keys, its query tokens among them; query i attends the keys before position
+ * lens[b] - (queries - 1 - i) (one query: all of them).  A query that sees no key gives 0.  q FP16 [batch * queries]
+ * tokens of n_q_heads * head_dim values, q_stride elements apart, already rotated; out FP16 [batch][queries][n_q_heads
+ * * head_dim].  n_q_heads a multiple of n_kv_heads.  workspace: thinfer_kv4_attention_workspace bytes, 16-byte
+ * aligned; its contents mean nothing between calls, but calls that may overlap on the device need their own. */
+int thinfer_kv4_attention_workspace(int32_t batch, int32_t queries, int32_t n_q_heads, int32_t n_kv_heads,
+                                    int32_t head_dim, size_t* bytes);
+int thinfer_op_kv4_attention(const void* q, int64_t q_stride, const void* pool, int32_t n_pages, const int32_t* table,
+                             int32_t max_pages, const int32_t* lens, void* out, int32_t batch, int32_t queries,
+                             int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t page_size, void* workspace,
+                             size_t workspace_bytes, void* cuda_stream);
+
+/* Rows from rows: new row r holds what old row source[r] held (int32 [n_rows]; negative: nothing, the row is freed;
+ * source[r] = r keeps it).  Full pages are shared.  A partly filled last page stays with its own row where that row is
+ * kept, else with the lowest new row that took it over; every other heir gets a copy on the lowest page not in use
+ * before the call, in ascending row order, in all n_layers layers (filled tokens only, in groups of 16).  A row for
+ * which no page is left, or whose source is no row, becomes empty and is counted in *refused.  Entries of table_out
+ * behind a row's pages are -1.  table_out, lens_out and refused must not overlap the inputs.  The pool's pages in use
+ * before the call are not changed.  n_rows <= 4096, n_pages <= 262144. */
+int thinfer_kv4_pages_workspace(int32_t n_rows, int32_t n_pages, size_t* bytes);
+int thinfer_op_kv4_fork(void* pool, int32_t n_layers, int32_t n_pages, const int32_t* table, const int32_t* lens,
+                        const int32_t* source, int32_t* table_out, int32_t* lens_out, int32_t* refused, int32_t n_rows,
+                        int32_t max_pages, int32_t n_kv_heads, int32_t head_dim, int32_t page_size, void* workspace,
+                        size_t workspace_bytes, void* cuda_stream);
+
+/* Moves the pages in use to the front of the pool: with L pages in use, those numbered L and above move in ascending
+ * order into the free pages below L, in all n_layers layers (filled tokens only, in groups of 16).  table_out: the table
+ * with the new numbers, -1 behind a row's pages; *live_pages (int32) = L: the pool behind L pages may be given back.
+ * The outputs must not overlap the inputs. */
+int thinfer_op_kv4_compact(void* pool, int32_t n_layers, int32_t n_pages, const int32_t* table, const int32_t* lens,
+                           int32_t* table_out, int32_t* live_pages, int32_t n_rows, int32_t max_pages,
+                           int32_t n_kv_heads, int32_t head_dim, int32_t page_size, void* workspace,
+                           size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,348 @@
+// C entry points (include/thinfer.h) of the per-head norm with rotation and of the 4-bit paged cache.  Every call
+// checks its arguments on the host, enqueues its kernels on the given stream and returns; no call allocates, waits or
+// keeps anything for the next.
+#include <cmath>
+
+#include "kv4_attn.cuh"
+#include "kv4_cache.cuh"
+#include "kv4_pages.cuh"
+#include "op_host.cuh"
+#include "qk_norm_rope.cuh"
+
+using namespace thinfer;
+
+namespace {
+
+int page_shift_of(int page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : page == 128 ? 7 : -1; }
+
+int check_layout(int32_t n_kv, int32_t head_dim, int32_t page_size) {
+  if (n_kv <= 0 || head_dim <= 0 || page_size <= 0) return op_fail(THINFER_EINVAL, "n_kv_heads, head_dim and page_size must be positive");
+  if (head_dim != 64 && head_dim != 128) return op_fail(THINFER_EUNSUPPORTED, "head_dim %d: 64 and 128 are supported", head_dim);
+  if (page_shift_of(page_size) < 0) return op_fail(THINFER_EUNSUPPORTED, "page_size %d: 16, 32, 64 and 128 are supported", page_size);
+  if (n_kv > 1024) return op_fail(THINFER_EUNSUPPORTED, "n_kv_heads %d > 1024", n_kv);
+  return THINFER_OK;
+}
+
+int check_tables(const void* table, int32_t rows, int32_t max_pages, int32_t n_pages) {
+  if (table == nullptr || !aligned4(table)) return op_fail(THINFER_EINVAL, "the page table is NULL or not 4-byte aligned");
+  if (rows <= 0 || max_pages <= 0 || n_pages <= 0) return op_fail(THINFER_EINVAL, "rows, max_pages and n_pages must be positive");
+  return THINFER_OK;
+}
+
+int check_cache(const void* pool, const void* table, int32_t rows, int32_t max_pages, int32_t n_pages, int32_t n_kv,
+                int32_t head_dim, int32_t page_size) {
+  if (pool == nullptr || !aligned16(pool)) return op_fail(THINFER_EINVAL, "the pool is NULL or not 16-byte aligned");
+  int rc = check_layout(n_kv, head_dim, page_size);
+  if (rc == THINFER_OK) rc = check_tables(table, rows, max_pages, n_pages);
+  if (rc != THINFER_OK) return rc;
+  if ((static_cast<int64_t>(max_pages) << page_shift_of(page_size)) > 0x7fffffff)
+    return op_fail(THINFER_EUNSUPPORTED, "max_pages %d: a row holds fewer than 2^31 tokens", max_pages);
+  return THINFER_OK;
+}
+
+Kv4Cache make_cache(const void* pool, const int32_t* table, int32_t rows, int32_t max_pages, int32_t n_pages, int32_t n_kv,
+                    int32_t head_dim, int32_t page_size) {
+  Kv4Cache c{};
+  c.pool = static_cast<uint8_t*>(const_cast<void*>(pool));
+  c.table = table;
+  c.n_rows = rows;
+  c.max_pages = max_pages;
+  c.n_pages = n_pages;
+  c.page_shift = page_shift_of(page_size);
+  c.n_kv = n_kv;
+  c.block_bytes = page_size * (head_dim + 8);
+  c.page_bytes = static_cast<size_t>(n_kv) * c.block_bytes;
+  return c;
+}
+
+bool stride_ok(int64_t stride, int64_t least) { return stride >= least && stride % 8 == 0; }
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+
+// Opts a kernel in to more than 48 KB of dynamic shared memory on the current device.
+template <typename K>
+int opt_in(K kernel, size_t bytes) {
+  if (bytes <= 48 * 1024) return THINFER_OK;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)) != cudaSuccess)
+    return op_fail(THINFER_ECUDA, "cannot reserve %zu bytes of shared memory", bytes);
+  return THINFER_OK;
+}
+
+int check_plan(int32_t rows, int32_t n_pages) {
+  if (rows > kPlanMaxRows) return op_fail(THINFER_EUNSUPPORTED, "%d rows > %d", rows, kPlanMaxRows);
+  if (n_pages > kPlanMaxPages) return op_fail(THINFER_EUNSUPPORTED, "%d pages > %d", n_pages, kPlanMaxPages);
+  return THINFER_OK;
+}
+
+size_t moves_bytes(int32_t most) { return 16 + static_cast<size_t>(most) * sizeof(PageMove); }
+
+int copy_pages(void* pool, const int* count, const PageMove* moves, int most_moves, int layers, int n_kv, int d, int page,
+               int n_pages, cudaStream_t st) {
+  const size_t page_bytes = static_cast<size_t>(n_kv) * page * (d + 8);
+  const long long items = static_cast<long long>(most_moves) * layers * n_kv;
+  const long long ctas = (items + 7) / 8, room = static_cast<long long>(op_sm_count()) * 8;
+  return op_launch(kv4_copy_pages_kernel, dim3(static_cast<unsigned>(ctas < room ? ctas : room)), dim3(256), 0, st, true,
+                   static_cast<uint8_t*>(pool), count, moves, layers, n_kv, d, page, page_bytes,
+                   page_bytes * static_cast<size_t>(n_pages));
+}
+
+}  // namespace
+
+extern "C" {
+
+int thinfer_rope_turns(float base, int32_t rotary_dim, double* host_out) {
+  if (host_out == nullptr || !(base > 0.f) || rotary_dim <= 0 || rotary_dim % 2 != 0)
+    return op_fail(THINFER_EINVAL, "rope_turns: base must be positive, rotary_dim positive and even");
+  for (int j = 0; j < rotary_dim / 2; ++j)
+    host_out[j] = std::pow(static_cast<double>(base), -2.0 * j / rotary_dim) / 6.283185307179586476925286766559;
+  return THINFER_OK;
+}
+
+int thinfer_op_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out,
+                            int64_t q_out_stride, void* k_out, int64_t k_out_stride, const void* q_gain,
+                            const void* k_gain, const double* turns, const int32_t* positions, int32_t tokens,
+                            int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t rotary_dim, int32_t halves,
+                            float eps, void* cuda_stream) {
+  if (q == nullptr || k == nullptr || q_out == nullptr || k_out == nullptr || q_gain == nullptr || k_gain == nullptr ||
+      (turns == nullptr && rotary_dim > 0) || positions == nullptr)
+    return op_fail(THINFER_EINVAL, "qk_norm_rope: NULL pointer");
+  if (tokens <= 0 || n_q_heads <= 0 || n_kv_heads <= 0 || head_dim <= 0 || rotary_dim < 0 || !(eps >= 0.f))
+    return op_fail(THINFER_EINVAL, "qk_norm_rope: a size is not positive, or eps is negative");
+  if (head_dim != 64 && head_dim != 128) return op_fail(THINFER_EUNSUPPORTED, "head_dim %d: 64 and 128 are supported", head_dim);
+  if (rotary_dim > head_dim || rotary_dim % 16 != 0)
+    return op_fail(THINFER_EUNSUPPORTED, "rotary_dim %d: a multiple of 16 up to head_dim", rotary_dim);
+  if (halves != 0 && halves != 1) return op_fail(THINFER_EINVAL, "halves must be 0 or 1");
+  if (n_q_heads > 65536 || n_kv_heads > 65536) return op_fail(THINFER_EUNSUPPORTED, "more than 65536 heads");
+  const int64_t q_row = static_cast<int64_t>(n_q_heads) * head_dim, k_row = static_cast<int64_t>(n_kv_heads) * head_dim;
+  if (!stride_ok(q_stride, q_row) || !stride_ok(q_out_stride, q_row) || !stride_ok(k_stride, k_row) || !stride_ok(k_out_stride, k_row))
+    return op_fail(THINFER_EINVAL, "qk_norm_rope: a token stride is below heads * head_dim or no multiple of 8");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(q_gain) || !aligned16(k_gain) ||
+      !aligned4(positions) || (reinterpret_cast<uintptr_t>(turns) & 7u) != 0)
+    return op_fail(THINFER_EINVAL, "qk_norm_rope: a pointer is not aligned");
+  QkNormRopeArgs a{};
+  a.q = static_cast<const half_t*>(q);
+  a.k = static_cast<const half_t*>(k);
+  a.q_out = static_cast<half_t*>(q_out);
+  a.k_out = static_cast<half_t*>(k_out);
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.q_out_stride = q_out_stride;
+  a.k_out_stride = k_out_stride;
+  a.q_gain = static_cast<const half_t*>(q_gain);
+  a.k_gain = static_cast<const half_t*>(k_gain);
+  a.turns = turns;
+  a.positions = positions;
+  a.tokens = tokens;
+  a.n_q = n_q_heads;
+  a.n_kv = n_kv_heads;
+  a.half = rotary_dim / 2;
+  a.eps = eps;
+  a.chunks = n_q_heads + n_kv_heads;
+  const int64_t groups = static_cast<int64_t>(tokens) * a.chunks, per_cta = 256 / (head_dim / 8);
+  const int64_t ctas = (groups + per_cta - 1) / per_cta;
+  if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "qk_norm_rope: too many tokens");
+  auto kernel = head_dim == 128 ? (halves ? qk_norm_rope_kernel<128, true> : qk_norm_rope_kernel<128, false>)
+                                : (halves ? qk_norm_rope_kernel<64, true> : qk_norm_rope_kernel<64, false>);
+  return op_launch(kernel, dim3(static_cast<unsigned>(ctas)), dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), false, a);
+}
+
+int thinfer_kv4_page_bytes(int32_t n_kv_heads, int32_t head_dim, int32_t page_size, size_t* bytes) {
+  if (bytes == nullptr) return op_fail(THINFER_EINVAL, "bytes is NULL");
+  const int rc = check_layout(n_kv_heads, head_dim, page_size);
+  if (rc != THINFER_OK) return rc;
+  *bytes = static_cast<size_t>(n_kv_heads) * page_size * (head_dim + 8);
+  return THINFER_OK;
+}
+
+int thinfer_op_kv4_append(void* pool, int32_t n_pages, const int32_t* table, int32_t n_rows, int32_t max_pages,
+                          const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* rows,
+                          const int32_t* positions, int32_t tokens, int32_t n_kv_heads, int32_t head_dim,
+                          int32_t page_size, void* cuda_stream) {
+  const int rc = check_cache(pool, table, n_rows, max_pages, n_pages, n_kv_heads, head_dim, page_size);
+  if (rc != THINFER_OK) return rc;
+  if (k == nullptr || v == nullptr || rows == nullptr || positions == nullptr || tokens <= 0)
+    return op_fail(THINFER_EINVAL, "kv4_append: NULL pointer or no tokens");
+  const int64_t row = static_cast<int64_t>(n_kv_heads) * head_dim;
+  if (!stride_ok(k_stride, row) || !stride_ok(v_stride, row) || !aligned16(k) || !aligned16(v) || !aligned4(rows) || !aligned4(positions))
+    return op_fail(THINFER_EINVAL, "kv4_append: a pointer or a token stride is not aligned, or a stride is below heads * head_dim");
+  Kv4TokensArgs a{};
+  a.c = make_cache(pool, table, n_rows, max_pages, n_pages, n_kv_heads, head_dim, page_size);
+  a.rows = rows;
+  a.positions = positions;
+  a.tokens = tokens;
+  a.k = static_cast<const half_t*>(k);
+  a.v = static_cast<const half_t*>(v);
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  const int64_t per_cta = 256 / (head_dim / 8), ctas = (static_cast<int64_t>(tokens) * 2 * n_kv_heads + per_cta - 1) / per_cta;
+  if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "kv4_append: too many tokens");
+  return op_launch(head_dim == 128 ? kv4_append_kernel<128> : kv4_append_kernel<64>, dim3(static_cast<unsigned>(ctas)),
+                   dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), false, a);
+}
+
+int thinfer_op_kv4_read(const void* pool, int32_t n_pages, const int32_t* table, int32_t n_rows, int32_t max_pages,
+                        void* k_out, void* v_out, int64_t token_stride, int64_t head_stride, const int32_t* rows,
+                        const int32_t* positions, int32_t tokens, int32_t n_kv_heads, int32_t head_dim,
+                        int32_t page_size, void* cuda_stream) {
+  const int rc = check_cache(pool, table, n_rows, max_pages, n_pages, n_kv_heads, head_dim, page_size);
+  if (rc != THINFER_OK) return rc;
+  if (k_out == nullptr || v_out == nullptr || rows == nullptr || positions == nullptr || tokens <= 0)
+    return op_fail(THINFER_EINVAL, "kv4_read: NULL pointer or no tokens");
+  if (!stride_ok(token_stride, head_dim) || !stride_ok(head_stride, head_dim) || !aligned16(k_out) || !aligned16(v_out) ||
+      !aligned4(rows) || !aligned4(positions))
+    return op_fail(THINFER_EINVAL, "kv4_read: a pointer or a stride is not aligned, or a stride is below head_dim");
+  Kv4TokensArgs a{};
+  a.c = make_cache(pool, table, n_rows, max_pages, n_pages, n_kv_heads, head_dim, page_size);
+  a.rows = rows;
+  a.positions = positions;
+  a.tokens = tokens;
+  a.k_out = static_cast<half_t*>(k_out);
+  a.v_out = static_cast<half_t*>(v_out);
+  a.k_stride = a.v_stride = token_stride;
+  a.k_head = a.v_head = head_stride;
+  const int64_t per_cta = 256 / (head_dim / 8), ctas = (static_cast<int64_t>(tokens) * 2 * n_kv_heads + per_cta - 1) / per_cta;
+  if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "kv4_read: too many tokens");
+  return op_launch(head_dim == 128 ? kv4_read_kernel<128> : kv4_read_kernel<64>, dim3(static_cast<unsigned>(ctas)),
+                   dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), false, a);
+}
+
+int thinfer_kv4_attention_workspace(int32_t batch, int32_t queries, int32_t n_q_heads, int32_t n_kv_heads,
+                                    int32_t head_dim, size_t* bytes) {
+  if (bytes == nullptr || batch <= 0 || queries <= 0 || n_q_heads <= 0 || n_kv_heads <= 0)
+    return op_fail(THINFER_EINVAL, "kv4_attention: a size is not positive, or bytes is NULL");
+  (void)head_dim;
+  *bytes = 16;
+  return THINFER_OK;
+}
+
+int thinfer_op_kv4_attention(const void* q, int64_t q_stride, const void* pool, int32_t n_pages, const int32_t* table,
+                             int32_t max_pages, const int32_t* lens, void* out, int32_t batch, int32_t queries,
+                             int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t page_size, void* workspace,
+                             size_t workspace_bytes, void* cuda_stream) {
+  int rc = check_cache(pool, table, batch, max_pages, n_pages, n_kv_heads, head_dim, page_size);
+  if (rc != THINFER_OK) return rc;
+  if (q == nullptr || lens == nullptr || out == nullptr || workspace == nullptr || queries <= 0 || n_q_heads <= 0)
+    return op_fail(THINFER_EINVAL, "kv4_attention: NULL pointer, or a size that is not positive");
+  if (n_q_heads % n_kv_heads != 0) return op_fail(THINFER_EUNSUPPORTED, "n_q_heads must be a multiple of n_kv_heads");
+  if (!stride_ok(q_stride, static_cast<int64_t>(n_q_heads) * head_dim) || !aligned16(q) || !aligned16(out) || !aligned4(lens) || !aligned16(workspace))
+    return op_fail(THINFER_EINVAL, "kv4_attention: a pointer or the token stride is not aligned, or the stride is below heads * head_dim");
+  size_t need = 0;
+  rc = thinfer_kv4_attention_workspace(batch, queries, n_q_heads, n_kv_heads, head_dim, &need);
+  if (rc != THINFER_OK) return rc;
+  if (workspace_bytes < need) return op_fail(THINFER_ECAPACITY, "kv4_attention: the workspace has %zu bytes of %zu", workspace_bytes, need);
+  Kv4AttnArgs a{};
+  a.c = make_cache(pool, table, batch, max_pages, n_pages, n_kv_heads, head_dim, page_size);
+  a.lens = lens;
+  a.q = static_cast<const half_t*>(q);
+  a.out = static_cast<half_t*>(out);
+  a.q_stride = q_stride;
+  a.batch = batch;
+  a.queries = queries;
+  a.n_q = n_q_heads;
+  a.group = n_q_heads / n_kv_heads;
+  a.scale = 1.f / sqrtf(static_cast<float>(head_dim));
+  const int64_t tokens = static_cast<int64_t>(batch) * queries;
+  if (tokens > 0x7fffffff || n_q_heads > 65535) return op_fail(THINFER_EUNSUPPORTED, "kv4_attention: too many query tokens or heads");
+  return op_launch(head_dim == 128 ? kv4_attn_simple_kernel<128> : kv4_attn_simple_kernel<64>,
+                   dim3(static_cast<unsigned>(tokens), static_cast<unsigned>(n_q_heads)), dim3(kKv4SimpleThreads), 0,
+                   static_cast<cudaStream_t>(cuda_stream), false, a);
+}
+
+int thinfer_op_kv4_reserve(int32_t* table, const int32_t* lens, const int32_t* add, int32_t* lens_out, int32_t* refused,
+                           int32_t n_rows, int32_t max_pages, int32_t n_pages, int32_t page_size, void* cuda_stream) {
+  int rc = check_tables(table, n_rows, max_pages, n_pages);
+  if (rc == THINFER_OK) rc = check_layout(1, 64, page_size);
+  if (rc == THINFER_OK) rc = check_plan(n_rows, n_pages);
+  if (rc != THINFER_OK) return rc;
+  if (lens == nullptr || add == nullptr || lens_out == nullptr || refused == nullptr || !aligned4(lens) || !aligned4(add) ||
+      !aligned4(lens_out) || !aligned4(refused))
+    return op_fail(THINFER_EINVAL, "kv4_reserve: a pointer is NULL or not 4-byte aligned");
+  const size_t nb = static_cast<size_t>(n_rows) * 4;
+  if ((lens_out != lens && overlap(lens_out, nb, lens, nb)) || overlap(lens_out, nb, add, nb) || overlap(refused, 4, lens, nb) ||
+      overlap(refused, 4, add, nb) || overlap(refused, 4, lens_out, nb))
+    return op_fail(THINFER_EINVAL, "kv4_reserve: lens_out may be lens itself; other outputs must not overlap inputs");
+  if ((static_cast<int64_t>(max_pages) * page_size) > 0x7fffffff)
+    return op_fail(THINFER_EUNSUPPORTED, "max_pages %d: a row holds fewer than 2^31 tokens", max_pages);
+  const PageTables t{table, lens, n_rows, max_pages, n_pages, page_shift_of(page_size)};
+  const size_t smem = static_cast<size_t>(plan_words(n_pages)) * 8;
+  rc = opt_in(kv4_reserve_kernel, smem);
+  if (rc != THINFER_OK) return rc;
+  return op_launch(kv4_reserve_kernel, dim3(1), dim3(kPlanThreads), smem, static_cast<cudaStream_t>(cuda_stream), false, t,
+                   table, add, lens_out, refused);
+}
+
+int thinfer_kv4_pages_workspace(int32_t n_rows, int32_t n_pages, size_t* bytes) {
+  if (bytes == nullptr || n_rows <= 0 || n_pages <= 0) return op_fail(THINFER_EINVAL, "kv4_pages_workspace: a size is not positive, or bytes is NULL");
+  const int rc = check_plan(n_rows, n_pages);
+  if (rc != THINFER_OK) return rc;
+  *bytes = moves_bytes(n_rows > n_pages / 2 ? n_rows : n_pages / 2);  // a compaction moves at most half of the pages
+  return THINFER_OK;
+}
+
+int thinfer_op_kv4_fork(void* pool, int32_t n_layers, int32_t n_pages, const int32_t* table, const int32_t* lens,
+                        const int32_t* source, int32_t* table_out, int32_t* lens_out, int32_t* refused, int32_t n_rows,
+                        int32_t max_pages, int32_t n_kv_heads, int32_t head_dim, int32_t page_size, void* workspace,
+                        size_t workspace_bytes, void* cuda_stream) {
+  int rc = check_cache(pool, table, n_rows, max_pages, n_pages, n_kv_heads, head_dim, page_size);
+  if (rc == THINFER_OK) rc = check_plan(n_rows, n_pages);
+  if (rc != THINFER_OK) return rc;
+  if (n_layers <= 0 || lens == nullptr || source == nullptr || table_out == nullptr || lens_out == nullptr || refused == nullptr ||
+      workspace == nullptr || !aligned4(lens) || !aligned4(source) || !aligned4(table_out) || !aligned4(lens_out) ||
+      !aligned4(refused) || !aligned16(workspace))
+    return op_fail(THINFER_EINVAL, "kv4_fork: a pointer is NULL or not aligned, or n_layers is not positive");
+  const size_t nb = static_cast<size_t>(n_rows) * 4, tb = nb * max_pages;
+  const void* ins[3] = {table, lens, source};
+  const size_t in_b[3] = {tb, nb, nb};
+  void* outs[3] = {table_out, lens_out, refused};
+  const size_t out_b[3] = {tb, nb, 4};
+  for (int o = 0; o < 3; ++o) {
+    for (int i = 0; i < 3; ++i)
+      if (overlap(outs[o], out_b[o], ins[i], in_b[i])) return op_fail(THINFER_EINVAL, "kv4_fork: an output overlaps an input");
+    for (int p = 0; p < o; ++p)
+      if (overlap(outs[o], out_b[o], outs[p], out_b[p])) return op_fail(THINFER_EINVAL, "kv4_fork: two outputs overlap");
+  }
+  if (workspace_bytes < moves_bytes(n_rows)) return op_fail(THINFER_ECAPACITY, "kv4_fork: the workspace is too small");
+  const PageTables t{table, lens, n_rows, max_pages, n_pages, page_shift_of(page_size)};
+  const size_t smem = static_cast<size_t>(plan_words(n_pages)) * 8 + nb * 2;
+  rc = opt_in(kv4_fork_kernel, smem);
+  if (rc != THINFER_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  int* count = static_cast<int*>(workspace);
+  PageMove* moves = reinterpret_cast<PageMove*>(static_cast<char*>(workspace) + 16);
+  rc = op_launch(kv4_fork_kernel, dim3(1), dim3(kPlanThreads), smem, st, false, t, source, table_out, lens_out, refused, count, moves);
+  if (rc != THINFER_OK) return rc;
+  return copy_pages(pool, count, moves, n_rows, n_layers, n_kv_heads, head_dim, page_size, n_pages, st);
+}
+
+int thinfer_op_kv4_compact(void* pool, int32_t n_layers, int32_t n_pages, const int32_t* table, const int32_t* lens,
+                           int32_t* table_out, int32_t* live_pages, int32_t n_rows, int32_t max_pages,
+                           int32_t n_kv_heads, int32_t head_dim, int32_t page_size, void* workspace,
+                           size_t workspace_bytes, void* cuda_stream) {
+  int rc = check_cache(pool, table, n_rows, max_pages, n_pages, n_kv_heads, head_dim, page_size);
+  if (rc == THINFER_OK) rc = check_plan(n_rows, n_pages);
+  if (rc != THINFER_OK) return rc;
+  if (n_layers <= 0 || lens == nullptr || table_out == nullptr || live_pages == nullptr || workspace == nullptr || !aligned4(lens) ||
+      !aligned4(table_out) || !aligned4(live_pages) || !aligned16(workspace))
+    return op_fail(THINFER_EINVAL, "kv4_compact: a pointer is NULL or not aligned, or n_layers is not positive");
+  const size_t nb = static_cast<size_t>(n_rows) * 4, tb = nb * max_pages;
+  if (overlap(table_out, tb, table, tb) || overlap(table_out, tb, lens, nb) || overlap(live_pages, 4, table, tb) ||
+      overlap(live_pages, 4, lens, nb) || overlap(live_pages, 4, table_out, tb))
+    return op_fail(THINFER_EINVAL, "kv4_compact: an output overlaps another tensor");
+  const int most = n_pages / 2 > 0 ? n_pages / 2 : 1;
+  if (workspace_bytes < moves_bytes(n_pages / 2)) return op_fail(THINFER_ECAPACITY, "kv4_compact: the workspace is too small");
+  const PageTables t{table, lens, n_rows, max_pages, n_pages, page_shift_of(page_size)};
+  const size_t smem = static_cast<size_t>(plan_words(n_pages)) * 8;
+  rc = opt_in(kv4_compact_kernel, smem);
+  if (rc != THINFER_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  int* count = static_cast<int*>(workspace);
+  PageMove* moves = reinterpret_cast<PageMove*>(static_cast<char*>(workspace) + 16);
+  rc = op_launch(kv4_compact_kernel, dim3(1), dim3(kPlanThreads), smem, st, false, t, table_out, live_pages, count, moves);
+  if (rc != THINFER_OK) return rc;
+  return copy_pages(pool, count, moves, most, n_layers, n_kv_heads, head_dim, page_size, n_pages, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,340 @@
+// Page tables of the 4-bit cache on the device: reserving pages for new tokens, forking rows, compacting the pool.
+//
+// A page is in use when a row's table names it among its first ceil(len / P) entries; nothing else records ownership,
+// so no reference counts can go wrong and no host state has to follow the device.  One CTA marks the pages in use in
+// a shared-memory bitmap (one bit per page of the pool), takes prefix counts of it, and answers "the k-th free page"
+// by a binary search: all choices go to the lowest page number first and depend on nothing but the tables.
+// The pages that have to move are written to a list that a second kernel, chained to the first, copies with all SMs.
+#pragma once
+#include "kv4_layout.cuh"
+
+namespace thinfer {
+
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanMaxPages = 1 << 18;
+constexpr int kPlanMaxRows = 4096;
+
+struct PageMove {
+  int src, dst, tokens;  // tokens: the filled ones, rounded up to 16 by the copy
+};
+
+struct PageTables {
+  const int32_t* table;
+  const int32_t* lens;
+  int rows, max_pages, n_pages, page_shift;
+};
+
+__device__ __forceinline__ int tables_len(const PageTables& t, int r) {  // tokens of a row, within what its table can name
+  const int n = t.lens[r];
+  const long long cap = static_cast<long long>(t.max_pages) << t.page_shift;
+  return n < 0 ? 0 : (n > cap ? static_cast<int>(cap) : n);
+}
+__device__ __forceinline__ int pages_for(int tokens, int shift) {
+  return static_cast<int>((static_cast<long long>(tokens) + (1 << shift) - 1) >> shift);
+}
+
+// Calls f(row, column, page) for every page in use, entries outside the pool left out.
+constexpr int kPlanSpan = 256;  // table columns of one warp task
+template <typename F>
+__device__ __forceinline__ void for_pages_in_use(const PageTables& t, F f) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const int spans = (t.max_pages + kPlanSpan - 1) / kPlanSpan;
+  const long long tasks = static_cast<long long>(t.rows) * spans;
+  for (long long k = warp; k < tasks; k += warps) {
+    const int r = static_cast<int>(k / spans), c0 = static_cast<int>(k - static_cast<long long>(r) * spans) * kPlanSpan;
+    const int n = pages_for(tables_len(t, r), t.page_shift);
+    const int c1 = min(n, c0 + kPlanSpan);
+    const int32_t* row = t.table + static_cast<size_t>(r) * t.max_pages;
+    for (int c = c0 + lane; c < c1; c += 32) {
+      const int p = row[c];
+      if (p >= 0 && p < t.n_pages) f(r, c, p);
+    }
+  }
+}
+
+// Exclusive sum over the CTA of one value per thread; total for everybody.  buf: 33 ints of shared memory.
+__device__ __forceinline__ int block_exclusive(int v, int* buf, int* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  int s = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += u;
+  }
+  __syncthreads();
+  if (lane == 31) buf[warp] = s;
+  __syncthreads();
+  if (warp == 0) {
+    int w = lane < warps ? buf[lane] : 0, ws = w;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, ws, o);
+      if (lane >= o) ws += u;
+    }
+    buf[lane] = ws - w;
+    if (lane == 31) buf[32] = ws;
+  }
+  __syncthreads();
+  *total = buf[32];
+  return buf[warp] + s - v;
+}
+
+// Bitmap of the pages in use and, per 32-page word, the number of pages in use in the words before it.
+struct PageMap {
+  uint32_t* bits;
+  int* before;
+  int words, live;
+  __device__ int live_below(int p) const {
+    const int w = p >> 5;
+    if (w >= words) return live;
+    return before[w] + __popc(bits[w] & ((1u << (p & 31)) - 1u));
+  }
+  __device__ bool used(int p) const { return (bits[p >> 5] >> (p & 31)) & 1u; }
+  // the k-th free page (from 0), k < n_pages - live: the bits behind the last page count as free and come last
+  __device__ int free_page(int k) const {
+    int lo = 0, hi = words - 1;
+    while (lo < hi) {  // the last word with at most k free pages before it
+      const int mid = (lo + hi + 1) >> 1;
+      if (32 * mid - before[mid] <= k) lo = mid;
+      else hi = mid - 1;
+    }
+    uint32_t z = ~bits[lo];
+    for (int i = k - (32 * lo - before[lo]); i > 0; --i) z &= z - 1;
+    return 32 * lo + __ffs(z) - 1;
+  }
+};
+
+__host__ __device__ constexpr int plan_words(int n_pages) { return (n_pages + 31) / 32; }
+
+// Whole CTA.  mem: 2 * plan_words ints of shared memory.
+__device__ __forceinline__ PageMap map_pages(const PageTables& t, int* mem, int* buf) {
+  PageMap m;
+  m.words = plan_words(t.n_pages);
+  m.bits = reinterpret_cast<uint32_t*>(mem);
+  m.before = mem + m.words;
+  for (int w = threadIdx.x; w < m.words; w += blockDim.x) m.bits[w] = 0;
+  __syncthreads();
+  for_pages_in_use(t, [&](int, int, int p) { atomicOr(&m.bits[p >> 5], 1u << (p & 31)); });
+  __syncthreads();
+  const int per = (m.words + blockDim.x - 1) / blockDim.x;
+  const int w0 = min(m.words, static_cast<int>(threadIdx.x) * per), w1 = min(m.words, w0 + per);
+  int mine = 0;
+  for (int w = w0; w < w1; ++w) mine += __popc(m.bits[w]);
+  int run = block_exclusive(mine, buf, &m.live);
+  for (int w = w0; w < w1; ++w) {
+    m.before[w] = run;
+    run += __popc(m.bits[w]);
+  }
+  __syncthreads();
+  return m;
+}
+
+// ---------------------------------------------------------------- reserve
+// Rows in ascending order take the lowest free pages for `add` more tokens each; a row whose pages, with those of the
+// rows before it, do not fit the pool or its table keeps its length and is counted in *refused.
+__global__ void __launch_bounds__(kPlanThreads) kv4_reserve_kernel(const PageTables t, int32_t* table, const int32_t* add,
+                                                                   int32_t* lens_out, int32_t* refused) {
+  extern __shared__ int plan_mem[];
+  __shared__ int buf[33];
+  __shared__ int wanted, bad;
+  if (threadIdx.x == 0) wanted = bad = 0;
+  __syncthreads();
+  auto need_of = [&](int r, int* first, long long* after) {
+    const int n = tables_len(t, r), a = max(add[r], 0);
+    *first = pages_for(n, t.page_shift);
+    *after = static_cast<long long>(n) + a;
+    return static_cast<int>(((*after + (1 << t.page_shift) - 1) >> t.page_shift) - *first);
+  };
+  int first;
+  long long after;
+  for (int r = threadIdx.x; r < t.rows; r += blockDim.x)
+    if (need_of(r, &first, &after) > 0) wanted = 1;
+  __syncthreads();
+  PageMap m{};
+  if (wanted) m = map_pages(t, plan_mem, buf);  // most decode steps stay inside their pages and need no map
+  const int free_pages = t.n_pages - m.live;
+  long long carry = 0;
+  for (int r0 = 0; r0 < t.rows; r0 += blockDim.x) {
+    const int r = r0 + threadIdx.x;
+    int need = 0;
+    if (r < t.rows) need = need_of(r, &first, &after);
+    // a need beyond the pool refuses its row and those behind it whatever its size: clamped so that the sum stays small
+    const int asked = min(need, t.n_pages + 1);
+    int total;
+    const long long begin = carry + block_exclusive(asked, buf, &total);
+    carry += total;
+    if (r < t.rows) {
+      // a row that claims more tokens than its table can name is refused as well
+      const bool fits = t.lens[r] <= (static_cast<long long>(t.max_pages) << t.page_shift) &&
+                        (need == 0 || (begin + need <= free_pages && first + need <= t.max_pages));
+      if (fits) {
+        for (int j = 0; j < need; ++j)
+          table[static_cast<size_t>(r) * t.max_pages + first + j] = m.free_page(static_cast<int>(begin) + j);
+      } else {
+        atomicAdd(&bad, 1);
+      }
+      lens_out[r] = fits ? static_cast<int>(after) : t.lens[r];
+    }
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *refused = bad;
+}
+
+// ---------------------------------------------------------------- fork
+__global__ void __launch_bounds__(kPlanThreads) kv4_fork_kernel(const PageTables t, const int32_t* source, int32_t* table_out,
+                                                                int32_t* lens_out, int32_t* refused, int* move_count,
+                                                                PageMove* moves) {
+  extern __shared__ int plan_mem[];
+  __shared__ int buf[33];
+  __shared__ int bad;
+  pdl_launch_dependents();
+  int* owner = plan_mem;            // [rows] who keeps the partly filled last page of a source
+  int* fresh = plan_mem + t.rows;   // [rows] page of a row's own copy, or -1
+  for (int r = threadIdx.x; r < t.rows; r += blockDim.x) owner[r] = 0x7fffffff;
+  if (threadIdx.x == 0) bad = 0;
+  const PageMap m = map_pages(t, plan_mem + 2 * t.rows, buf);
+  for (int r = threadIdx.x; r < t.rows; r += blockDim.x) {
+    const int s = source[r];
+    if (s >= 0 && s < t.rows) atomicMin(&owner[s], s == r ? -1 : r);
+  }
+  __syncthreads();
+  const int free_pages = t.n_pages - m.live, page = 1 << t.page_shift;
+  int carry = 0;
+  for (int r0 = 0; r0 < t.rows; r0 += blockDim.x) {
+    const int r = r0 + threadIdx.x;
+    int s = -1, n = 0, old = -1;
+    bool ok = true;
+    if (r < t.rows) {
+      s = source[r];
+      if (s >= t.rows) {
+        ok = false;
+        s = -1;
+      }
+      if (s >= 0) n = tables_len(t, s);
+      if ((n & (page - 1)) != 0 && owner[s] != r && !(owner[s] == -1 && s == r)) {
+        old = t.table[static_cast<size_t>(s) * t.max_pages + (n >> t.page_shift)];
+        if (old >= t.n_pages) old = -1;  // no page of the pool: the entry is taken over as it is
+      }
+    }
+    int total;
+    const int k = carry + block_exclusive(old >= 0 ? 1 : 0, buf, &total);
+    if (r < t.rows) {
+      fresh[r] = -1;
+      if (old >= 0) {
+        if (k < free_pages) {
+          fresh[r] = m.free_page(k);
+          moves[k] = PageMove{old, fresh[r], n & (page - 1)};
+        } else {
+          ok = false;
+        }
+      }
+      if (!ok) {
+        n = 0;
+        atomicAdd(&bad, 1);
+      }
+      lens_out[r] = n;
+    }
+    carry += total;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) {
+    *refused = bad;
+    *move_count = min(carry, free_pages);
+  }
+  // the new tables: warps take spans of one row
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const int spans = (t.max_pages + kPlanSpan - 1) / kPlanSpan;
+  const long long tasks = static_cast<long long>(t.rows) * spans;
+  for (long long task = warp; task < tasks; task += warps) {
+    const int r = static_cast<int>(task / spans), c0 = static_cast<int>(task - static_cast<long long>(r) * spans) * kPlanSpan;
+    const int n = lens_out[r], pages = pages_for(n, t.page_shift), s = source[r];
+    const int own_page = fresh[r];
+    const int c1 = min(t.max_pages, c0 + kPlanSpan);
+    for (int c = c0 + lane; c < c1; c += 32) {
+      int p = -1;
+      if (c < pages) p = own_page >= 0 && c == pages - 1 ? own_page : t.table[static_cast<size_t>(s) * t.max_pages + c];
+      table_out[static_cast<size_t>(r) * t.max_pages + c] = p;
+    }
+  }
+}
+
+// ---------------------------------------------------------------- compact
+// Live pages with a number >= the number of live pages move, in ascending order, into the free pages below it.
+__global__ void __launch_bounds__(kPlanThreads) kv4_compact_kernel(const PageTables t, int32_t* table_out, int32_t* live_out,
+                                                                   int* move_count, PageMove* moves) {
+  extern __shared__ int plan_mem[];
+  __shared__ int buf[33];
+  pdl_launch_dependents();
+  const PageMap m = map_pages(t, plan_mem, buf);
+  const int stay = m.live_below(m.live), n_moves = m.live - stay;
+  // moves in the order of their sources
+  for (int w = (m.live >> 5) + threadIdx.x; w < m.words; w += blockDim.x) {
+    uint32_t z = m.bits[w];
+    if (w == (m.live >> 5)) z &= ~((1u << (m.live & 31)) - 1u);
+    for (; z != 0; z &= z - 1) {
+      const int p = 32 * w + __ffs(z) - 1, k = m.live_below(p) - stay;
+      moves[k] = PageMove{p, m.free_page(k), 0};
+    }
+  }
+  if (threadIdx.x == 0) {
+    *live_out = m.live;
+    *move_count = n_moves;
+  }
+  __syncthreads();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const int spans = (t.max_pages + kPlanSpan - 1) / kPlanSpan;
+  const long long tasks = static_cast<long long>(t.rows) * spans;
+  for (long long task = warp; task < tasks; task += warps) {
+    const int r = static_cast<int>(task / spans), c0 = static_cast<int>(task - static_cast<long long>(r) * spans) * kPlanSpan;
+    const int n = tables_len(t, r), pages = pages_for(n, t.page_shift);
+    const int c1 = min(t.max_pages, c0 + kPlanSpan);
+    const size_t row = static_cast<size_t>(r) * t.max_pages;
+    for (int c = c0 + lane; c < c1; c += 32) {
+      int p = -1;
+      if (c < pages) {
+        p = t.table[row + c];
+        if (p >= m.live && p < t.n_pages) {
+          const int k = m.live_below(p) - stay;
+          atomicMax(&moves[k].tokens, min(1 << t.page_shift, n - (c << t.page_shift)));
+          p = moves[k].dst;
+        }
+      }
+      table_out[row + c] = p;
+    }
+  }
+}
+
+// ---------------------------------------------------------------- the copies
+// A warp takes one (move, layer, head) block at a time and copies the filled tokens, 16 at a time, of its four parts.
+__global__ void __launch_bounds__(256) kv4_copy_pages_kernel(uint8_t* pool, const int* move_count, const PageMove* moves,
+                                                             int layers, int n_kv, int d, int page, size_t page_bytes,
+                                                             size_t layer_bytes) {
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  const long long warps = static_cast<long long>(gridDim.x) * (blockDim.x >> 5);
+  const long long first = static_cast<long long>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  const int per_move = layers * n_kv;
+  const long long items = static_cast<long long>(*move_count) * per_move;
+  const int block = page * (d + 8);
+  for (long long i = first; i < items; i += warps) {
+    const int k = static_cast<int>(i / per_move), rest = static_cast<int>(i - static_cast<long long>(k) * per_move);
+    const int layer = rest / n_kv, head = rest - layer * n_kv;
+    const PageMove mv = moves[k];
+    const int filled = min(page, (mv.tokens + 15) & ~15);
+    const size_t base = static_cast<size_t>(layer) * layer_bytes + static_cast<size_t>(head) * block;
+    const uint4* src = reinterpret_cast<const uint4*>(pool + base + static_cast<size_t>(mv.src) * page_bytes);
+    uint4* dst = reinterpret_cast<uint4*>(pool + base + static_cast<size_t>(mv.dst) * page_bytes);
+    const int codes = filled * d / 32, params = filled / 4;  // 16-byte pieces of one of the two code and param parts
+    const int pieces = 2 * (codes + params);
+    for (int u = lane; u < pieces; u += 32) {
+      int at;
+      if (u < codes) at = u;
+      else if (u < 2 * codes) at = page * d / 32 + (u - codes);
+      else if (u < 2 * codes + params) at = page * d / 16 + (u - 2 * codes);
+      else at = page * (d + 4) / 16 + (u - 2 * codes - params);
+      dst[at] = src[at];
+    }
+  }
+}
+
+}  // namespace thinfer

@@ -1,0 +1,54 @@
+// Host helpers of the context-free operators that live outside thinfer_api.cu: error text, launch, device queries.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <cstdarg>
+#include <cstdio>
+
+#include "../../include/thinfer.h"
+
+namespace thinfer {
+
+// Text that thinfer_last_error(NULL) returns (thread-local; defined in thinfer_api.cu).
+void op_set_error(const char* text) noexcept;
+
+inline int op_fail(int code, const char* fmt, ...) {
+  char buf[256];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof(buf), fmt, ap);
+  va_end(ap);
+  op_set_error(buf);
+  return code;
+}
+
+// SM count of the current device (asked once per device).
+int op_sm_count();
+
+// One launch.  chained: the kernel may start while its predecessor in the stream is still running and waits for it
+// on the device (programmatic dependent launch).
+template <typename... KArgs, typename... Args>
+int op_launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, bool chained, Args&&... args) {
+  cudaLaunchConfig_t lc{};
+  lc.gridDim = grid;
+  lc.blockDim = block;
+  lc.dynamicSmemBytes = smem;
+  lc.stream = st;
+  cudaLaunchAttribute attr[1];
+  lc.attrs = attr;
+  lc.numAttrs = 0;
+  if (chained) {
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.numAttrs = 1;
+  }
+  const cudaError_t e = cudaLaunchKernelEx(&lc, kernel, static_cast<KArgs>(args)...);
+  if (e != cudaSuccess) return op_fail(THINFER_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+  return THINFER_OK;
+}
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+}  // namespace thinfer

@@ -19,6 +19,7 @@
 #include "decode_mega.cuh"
 #include "decode_mma.cuh"
 #include "misc_kernels.cuh"
+#include "op_host.cuh"
 #include "prefill_attn.cuh"
 #include "tc_gemm.cuh"
 
@@ -1863,3 +1864,16 @@ int thinfer_op_rmsnorm(const void* x, const void* gain, void* y, int32_t rows, i
 }
 
 }  // extern "C"
+
+// ---------------------------------------------------------------------------
+// What the context-free operators of the other source files share with this one.
+// ---------------------------------------------------------------------------
+namespace thinfer {
+void op_set_error(const char* text) noexcept {
+  try {
+    g_global_err = text;
+  } catch (...) {  // no memory for the text: the code alone has to do
+  }
+}
+int op_sm_count() { return current_sm_count(); }
+}  // namespace thinfer

@@ -28,6 +28,9 @@ EXPORTS = (
     "thinfer_profile_read", "thinfer_trace_unified", "thinfer_launch_count", "thinfer_last_error", "thinfer_destroy",
     "thinfer_op_linear", "thinfer_op_linear_noalloc", "thinfer_op_attention_prefill", "thinfer_op_rmsnorm",
     "thinfer_op_argmax", "thinfer_op_attention_decode", "thinfer_selftest_bounded_wait",
+    "thinfer_rope_turns", "thinfer_op_qk_norm_rope", "thinfer_kv4_page_bytes", "thinfer_op_kv4_reserve",
+    "thinfer_op_kv4_append", "thinfer_op_kv4_read", "thinfer_kv4_attention_workspace", "thinfer_op_kv4_attention",
+    "thinfer_kv4_pages_workspace", "thinfer_op_kv4_fork", "thinfer_op_kv4_compact",
 )
 
 
@@ -110,6 +113,19 @@ def lib(storage="f16"):
     L.thinfer_op_argmax.argtypes = [vp, vp, i32, i32, vp]
     L.thinfer_op_attention_decode.argtypes = [vp, i32, i32, vp, vp, i32, i32, C.POINTER(i32), vp]
     L.thinfer_selftest_bounded_wait.argtypes = [vp, i64, vp]
+    szp = C.POINTER(C.c_size_t)
+    L.thinfer_rope_turns.argtypes = [C.c_float, i32, C.POINTER(C.c_double)]
+    L.thinfer_op_qk_norm_rope.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32,
+                                          C.c_float, vp]
+    L.thinfer_kv4_page_bytes.argtypes = [i32, i32, i32, szp]
+    L.thinfer_op_kv4_reserve.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp]
+    L.thinfer_op_kv4_append.argtypes = [vp, i32, vp, i32, i32, vp, i64, vp, i64, vp, vp, i32, i32, i32, i32, vp]
+    L.thinfer_op_kv4_read.argtypes = [vp, i32, vp, i32, i32, vp, vp, i64, i64, vp, vp, i32, i32, i32, i32, vp]
+    L.thinfer_kv4_attention_workspace.argtypes = [i32, i32, i32, i32, i32, szp]
+    L.thinfer_op_kv4_attention.argtypes = [vp, i64, vp, i32, vp, i32, vp, vp, i32, i32, i32, i32, i32, i32, vp, C.c_size_t, vp]
+    L.thinfer_kv4_pages_workspace.argtypes = [i32, i32, szp]
+    L.thinfer_op_kv4_fork.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, C.c_size_t, vp]
+    L.thinfer_op_kv4_compact.argtypes = [vp, i32, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, C.c_size_t, vp]
     _libs[storage] = L
     return L
 
@@ -378,6 +394,232 @@ def op_argmax(logits, stream=None):
     ids = torch.empty(rows, dtype=torch.int32, device=logits.device)
     _check(lib().thinfer_op_argmax(logits.data_ptr(), ids.data_ptr(), rows, n, _stream_ptr(stream)))
     return ids
+
+
+# ------------------------------------- per-head norm + rotation, 4-bit paged cache
+class _On:
+    """Checks that tensors live on one CUDA device and makes it the current one for the call; hands out its stream."""
+
+    def __init__(self, device, stream=None):
+        import torch
+        if device.type != "cuda":
+            raise ThinferError(EINVAL, f"tensors must be on a CUDA device, not {device}")
+        self.device, self.torch = device, torch
+        if stream is not None and stream.device != device:
+            raise ThinferError(EINVAL, f"the stream belongs to {stream.device}, the tensors to {device}")
+        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+        self.stream = stream
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        s = self.stream if self.stream is not None else self.torch.cuda.current_stream(self.device)
+        return s.cuda_stream
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _want(ok, what):
+    if not ok:
+        raise ThinferError(EINVAL, what)
+
+
+def _want_int32(device, **tensors):
+    import torch
+    for name, (t, shape) in tensors.items():
+        _want(t.dtype == torch.int32 and t.device == device and t.is_contiguous() and tuple(t.shape) == tuple(shape),
+              f"{name}: a contiguous int32 tensor of shape {tuple(shape)} on {device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _token_stride(t, name, dtype, device):
+    """Elements between the tokens of [tokens, heads, head_dim], whose heads lie side by side."""
+    _want(t.dim() == 3 and t.dtype == dtype and t.device == device, f"{name}: [tokens, heads, head_dim] {dtype} on {device}")
+    n, h, d = t.shape
+    _want(n > 0 and h > 0 and t.stride(2) == 1 and (h == 1 or t.stride(1) == d), f"{name}: the heads of a token must be contiguous")
+    return t.stride(0) if n > 1 else -(-max(t.stride(0), h * d) // 8) * 8
+
+
+def rope_turns(base, rotary_dim, device="cuda:0"):
+    """FP64 [rotary_dim / 2]: revolutions per position of each rotated pair, base^(-2j/rotary_dim) / (2 pi)."""
+    import torch
+    buf = (C.c_double * (rotary_dim // 2))()
+    _check(lib().thinfer_rope_turns(base, rotary_dim, buf))
+    return torch.tensor(list(buf), dtype=torch.float64, device=device)
+
+
+def op_qk_norm_rope(q, k, q_gain, k_gain, eps, turns, positions, halves=False, q_out=None, k_out=None, stream=None):
+    """Per-head RMSNorm and rotation of q [tokens, n_q_heads, d] and k [tokens, n_kv_heads, d] (token strides as they
+    come, e.g. slices of a fused projection output); turns from rope_turns (its length sets the rotated dimensions);
+    positions int32 [tokens], negative: left as they were.  Returns (q_out, k_out); they may be q and k themselves."""
+    import torch
+    dev = q.device
+    with _On(dev, stream) as st:
+        n, hq, d = q.shape if q.dim() == 3 else (0, 0, 0)
+        qs, ks = _token_stride(q, "q", q.dtype, dev), _token_stride(k, "k", q.dtype, dev)
+        hkv = k.shape[1]
+        _want(k.shape[0] == n and k.shape[2] == d, "q and k must agree in tokens and head_dim")
+        for name, g in (("q_gain", q_gain), ("k_gain", k_gain)):
+            _want(g.dtype == q.dtype and g.device == dev and g.is_contiguous() and tuple(g.shape) == (d,), f"{name}: [head_dim] {q.dtype} on {dev}")
+        _want(turns.dtype == torch.float64 and turns.device == dev and turns.is_contiguous() and turns.dim() == 1, "turns: FP64 [rotary_dim / 2]")
+        _want_int32(dev, positions=(positions, (n,)))
+        q_out = torch.empty(n, hq, d, dtype=q.dtype, device=dev) if q_out is None else q_out
+        k_out = torch.empty(n, hkv, d, dtype=q.dtype, device=dev) if k_out is None else k_out
+        _want(tuple(q_out.shape) == (n, hq, d) and tuple(k_out.shape) == (n, hkv, d), "q_out / k_out: the shapes of q / k")
+        qos, kos = _token_stride(q_out, "q_out", q.dtype, dev), _token_stride(k_out, "k_out", q.dtype, dev)
+        s = storage_of(q)
+        _check(lib(s).thinfer_op_qk_norm_rope(q.data_ptr(), qs, k.data_ptr(), ks, q_out.data_ptr(), qos, k_out.data_ptr(), kos,
+                                              q_gain.data_ptr(), k_gain.data_ptr(), turns.data_ptr(), positions.data_ptr(), n, hq,
+                                              hkv, d, 2 * turns.shape[0], int(halves), eps, st), None, s)
+    return q_out, k_out
+
+
+def kv4_page_bytes(n_kv_heads, head_dim, page_size):
+    """Bytes of one page of one layer of the 4-bit cache; a pool is a uint8 tensor [n_layers, n_pages, page bytes]."""
+    n = C.c_size_t(0)
+    _check(lib().thinfer_kv4_page_bytes(n_kv_heads, head_dim, page_size, C.byref(n)))
+    return n.value
+
+
+def _pool(pool, dims, page_size, head_dim):
+    """Number of KV heads of a uint8 pool tensor whose last dimension is a page."""
+    import torch
+    _want(pool.dtype == torch.uint8 and pool.dim() == dims and pool.is_contiguous(), f"pool: a contiguous uint8 tensor of {dims} dimensions")
+    per = kv4_page_bytes(1, head_dim, page_size)
+    _want(pool.shape[-1] > 0 and pool.shape[-1] % per == 0, f"pool: a page has a multiple of {per} bytes, not {pool.shape[-1]}")
+    return pool.shape[-1] // per
+
+
+def op_kv4_reserve(table, lens, add, n_pages, page_size, lens_out=None, refused=None, stream=None):
+    """Room for add[r] more tokens of every row: writes page numbers into table (int32 [rows, max_pages]); returns
+    (lens_out, refused): the new lengths and how many rows did not fit (they keep their length)."""
+    import torch
+    dev = table.device
+    with _On(dev, stream) as st:
+        rows, max_pages = table.shape
+        lens_out = torch.empty_like(lens) if lens_out is None else lens_out
+        refused = torch.empty(1, dtype=torch.int32, device=dev) if refused is None else refused
+        _want_int32(dev, table=(table, (rows, max_pages)), lens=(lens, (rows,)), add=(add, (rows,)), lens_out=(lens_out, (rows,)),
+                    refused=(refused, (1,)))
+        _check(lib().thinfer_op_kv4_reserve(table.data_ptr(), lens.data_ptr(), add.data_ptr(), lens_out.data_ptr(), refused.data_ptr(),
+                                            rows, max_pages, n_pages, page_size, st))
+    return lens_out, refused
+
+
+def op_kv4_append(pool, table, k, v, rows, positions, page_size, stream=None):
+    """Quantises k, v [tokens, n_kv_heads, d] into one layer's pool [n_pages, page bytes]: token i goes to position
+    positions[i] of table row rows[i] (int32 [tokens]; negative: skipped)."""
+    dev = pool.device
+    with _On(dev, stream) as st:
+        ks, vs = _token_stride(k, "k", k.dtype, dev), _token_stride(v, "v", k.dtype, dev)
+        n, hkv, d = k.shape
+        _want(tuple(v.shape) == (n, hkv, d), "k and v must have one shape")
+        _want(_pool(pool, 2, page_size, d) == hkv, "the pool's pages are for another number of heads")
+        _want_int32(dev, table=(table, table.shape), rows=(rows, (n,)), positions=(positions, (n,)))
+        _want(table.dim() == 2, "table: [rows, max_pages]")
+        s = storage_of(k)
+        _check(lib(s).thinfer_op_kv4_append(pool.data_ptr(), pool.shape[0], table.data_ptr(), table.shape[0], table.shape[1],
+                                            k.data_ptr(), ks, v.data_ptr(), vs, rows.data_ptr(), positions.data_ptr(), n, hkv, d,
+                                            page_size, st), None, s)
+
+
+def op_kv4_read(pool, table, rows, positions, page_size, head_dim, dtype, k_out=None, v_out=None, stream=None):
+    """Values of tokens (rows[i], positions[i]) of one layer: (k, v) [tokens, n_kv_heads, d] of `dtype` (the type the
+    pool was written with).  k_out / v_out: two tensors of that shape with equal strides (e.g. transposed views)."""
+    import torch
+    dev = pool.device
+    with _On(dev, stream) as st:
+        hkv = _pool(pool, 2, page_size, head_dim)
+        n = positions.shape[0]
+        k_out = torch.empty(n, hkv, head_dim, dtype=dtype, device=dev) if k_out is None else k_out
+        v_out = torch.empty(n, hkv, head_dim, dtype=dtype, device=dev) if v_out is None else v_out
+        for t in (k_out, v_out):
+            _want(tuple(t.shape) == (n, hkv, head_dim) and t.dtype == dtype and t.device == dev and t.stride(2) == 1 and
+                  t.stride() == k_out.stride(), "k_out, v_out: [tokens, heads, head_dim], equal strides")
+        _want(table.dim() == 2, "table: [rows, max_pages]")
+        _want_int32(dev, table=(table, table.shape), rows=(rows, (n,)), positions=(positions, (n,)))
+        s = storage_of(k_out)
+        _check(lib(s).thinfer_op_kv4_read(pool.data_ptr(), pool.shape[0], table.data_ptr(), table.shape[0], table.shape[1],
+                                          k_out.data_ptr(), v_out.data_ptr(), k_out.stride(0), k_out.stride(1), rows.data_ptr(),
+                                          positions.data_ptr(), n, hkv, head_dim, page_size, st), None, s)
+    return k_out, v_out
+
+
+def op_kv4_attention(q, pool, table, lens, page_size, out=None, workspace=None, stream=None):
+    """q [batch, queries, n_q_heads, d] (already rotated) over one layer's 4-bit pool [n_pages, page bytes]: request b is
+    row b of table and holds lens[b] keys, the query tokens the last among them.  Returns [batch, queries, n_q_heads, d]."""
+    import torch
+    dev = q.device
+    with _On(dev, stream) as st:
+        _want(q.dim() == 4, "q: [batch, queries, n_q_heads, head_dim]")
+        b, n, hq, d = q.shape
+        _want(b == 1 or n == 1 or q.stride(0) == n * q.stride(1), "q: the query tokens must be evenly spaced")
+        flat = q.reshape(b * n, hq, d) if n == 1 or q.is_contiguous() else q.view(b * n, hq, d)
+        qs = _token_stride(flat, "q", q.dtype, dev)
+        hkv = _pool(pool, 2, page_size, d)
+        _want(pool.device == dev, f"pool: on {dev}")
+        _want(table.dim() == 2, "table: [batch, max_pages]")
+        _want_int32(dev, table=(table, (b, table.shape[1])), lens=(lens, (b,)))
+        out = torch.empty(b, n, hq, d, dtype=q.dtype, device=dev) if out is None else out
+        _want(tuple(out.shape) == (b, n, hq, d) and out.dtype == q.dtype and out.device == dev and out.is_contiguous(), "out: contiguous, the shape of q")
+        s = storage_of(q)
+        L = lib(s)
+        if workspace is None:
+            need = C.c_size_t(0)
+            _check(L.thinfer_kv4_attention_workspace(b, n, hq, hkv, d, C.byref(need)), None, s)
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        _check(L.thinfer_op_kv4_attention(flat.data_ptr(), qs, pool.data_ptr(), pool.shape[0], table.data_ptr(), table.shape[1],
+                                          lens.data_ptr(), out.data_ptr(), b, n, hq, hkv, d, page_size, workspace.data_ptr(),
+                                          workspace.numel() * workspace.element_size(), st), None, s)
+    return out
+
+
+def _pages_workspace(rows, n_pages, device):
+    import torch
+    need = C.c_size_t(0)
+    _check(lib().thinfer_kv4_pages_workspace(rows, n_pages, C.byref(need)))
+    return torch.empty(need.value, dtype=torch.uint8, device=device)
+
+
+def op_kv4_fork(pool, table, lens, source, page_size, head_dim, table_out=None, lens_out=None, refused=None, stream=None):
+    """New row r takes over old row source[r] (negative: freed) of a pool [n_layers, n_pages, page bytes]: full pages are
+    shared, a partly filled last page is copied for every heir but one.  Returns (table_out, lens_out, refused)."""
+    import torch
+    dev = pool.device
+    with _On(dev, stream) as st:
+        hkv = _pool(pool, 3, page_size, head_dim)
+        _want(table.dim() == 2, "table: [rows, max_pages]")
+        rows, max_pages = table.shape
+        table_out = torch.empty_like(table) if table_out is None else table_out
+        lens_out = torch.empty_like(lens) if lens_out is None else lens_out
+        refused = torch.empty(1, dtype=torch.int32, device=dev) if refused is None else refused
+        _want_int32(dev, table=(table, (rows, max_pages)), lens=(lens, (rows,)), source=(source, (rows,)),
+                    table_out=(table_out, (rows, max_pages)), lens_out=(lens_out, (rows,)), refused=(refused, (1,)))
+        ws = _pages_workspace(rows, pool.shape[1], dev)
+        _check(lib().thinfer_op_kv4_fork(pool.data_ptr(), pool.shape[0], pool.shape[1], table.data_ptr(), lens.data_ptr(),
+                                         source.data_ptr(), table_out.data_ptr(), lens_out.data_ptr(), refused.data_ptr(), rows,
+                                         max_pages, hkv, head_dim, page_size, ws.data_ptr(), ws.numel(), st))
+    return table_out, lens_out, refused
+
+
+def op_kv4_compact(pool, table, lens, page_size, head_dim, table_out=None, live=None, stream=None):
+    """Moves the pages in use of a pool [n_layers, n_pages, page bytes] to its front.  Returns (table_out, live): the table
+    with the new page numbers and the number of pages in use."""
+    import torch
+    dev = pool.device
+    with _On(dev, stream) as st:
+        hkv = _pool(pool, 3, page_size, head_dim)
+        _want(table.dim() == 2, "table: [rows, max_pages]")
+        rows, max_pages = table.shape
+        table_out = torch.empty_like(table) if table_out is None else table_out
+        live = torch.empty(1, dtype=torch.int32, device=dev) if live is None else live
+        _want_int32(dev, table=(table, (rows, max_pages)), lens=(lens, (rows,)), table_out=(table_out, (rows, max_pages)), live=(live, (1,)))
+        ws = _pages_workspace(rows, pool.shape[1], dev)
+        _check(lib().thinfer_op_kv4_compact(pool.data_ptr(), pool.shape[0], pool.shape[1], table.data_ptr(), lens.data_ptr(),
+                                            table_out.data_ptr(), live.data_ptr(), rows, max_pages, hkv, head_dim, page_size,
+                                            ws.data_ptr(), ws.numel(), st))
+    return table_out, live
 
 
 def to_device_layers(np_layers, device="cuda:0"):
