@@ -377,8 +377,8 @@ int thinfer_kv4_page_bytes(int32_t n_kv_heads, int32_t head_dim, int32_t page_si
 /* Makes room for add[r] more tokens of every row (negative: none): rows in ascending order take the lowest free pages,
  * their numbers are written into table, lens_out[r] = lens[r] + add[r].  A row whose pages, together with those asked
  * for by the rows before it, exceed the free pages, or that would not fit max_pages, keeps its length and table;
- * *refused (int32) counts those rows.  lens_out may be lens.  n_rows <= 4096, n_pages <= 262144. */
-int thinfer_op_kv4_reserve(int32_t* table, const int32_t* lens, const int32_t* add, int32_t* lens_out, int32_t* refused,
+ * *refused (int64) counts those rows.  lens_out may be lens.  n_rows <= 4096, n_pages <= 262144. */
+int thinfer_op_kv4_reserve(int32_t* table, const int32_t* lens, const int32_t* add, int32_t* lens_out, int64_t* refused,
                            int32_t n_rows, int32_t max_pages, int32_t n_pages, int32_t page_size, void* cuda_stream);
 
 /* Quantises tokens into one layer's pages: k, v FP16 [tokens][n_kv_heads * head_dim], strides in elements between
@@ -401,7 +401,7 @@ int thinfer_op_kv4_read(const void* pool, int32_t n_pages, const int32_t* table,
  * table with lens[b] keys, its query tokens among them; query i attends the keys before position
  * lens[b] - (queries - 1 - i) (one query: all of them).  A query that sees no key gives 0.  q FP16 [batch * queries]
  * tokens of n_q_heads * head_dim values, q_stride elements apart, already rotated; out FP16 [batch][queries][n_q_heads
- * * head_dim].  n_q_heads a multiple of n_kv_heads.  workspace: thinfer_kv4_attention_workspace bytes, 16-byte
+ * * head_dim].  n_q_heads a multiple of n_kv_heads; batch <= 4096.  workspace: thinfer_kv4_attention_workspace bytes, 16-byte
  * aligned; its contents mean nothing between calls, but calls that may overlap on the device need their own. */
 int thinfer_kv4_attention_workspace(int32_t batch, int32_t queries, int32_t n_q_heads, int32_t n_kv_heads,
                                     int32_t head_dim, size_t* bytes);
@@ -419,16 +419,16 @@ int thinfer_op_kv4_attention(const void* q, int64_t q_stride, const void* pool, 
  * before the call are not changed.  n_rows <= 4096, n_pages <= 262144. */
 int thinfer_kv4_pages_workspace(int32_t n_rows, int32_t n_pages, size_t* bytes);
 int thinfer_op_kv4_fork(void* pool, int32_t n_layers, int32_t n_pages, const int32_t* table, const int32_t* lens,
-                        const int32_t* source, int32_t* table_out, int32_t* lens_out, int32_t* refused, int32_t n_rows,
+                        const int32_t* source, int32_t* table_out, int32_t* lens_out, int64_t* refused, int32_t n_rows,
                         int32_t max_pages, int32_t n_kv_heads, int32_t head_dim, int32_t page_size, void* workspace,
                         size_t workspace_bytes, void* cuda_stream);
 
 /* Moves the pages in use to the front of the pool: with L pages in use, those numbered L and above move in ascending
  * order into the free pages below L, in all n_layers layers (filled tokens only, in groups of 16).  table_out: the table
- * with the new numbers, -1 behind a row's pages; *live_pages (int32) = L: the pool behind L pages may be given back.
+ * with the new numbers, -1 behind a row's pages; *live_pages (int64) = L: the pool behind L pages may be given back.
  * The outputs must not overlap the inputs. */
 int thinfer_op_kv4_compact(void* pool, int32_t n_layers, int32_t n_pages, const int32_t* table, const int32_t* lens,
-                           int32_t* table_out, int32_t* live_pages, int32_t n_rows, int32_t max_pages,
+                           int32_t* table_out, int64_t* live_pages, int32_t n_rows, int32_t max_pages,
                            int32_t n_kv_heads, int32_t head_dim, int32_t page_size, void* workspace,
                            size_t workspace_bytes, void* cuda_stream);
 

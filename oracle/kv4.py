@@ -109,8 +109,8 @@ def keys_values(pool, table_row, n):
 
 
 def attention(q, kv, n_keys, limit_shift):
-    """q [hq][d] over the first n_keys - limit_shift keys of kv = (K, V); also sum_t p_t |v_t| and max_t sum |q k| / sqrt d
-    (what rounding the weights, and the scores, can move)."""
+    """q [hq][d] over the first n_keys - limit_shift keys of kv = (K, V); also sum_t p_t (|v_t - middle of the row| + 1/28 of
+    its range) and max_t sum |q k| / sqrt d: what rounding the weights, and the scores, can move."""
     hq, d = q.shape
     k, v = kv
     m = n_keys - limit_shift
@@ -123,7 +123,8 @@ def attention(q, kv, n_keys, limit_shift):
         s = kh @ q[h].astype(np.float64) / np.sqrt(d)
         p = np.exp(s - s.max()) if np.all(np.isfinite(s)) else np.full(m, np.nan)
         p = p / p.sum()
-        out[h], spread[h] = p @ vh, p @ np.abs(vh)
+        low, high = vh.min(-1, keepdims=True), vh.max(-1, keepdims=True)
+        out[h], spread[h] = p @ vh, p @ (np.abs(vh - (low + high) / 2) + (high - low) / 28)
         mag[h] = np.max(np.abs(kh) @ np.abs(q[h].astype(np.float64))) / np.sqrt(d)
     return out, spread, mag
 

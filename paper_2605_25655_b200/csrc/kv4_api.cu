@@ -89,6 +89,36 @@ int copy_pages(void* pool, const int* count, const PageMove* moves, int most_mov
                    page_bytes * static_cast<size_t>(n_pages));
 }
 
+// Column tiles of 8 (16 where a KV head has more query columns than 8, so that its keys are unpacked half as often) and
+// one resident wave of CTAs: the 16-column kernel needs the registers of a whole SM.
+struct AttnPlan {
+  int tiles, col_tiles, grid;
+  size_t split_bytes, part_bytes;
+};
+int plan_attention(int32_t batch, int32_t queries, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, AttnPlan* p) {
+  if (head_dim != 64 && head_dim != 128) return op_fail(THINFER_EUNSUPPORTED, "head_dim %d: 64 and 128 are supported", head_dim);
+  if (n_q_heads % n_kv_heads != 0) return op_fail(THINFER_EUNSUPPORTED, "n_q_heads must be a multiple of n_kv_heads");
+  const int64_t cols = static_cast<int64_t>(n_q_heads / n_kv_heads) * queries;
+  p->tiles = cols > 8 ? 2 : 1;
+  const int64_t col_tiles = (cols + 8 * p->tiles - 1) / (8 * p->tiles);
+  if (batch > 4096 || col_tiles * n_kv_heads > 16384)
+    return op_fail(THINFER_EUNSUPPORTED, "kv4_attention: batch %d > 4096, or more than 262144 query columns per request", batch);
+  p->col_tiles = static_cast<int>(col_tiles);
+  p->grid = op_sm_count() * (p->tiles == 1 ? 2 : 1);
+  p->split_bytes = (static_cast<size_t>(p->grid) * sizeof(Kv4Split) + 255) / 256 * 256;
+  p->part_bytes = static_cast<size_t>(p->grid) * 2 * p->tiles * 8 * (head_dim + 2) * 4;
+  return THINFER_OK;
+}
+
+template <int D, int NT>
+int launch_attention(const Kv4AttnArgs& a, int grid, cudaStream_t st) {
+  const size_t smem = kKv4Warps * kv4_warp_bytes<D, NT>() + (static_cast<size_t>(a.batch) + 1) * 8;
+  int rc = opt_in(kv4_attn_kernel<D, NT>, smem);
+  if (rc == THINFER_OK) rc = op_launch(kv4_attn_kernel<D, NT>, dim3(grid), dim3(kKv4Warps * 32), smem, st, false, a);
+  if (rc == THINFER_OK) rc = op_launch(kv4_attn_join_kernel<D, NT>, dim3(grid, NT * 8), dim3(256), 0, st, true, a);
+  return rc;
+}
+
 }  // namespace
 
 extern "C" {
@@ -213,8 +243,10 @@ int thinfer_kv4_attention_workspace(int32_t batch, int32_t queries, int32_t n_q_
                                     int32_t head_dim, size_t* bytes) {
   if (bytes == nullptr || batch <= 0 || queries <= 0 || n_q_heads <= 0 || n_kv_heads <= 0)
     return op_fail(THINFER_EINVAL, "kv4_attention: a size is not positive, or bytes is NULL");
-  (void)head_dim;
-  *bytes = 16;
+  AttnPlan p;
+  const int rc = plan_attention(batch, queries, n_q_heads, n_kv_heads, head_dim, &p);
+  if (rc != THINFER_OK) return rc;
+  *bytes = p.split_bytes + p.part_bytes;
   return THINFER_OK;
 }
 
@@ -226,13 +258,13 @@ int thinfer_op_kv4_attention(const void* q, int64_t q_stride, const void* pool, 
   if (rc != THINFER_OK) return rc;
   if (q == nullptr || lens == nullptr || out == nullptr || workspace == nullptr || queries <= 0 || n_q_heads <= 0)
     return op_fail(THINFER_EINVAL, "kv4_attention: NULL pointer, or a size that is not positive");
-  if (n_q_heads % n_kv_heads != 0) return op_fail(THINFER_EUNSUPPORTED, "n_q_heads must be a multiple of n_kv_heads");
+  AttnPlan p;
+  rc = plan_attention(batch, queries, n_q_heads, n_kv_heads, head_dim, &p);
+  if (rc != THINFER_OK) return rc;
   if (!stride_ok(q_stride, static_cast<int64_t>(n_q_heads) * head_dim) || !aligned16(q) || !aligned16(out) || !aligned4(lens) || !aligned16(workspace))
     return op_fail(THINFER_EINVAL, "kv4_attention: a pointer or the token stride is not aligned, or the stride is below heads * head_dim");
-  size_t need = 0;
-  rc = thinfer_kv4_attention_workspace(batch, queries, n_q_heads, n_kv_heads, head_dim, &need);
-  if (rc != THINFER_OK) return rc;
-  if (workspace_bytes < need) return op_fail(THINFER_ECAPACITY, "kv4_attention: the workspace has %zu bytes of %zu", workspace_bytes, need);
+  if (workspace_bytes < p.split_bytes + p.part_bytes)
+    return op_fail(THINFER_ECAPACITY, "kv4_attention: the workspace has %zu bytes of %zu", workspace_bytes, p.split_bytes + p.part_bytes);
   Kv4AttnArgs a{};
   a.c = make_cache(pool, table, batch, max_pages, n_pages, n_kv_heads, head_dim, page_size);
   a.lens = lens;
@@ -243,26 +275,33 @@ int thinfer_op_kv4_attention(const void* q, int64_t q_stride, const void* pool, 
   a.queries = queries;
   a.n_q = n_q_heads;
   a.group = n_q_heads / n_kv_heads;
-  a.scale = 1.f / sqrtf(static_cast<float>(head_dim));
-  const int64_t tokens = static_cast<int64_t>(batch) * queries;
-  if (tokens > 0x7fffffff || n_q_heads > 65535) return op_fail(THINFER_EUNSUPPORTED, "kv4_attention: too many query tokens or heads");
-  return op_launch(head_dim == 128 ? kv4_attn_simple_kernel<128> : kv4_attn_simple_kernel<64>,
-                   dim3(static_cast<unsigned>(tokens), static_cast<unsigned>(n_q_heads)), dim3(kKv4SimpleThreads), 0,
-                   static_cast<cudaStream_t>(cuda_stream), false, a);
+  a.cols = a.group * queries;
+  a.col_tiles = p.col_tiles;
+  a.splits = static_cast<Kv4Split*>(workspace);
+  a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.split_bytes);
+  a.scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(head_dim));
+  // no more CTAs than the table's capacity could give a unit per warp
+  const int64_t units = static_cast<int64_t>(batch) * n_kv_heads * p.col_tiles *
+                        ((static_cast<int64_t>(max_pages) * page_size + kKv4Unit - 1) / kKv4Unit);
+  const int64_t most = (units + kKv4Warps - 1) / kKv4Warps;
+  const int grid = most < p.grid ? static_cast<int>(most) : p.grid;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (head_dim == 128) return p.tiles == 1 ? launch_attention<128, 1>(a, grid, st) : launch_attention<128, 2>(a, grid, st);
+  return p.tiles == 1 ? launch_attention<64, 1>(a, grid, st) : launch_attention<64, 2>(a, grid, st);
 }
 
-int thinfer_op_kv4_reserve(int32_t* table, const int32_t* lens, const int32_t* add, int32_t* lens_out, int32_t* refused,
+int thinfer_op_kv4_reserve(int32_t* table, const int32_t* lens, const int32_t* add, int32_t* lens_out, int64_t* refused,
                            int32_t n_rows, int32_t max_pages, int32_t n_pages, int32_t page_size, void* cuda_stream) {
   int rc = check_tables(table, n_rows, max_pages, n_pages);
   if (rc == THINFER_OK) rc = check_layout(1, 64, page_size);
   if (rc == THINFER_OK) rc = check_plan(n_rows, n_pages);
   if (rc != THINFER_OK) return rc;
   if (lens == nullptr || add == nullptr || lens_out == nullptr || refused == nullptr || !aligned4(lens) || !aligned4(add) ||
-      !aligned4(lens_out) || !aligned4(refused))
+      !aligned4(lens_out) || !aligned8(refused))
     return op_fail(THINFER_EINVAL, "kv4_reserve: a pointer is NULL or not 4-byte aligned");
   const size_t nb = static_cast<size_t>(n_rows) * 4;
-  if ((lens_out != lens && overlap(lens_out, nb, lens, nb)) || overlap(lens_out, nb, add, nb) || overlap(refused, 4, lens, nb) ||
-      overlap(refused, 4, add, nb) || overlap(refused, 4, lens_out, nb))
+  if ((lens_out != lens && overlap(lens_out, nb, lens, nb)) || overlap(lens_out, nb, add, nb) || overlap(refused, 8, lens, nb) ||
+      overlap(refused, 8, add, nb) || overlap(refused, 8, lens_out, nb))
     return op_fail(THINFER_EINVAL, "kv4_reserve: lens_out may be lens itself; other outputs must not overlap inputs");
   if ((static_cast<int64_t>(max_pages) * page_size) > 0x7fffffff)
     return op_fail(THINFER_EUNSUPPORTED, "max_pages %d: a row holds fewer than 2^31 tokens", max_pages);
@@ -283,7 +322,7 @@ int thinfer_kv4_pages_workspace(int32_t n_rows, int32_t n_pages, size_t* bytes) 
 }
 
 int thinfer_op_kv4_fork(void* pool, int32_t n_layers, int32_t n_pages, const int32_t* table, const int32_t* lens,
-                        const int32_t* source, int32_t* table_out, int32_t* lens_out, int32_t* refused, int32_t n_rows,
+                        const int32_t* source, int32_t* table_out, int32_t* lens_out, int64_t* refused, int32_t n_rows,
                         int32_t max_pages, int32_t n_kv_heads, int32_t head_dim, int32_t page_size, void* workspace,
                         size_t workspace_bytes, void* cuda_stream) {
   int rc = check_cache(pool, table, n_rows, max_pages, n_pages, n_kv_heads, head_dim, page_size);
@@ -291,13 +330,13 @@ int thinfer_op_kv4_fork(void* pool, int32_t n_layers, int32_t n_pages, const int
   if (rc != THINFER_OK) return rc;
   if (n_layers <= 0 || lens == nullptr || source == nullptr || table_out == nullptr || lens_out == nullptr || refused == nullptr ||
       workspace == nullptr || !aligned4(lens) || !aligned4(source) || !aligned4(table_out) || !aligned4(lens_out) ||
-      !aligned4(refused) || !aligned16(workspace))
+      !aligned8(refused) || !aligned16(workspace))
     return op_fail(THINFER_EINVAL, "kv4_fork: a pointer is NULL or not aligned, or n_layers is not positive");
   const size_t nb = static_cast<size_t>(n_rows) * 4, tb = nb * max_pages;
   const void* ins[3] = {table, lens, source};
   const size_t in_b[3] = {tb, nb, nb};
   void* outs[3] = {table_out, lens_out, refused};
-  const size_t out_b[3] = {tb, nb, 4};
+  const size_t out_b[3] = {tb, nb, 8};
   for (int o = 0; o < 3; ++o) {
     for (int i = 0; i < 3; ++i)
       if (overlap(outs[o], out_b[o], ins[i], in_b[i])) return op_fail(THINFER_EINVAL, "kv4_fork: an output overlaps an input");
@@ -318,18 +357,18 @@ int thinfer_op_kv4_fork(void* pool, int32_t n_layers, int32_t n_pages, const int
 }
 
 int thinfer_op_kv4_compact(void* pool, int32_t n_layers, int32_t n_pages, const int32_t* table, const int32_t* lens,
-                           int32_t* table_out, int32_t* live_pages, int32_t n_rows, int32_t max_pages,
+                           int32_t* table_out, int64_t* live_pages, int32_t n_rows, int32_t max_pages,
                            int32_t n_kv_heads, int32_t head_dim, int32_t page_size, void* workspace,
                            size_t workspace_bytes, void* cuda_stream) {
   int rc = check_cache(pool, table, n_rows, max_pages, n_pages, n_kv_heads, head_dim, page_size);
   if (rc == THINFER_OK) rc = check_plan(n_rows, n_pages);
   if (rc != THINFER_OK) return rc;
   if (n_layers <= 0 || lens == nullptr || table_out == nullptr || live_pages == nullptr || workspace == nullptr || !aligned4(lens) ||
-      !aligned4(table_out) || !aligned4(live_pages) || !aligned16(workspace))
+      !aligned4(table_out) || !aligned8(live_pages) || !aligned16(workspace))
     return op_fail(THINFER_EINVAL, "kv4_compact: a pointer is NULL or not aligned, or n_layers is not positive");
   const size_t nb = static_cast<size_t>(n_rows) * 4, tb = nb * max_pages;
-  if (overlap(table_out, tb, table, tb) || overlap(table_out, tb, lens, nb) || overlap(live_pages, 4, table, tb) ||
-      overlap(live_pages, 4, lens, nb) || overlap(live_pages, 4, table_out, tb))
+  if (overlap(table_out, tb, table, tb) || overlap(table_out, tb, lens, nb) || overlap(live_pages, 8, table, tb) ||
+      overlap(live_pages, 8, lens, nb) || overlap(live_pages, 8, table_out, tb))
     return op_fail(THINFER_EINVAL, "kv4_compact: an output overlaps another tensor");
   const int most = n_pages / 2 > 0 ? n_pages / 2 : 1;
   if (workspace_bytes < moves_bytes(n_pages / 2)) return op_fail(THINFER_ECAPACITY, "kv4_compact: the workspace is too small");

@@ -3,12 +3,53 @@
 //   S[i, t] = q_i . k_t / sqrt(D),  t < len - (queries - 1 - i)        (the query tokens are the last of the len keys)
 //   out_i   = sum_t softmax_t(S[i, t]) v_t,   k_t, v_t = offset + scale * code;   0 where a query sees no key
 //
-// One CTA per (request, query token, query head): D / 8 lanes per key, an online softmax per lane group, merged at
-// the end.  FP32 throughout.
+// Scale and offset of a row belong to all its D values, so neither has to touch the codes:
+//
+//   S[i, t]  = scale_t (q_i . code_t) + offset_t (sum of q_i)
+//   out_i    = ( sum_t w_t code_t - 7.5 sum_t w_t + sum_t p_t (offset_t + 7.5 scale_t) ) / sum_t p_t,   w_t = p_t scale_t
+//
+// and the matrix instructions multiply by the codes themselves.  A code in the low mantissa bits of an FP16 number is
+// the subnormal code * 2^-24 (bits 0-3) or code * 2^-20 (bits 4-7), which the tensor cores take at face value: one AND
+// turns two codes into two operands, one shift per eight codes reaches the other byte of a half, and the powers of two
+// are put back in FP32.  All products q * code and weight * code are then exact in FP32.  Both builds use FP16
+// operands: a query row is scaled by the power of two that brings its largest value to [2^12, 2^13), which loses
+// nothing within 2^-22 of that value.
+//
+// Cache rows are the A operand (16 tokens, or 16 dimensions, per instruction) and up to 8 query columns - the query
+// heads of one KV head times the query tokens - are the B operand, so that each instruction consumes 256 codes:
+//
+//   S^T[token, column] = K[token, :] Q^T        A = K codes, B = Q (registers, once per segment)
+//   O^T[dim, column]  += V^T[dim, token] P^T    A = V codes (the layout keeps token pairs together), B = weights
+//
+// The weights w go to FP16 relative to a running reference per column; sums of p and of p times the middle of the row
+// stay in FP32, and the second sum above is taken over the rounded weights (one more instruction per 16 tokens, against
+// a matrix of ones), so that a rounding of w counts with the distance from the middle of the row, at most 7.5 scale,
+// instead of the whole code: without it the FP16 error against 64 bits was 1.6 times that of an FP32 attention.  The running maximum and that reference move only when a weight
+// would exceed 2^8 (one vote per 32 tokens): the shuffles and the rescaling of the output are then off the usual path.
+//
+// Bound: HBM, D + 8 bytes per key and KV head; at 6.4 TB/s an SM has to consume 48 codes a cycle, which leaves 2.7
+// issue slots per code.  Work: all (request, KV head, column tile) pairs are cut into units of 32 tokens, laid end to
+// end and dealt out in equal runs, first to the CTAs, then to the warps of a CTA; the lengths are only known on the
+// device, so each CTA sums them up itself.  A warp streams its units through a private ring in shared memory filled by
+// bulk asynchronous copies (one lane issues, no synchronisation between warps).  What a warp cannot finish is merged
+// in shared memory; what a CTA cannot finish goes to the workspace and a second kernel, chained to this one, merges it
+// in CTA order: the result does not depend on timing, and the workspace needs no initial state.
 #pragma once
 #include "kv4_layout.cuh"
 
 namespace thinfer {
+
+constexpr int kKv4Warps = 8;
+constexpr int kKv4Unit = 32;         // tokens of one ring stage
+constexpr int kKv4Stages = 2;        // with 8 warps and 2 CTAs per SM 70 to 140 KB are in flight, two to four times what
+                                     // HBM latency asks for
+constexpr float kKv4Low = -1e30f;    // running maximum before the first key
+
+// What a CTA leaves for the second kernel about the pair that begins in it and ends in a later one.
+struct Kv4Split {
+  int b, pair_in_b, last;   // last: the CTA it ends in, -1: there is no such pair
+  int pad;
+};
 
 struct Kv4AttnArgs {
   Kv4Cache c;
@@ -17,75 +58,638 @@ struct Kv4AttnArgs {
   half_t* out;           // [batch * queries][n_q][D]
   long long q_stride;
   int batch, queries, n_q, group;
-  float scale;           // 1 / sqrt(D)
+  int cols;              // group * queries: query columns of one KV head
+  int col_tiles;
+  Kv4Split* splits;      // [grid]
+  float* parts;          // [grid][2] unfinished pieces of CTAs: [columns][D] outputs, then [columns][2] maximum and sum;
+                         // piece 0 began in an earlier CTA, piece 1 begins here
+  float scale_log2;      // log2(e) / sqrt(D)
 };
 
-constexpr int kKv4SimpleThreads = 128;
-
 template <int D>
-__global__ void __launch_bounds__(kKv4SimpleThreads) kv4_attn_simple_kernel(const Kv4AttnArgs a) {
-  constexpr int LPR = D / 8;
-  constexpr int NG = kKv4SimpleThreads / LPR;
-  __shared__ float sm[NG], sl[NG], so[NG][D];
-  const int g = threadIdx.x / LPR, sub = threadIdx.x % LPR;
-  const int token = blockIdx.x, b = token / a.queries, i = token - b * a.queries;
-  const int h = blockIdx.y, hk = h / a.group;
-  const int page = 1 << a.c.page_shift;
-  const long long cap = static_cast<long long>(a.c.max_pages) << a.c.page_shift;
-  long long lim = static_cast<long long>(__ldg(a.lens + b)) - (a.queries - 1 - i);
-  if (lim > cap) lim = cap;
-  const int limit = static_cast<int>(lim);
-  float q[8], o[8];
-  unpack8(*reinterpret_cast<const uint4*>(a.q + token * a.q_stride + static_cast<long long>(h) * D + sub * 8), q);
-  float m = -INFINITY, l = 0.f;
+__host__ __device__ constexpr int kv4_stage_bytes() {
+  return kKv4Unit * (D + 8);
+}
+template <int D, int NT>
+__host__ __device__ constexpr int kv4_partial_floats() {  // one unfinished piece: outputs, then maximum and sum
+  return NT * 8 * (D + 2);
+}
+// Memory of one warp: its ring, which takes the piece that ends its range once it has drained, and room for the piece
+// that begins its range.
+template <int D, int NT>
+__host__ __device__ constexpr int kv4_warp_bytes() {
+  return kKv4Stages * kv4_stage_bytes<D>() + kv4_partial_floats<D, NT>() * 4;
+}
+
+// ------------------------------------------------------------------ schedule
+// Units of request b times (KV heads x column tiles), summed over the requests: pref[b] is the first unit of b.
+// A length beyond what the table can name gives NaN whatever it is: it counts as one unit more than the table holds,
+// behind the last key of every query.
+__device__ __forceinline__ int kv4_len(const Kv4AttnArgs& a, int b) {
+  const long long cap = min((static_cast<long long>(a.c.max_pages) << a.c.page_shift) + kKv4Unit + a.queries, 0x7fffffc0ll);
+  const int n = __ldg(a.lens + b);
+  return n < 0 ? 0 : static_cast<int>(min(static_cast<long long>(n), cap));
+}
+__device__ __forceinline__ int kv4_units(int len) { return len <= kKv4Unit ? 1 : (len + kKv4Unit - 1) / kKv4Unit; }
+
+__device__ __forceinline__ void kv4_prefix(const Kv4AttnArgs& a, long long* pref, long long* warp_sums) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const long long per_unit = static_cast<long long>(a.c.n_kv) * a.col_tiles;
+  long long carry = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += blockDim.x) {
+    const int b = b0 + threadIdx.x;
+    const long long v = b < a.batch ? kv4_units(kv4_len(a, b)) * per_unit : 0;
+    long long s = v;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) o[j] = 0.f;
-  for (int t0 = 0; t0 < limit; t0 += NG) {   // uniform trip count: the shuffles need the whole warp
-    const int t = t0 + g;
-    const uint8_t* block = t < limit ? kv4_block(a.c, b, t, hk) : nullptr;
-    uint32_t kw = 0, vw = 0;
-    float2 kp = make_float2(__int_as_float(0x7fffffff), 0.f), vp = kp;
-    if (block != nullptr) {
-      const int slot = t & (page - 1);
-      kw = *reinterpret_cast<const uint32_t*>(block + slot * (D / 2) + sub * 4);
-      const uint16_t* vs = reinterpret_cast<const uint16_t*>(block + page * (D / 2) + (slot >> 1) * D + sub * 8) + (slot & 1);
-      vw = vs[0] | (static_cast<uint32_t>(vs[2]) << 16);
-      kp = kv4_unpack_params(*reinterpret_cast<const uint32_t*>(block + page * D + slot * 4));
-      vp = kv4_unpack_params(*reinterpret_cast<const uint32_t*>(block + page * D + page * 4 + slot * 4));
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long u = __shfl_up_sync(0xffffffffu, s, o);
+      if (lane >= o) s += u;
     }
-    float s = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) s = fmaf(q[j], fmaf(kp.x, static_cast<float>((kw >> (4 * j)) & 15u), kp.y), s);
-#pragma unroll
-    for (int off = LPR / 2; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-    if (t < limit) {
-      s *= a.scale;
-      const float mn = fmaxf(m, s), ms = mn == -INFINITY ? 0.f : mn;
-      const float al = __expf(m - ms), p = __expf(s - ms);
-      m = mn;
-      l = l * al + p;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = o[j] * al + p * fmaf(vp.x, static_cast<float>((vw >> (4 * j)) & 15u), vp.y);
+    if (lane == 31) warp_sums[warp] = s;
+    __syncthreads();
+    long long before = carry, all = 0;
+    for (int w = 0; w < warps; ++w) {
+      if (w < warp) before += warp_sums[w];
+      all += warp_sums[w];
     }
+    if (b < a.batch) pref[b] = before + s - v;
+    carry += all;
+    __syncthreads();
   }
-  if (sub == 0) {
-    sm[g] = m;
-    sl[g] = l;
-  }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) so[g][sub * 8 + j] = o[j];
+  if (threadIdx.x == 0) pref[a.batch] = carry;
   __syncthreads();
-  for (int e = threadIdx.x; e < D; e += kKv4SimpleThreads) {
-    float mx = -INFINITY;
-    for (int w = 0; w < NG; ++w) mx = fmaxf(mx, sm[w]);
-    const float ms = mx == -INFINITY ? 0.f : mx;
-    float L = 0.f, O = 0.f;
-    for (int w = 0; w < NG; ++w) {
-      const float al = __expf(sm[w] - ms);
-      L += sl[w] * al;
-      O += so[w][e] * al;
+}
+
+struct Kv4Place {
+  int b, pair_in_b, unit, units, len;
+  long long pair_first;  // first unit of the pair
+};
+__device__ __forceinline__ Kv4Place kv4_place(const Kv4AttnArgs& a, const long long* pref, long long u) {
+  int lo = 0, hi = a.batch - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (pref[mid] <= u) lo = mid;
+    else hi = mid - 1;
+  }
+  Kv4Place p;
+  p.b = lo;
+  p.len = kv4_len(a, lo);
+  p.units = kv4_units(p.len);
+  const long long in_b = u - pref[lo];
+  p.pair_in_b = static_cast<int>(in_b / p.units);
+  p.unit = static_cast<int>(in_b - static_cast<long long>(p.pair_in_b) * p.units);
+  p.pair_first = u - p.unit;
+  return p;
+}
+// CTAs that take part: with few units some stay idle rather than split pairs further.
+__device__ __forceinline__ long long kv4_ctas(long long total, int grid) {
+  const long long want = (total + kKv4Warps - 1) / kKv4Warps;
+  return want < grid ? want : grid;
+}
+__device__ __forceinline__ long long kv4_cta_first(long long total, long long ctas, long long i) { return i * total / ctas; }
+__device__ __forceinline__ long long kv4_cta_of(long long total, long long ctas, long long u) { return ((u + 1) * ctas - 1) / total; }
+
+// ------------------------------------------------------------------ instructions
+__device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// Untiled copy global -> shared; both addresses 16-byte aligned, bytes a multiple of 16.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
+template <int W>
+__device__ __forceinline__ void lds_words(uint32_t (&r)[W], uint32_t addr) {
+  if constexpr (W == 4)
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+  else
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr));
+}
+__device__ __forceinline__ float2 lds_params(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr));
+  return kv4_unpack_params(v);
+}
+
+// Where lane (r, c) = (lane / 4, lane % 4) finds things in a block of 16 tokens.  Row r of the score tile is token
+// 4 (r / 2) + r % 2 and row r + 8 the token two further: after the 8 x 8 transposes lane c then holds the weights of
+// tokens 4c .. 4c + 3, two neighbouring pairs of the V layout.
+__device__ __forceinline__ int kv4_row_token(int r) { return 4 * (r >> 1) + (r & 1); }
+
+// State of one warp's current pair: columns 2c and 2c + 1 of every column tile.
+template <int D, int NT>
+struct Kv4Acc {
+  float o[NT][D / 16][4];
+  float ones[NT][4];                               // sum of the rounded weights, in every row
+  float m[NT][2], l[NT][2], z[NT][2], ref[NT][2];  // maximum, sum of p, sum of p times row middle, reference of w
+  float qf[NT][2], qs[NT][2];                      // scale of the code product, scaled sum of the query
+  int lim[NT][2];                                  // keys a column sees
+  uint32_t q[NT][D / 16][2];                       // B operand
+
+  __device__ __forceinline__ void reset() {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) ones[n][e] = 0.f;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        m[n][j] = kKv4Low;
+        l[n][j] = z[n][j] = 0.f;
+        ref[n][j] = __int_as_float(227 << 23);  // 2^100: the first weight sets it
+      }
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[n][i][e] = 0.f;
     }
-    a.out[(static_cast<size_t>(token) * a.n_q + h) * D + e] = f_to_h(limit > 0 ? O / L : 0.f);
+  }
+};
+
+__device__ __forceinline__ float exact_inverse(float pow2) { return __int_as_float((254 << 23) - __float_as_int(pow2)); }
+
+// The query columns of a pair as B operand: lane (r, c) converts the D / 4 values of column r that start at c D / 4.
+template <int D, int NT>
+__device__ __forceinline__ void kv4_load_queries(const Kv4AttnArgs& a, Kv4Acc<D, NT>& s, const Kv4Place& pl, int hk, int col0) {
+  constexpr int W = D / 32;
+  const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int col = col0 + 8 * n + r;
+    float x[8 * W];
+    if (col < a.cols) {
+      const int i = col / a.group, h = hk * a.group + (col - i * a.group);
+      const half_t* src = a.q + (static_cast<long long>(pl.b) * a.queries + i) * a.q_stride + static_cast<long long>(h) * D + c * (D / 4);
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        float f[8];
+        unpack8(ldg_cached(src + 8 * w), f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[8 * w + e] = f[e];
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8 * W; ++e) x[e] = 0.f;
+    }
+    float top = 0.f, sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8 * W; ++e) {
+      top = fmaxf(top, fabsf(x[e]));
+      sum += x[e];
+    }
+#pragma unroll
+    for (int off = 1; off < 4; off <<= 1) {
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+      sum += __shfl_xor_sync(0xffffffffu, sum, off);
+    }
+    const int ex = min(max(__float_as_int(top) >> 23, 13), 253);
+    const float up = __int_as_float((266 - ex) << 23), down = __int_as_float((ex - 12) << 23);
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float* y = x + 8 * w;
+      s.q[n][2 * w][0] = pack_f16(y[0] * up, y[4] * up);
+      s.q[n][2 * w][1] = pack_f16(y[1] * up * 0.0625f, y[5] * up * 0.0625f);   // codes in bits 4-7 weigh 16 times more
+      s.q[n][2 * w + 1][0] = pack_f16(y[2] * up, y[6] * up);
+      s.q[n][2 * w + 1][1] = pack_f16(y[3] * up * 0.0625f, y[7] * up * 0.0625f);
+    }
+    const float qf = 16777216.f * down * a.scale_log2, qs = sum * a.scale_log2;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      s.qf[n][j] = __shfl_sync(0xffffffffu, qf, 8 * c + 4 * j);
+      s.qs[n][j] = __shfl_sync(0xffffffffu, qs, 8 * c + 4 * j);
+      const int cj = col0 + 8 * n + 2 * c + j;
+      s.lim[n][j] = cj < a.cols ? pl.len - (a.queries - 1 - cj / a.group) : 0;
+    }
+  }
+}
+
+// 32 tokens of a ring stage.  MASKED: some of them are behind the end for some column, or on no page (bit b of `bad`:
+// the tokens 16 b .. 16 b + 15).
+template <int D, int NT, bool MASKED>
+__device__ __forceinline__ void kv4_stage(Kv4Acc<D, NT>& s, uint32_t stage, int t0, uint32_t bad) {
+  constexpr int W = D / 32, MT = D / 16;
+  constexpr uint32_t LO = 0x000f000fu, HI = 0x00f000f0u, ONE = 0x3c003c00u;
+  const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+  const int tr = kv4_row_token(r);
+  float sc[2][NT][4];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sc[b][n][e] = 0.f;
+    uint32_t ka[W], kb[W];
+    lds_words<W>(ka, stage + (16 * b + tr) * (D / 2) + c * (D / 8));
+    lds_words<W>(kb, stage + (16 * b + tr + 2) * (D / 2) + c * (D / 8));
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const uint32_t x = hf ? ka[w] >> 8 : ka[w], y = hf ? kb[w] >> 8 : kb[w];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          mma_f16_16816(sc[b][n], x & LO, y & LO, x & HI, y & HI, s.q[n][2 * w + hf][0], s.q[n][2 * w + hf][1]);
+      }
+  }
+  float2 kp[2][2], vp[2][2];   // [block][row r | row r + 8] scale, offset
+  constexpr int KP = kKv4Unit * D, VP = KP + kKv4Unit * 4;
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int t = 16 * b + tr + 2 * e;
+      kp[b][e] = lds_params(stage + KP + t * 4);
+      vp[b][e] = lds_params(stage + VP + t * 4);
+      vp[b][e].y = fmaf(7.5f, vp[b][e].x, vp[b][e].y);   // the middle of the row
+    }
+  auto seen = [&](int b, int e, int n, int j) { return !MASKED || t0 + 16 * b + tr + 2 * e < s.lim[n][j]; };
+  auto raw = [&](int b, int e, int n, int j, float minus) {   // score - minus, log2 units
+    float x = fmaf(kp[b][e].x, sc[b][n][2 * e + j] * s.qf[n][j], fmaf(kp[b][e].y, s.qs[n][j], -minus));
+    if (MASKED) {
+      if ((bad >> b) & 1u) x = __int_as_float(0x7fffffff);
+      if (!seen(b, e, n, j)) x = -INFINITY;
+    }
+    return x;
+  };
+  // value params of a masked token may be anything: they must not meet a weight of zero
+  auto vscale = [&](int b, int e, int n, int j) { return !MASKED || seen(b, e, n, j) ? vp[b][e].x : 0.f; };
+  auto vmid = [&](int b, int e, int n, int j) { return !MASKED || seen(b, e, n, j) ? vp[b][e].y : 0.f; };
+  float p[2][NT][4], w[2][NT][4];
+  float top = 0.f;
+  auto weights = [&]() {
+    top = 0.f;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const float x = ex2_approx(raw(b, e, n, j, s.m[n][j]));
+            const float y = x * s.ref[n][j] * vscale(b, e, n, j);
+            p[b][n][2 * e + j] = x;
+            w[b][n][2 * e + j] = y;
+            top = fmax3(top, x, y);
+          }
+  };
+  weights();
+  if (__any_sync(0xffffffffu, top > 256.f)) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float mx = s.m[n][j];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) mx = fmaxf(mx, raw(b, e, n, j, 0.f));
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+        const float al = ex2_approx(s.m[n][j] - mx);
+        float big = exact_inverse(s.ref[n][j]) * al;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) big = fmaxf(big, ex2_approx(raw(b, e, n, j, mx)) * vscale(b, e, n, j));
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, off));
+        const int ex = min(max(__float_as_int(big) >> 23, 27), 227);
+        const float ref = __int_as_float((254 - ex) << 23);
+        const float move = al * (ref * exact_inverse(s.ref[n][j]));
+        s.m[n][j] = mx;
+        s.ref[n][j] = ref;
+        s.l[n][j] *= al;
+        s.z[n][j] *= al;
+        s.ones[n][j] *= move;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          s.o[n][i][j] *= move;
+          s.o[n][i][2 + j] *= move;
+        }
+      }
+    weights();
+  }
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    uint32_t pb[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          s.l[n][j] += p[b][n][2 * e + j];
+          s.z[n][j] = fmaf(p[b][n][2 * e + j], vmid(b, e, n, j), s.z[n][j]);
+        }
+        pb[n][e] = transpose_8x8(pack_f16(w[b][n][2 * e], w[b][n][2 * e + 1]));
+      }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) mma_f16_16816(s.ones[n], ONE, ONE, ONE, ONE, pb[n][0], pb[n][1]);
+    uint32_t va[W], vb[W];
+    const uint32_t v = stage + kKv4Unit * (D / 2) + (8 * b + 2 * c) * D + r * (D / 8);
+    lds_words<W>(va, v);
+    lds_words<W>(vb, v + D);
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const uint32_t x = hf ? va[i] >> 8 : va[i], y = hf ? vb[i] >> 8 : vb[i];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma_f16_16816(s.o[n][2 * i + hf], x & LO, x & HI, y & LO, y & HI, pb[n][0], pb[n][1]);
+      }
+  }
+}
+
+// Values of column (n, j), dimensions r D / 8 + 4 i + {0, 1, 2, 3}, i < D / 32.
+template <int D, int NT>
+__device__ __forceinline__ float4 kv4_value4(const Kv4Acc<D, NT>& s, int n, int j, int i, float z, float back) {
+  constexpr float F0 = 16777216.f, F1 = 1048576.f;  // 2^24 and 2^20: the place of the code in its operand
+  return make_float4(fmaf(s.o[n][2 * i][j], F0 * back, z), fmaf(s.o[n][2 * i][2 + j], F1 * back, z),
+                     fmaf(s.o[n][2 * i + 1][j], F0 * back, z), fmaf(s.o[n][2 * i + 1][2 + j], F1 * back, z));
+}
+__device__ __forceinline__ void kv4_store4(half_t* dst, float4 v) {
+  *reinterpret_cast<uint2*>(dst) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
+}
+// First output element of a column.
+template <int D>
+__device__ __forceinline__ half_t* kv4_out(const Kv4AttnArgs& a, int b, int hk, int col) {
+  const int i = col / a.group, h = hk * a.group + (col - i * a.group);
+  return a.out + ((static_cast<size_t>(b) * a.queries + i) * a.n_q + h) * D;
+}
+
+template <int D, int NT>
+__global__ void __launch_bounds__(kKv4Warps * 32, NT == 1 ? 2 : 1) kv4_attn_kernel(const Kv4AttnArgs a) {
+  constexpr int W = D / 32, NC = NT * 8, NS = kKv4Stages, STAGE = kv4_stage_bytes<D>();
+  constexpr int PART = kv4_partial_floats<D, NT>();
+  extern __shared__ __align__(128) uint8_t kv4_mem[];
+  __shared__ __align__(8) uint64_t bars[kKv4Warps][NS];
+  __shared__ long long warp_sums[kKv4Warps];
+  __shared__ long long part_pair[2 * kKv4Warps];   // first unit of an unfinished piece's pair, or -1; 2 w: head, 2 w + 1: tail
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
+  uint8_t* const mine = kv4_mem + warp * kv4_warp_bytes<D, NT>();
+  long long* pref = reinterpret_cast<long long*>(kv4_mem + kKv4Warps * kv4_warp_bytes<D, NT>());
+  if (lane == 0) {
+#pragma unroll
+    for (int i = 0; i < NS; ++i) mbar_init(&bars[warp][i], 1);
+    fence_barrier_init();
+    part_pair[2 * warp] = part_pair[2 * warp + 1] = -1;
+  }
+  kv4_prefix(a, pref, warp_sums);
+  const long long total = pref[a.batch], ctas = kv4_ctas(total, gridDim.x);
+  if (threadIdx.x == 0) a.splits[blockIdx.x].last = -1;
+  if (blockIdx.x >= ctas) return;
+  const long long c_beg = kv4_cta_first(total, ctas, blockIdx.x), c_end = kv4_cta_first(total, ctas, blockIdx.x + 1);
+  const long long w_beg = c_beg + warp * (c_end - c_beg) / kKv4Warps;
+  const int w_units = static_cast<int>(c_beg + (warp + 1) * (c_end - c_beg) / kKv4Warps - w_beg);
+  const uint32_t ring = smem_u32(mine);
+  const int shift = a.c.page_shift;
+
+  // ---- producer: walks the warp's units ahead of the consumer
+  int f_u = 0, f_end = 0;              // next unit to request and end of the segment it is in, from w_beg
+  int f_t = 0, f_len = 0, f_base = 0;  // its first token, the pair's length, table column of `ids`
+  const uint8_t* f_blocks = nullptr;   // pool + head offset
+  const int32_t* f_row = nullptr;
+  int ids = -1, ids_next = -1;         // page numbers of 32 table columns from f_base, and of the next 32
+  int filled = 0;
+  uint32_t bad_of = 0;                 // two bits for each ring stage
+  auto load_ids = [&](int base) {
+    const int col = base + lane;
+    return col < a.c.max_pages && (static_cast<long long>(col) << shift) < f_len ? __ldg(f_row + col) : -1;
+  };
+  auto request = [&]() {               // one stage, if there is one left
+    while (f_u < w_units) {
+      if (f_u >= f_end) {              // enter the next segment
+        const Kv4Place pl = kv4_place(a, pref, w_beg + f_u);
+        f_end = f_u + min(w_units - f_u, pl.units - pl.unit);
+        f_t = pl.unit * kKv4Unit;
+        f_len = pl.len;
+        f_blocks = a.c.pool + static_cast<size_t>(pl.pair_in_b / a.col_tiles) * a.c.block_bytes;
+        f_row = a.c.table + static_cast<size_t>(pl.b) * a.c.max_pages;
+        f_base = (f_t >> shift) & ~31;
+        ids = load_ids(f_base);
+        ids_next = load_ids(f_base + 32);
+      }
+      ++f_u;
+      const int t = f_t;
+      f_t += kKv4Unit;
+      if (t >= f_len) continue;        // the one unit of an empty row holds nothing
+      if ((t >> shift) - f_base >= 32) {
+        f_base += 32;
+        ids = ids_next;
+        ids_next = load_ids(f_base + 32);
+      }
+      const int slot = filled % NS;
+      uint64_t* bar = &bars[warp][slot];
+      const uint32_t dst = ring + slot * STAGE;
+      const int n = shift == 4 ? 2 : 1, part = kKv4Unit / n;   // pieces of a stage: two pages of 16 tokens, or one page
+      uint32_t bad = 0, bytes = 0;
+      int page[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        page[k] = __shfl_sync(0xffffffffu, ids, ((t >> shift) - f_base + k) & 31);
+        if (k < n && t + k * part < f_len) {
+          if (page[k] < 0 || page[k] >= a.c.n_pages) {
+            bad |= n == 2 ? 1u << k : 3u;
+            page[k] = -1;
+          } else {
+            bytes += part * (D + 8);
+          }
+        } else {
+          page[k] = -1;
+        }
+      }
+      bad_of = (bad_of & ~(3u << (2 * slot))) | bad << (2 * slot);
+      if (lane == 0) {
+        mbar_expect_tx(bar, bytes);    // arrives; with no byte to come the phase is complete
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          if (page[k] >= 0) {
+            const uint8_t* block = f_blocks + static_cast<size_t>(page[k]) * a.c.page_bytes;
+            const int P = 1 << shift, at = t & (P - 1), d0 = k * part;
+            bulk_load(dst + d0 * (D / 2), block + at * (D / 2), part * (D / 2), bar);
+            bulk_load(dst + kKv4Unit * (D / 2) + d0 * (D / 2), block + P * (D / 2) + at * (D / 2), part * (D / 2), bar);
+            bulk_load(dst + kKv4Unit * D + d0 * 4, block + P * D + at * 4, part * 4, bar);
+            bulk_load(dst + kKv4Unit * (D + 4) + d0 * 4, block + P * (D + 4) + at * 4, part * 4, bar);
+          }
+      }
+      ++filled;
+      return;
+    }
+  };
+  __syncwarp();                        // the barriers are initialised
+#pragma unroll
+  for (int i = 0; i < NS; ++i) request();
+
+  // ---- consumer
+  Kv4Acc<D, NT> s;
+  int taken = 0;
+  bool alive = true;                   // false once a wait has run out: everything left becomes NaN
+  for (int u = 0; u < w_units;) {
+    const Kv4Place pl = kv4_place(a, pref, w_beg + u);
+    const int n_units = min(w_units - u, pl.units - pl.unit);
+    const int hk = pl.pair_in_b / a.col_tiles, col0 = (pl.pair_in_b - hk * a.col_tiles) * NC;
+    s.reset();
+    kv4_load_queries<D, NT>(a, s, pl, hk, col0);
+    const int t_end = min(pl.len, (pl.unit + n_units) * kKv4Unit);
+    for (int t0 = pl.unit * kKv4Unit; t0 < t_end && alive; t0 += kKv4Unit) {
+      const int slot = taken % NS;
+      alive = __all_sync(0xffffffffu, mbar_wait(&bars[warp][slot], (taken / NS) & 1, nullptr));
+      if (!alive) {                    // wait once more for the copies in flight before their memory is used again
+        for (int k = taken; k < filled; ++k) mbar_wait(&bars[warp][k % NS], (k / NS) & 1, nullptr);
+        break;
+      }
+      const uint32_t bad = (bad_of >> (2 * slot)) & 3u;
+      const uint32_t stage = ring + slot * STAGE;
+      if (bad == 0 && t0 + kKv4Unit <= pl.len - (a.queries - 1)) kv4_stage<D, NT, false>(s, stage, t0, 0);
+      else kv4_stage<D, NT, true>(s, stage, t0, bad);
+      ++taken;
+      __syncwarp();                    // every lane has read the stage
+      request();
+    }
+    // ---- the segment's result: sums over the lanes that hold other tokens of the same columns
+    const bool head = pl.unit > 0, whole = !head && n_units == pl.units;
+    float* part = head ? reinterpret_cast<float*>(mine + NS * STAGE) : reinterpret_cast<float*>(mine);
+    if (!whole && lane == 0) part_pair[2 * warp + (head ? 0 : 1)] = pl.pair_first;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float l = alive ? s.l[n][j] : __int_as_float(0x7fffffff), z = s.z[n][j];
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) {
+          l += __shfl_xor_sync(0xffffffffu, l, off);
+          z += __shfl_xor_sync(0xffffffffu, z, off);
+        }
+        const float back = exact_inverse(s.ref[n][j]);
+        z = fmaf(-7.5f * back, s.ones[n][j], z);
+        const int col = 8 * n + 2 * c + j;
+        if (whole) {
+          if (col0 + col < a.cols) {
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            half_t* dst = kv4_out<D>(a, pl.b, hk, col0 + col) + r * (D / 8);
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+              const float4 v = kv4_value4<D, NT>(s, n, j, i, z, back);
+              kv4_store4(dst + 4 * i, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < W; ++i)
+            *reinterpret_cast<float4*>(part + col * D + r * (D / 8) + 4 * i) = kv4_value4<D, NT>(s, n, j, i, z, back);
+          if (r == 0) *reinterpret_cast<float2*>(part + NC * D + 2 * col) = make_float2(s.m[n][j], l);
+        }
+      }
+    u += n_units;
+  }
+  __syncthreads();
+
+  // ---- unfinished pieces: those of one pair are neighbours in the order head, tail of warp 0, of warp 1, ...
+  auto piece = [&](int k) {
+    return reinterpret_cast<const float*>(kv4_mem + (k >> 1) * kv4_warp_bytes<D, NT>() + ((k & 1) ? 0 : NS * STAGE));
+  };
+  for (int k = 0; k < 2 * kKv4Warps;) {
+    const long long pair = part_pair[k];
+    if (pair < 0) {
+      ++k;
+      continue;
+    }
+    int k1 = k + 1;
+    while (k1 < 2 * kKv4Warps && (part_pair[k1] < 0 || part_pair[k1] == pair)) ++k1;
+    const Kv4Place pl = kv4_place(a, pref, pair);
+    const int hk = pl.pair_in_b / a.col_tiles, col0 = (pl.pair_in_b - hk * a.col_tiles) * NC;
+    const bool done = pair >= c_beg && pair + pl.units <= c_end;
+    float* ws = a.parts + (static_cast<size_t>(blockIdx.x) * 2 + (pair < c_beg ? 0 : 1)) * PART;
+    for (int e = threadIdx.x; e < NC * D / 4; e += kKv4Warps * 32) {
+      const int col = e / (D / 4), d = (e - col * (D / 4)) * 4;
+      float top = kKv4Low;
+      for (int i = k; i < k1; ++i)
+        if (part_pair[i] >= 0) top = fmaxf(top, piece(i)[NC * D + 2 * col]);
+      float l = 0.f;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = k; i < k1; ++i)
+        if (part_pair[i] >= 0) {
+          const float* q = piece(i);
+          const float f = ex2_approx(q[NC * D + 2 * col] - top);
+          const float4 x = *reinterpret_cast<const float4*>(q + col * D + d);
+          l = fmaf(q[NC * D + 2 * col + 1], f, l);
+          v = make_float4(fmaf(x.x, f, v.x), fmaf(x.y, f, v.y), fmaf(x.z, f, v.z), fmaf(x.w, f, v.w));
+        }
+      if (done) {
+        if (col0 + col < a.cols) {
+          const float inv = l == 0.f ? 0.f : 1.f / l;
+          kv4_store4(kv4_out<D>(a, pl.b, hk, col0 + col) + d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+        }
+      } else {
+        *reinterpret_cast<float4*>(ws + col * D + d) = v;
+        if (d == 0) *reinterpret_cast<float2*>(ws + NC * D + 2 * col) = make_float2(top, l);
+      }
+    }
+    if (!done && pair >= c_beg && threadIdx.x == 0)
+      a.splits[blockIdx.x] = Kv4Split{pl.b, pl.pair_in_b, static_cast<int>(kv4_cta_of(total, ctas, pair + pl.units - 1)), 0};
+    k = k1;
+  }
+}
+
+// Merges the pieces of the pair that begins in CTA blockIdx.x of the kernel above and ends in a later one.  One CTA per
+// column; the warps take the pieces in turn.
+template <int D, int NT>
+__global__ void __launch_bounds__(256) kv4_attn_join_kernel(const Kv4AttnArgs a) {
+  constexpr int NC = NT * 8, PART = kv4_partial_floats<D, NT>(), V = D / 32;
+  __shared__ float sm[8], sl[8], so[8][D];
+  pdl_wait();
+  const int first = blockIdx.x, col = blockIdx.y;
+  const Kv4Split sp = a.splits[first];
+  if (sp.last < 0) return;
+  const int hk = sp.pair_in_b / a.col_tiles, out_col = (sp.pair_in_b - hk * a.col_tiles) * NC + col;
+  if (out_col >= a.cols) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto piece = [&](int i) { return a.parts + (static_cast<size_t>(i) * 2 + (i == first ? 1 : 0)) * PART; };
+  float m = kKv4Low, l = 0.f, o[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) o[e] = 0.f;
+#pragma unroll 4
+  for (int i = first + warp; i <= sp.last; i += 8) {
+    const float* q = piece(i);
+    const float2 ml = *reinterpret_cast<const float2*>(q + NC * D + 2 * col);
+    const float mn = fmaxf(m, ml.x), f0 = ex2_approx(m - mn), f1 = ex2_approx(ml.x - mn);
+    m = mn;
+    l = l * f0 + ml.y * f1;
+#pragma unroll
+    for (int e = 0; e < V; ++e) o[e] = o[e] * f0 + q[col * D + e * 32 + lane] * f1;
+  }
+  if (lane == 0) {
+    sm[warp] = m;
+    sl[warp] = l;
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) so[warp][e * 32 + lane] = o[e];
+  __syncthreads();
+  if (threadIdx.x < D) {
+    float top = kKv4Low, L = 0.f, O = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) top = fmaxf(top, sm[w]);
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      const float f = ex2_approx(sm[w] - top);
+      L += sl[w] * f;
+      O += so[w][threadIdx.x] * f;
+    }
+    kv4_out<D>(a, sp.b, hk, out_col)[threadIdx.x] = f_to_h(L == 0.f ? 0.f : O / L);
   }
 }
 

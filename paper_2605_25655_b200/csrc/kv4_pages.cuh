@@ -133,7 +133,7 @@ __device__ __forceinline__ PageMap map_pages(const PageTables& t, int* mem, int*
 // Rows in ascending order take the lowest free pages for `add` more tokens each; a row whose pages, with those of the
 // rows before it, do not fit the pool or its table keeps its length and is counted in *refused.
 __global__ void __launch_bounds__(kPlanThreads) kv4_reserve_kernel(const PageTables t, int32_t* table, const int32_t* add,
-                                                                   int32_t* lens_out, int32_t* refused) {
+                                                                   int32_t* lens_out, int64_t* refused) {
   extern __shared__ int plan_mem[];
   __shared__ int buf[33];
   __shared__ int wanted, bad;
@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_reserve_kernel(const PageTab
 
 // ---------------------------------------------------------------- fork
 __global__ void __launch_bounds__(kPlanThreads) kv4_fork_kernel(const PageTables t, const int32_t* source, int32_t* table_out,
-                                                                int32_t* lens_out, int32_t* refused, int* move_count,
+                                                                int32_t* lens_out, int64_t* refused, int* move_count,
                                                                 PageMove* moves) {
   extern __shared__ int plan_mem[];
   __shared__ int buf[33];
@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_fork_kernel(const PageTables
 
 // ---------------------------------------------------------------- compact
 // Live pages with a number >= the number of live pages move, in ascending order, into the free pages below it.
-__global__ void __launch_bounds__(kPlanThreads) kv4_compact_kernel(const PageTables t, int32_t* table_out, int32_t* live_out,
+__global__ void __launch_bounds__(kPlanThreads) kv4_compact_kernel(const PageTables t, int32_t* table_out, int64_t* live_out,
                                                                    int* move_count, PageMove* moves) {
   extern __shared__ int plan_mem[];
   __shared__ int buf[33];

@@ -397,54 +397,75 @@ def op_argmax(logits, stream=None):
 
 
 # ------------------------------------- per-head norm + rotation, 4-bit paged cache
-class _On:
-    """Checks that tensors live on one CUDA device and makes it the current one for the call; hands out its stream."""
+# These run once per layer and decode step, so their Python side is kept to plain comparisons: no helper objects, no
+# library query for what a few multiplications give.
+class _on:
+    """Makes the tensors' CUDA device the current one for a call that finds another one current."""
 
-    def __init__(self, device, stream=None):
+    def __init__(self, device):
         import torch
-        if device.type != "cuda":
-            raise ThinferError(EINVAL, f"tensors must be on a CUDA device, not {device}")
-        self.device, self.torch = device, torch
-        if stream is not None and stream.device != device:
-            raise ThinferError(EINVAL, f"the stream belongs to {stream.device}, the tensors to {device}")
-        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-        self.stream = stream
+        self.guard = torch.cuda.device(device)
 
     def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        s = self.stream if self.stream is not None else self.torch.cuda.current_stream(self.device)
-        return s.cuda_stream
+        self.guard.__enter__()
 
     def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+        self.guard.__exit__(*exc)
 
 
-def _want(ok, what):
-    if not ok:
-        raise ThinferError(EINVAL, what)
+class _nothing:
+    def __enter__(self):
+        pass
+
+    def __exit__(self, *exc):
+        pass
 
 
-def _want_int32(device, **tensors):
-    import torch
-    for name, (t, shape) in tensors.items():
-        _want(t.dtype == torch.int32 and t.device == device and t.is_contiguous() and tuple(t.shape) == tuple(shape),
-              f"{name}: a contiguous int32 tensor of shape {tuple(shape)} on {device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+_nothing = _nothing()
 
 
-def _token_stride(t, name, dtype, device):
+def _bad(what):
+    raise ThinferError(EINVAL, what)
+
+
+def _enter(device, stream):
+    """(guard, raw stream) of a call whose tensors live on `device`: the given stream, or the device's current one."""
+    from torch._C import _cuda_getCurrentRawStream, _cuda_getDevice
+    if device.type != "cuda":
+        _bad(f"tensors must be on a CUDA device, not {device}")
+    if stream is None:
+        raw = _cuda_getCurrentRawStream(device.index)
+    else:
+        if stream.device != device:
+            _bad(f"the stream belongs to {stream.device}, the tensors to {device}")
+        raw = stream.cuda_stream
+    return (_nothing if _cuda_getDevice() == device.index else _on(device)), raw
+
+
+def _ints(t, name, device, shape, dtype=None):
+    """Address of a contiguous int32 (or `dtype`) tensor of the given shape."""
+    if dtype is None:
+        from torch import int32 as dtype
+    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        _bad(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _token_stride(t, name, dtype, device, shape=None):
     """Elements between the tokens of [tokens, heads, head_dim], whose heads lie side by side."""
-    _want(t.dim() == 3 and t.dtype == dtype and t.device == device, f"{name}: [tokens, heads, head_dim] {dtype} on {device}")
+    if t.dim() != 3 or t.dtype is not dtype or t.device != device or (shape is not None and t.shape != shape):
+        _bad(f"{name}: a {dtype} tensor [tokens, heads, head_dim] on {device}" + (f" of shape {tuple(shape)}" if shape is not None else ""))
     n, h, d = t.shape
-    _want(n > 0 and h > 0 and t.stride(2) == 1 and (h == 1 or t.stride(1) == d), f"{name}: the heads of a token must be contiguous")
-    return t.stride(0) if n > 1 else -(-max(t.stride(0), h * d) // 8) * 8
+    s0, s1, s2 = t.stride()
+    if n == 0 or h == 0 or s2 != 1 or (h != 1 and s1 != d):
+        _bad(f"{name}: the heads of a token must be contiguous, and there must be some")
+    return s0 if n > 1 else h * d
 
 
 def rope_turns(base, rotary_dim, device="cuda:0"):
     """FP64 [rotary_dim / 2]: revolutions per position of each rotated pair, base^(-2j/rotary_dim) / (2 pi)."""
     import torch
-    buf = (C.c_double * (rotary_dim // 2))()
+    buf = (C.c_double * max(rotary_dim // 2, 1))()
     _check(lib().thinfer_rope_turns(base, rotary_dim, buf))
     return torch.tensor(list(buf), dtype=torch.float64, device=device)
 
@@ -454,24 +475,29 @@ def op_qk_norm_rope(q, k, q_gain, k_gain, eps, turns, positions, halves=False, q
     come, e.g. slices of a fused projection output); turns from rope_turns (its length sets the rotated dimensions);
     positions int32 [tokens], negative: left as they were.  Returns (q_out, k_out); they may be q and k themselves."""
     import torch
-    dev = q.device
-    with _On(dev, stream) as st:
-        n, hq, d = q.shape if q.dim() == 3 else (0, 0, 0)
-        qs, ks = _token_stride(q, "q", q.dtype, dev), _token_stride(k, "k", q.dtype, dev)
-        hkv = k.shape[1]
-        _want(k.shape[0] == n and k.shape[2] == d, "q and k must agree in tokens and head_dim")
-        for name, g in (("q_gain", q_gain), ("k_gain", k_gain)):
-            _want(g.dtype == q.dtype and g.device == dev and g.is_contiguous() and tuple(g.shape) == (d,), f"{name}: [head_dim] {q.dtype} on {dev}")
-        _want(turns.dtype == torch.float64 and turns.device == dev and turns.is_contiguous() and turns.dim() == 1, "turns: FP64 [rotary_dim / 2]")
-        _want_int32(dev, positions=(positions, (n,)))
-        q_out = torch.empty(n, hq, d, dtype=q.dtype, device=dev) if q_out is None else q_out
-        k_out = torch.empty(n, hkv, d, dtype=q.dtype, device=dev) if k_out is None else k_out
-        _want(tuple(q_out.shape) == (n, hq, d) and tuple(k_out.shape) == (n, hkv, d), "q_out / k_out: the shapes of q / k")
-        qos, kos = _token_stride(q_out, "q_out", q.dtype, dev), _token_stride(k_out, "k_out", q.dtype, dev)
-        s = storage_of(q)
-        _check(lib(s).thinfer_op_qk_norm_rope(q.data_ptr(), qs, k.data_ptr(), ks, q_out.data_ptr(), qos, k_out.data_ptr(), kos,
-                                              q_gain.data_ptr(), k_gain.data_ptr(), turns.data_ptr(), positions.data_ptr(), n, hq,
-                                              hkv, d, 2 * turns.shape[0], int(halves), eps, st), None, s)
+    dev, dt = q.device, q.dtype
+    guard, st = _enter(dev, stream)
+    qs, ks = _token_stride(q, "q", dt, dev), _token_stride(k, "k", dt, dev)
+    n, hq, d = q.shape
+    hkv = k.shape[1]
+    if k.shape[0] != n or k.shape[2] != d:
+        _bad("q and k must agree in tokens and head_dim")
+    if q_out is None:
+        q_out, qos = torch.empty((n, hq, d), dtype=dt, device=dev), hq * d
+    else:
+        qos = _token_stride(q_out, "q_out", dt, dev, q.shape)
+    if k_out is None:
+        k_out, kos = torch.empty((n, hkv, d), dtype=dt, device=dev), hkv * d
+    else:
+        kos = _token_stride(k_out, "k_out", dt, dev, k.shape)
+    if turns.dim() != 1:
+        _bad("turns: FP64 [rotary_dim / 2]")
+    s = storage_of(q)
+    with guard:
+        _check(lib(s).thinfer_op_qk_norm_rope(
+            q.data_ptr(), qs, k.data_ptr(), ks, q_out.data_ptr(), qos, k_out.data_ptr(), kos, _ints(q_gain, "q_gain", dev, (d,), dt),
+            _ints(k_gain, "k_gain", dev, (d,), dt), _ints(turns, "turns", dev, turns.shape, torch.float64),
+            _ints(positions, "positions", dev, (n,)), n, hq, hkv, d, 2 * turns.shape[0], int(halves), eps, st), None, s)
     return q_out, k_out
 
 
@@ -482,28 +508,40 @@ def kv4_page_bytes(n_kv_heads, head_dim, page_size):
     return n.value
 
 
-def _pool(pool, dims, page_size, head_dim):
+def _pool(pool, dims, page_size, head_dim, device):
     """Number of KV heads of a uint8 pool tensor whose last dimension is a page."""
     import torch
-    _want(pool.dtype == torch.uint8 and pool.dim() == dims and pool.is_contiguous(), f"pool: a contiguous uint8 tensor of {dims} dimensions")
-    per = kv4_page_bytes(1, head_dim, page_size)
-    _want(pool.shape[-1] > 0 and pool.shape[-1] % per == 0, f"pool: a page has a multiple of {per} bytes, not {pool.shape[-1]}")
-    return pool.shape[-1] // per
+    if pool.dtype is not torch.uint8 or pool.dim() != dims or not pool.is_contiguous() or pool.device != device:
+        _bad(f"pool: a contiguous uint8 tensor of {dims} dimensions on {device}")
+    per = page_size * (head_dim + 8)
+    heads = pool.shape[-1] // per if per > 0 else 0
+    if heads == 0 or heads * per != pool.shape[-1]:
+        _bad(f"pool: a page has a multiple of {per} bytes, not {pool.shape[-1]}")
+    return heads
+
+
+def _table(table, device):
+    if table.dim() != 2:
+        _bad("table: int32 [rows, max_pages]")
+    return _ints(table, "table", device, table.shape)
 
 
 def op_kv4_reserve(table, lens, add, n_pages, page_size, lens_out=None, refused=None, stream=None):
     """Room for add[r] more tokens of every row: writes page numbers into table (int32 [rows, max_pages]); returns
-    (lens_out, refused): the new lengths and how many rows did not fit (they keep their length)."""
+    (lens_out, refused): the new lengths (may be lens itself) and, int64 [1], how many rows did not fit and keep theirs."""
     import torch
     dev = table.device
-    with _On(dev, stream) as st:
-        rows, max_pages = table.shape
-        lens_out = torch.empty_like(lens) if lens_out is None else lens_out
-        refused = torch.empty(1, dtype=torch.int32, device=dev) if refused is None else refused
-        _want_int32(dev, table=(table, (rows, max_pages)), lens=(lens, (rows,)), add=(add, (rows,)), lens_out=(lens_out, (rows,)),
-                    refused=(refused, (1,)))
-        _check(lib().thinfer_op_kv4_reserve(table.data_ptr(), lens.data_ptr(), add.data_ptr(), lens_out.data_ptr(), refused.data_ptr(),
-                                            rows, max_pages, n_pages, page_size, st))
+    guard, st = _enter(dev, stream)
+    tab = _table(table, dev)
+    rows, max_pages = table.shape
+    if lens_out is None:
+        lens_out = torch.empty(rows, dtype=torch.int32, device=dev)
+    if refused is None:
+        refused = torch.empty(1, dtype=torch.int64, device=dev)
+    with guard:
+        _check(lib().thinfer_op_kv4_reserve(
+            tab, _ints(lens, "lens", dev, (rows,)), _ints(add, "add", dev, (rows,)), _ints(lens_out, "lens_out", dev, (rows,)),
+            _ints(refused, "refused", dev, (1,), torch.int64), rows, max_pages, n_pages, page_size, st))
     return lens_out, refused
 
 
@@ -511,17 +549,16 @@ def op_kv4_append(pool, table, k, v, rows, positions, page_size, stream=None):
     """Quantises k, v [tokens, n_kv_heads, d] into one layer's pool [n_pages, page bytes]: token i goes to position
     positions[i] of table row rows[i] (int32 [tokens]; negative: skipped)."""
     dev = pool.device
-    with _On(dev, stream) as st:
-        ks, vs = _token_stride(k, "k", k.dtype, dev), _token_stride(v, "v", k.dtype, dev)
-        n, hkv, d = k.shape
-        _want(tuple(v.shape) == (n, hkv, d), "k and v must have one shape")
-        _want(_pool(pool, 2, page_size, d) == hkv, "the pool's pages are for another number of heads")
-        _want_int32(dev, table=(table, table.shape), rows=(rows, (n,)), positions=(positions, (n,)))
-        _want(table.dim() == 2, "table: [rows, max_pages]")
-        s = storage_of(k)
-        _check(lib(s).thinfer_op_kv4_append(pool.data_ptr(), pool.shape[0], table.data_ptr(), table.shape[0], table.shape[1],
-                                            k.data_ptr(), ks, v.data_ptr(), vs, rows.data_ptr(), positions.data_ptr(), n, hkv, d,
-                                            page_size, st), None, s)
+    guard, st = _enter(dev, stream)
+    ks, vs = _token_stride(k, "k", k.dtype, dev), _token_stride(v, "v", k.dtype, dev, k.shape)
+    n, hkv, d = k.shape
+    if _pool(pool, 2, page_size, d, dev) != hkv:
+        _bad("the pool's pages are for another number of heads")
+    s = storage_of(k)
+    with guard:
+        _check(lib(s).thinfer_op_kv4_append(
+            pool.data_ptr(), pool.shape[0], _table(table, dev), table.shape[0], table.shape[1], k.data_ptr(), ks, v.data_ptr(), vs,
+            _ints(rows, "rows", dev, (n,)), _ints(positions, "positions", dev, (n,)), n, hkv, d, page_size, st), None, s)
 
 
 def op_kv4_read(pool, table, rows, positions, page_size, head_dim, dtype, k_out=None, v_out=None, stream=None):
@@ -529,96 +566,130 @@ def op_kv4_read(pool, table, rows, positions, page_size, head_dim, dtype, k_out=
     pool was written with).  k_out / v_out: two tensors of that shape with equal strides (e.g. transposed views)."""
     import torch
     dev = pool.device
-    with _On(dev, stream) as st:
-        hkv = _pool(pool, 2, page_size, head_dim)
-        n = positions.shape[0]
-        k_out = torch.empty(n, hkv, head_dim, dtype=dtype, device=dev) if k_out is None else k_out
-        v_out = torch.empty(n, hkv, head_dim, dtype=dtype, device=dev) if v_out is None else v_out
-        for t in (k_out, v_out):
-            _want(tuple(t.shape) == (n, hkv, head_dim) and t.dtype == dtype and t.device == dev and t.stride(2) == 1 and
-                  t.stride() == k_out.stride(), "k_out, v_out: [tokens, heads, head_dim], equal strides")
-        _want(table.dim() == 2, "table: [rows, max_pages]")
-        _want_int32(dev, table=(table, table.shape), rows=(rows, (n,)), positions=(positions, (n,)))
-        s = storage_of(k_out)
-        _check(lib(s).thinfer_op_kv4_read(pool.data_ptr(), pool.shape[0], table.data_ptr(), table.shape[0], table.shape[1],
-                                          k_out.data_ptr(), v_out.data_ptr(), k_out.stride(0), k_out.stride(1), rows.data_ptr(),
-                                          positions.data_ptr(), n, hkv, head_dim, page_size, st), None, s)
+    guard, st = _enter(dev, stream)
+    hkv = _pool(pool, 2, page_size, head_dim, dev)
+    n = positions.numel()
+    shape = (n, hkv, head_dim)
+    if k_out is None:
+        k_out = torch.empty(shape, dtype=dtype, device=dev)
+    if v_out is None:
+        v_out = torch.empty_strided(shape, k_out.stride(), dtype=dtype, device=dev)
+    strides = k_out.stride()
+    for t in (k_out, v_out):
+        if t.shape != shape or t.dtype is not dtype or t.device != dev or t.stride() != strides:
+            _bad("k_out, v_out: [tokens, heads, head_dim] of one type, device and strides")
+    if strides[2] != 1:
+        _bad("k_out, v_out: the values of a head must be contiguous")
+    s = storage_of(k_out)
+    with guard:
+        _check(lib(s).thinfer_op_kv4_read(
+            pool.data_ptr(), pool.shape[0], _table(table, dev), table.shape[0], table.shape[1], k_out.data_ptr(), v_out.data_ptr(),
+            strides[0], strides[1], _ints(rows, "rows", dev, (n,)), _ints(positions, "positions", dev, (n,)), n, hkv, head_dim,
+            page_size, st), None, s)
     return k_out, v_out
+
+
+_workspaces = {}   # sizes -> bytes: what the library answered for them
 
 
 def op_kv4_attention(q, pool, table, lens, page_size, out=None, workspace=None, stream=None):
     """q [batch, queries, n_q_heads, d] (already rotated) over one layer's 4-bit pool [n_pages, page bytes]: request b is
-    row b of table and holds lens[b] keys, the query tokens the last among them.  Returns [batch, queries, n_q_heads, d]."""
+    row b of table and holds lens[b] keys, the query tokens the last among them.  Returns [batch, queries, n_q_heads, d].
+    workspace: uint8, at least thinfer_kv4_attention_workspace bytes (default: allocated for the call)."""
     import torch
-    dev = q.device
-    with _On(dev, stream) as st:
-        _want(q.dim() == 4, "q: [batch, queries, n_q_heads, head_dim]")
-        b, n, hq, d = q.shape
-        _want(b == 1 or n == 1 or q.stride(0) == n * q.stride(1), "q: the query tokens must be evenly spaced")
-        flat = q.reshape(b * n, hq, d) if n == 1 or q.is_contiguous() else q.view(b * n, hq, d)
-        qs = _token_stride(flat, "q", q.dtype, dev)
-        hkv = _pool(pool, 2, page_size, d)
-        _want(pool.device == dev, f"pool: on {dev}")
-        _want(table.dim() == 2, "table: [batch, max_pages]")
-        _want_int32(dev, table=(table, (b, table.shape[1])), lens=(lens, (b,)))
-        out = torch.empty(b, n, hq, d, dtype=q.dtype, device=dev) if out is None else out
-        _want(tuple(out.shape) == (b, n, hq, d) and out.dtype == q.dtype and out.device == dev and out.is_contiguous(), "out: contiguous, the shape of q")
-        s = storage_of(q)
-        L = lib(s)
+    dev, dt = q.device, q.dtype
+    guard, st = _enter(dev, stream)
+    if q.dim() != 4:
+        _bad("q: [batch, queries, n_q_heads, head_dim]")
+    b, n, hq, d = q.shape
+    s0, s1, s2, s3 = q.stride()
+    if b * n * hq == 0 or s3 != 1 or (hq != 1 and s2 != d) or (n > 1 and b > 1 and s0 != n * s1):
+        _bad("q: the heads of a token must be contiguous and the query tokens evenly spaced")
+    qs = s1 if n > 1 else s0 if b > 1 else hq * d
+    hkv = _pool(pool, 2, page_size, d, dev)
+    if out is None:
+        out = torch.empty((b, n, hq, d), dtype=dt, device=dev)
+    s = storage_of(q)
+    L = lib(s)
+    with guard:
         if workspace is None:
-            need = C.c_size_t(0)
-            _check(L.thinfer_kv4_attention_workspace(b, n, hq, hkv, d, C.byref(need)), None, s)
-            workspace = torch.empty(need.value, dtype=torch.uint8, device=dev)
-        _check(L.thinfer_op_kv4_attention(flat.data_ptr(), qs, pool.data_ptr(), pool.shape[0], table.data_ptr(), table.shape[1],
-                                          lens.data_ptr(), out.data_ptr(), b, n, hq, hkv, d, page_size, workspace.data_ptr(),
-                                          workspace.numel() * workspace.element_size(), st), None, s)
+            key = (dev.index, b, n, hq, hkv, d)
+            need = _workspaces.get(key)
+            if need is None:
+                size = C.c_size_t(0)
+                _check(L.thinfer_kv4_attention_workspace(b, n, hq, hkv, d, C.byref(size)), None, s)
+                need = size.value
+                if len(_workspaces) >= 4096:
+                    _workspaces.clear()
+                _workspaces[key] = need
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        elif workspace.dtype is not torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
+            _bad(f"workspace: a contiguous uint8 tensor on {dev}")
+        _check(L.thinfer_op_kv4_attention(
+            q.data_ptr(), qs, pool.data_ptr(), pool.shape[0], _table(table, dev) if table.shape[0] == b else _bad("table: one row per request"),
+            table.shape[1], _ints(lens, "lens", dev, (b,)), _ints(out, "out", dev, (b, n, hq, d), dt), b, n, hq, hkv, d, page_size,
+            workspace.data_ptr(), workspace.numel(), st), None, s)
     return out
 
 
 def _pages_workspace(rows, n_pages, device):
     import torch
-    need = C.c_size_t(0)
-    _check(lib().thinfer_kv4_pages_workspace(rows, n_pages, C.byref(need)))
-    return torch.empty(need.value, dtype=torch.uint8, device=device)
+    key = (rows, n_pages)
+    need = _workspaces.get(key)
+    if need is None:
+        size = C.c_size_t(0)
+        _check(lib().thinfer_kv4_pages_workspace(rows, n_pages, C.byref(size)))
+        need = size.value
+        if len(_workspaces) >= 4096:
+            _workspaces.clear()
+        _workspaces[key] = need
+    return torch.empty(need, dtype=torch.uint8, device=device)
 
 
 def op_kv4_fork(pool, table, lens, source, page_size, head_dim, table_out=None, lens_out=None, refused=None, stream=None):
     """New row r takes over old row source[r] (negative: freed) of a pool [n_layers, n_pages, page bytes]: full pages are
-    shared, a partly filled last page is copied for every heir but one.  Returns (table_out, lens_out, refused)."""
+    shared, a partly filled last page is copied for every heir but one.  Returns (table_out, lens_out, refused), the last
+    int64 [1]."""
     import torch
     dev = pool.device
-    with _On(dev, stream) as st:
-        hkv = _pool(pool, 3, page_size, head_dim)
-        _want(table.dim() == 2, "table: [rows, max_pages]")
-        rows, max_pages = table.shape
-        table_out = torch.empty_like(table) if table_out is None else table_out
-        lens_out = torch.empty_like(lens) if lens_out is None else lens_out
-        refused = torch.empty(1, dtype=torch.int32, device=dev) if refused is None else refused
-        _want_int32(dev, table=(table, (rows, max_pages)), lens=(lens, (rows,)), source=(source, (rows,)),
-                    table_out=(table_out, (rows, max_pages)), lens_out=(lens_out, (rows,)), refused=(refused, (1,)))
-        ws = _pages_workspace(rows, pool.shape[1], dev)
-        _check(lib().thinfer_op_kv4_fork(pool.data_ptr(), pool.shape[0], pool.shape[1], table.data_ptr(), lens.data_ptr(),
-                                         source.data_ptr(), table_out.data_ptr(), lens_out.data_ptr(), refused.data_ptr(), rows,
-                                         max_pages, hkv, head_dim, page_size, ws.data_ptr(), ws.numel(), st))
+    guard, st = _enter(dev, stream)
+    hkv = _pool(pool, 3, page_size, head_dim, dev)
+    tab = _table(table, dev)
+    rows, max_pages = table.shape
+    if table_out is None:
+        table_out = torch.empty((rows, max_pages), dtype=torch.int32, device=dev)
+    if lens_out is None:
+        lens_out = torch.empty(rows, dtype=torch.int32, device=dev)
+    if refused is None:
+        refused = torch.empty(1, dtype=torch.int64, device=dev)
+    ws = _pages_workspace(rows, pool.shape[1], dev)
+    with guard:
+        _check(lib().thinfer_op_kv4_fork(
+            pool.data_ptr(), pool.shape[0], pool.shape[1], tab, _ints(lens, "lens", dev, (rows,)), _ints(source, "source", dev, (rows,)),
+            _ints(table_out, "table_out", dev, (rows, max_pages)), _ints(lens_out, "lens_out", dev, (rows,)),
+            _ints(refused, "refused", dev, (1,), torch.int64), rows, max_pages, hkv, head_dim, page_size, ws.data_ptr(), ws.numel(), st))
     return table_out, lens_out, refused
 
 
 def op_kv4_compact(pool, table, lens, page_size, head_dim, table_out=None, live=None, stream=None):
     """Moves the pages in use of a pool [n_layers, n_pages, page bytes] to its front.  Returns (table_out, live): the table
-    with the new page numbers and the number of pages in use."""
+    with the new page numbers and, int64 [1], the number of pages in use."""
     import torch
     dev = pool.device
-    with _On(dev, stream) as st:
-        hkv = _pool(pool, 3, page_size, head_dim)
-        _want(table.dim() == 2, "table: [rows, max_pages]")
-        rows, max_pages = table.shape
-        table_out = torch.empty_like(table) if table_out is None else table_out
-        live = torch.empty(1, dtype=torch.int32, device=dev) if live is None else live
-        _want_int32(dev, table=(table, (rows, max_pages)), lens=(lens, (rows,)), table_out=(table_out, (rows, max_pages)), live=(live, (1,)))
-        ws = _pages_workspace(rows, pool.shape[1], dev)
-        _check(lib().thinfer_op_kv4_compact(pool.data_ptr(), pool.shape[0], pool.shape[1], table.data_ptr(), lens.data_ptr(),
-                                            table_out.data_ptr(), live.data_ptr(), rows, max_pages, hkv, head_dim, page_size,
-                                            ws.data_ptr(), ws.numel(), st))
+    guard, st = _enter(dev, stream)
+    hkv = _pool(pool, 3, page_size, head_dim, dev)
+    tab = _table(table, dev)
+    rows, max_pages = table.shape
+    if table_out is None:
+        table_out = torch.empty((rows, max_pages), dtype=torch.int32, device=dev)
+    if live is None:
+        live = torch.empty(1, dtype=torch.int64, device=dev)
+    ws = _pages_workspace(rows, pool.shape[1], dev)
+    with guard:
+        _check(lib().thinfer_op_kv4_compact(
+            pool.data_ptr(), pool.shape[0], pool.shape[1], tab, _ints(lens, "lens", dev, (rows,)),
+            _ints(table_out, "table_out", dev, (rows, max_pages)), _ints(live, "live", dev, (1,), torch.int64), rows, max_pages, hkv,
+            head_dim, page_size, ws.data_ptr(), ws.numel(), st))
     return table_out, live
 
 

@@ -240,6 +240,11 @@ def _filled(T, rng, t, hkv, d, page, lens, extra=3, k_std=1.0, v_std=1.0, spread
     return pool, tab, table
 
 
+def kv4_abs(kv, q, n, shift):
+    """sum_t p_t |v_t| of every head."""
+    return kv4.attention(q, (kv[0], np.abs(kv[1])), n, shift)[0]
+
+
 def _check_attention(T, rng, t, hq, hkv, d, page, lens, queries, pool, tab, table, q_std=1.0, strided=False, lens_dev=None):
     torch, thinfer = T
     b = len(lens)
@@ -259,10 +264,16 @@ def _check_attention(T, rng, t, hq, hkv, d, page, lens, queries, pool, tab, tabl
         kv = kv4.keys_values(ref, table[i], lens[i])
         for n in range(queries):
             want, spread, mag = kv4.attention(q[i, n], kv, lens[i], queries - 1 - n)
-            # weights rounded to 11 bits before the product with V: 2^-11 of sum p |v|; scores in FP32 from exact products,
-            # offset part and code part separately: an error of 2^-20 of the largest sum |q k| / sqrt(d), in the exponent
-            # of numerator and denominator
-            tol = EPS[t] * np.abs(want) + (2.0 ** -11 + 2.0 ** -19 * (1 + 16 * mag)) * spread + 2.0 ** -25
+            # v = mid + scale (code - 7.5) with mid = offset + 7.5 scale: sum p mid is FP32, and the weights p scale of the
+            # second part are rounded to 11 bits, so that each rounding moves the result by at most
+            # 2^-11 p scale |code - 7.5| = 2^-11 p |v - mid|.  mid is the middle of the row's range, or half a step from
+            # it where no code is 15 (then 14 is the largest): |v - mid| <= |v - middle| + range / 28 = a term of `spread`.
+            # Scores in FP32 from exact products: the code part sums terms of up to 15 steps of a row, about four times |k|,
+            # in eight accumulation steps of 2^-22: 8 * 4 * 2^-22 = 2^-17 of the largest sum |q k| / sqrt(d) in the exponent
+            # of numerator and denominator, 2^-16 in all (2^-15 with the offset part), times the distance of a key's value
+            # from the result, at most spread + |want| + sum p |v|
+            far = spread + np.abs(want) + kv4_abs(kv, q[i, n], lens[i], queries - 1 - n)
+            tol = EPS[t] * np.abs(want) + 2.0 ** -11 * spread + 2.0 ** -19 * (1 + 16 * mag) * far + 2.0 ** -25
             bad = np.abs(got[i, n] - want) > tol
             assert not bad.any(), (i, n, lens[i], np.argwhere(bad)[:3], np.max(np.abs(got[i, n] - want) / tol))
 
@@ -309,8 +320,11 @@ def test_attention_over_many_and_long_rows(T, batch, n):
         s = torch.einsum("hgd,thd->hgt", q[i, 0].double().view(hkv, 4, d), kk) / 8.0
         p = torch.softmax(s, -1)
         want = torch.einsum("hgt,thd->hgd", p, vv).reshape(hq, d)
-        spread = torch.einsum("hgt,thd->hgd", p, vv.abs()).reshape(hq, d)
-        tol = EPS["f16"] * want.abs() + (2.0 ** -11 + 2.0 ** -13) * spread + 2.0 ** -25      # as above with |q k| / sqrt(d) < 4
+        low, high = vv.amin(-1, keepdim=True), vv.amax(-1, keepdim=True)
+        spread = torch.einsum("hgt,thd->hgd", p, (vv - (low + high) / 2).abs() + (high - low) / 28).reshape(hq, d)
+        mag = torch.einsum("hgd,thd->hgt", q[i, 0].double().view(hkv, 4, d).abs(), kk.abs()).amax(-1).reshape(hq, 1) / 8.0      # as above
+        far = spread + want.abs() + torch.einsum("hgt,thd->hgd", p, vv.abs()).reshape(hq, d)
+        tol = EPS["f16"] * want.abs() + 2.0 ** -11 * spread + 2.0 ** -19 * (1 + 16 * mag) * far + 2.0 ** -25
         assert torch.all((got[i, 0] - want).abs() <= tol)
         del pos
 
@@ -514,7 +528,7 @@ def test_a_run_of_them_together(T, t):
     fresh = torch.zeros(layers, rows, (hq + 2 * hkv) * d, dtype=tt, device="cuda")
     outs, qs = torch.zeros(layers, rows, 1, hq, d, dtype=tt, device="cuda"), torch.zeros(layers, rows, hq, d, dtype=tt, device="cuda")
     ks = torch.zeros(layers, rows, hkv, d, dtype=tt, device="cuda")
-    bad = torch.zeros(1, dtype=torch.int32, device="cuda")
+    bad = torch.zeros(1, dtype=torch.int64, device="cuda")
 
     def step():
         at = lens.clone()

@@ -180,7 +180,7 @@ def test_page_table_calls_refuse(lib):
     args = dict(t=T, l=L, a=A, lo=LO, r=R, rows=4, maxp=8, n_pages=32, page=16, st=None)
     _refusals(lib.thinfer_op_kv4_reserve, args, [
         *(({n: None}, E) for n in "tla"), ({"lo": None}, E), ({"r": None}, E), ({"rows": 0}, E), ({"maxp": 0}, E), ({"n_pages": -1}, E), ({"page": 17}, U),
-        ({"rows": 4097}, U), ({"n_pages": (1 << 18) + 1}, U), ({"lo": L + 4}, E), ({"lo": A}, E), ({"r": L}, E), ({"r": LO + 4}, E), ({"l": L + 2}, E)])
+        ({"rows": 4097}, U), ({"n_pages": (1 << 18) + 1}, U), ({"lo": L + 4}, E), ({"lo": A}, E), ({"r": L}, E), ({"r": LO + 8}, E), ({"l": L + 2}, E)])
     need = C.c_size_t(0)
     assert lib.thinfer_kv4_pages_workspace(4, 32, C.byref(need)) == thinfer.OK and need.value >= 16 + 16 * 12
     assert lib.thinfer_kv4_pages_workspace(0, 32, C.byref(need)) == E and lib.thinfer_kv4_pages_workspace(4, 1 << 20, C.byref(need)) == U
@@ -188,7 +188,7 @@ def test_page_table_calls_refuse(lib):
     args = dict(pool=P, layers=2, n_pages=32, t=T, l=L, s=S, to=TO, lo=LO, r=R, rows=4, maxp=8, hkv=2, d=64, page=16, ws=P, wb=1 << 12, st=None)
     _refusals(lib.thinfer_op_kv4_fork, args, [
         *(({n: None}, E) for n in ("pool", "t", "l", "s", "to", "lo", "r", "ws")), ({"layers": 0}, E), ({"rows": 4097}, U), ({"to": T}, E), ({"to": T + 64}, E),
-        ({"lo": L}, E), ({"lo": S}, E), ({"r": LO}, E), ({"r": TO + 4}, E), ({"wb": 32}, thinfer.ECAPACITY), ({"d": 72}, U)])
+        ({"lo": L}, E), ({"lo": S}, E), ({"r": LO}, E), ({"r": TO + 8}, E), ({"r": R + 4}, E), ({"wb": 32}, thinfer.ECAPACITY), ({"d": 72}, U)])
     args = dict(pool=P, layers=2, n_pages=32, t=T, l=L, to=TO, live=R, rows=4, maxp=8, hkv=2, d=64, page=16, ws=P, wb=1 << 12, st=None)
     _refusals(lib.thinfer_op_kv4_compact, args, [
         *(({n: None}, E) for n in ("pool", "t", "l", "to", "live", "ws")), ({"layers": -1}, E), ({"to": T}, E), ({"live": L}, E), ({"live": TO}, E),
