@@ -90,7 +90,7 @@ int copy_pages(void* pool, const int* count, const PageMove* moves, int most_mov
 }
 
 // Column tiles of 8 (16 where a KV head has more query columns than 8, so that its keys are unpacked half as often) and
-// one resident wave of CTAs: the 16-column kernel needs the registers of a whole SM.
+// one CTA per SM.
 struct AttnPlan {
   int tiles, col_tiles, grid;
   size_t split_bytes, part_bytes;
@@ -101,10 +101,10 @@ int plan_attention(int32_t batch, int32_t queries, int32_t n_q_heads, int32_t n_
   const int64_t cols = static_cast<int64_t>(n_q_heads / n_kv_heads) * queries;
   p->tiles = cols > 8 ? 2 : 1;
   const int64_t col_tiles = (cols + 8 * p->tiles - 1) / (8 * p->tiles);
-  if (batch > 4096 || col_tiles * n_kv_heads > 16384)
-    return op_fail(THINFER_EUNSUPPORTED, "kv4_attention: batch %d > 4096, or more than 262144 query columns per request", batch);
+  if (batch > 2048 || col_tiles * n_kv_heads > 16384)
+    return op_fail(THINFER_EUNSUPPORTED, "kv4_attention: batch %d > 2048, or more than 262144 query columns per request", batch);
   p->col_tiles = static_cast<int>(col_tiles);
-  p->grid = op_sm_count() * (p->tiles == 1 ? 2 : 1);
+  p->grid = op_sm_count();
   p->split_bytes = (static_cast<size_t>(p->grid) * sizeof(Kv4Split) + 255) / 256 * 256;
   p->part_bytes = static_cast<size_t>(p->grid) * 2 * p->tiles * 8 * (head_dim + 2) * 4;
   return THINFER_OK;
@@ -112,9 +112,9 @@ int plan_attention(int32_t batch, int32_t queries, int32_t n_q_heads, int32_t n_
 
 template <int D, int NT>
 int launch_attention(const Kv4AttnArgs& a, int grid, cudaStream_t st) {
-  const size_t smem = kKv4Warps * kv4_warp_bytes<D, NT>() + (static_cast<size_t>(a.batch) + 1) * 8;
+  const size_t smem = kv4_warps<NT>() * kv4_warp_bytes<D, NT>() + (static_cast<size_t>(a.batch) + 1) * 8;
   int rc = opt_in(kv4_attn_kernel<D, NT>, smem);
-  if (rc == THINFER_OK) rc = op_launch(kv4_attn_kernel<D, NT>, dim3(grid), dim3(kKv4Warps * 32), smem, st, false, a);
+  if (rc == THINFER_OK) rc = op_launch(kv4_attn_kernel<D, NT>, dim3(grid), dim3(kv4_warps<NT>() * 32), smem, st, false, a);
   if (rc == THINFER_OK) rc = op_launch(kv4_attn_join_kernel<D, NT>, dim3(grid, NT * 8), dim3(256), 0, st, true, a);
   return rc;
 }
@@ -283,7 +283,8 @@ int thinfer_op_kv4_attention(const void* q, int64_t q_stride, const void* pool, 
   // no more CTAs than the table's capacity could give a unit per warp
   const int64_t units = static_cast<int64_t>(batch) * n_kv_heads * p.col_tiles *
                         ((static_cast<int64_t>(max_pages) * page_size + kKv4Unit - 1) / kKv4Unit);
-  const int64_t most = (units + kKv4Warps - 1) / kKv4Warps;
+  const int warps = p.tiles == 1 ? kv4_warps<1>() : kv4_warps<2>();
+  const int64_t most = (units + warps - 1) / warps;
   const int grid = most < p.grid ? static_cast<int>(most) : p.grid;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (head_dim == 128) return p.tiles == 1 ? launch_attention<128, 1>(a, grid, st) : launch_attention<128, 2>(a, grid, st);

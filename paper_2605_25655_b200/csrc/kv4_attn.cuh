@@ -6,7 +6,7 @@
 // Scale and offset of a row belong to all its D values, so neither has to touch the codes:
 //
 //   S[i, t]  = scale_t (q_i . code_t) + offset_t (sum of q_i)
-//   out_i    = ( sum_t w_t code_t - 7.5 sum_t w_t + sum_t p_t (offset_t + 7.5 scale_t) ) / sum_t p_t,   w_t = p_t scale_t
+//   out_i    = ( sum_t w_t (code_t - 8) + sum_t p_t (offset_t + 8 scale_t) ) / sum_t p_t,   w_t = p_t scale_t
 //
 // and the matrix instructions multiply by the codes themselves.  A code in the low mantissa bits of an FP16 number is
 // the subnormal code * 2^-24 (bits 0-3) or code * 2^-20 (bits 4-7), which the tensor cores take at face value: one AND
@@ -22,27 +22,35 @@
 //   O^T[dim, column]  += V^T[dim, token] P^T    A = V codes (the layout keeps token pairs together), B = weights
 //
 // The weights w go to FP16 relative to a running reference per column; sums of p and of p times the middle of the row
-// stay in FP32, and the second sum above is taken over the rounded weights (one more instruction per 16 tokens, against
-// a matrix of ones), so that a rounding of w counts with the distance from the middle of the row, at most 7.5 scale,
-// instead of the whole code: without it the FP16 error against 64 bits was 1.6 times that of an FP32 attention.  The running maximum and that reference move only when a weight
+// stay in FP32.  The 8 is taken off the codes by one more instruction per 16 tokens (a matrix of ones gives the sum of
+// the rounded weights) and a packed FP32 multiply-add per pair of accumulators and 32 tokens: a rounding of w then
+// counts with the distance from the middle of the row, not with the whole code, and the accumulators stay as small as
+// the result, so that the truncation of the matrix unit's additions does not add up (over 16384 keys the FP16 error
+// against 64 bits was 3.2e-4 with the 8 taken off at the end, 2.1e-4 is the rounding of the result).
+// The running maximum and that reference move only when a weight
 // would exceed 2^8 (one vote per 32 tokens): the shuffles and the rescaling of the output are then off the usual path.
 //
 // Bound: HBM, D + 8 bytes per key and KV head; at 6.4 TB/s an SM has to consume 48 codes a cycle, which leaves 2.7
-// issue slots per code.  Work: all (request, KV head, column tile) pairs are cut into units of 32 tokens, laid end to
-// end and dealt out in equal runs, first to the CTAs, then to the warps of a CTA; the lengths are only known on the
-// device, so each CTA sums them up itself.  A warp streams its units through a private ring in shared memory filled by
-// bulk asynchronous copies (one lane issues, no synchronisation between warps).  What a warp cannot finish is merged
-// in shared memory; what a CTA cannot finish goes to the workspace and a second kernel, chained to this one, merges it
-// in CTA order: the result does not depend on timing, and the workspace needs no initial state.
+// issue slots per code and half as many for the ANDs and shifts (half rate).  Work: all (request, KV head, column tile)
+// pairs are cut into units of 32 tokens, laid end to end and dealt out in equal runs, first to the CTAs (one per SM),
+// then to the warps of a CTA; the lengths are only known on the device, so each CTA sums them up itself.  Each warp
+// streams its units through a private ring in shared memory with 16-byte asynchronous copies, and needs no other warp
+// until its range is done.  (Bulk copies took fewer instructions to write but more to issue: four of them per 32 tokens
+// cost 150 issue cycles where nine 16-byte copies by all lanes cost 30, 209 against 1xx us for 64 x 16384 keys.)  What a warp
+// cannot finish is merged in shared memory; what a CTA cannot finish goes to the workspace and a second kernel, chained
+// to this one, merges it in CTA order: the result does not depend on timing, and the workspace needs no initial state.
 #pragma once
 #include "kv4_layout.cuh"
 
 namespace thinfer {
 
-constexpr int kKv4Warps = 8;
 constexpr int kKv4Unit = 32;         // tokens of one ring stage
-constexpr int kKv4Stages = 2;        // with 8 warps and 2 CTAs per SM 70 to 140 KB are in flight, two to four times what
-                                     // HBM latency asks for
+constexpr int kKv4Stages = 3;
+// Warps of a CTA, one CTA per SM: what the registers allow (168 and 255 a thread).
+template <int NT>
+__host__ __device__ constexpr int kv4_warps() {
+  return NT == 1 ? 12 : 8;
+}
 constexpr float kKv4Low = -1e30f;    // running maximum before the first key
 
 // What a CTA leaves for the second kernel about the pair that begins in it and ends in a later one.
@@ -90,6 +98,10 @@ __device__ __forceinline__ int kv4_len(const Kv4AttnArgs& a, int b) {
   const int n = __ldg(a.lens + b);
   return n < 0 ? 0 : static_cast<int>(min(static_cast<long long>(n), cap));
 }
+// a / b of numbers that are not negative; nearly always both fit 32 bits, where a division costs a fifth
+__device__ __forceinline__ long long div_pos(long long a, long long b) {
+  return ((a | b) >> 32) == 0 ? static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
+}
 __device__ __forceinline__ int kv4_units(int len) { return len <= kKv4Unit ? 1 : (len + kKv4Unit - 1) / kKv4Unit; }
 
 __device__ __forceinline__ void kv4_prefix(const Kv4AttnArgs& a, long long* pref, long long* warp_sums) {
@@ -136,64 +148,79 @@ __device__ __forceinline__ Kv4Place kv4_place(const Kv4AttnArgs& a, const long l
   p.len = kv4_len(a, lo);
   p.units = kv4_units(p.len);
   const long long in_b = u - pref[lo];
-  p.pair_in_b = static_cast<int>(in_b / p.units);
+  p.pair_in_b = static_cast<int>(div_pos(in_b, p.units));
   p.unit = static_cast<int>(in_b - static_cast<long long>(p.pair_in_b) * p.units);
   p.pair_first = u - p.unit;
   return p;
 }
 // CTAs that take part: with few units some stay idle rather than split pairs further.
-__device__ __forceinline__ long long kv4_ctas(long long total, int grid) {
-  const long long want = (total + kKv4Warps - 1) / kKv4Warps;
-  return want < grid ? want : grid;
+__device__ __forceinline__ long long kv4_ctas(long long total, int grid, int warps) {
+  return total < static_cast<long long>(grid) * warps ? (static_cast<int>(total) + warps - 1) / warps : grid;
 }
-__device__ __forceinline__ long long kv4_cta_first(long long total, long long ctas, long long i) { return i * total / ctas; }
-__device__ __forceinline__ long long kv4_cta_of(long long total, long long ctas, long long u) { return ((u + 1) * ctas - 1) / total; }
+__device__ __forceinline__ long long kv4_cta_first(long long total, long long ctas, long long i) { return div_pos(i * total, ctas); }
+__device__ __forceinline__ long long kv4_cta_of(long long total, long long ctas, long long u) { return div_pos((u + 1) * ctas - 1, total); }
 
 // ------------------------------------------------------------------ instructions
 __device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
   uint32_t d;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
   return d;
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-// Untiled copy global -> shared; both addresses 16-byte aligned, bytes a multiple of 16.
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
-               "r"(bytes), "r"(smem_u32(bar))
-               : "memory");
+__device__ __forceinline__ void async_copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 template <int W>
-__device__ __forceinline__ void lds_words(uint32_t (&r)[W], uint32_t addr) {
-  if constexpr (W == 4)
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-  else
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr));
+__device__ __forceinline__ void lds_words(uint32_t (&r)[W], const uint8_t* p) {
+  if constexpr (W == 4) {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    r[0] = v.x;
+    r[1] = v.y;
+    r[2] = v.z;
+    r[3] = v.w;
+  } else {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    r[0] = v.x;
+    r[1] = v.y;
+  }
 }
-__device__ __forceinline__ float2 lds_params(uint32_t addr) {
-  uint32_t v;
-  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr));
-  return kv4_unpack_params(v);
-}
+__device__ __forceinline__ float2 lds_params(const uint8_t* p) { return kv4_unpack_params(*reinterpret_cast<const uint32_t*>(p)); }
 
 // Where lane (r, c) = (lane / 4, lane % 4) finds things in a block of 16 tokens.  Row r of the score tile is token
 // 4 (r / 2) + r % 2 and row r + 8 the token two further: after the 8 x 8 transposes lane c then holds the weights of
 // tokens 4c .. 4c + 3, two neighbouring pairs of the V layout.
 __device__ __forceinline__ int kv4_row_token(int r) { return 4 * (r >> 1) + (r & 1); }
 
+// A ring stage: K codes and V codes of 32 tokens as in a page, then the params.  Within each 128 bytes of codes the
+// 16-byte pieces are permuted so that the lanes that read together (four token pairs of V, or tokens 0, 1, 4, 5 of K
+// where two rows share 64 bytes) meet different banks: piece p of line n is at p ^ kv4_key(n).
+template <int D, bool V>
+__host__ __device__ constexpr int kv4_key(int line) {
+  return V ? 2 * ((D == 128 ? line >> 1 : line) & 3) : (D == 128 ? 0 : 4 * (line & 1));
+}
+// Byte offset of byte `at` of a code part.
+template <int D, bool V>
+__device__ __forceinline__ int kv4_at(int at) {
+  return at ^ (kv4_key<D, V>(at >> 7) << 4);
+}
+
 // State of one warp's current pair: columns 2c and 2c + 1 of every column tile.
 template <int D, int NT>
 struct Kv4Acc {
   float o[NT][D / 16][4];
-  float ones[NT][4];                               // sum of the rounded weights, in every row
   float m[NT][2], l[NT][2], z[NT][2], ref[NT][2];  // maximum, sum of p, sum of p times row middle, reference of w
   float qf[NT][2], qs[NT][2];                      // scale of the code product, scaled sum of the query
   int lim[NT][2];                                  // keys a column sees
@@ -202,8 +229,6 @@ struct Kv4Acc {
   __device__ __forceinline__ void reset() {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) ones[n][e] = 0.f;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         m[n][j] = kKv4Low;
@@ -275,141 +300,151 @@ __device__ __forceinline__ void kv4_load_queries(const Kv4AttnArgs& a, Kv4Acc<D,
   }
 }
 
-// 32 tokens of a ring stage.  MASKED: some of them are behind the end for some column, or on no page (bit b of `bad`:
-// the tokens 16 b .. 16 b + 15).
+// 32 tokens of a ring stage, 16 at a time.  MASKED: some of them are behind the end for some column, or on no page (bit
+// b of `bad`: the tokens 16 b .. 16 b + 15).
 template <int D, int NT, bool MASKED>
-__device__ __forceinline__ void kv4_stage(Kv4Acc<D, NT>& s, uint32_t stage, int t0, uint32_t bad) {
+__device__ __forceinline__ void kv4_stage(Kv4Acc<D, NT>& s, const uint8_t* stage, int t0, uint32_t bad) {
   constexpr int W = D / 32, MT = D / 16;
-  constexpr uint32_t LO = 0x000f000fu, HI = 0x00f000f0u, ONE = 0x3c003c00u;
+  constexpr uint32_t LO = 0x000f000fu, HI = 0x00f000f0u, BOTH = 0x00ff00ffu, ONE = 0x3c003c00u;
+  constexpr int KP = kKv4Unit * D, VP = KP + kKv4Unit * 4;
   const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
   const int tr = kv4_row_token(r);
-  float sc[2][NT][4];
+  float ones[NT][4];
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) ones[n][e] = 0.f;
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
+    // ---- scores
+    float sc[NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sc[b][n][e] = 0.f;
-    uint32_t ka[W], kb[W];
-    lds_words<W>(ka, stage + (16 * b + tr) * (D / 2) + c * (D / 8));
-    lds_words<W>(kb, stage + (16 * b + tr + 2) * (D / 2) + c * (D / 8));
+      for (int e = 0; e < 4; ++e) sc[n][e] = 0.f;
+    {
+      uint32_t ka[W], kb[W];
+      lds_words<W>(ka, stage + 16 * b * (D / 2) + kv4_at<D, false>(tr * (D / 2) + c * (D / 8)));
+      lds_words<W>(kb, stage + 16 * b * (D / 2) + kv4_at<D, false>((tr + 2) * (D / 2) + c * (D / 8)));
 #pragma unroll
-    for (int w = 0; w < W; ++w)
+      for (int w = 0; w < W; ++w)
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        const uint32_t x = hf ? ka[w] >> 8 : ka[w], y = hf ? kb[w] >> 8 : kb[w];
+        for (int hf = 0; hf < 2; ++hf) {
+          const uint32_t x = hf ? ka[w] >> 8 : ka[w], y = hf ? kb[w] >> 8 : kb[w];
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-          mma_f16_16816(sc[b][n], x & LO, y & LO, x & HI, y & HI, s.q[n][2 * w + hf][0], s.q[n][2 * w + hf][1]);
-      }
-  }
-  float2 kp[2][2], vp[2][2];   // [block][row r | row r + 8] scale, offset
-  constexpr int KP = kKv4Unit * D, VP = KP + kKv4Unit * 4;
-#pragma unroll
-  for (int b = 0; b < 2; ++b)
+          for (int n = 0; n < NT; ++n) mma_f16_16816(sc[n], x & LO, y & LO, x & HI, y & HI, s.q[n][2 * w + hf][0], s.q[n][2 * w + hf][1]);
+        }
+    }
+    // ---- weights
+    float2 kp[2], vp[2];   // [row r | row r + 8] scale, offset; for V scale, middle of the row
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int t = 16 * b + tr + 2 * e;
-      kp[b][e] = lds_params(stage + KP + t * 4);
-      vp[b][e] = lds_params(stage + VP + t * 4);
-      vp[b][e].y = fmaf(7.5f, vp[b][e].x, vp[b][e].y);   // the middle of the row
+      kp[e] = lds_params(stage + KP + t * 4);
+      vp[e] = lds_params(stage + VP + t * 4);
+      vp[e].y = fmaf(8.f, vp[e].x, vp[e].y);
     }
-  auto seen = [&](int b, int e, int n, int j) { return !MASKED || t0 + 16 * b + tr + 2 * e < s.lim[n][j]; };
-  auto raw = [&](int b, int e, int n, int j, float minus) {   // score - minus, log2 units
-    float x = fmaf(kp[b][e].x, sc[b][n][2 * e + j] * s.qf[n][j], fmaf(kp[b][e].y, s.qs[n][j], -minus));
-    if (MASKED) {
-      if ((bad >> b) & 1u) x = __int_as_float(0x7fffffff);
-      if (!seen(b, e, n, j)) x = -INFINITY;
-    }
-    return x;
-  };
-  // value params of a masked token may be anything: they must not meet a weight of zero
-  auto vscale = [&](int b, int e, int n, int j) { return !MASKED || seen(b, e, n, j) ? vp[b][e].x : 0.f; };
-  auto vmid = [&](int b, int e, int n, int j) { return !MASKED || seen(b, e, n, j) ? vp[b][e].y : 0.f; };
-  float p[2][NT][4], w[2][NT][4];
-  float top = 0.f;
-  auto weights = [&]() {
-    top = 0.f;
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
+    auto seen = [&](int e, int n, int j) { return !MASKED || t0 + 16 * b + tr + 2 * e < s.lim[n][j]; };
+    auto raw = [&](int e, int n, int j, float minus) {   // score - minus, log2 units
+      float x = fmaf(kp[e].x, sc[n][2 * e + j] * s.qf[n][j], fmaf(kp[e].y, s.qs[n][j], -minus));
+      if (MASKED) {
+        if ((bad >> b) & 1u) x = __int_as_float(0x7fffffff);
+        if (!seen(e, n, j)) x = -INFINITY;
+      }
+      return x;
+    };
+    // value params of a masked token may be anything: they must not meet a weight of zero
+    auto vscale = [&](int e, int n, int j) { return !MASKED || seen(e, n, j) ? vp[e].x : 0.f; };
+    auto vmid = [&](int e, int n, int j) { return !MASKED || seen(e, n, j) ? vp[e].y : 0.f; };
+    float p[NT][4], w[NT][4];
+    float top = 0.f;
+    auto weights = [&]() {
+      top = 0.f;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const float x = ex2_approx(raw(b, e, n, j, s.m[n][j]));
-            const float y = x * s.ref[n][j] * vscale(b, e, n, j);
-            p[b][n][2 * e + j] = x;
-            w[b][n][2 * e + j] = y;
+            const float x = ex2_approx(raw(e, n, j, s.m[n][j]));
+            const float y = x * s.ref[n][j] * vscale(e, n, j);
+            p[n][2 * e + j] = x;
+            w[n][2 * e + j] = y;
             top = fmax3(top, x, y);
           }
-  };
-  weights();
-  if (__any_sync(0xffffffffu, top > 256.f)) {
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        float mx = s.m[n][j];
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) mx = fmaxf(mx, raw(b, e, n, j, 0.f));
-#pragma unroll
-        for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-        const float al = ex2_approx(s.m[n][j] - mx);
-        float big = exact_inverse(s.ref[n][j]) * al;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) big = fmaxf(big, ex2_approx(raw(b, e, n, j, mx)) * vscale(b, e, n, j));
-#pragma unroll
-        for (int off = 4; off < 32; off <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, off));
-        const int ex = min(max(__float_as_int(big) >> 23, 27), 227);
-        const float ref = __int_as_float((254 - ex) << 23);
-        const float move = al * (ref * exact_inverse(s.ref[n][j]));
-        s.m[n][j] = mx;
-        s.ref[n][j] = ref;
-        s.l[n][j] *= al;
-        s.z[n][j] *= al;
-        s.ones[n][j] *= move;
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          s.o[n][i][j] *= move;
-          s.o[n][i][2 + j] *= move;
-        }
-      }
+    };
     weights();
-  }
+    if (__any_sync(0xffffffffu, top > 256.f)) {
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float mx = fmax3(s.m[n][j], raw(0, n, j, 0.f), raw(1, n, j, 0.f));
+#pragma unroll
+          for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+          const float al = ex2_approx(s.m[n][j] - mx);
+          float big = exact_inverse(s.ref[n][j]) * al;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) big = fmaxf(big, ex2_approx(raw(e, n, j, mx)) * vscale(e, n, j));
+#pragma unroll
+          for (int off = 4; off < 32; off <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, off));
+          const int ex = min(max(__float_as_int(big) >> 23, 27), 227);
+          const float ref = __int_as_float((254 - ex) << 23);
+          const float move = al * (ref * exact_inverse(s.ref[n][j]));
+          s.m[n][j] = mx;
+          s.ref[n][j] = ref;
+          s.l[n][j] *= al;
+          s.z[n][j] *= al;
+          ones[n][j] *= move;
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            s.o[n][i][j] *= move;
+            s.o[n][i][2 + j] *= move;
+          }
+        }
+      weights();
+    }
     uint32_t pb[NT][2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NT; ++n) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          s.l[n][j] += p[b][n][2 * e + j];
-          s.z[n][j] = fmaf(p[b][n][2 * e + j], vmid(b, e, n, j), s.z[n][j]);
+          s.l[n][j] += p[n][2 * e + j];
+          s.z[n][j] = fmaf(p[n][2 * e + j], vmid(e, n, j), s.z[n][j]);
         }
-        pb[n][e] = transpose_8x8(pack_f16(w[b][n][2 * e], w[b][n][2 * e + 1]));
+        pb[n][e] = transpose_8x8(pack_f16(w[n][2 * e], w[n][2 * e + 1]));
       }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) mma_f16_16816(s.ones[n], ONE, ONE, ONE, ONE, pb[n][0], pb[n][1]);
+      mma_f16_16816(ones[n], ONE, ONE, ONE, ONE, pb[n][0], pb[n][1]);
+    }
+    // ---- output: row r of a tile collects code + 16 code', row r + 8 collects 16 code' (code' the next dimension)
     uint32_t va[W], vb[W];
-    const uint32_t v = stage + kKv4Unit * (D / 2) + (8 * b + 2 * c) * D + r * (D / 8);
-    lds_words<W>(va, v);
-    lds_words<W>(vb, v + D);
+    const uint8_t* v = stage + kKv4Unit * (D / 2) + 8 * b * D;   // 8 pairs: a multiple of the lines the keys repeat after
+    lds_words<W>(va, v + kv4_at<D, true>(2 * c * D + r * (D / 8)));
+    lds_words<W>(vb, v + kv4_at<D, true>((2 * c + 1) * D + r * (D / 8)));
 #pragma unroll
     for (int i = 0; i < W; ++i)
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
-        const uint32_t x = hf ? va[i] >> 8 : va[i], y = hf ? vb[i] >> 8 : vb[i];
+        const uint32_t x = hf ? __byte_perm(va[i], 0, 0x4341) : va[i] & BOTH, y = hf ? __byte_perm(vb[i], 0, 0x4341) : vb[i] & BOTH;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) mma_f16_16816(s.o[n][2 * i + hf], x & LO, x & HI, y & LO, y & HI, pb[n][0], pb[n][1]);
+        for (int n = 0; n < NT; ++n) mma_f16_16816(s.o[n][2 * i + hf], x, x & HI, y, y & HI, pb[n][0], pb[n][1]);
       }
+  }
+  // ---- 8 off every code
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const uint64_t sum = f32x2(ones[n][0], ones[n][1]);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const float2 x = f32x2_unpack(fma_f32x2(sum, f32x2(-136 * 0x1p-24f, -136 * 0x1p-24f), f32x2(s.o[n][i][0], s.o[n][i][1])));
+      const float2 y = f32x2_unpack(fma_f32x2(sum, f32x2(-0x1p-17f, -0x1p-17f), f32x2(s.o[n][i][2], s.o[n][i][3])));
+      s.o[n][i][0] = x.x;
+      s.o[n][i][1] = x.y;
+      s.o[n][i][2] = y.x;
+      s.o[n][i][3] = y.y;
+    }
   }
 }
 
@@ -417,8 +452,9 @@ __device__ __forceinline__ void kv4_stage(Kv4Acc<D, NT>& s, uint32_t stage, int 
 template <int D, int NT>
 __device__ __forceinline__ float4 kv4_value4(const Kv4Acc<D, NT>& s, int n, int j, int i, float z, float back) {
   constexpr float F0 = 16777216.f, F1 = 1048576.f;  // 2^24 and 2^20: the place of the code in its operand
-  return make_float4(fmaf(s.o[n][2 * i][j], F0 * back, z), fmaf(s.o[n][2 * i][2 + j], F1 * back, z),
-                     fmaf(s.o[n][2 * i + 1][j], F0 * back, z), fmaf(s.o[n][2 * i + 1][2 + j], F1 * back, z));
+  const float(&x)[4] = s.o[n][2 * i], (&y)[4] = s.o[n][2 * i + 1];
+  return make_float4(fmaf(x[j] - x[2 + j], F0 * back, z), fmaf(x[2 + j], F1 * back, z), fmaf(y[j] - y[2 + j], F0 * back, z),
+                     fmaf(y[2 + j], F1 * back, z));
 }
 __device__ __forceinline__ void kv4_store4(half_t* dst, float4 v) {
   *reinterpret_cast<uint2*>(dst) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
@@ -431,41 +467,39 @@ __device__ __forceinline__ half_t* kv4_out(const Kv4AttnArgs& a, int b, int hk, 
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(kKv4Warps * 32, NT == 1 ? 2 : 1) kv4_attn_kernel(const Kv4AttnArgs a) {
-  constexpr int W = D / 32, NC = NT * 8, NS = kKv4Stages, STAGE = kv4_stage_bytes<D>();
-  constexpr int PART = kv4_partial_floats<D, NT>();
+__global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const Kv4AttnArgs a) {
+  constexpr int W = D / 32, NC = NT * 8, NS = kKv4Stages, STAGE = kv4_stage_bytes<D>(), CW = kv4_warps<NT>();
+  constexpr int PART = kv4_partial_floats<D, NT>(), WARP_BYTES = kv4_warp_bytes<D, NT>();
   extern __shared__ __align__(128) uint8_t kv4_mem[];
-  __shared__ __align__(8) uint64_t bars[kKv4Warps][NS];
-  __shared__ long long warp_sums[kKv4Warps];
-  __shared__ long long part_pair[2 * kKv4Warps];   // first unit of an unfinished piece's pair, or -1; 2 w: head, 2 w + 1: tail
+  __shared__ long long warp_sums[CW];
+  __shared__ long long part_pair[2 * CW];   // first unit of an unfinished piece's pair, or -1; 2 w: head, 2 w + 1: tail
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
-  uint8_t* const mine = kv4_mem + warp * kv4_warp_bytes<D, NT>();
-  long long* pref = reinterpret_cast<long long*>(kv4_mem + kKv4Warps * kv4_warp_bytes<D, NT>());
-  if (lane == 0) {
-#pragma unroll
-    for (int i = 0; i < NS; ++i) mbar_init(&bars[warp][i], 1);
-    fence_barrier_init();
-    part_pair[2 * warp] = part_pair[2 * warp + 1] = -1;
-  }
-  kv4_prefix(a, pref, warp_sums);
-  const long long total = pref[a.batch], ctas = kv4_ctas(total, gridDim.x);
+  long long* pref = reinterpret_cast<long long*>(kv4_mem + CW * WARP_BYTES);
+  if (threadIdx.x < 2 * CW) part_pair[threadIdx.x] = -1;
   if (threadIdx.x == 0) a.splits[blockIdx.x].last = -1;
+  kv4_prefix(a, pref, warp_sums);
+  const long long total = pref[a.batch], ctas = kv4_ctas(total, gridDim.x, CW);
   if (blockIdx.x >= ctas) return;
-  const long long c_beg = kv4_cta_first(total, ctas, blockIdx.x), c_end = kv4_cta_first(total, ctas, blockIdx.x + 1);
-  const long long w_beg = c_beg + warp * (c_end - c_beg) / kKv4Warps;
-  const int w_units = static_cast<int>(c_beg + (warp + 1) * (c_end - c_beg) / kKv4Warps - w_beg);
+  const long long c_beg = kv4_cta_first(total, ctas, blockIdx.x), c_units = kv4_cta_first(total, ctas, blockIdx.x + 1) - c_beg;
+  const long long w_beg = c_beg + div_pos(warp * c_units, CW);
+  const int w_units = static_cast<int>(c_beg + div_pos((warp + 1) * c_units, CW) - w_beg);
+  uint8_t* const mine = kv4_mem + warp * WARP_BYTES;
   const uint32_t ring = smem_u32(mine);
-  const int shift = a.c.page_shift;
+  const int shift = a.c.page_shift, P = 1 << shift;
 
-  // ---- producer: walks the warp's units ahead of the consumer
+  // ---- requests: walk the warp's units ahead of the arithmetic, across segments
   int f_u = 0, f_end = 0;              // next unit to request and end of the segment it is in, from w_beg
   int f_t = 0, f_len = 0, f_base = 0;  // its first token, the pair's length, table column of `ids`
   const uint8_t* f_blocks = nullptr;   // pool + head offset
   const int32_t* f_row = nullptr;
   int ids = -1, ids_next = -1;         // page numbers of 32 table columns from f_base, and of the next 32
-  int filled = 0;
-  uint32_t bad_of = 0;                 // two bits for each ring stage
+  int f_slot = 0;
+  uint32_t bad_of = 0;                 // two bits for each ring stage: tokens 0 .. 15 or 16 .. 31 are on no page
+  // this lane's place in a copy of 512 bytes of codes (line lane / 8), in an even and an odd one, and in the params
+  const uint32_t k_to = kv4_at<D, false>(lane * 16);
+  const uint32_t v_to[2] = {static_cast<uint32_t>(kv4_at<D, true>(lane * 16)), static_cast<uint32_t>(kv4_at<D, true>(512 + lane * 16) - 512)};
+  const int par_from = P * D + (lane & 8 ? P * 4 : 0) + (lane & 3) * 16;
   auto load_ids = [&](int base) {
     const int col = base + lane;
     return col < a.c.max_pages && (static_cast<long long>(col) << shift) < f_len ? __ldg(f_row + col) : -1;
@@ -487,95 +521,95 @@ __global__ void __launch_bounds__(kKv4Warps * 32, NT == 1 ? 2 : 1) kv4_attn_kern
       const int t = f_t;
       f_t += kKv4Unit;
       if (t >= f_len) continue;        // the one unit of an empty row holds nothing
-      if ((t >> shift) - f_base >= 32) {
+      int col = (t >> shift) - f_base;
+      if (col >= 32) {
         f_base += 32;
+        col -= 32;
         ids = ids_next;
         ids_next = load_ids(f_base + 32);
       }
-      const int slot = filled % NS;
-      uint64_t* bar = &bars[warp][slot];
-      const uint32_t dst = ring + slot * STAGE;
-      const int n = shift == 4 ? 2 : 1, part = kKv4Unit / n;   // pieces of a stage: two pages of 16 tokens, or one page
-      uint32_t bad = 0, bytes = 0;
-      int page[2];
+      // the two halves of 16 tokens: on one page, or on two of 16 tokens; no request for what lies behind the end
+      const int at0 = t & (P - 1), at1 = (t + 16) & (P - 1);
+      const int page0 = __shfl_sync(0xffffffffu, ids, col), page1 = shift == 4 ? __shfl_sync(0xffffffffu, ids, (col + 1) & 31) : page0;
+      const bool there1 = t + 16 < f_len;
+      const bool ok0 = static_cast<unsigned>(page0) < static_cast<unsigned>(a.c.n_pages);
+      const bool ok1 = static_cast<unsigned>(page1) < static_cast<unsigned>(a.c.n_pages);
+      const uint32_t bad = (ok0 ? 0u : 1u) | (ok1 || !there1 ? 0u : 2u);
+      bad_of = (bad_of & ~(3u << (2 * f_slot))) | bad << (2 * f_slot);
+      const uint32_t dst = ring + f_slot * STAGE;
+      const uint8_t* from0 = f_blocks + static_cast<size_t>(page0) * a.c.page_bytes;
+      const uint8_t* from1 = shift == 4 ? f_blocks + static_cast<size_t>(page1) * a.c.page_bytes : from0;
+      constexpr int HALF = 8 * D;      // code bytes of 16 tokens
+      if (ok0) {
+        const uint8_t* k = from0 + at0 * (D / 2) + lane * 16;
+        const uint8_t* v = k + P * (D / 2);
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        page[k] = __shfl_sync(0xffffffffu, ids, ((t >> shift) - f_base + k) & 31);
-        if (k < n && t + k * part < f_len) {
-          if (page[k] < 0 || page[k] >= a.c.n_pages) {
-            bad |= n == 2 ? 1u << k : 3u;
-            page[k] = -1;
-          } else {
-            bytes += part * (D + 8);
-          }
-        } else {
-          page[k] = -1;
+        for (int i = 0; i < HALF / 512; ++i) {
+          async_copy16(dst + i * 512 + k_to, k + i * 512);
+          async_copy16(dst + 2 * HALF + i * 512 + v_to[i & 1], v + i * 512);
         }
       }
-      bad_of = (bad_of & ~(3u << (2 * slot))) | bad << (2 * slot);
-      if (lane == 0) {
-        mbar_expect_tx(bar, bytes);    // arrives; with no byte to come the phase is complete
+      if (ok1 && there1) {
+        const uint8_t* k = from1 + at1 * (D / 2) + lane * 16;
+        const uint8_t* v = k + P * (D / 2);
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-          if (page[k] >= 0) {
-            const uint8_t* block = f_blocks + static_cast<size_t>(page[k]) * a.c.page_bytes;
-            const int P = 1 << shift, at = t & (P - 1), d0 = k * part;
-            bulk_load(dst + d0 * (D / 2), block + at * (D / 2), part * (D / 2), bar);
-            bulk_load(dst + kKv4Unit * (D / 2) + d0 * (D / 2), block + P * (D / 2) + at * (D / 2), part * (D / 2), bar);
-            bulk_load(dst + kKv4Unit * D + d0 * 4, block + P * D + at * 4, part * 4, bar);
-            bulk_load(dst + kKv4Unit * (D + 4) + d0 * 4, block + P * (D + 4) + at * 4, part * 4, bar);
-          }
+        for (int i = 0; i < HALF / 512; ++i) {
+          const int j = HALF / 512 + i;
+          async_copy16(dst + HALF + i * 512 + k_to, k + i * 512);
+          async_copy16(dst + 3 * HALF + i * 512 + v_to[j & 1], v + i * 512);
+        }
       }
-      ++filled;
+      // params: lanes 0-3, 4-7 K of the halves, 8-11, 12-15 V of the halves
+      const bool second = (lane & 4) != 0;
+      if (lane < 16 && (second ? ok1 && there1 : ok0))
+        async_copy16(dst + 4 * HALF + lane * 16, (second ? from1 + at1 * 4 : from0 + at0 * 4) + par_from);
+      f_slot = f_slot + 1 == NS ? 0 : f_slot + 1;
       return;
     }
   };
-  __syncwarp();                        // the barriers are initialised
 #pragma unroll
-  for (int i = 0; i < NS; ++i) request();
+  for (int i = 0; i < NS - 1; ++i) {
+    request();
+    async_commit();
+  }
 
-  // ---- consumer
   Kv4Acc<D, NT> s;
-  int taken = 0;
-  bool alive = true;                   // false once a wait has run out: everything left becomes NaN
+  int slot = 0;
   for (int u = 0; u < w_units;) {
     const Kv4Place pl = kv4_place(a, pref, w_beg + u);
     const int n_units = min(w_units - u, pl.units - pl.unit);
     const int hk = pl.pair_in_b / a.col_tiles, col0 = (pl.pair_in_b - hk * a.col_tiles) * NC;
     s.reset();
     kv4_load_queries<D, NT>(a, s, pl, hk, col0);
-    const int t_end = min(pl.len, (pl.unit + n_units) * kKv4Unit);
-    for (int t0 = pl.unit * kKv4Unit; t0 < t_end && alive; t0 += kKv4Unit) {
-      const int slot = taken % NS;
-      alive = __all_sync(0xffffffffu, mbar_wait(&bars[warp][slot], (taken / NS) & 1, nullptr));
-      if (!alive) {                    // wait once more for the copies in flight before their memory is used again
-        for (int k = taken; k < filled; ++k) mbar_wait(&bars[warp][k % NS], (k / NS) & 1, nullptr);
-        break;
-      }
+    const int t_end = min(pl.len, (pl.unit + n_units) * kKv4Unit), t_all = pl.len - (a.queries - 1) - kKv4Unit;
+    for (int t0 = pl.unit * kKv4Unit; t0 < t_end; t0 += kKv4Unit) {
+      async_wait<NS - 2>();              // this lane's copies of the stage have landed
       const uint32_t bad = (bad_of >> (2 * slot)) & 3u;
-      const uint32_t stage = ring + slot * STAGE;
-      if (bad == 0 && t0 + kKv4Unit <= pl.len - (a.queries - 1)) kv4_stage<D, NT, false>(s, stage, t0, 0);
-      else kv4_stage<D, NT, true>(s, stage, t0, bad);
-      ++taken;
-      __syncwarp();                    // every lane has read the stage
+      __syncwarp();                      // everybody's have, and everybody has read the stage before it, which is filled next
       request();
+      async_commit();
+      const uint8_t* stage = mine + slot * STAGE;
+      if (bad == 0 && t0 <= t_all) kv4_stage<D, NT, false>(s, stage, t0, 0);
+      else kv4_stage<D, NT, true>(s, stage, t0, bad);
+      slot = slot + 1 == NS ? 0 : slot + 1;
     }
     // ---- the segment's result: sums over the lanes that hold other tokens of the same columns
     const bool head = pl.unit > 0, whole = !head && n_units == pl.units;
-    float* part = head ? reinterpret_cast<float*>(mine + NS * STAGE) : reinterpret_cast<float*>(mine);
+    // the piece that ends the range takes the ring, which nobody fills any more
+    float* part = reinterpret_cast<float*>(mine + (head ? NS * STAGE : 0));
     if (!whole && lane == 0) part_pair[2 * warp + (head ? 0 : 1)] = pl.pair_first;
+    __syncwarp();
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        float l = alive ? s.l[n][j] : __int_as_float(0x7fffffff), z = s.z[n][j];
+        float l = s.l[n][j], z = s.z[n][j];
 #pragma unroll
         for (int off = 4; off < 32; off <<= 1) {
           l += __shfl_xor_sync(0xffffffffu, l, off);
           z += __shfl_xor_sync(0xffffffffu, z, off);
         }
         const float back = exact_inverse(s.ref[n][j]);
-        z = fmaf(-7.5f * back, s.ones[n][j], z);
         const int col = 8 * n + 2 * c + j;
         if (whole) {
           if (col0 + col < a.cols) {
@@ -598,49 +632,51 @@ __global__ void __launch_bounds__(kKv4Warps * 32, NT == 1 ? 2 : 1) kv4_attn_kern
   }
   __syncthreads();
 
-  // ---- unfinished pieces: those of one pair are neighbours in the order head, tail of warp 0, of warp 1, ...
-  auto piece = [&](int k) {
-    return reinterpret_cast<const float*>(kv4_mem + (k >> 1) * kv4_warp_bytes<D, NT>() + ((k & 1) ? 0 : NS * STAGE));
-  };
-  for (int k = 0; k < 2 * kKv4Warps;) {
+  // ---- unfinished pieces: those of one pair are neighbours in the order head, tail of warp 0, of warp 1, ...  A warp
+  // takes some columns of a pair at a time (two in a pass where 16 lanes cover one).
+  constexpr int PASS = 128 / D, TASKS = NC / PASS;
+  int task = -warp;                      // the warp's next task among those of the pairs so far
+  for (int k = 0; k < 2 * CW;) {
     const long long pair = part_pair[k];
     if (pair < 0) {
       ++k;
       continue;
     }
     int k1 = k + 1;
-    while (k1 < 2 * kKv4Warps && (part_pair[k1] < 0 || part_pair[k1] == pair)) ++k1;
-    const Kv4Place pl = kv4_place(a, pref, pair);
-    const int hk = pl.pair_in_b / a.col_tiles, col0 = (pl.pair_in_b - hk * a.col_tiles) * NC;
-    const bool done = pair >= c_beg && pair + pl.units <= c_end;
-    float* ws = a.parts + (static_cast<size_t>(blockIdx.x) * 2 + (pair < c_beg ? 0 : 1)) * PART;
-    for (int e = threadIdx.x; e < NC * D / 4; e += kKv4Warps * 32) {
-      const int col = e / (D / 4), d = (e - col * (D / 4)) * 4;
-      float top = kKv4Low;
-      for (int i = k; i < k1; ++i)
-        if (part_pair[i] >= 0) top = fmaxf(top, piece(i)[NC * D + 2 * col]);
-      float l = 0.f;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int i = k; i < k1; ++i)
-        if (part_pair[i] >= 0) {
-          const float* q = piece(i);
-          const float f = ex2_approx(q[NC * D + 2 * col] - top);
-          const float4 x = *reinterpret_cast<const float4*>(q + col * D + d);
-          l = fmaf(q[NC * D + 2 * col + 1], f, l);
-          v = make_float4(fmaf(x.x, f, v.x), fmaf(x.y, f, v.y), fmaf(x.z, f, v.z), fmaf(x.w, f, v.w));
+    while (k1 < 2 * CW && (part_pair[k1] < 0 || part_pair[k1] == pair)) ++k1;
+    task += TASKS;
+    if (task > 0) {
+      const Kv4Place pl = kv4_place(a, pref, pair);
+      const int hk = pl.pair_in_b / a.col_tiles, col0 = (pl.pair_in_b - hk * a.col_tiles) * NC;
+      const bool done = pair >= c_beg && pair + pl.units <= c_beg + c_units;
+      float* ws = a.parts + (static_cast<size_t>(blockIdx.x) * 2 + (pair < c_beg ? 0 : 1)) * PART;
+      if (!done && pair >= c_beg && task == TASKS && lane == 0)
+        a.splits[blockIdx.x] = Kv4Split{pl.b, pl.pair_in_b, static_cast<int>(kv4_cta_of(total, ctas, pair + pl.units - 1)), 0};
+      for (; task > 0; task -= CW) {
+        const int col = (TASKS - task) * PASS + lane * 4 / D, d = (lane * 4) % D;
+        float top = kKv4Low, l = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i = k; i < k1; ++i)
+          if (part_pair[i] >= 0) {
+            const float* q = reinterpret_cast<const float*>(kv4_mem + (i >> 1) * WARP_BYTES + ((i & 1) ? 0 : NS * STAGE));
+            const float2 ml = *reinterpret_cast<const float2*>(q + NC * D + 2 * col);
+            const float4 x = *reinterpret_cast<const float4*>(q + col * D + d);
+            const float mx = fmaxf(top, ml.x), f0 = ex2_approx(top - mx), f1 = ex2_approx(ml.x - mx);
+            top = mx;
+            l = fmaf(ml.y, f1, l * f0);
+            v = make_float4(fmaf(x.x, f1, v.x * f0), fmaf(x.y, f1, v.y * f0), fmaf(x.z, f1, v.z * f0), fmaf(x.w, f1, v.w * f0));
+          }
+        if (done) {
+          if (col0 + col < a.cols) {
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            kv4_store4(kv4_out<D>(a, pl.b, hk, col0 + col) + d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+          }
+        } else {
+          *reinterpret_cast<float4*>(ws + col * D + d) = v;
+          if (d == 0) *reinterpret_cast<float2*>(ws + NC * D + 2 * col) = make_float2(top, l);
         }
-      if (done) {
-        if (col0 + col < a.cols) {
-          const float inv = l == 0.f ? 0.f : 1.f / l;
-          kv4_store4(kv4_out<D>(a, pl.b, hk, col0 + col) + d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
-        }
-      } else {
-        *reinterpret_cast<float4*>(ws + col * D + d) = v;
-        if (d == 0) *reinterpret_cast<float2*>(ws + NC * D + 2 * col) = make_float2(top, l);
       }
     }
-    if (!done && pair >= c_beg && threadIdx.x == 0)
-      a.splits[blockIdx.x] = Kv4Split{pl.b, pl.pair_in_b, static_cast<int>(kv4_cta_of(total, ctas, pair + pl.units - 1)), 0};
     k = k1;
   }
 }

@@ -264,16 +264,17 @@ def _check_attention(T, rng, t, hq, hkv, d, page, lens, queries, pool, tab, tabl
         kv = kv4.keys_values(ref, table[i], lens[i])
         for n in range(queries):
             want, spread, mag = kv4.attention(q[i, n], kv, lens[i], queries - 1 - n)
-            # v = mid + scale (code - 7.5) with mid = offset + 7.5 scale: sum p mid is FP32, and the weights p scale of the
-            # second part are rounded to 11 bits, so that each rounding moves the result by at most
-            # 2^-11 p scale |code - 7.5| = 2^-11 p |v - mid|.  mid is the middle of the row's range, or half a step from
-            # it where no code is 15 (then 14 is the largest): |v - mid| <= |v - middle| + range / 28 = a term of `spread`.
+            # v = mid + scale (code - 8) with mid = offset + 8 scale: sum p mid is FP32, and the weights p scale of the second
+            # part are rounded to 11 bits, so that each rounding moves the result by at most
+            # 2^-11 p scale |code - 8| = 2^-11 p |v - mid|.  mid is half a step above the middle of the row's range, or a
+            # whole one where no code is 15 (then 14 is the largest): |v - mid| <= |v - middle| + range / 14, which is less
+            # than twice a term of `spread`
             # Scores in FP32 from exact products: the code part sums terms of up to 15 steps of a row, about four times |k|,
             # in eight accumulation steps of 2^-22: 8 * 4 * 2^-22 = 2^-17 of the largest sum |q k| / sqrt(d) in the exponent
             # of numerator and denominator, 2^-16 in all (2^-15 with the offset part), times the distance of a key's value
             # from the result, at most spread + |want| + sum p |v|
             far = spread + np.abs(want) + kv4_abs(kv, q[i, n], lens[i], queries - 1 - n)
-            tol = EPS[t] * np.abs(want) + 2.0 ** -11 * spread + 2.0 ** -19 * (1 + 16 * mag) * far + 2.0 ** -25
+            tol = EPS[t] * np.abs(want) + 2.0 ** -10 * spread + 2.0 ** -19 * (1 + 16 * mag) * far + 2.0 ** -25
             bad = np.abs(got[i, n] - want) > tol
             assert not bad.any(), (i, n, lens[i], np.argwhere(bad)[:3], np.max(np.abs(got[i, n] - want) / tol))
 
@@ -324,7 +325,7 @@ def test_attention_over_many_and_long_rows(T, batch, n):
         spread = torch.einsum("hgt,thd->hgd", p, (vv - (low + high) / 2).abs() + (high - low) / 28).reshape(hq, d)
         mag = torch.einsum("hgd,thd->hgt", q[i, 0].double().view(hkv, 4, d).abs(), kk.abs()).amax(-1).reshape(hq, 1) / 8.0      # as above
         far = spread + want.abs() + torch.einsum("hgt,thd->hgd", p, vv.abs()).reshape(hq, d)
-        tol = EPS["f16"] * want.abs() + 2.0 ** -11 * spread + 2.0 ** -19 * (1 + 16 * mag) * far + 2.0 ** -25
+        tol = EPS["f16"] * want.abs() + 2.0 ** -10 * spread + 2.0 ** -19 * (1 + 16 * mag) * far + 2.0 ** -25
         assert torch.all((got[i, 0] - want).abs() <= tol)
         del pos
 
