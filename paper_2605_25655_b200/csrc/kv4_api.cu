@@ -115,7 +115,7 @@ int launch_attention(const Kv4AttnArgs& a, int grid, cudaStream_t st) {
   const size_t smem = kv4_warps<NT>() * kv4_warp_bytes<D, NT>() + (static_cast<size_t>(a.batch) + 1) * 8;
   int rc = opt_in(kv4_attn_kernel<D, NT>, smem);
   if (rc == THINFER_OK) rc = op_launch(kv4_attn_kernel<D, NT>, dim3(grid), dim3(kv4_warps<NT>() * 32), smem, st, false, a);
-  if (rc == THINFER_OK) rc = op_launch(kv4_attn_join_kernel<D, NT>, dim3(grid, NT * 8), dim3(256), 0, st, true, a);
+  if (rc == THINFER_OK) rc = op_launch(kv4_attn_join_kernel<D, NT>, dim3(grid), dim3(NT * 256), 0, st, true, a);
   return rc;
 }
 

@@ -45,7 +45,7 @@
 namespace thinfer {
 
 constexpr int kKv4Unit = 32;         // tokens of one ring stage
-constexpr int kKv4Stages = 3;
+constexpr int kKv4Stages = 2;        // more made no difference: 12 warps keep 50 to 100 KB of an SM in flight
 // Warps of a CTA, one CTA per SM: what the registers allow (168 and 255 a thread).
 template <int NT>
 __host__ __device__ constexpr int kv4_warps() {
@@ -82,11 +82,19 @@ template <int D, int NT>
 __host__ __device__ constexpr int kv4_partial_floats() {  // one unfinished piece: outputs, then maximum and sum
   return NT * 8 * (D + 2);
 }
-// Memory of one warp: its ring, which takes the piece that ends its range once it has drained, and room for the piece
-// that begins its range.
+// Memory of one warp: its ring, which takes the piece that ends its range once it has drained; the query columns of the
+// pairs that begin in each ring stage; room for the piece that begins its range.
+template <int D, int NT>
+__host__ __device__ constexpr int kv4_query_bytes() {
+  return NT * 8 * D * 2;
+}
+template <int D, int NT>
+__host__ __device__ constexpr int kv4_ring_bytes() {
+  return kKv4Stages * kv4_stage_bytes<D>();
+}
 template <int D, int NT>
 __host__ __device__ constexpr int kv4_warp_bytes() {
-  return kKv4Stages * kv4_stage_bytes<D>() + kv4_partial_floats<D, NT>() * 4;
+  return kv4_ring_bytes<D, NT>() + kKv4Stages * kv4_query_bytes<D, NT>() + kv4_partial_floats<D, NT>() * 4;
 }
 
 // ------------------------------------------------------------------ schedule
@@ -245,28 +253,38 @@ struct Kv4Acc {
 
 __device__ __forceinline__ float exact_inverse(float pow2) { return __int_as_float((254 << 23) - __float_as_int(pow2)); }
 
+// Requests the query columns of a pair: 16-byte pieces, piece k of column i at k ^ (i & 7).  Columns behind the last one
+// are not written.
+template <int D, int NT>
+__device__ __forceinline__ void kv4_request_queries(const Kv4AttnArgs& a, uint32_t dst, int b, int hk, int col0) {
+  constexpr int PER = D / 8;           // pieces of a column
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int n = 0; n < NT * 8 * PER / 32; ++n) {
+    const int i = (n * 32 + lane) / PER, k = lane % PER, col = col0 + i;
+    if (col < a.cols) {
+      const int qi = a.queries == 1 ? 0 : col / a.group, h = hk * a.group + (col - qi * a.group);
+      const half_t* src = a.q + (static_cast<long long>(b) * a.queries + qi) * a.q_stride + static_cast<long long>(h) * D + k * 8;
+      async_copy16(dst + i * (2 * D) + ((k ^ (i & 7)) << 4), src);
+    }
+  }
+}
+
 // The query columns of a pair as B operand: lane (r, c) converts the D / 4 values of column r that start at c D / 4.
 template <int D, int NT>
-__device__ __forceinline__ void kv4_load_queries(const Kv4AttnArgs& a, Kv4Acc<D, NT>& s, const Kv4Place& pl, int hk, int col0) {
+__device__ __forceinline__ void kv4_load_queries(const Kv4AttnArgs& a, Kv4Acc<D, NT>& s, const uint8_t* from, int len, int col0) {
   constexpr int W = D / 32;
   const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    const int col = col0 + 8 * n + r;
+    const bool there = col0 + 8 * n + r < a.cols;
     float x[8 * W];
-    if (col < a.cols) {
-      const int i = col / a.group, h = hk * a.group + (col - i * a.group);
-      const half_t* src = a.q + (static_cast<long long>(pl.b) * a.queries + i) * a.q_stride + static_cast<long long>(h) * D + c * (D / 4);
 #pragma unroll
-      for (int w = 0; w < W; ++w) {
-        float f[8];
-        unpack8(ldg_cached(src + 8 * w), f);
+    for (int w = 0; w < W; ++w) {
+      float f[8];
+      unpack8(*reinterpret_cast<const uint4*>(from + (8 * n + r) * (2 * D) + (((c * W + w) ^ r) << 4)), f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[8 * w + e] = f[e];
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8 * W; ++e) x[e] = 0.f;
+      for (int e = 0; e < 8; ++e) x[8 * w + e] = there ? f[e] : 0.f;
     }
     float top = 0.f, sum = 0.f;
 #pragma unroll
@@ -295,7 +313,7 @@ __device__ __forceinline__ void kv4_load_queries(const Kv4AttnArgs& a, Kv4Acc<D,
       s.qf[n][j] = __shfl_sync(0xffffffffu, qf, 8 * c + 4 * j);
       s.qs[n][j] = __shfl_sync(0xffffffffu, qs, 8 * c + 4 * j);
       const int cj = col0 + 8 * n + 2 * c + j;
-      s.lim[n][j] = cj < a.cols ? pl.len - (a.queries - 1 - cj / a.group) : 0;
+      s.lim[n][j] = cj < a.cols ? len - (a.queries == 1 ? 0 : a.queries - 1 - cj / a.group) : 0;
     }
   }
 }
@@ -317,11 +335,11 @@ __device__ __forceinline__ void kv4_stage(Kv4Acc<D, NT>& s, const uint8_t* stage
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     // ---- scores
-    float sc[NT][4];
+    float sc[NT][4], sd[NT][4];   // two chains of instructions
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sc[n][e] = 0.f;
+      for (int e = 0; e < 4; ++e) sc[n][e] = sd[n][e] = 0.f;
     {
       uint32_t ka[W], kb[W];
       lds_words<W>(ka, stage + 16 * b * (D / 2) + kv4_at<D, false>(tr * (D / 2) + c * (D / 8)));
@@ -332,8 +350,13 @@ __device__ __forceinline__ void kv4_stage(Kv4Acc<D, NT>& s, const uint8_t* stage
         for (int hf = 0; hf < 2; ++hf) {
           const uint32_t x = hf ? ka[w] >> 8 : ka[w], y = hf ? kb[w] >> 8 : kb[w];
 #pragma unroll
-          for (int n = 0; n < NT; ++n) mma_f16_16816(sc[n], x & LO, y & LO, x & HI, y & HI, s.q[n][2 * w + hf][0], s.q[n][2 * w + hf][1]);
+          for (int n = 0; n < NT; ++n)
+            mma_f16_16816(hf ? sd[n] : sc[n], x & LO, y & LO, x & HI, y & HI, s.q[n][2 * w + hf][0], s.q[n][2 * w + hf][1]);
         }
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[n][e] += sd[n][e];
     }
     // ---- weights
     float2 kp[2], vp[2];   // [row r | row r + 8] scale, offset; for V scale, middle of the row
@@ -466,17 +489,22 @@ __device__ __forceinline__ half_t* kv4_out(const Kv4AttnArgs& a, int b, int hk, 
   return a.out + ((static_cast<size_t>(b) * a.queries + i) * a.n_q + h) * D;
 }
 
+struct Kv4Piece {
+  long long pair;          // first unit of the pair, -1: no piece
+  int units, b, hk, col0, pair_in_b;
+};
+
 template <int D, int NT>
 __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const Kv4AttnArgs a) {
   constexpr int W = D / 32, NC = NT * 8, NS = kKv4Stages, STAGE = kv4_stage_bytes<D>(), CW = kv4_warps<NT>();
   constexpr int PART = kv4_partial_floats<D, NT>(), WARP_BYTES = kv4_warp_bytes<D, NT>();
   extern __shared__ __align__(128) uint8_t kv4_mem[];
   __shared__ long long warp_sums[CW];
-  __shared__ long long part_pair[2 * CW];   // first unit of an unfinished piece's pair, or -1; 2 w: head, 2 w + 1: tail
+  __shared__ Kv4Piece pieces[2 * CW];       // unfinished pieces, 2 w: head, 2 w + 1: tail of warp w
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
   long long* pref = reinterpret_cast<long long*>(kv4_mem + CW * WARP_BYTES);
-  if (threadIdx.x < 2 * CW) part_pair[threadIdx.x] = -1;
+  if (threadIdx.x < 2 * CW) pieces[threadIdx.x].pair = -1;
   if (threadIdx.x == 0) a.splits[blockIdx.x].last = -1;
   kv4_prefix(a, pref, warp_sums);
   const long long total = pref[a.batch], ctas = kv4_ctas(total, gridDim.x, CW);
@@ -516,6 +544,11 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
         f_base = (f_t >> shift) & ~31;
         ids = load_ids(f_base);
         ids_next = load_ids(f_base + 32);
+        if (f_len > 0) {
+          const int hk = pl.pair_in_b / a.col_tiles;
+          kv4_request_queries<D, NT>(a, ring + kv4_ring_bytes<D, NT>() + f_slot * kv4_query_bytes<D, NT>(), pl.b, hk,
+                                     (pl.pair_in_b - hk * a.col_tiles) * NC);
+        }
       }
       ++f_u;
       const int t = f_t;
@@ -580,15 +613,16 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
     const int n_units = min(w_units - u, pl.units - pl.unit);
     const int hk = pl.pair_in_b / a.col_tiles, col0 = (pl.pair_in_b - hk * a.col_tiles) * NC;
     s.reset();
-    kv4_load_queries<D, NT>(a, s, pl, hk, col0);
     const int t_end = min(pl.len, (pl.unit + n_units) * kKv4Unit), t_all = pl.len - (a.queries - 1) - kKv4Unit;
-    for (int t0 = pl.unit * kKv4Unit; t0 < t_end; t0 += kKv4Unit) {
+    const int t_beg = pl.unit * kKv4Unit;
+    for (int t0 = t_beg; t0 < t_end; t0 += kKv4Unit) {
       async_wait<NS - 2>();              // this lane's copies of the stage have landed
       const uint32_t bad = (bad_of >> (2 * slot)) & 3u;
       __syncwarp();                      // everybody's have, and everybody has read the stage before it, which is filled next
       request();
       async_commit();
       const uint8_t* stage = mine + slot * STAGE;
+      if (t0 == t_beg) kv4_load_queries<D, NT>(a, s, mine + kv4_ring_bytes<D, NT>() + slot * kv4_query_bytes<D, NT>(), pl.len, col0);
       if (bad == 0 && t0 <= t_all) kv4_stage<D, NT, false>(s, stage, t0, 0);
       else kv4_stage<D, NT, true>(s, stage, t0, bad);
       slot = slot + 1 == NS ? 0 : slot + 1;
@@ -596,8 +630,8 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
     // ---- the segment's result: sums over the lanes that hold other tokens of the same columns
     const bool head = pl.unit > 0, whole = !head && n_units == pl.units;
     // the piece that ends the range takes the ring, which nobody fills any more
-    float* part = reinterpret_cast<float*>(mine + (head ? NS * STAGE : 0));
-    if (!whole && lane == 0) part_pair[2 * warp + (head ? 0 : 1)] = pl.pair_first;
+    float* part = reinterpret_cast<float*>(mine + (head ? WARP_BYTES - PART * 4 : 0));
+    if (!whole && lane == 0) pieces[2 * warp + (head ? 0 : 1)] = Kv4Piece{pl.pair_first, pl.units, pl.b, hk, col0, pl.pair_in_b};
     __syncwarp();
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -637,28 +671,27 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
   constexpr int PASS = 128 / D, TASKS = NC / PASS;
   int task = -warp;                      // the warp's next task among those of the pairs so far
   for (int k = 0; k < 2 * CW;) {
-    const long long pair = part_pair[k];
+    const long long pair = pieces[k].pair;
     if (pair < 0) {
       ++k;
       continue;
     }
     int k1 = k + 1;
-    while (k1 < 2 * CW && (part_pair[k1] < 0 || part_pair[k1] == pair)) ++k1;
+    while (k1 < 2 * CW && (pieces[k1].pair < 0 || pieces[k1].pair == pair)) ++k1;
     task += TASKS;
     if (task > 0) {
-      const Kv4Place pl = kv4_place(a, pref, pair);
-      const int hk = pl.pair_in_b / a.col_tiles, col0 = (pl.pair_in_b - hk * a.col_tiles) * NC;
-      const bool done = pair >= c_beg && pair + pl.units <= c_beg + c_units;
+      const Kv4Piece pc = pieces[k];
+      const bool done = pair >= c_beg && pair + pc.units <= c_beg + c_units;
       float* ws = a.parts + (static_cast<size_t>(blockIdx.x) * 2 + (pair < c_beg ? 0 : 1)) * PART;
       if (!done && pair >= c_beg && task == TASKS && lane == 0)
-        a.splits[blockIdx.x] = Kv4Split{pl.b, pl.pair_in_b, static_cast<int>(kv4_cta_of(total, ctas, pair + pl.units - 1)), 0};
+        a.splits[blockIdx.x] = Kv4Split{pc.b, pc.pair_in_b, static_cast<int>(kv4_cta_of(total, ctas, pair + pc.units - 1)), 0};
       for (; task > 0; task -= CW) {
         const int col = (TASKS - task) * PASS + lane * 4 / D, d = (lane * 4) % D;
         float top = kKv4Low, l = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int i = k; i < k1; ++i)
-          if (part_pair[i] >= 0) {
-            const float* q = reinterpret_cast<const float*>(kv4_mem + (i >> 1) * WARP_BYTES + ((i & 1) ? 0 : NS * STAGE));
+          if (pieces[i].pair >= 0) {
+            const float* q = reinterpret_cast<const float*>(kv4_mem + (i >> 1) * WARP_BYTES + ((i & 1) ? 0 : WARP_BYTES - PART * 4));
             const float2 ml = *reinterpret_cast<const float2*>(q + NC * D + 2 * col);
             const float4 x = *reinterpret_cast<const float4*>(q + col * D + d);
             const float mx = fmaxf(top, ml.x), f0 = ex2_approx(top - mx), f1 = ex2_approx(ml.x - mx);
@@ -667,9 +700,9 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
             v = make_float4(fmaf(x.x, f1, v.x * f0), fmaf(x.y, f1, v.y * f0), fmaf(x.z, f1, v.z * f0), fmaf(x.w, f1, v.w * f0));
           }
         if (done) {
-          if (col0 + col < a.cols) {
+          if (pc.col0 + col < a.cols) {
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            kv4_store4(kv4_out<D>(a, pl.b, hk, col0 + col) + d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+            kv4_store4(kv4_out<D>(a, pc.b, pc.hk, pc.col0 + col) + d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
           }
         } else {
           *reinterpret_cast<float4*>(ws + col * D + d) = v;
@@ -681,52 +714,34 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
   }
 }
 
-// Merges the pieces of the pair that begins in CTA blockIdx.x of the kernel above and ends in a later one.  One CTA per
-// column; the warps take the pieces in turn.
+// Merges the pieces of the pair that begins in CTA blockIdx.x of the kernel above and ends in a later one, one warp per
+// column.
 template <int D, int NT>
-__global__ void __launch_bounds__(256) kv4_attn_join_kernel(const Kv4AttnArgs a) {
+__global__ void __launch_bounds__(NT * 256) kv4_attn_join_kernel(const Kv4AttnArgs a) {
   constexpr int NC = NT * 8, PART = kv4_partial_floats<D, NT>(), V = D / 32;
-  __shared__ float sm[8], sl[8], so[8][D];
   pdl_wait();
-  const int first = blockIdx.x, col = blockIdx.y;
+  const int first = blockIdx.x, col = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Kv4Split sp = a.splits[first];
   if (sp.last < 0) return;
   const int hk = sp.pair_in_b / a.col_tiles, out_col = (sp.pair_in_b - hk * a.col_tiles) * NC + col;
   if (out_col >= a.cols) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  auto piece = [&](int i) { return a.parts + (static_cast<size_t>(i) * 2 + (i == first ? 1 : 0)) * PART; };
   float m = kKv4Low, l = 0.f, o[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) o[e] = 0.f;
 #pragma unroll 4
-  for (int i = first + warp; i <= sp.last; i += 8) {
-    const float* q = piece(i);
+  for (int i = first; i <= sp.last; ++i) {   // piece 1 of the first CTA, piece 0 of the others
+    const float* q = a.parts + (static_cast<size_t>(i) * 2 + (i == first ? 1 : 0)) * PART;
     const float2 ml = *reinterpret_cast<const float2*>(q + NC * D + 2 * col);
     const float mn = fmaxf(m, ml.x), f0 = ex2_approx(m - mn), f1 = ex2_approx(ml.x - mn);
     m = mn;
-    l = l * f0 + ml.y * f1;
+    l = fmaf(l, f0, ml.y * f1);
 #pragma unroll
-    for (int e = 0; e < V; ++e) o[e] = o[e] * f0 + q[col * D + e * 32 + lane] * f1;
+    for (int e = 0; e < V; ++e) o[e] = fmaf(o[e], f0, q[col * D + e * 32 + lane] * f1);
   }
-  if (lane == 0) {
-    sm[warp] = m;
-    sl[warp] = l;
-  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  half_t* dst = kv4_out<D>(a, sp.b, hk, out_col);
 #pragma unroll
-  for (int e = 0; e < V; ++e) so[warp][e * 32 + lane] = o[e];
-  __syncthreads();
-  if (threadIdx.x < D) {
-    float top = kKv4Low, L = 0.f, O = 0.f;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) top = fmaxf(top, sm[w]);
-#pragma unroll
-    for (int w = 0; w < 8; ++w) {
-      const float f = ex2_approx(sm[w] - top);
-      L += sl[w] * f;
-      O += so[w][threadIdx.x] * f;
-    }
-    kv4_out<D>(a, sp.b, hk, out_col)[threadIdx.x] = f_to_h(L == 0.f ? 0.f : O / L);
-  }
+  for (int e = 0; e < V; ++e) dst[e * 32 + lane] = f_to_h(o[e] * inv);
 }
 
 }  // namespace thinfer
