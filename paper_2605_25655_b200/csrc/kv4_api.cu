@@ -57,6 +57,14 @@ Kv4Cache make_cache(const void* pool, const int32_t* table, int32_t rows, int32_
 
 bool stride_ok(int64_t stride, int64_t least) { return stride >= least && stride % 8 == 0; }
 
+// Lane groups of head_dim / 8 lanes that share the rows of one token: as many as fill the device twice (2048 threads an
+// SM), one row each at most.
+int share(int64_t tokens, int64_t rows, int head_dim) {
+  const int64_t want = 2 * static_cast<int64_t>(op_sm_count()) * 2048 / (head_dim / 8);
+  const int64_t n = (want + tokens - 1) / tokens;
+  return static_cast<int>(n < 1 ? 1 : n > rows ? rows : n);
+}
+
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + nb && y < x + na;
@@ -170,7 +178,7 @@ int thinfer_op_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int6
   a.n_kv = n_kv_heads;
   a.half = rotary_dim / 2;
   a.eps = eps;
-  a.chunks = n_q_heads + n_kv_heads;
+  a.chunks = share(tokens, static_cast<int64_t>(n_q_heads) + n_kv_heads, head_dim);
   const int64_t groups = static_cast<int64_t>(tokens) * a.chunks, per_cta = 256 / (head_dim / 8);
   const int64_t ctas = (groups + per_cta - 1) / per_cta;
   if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "qk_norm_rope: too many tokens");
@@ -203,11 +211,12 @@ int thinfer_op_kv4_append(void* pool, int32_t n_pages, const int32_t* table, int
   a.rows = rows;
   a.positions = positions;
   a.tokens = tokens;
+  a.chunks = share(tokens, 2 * static_cast<int64_t>(n_kv_heads), head_dim);
   a.k = static_cast<const half_t*>(k);
   a.v = static_cast<const half_t*>(v);
   a.k_stride = k_stride;
   a.v_stride = v_stride;
-  const int64_t per_cta = 256 / (head_dim / 8), ctas = (static_cast<int64_t>(tokens) * 2 * n_kv_heads + per_cta - 1) / per_cta;
+  const int64_t per_cta = 256 / (head_dim / 8), ctas = (static_cast<int64_t>(tokens) * a.chunks + per_cta - 1) / per_cta;
   if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "kv4_append: too many tokens");
   return op_launch(head_dim == 128 ? kv4_append_kernel<128> : kv4_append_kernel<64>, dim3(static_cast<unsigned>(ctas)),
                    dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), false, a);
@@ -229,11 +238,12 @@ int thinfer_op_kv4_read(const void* pool, int32_t n_pages, const int32_t* table,
   a.rows = rows;
   a.positions = positions;
   a.tokens = tokens;
+  a.chunks = share(tokens, 2 * static_cast<int64_t>(n_kv_heads), head_dim);
   a.k_out = static_cast<half_t*>(k_out);
   a.v_out = static_cast<half_t*>(v_out);
   a.k_stride = a.v_stride = token_stride;
   a.k_head = a.v_head = head_stride;
-  const int64_t per_cta = 256 / (head_dim / 8), ctas = (static_cast<int64_t>(tokens) * 2 * n_kv_heads + per_cta - 1) / per_cta;
+  const int64_t per_cta = 256 / (head_dim / 8), ctas = (static_cast<int64_t>(tokens) * a.chunks + per_cta - 1) / per_cta;
   if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "kv4_read: too many tokens");
   return op_launch(head_dim == 128 ? kv4_read_kernel<128> : kv4_read_kernel<64>, dim3(static_cast<unsigned>(ctas)),
                    dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), false, a);

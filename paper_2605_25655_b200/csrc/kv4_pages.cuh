@@ -326,13 +326,21 @@ __global__ void __launch_bounds__(256) kv4_copy_pages_kernel(uint8_t* pool, cons
     uint4* dst = reinterpret_cast<uint4*>(pool + base + static_cast<size_t>(mv.dst) * page_bytes);
     const int codes = filled * d / 32, params = filled / 4;  // 16-byte pieces of one of the two code and param parts
     const int pieces = 2 * (codes + params);
-    for (int u = lane; u < pieces; u += 32) {
-      int at;
-      if (u < codes) at = u;
-      else if (u < 2 * codes) at = page * d / 32 + (u - codes);
-      else if (u < 2 * codes + params) at = page * d / 16 + (u - 2 * codes);
-      else at = page * (d + 4) / 16 + (u - 2 * codes - params);
-      dst[at] = src[at];
+    auto at = [&](int u) {
+      if (u < codes) return u;
+      if (u < 2 * codes) return page * d / 32 + (u - codes);
+      if (u < 2 * codes + params) return page * d / 16 + (u - 2 * codes);
+      return page * (d + 4) / 16 + (u - 2 * codes - params);
+    };
+    constexpr int U = 8;   // 16-byte pieces in flight per lane
+    for (int u0 = lane; u0 < pieces; u0 += 32 * U) {
+      uint4 v[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (u0 + 32 * i < pieces) v[i] = ld_stream(src + at(u0 + 32 * i));
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (u0 + 32 * i < pieces) dst[at(u0 + 32 * i)] = v[i];
     }
   }
 }

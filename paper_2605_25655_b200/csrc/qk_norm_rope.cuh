@@ -8,7 +8,9 @@
 // about ten FP32 operations, so a row of D values belongs to D / 8 lanes with one 16-byte access each; nothing goes
 // through shared memory.  The angle is reduced in FP64 (position times turns keeps 2^-22 of a turn at position 2^31)
 // and only its fraction goes to FP32; sine and cosine are computed once per token and lane and reused for all the
-// heads that a lane group walks.
+// heads that a lane group walks, four rows in flight at a time.  How many groups share the heads of a token is set so
+// that the device is full about twice: one group per head for a few tokens, a few for a long prompt (16384 tokens of 80
+// heads: 404 us with one group per head, where the sines cost more than the memory).
 #pragma once
 #include "common.cuh"
 
@@ -55,47 +57,53 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const QkNormRopeArgs 
   const int step = HALVES ? a.half / 8 : 0;                       // lanes between the two halves of a pair
   const int partner = HALVES && rotated ? (e0 < a.half ? lane + step : lane - step) : lane;
   const float sign = e0 < a.half ? -1.f : 1.f;
-  for (int h0 = 0; h0 < heads; h0 += a.chunks) {
-    const int h = h0 + chunk;
-    const bool on = live && h < heads;
-    const bool is_q = h < a.n_q;
-    uint4 raw = make_uint4(0, 0, 0, 0), graw = make_uint4(0, 0, 0, 0);
-    if (on) {
-      const half_t* src = is_q ? a.q + token * a.q_stride + static_cast<long long>(h) * D
-                               : a.k + token * a.k_stride + static_cast<long long>(h - a.n_q) * D;
-      raw = *reinterpret_cast<const uint4*>(src + e0);
-      graw = ldg_cached((is_q ? a.q_gain : a.k_gain) + e0);
+  const uint4 gq = ldg_cached(a.q_gain + e0), gk = ldg_cached(a.k_gain + e0);
+  const half_t* const q = a.q + token * a.q_stride + e0;
+  const half_t* const k = a.k + token * a.k_stride + e0;
+  half_t* const q_out = a.q_out + token * a.q_out_stride + e0;
+  half_t* const k_out = a.k_out + token * a.k_out_stride + e0;
+  constexpr int U = 4;
+  for (int h0 = 0; h0 < heads; h0 += U * a.chunks) {
+    uint4 raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int h = h0 + u * a.chunks + chunk;
+      raw[u] = make_uint4(0, 0, 0, 0);
+      if (live && h < heads)
+        raw[u] = *reinterpret_cast<const uint4*>(h < a.n_q ? q + static_cast<long long>(h) * D : k + static_cast<long long>(h - a.n_q) * D);
     }
-    float x[8], g[8];
-    unpack8(raw, x);
-    unpack8(graw, g);
-    float ss = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
+    for (int u = 0; u < U; ++u) {
+      if (h0 + u * a.chunks >= heads) break;                       // the same for the whole warp: the shuffles need all of it
+      const int h = h0 + u * a.chunks + chunk;
+      float x[8], g[8];
+      unpack8(raw[u], x);
+      unpack8(h < a.n_q ? gq : gk, g);
+      float ss = 0.f;
 #pragma unroll
-    for (int o = LPR / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    const float rstd = rsqrtf(ss / static_cast<float>(D) + a.eps);
+      for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = x[i] * rstd * g[i];
-    float y[8];
-    if (HALVES) {
+      for (int o = LPR / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+      const float rstd = rsqrtf(ss / static_cast<float>(D) + a.eps);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float other = __shfl_sync(0xffffffffu, x[i], partner);
-        y[i] = rotated ? x[i] * cs[i] + sign * other * sn[i] : x[i];
+      for (int i = 0; i < 8; ++i) x[i] = x[i] * rstd * g[i];
+      float y[8];
+      if (HALVES) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float other = __shfl_sync(0xffffffffu, x[i], partner);
+          y[i] = rotated ? x[i] * cs[i % NCS] + sign * other * sn[i % NCS] : x[i];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          y[2 * i] = rotated ? x[2 * i] * cs[i] - x[2 * i + 1] * sn[i] : x[2 * i];
+          y[2 * i + 1] = rotated ? x[2 * i + 1] * cs[i] + x[2 * i] * sn[i] : x[2 * i + 1];
+        }
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float c = cs[i % NCS], s = sn[i % NCS];
-        y[2 * i] = rotated ? x[2 * i] * c - x[2 * i + 1] * s : x[2 * i];
-        y[2 * i + 1] = rotated ? x[2 * i + 1] * c + x[2 * i] * s : x[2 * i + 1];
-      }
-    }
-    if (on) {
-      half_t* dst = is_q ? a.q_out + token * a.q_out_stride + static_cast<long long>(h) * D
-                         : a.k_out + token * a.k_out_stride + static_cast<long long>(h - a.n_q) * D;
-      *reinterpret_cast<uint4*>(dst + e0) = make_uint4(pack2(y[0], y[1]), pack2(y[2], y[3]), pack2(y[4], y[5]), pack2(y[6], y[7]));
+      if (live && h < heads)
+        *reinterpret_cast<uint4*>(h < a.n_q ? q_out + static_cast<long long>(h) * D : k_out + static_cast<long long>(h - a.n_q) * D) =
+            make_uint4(pack2(y[0], y[1]), pack2(y[2], y[3]), pack2(y[4], y[5]), pack2(y[6], y[7]));
     }
   }
 }
