@@ -90,11 +90,11 @@ size_t moves_bytes(int32_t most) { return 16 + static_cast<size_t>(most) * sizeo
 int copy_pages(void* pool, const int* count, const PageMove* moves, int most_moves, int layers, int n_kv, int d, int page,
                int n_pages, cudaStream_t st) {
   const size_t page_bytes = static_cast<size_t>(n_kv) * page * (d + 8);
-  const long long items = static_cast<long long>(most_moves) * layers * n_kv;
-  const long long ctas = (items + 7) / 8, room = static_cast<long long>(op_sm_count()) * 8;
-  return op_launch(kv4_copy_pages_kernel, dim3(static_cast<unsigned>(ctas < room ? ctas : room)), dim3(256), 0, st, true,
-                   static_cast<uint8_t*>(pool), count, moves, layers, n_kv, d, page, page_bytes,
-                   page_bytes * static_cast<size_t>(n_pages));
+  const long long units = static_cast<long long>(most_moves) * layers * n_kv * (page / 16);
+  const long long ctas = (units + 15) / 16, room = static_cast<long long>(op_sm_count()) * 8;   // 8 warps, two units each
+  return op_launch(d == 128 ? kv4_copy_pages_kernel<128> : kv4_copy_pages_kernel<64>,
+                   dim3(static_cast<unsigned>(ctas < room ? ctas : room)), dim3(256), 0, st, true, static_cast<uint8_t*>(pool),
+                   count, moves, layers, n_kv, page_shift_of(page), page_bytes, page_bytes * static_cast<size_t>(n_pages));
 }
 
 // Column tiles of 8 (16 where a KV head has more query columns than 8, so that its keys are unpacked half as often) and

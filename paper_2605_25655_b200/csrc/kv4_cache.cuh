@@ -39,6 +39,52 @@ __device__ __forceinline__ Kv4Spot kv4_spot(const Kv4TokensArgs& a, long long to
 
 constexpr int kKv4RowsInFlight = 4;
 
+__device__ __forceinline__ half2_t low_pair(half2_t a, half2_t b) {
+  half2_t d;
+  d.x = a.x;
+  d.y = b.x;
+  return d;
+}
+__device__ __forceinline__ half2_t high_pair(half2_t a, half2_t b) {
+  half2_t d;
+  d.x = a.y;
+  d.y = b.y;
+  return d;
+}
+// Largest of packed pairs, a NaN if there is one.
+__device__ __forceinline__ half2_t max2_nan(half2_t a, half2_t b) { return __hmax2_nan(a, b); }
+
+// Codes of eight values of a row with the given offset and scale, four bits each.  The quotient (x - offset) / scale is
+// taken with a reciprocal, off by less than 2^-18, and rounded by adding 1.5 * 2^23; the residual x - offset - c scale
+// then tells how far it was from the border between two codes.  Within 2^-16 of one, or with a scale too small for a
+// reciprocal, `sure` comes back false and the caller divides.
+__device__ __forceinline__ uint32_t kv4_codes_fast(const float (&x)[8], float lo, float scale, bool& sure) {
+  constexpr float MAGIC = 12582912.f;
+  constexpr uint32_t M = 0x4b400000u;
+  const float inv = __fdividef(1.f, scale);
+  float far = 0.f;
+  uint32_t word = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float d = x[j] - lo, t = fmaf(d, inv, MAGIC), e = fmaf(MAGIC - t, scale, d);
+    far = fmaxf(far, fabsf(e));
+    word += static_cast<uint32_t>(__float_as_int(t)) << (4 * j);
+  }
+  // a normal scale is within 2^-8 of (max - min) / 15, so that no code can pass 15
+  const float smallest = kStorageType == 1 ? 0x1p-100f : 0x1p-14f;
+  sure = scale >= smallest && scale < 0x1p100f && far <= scale * (0.5f - 0x1p-16f);
+  return word - (M + (M << 4) + (M << 8) + (M << 12) + (M << 16) + (M << 20) + (M << 24) + (M << 28));
+}
+__device__ __forceinline__ uint32_t kv4_codes_exact(const float (&x)[8], float lo, float scale) {
+  uint32_t word = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float c = scale > 0.f ? fminf(rintf(__fdiv_rn(x[j] - lo, scale)), 15.f) : 0.f;
+    word |= static_cast<uint32_t>(c) << (4 * j);
+  }
+  return word;
+}
+
 template <int D>
 __global__ void __launch_bounds__(256) kv4_append_kernel(const Kv4TokensArgs a) {
   constexpr int LPR = D / 8, U = kKv4RowsInFlight;
@@ -63,28 +109,24 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(const Kv4TokensArgs a) 
     for (int u = 0; u < U; ++u) {
       if (r0 + u * a.chunks >= rows) break;           // the same for the whole warp: the shuffles need all of it
       const int r = r0 + u * a.chunks + chunk;
-      float x[8];
-      unpack8(raw[u], x);
-      float lo = x[0], hi = x[0], probe = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        lo = fminf(lo, x[j]);
-        hi = fmaxf(hi, x[j]);
-        probe += x[j] * 0.f;  // NaN as soon as one value is NaN or infinite
-      }
+      // largest value and largest negated value of the row, as a pair: both are exact in 16 bits
+      const half2_t* h = reinterpret_cast<const half2_t*>(&raw[u]);
+      const half2_t up = max2_nan(max2_nan(h[0], h[1]), max2_nan(h[2], h[3]));
+      const half2_t down = max2_nan(max2_nan(__hneg2(h[0]), __hneg2(h[1])), max2_nan(__hneg2(h[2]), __hneg2(h[3])));
+      half2_t ends = max2_nan(low_pair(up, down), high_pair(up, down));
 #pragma unroll
       for (int o = LPR / 2; o > 0; o >>= 1) {
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-        probe += __shfl_xor_sync(0xffffffffu, probe, o);
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<const uint32_t*>(&ends), o);
+        ends = max2_nan(ends, *reinterpret_cast<const half2_t*>(&other));
       }
+      const float2 hl = h2_to_f2(ends);
+      const float hi = hl.x, lo = -hl.y, probe = (hi - lo) * 0.f;   // probe: NaN as soon as one value is NaN or infinite
       const float scale = h_to_f(f_to_h(__fdiv_rn(hi - lo, 15.f)));
-      uint32_t word = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float c = scale > 0.f ? fminf(rintf(__fdiv_rn(x[j] - lo, scale)), 15.f) : 0.f;
-        word |= static_cast<uint32_t>(c) << (4 * j);
-      }
+      float x[8];
+      unpack8(raw[u], x);
+      bool sure;
+      uint32_t word = kv4_codes_fast(x, lo, scale, sure);
+      if (!sure) word = kv4_codes_exact(x, lo, scale);
       if (s.page != nullptr && r < rows) {
         const bool is_v = r >= a.c.n_kv;
         uint8_t* block = s.page + static_cast<size_t>(is_v ? r - a.c.n_kv : r) * a.c.block_bytes;

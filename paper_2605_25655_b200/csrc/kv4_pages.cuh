@@ -98,9 +98,19 @@ struct PageMap {
       if (32 * mid - before[mid] <= k) lo = mid;
       else hi = mid - 1;
     }
+    // the (k+1)-th set bit of the word, by halves
     uint32_t z = ~bits[lo];
-    for (int i = k - (32 * lo - before[lo]); i > 0; --i) z &= z - 1;
-    return 32 * lo + __ffs(z) - 1;
+    int left = k - (32 * lo - before[lo]), at = 0;
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) {
+      const int n = __popc(z & ((1u << w) - 1u));
+      if (left >= n) {
+        left -= n;
+        at += w;
+        z >>= w;
+      }
+    }
+    return 32 * lo + at;
   }
 };
 
@@ -145,8 +155,9 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_reserve_kernel(const PageTab
     *after = static_cast<long long>(n) + a;
     return static_cast<int>(((*after + (1 << t.page_shift) - 1) >> t.page_shift) - *first);
   };
-  int first;
-  long long after;
+  int first = 0;
+  long long after = 0;
+  const int lane = threadIdx.x & 31;
   for (int r = threadIdx.x; r < t.rows; r += blockDim.x)
     if (need_of(r, &first, &after) > 0) wanted = 1;
   __syncthreads();
@@ -167,13 +178,15 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_reserve_kernel(const PageTab
       // a row that claims more tokens than its table can name is refused as well
       const bool fits = t.lens[r] <= (static_cast<long long>(t.max_pages) << t.page_shift) &&
                         (need == 0 || (begin + need <= free_pages && first + need <= t.max_pages));
-      if (fits) {
-        for (int j = 0; j < need; ++j)
-          table[static_cast<size_t>(r) * t.max_pages + first + j] = m.free_page(static_cast<int>(begin) + j);
-      } else {
-        atomicAdd(&bad, 1);
-      }
+      if (!fits) atomicAdd(&bad, 1);
       lens_out[r] = fits ? static_cast<int>(after) : t.lens[r];
+      need = fits ? need : 0;
+    }
+    // the pages of 32 rows at a time, one warp per 32 rows, its lanes over the pages of a row
+    for (int l = 0; l < 32 && __any_sync(0xffffffffu, need > 0 && lane >= l); ++l) {
+      const int n = __shfl_sync(0xffffffffu, need, l), f = __shfl_sync(0xffffffffu, first, l), row = __shfl_sync(0xffffffffu, r, l);
+      const int k = __shfl_sync(0xffffffffu, static_cast<int>(begin), l);
+      for (int j = lane; j < n; j += 32) table[static_cast<size_t>(row) * t.max_pages + f + j] = m.free_page(k + j);
     }
     __syncthreads();
   }
@@ -305,42 +318,56 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_compact_kernel(const PageTab
 }
 
 // ---------------------------------------------------------------- the copies
-// A warp takes one (move, layer, head) block at a time and copies the filled tokens, 16 at a time, of its four parts.
+// A warp takes 16 tokens of one (move, layer, head) block at a time: D / 4 pieces of 16 bytes of K codes, as many of V
+// codes and four of each kind of params.  Two such units are in flight at a time.
+template <int D>
 __global__ void __launch_bounds__(256) kv4_copy_pages_kernel(uint8_t* pool, const int* move_count, const PageMove* moves,
-                                                             int layers, int n_kv, int d, int page, size_t page_bytes,
+                                                             int layers, int n_kv, int page_shift, size_t page_bytes,
                                                              size_t layer_bytes) {
+  constexpr int R = D / 64, U = 2;     // rows of 32 pieces of each kind of codes
   pdl_wait();
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, page = 1 << page_shift, group_shift = page_shift - 4;
   const long long warps = static_cast<long long>(gridDim.x) * (blockDim.x >> 5);
   const long long first = static_cast<long long>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5);
-  const int per_move = layers * n_kv;
-  const long long items = static_cast<long long>(*move_count) * per_move;
-  const int block = page * (d + 8);
-  for (long long i = first; i < items; i += warps) {
-    const int k = static_cast<int>(i / per_move), rest = static_cast<int>(i - static_cast<long long>(k) * per_move);
-    const int layer = rest / n_kv, head = rest - layer * n_kv;
-    const PageMove mv = moves[k];
-    const int filled = min(page, (mv.tokens + 15) & ~15);
-    const size_t base = static_cast<size_t>(layer) * layer_bytes + static_cast<size_t>(head) * block;
-    const uint4* src = reinterpret_cast<const uint4*>(pool + base + static_cast<size_t>(mv.src) * page_bytes);
-    uint4* dst = reinterpret_cast<uint4*>(pool + base + static_cast<size_t>(mv.dst) * page_bytes);
-    const int codes = filled * d / 32, params = filled / 4;  // 16-byte pieces of one of the two code and param parts
-    const int pieces = 2 * (codes + params);
-    auto at = [&](int u) {
-      if (u < codes) return u;
-      if (u < 2 * codes) return page * d / 32 + (u - codes);
-      if (u < 2 * codes + params) return page * d / 16 + (u - 2 * codes);
-      return page * (d + 4) / 16 + (u - 2 * codes - params);
-    };
-    constexpr int U = 8;   // 16-byte pieces in flight per lane
-    for (int u0 = lane; u0 < pieces; u0 += 32 * U) {
-      uint4 v[U];
+  const int blocks = layers * n_kv;    // of one move
+  const long long units = (static_cast<long long>(*move_count) * blocks) << group_shift;
+  for (long long i0 = first; i0 < units; i0 += U * warps) {
+    uint4 v[U][2 * R + 1];
+    uint8_t* dst[U];
 #pragma unroll
-      for (int i = 0; i < U; ++i)
-        if (u0 + 32 * i < pieces) v[i] = ld_stream(src + at(u0 + 32 * i));
+    for (int u = 0; u < U; ++u) {
+      const long long i = i0 + u * warps;
+      dst[u] = nullptr;
+      if (i >= units) continue;
+      const long long b = i >> group_shift;
+      const int g = static_cast<int>(i) & ((1 << group_shift) - 1);
+      const int k = (b >> 32) == 0 ? static_cast<int>(static_cast<uint32_t>(b) / static_cast<uint32_t>(blocks)) : static_cast<int>(b / blocks);
+      const int rest = static_cast<int>(b - static_cast<long long>(k) * blocks), layer = rest / n_kv, head = rest - layer * n_kv;
+      const PageMove mv = moves[k];
+      if (16 * g >= mv.tokens) continue;
+      const size_t base = static_cast<size_t>(layer) * layer_bytes + static_cast<size_t>(head) * (page * (D + 8)) + g * (8 * D);
+      const uint8_t* src = pool + base + static_cast<size_t>(mv.src) * page_bytes;
+      dst[u] = pool + base + static_cast<size_t>(mv.dst) * page_bytes;
 #pragma unroll
-      for (int i = 0; i < U; ++i)
-        if (u0 + 32 * i < pieces) dst[at(u0 + 32 * i)] = v[i];
+      for (int r = 0; r < R; ++r) {
+        v[u][r] = ld_stream(src + (r * 32 + lane) * 16);
+        v[u][R + r] = ld_stream(src + page * (D / 2) + (r * 32 + lane) * 16);
+      }
+      // params: lanes 0-3 of K, 4-7 of V; 64 bytes for 16 tokens, 8 D back to the start of the block's codes
+      const int par = page * D - g * (8 * D) + g * 64 + (lane & 4 ? page * 4 : 0) + (lane & 3) * 16;
+      if (lane < 8) v[u][2 * R] = ld_stream(src + par);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (dst[u] == nullptr) continue;
+      const int g = static_cast<int>(i0 + u * warps) & ((1 << group_shift) - 1);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        *reinterpret_cast<uint4*>(dst[u] + (r * 32 + lane) * 16) = v[u][r];
+        *reinterpret_cast<uint4*>(dst[u] + page * (D / 2) + (r * 32 + lane) * 16) = v[u][R + r];
+      }
+      const int par = page * D - g * (8 * D) + g * 64 + (lane & 4 ? page * 4 : 0) + (lane & 3) * 16;
+      if (lane < 8) *reinterpret_cast<uint4*>(dst[u] + par) = v[u][2 * R];
     }
   }
 }
