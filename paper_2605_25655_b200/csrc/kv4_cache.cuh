@@ -54,33 +54,52 @@ __device__ __forceinline__ half2_t high_pair(half2_t a, half2_t b) {
 // Largest of packed pairs, a NaN if there is one.
 __device__ __forceinline__ half2_t max2_nan(half2_t a, half2_t b) { return __hmax2_nan(a, b); }
 
+// x / 15, correctly rounded: a product with the rounded reciprocal and one correction by the exact residual (Markstein's
+// division theorem).
+__device__ __forceinline__ float by_15(float x) {
+  const float q = x * (1.f / 15.f);
+  return fmaf(fmaf(-15.f, q, x), 1.f / 15.f, q);
+}
+
 // Codes of eight values of a row with the given offset and scale, four bits each.  The quotient (x - offset) / scale is
-// taken with a reciprocal, off by less than 2^-18, and rounded by adding 1.5 * 2^23; the residual x - offset - c scale
-// then tells how far it was from the border between two codes.  Within 2^-16 of one, or with a scale too small for a
-// reciprocal, `sure` comes back false and the caller divides.
-__device__ __forceinline__ uint32_t kv4_codes_fast(const float (&x)[8], float lo, float scale, bool& sure) {
+// taken with a reciprocal, off by less than 2^-18, and rounded by adding 1.5 * 2^23.  The residual x - offset - c scale,
+// which is exact where it matters, then tells on which side of the border between two codes the quotient lies: beyond
+// half a scale the code moves by one, at exactly half (common: 16-bit values lie on a grid) to the even one.
+// A scale too small for a reciprocal is left to a division.
+__device__ __forceinline__ uint32_t kv4_codes(const float (&x)[8], float lo, float scale) {
   constexpr float MAGIC = 12582912.f;
   constexpr uint32_t M = 0x4b400000u;
-  const float inv = __fdividef(1.f, scale);
-  float far = 0.f;
-  uint32_t word = 0;
+  const float inv = __fdividef(1.f, scale), half = 0.5f * scale;
+  float far = 0.f, e[8];
+  uint32_t c[8], word = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float d = x[j] - lo, t = fmaf(d, inv, MAGIC), e = fmaf(MAGIC - t, scale, d);
-    far = fmaxf(far, fabsf(e));
-    word += static_cast<uint32_t>(__float_as_int(t)) << (4 * j);
+    const float d = x[j] - lo, t = fmaf(d, inv, MAGIC);
+    e[j] = fmaf(MAGIC - t, scale, d);
+    c[j] = static_cast<uint32_t>(__float_as_int(t));
+    far = fmaxf(far, fabsf(e[j]));
+    word += c[j] << (4 * j);
   }
   // a normal scale is within 2^-8 of (max - min) / 15, so that no code can pass 15
   const float smallest = kStorageType == 1 ? 0x1p-100f : 0x1p-14f;
-  sure = scale >= smallest && scale < 0x1p100f && far <= scale * (0.5f - 0x1p-16f);
-  return word - (M + (M << 4) + (M << 8) + (M << 12) + (M << 16) + (M << 20) + (M << 24) + (M << 28));
-}
-__device__ __forceinline__ uint32_t kv4_codes_exact(const float (&x)[8], float lo, float scale) {
-  uint32_t word = 0;
+  if (scale >= smallest && scale < 0x1p100f) {
+    if (far > scale * (0.5f - 0x1p-16f)) {
+      word = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const bool odd = c[j] & 1u;
+        if (e[j] > half || (e[j] == half && odd)) ++c[j];
+        if (e[j] < -half || (e[j] == -half && odd)) --c[j];
+        word += c[j] << (4 * j);
+      }
+    }
+    return word - (M + (M << 4) + (M << 8) + (M << 12) + (M << 16) + (M << 20) + (M << 24) + (M << 28));
+  }
+  word = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float c = scale > 0.f ? fminf(rintf(__fdiv_rn(x[j] - lo, scale)), 15.f) : 0.f;
-    word |= static_cast<uint32_t>(c) << (4 * j);
+    const float q = scale > 0.f ? fminf(rintf(__fdiv_rn(x[j] - lo, scale)), 15.f) : 0.f;
+    word |= static_cast<uint32_t>(q) << (4 * j);
   }
   return word;
 }
@@ -121,12 +140,10 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(const Kv4TokensArgs a) 
       }
       const float2 hl = h2_to_f2(ends);
       const float hi = hl.x, lo = -hl.y, probe = (hi - lo) * 0.f;   // probe: NaN as soon as one value is NaN or infinite
-      const float scale = h_to_f(f_to_h(__fdiv_rn(hi - lo, 15.f)));
+      const float scale = h_to_f(f_to_h(by_15(hi - lo)));
       float x[8];
       unpack8(raw[u], x);
-      bool sure;
-      uint32_t word = kv4_codes_fast(x, lo, scale, sure);
-      if (!sure) word = kv4_codes_exact(x, lo, scale);
+      const uint32_t word = kv4_codes(x, lo, scale);
       if (s.page != nullptr && r < rows) {
         const bool is_v = r >= a.c.n_kv;
         uint8_t* block = s.page + static_cast<size_t>(is_v ? r - a.c.n_kv : r) * a.c.block_bytes;
@@ -145,7 +162,7 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(const Kv4TokensArgs a) 
 
 template <int D>
 __global__ void __launch_bounds__(256) kv4_read_kernel(const Kv4TokensArgs a) {
-  constexpr int LPR = D / 8, U = kKv4RowsInFlight;
+  constexpr int LPR = D / 8, U = 2 * kKv4RowsInFlight;   // rows are a quarter as large here
   const int sub = (threadIdx.x & 31) % LPR;
   const long long group = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) / LPR;
   const long long token = group / a.chunks;
@@ -177,9 +194,16 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(const Kv4TokensArgs a) {
       const int r = r0 + u * a.chunks;
       if (r >= rows) break;
       const float2 p = kv4_unpack_params(par[u]);
+      // two codes at a time as the low mantissa bits of FP16 numbers: code * 2^-24, or 2^-20 from the high nibbles
       float x[8];
+      const float s0 = p.x * 0x1p24f, s1 = p.x * 0x1p20f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = fmaf(p.x, static_cast<float>((word[u] >> (4 * j)) & 15u), p.y);
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t b = (j & 2 ? word[u] >> 8 : word[u]) & (j & 1 ? 0x00f000f0u : 0x000f000fu);
+        const float2 c = __half22float2(*reinterpret_cast<const __half2*>(&b));
+        x[j] = fmaf(j & 1 ? s1 : s0, c.x, p.y);
+        x[j + 4] = fmaf(j & 1 ? s1 : s0, c.y, p.y);
+      }
       half_t* dst = r < a.c.n_kv ? a.k_out + token * a.k_stride + r * a.k_head : a.v_out + token * a.v_stride + (r - a.c.n_kv) * a.v_head;
       *reinterpret_cast<uint4*>(dst + sub * 8) = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
     }

@@ -31,7 +31,7 @@ struct QkNormRopeArgs {
 };
 
 template <int D, bool HALVES>
-__global__ void __launch_bounds__(256) qk_norm_rope_kernel(const QkNormRopeArgs a) {
+__global__ void __launch_bounds__(256, 4) qk_norm_rope_kernel(const QkNormRopeArgs a) {
   constexpr int LPR = D / 8;        // lanes per row
   constexpr int U = 4;
   const int lane = threadIdx.x & 31, sub = lane % LPR;
