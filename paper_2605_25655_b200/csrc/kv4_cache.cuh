@@ -104,38 +104,35 @@ __device__ __forceinline__ uint32_t kv4_codes(const float (&x)[8], float lo, flo
   return word;
 }
 
-template <int D>
-__global__ void __launch_bounds__(256) kv4_append_kernel(const Kv4TokensArgs a) {
+// Heads chunk, chunk + chunks, ... of K and then of V, as one sequence of 2 n_kv rows: the first head of V.
+__device__ __forceinline__ int kv4_first_v(int chunk, int chunks, int n_kv) {
+  return chunk >= n_kv ? chunk - n_kv : (chunks - (n_kv - chunk) % chunks) % chunks;
+}
+
+template <int D, bool V>
+__device__ __forceinline__ void kv4_append_rows(const Kv4TokensArgs& a, const Kv4Spot& s, const half_t* src, int first, unsigned mask, int sub) {
   constexpr int LPR = D / 8, U = kKv4RowsInFlight;
-  const int sub = (threadIdx.x & 31) % LPR;
-  const long long group = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) / LPR;
-  const long long token = group / a.chunks;
-  const int chunk = static_cast<int>(group - token * a.chunks), rows = 2 * a.c.n_kv;
-  const Kv4Spot s = kv4_spot(a, token);
-  const half_t* const k = a.k + token * a.k_stride + sub * 8;
-  const half_t* const v = a.v + token * a.v_stride + sub * 8;
-  const int page = 1 << a.c.page_shift;
-  for (int r0 = 0; r0 < rows; r0 += U * a.chunks) {   // K of all heads, then V of all heads
+  const int n = a.c.n_kv, page = 1 << a.c.page_shift, step = a.chunks;
+  uint8_t* const params = s.page + page * D + (V ? page * 4 : 0) + s.slot * 4;
+  uint8_t* const codes = s.page + (V ? page * (D / 2) + (s.slot >> 1) * D + sub * 8 + (s.slot & 1) * 2 : s.slot * (D / 2) + sub * 4);
+  src += sub * 8;
+  for (int h0 = first; h0 < n; h0 += U * step) {
     uint4 raw[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int r = r0 + u * a.chunks + chunk;
-      raw[u] = make_uint4(0, 0, 0, 0);
-      if (s.page != nullptr && r < rows)
-        raw[u] = *reinterpret_cast<const uint4*>(r < a.c.n_kv ? k + static_cast<long long>(r) * D : v + static_cast<long long>(r - a.c.n_kv) * D);
-    }
+    for (int u = 0; u < U; ++u)
+      if (h0 + u * step < n) raw[u] = *reinterpret_cast<const uint4*>(src + (h0 + u * step) * D);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (r0 + u * a.chunks >= rows) break;           // the same for the whole warp: the shuffles need all of it
-      const int r = r0 + u * a.chunks + chunk;
+      const int h = h0 + u * step;
+      if (h >= n) break;
       // largest value and largest negated value of the row, as a pair: both are exact in 16 bits
-      const half2_t* h = reinterpret_cast<const half2_t*>(&raw[u]);
-      const half2_t up = max2_nan(max2_nan(h[0], h[1]), max2_nan(h[2], h[3]));
-      const half2_t down = max2_nan(max2_nan(__hneg2(h[0]), __hneg2(h[1])), max2_nan(__hneg2(h[2]), __hneg2(h[3])));
+      const half2_t* x2 = reinterpret_cast<const half2_t*>(&raw[u]);
+      const half2_t up = max2_nan(max2_nan(x2[0], x2[1]), max2_nan(x2[2], x2[3]));
+      const half2_t down = max2_nan(max2_nan(__hneg2(x2[0]), __hneg2(x2[1])), max2_nan(__hneg2(x2[2]), __hneg2(x2[3])));
       half2_t ends = max2_nan(low_pair(up, down), high_pair(up, down));
 #pragma unroll
       for (int o = LPR / 2; o > 0; o >>= 1) {
-        const uint32_t other = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<const uint32_t*>(&ends), o);
+        const uint32_t other = __shfl_xor_sync(mask, *reinterpret_cast<const uint32_t*>(&ends), o);
         ends = max2_nan(ends, *reinterpret_cast<const half2_t*>(&other));
       }
       const float2 hl = h2_to_f2(ends);
@@ -144,55 +141,60 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(const Kv4TokensArgs a) 
       float x[8];
       unpack8(raw[u], x);
       const uint32_t word = kv4_codes(x, lo, scale);
-      if (s.page != nullptr && r < rows) {
-        const bool is_v = r >= a.c.n_kv;
-        uint8_t* block = s.page + static_cast<size_t>(is_v ? r - a.c.n_kv : r) * a.c.block_bytes;
-        if (sub == 0) *reinterpret_cast<uint32_t*>(block + page * D + (is_v ? page * 4 : 0) + s.slot * 4) = kv4_pack_params(scale + probe, lo + probe);
-        if (!is_v) {
-          *reinterpret_cast<uint32_t*>(block + s.slot * (D / 2) + sub * 4) = word;
-        } else {  // two groups of four dimensions, 16 bits each, in the halves that belong to this token of the pair
-          uint16_t* dst = reinterpret_cast<uint16_t*>(block + page * (D / 2) + (s.slot >> 1) * D + sub * 8) + (s.slot & 1);
-          dst[0] = static_cast<uint16_t>(word);
-          dst[2] = static_cast<uint16_t>(word >> 16);
-        }
+      const int at = h * a.c.block_bytes;
+      if (sub == 0) *reinterpret_cast<uint32_t*>(params + at) = kv4_pack_params(scale + probe, lo + probe);
+      if (!V) {
+        *reinterpret_cast<uint32_t*>(codes + at) = word;
+      } else {  // two groups of four dimensions, 16 bits each, in the halves that belong to this token of the pair
+        *reinterpret_cast<uint16_t*>(codes + at) = static_cast<uint16_t>(word);
+        *reinterpret_cast<uint16_t*>(codes + at + 4) = static_cast<uint16_t>(word >> 16);
       }
     }
   }
 }
 
 template <int D>
-__global__ void __launch_bounds__(256) kv4_read_kernel(const Kv4TokensArgs a) {
-  constexpr int LPR = D / 8, U = 2 * kKv4RowsInFlight;   // rows are a quarter as large here
-  const int sub = (threadIdx.x & 31) % LPR;
+__global__ void __launch_bounds__(256, 4) kv4_append_kernel(const Kv4TokensArgs a) {
+  constexpr int LPR = D / 8;
+  const int lane = threadIdx.x & 31, sub = lane % LPR;
+  const unsigned mask = (LPR == 16 ? 0xffffu : 0xffu) << (lane & ~(LPR - 1));
   const long long group = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) / LPR;
   const long long token = group / a.chunks;
-  const int chunk = static_cast<int>(group - token * a.chunks), rows = 2 * a.c.n_kv;
+  const int chunk = static_cast<int>(group - token * a.chunks);
   const Kv4Spot s = kv4_spot(a, token);
-  if (s.skip) return;
-  const int page = 1 << a.c.page_shift;
-  for (int r0 = chunk; r0 < rows; r0 += U * a.chunks) {
+  if (s.page == nullptr) return;      // the same for the group, and shuffles stay inside it
+  kv4_append_rows<D, false>(a, s, a.k + token * a.k_stride, chunk, mask, sub);
+  kv4_append_rows<D, true>(a, s, a.v + token * a.v_stride, kv4_first_v(chunk, a.chunks, a.c.n_kv), mask, sub);
+}
+
+template <int D, bool V>
+__device__ __forceinline__ void kv4_read_rows(const Kv4TokensArgs& a, const Kv4Spot& s, half_t* dst, long long head_stride, int first, int sub) {
+  constexpr int U = 2 * kKv4RowsInFlight;   // rows are a quarter as large here
+  const int n = a.c.n_kv, page = 1 << a.c.page_shift, step = a.chunks;
+  const uint8_t* const params = s.page + page * D + (V ? page * 4 : 0) + s.slot * 4;
+  const uint8_t* const codes = s.page + (V ? page * (D / 2) + (s.slot >> 1) * D + sub * 8 : s.slot * (D / 2) + sub * 4);
+  dst += sub * 8;
+  for (int h0 = first; h0 < n; h0 += U * step) {
     uint32_t word[U], par[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int r = r0 + u * a.chunks;
+      const int at = (h0 + u * step) * a.c.block_bytes;
       word[u] = 0;
       par[u] = 0x7fff7fffu;                            // no page there: NaN
-      if (s.page != nullptr && r < rows) {
-        const bool is_v = r >= a.c.n_kv;
-        const uint8_t* block = s.page + static_cast<size_t>(is_v ? r - a.c.n_kv : r) * a.c.block_bytes;
-        par[u] = *reinterpret_cast<const uint32_t*>(block + page * D + (is_v ? page * 4 : 0) + s.slot * 4);
-        if (!is_v) {
-          word[u] = *reinterpret_cast<const uint32_t*>(block + s.slot * (D / 2) + sub * 4);
+      if (s.page != nullptr && h0 + u * step < n) {
+        par[u] = *reinterpret_cast<const uint32_t*>(params + at);
+        if (!V) {
+          word[u] = *reinterpret_cast<const uint32_t*>(codes + at);
         } else {  // both tokens of the pair: 8 bytes, this token's halves
-          const uint2 w = *reinterpret_cast<const uint2*>(block + page * (D / 2) + (s.slot >> 1) * D + sub * 8);
-          word[u] = s.slot & 1 ? (w.x >> 16) | (w.y & 0xffff0000u) : (w.x & 0xffffu) | (w.y << 16);
+          const uint2 w = *reinterpret_cast<const uint2*>(codes + at);
+          word[u] = __byte_perm(w.x, w.y, s.slot & 1 ? 0x7632 : 0x5410);
         }
       }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int r = r0 + u * a.chunks;
-      if (r >= rows) break;
+      const int h = h0 + u * step;
+      if (h >= n) break;
       const float2 p = kv4_unpack_params(par[u]);
       // two codes at a time as the low mantissa bits of FP16 numbers: code * 2^-24, or 2^-20 from the high nibbles
       float x[8];
@@ -204,10 +206,22 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(const Kv4TokensArgs a) {
         x[j] = fmaf(j & 1 ? s1 : s0, c.x, p.y);
         x[j + 4] = fmaf(j & 1 ? s1 : s0, c.y, p.y);
       }
-      half_t* dst = r < a.c.n_kv ? a.k_out + token * a.k_stride + r * a.k_head : a.v_out + token * a.v_stride + (r - a.c.n_kv) * a.v_head;
-      *reinterpret_cast<uint4*>(dst + sub * 8) = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
+      *reinterpret_cast<uint4*>(dst + h * head_stride) = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
     }
   }
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) kv4_read_kernel(const Kv4TokensArgs a) {
+  constexpr int LPR = D / 8;
+  const int sub = (threadIdx.x & 31) % LPR;
+  const long long group = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) / LPR;
+  const long long token = group / a.chunks;
+  const int chunk = static_cast<int>(group - token * a.chunks);
+  const Kv4Spot s = kv4_spot(a, token);
+  if (s.skip) return;
+  kv4_read_rows<D, false>(a, s, a.k_out + token * a.k_stride, a.k_head, chunk, sub);
+  kv4_read_rows<D, true>(a, s, a.v_out + token * a.v_stride, a.v_head, kv4_first_v(chunk, a.chunks, a.c.n_kv), sub);
 }
 
 }  // namespace thinfer

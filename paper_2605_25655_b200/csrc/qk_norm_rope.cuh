@@ -8,10 +8,10 @@
 // about ten FP32 operations, so a row of D values belongs to D / 8 lanes, with both members of every pair in one lane:
 // neighbours come with one 16-byte access, halves with two of 8 bytes.  Nothing goes through shared memory.  The angle
 // is reduced in FP64 (position times turns keeps 2^-22 of a turn at position 2^31) and only its fraction goes to FP32;
-// sine and cosine are computed once per token and lane and reused for all the heads that a lane group walks, four rows in
-// flight at a time.  How many groups share the heads of a token is set so that the device is full about twice: one group
-// per head for a few tokens, a few for a long prompt (16384 tokens of 80 heads: 402 us with one group per head, where the
-// sines cost more than the memory).
+// sine and cosine are computed once per token and lane and reused for all the heads that a lane group walks, two rows in
+// flight at a time.  How many groups share the heads of a token is set so that the device is full once: one group per head
+// for a few tokens, one or two for a long prompt (16384 tokens of 80 heads: 402 us with one group per head, where the
+// sines cost more than the memory, 125 us with two).
 #pragma once
 #include "common.cuh"
 
@@ -33,7 +33,7 @@ struct QkNormRopeArgs {
 template <int D, bool HALVES>
 __global__ void __launch_bounds__(256, 4) qk_norm_rope_kernel(const QkNormRopeArgs a) {
   constexpr int LPR = D / 8;        // lanes per row
-  constexpr int U = 4;
+  constexpr int U = 2;
   const int lane = threadIdx.x & 31, sub = lane % LPR;
   const unsigned group_mask = (LPR == 16 ? 0xffffu : 0xffu) << (lane & ~(LPR - 1));
   const long long group = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) / LPR;
