@@ -1,15 +1,19 @@
-"""Builds libthinfer.so in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
+"""Builds libthinfer.so in-tree with nvcc for sm_100a (cross-compiles without a GPU), and the torch marshalling module
+_ops.so with the host compiler."""
 from __future__ import annotations
 
 import os
 import shutil
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libthinfer.so")            # IEEE FP16 storage
 LIB_BF16 = os.path.join(HERE, "libthinfer_bf16.so")  # BF16 storage: the same sources with -DTHINFER_BF16
 VARIANTS = ((LIB, []), (LIB_BF16, ["-DTHINFER_BF16"]))
+OPS = os.path.join(HERE, "_ops.so")                  # Python module: torch tensors -> the C entry points
+OPS_SRC = os.path.join(CSRC, "torch_ops.cpp")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
@@ -31,8 +35,25 @@ def sources():
         os.path.join(os.path.dirname(HERE), "include", "thinfer.h")]
 
 
+def _ops_is_stale() -> bool:
+    deps = (OPS_SRC, os.path.join(os.path.dirname(HERE), "include", "thinfer.h"))
+    return not os.path.exists(OPS) or any(os.path.getmtime(s) > os.path.getmtime(OPS) for s in deps)
+
+
+def _ops_command():
+    import torch
+    root = os.path.dirname(torch.__file__)
+    inc, lib = os.path.join(root, "include"), os.path.join(root, "lib")
+    cuda = os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            "-isystem", sysconfig.get_paths()["include"], "-isystem", inc, "-isystem", os.path.join(inc, "torch", "csrc", "api", "include"), "-isystem", cuda,
+            OPS_SRC, "-o", OPS, "-L" + lib, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-Wl,-rpath," + lib]
+
+
 def is_stale(lib: str = None) -> bool:
     libs = [lib] if lib else [v[0] for v in VARIANTS]
+    if lib is None and _ops_is_stale():
+        return True
     for l in libs:
         if not os.path.exists(l):
             return True
@@ -43,8 +64,8 @@ def is_stale(lib: str = None) -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compiles every .cu of csrc/ into one shared library per storage type (the two compilations run side by
-    side); returns the path of the FP16 library."""
+    """Compiles every .cu of csrc/ into one shared library per storage type and torch_ops.cpp into _ops.so (the
+    compilations run side by side); returns the path of the FP16 library."""
     cus = [s for s in sources() if s.endswith(".cu")]
     extra = os.environ.get("THINFER_NVCC_EXTRA", "").split()
     procs = []
@@ -53,10 +74,12 @@ def build(force: bool = False, verbose: bool = False) -> str:
             continue
         cmd = [_nvcc()] + NVCC_FLAGS + defs + extra + (["-Xptxas", "-v"] if verbose else []) + ["-o", lib] + cus
         procs.append((lib, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    if force or _ops_is_stale():
+        procs.append((OPS, subprocess.Popen(_ops_command(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     for lib, p in procs:
         out, _ = p.communicate()
         if p.returncode != 0:
-            raise RuntimeError(f"nvcc failed for {os.path.basename(lib)}:\n" + out)
+            raise RuntimeError(f"the compiler failed for {os.path.basename(lib)}:\n" + out)
         if verbose:
             print(out)
     return LIB

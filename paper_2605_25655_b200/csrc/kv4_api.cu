@@ -1,6 +1,7 @@
 // C entry points (include/thinfer.h) of the per-head norm with rotation and of the 4-bit paged cache.  Every call
 // checks its arguments on the host, enqueues its kernels on the given stream and returns; no call allocates, waits or
 // keeps anything for the next.
+#include <atomic>
 #include <cmath>
 
 #include "kv4_attn.cuh"
@@ -65,17 +66,32 @@ int share(int64_t tokens, int64_t rows, int head_dim) {
   return static_cast<int>(n < 1 ? 1 : n > rows ? rows : n);
 }
 
+// CTAs of 256 threads for that many groups per token: one resident wave (four per SM) at most, and at least one token's.
+int token_ctas(int64_t tokens, int chunks, int head_dim) {
+  const int64_t per_cta = 256 / (head_dim / 8), most = 4 * static_cast<int64_t>(op_sm_count());
+  const int64_t ctas = (tokens * chunks + per_cta - 1) / per_cta, least = (chunks + per_cta - 1) / per_cta;
+  return static_cast<int>(ctas < most ? ctas : most > least ? most : least);
+}
+
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + nb && y < x + na;
 }
 
-// Opts a kernel in to more than 48 KB of dynamic shared memory on the current device.
-template <typename K>
-int opt_in(K kernel, size_t bytes) {
+// Opts a kernel in to more than 48 KB of dynamic shared memory: a property of the kernel on a device, asked for once for
+// each new maximum.
+template <auto Kernel>
+int opt_in(size_t bytes) {
+  constexpr int kDevices = 64;
+  static std::atomic<int> reserved[kDevices];
   if (bytes <= 48 * 1024) return THINFER_OK;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)) != cudaSuccess)
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return op_fail(THINFER_ECUDA, "no current CUDA device");
+  const int want = static_cast<int>(bytes);
+  if (dev >= 0 && dev < kDevices && reserved[dev].load(std::memory_order_relaxed) >= want) return THINFER_OK;
+  if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, want) != cudaSuccess)
     return op_fail(THINFER_ECUDA, "cannot reserve %zu bytes of shared memory", bytes);
+  if (dev >= 0 && dev < kDevices) reserved[dev].store(want, std::memory_order_relaxed);
   return THINFER_OK;
 }
 
@@ -121,7 +137,7 @@ int plan_attention(int32_t batch, int32_t queries, int32_t n_q_heads, int32_t n_
 template <int D, int NT>
 int launch_attention(const Kv4AttnArgs& a, int grid, cudaStream_t st) {
   const size_t smem = kv4_warps<NT>() * kv4_warp_bytes<D, NT>() + (static_cast<size_t>(a.batch) + 1) * 8;
-  int rc = opt_in(kv4_attn_kernel<D, NT>, smem);
+  int rc = opt_in<kv4_attn_kernel<D, NT>>(smem);
   if (rc == THINFER_OK) rc = op_launch(kv4_attn_kernel<D, NT>, dim3(grid), dim3(kv4_warps<NT>() * 32), smem, st, false, a);
   if (rc == THINFER_OK) rc = op_launch(kv4_attn_join_kernel<D, NT>, dim3(grid), dim3(NT * 256), 0, st, true, a);
   return rc;
@@ -216,8 +232,7 @@ int thinfer_op_kv4_append(void* pool, int32_t n_pages, const int32_t* table, int
   a.v = static_cast<const half_t*>(v);
   a.k_stride = k_stride;
   a.v_stride = v_stride;
-  const int64_t per_cta = 256 / (head_dim / 8), ctas = (static_cast<int64_t>(tokens) * a.chunks + per_cta - 1) / per_cta;
-  if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "kv4_append: too many tokens");
+  const int ctas = token_ctas(tokens, a.chunks, head_dim);
   return op_launch(head_dim == 128 ? kv4_append_kernel<128> : kv4_append_kernel<64>, dim3(static_cast<unsigned>(ctas)),
                    dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), false, a);
 }
@@ -243,8 +258,7 @@ int thinfer_op_kv4_read(const void* pool, int32_t n_pages, const int32_t* table,
   a.v_out = static_cast<half_t*>(v_out);
   a.k_stride = a.v_stride = token_stride;
   a.k_head = a.v_head = head_stride;
-  const int64_t per_cta = 256 / (head_dim / 8), ctas = (static_cast<int64_t>(tokens) * a.chunks + per_cta - 1) / per_cta;
-  if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "kv4_read: too many tokens");
+  const int ctas = token_ctas(tokens, a.chunks, head_dim);
   return op_launch(head_dim == 128 ? kv4_read_kernel<128> : kv4_read_kernel<64>, dim3(static_cast<unsigned>(ctas)),
                    dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), false, a);
 }
@@ -318,7 +332,7 @@ int thinfer_op_kv4_reserve(int32_t* table, const int32_t* lens, const int32_t* a
     return op_fail(THINFER_EUNSUPPORTED, "max_pages %d: a row holds fewer than 2^31 tokens", max_pages);
   const PageTables t{table, lens, n_rows, max_pages, n_pages, page_shift_of(page_size)};
   const size_t smem = static_cast<size_t>(plan_words(n_pages)) * 8;
-  rc = opt_in(kv4_reserve_kernel, smem);
+  rc = opt_in<kv4_reserve_kernel>(smem);
   if (rc != THINFER_OK) return rc;
   return op_launch(kv4_reserve_kernel, dim3(1), dim3(kPlanThreads), smem, static_cast<cudaStream_t>(cuda_stream), false, t,
                    table, add, lens_out, refused);
@@ -357,7 +371,7 @@ int thinfer_op_kv4_fork(void* pool, int32_t n_layers, int32_t n_pages, const int
   if (workspace_bytes < moves_bytes(n_rows)) return op_fail(THINFER_ECAPACITY, "kv4_fork: the workspace is too small");
   const PageTables t{table, lens, n_rows, max_pages, n_pages, page_shift_of(page_size)};
   const size_t smem = static_cast<size_t>(plan_words(n_pages)) * 8 + nb * 2;
-  rc = opt_in(kv4_fork_kernel, smem);
+  rc = opt_in<kv4_fork_kernel>(smem);
   if (rc != THINFER_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   int* count = static_cast<int*>(workspace);
@@ -385,7 +399,7 @@ int thinfer_op_kv4_compact(void* pool, int32_t n_layers, int32_t n_pages, const 
   if (workspace_bytes < moves_bytes(n_pages / 2)) return op_fail(THINFER_ECAPACITY, "kv4_compact: the workspace is too small");
   const PageTables t{table, lens, n_rows, max_pages, n_pages, page_shift_of(page_size)};
   const size_t smem = static_cast<size_t>(plan_words(n_pages)) * 8;
-  rc = opt_in(kv4_compact_kernel, smem);
+  rc = opt_in<kv4_compact_kernel>(smem);
   if (rc != THINFER_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   int* count = static_cast<int*>(workspace);

@@ -1,7 +1,8 @@
 // Writing tokens into the 4-bit paged cache and reading them back.  Both are bound by memory: D / 8 lanes hold one
 // row (token, head, K or V) with one 16-byte access each, the row's extremes come from shuffles, and the codes leave
-// as one 32-bit word per lane.  A lane group looks its token's page up once and walks rows of that token, four in flight
-// at a time; how many groups share a token is set so that the device is full about twice.
+// as one 32-bit word per lane.  A lane group looks its token's page up once and walks rows of that token, several in
+// flight at a time; how many groups share a token is set so that the device is full once, and each group goes on to
+// further tokens.
 #pragma once
 #include "kv4_layout.cuh"
 
@@ -24,18 +25,41 @@ struct Kv4Spot {
   int slot;
   bool skip;       // the token is padding
 };
-__device__ __forceinline__ Kv4Spot kv4_spot(const Kv4TokensArgs& a, long long token) {
-  Kv4Spot s{nullptr, 0, true};
-  if (token < a.tokens) {
-    const int row = __ldg(a.rows + token), pos = __ldg(a.positions + token);
-    if (row >= 0 && pos >= 0) {
-      s.skip = false;
-      s.page = kv4_block(a.c, row, pos, 0);
-      s.slot = pos & ((1 << a.c.page_shift) - 1);
-    }
+
+// The tokens of a lane group: first, first + step, ...  Row and position are read two tokens ahead and the page number
+// one token ahead, so that only the first token waits for the chain of three loads.
+struct Kv4Walk {
+  const Kv4TokensArgs& a;
+  long long token, step;
+  int row1, pos1, row2, pos2, page1;   // of the next token, of the one after it; page of the next
+  __device__ __forceinline__ void look(long long t, int& row, int& pos) const {
+    row = t < a.tokens ? __ldg(a.rows + t) : -1;
+    pos = t < a.tokens ? __ldg(a.positions + t) : -1;
   }
-  return s;
-}
+  __device__ __forceinline__ int page_of(int row, int pos) const {
+    if (row < 0 || pos < 0 || row >= a.c.n_rows || (pos >> a.c.page_shift) >= a.c.max_pages) return -1;
+    return __ldg(a.c.table + static_cast<size_t>(row) * a.c.max_pages + (pos >> a.c.page_shift));
+  }
+  __device__ __forceinline__ Kv4Walk(const Kv4TokensArgs& args, long long first, long long step_) : a(args), token(first - step_), step(step_) {
+    look(first, row1, pos1);
+    look(first + step, row2, pos2);
+    page1 = page_of(row1, pos1);
+  }
+  // Moves to the next token; false behind the last one.
+  __device__ __forceinline__ bool next(Kv4Spot& s) {
+    token += step;
+    if (token >= a.tokens) return false;
+    const bool there = page1 >= 0 && page1 < a.c.n_pages;
+    s.skip = row1 < 0 || pos1 < 0;
+    s.slot = pos1 & ((1 << a.c.page_shift) - 1);
+    s.page = there ? a.c.pool + static_cast<size_t>(page1) * a.c.page_bytes : nullptr;
+    row1 = row2;
+    pos1 = pos2;
+    page1 = page_of(row1, pos1);
+    look(token + 2 * step, row2, pos2);
+    return true;
+  }
+};
 
 constexpr int kKv4RowsInFlight = 4;
 
@@ -61,41 +85,24 @@ __device__ __forceinline__ float by_15(float x) {
   return fmaf(fmaf(-15.f, q, x), 1.f / 15.f, q);
 }
 
-// Codes of eight values of a row with the given offset and scale, four bits each.  The quotient (x - offset) / scale is
-// taken with a reciprocal, off by less than 2^-18, and rounded by adding 1.5 * 2^23.  The residual x - offset - c scale,
-// which is exact where it matters, then tells on which side of the border between two codes the quotient lies: beyond
-// half a scale the code moves by one, at exactly half (common: 16-bit values lie on a grid) to the even one.
-// A scale too small for a reciprocal is left to a division.
+// Codes of eight values of a row with the given offset and scale, four bits each.  The quotient (x - offset) / scale is a
+// product with a reciprocal and one correction by the residual, so that a quotient half way between two codes (common:
+// 16-bit values lie on a grid) comes out as exactly that and the addition of 1.5 * 2^23 rounds it to the even code.  A
+// scale too small for a reciprocal is left to a division.
 __device__ __forceinline__ uint32_t kv4_codes(const float (&x)[8], float lo, float scale) {
-  constexpr float MAGIC = 12582912.f;
-  constexpr uint32_t M = 0x4b400000u;
-  const float inv = __fdividef(1.f, scale), half = 0.5f * scale;
-  float far = 0.f, e[8];
-  uint32_t c[8], word = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float d = x[j] - lo, t = fmaf(d, inv, MAGIC);
-    e[j] = fmaf(MAGIC - t, scale, d);
-    c[j] = static_cast<uint32_t>(__float_as_int(t));
-    far = fmaxf(far, fabsf(e[j]));
-    word += c[j] << (4 * j);
-  }
+  uint32_t word = 0;
   // a normal scale is within 2^-8 of (max - min) / 15, so that no code can pass 15
   const float smallest = kStorageType == 1 ? 0x1p-100f : 0x1p-14f;
   if (scale >= smallest && scale < 0x1p100f) {
-    if (far > scale * (0.5f - 0x1p-16f)) {
-      word = 0;
+    constexpr uint32_t M = 0x4b400000u;
+    const float inv = __fdividef(1.f, scale);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool odd = c[j] & 1u;
-        if (e[j] > half || (e[j] == half && odd)) ++c[j];
-        if (e[j] < -half || (e[j] == -half && odd)) --c[j];
-        word += c[j] << (4 * j);
-      }
+    for (int j = 0; j < 8; ++j) {
+      const float d = x[j] - lo, q = d * inv;
+      word += static_cast<uint32_t>(__float_as_int(fmaf(fmaf(-q, scale, d), inv, q) + 12582912.f)) << (4 * j);
     }
     return word - (M + (M << 4) + (M << 8) + (M << 12) + (M << 16) + (M << 20) + (M << 24) + (M << 28));
   }
-  word = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const float q = scale > 0.f ? fminf(rintf(__fdiv_rn(x[j] - lo, scale)), 15.f) : 0.f;
@@ -159,12 +166,15 @@ __global__ void __launch_bounds__(256, 4) kv4_append_kernel(const Kv4TokensArgs 
   const int lane = threadIdx.x & 31, sub = lane % LPR;
   const unsigned mask = (LPR == 16 ? 0xffffu : 0xffu) << (lane & ~(LPR - 1));
   const long long group = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) / LPR;
-  const long long token = group / a.chunks;
-  const int chunk = static_cast<int>(group - token * a.chunks);
-  const Kv4Spot s = kv4_spot(a, token);
-  if (s.page == nullptr) return;      // the same for the group, and shuffles stay inside it
-  kv4_append_rows<D, false>(a, s, a.k + token * a.k_stride, chunk, mask, sub);
-  kv4_append_rows<D, true>(a, s, a.v + token * a.v_stride, kv4_first_v(chunk, a.chunks, a.c.n_kv), mask, sub);
+  const long long first = group / a.chunks, step = static_cast<long long>(gridDim.x) * blockDim.x / LPR / a.chunks;
+  const int chunk = static_cast<int>(group - first * a.chunks), first_v = kv4_first_v(chunk, a.chunks, a.c.n_kv);
+  if (first >= step) return;
+  Kv4Walk walk(a, first, step);
+  for (Kv4Spot s; walk.next(s);) {
+    if (s.page == nullptr) continue;  // the same for the group, and shuffles stay inside it
+    kv4_append_rows<D, false>(a, s, a.k + walk.token * a.k_stride, chunk, mask, sub);
+    kv4_append_rows<D, true>(a, s, a.v + walk.token * a.v_stride, first_v, mask, sub);
+  }
 }
 
 template <int D, bool V>
@@ -212,16 +222,19 @@ __device__ __forceinline__ void kv4_read_rows(const Kv4TokensArgs& a, const Kv4S
 }
 
 template <int D>
-__global__ void __launch_bounds__(256) kv4_read_kernel(const Kv4TokensArgs a) {
+__global__ void __launch_bounds__(256, 4) kv4_read_kernel(const Kv4TokensArgs a) {
   constexpr int LPR = D / 8;
   const int sub = (threadIdx.x & 31) % LPR;
   const long long group = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) / LPR;
-  const long long token = group / a.chunks;
-  const int chunk = static_cast<int>(group - token * a.chunks);
-  const Kv4Spot s = kv4_spot(a, token);
-  if (s.skip) return;
-  kv4_read_rows<D, false>(a, s, a.k_out + token * a.k_stride, a.k_head, chunk, sub);
-  kv4_read_rows<D, true>(a, s, a.v_out + token * a.v_stride, a.v_head, kv4_first_v(chunk, a.chunks, a.c.n_kv), sub);
+  const long long first = group / a.chunks, step = static_cast<long long>(gridDim.x) * blockDim.x / LPR / a.chunks;
+  const int chunk = static_cast<int>(group - first * a.chunks), first_v = kv4_first_v(chunk, a.chunks, a.c.n_kv);
+  if (first >= step) return;
+  Kv4Walk walk(a, first, step);
+  for (Kv4Spot s; walk.next(s);) {
+    if (s.skip) continue;
+    kv4_read_rows<D, false>(a, s, a.k_out + walk.token * a.k_stride, a.k_head, chunk, sub);
+    kv4_read_rows<D, true>(a, s, a.v_out + walk.token * a.v_stride, a.v_head, first_v, sub);
+  }
 }
 
 }  // namespace thinfer

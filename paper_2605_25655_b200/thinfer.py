@@ -397,69 +397,33 @@ def op_argmax(logits, stream=None):
 
 
 # ------------------------------------- per-head norm + rotation, 4-bit paged cache
-# These run once per layer and decode step, so their Python side is kept to plain comparisons: no helper objects, no
-# library query for what a few multiplications give.
-class _on:
-    """Makes the tensors' CUDA device the current one for a call that finds another one current."""
-
-    def __init__(self, device):
-        import torch
-        self.guard = torch.cuda.device(device)
-
-    def __enter__(self):
-        self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        self.guard.__exit__(*exc)
+# These run once per layer and decode step: their checks, allocations and calls are in csrc/torch_ops.cpp (_ops.so).
+_FAST_NAMES = ("thinfer_op_qk_norm_rope", "thinfer_op_kv4_reserve", "thinfer_op_kv4_append", "thinfer_op_kv4_read",
+               "thinfer_kv4_attention_workspace", "thinfer_op_kv4_attention", "thinfer_kv4_pages_workspace", "thinfer_op_kv4_fork",
+               "thinfer_op_kv4_compact", "thinfer_last_error")
+_fast = None
 
 
-class _nothing:
-    def __enter__(self):
-        pass
-
-    def __exit__(self, *exc):
-        pass
-
-
-_nothing = _nothing()
-
-
-def _bad(what):
-    raise ThinferError(EINVAL, what)
-
-
-def _enter(device, stream):
-    """(guard, raw stream) of a call whose tensors live on `device`: the given stream, or the device's current one."""
-    from torch._C import _cuda_getCurrentRawStream, _cuda_getDevice
-    if device.type != "cuda":
-        _bad(f"tensors must be on a CUDA device, not {device}")
-    if stream is None:
-        raw = _cuda_getCurrentRawStream(device.index)
-    else:
-        if stream.device != device:
-            _bad(f"the stream belongs to {stream.device}, the tensors to {device}")
-        raw = stream.cuda_stream
-    return (_nothing if _cuda_getDevice() == device.index else _on(device)), raw
+def _load_fast():
+    """The marshalling module, bound to the entry points of both builds.  Fails loudly when it has not been built."""
+    global _fast
+    if _fast is None:
+        import torch  # noqa: F401  (its libraries come first)
+        try:
+            from . import _ops
+        except ImportError as e:
+            raise ThinferError(ECUDA, f"_ops.so cannot be loaded ({e}): build it with `python -m paper_2605_25655_b200._build`") from e
+        _ops.bind(ThinferError, *([C.cast(getattr(lib(s), n), C.c_void_p).value for n in _FAST_NAMES] for s in ("f16", "bf16")))
+        _fast = _ops
+    return _fast
 
 
-def _ints(t, name, device, shape, dtype=None):
-    """Address of a contiguous int32 (or `dtype`) tensor of the given shape."""
-    if dtype is None:
-        from torch import int32 as dtype
-    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        _bad(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
-
-
-def _token_stride(t, name, dtype, device, shape=None):
-    """Elements between the tokens of [tokens, heads, head_dim], whose heads lie side by side."""
-    if t.dim() != 3 or t.dtype is not dtype or t.device != device or (shape is not None and t.shape != shape):
-        _bad(f"{name}: a {dtype} tensor [tokens, heads, head_dim] on {device}" + (f" of shape {tuple(shape)}" if shape is not None else ""))
-    n, h, d = t.shape
-    s0, s1, s2 = t.stride()
-    if n == 0 or h == 0 or s2 != 1 or (h != 1 and s1 != d):
-        _bad(f"{name}: the heads of a token must be contiguous, and there must be some")
-    return s0 if n > 1 else h * d
+def _on(stream, tensor):
+    """Makes `stream` (and its device) current, so that what a call allocates belongs to it."""
+    import torch
+    if not tensor.is_cuda or stream.device != tensor.device:
+        raise ThinferError(EINVAL, f"the stream belongs to {stream.device}, the tensors to {tensor.device}: they must share a CUDA device")
+    return torch.cuda.stream(stream)
 
 
 def rope_turns(base, rotary_dim, device="cuda:0"):
@@ -474,31 +438,10 @@ def op_qk_norm_rope(q, k, q_gain, k_gain, eps, turns, positions, halves=False, q
     """Per-head RMSNorm and rotation of q [tokens, n_q_heads, d] and k [tokens, n_kv_heads, d] (token strides as they
     come, e.g. slices of a fused projection output); turns from rope_turns (its length sets the rotated dimensions);
     positions int32 [tokens], negative: left as they were.  Returns (q_out, k_out); they may be q and k themselves."""
-    import torch
-    dev, dt = q.device, q.dtype
-    guard, st = _enter(dev, stream)
-    qs, ks = _token_stride(q, "q", dt, dev), _token_stride(k, "k", dt, dev)
-    n, hq, d = q.shape
-    hkv = k.shape[1]
-    if k.shape[0] != n or k.shape[2] != d:
-        _bad("q and k must agree in tokens and head_dim")
-    if q_out is None:
-        q_out, qos = torch.empty((n, hq, d), dtype=dt, device=dev), hq * d
-    else:
-        qos = _token_stride(q_out, "q_out", dt, dev, q.shape)
-    if k_out is None:
-        k_out, kos = torch.empty((n, hkv, d), dtype=dt, device=dev), hkv * d
-    else:
-        kos = _token_stride(k_out, "k_out", dt, dev, k.shape)
-    if turns.dim() != 1:
-        _bad("turns: FP64 [rotary_dim / 2]")
-    s = storage_of(q)
-    with guard:
-        _check(lib(s).thinfer_op_qk_norm_rope(
-            q.data_ptr(), qs, k.data_ptr(), ks, q_out.data_ptr(), qos, k_out.data_ptr(), kos, _ints(q_gain, "q_gain", dev, (d,), dt),
-            _ints(k_gain, "k_gain", dev, (d,), dt), _ints(turns, "turns", dev, turns.shape, torch.float64),
-            _ints(positions, "positions", dev, (n,)), n, hq, hkv, d, 2 * turns.shape[0], int(halves), eps, st), None, s)
-    return q_out, k_out
+    if stream is not None:
+        with _on(stream, q):
+            return op_qk_norm_rope(q, k, q_gain, k_gain, eps, turns, positions, halves, q_out, k_out)
+    return (_fast or _load_fast()).qk_norm_rope(q, k, q_gain, k_gain, eps, turns, positions, halves, q_out, k_out)
 
 
 def kv4_page_bytes(n_kv_heads, head_dim, page_size):
@@ -508,189 +451,63 @@ def kv4_page_bytes(n_kv_heads, head_dim, page_size):
     return n.value
 
 
-def _pool(pool, dims, page_size, head_dim, device):
-    """Number of KV heads of a uint8 pool tensor whose last dimension is a page."""
-    import torch
-    if pool.dtype is not torch.uint8 or pool.dim() != dims or not pool.is_contiguous() or pool.device != device:
-        _bad(f"pool: a contiguous uint8 tensor of {dims} dimensions on {device}")
-    per = page_size * (head_dim + 8)
-    heads = pool.shape[-1] // per if per > 0 else 0
-    if heads == 0 or heads * per != pool.shape[-1]:
-        _bad(f"pool: a page has a multiple of {per} bytes, not {pool.shape[-1]}")
-    return heads
-
-
-def _table(table, device):
-    if table.dim() != 2:
-        _bad("table: int32 [rows, max_pages]")
-    return _ints(table, "table", device, table.shape)
-
-
 def op_kv4_reserve(table, lens, add, n_pages, page_size, lens_out=None, refused=None, stream=None):
     """Room for add[r] more tokens of every row: writes page numbers into table (int32 [rows, max_pages]); returns
     (lens_out, refused): the new lengths (may be lens itself) and, int64 [1], how many rows did not fit and keep theirs."""
-    import torch
-    dev = table.device
-    guard, st = _enter(dev, stream)
-    tab = _table(table, dev)
-    rows, max_pages = table.shape
-    if lens_out is None:
-        lens_out = torch.empty(rows, dtype=torch.int32, device=dev)
-    if refused is None:
-        refused = torch.empty(1, dtype=torch.int64, device=dev)
-    with guard:
-        _check(lib().thinfer_op_kv4_reserve(
-            tab, _ints(lens, "lens", dev, (rows,)), _ints(add, "add", dev, (rows,)), _ints(lens_out, "lens_out", dev, (rows,)),
-            _ints(refused, "refused", dev, (1,), torch.int64), rows, max_pages, n_pages, page_size, st))
-    return lens_out, refused
+    if stream is not None:
+        with _on(stream, table):
+            return op_kv4_reserve(table, lens, add, n_pages, page_size, lens_out, refused)
+    return (_fast or _load_fast()).reserve(table, lens, add, n_pages, page_size, lens_out, refused)
 
 
 def op_kv4_append(pool, table, k, v, rows, positions, page_size, stream=None):
     """Quantises k, v [tokens, n_kv_heads, d] into one layer's pool [n_pages, page bytes]: token i goes to position
     positions[i] of table row rows[i] (int32 [tokens]; negative: skipped)."""
-    dev = pool.device
-    guard, st = _enter(dev, stream)
-    ks, vs = _token_stride(k, "k", k.dtype, dev), _token_stride(v, "v", k.dtype, dev, k.shape)
-    n, hkv, d = k.shape
-    if _pool(pool, 2, page_size, d, dev) != hkv:
-        _bad("the pool's pages are for another number of heads")
-    s = storage_of(k)
-    with guard:
-        _check(lib(s).thinfer_op_kv4_append(
-            pool.data_ptr(), pool.shape[0], _table(table, dev), table.shape[0], table.shape[1], k.data_ptr(), ks, v.data_ptr(), vs,
-            _ints(rows, "rows", dev, (n,)), _ints(positions, "positions", dev, (n,)), n, hkv, d, page_size, st), None, s)
+    if stream is not None:
+        with _on(stream, pool):
+            return op_kv4_append(pool, table, k, v, rows, positions, page_size)
+    return (_fast or _load_fast()).append(pool, table, k, v, rows, positions, page_size)
 
 
 def op_kv4_read(pool, table, rows, positions, page_size, head_dim, dtype, k_out=None, v_out=None, stream=None):
     """Values of tokens (rows[i], positions[i]) of one layer: (k, v) [tokens, n_kv_heads, d] of `dtype` (the type the
     pool was written with).  k_out / v_out: two tensors of that shape with equal strides (e.g. transposed views)."""
     import torch
-    dev = pool.device
-    guard, st = _enter(dev, stream)
-    hkv = _pool(pool, 2, page_size, head_dim, dev)
-    n = positions.numel()
-    shape = (n, hkv, head_dim)
-    if k_out is None:
-        k_out = torch.empty(shape, dtype=dtype, device=dev)
-    if v_out is None:
-        v_out = torch.empty_strided(shape, k_out.stride(), dtype=dtype, device=dev)
-    strides = k_out.stride()
-    for t in (k_out, v_out):
-        if t.shape != shape or t.dtype is not dtype or t.device != dev or t.stride() != strides:
-            _bad("k_out, v_out: [tokens, heads, head_dim] of one type, device and strides")
-    if strides[2] != 1:
-        _bad("k_out, v_out: the values of a head must be contiguous")
-    s = storage_of(k_out)
-    with guard:
-        _check(lib(s).thinfer_op_kv4_read(
-            pool.data_ptr(), pool.shape[0], _table(table, dev), table.shape[0], table.shape[1], k_out.data_ptr(), v_out.data_ptr(),
-            strides[0], strides[1], _ints(rows, "rows", dev, (n,)), _ints(positions, "positions", dev, (n,)), n, hkv, head_dim,
-            page_size, st), None, s)
-    return k_out, v_out
-
-
-_workspaces = {}   # sizes -> bytes: what the library answered for them
+    if stream is not None:
+        with _on(stream, pool):
+            return op_kv4_read(pool, table, rows, positions, page_size, head_dim, dtype, k_out, v_out)
+    if dtype is not torch.float16 and dtype is not torch.bfloat16:
+        raise ThinferError(EUNSUPPORTED, f"storage type {dtype}: the library is built for float16 and bfloat16")
+    return (_fast or _load_fast()).read(pool, table, rows, positions, page_size, head_dim, dtype is torch.bfloat16, k_out, v_out)
 
 
 def op_kv4_attention(q, pool, table, lens, page_size, out=None, workspace=None, stream=None):
     """q [batch, queries, n_q_heads, d] (already rotated) over one layer's 4-bit pool [n_pages, page bytes]: request b is
     row b of table and holds lens[b] keys, the query tokens the last among them.  Returns [batch, queries, n_q_heads, d].
     workspace: uint8, at least thinfer_kv4_attention_workspace bytes (default: allocated for the call)."""
-    import torch
-    dev, dt = q.device, q.dtype
-    guard, st = _enter(dev, stream)
-    if q.dim() != 4:
-        _bad("q: [batch, queries, n_q_heads, head_dim]")
-    b, n, hq, d = q.shape
-    s0, s1, s2, s3 = q.stride()
-    if b * n * hq == 0 or s3 != 1 or (hq != 1 and s2 != d) or (n > 1 and b > 1 and s0 != n * s1):
-        _bad("q: the heads of a token must be contiguous and the query tokens evenly spaced")
-    qs = s1 if n > 1 else s0 if b > 1 else hq * d
-    hkv = _pool(pool, 2, page_size, d, dev)
-    if out is None:
-        out = torch.empty((b, n, hq, d), dtype=dt, device=dev)
-    s = storage_of(q)
-    L = lib(s)
-    with guard:
-        if workspace is None:
-            key = (dev.index, b, n, hq, hkv, d)
-            need = _workspaces.get(key)
-            if need is None:
-                size = C.c_size_t(0)
-                _check(L.thinfer_kv4_attention_workspace(b, n, hq, hkv, d, C.byref(size)), None, s)
-                need = size.value
-                if len(_workspaces) >= 4096:
-                    _workspaces.clear()
-                _workspaces[key] = need
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-        elif workspace.dtype is not torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
-            _bad(f"workspace: a contiguous uint8 tensor on {dev}")
-        _check(L.thinfer_op_kv4_attention(
-            q.data_ptr(), qs, pool.data_ptr(), pool.shape[0], _table(table, dev) if table.shape[0] == b else _bad("table: one row per request"),
-            table.shape[1], _ints(lens, "lens", dev, (b,)), _ints(out, "out", dev, (b, n, hq, d), dt), b, n, hq, hkv, d, page_size,
-            workspace.data_ptr(), workspace.numel(), st), None, s)
-    return out
-
-
-def _pages_workspace(rows, n_pages, device):
-    import torch
-    key = (rows, n_pages)
-    need = _workspaces.get(key)
-    if need is None:
-        size = C.c_size_t(0)
-        _check(lib().thinfer_kv4_pages_workspace(rows, n_pages, C.byref(size)))
-        need = size.value
-        if len(_workspaces) >= 4096:
-            _workspaces.clear()
-        _workspaces[key] = need
-    return torch.empty(need, dtype=torch.uint8, device=device)
+    if stream is not None:
+        with _on(stream, q):
+            return op_kv4_attention(q, pool, table, lens, page_size, out, workspace)
+    return (_fast or _load_fast()).attention(q, pool, table, lens, page_size, out, workspace)
 
 
 def op_kv4_fork(pool, table, lens, source, page_size, head_dim, table_out=None, lens_out=None, refused=None, stream=None):
     """New row r takes over old row source[r] (negative: freed) of a pool [n_layers, n_pages, page bytes]: full pages are
     shared, a partly filled last page is copied for every heir but one.  Returns (table_out, lens_out, refused), the last
     int64 [1]."""
-    import torch
-    dev = pool.device
-    guard, st = _enter(dev, stream)
-    hkv = _pool(pool, 3, page_size, head_dim, dev)
-    tab = _table(table, dev)
-    rows, max_pages = table.shape
-    if table_out is None:
-        table_out = torch.empty((rows, max_pages), dtype=torch.int32, device=dev)
-    if lens_out is None:
-        lens_out = torch.empty(rows, dtype=torch.int32, device=dev)
-    if refused is None:
-        refused = torch.empty(1, dtype=torch.int64, device=dev)
-    ws = _pages_workspace(rows, pool.shape[1], dev)
-    with guard:
-        _check(lib().thinfer_op_kv4_fork(
-            pool.data_ptr(), pool.shape[0], pool.shape[1], tab, _ints(lens, "lens", dev, (rows,)), _ints(source, "source", dev, (rows,)),
-            _ints(table_out, "table_out", dev, (rows, max_pages)), _ints(lens_out, "lens_out", dev, (rows,)),
-            _ints(refused, "refused", dev, (1,), torch.int64), rows, max_pages, hkv, head_dim, page_size, ws.data_ptr(), ws.numel(), st))
-    return table_out, lens_out, refused
+    if stream is not None:
+        with _on(stream, pool):
+            return op_kv4_fork(pool, table, lens, source, page_size, head_dim, table_out, lens_out, refused)
+    return (_fast or _load_fast()).fork(pool, table, lens, source, page_size, head_dim, table_out, lens_out, refused)
 
 
 def op_kv4_compact(pool, table, lens, page_size, head_dim, table_out=None, live=None, stream=None):
     """Moves the pages in use of a pool [n_layers, n_pages, page bytes] to its front.  Returns (table_out, live): the table
     with the new page numbers and, int64 [1], the number of pages in use."""
-    import torch
-    dev = pool.device
-    guard, st = _enter(dev, stream)
-    hkv = _pool(pool, 3, page_size, head_dim, dev)
-    tab = _table(table, dev)
-    rows, max_pages = table.shape
-    if table_out is None:
-        table_out = torch.empty((rows, max_pages), dtype=torch.int32, device=dev)
-    if live is None:
-        live = torch.empty(1, dtype=torch.int64, device=dev)
-    ws = _pages_workspace(rows, pool.shape[1], dev)
-    with guard:
-        _check(lib().thinfer_op_kv4_compact(
-            pool.data_ptr(), pool.shape[0], pool.shape[1], tab, _ints(lens, "lens", dev, (rows,)),
-            _ints(table_out, "table_out", dev, (rows, max_pages)), _ints(live, "live", dev, (1,), torch.int64), rows, max_pages, hkv,
-            head_dim, page_size, ws.data_ptr(), ws.numel(), st))
-    return table_out, live
+    if stream is not None:
+        with _on(stream, pool):
+            return op_kv4_compact(pool, table, lens, page_size, head_dim, table_out, live)
+    return (_fast or _load_fast()).compact(pool, table, lens, page_size, head_dim, table_out, live)
 
 
 def to_device_layers(np_layers, device="cuda:0"):

@@ -604,3 +604,22 @@ def test_calls_on_a_side_stream_and_two_at_once(T):
     for i in range(2):
         assert all(torch.equal(g, want[i]) for g in got[i])
     assert torch.equal(explicit, want[0])
+
+
+def test_workspaces_of_a_call_on_an_explicit_stream_belong_to_that_stream(T):
+    """The call's workspace is given back when it returns; memory taken on the current stream meanwhile must not be it."""
+    torch, thinfer = T
+    rng = np.random.default_rng(6)
+    pool, tab, _ = _filled(T, rng, "f16", 4, 128, 64, [3000, 2000])
+    lens, q = _int(torch, [3000, 2000]), torch.randn(2, 1, 16, 128, device="cuda").half()
+    want = thinfer.op_kv4_attention(q, pool, tab, lens, 64)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)                    # some 10 ms: the call below waits in line
+    out = thinfer.op_kv4_attention(q, pool, tab, lens, 64, stream=side)
+    taken = [torch.full((1 << 20,), 255, dtype=torch.uint8, device="cuda") for _ in range(64)]
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and len(taken) == 64
+    with pytest.raises(thinfer.ThinferError):
+        thinfer.op_kv4_attention(q.cpu(), pool, tab, lens, 64, stream=side)
