@@ -666,51 +666,59 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
   }
   __syncthreads();
 
-  // ---- unfinished pieces: those of one pair are neighbours in the order head, tail of warp 0, of warp 1, ...  A warp
-  // takes some columns of a pair at a time (two in a pass where 16 lanes cover one).
+  // ---- unfinished pieces, pair by pair: a warp takes some columns of a pair at a time (two in a pass where 16 lanes cover
+  // one).  Lane i knows piece i.
   constexpr int PASS = 128 / D, TASKS = NC / PASS;
+  static_assert(2 * CW <= 32, "a lane for every piece");
+  const long long my_pair = lane < 2 * CW ? pieces[lane].pair : -1;
+  const float* const my_part = reinterpret_cast<const float*>(kv4_mem + (lane >> 1) * WARP_BYTES + ((lane & 1) ? 0 : WARP_BYTES - PART * 4));
   int task = -warp;                      // the warp's next task among those of the pairs so far
-  for (int k = 0; k < 2 * CW;) {
-    const long long pair = pieces[k].pair;
-    if (pair < 0) {
-      ++k;
-      continue;
-    }
-    int k1 = k + 1;
-    while (k1 < 2 * CW && (pieces[k1].pair < 0 || pieces[k1].pair == pair)) ++k1;
+  for (unsigned left = __ballot_sync(0xffffffffu, my_pair >= 0); left != 0;) {
+    const int k = __ffs(left) - 1;
+    const long long pair = __shfl_sync(0xffffffffu, my_pair, k);
+    const unsigned members = __ballot_sync(0xffffffffu, my_pair == pair);
+    left &= ~members;
     task += TASKS;
-    if (task > 0) {
-      const Kv4Piece pc = pieces[k];
-      const bool done = pair >= c_beg && pair + pc.units <= c_beg + c_units;
-      float* ws = a.parts + (static_cast<size_t>(blockIdx.x) * 2 + (pair < c_beg ? 0 : 1)) * PART;
-      if (!done && pair >= c_beg && task == TASKS && lane == 0)
-        a.splits[blockIdx.x] = Kv4Split{pc.b, pc.pair_in_b, static_cast<int>(kv4_cta_of(total, ctas, pair + pc.units - 1)), 0};
-      for (; task > 0; task -= CW) {
-        const int col = (TASKS - task) * PASS + lane * 4 / D, d = (lane * 4) % D;
-        float top = kKv4Low, l = 0.f;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int i = k; i < k1; ++i)
-          if (pieces[i].pair >= 0) {
-            const float* q = reinterpret_cast<const float*>(kv4_mem + (i >> 1) * WARP_BYTES + ((i & 1) ? 0 : WARP_BYTES - PART * 4));
-            const float2 ml = *reinterpret_cast<const float2*>(q + NC * D + 2 * col);
-            const float4 x = *reinterpret_cast<const float4*>(q + col * D + d);
-            const float mx = fmaxf(top, ml.x), f0 = ex2_approx(top - mx), f1 = ex2_approx(ml.x - mx);
-            top = mx;
-            l = fmaf(ml.y, f1, l * f0);
-            v = make_float4(fmaf(x.x, f1, v.x * f0), fmaf(x.y, f1, v.y * f0), fmaf(x.z, f1, v.z * f0), fmaf(x.w, f1, v.w * f0));
-          }
-        if (done) {
-          if (pc.col0 + col < a.cols) {
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            kv4_store4(kv4_out<D>(a, pc.b, pc.hk, pc.col0 + col) + d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
-          }
-        } else {
-          *reinterpret_cast<float4*>(ws + col * D + d) = v;
-          if (d == 0) *reinterpret_cast<float2*>(ws + NC * D + 2 * col) = make_float2(top, l);
+    if (task <= 0) continue;
+    const Kv4Piece pc = pieces[k];
+    const bool done = pair >= c_beg && pair + pc.units <= c_beg + c_units;
+    float* ws = a.parts + (static_cast<size_t>(blockIdx.x) * 2 + (pair < c_beg ? 0 : 1)) * PART;
+    if (!done && pair >= c_beg && task == TASKS && lane == 0)
+      a.splits[blockIdx.x] = Kv4Split{pc.b, pc.pair_in_b, static_cast<int>(kv4_cta_of(total, ctas, pair + pc.units - 1)), 0};
+    const bool member = (members >> lane) & 1u;
+    for (; task > 0; task -= CW) {
+      const int col0 = (TASKS - task) * PASS;
+      float top[PASS], l[PASS], f[PASS];   // of the pass's columns; f: this lane's piece
+#pragma unroll
+      for (int i = 0; i < PASS; ++i) {
+        const float2 ml = member ? *reinterpret_cast<const float2*>(my_part + NC * D + 2 * (col0 + i)) : make_float2(kKv4Low, 0.f);
+        top[i] = warp_max(ml.x);
+        f[i] = ex2_approx(ml.x - top[i]);
+        l[i] = warp_sum(ml.y * f[i]);
+      }
+      const int mine_col = PASS == 1 ? 0 : lane >> 4, col = col0 + mine_col, d = (lane * 4) % D;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (unsigned rest = members; rest != 0; rest &= rest - 1) {
+        const int i = __ffs(rest) - 1;
+        float g = __shfl_sync(0xffffffffu, f[0], i);
+        if (PASS == 2) {
+          const float g1 = __shfl_sync(0xffffffffu, f[PASS - 1], i);
+          g = mine_col ? g1 : g;
         }
+        const float4 x = *reinterpret_cast<const float4*>(kv4_mem + (i >> 1) * WARP_BYTES + ((i & 1) ? 0 : WARP_BYTES - PART * 4) + (col * D + d) * 4);
+        v = make_float4(fmaf(x.x, g, v.x), fmaf(x.y, g, v.y), fmaf(x.z, g, v.z), fmaf(x.w, g, v.w));
+      }
+      const float sum = PASS == 2 && mine_col ? l[PASS - 1] : l[0], largest = PASS == 2 && mine_col ? top[PASS - 1] : top[0];
+      if (done) {
+        if (pc.col0 + col < a.cols) {
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+          kv4_store4(kv4_out<D>(a, pc.b, pc.hk, pc.col0 + col) + d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+        }
+      } else {
+        *reinterpret_cast<float4*>(ws + col * D + d) = v;
+        if (d == 0) *reinterpret_cast<float2*>(ws + NC * D + 2 * col) = make_float2(largest, sum);
       }
     }
-    k = k1;
   }
 }
 
