@@ -136,7 +136,7 @@ int plan_attention(int32_t batch, int32_t queries, int32_t n_q_heads, int32_t n_
 
 template <int D, int NT>
 int launch_attention(const Kv4AttnArgs& a, int grid, cudaStream_t st) {
-  const size_t smem = kv4_warps<NT>() * kv4_warp_bytes<D, NT>() + (static_cast<size_t>(a.batch) + 1) * 8;
+  const size_t smem = kv4_warps<NT>() * kv4_warp_bytes<D, NT>() + kv4_plan_bytes(a.batch);
   int rc = opt_in<kv4_attn_kernel<D, NT>>(smem);
   if (rc == THINFER_OK) rc = op_launch(kv4_attn_kernel<D, NT>, dim3(grid), dim3(kv4_warps<NT>() * 32), smem, st, false, a);
   if (rc == THINFER_OK) rc = op_launch(kv4_attn_join_kernel<D, NT>, dim3(grid), dim3(NT * 256), 0, st, true, a);
@@ -303,6 +303,7 @@ int thinfer_op_kv4_attention(const void* q, int64_t q_stride, const void* pool, 
   a.col_tiles = p.col_tiles;
   a.splits = static_cast<Kv4Split*>(workspace);
   a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.split_bytes);
+  a.inv_group = 1.f / static_cast<float>(a.group);
   a.scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(head_dim));
   // no more CTAs than the table's capacity could give a unit per warp
   const int64_t units = static_cast<int64_t>(batch) * n_kv_heads * p.col_tiles *

@@ -55,8 +55,7 @@ constexpr float kKv4Low = -1e30f;    // running maximum before the first key
 
 // What a CTA leaves for the second kernel about the pair that begins in it and ends in a later one.
 struct Kv4Split {
-  int b, pair_in_b, last;   // last: the CTA it ends in, -1: there is no such pair
-  int pad;
+  int b, hk, col0, last;   // last: the CTA it ends in, -1: there is no such pair
 };
 
 struct Kv4AttnArgs {
@@ -72,6 +71,7 @@ struct Kv4AttnArgs {
   float* parts;          // [grid][2] unfinished pieces of CTAs: [columns][D] outputs, then [columns][2] maximum and sum;
                          // piece 0 began in an earlier CTA, piece 1 begins here
   float scale_log2;      // log2(e) / sqrt(D)
+  float inv_group;       // 1 / group
 };
 
 template <int D>
@@ -110,15 +110,25 @@ __device__ __forceinline__ int kv4_len(const Kv4AttnArgs& a, int b) {
 __device__ __forceinline__ long long div_pos(long long a, long long b) {
   return ((a | b) >> 32) == 0 ? static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
 }
-__device__ __forceinline__ int kv4_units(int len) { return len <= kKv4Unit ? 1 : (len + kKv4Unit - 1) / kKv4Unit; }
+__device__ __forceinline__ int kv4_units(int len) { return (len + kKv4Unit - 1) / kKv4Unit; }
 
-__device__ __forceinline__ void kv4_prefix(const Kv4AttnArgs& a, long long* pref, long long* warp_sums) {
+// Shared memory of the schedule: pref[0 .. batch] first units of the requests, then their lengths.
+__host__ __device__ constexpr size_t kv4_plan_bytes(int batch) { return (static_cast<size_t>(batch) + 1) * 8 + static_cast<size_t>(batch) * 4; }
+struct Kv4Plan {
+  const long long* pref;
+  const int* len;
+};
+
+__device__ __forceinline__ Kv4Plan kv4_plan(const Kv4AttnArgs& a, uint8_t* mem, long long* warp_sums) {
+  long long* pref = reinterpret_cast<long long*>(mem);
+  int* lens = reinterpret_cast<int*>(pref + a.batch + 1);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  const long long per_unit = static_cast<long long>(a.c.n_kv) * a.col_tiles;
+  const int per_unit = a.c.n_kv * a.col_tiles;
   long long carry = 0;
   for (int b0 = 0; b0 < a.batch; b0 += blockDim.x) {
     const int b = b0 + threadIdx.x;
-    const long long v = b < a.batch ? kv4_units(kv4_len(a, b)) * per_unit : 0;
+    const int len = b < a.batch ? kv4_len(a, b) : 0;
+    const long long v = static_cast<long long>(kv4_units(len)) * per_unit;
     long long s = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -128,38 +138,65 @@ __device__ __forceinline__ void kv4_prefix(const Kv4AttnArgs& a, long long* pref
     if (lane == 31) warp_sums[warp] = s;
     __syncthreads();
     long long before = carry, all = 0;
-    for (int w = 0; w < warps; ++w) {
+    for (int w = 0; w < warps && b0 + w * 32 < a.batch; ++w) {
       if (w < warp) before += warp_sums[w];
       all += warp_sums[w];
     }
-    if (b < a.batch) pref[b] = before + s - v;
+    if (b < a.batch) {
+      pref[b] = before + s - v;
+      lens[b] = len;
+    }
     carry += all;
-    __syncthreads();
+    if (b0 + static_cast<int>(blockDim.x) < a.batch) __syncthreads();
   }
   if (threadIdx.x == 0) pref[a.batch] = carry;
   __syncthreads();
+  return Kv4Plan{pref, lens};
 }
 
+// A pair and a unit in it.
 struct Kv4Place {
-  int b, pair_in_b, unit, units, len;
+  int b, hk, ct, unit, units, len;
   long long pair_first;  // first unit of the pair
 };
-__device__ __forceinline__ Kv4Place kv4_place(const Kv4AttnArgs& a, const long long* pref, long long u) {
+// Where unit u lies.  Requests without keys have no units.
+__device__ __forceinline__ Kv4Place kv4_place(const Kv4AttnArgs& a, const Kv4Plan& plan, long long u) {
   int lo = 0, hi = a.batch - 1;
-  while (lo < hi) {
+  while (lo < hi) {      // the last request that begins at or before u
     const int mid = (lo + hi + 1) >> 1;
-    if (pref[mid] <= u) lo = mid;
+    if (plan.pref[mid] <= u) lo = mid;
     else hi = mid - 1;
   }
   Kv4Place p;
   p.b = lo;
-  p.len = kv4_len(a, lo);
+  p.len = plan.len[lo];
   p.units = kv4_units(p.len);
-  const long long in_b = u - pref[lo];
-  p.pair_in_b = static_cast<int>(div_pos(in_b, p.units));
-  p.unit = static_cast<int>(in_b - static_cast<long long>(p.pair_in_b) * p.units);
+  const long long in_b = u - plan.pref[lo];
+  const int pair = static_cast<int>(div_pos(in_b, p.units));
+  p.unit = static_cast<int>(in_b - static_cast<long long>(pair) * p.units);
   p.pair_first = u - p.unit;
+  p.hk = a.col_tiles == 1 ? pair : pair / a.col_tiles;
+  p.ct = pair - p.hk * a.col_tiles;
   return p;
+}
+// The pair behind p's; there has to be one.
+__device__ __forceinline__ void kv4_next_pair(const Kv4AttnArgs& a, const Kv4Plan& plan, Kv4Place& p) {
+  p.pair_first += p.units;
+  p.unit = 0;
+  if (++p.ct == a.col_tiles) {
+    p.ct = 0;
+    if (++p.hk == a.c.n_kv) {
+      p.hk = 0;
+      do {
+        p.len = plan.len[++p.b];
+      } while (p.len == 0);
+      p.units = kv4_units(p.len);
+    }
+  }
+}
+// col / group of a query column (below 2^18, where a rounded product is exact enough)
+__device__ __forceinline__ int kv4_query_of(const Kv4AttnArgs& a, int col) {
+  return a.queries == 1 ? 0 : static_cast<int>((static_cast<float>(col) + 0.5f) * a.inv_group);
 }
 // CTAs that take part: with few units some stay idle rather than split pairs further.
 __device__ __forceinline__ long long kv4_ctas(long long total, int grid, int warps) {
@@ -263,7 +300,7 @@ __device__ __forceinline__ void kv4_request_queries(const Kv4AttnArgs& a, uint32
   for (int n = 0; n < NT * 8 * PER / 32; ++n) {
     const int i = (n * 32 + lane) / PER, k = lane % PER, col = col0 + i;
     if (col < a.cols) {
-      const int qi = a.queries == 1 ? 0 : col / a.group, h = hk * a.group + (col - qi * a.group);
+      const int qi = kv4_query_of(a, col), h = hk * a.group + (col - qi * a.group);
       const half_t* src = a.q + (static_cast<long long>(b) * a.queries + qi) * a.q_stride + static_cast<long long>(h) * D + k * 8;
       async_copy16(dst + i * (2 * D) + ((k ^ (i & 7)) << 4), src);
     }
@@ -313,7 +350,7 @@ __device__ __forceinline__ void kv4_load_queries(const Kv4AttnArgs& a, Kv4Acc<D,
       s.qf[n][j] = __shfl_sync(0xffffffffu, qf, 8 * c + 4 * j);
       s.qs[n][j] = __shfl_sync(0xffffffffu, qs, 8 * c + 4 * j);
       const int cj = col0 + 8 * n + 2 * c + j;
-      s.lim[n][j] = cj < a.cols ? len - (a.queries == 1 ? 0 : a.queries - 1 - cj / a.group) : 0;
+      s.lim[n][j] = cj < a.cols ? len - (a.queries - 1 - kv4_query_of(a, cj)) : 0;
     }
   }
 }
@@ -332,10 +369,12 @@ __device__ __forceinline__ void kv4_stage(Kv4Acc<D, NT>& s, const uint8_t* stage
   for (int n = 0; n < NT; ++n)
 #pragma unroll
     for (int e = 0; e < 4; ++e) ones[n][e] = 0.f;
+  // ---- scores of all 32 tokens: their latency lies beside the weights of the first 16
+  float scores[2][NT][4];
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
-    // ---- scores
-    float sc[NT][4], sd[NT][4];   // two chains of instructions
+    float (&sc)[NT][4] = scores[b];
+    float sd[NT][4];   // a second chain of instructions
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -358,6 +397,10 @@ __device__ __forceinline__ void kv4_stage(Kv4Acc<D, NT>& s, const uint8_t* stage
 #pragma unroll
         for (int e = 0; e < 4; ++e) sc[n][e] += sd[n][e];
     }
+  }
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const float (&sc)[NT][4] = scores[b];
     // ---- weights
     float2 kp[2], vp[2];   // [row r | row r + 8] scale, offset; for V scale, middle of the row
 #pragma unroll
@@ -485,13 +528,13 @@ __device__ __forceinline__ void kv4_store4(half_t* dst, float4 v) {
 // First output element of a column.
 template <int D>
 __device__ __forceinline__ half_t* kv4_out(const Kv4AttnArgs& a, int b, int hk, int col) {
-  const int i = col / a.group, h = hk * a.group + (col - i * a.group);
+  const int i = kv4_query_of(a, col), h = hk * a.group + (col - i * a.group);
   return a.out + ((static_cast<size_t>(b) * a.queries + i) * a.n_q + h) * D;
 }
 
 struct Kv4Piece {
   long long pair;          // first unit of the pair, -1: no piece
-  int units, b, hk, col0, pair_in_b;
+  int units, b, hk, col0;
 };
 
 template <int D, int NT>
@@ -503,11 +546,17 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
   __shared__ Kv4Piece pieces[2 * CW];       // unfinished pieces, 2 w: head, 2 w + 1: tail of warp w
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
-  long long* pref = reinterpret_cast<long long*>(kv4_mem + CW * WARP_BYTES);
   if (threadIdx.x < 2 * CW) pieces[threadIdx.x].pair = -1;
   if (threadIdx.x == 0) a.splits[blockIdx.x].last = -1;
-  kv4_prefix(a, pref, warp_sums);
-  const long long total = pref[a.batch], ctas = kv4_ctas(total, gridDim.x, CW);
+  const Kv4Plan plan = kv4_plan(a, kv4_mem + CW * WARP_BYTES, warp_sums);
+  // requests without keys: zeros, dealt out over the CTAs
+  for (int b = blockIdx.x; b < a.batch; b += gridDim.x)
+    if (plan.len[b] == 0) {
+      uint4* dst = reinterpret_cast<uint4*>(a.out + static_cast<size_t>(b) * a.queries * a.n_q * D);
+      const int n = a.queries * a.n_q * (D / 8);
+      for (int i = threadIdx.x; i < n; i += CW * 32) dst[i] = make_uint4(0, 0, 0, 0);
+    }
+  const long long total = plan.pref[a.batch], ctas = kv4_ctas(total, gridDim.x, CW);
   if (blockIdx.x >= ctas) return;
   const long long c_beg = kv4_cta_first(total, ctas, blockIdx.x), c_units = kv4_cta_first(total, ctas, blockIdx.x + 1) - c_beg;
   const long long w_beg = c_beg + div_pos(warp * c_units, CW);
@@ -518,9 +567,12 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
 
   // ---- requests: walk the warp's units ahead of the arithmetic, across segments
   int f_u = 0, f_end = 0;              // next unit to request and end of the segment it is in, from w_beg
-  int f_t = 0, f_len = 0, f_base = 0;  // its first token, the pair's length, table column of `ids`
+  int f_t = 0, f_base = 0;             // its first token, table column of `ids`
   const uint8_t* f_blocks = nullptr;   // pool + head offset
   const int32_t* f_row = nullptr;
+  Kv4Place pl{}, f_pl;                 // of the arithmetic and of the requests
+  if (w_units > 0) pl = kv4_place(a, plan, w_beg);
+  f_pl = pl;
   int ids = -1, ids_next = -1;         // page numbers of 32 table columns from f_base, and of the next 32
   int f_slot = 0;
   uint32_t bad_of = 0;                 // two bits for each ring stage: tokens 0 .. 15 or 16 .. 31 are on no page
@@ -530,30 +582,24 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
   const int par_from = P * D + (lane & 8 ? P * 4 : 0) + (lane & 3) * 16;
   auto load_ids = [&](int base) {
     const int col = base + lane;
-    return col < a.c.max_pages && (static_cast<long long>(col) << shift) < f_len ? __ldg(f_row + col) : -1;
+    return col < a.c.max_pages && (static_cast<long long>(col) << shift) < f_pl.len ? __ldg(f_row + col) : -1;
   };
   auto request = [&]() {               // one stage, if there is one left
-    while (f_u < w_units) {
+    if (f_u < w_units) {
       if (f_u >= f_end) {              // enter the next segment
-        const Kv4Place pl = kv4_place(a, pref, w_beg + f_u);
-        f_end = f_u + min(w_units - f_u, pl.units - pl.unit);
-        f_t = pl.unit * kKv4Unit;
-        f_len = pl.len;
-        f_blocks = a.c.pool + static_cast<size_t>(pl.pair_in_b / a.col_tiles) * a.c.block_bytes;
-        f_row = a.c.table + static_cast<size_t>(pl.b) * a.c.max_pages;
+        if (f_u != 0) kv4_next_pair(a, plan, f_pl);
+        f_end = f_u + min(w_units - f_u, f_pl.units - f_pl.unit);
+        f_t = f_pl.unit * kKv4Unit;
+        f_blocks = a.c.pool + static_cast<size_t>(f_pl.hk) * a.c.block_bytes;
+        f_row = a.c.table + static_cast<size_t>(f_pl.b) * a.c.max_pages;
         f_base = (f_t >> shift) & ~31;
         ids = load_ids(f_base);
         ids_next = load_ids(f_base + 32);
-        if (f_len > 0) {
-          const int hk = pl.pair_in_b / a.col_tiles;
-          kv4_request_queries<D, NT>(a, ring + kv4_ring_bytes<D, NT>() + f_slot * kv4_query_bytes<D, NT>(), pl.b, hk,
-                                     (pl.pair_in_b - hk * a.col_tiles) * NC);
-        }
+        kv4_request_queries<D, NT>(a, ring + kv4_ring_bytes<D, NT>() + f_slot * kv4_query_bytes<D, NT>(), f_pl.b, f_pl.hk, f_pl.ct * NC);
       }
       ++f_u;
       const int t = f_t;
       f_t += kKv4Unit;
-      if (t >= f_len) continue;        // the one unit of an empty row holds nothing
       int col = (t >> shift) - f_base;
       if (col >= 32) {
         f_base += 32;
@@ -564,7 +610,7 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
       // the two halves of 16 tokens: on one page, or on two of 16 tokens; no request for what lies behind the end
       const int at0 = t & (P - 1), at1 = (t + 16) & (P - 1);
       const int page0 = __shfl_sync(0xffffffffu, ids, col), page1 = shift == 4 ? __shfl_sync(0xffffffffu, ids, (col + 1) & 31) : page0;
-      const bool there1 = t + 16 < f_len;
+      const bool there1 = t + 16 < f_pl.len;
       const bool ok0 = static_cast<unsigned>(page0) < static_cast<unsigned>(a.c.n_pages);
       const bool ok1 = static_cast<unsigned>(page1) < static_cast<unsigned>(a.c.n_pages);
       const uint32_t bad = (ok0 ? 0u : 1u) | (ok1 || !there1 ? 0u : 2u);
@@ -597,7 +643,6 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
       if (lane < 16 && (second ? ok1 && there1 : ok0))
         async_copy16(dst + 4 * HALF + lane * 16, (second ? from1 + at1 * 4 : from0 + at0 * 4) + par_from);
       f_slot = f_slot + 1 == NS ? 0 : f_slot + 1;
-      return;
     }
   };
 #pragma unroll
@@ -609,9 +654,7 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
   Kv4Acc<D, NT> s;
   int slot = 0;
   for (int u = 0; u < w_units;) {
-    const Kv4Place pl = kv4_place(a, pref, w_beg + u);
-    const int n_units = min(w_units - u, pl.units - pl.unit);
-    const int hk = pl.pair_in_b / a.col_tiles, col0 = (pl.pair_in_b - hk * a.col_tiles) * NC;
+    const int n_units = min(w_units - u, pl.units - pl.unit), col0 = pl.ct * NC;
     s.reset();
     const int t_end = min(pl.len, (pl.unit + n_units) * kKv4Unit), t_all = pl.len - (a.queries - 1) - kKv4Unit;
     const int t_beg = pl.unit * kKv4Unit;
@@ -631,7 +674,7 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
     const bool head = pl.unit > 0, whole = !head && n_units == pl.units;
     // the piece that ends the range takes the ring, which nobody fills any more
     float* part = reinterpret_cast<float*>(mine + (head ? WARP_BYTES - PART * 4 : 0));
-    if (!whole && lane == 0) pieces[2 * warp + (head ? 0 : 1)] = Kv4Piece{pl.pair_first, pl.units, pl.b, hk, col0, pl.pair_in_b};
+    if (!whole && lane == 0) pieces[2 * warp + (head ? 0 : 1)] = Kv4Piece{pl.pair_first, pl.units, pl.b, pl.hk, col0};
     __syncwarp();
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -648,7 +691,7 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
         if (whole) {
           if (col0 + col < a.cols) {
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            half_t* dst = kv4_out<D>(a, pl.b, hk, col0 + col) + r * (D / 8);
+            half_t* dst = kv4_out<D>(a, pl.b, pl.hk, col0 + col) + r * (D / 8);
 #pragma unroll
             for (int i = 0; i < W; ++i) {
               const float4 v = kv4_value4<D, NT>(s, n, j, i, z, back);
@@ -663,12 +706,14 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
         }
       }
     u += n_units;
+    if (u < w_units) kv4_next_pair(a, plan, pl);
   }
   __syncthreads();
 
   // ---- unfinished pieces, pair by pair: a warp takes some columns of a pair at a time (two in a pass where 16 lanes cover
   // one).  Lane i knows piece i.
-  constexpr int PASS = 128 / D, TASKS = NC / PASS;
+  constexpr int PASS = 128 / D;
+  const int TASKS = (min(NC, a.cols) + PASS - 1) / PASS;   // only the last tile of several has fewer columns
   static_assert(2 * CW <= 32, "a lane for every piece");
   const long long my_pair = lane < 2 * CW ? pieces[lane].pair : -1;
   const float* const my_part = reinterpret_cast<const float*>(kv4_mem + (lane >> 1) * WARP_BYTES + ((lane & 1) ? 0 : WARP_BYTES - PART * 4));
@@ -684,19 +729,19 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
     const bool done = pair >= c_beg && pair + pc.units <= c_beg + c_units;
     float* ws = a.parts + (static_cast<size_t>(blockIdx.x) * 2 + (pair < c_beg ? 0 : 1)) * PART;
     if (!done && pair >= c_beg && task == TASKS && lane == 0)
-      a.splits[blockIdx.x] = Kv4Split{pc.b, pc.pair_in_b, static_cast<int>(kv4_cta_of(total, ctas, pair + pc.units - 1)), 0};
+      a.splits[blockIdx.x] = Kv4Split{pc.b, pc.hk, pc.col0, static_cast<int>(kv4_cta_of(total, ctas, pair + pc.units - 1))};
     const bool member = (members >> lane) & 1u;
     for (; task > 0; task -= CW) {
-      const int col0 = (TASKS - task) * PASS;
+      const int first_col = (TASKS - task) * PASS;
       float top[PASS], l[PASS], f[PASS];   // of the pass's columns; f: this lane's piece
 #pragma unroll
       for (int i = 0; i < PASS; ++i) {
-        const float2 ml = member ? *reinterpret_cast<const float2*>(my_part + NC * D + 2 * (col0 + i)) : make_float2(kKv4Low, 0.f);
+        const float2 ml = member ? *reinterpret_cast<const float2*>(my_part + NC * D + 2 * (first_col + i)) : make_float2(kKv4Low, 0.f);
         top[i] = warp_max(ml.x);
         f[i] = ex2_approx(ml.x - top[i]);
         l[i] = warp_sum(ml.y * f[i]);
       }
-      const int mine_col = PASS == 1 ? 0 : lane >> 4, col = col0 + mine_col, d = (lane * 4) % D;
+      const int mine_col = PASS == 1 ? 0 : lane >> 4, col = first_col + mine_col, d = (lane * 4) % D;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       for (unsigned rest = members; rest != 0; rest &= rest - 1) {
         const int i = __ffs(rest) - 1;
@@ -731,7 +776,7 @@ __global__ void __launch_bounds__(NT * 256) kv4_attn_join_kernel(const Kv4AttnAr
   const int first = blockIdx.x, col = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Kv4Split sp = a.splits[first];
   if (sp.last < 0) return;
-  const int hk = sp.pair_in_b / a.col_tiles, out_col = (sp.pair_in_b - hk * a.col_tiles) * NC + col;
+  const int out_col = sp.col0 + col;
   if (out_col >= a.cols) return;
   float m = kKv4Low, l = 0.f, o[V];
 #pragma unroll
@@ -747,7 +792,7 @@ __global__ void __launch_bounds__(NT * 256) kv4_attn_join_kernel(const Kv4AttnAr
     for (int e = 0; e < V; ++e) o[e] = fmaf(o[e], f0, q[col * D + e * 32 + lane] * f1);
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  half_t* dst = kv4_out<D>(a, sp.b, hk, out_col);
+  half_t* dst = kv4_out<D>(a, sp.b, sp.hk, out_col);
 #pragma unroll
   for (int e = 0; e < V; ++e) dst[e * 32 + lane] = f_to_h(o[e] * inv);
 }
