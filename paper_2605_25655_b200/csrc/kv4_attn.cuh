@@ -743,15 +743,25 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
       }
       const int mine_col = PASS == 1 ? 0 : lane >> 4, col = first_col + mine_col, d = (lane * 4) % D;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (unsigned rest = members; rest != 0; rest &= rest - 1) {
-        const int i = __ffs(rest) - 1;
-        float g = __shfl_sync(0xffffffffu, f[0], i);
-        if (PASS == 2) {
-          const float g1 = __shfl_sync(0xffffffffu, f[PASS - 1], i);
-          g = mine_col ? g1 : g;
+      for (unsigned rest = members; rest != 0;) {   // four pieces at a time
+        float g[4];
+        float4 x[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const bool more = rest != 0;
+          const int i = more ? __ffs(rest) - 1 : k;  // behind the last piece: a piece of the pair again, with weight 0
+          rest &= rest - 1;
+          g[q] = __shfl_sync(0xffffffffu, f[0], i);
+          if (PASS == 2) {
+            const float g1 = __shfl_sync(0xffffffffu, f[PASS - 1], i);
+            g[q] = mine_col ? g1 : g[q];
+          }
+          if (!more) g[q] = 0.f;
+          x[q] = *reinterpret_cast<const float4*>(kv4_mem + (i >> 1) * WARP_BYTES + ((i & 1) ? 0 : WARP_BYTES - PART * 4) + (col * D + d) * 4);
         }
-        const float4 x = *reinterpret_cast<const float4*>(kv4_mem + (i >> 1) * WARP_BYTES + ((i & 1) ? 0 : WARP_BYTES - PART * 4) + (col * D + d) * 4);
-        v = make_float4(fmaf(x.x, g, v.x), fmaf(x.y, g, v.y), fmaf(x.z, g, v.z), fmaf(x.w, g, v.w));
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          v = make_float4(fmaf(x[q].x, g[q], v.x), fmaf(x[q].y, g[q], v.y), fmaf(x[q].z, g[q], v.z), fmaf(x[q].w, g[q], v.w));
       }
       const float sum = PASS == 2 && mine_col ? l[PASS - 1] : l[0], largest = PASS == 2 && mine_col ? top[PASS - 1] : top[0];
       if (done) {
@@ -781,15 +791,24 @@ __global__ void __launch_bounds__(NT * 256) kv4_attn_join_kernel(const Kv4AttnAr
   float m = kKv4Low, l = 0.f, o[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) o[e] = 0.f;
-#pragma unroll 4
-  for (int i = first; i <= sp.last; ++i) {   // piece 1 of the first CTA, piece 0 of the others
-    const float* q = a.parts + (static_cast<size_t>(i) * 2 + (i == first ? 1 : 0)) * PART;
-    const float2 ml = *reinterpret_cast<const float2*>(q + NC * D + 2 * col);
-    const float mn = fmaxf(m, ml.x), f0 = ex2_approx(m - mn), f1 = ex2_approx(ml.x - mn);
+  // 32 pieces at a time: lane i reads the maximum and sum of piece i, then all lanes add up the outputs, whose loads do not
+  // wait for one another.  Piece 1 of the first CTA, piece 0 of the others.
+  for (int i0 = first; i0 <= sp.last; i0 += 32) {
+    const int n = min(32, sp.last - i0 + 1);
+    auto piece = [&](int i) { return a.parts + (static_cast<size_t>(i0 + i) * 2 + (i0 + i == first ? 1 : 0)) * PART; };
+    const float2 ml = lane < n ? *reinterpret_cast<const float2*>(piece(lane) + NC * D + 2 * col) : make_float2(kKv4Low, 0.f);
+    const float mn = fmaxf(m, warp_max(ml.x)), f0 = ex2_approx(m - mn), f = ex2_approx(ml.x - mn);
     m = mn;
-    l = fmaf(l, f0, ml.y * f1);
+    l = fmaf(l, f0, warp_sum(ml.y * f));
 #pragma unroll
-    for (int e = 0; e < V; ++e) o[e] = fmaf(o[e], f0, q[col * D + e * 32 + lane] * f1);
+    for (int e = 0; e < V; ++e) o[e] *= f0;
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) {
+      const float g = __shfl_sync(0xffffffffu, f, i);
+      const float* q = piece(i) + col * D + lane;
+#pragma unroll
+      for (int e = 0; e < V; ++e) o[e] = fmaf(q[e * 32], g, o[e]);
+    }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   half_t* dst = kv4_out<D>(a, sp.b, sp.hk, out_col);
