@@ -360,7 +360,7 @@ __device__ __forceinline__ void kv4_load_queries(const Kv4AttnArgs& a, Kv4Acc<D,
 template <int D, int NT, bool MASKED>
 __device__ __forceinline__ void kv4_stage(Kv4Acc<D, NT>& s, const uint8_t* stage, int t0, uint32_t bad) {
   constexpr int W = D / 32, MT = D / 16;
-  constexpr uint32_t LO = 0x000f000fu, HI = 0x00f000f0u, BOTH = 0x00ff00ffu, ONE = 0x3c003c00u;
+  constexpr uint32_t LO = 0x000f000fu, HI = 0x00f000f0u, ONE = 0x3c003c00u;
   constexpr int KP = kKv4Unit * D, VP = KP + kKv4Unit * 4;
   const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
   const int tr = kv4_row_token(r);
@@ -484,7 +484,7 @@ __device__ __forceinline__ void kv4_stage(Kv4Acc<D, NT>& s, const uint8_t* stage
       }
       mma_f16_16816(ones[n], ONE, ONE, ONE, ONE, pb[n][0], pb[n][1]);
     }
-    // ---- output: row r of a tile collects code + 16 code', row r + 8 collects 16 code' (code' the next dimension)
+    // ---- output
     uint32_t va[W], vb[W];
     const uint8_t* v = stage + kKv4Unit * (D / 2) + 8 * b * D;   // 8 pairs: a multiple of the lines the keys repeat after
     lds_words<W>(va, v + kv4_at<D, true>(2 * c * D + r * (D / 8)));
@@ -493,9 +493,9 @@ __device__ __forceinline__ void kv4_stage(Kv4Acc<D, NT>& s, const uint8_t* stage
     for (int i = 0; i < W; ++i)
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
-        const uint32_t x = hf ? __byte_perm(va[i], 0, 0x4341) : va[i] & BOTH, y = hf ? __byte_perm(vb[i], 0, 0x4341) : vb[i] & BOTH;
+        const uint32_t x = hf ? va[i] >> 8 : va[i], y = hf ? vb[i] >> 8 : vb[i];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) mma_f16_16816(s.o[n][2 * i + hf], x, x & HI, y, y & HI, pb[n][0], pb[n][1]);
+        for (int n = 0; n < NT; ++n) mma_f16_16816(s.o[n][2 * i + hf], x & LO, x & HI, y & LO, y & HI, pb[n][0], pb[n][1]);
       }
   }
   // ---- 8 off every code
@@ -504,7 +504,7 @@ __device__ __forceinline__ void kv4_stage(Kv4Acc<D, NT>& s, const uint8_t* stage
     const uint64_t sum = f32x2(ones[n][0], ones[n][1]);
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      const float2 x = f32x2_unpack(fma_f32x2(sum, f32x2(-136 * 0x1p-24f, -136 * 0x1p-24f), f32x2(s.o[n][i][0], s.o[n][i][1])));
+      const float2 x = f32x2_unpack(fma_f32x2(sum, f32x2(-0x1p-21f, -0x1p-21f), f32x2(s.o[n][i][0], s.o[n][i][1])));
       const float2 y = f32x2_unpack(fma_f32x2(sum, f32x2(-0x1p-17f, -0x1p-17f), f32x2(s.o[n][i][2], s.o[n][i][3])));
       s.o[n][i][0] = x.x;
       s.o[n][i][1] = x.y;
@@ -519,8 +519,7 @@ template <int D, int NT>
 __device__ __forceinline__ float4 kv4_value4(const Kv4Acc<D, NT>& s, int n, int j, int i, float z, float back) {
   constexpr float F0 = 16777216.f, F1 = 1048576.f;  // 2^24 and 2^20: the place of the code in its operand
   const float(&x)[4] = s.o[n][2 * i], (&y)[4] = s.o[n][2 * i + 1];
-  return make_float4(fmaf(x[j] - x[2 + j], F0 * back, z), fmaf(x[2 + j], F1 * back, z), fmaf(y[j] - y[2 + j], F0 * back, z),
-                     fmaf(y[2 + j], F1 * back, z));
+  return make_float4(fmaf(x[j], F0 * back, z), fmaf(x[2 + j], F1 * back, z), fmaf(y[j], F0 * back, z), fmaf(y[2 + j], F1 * back, z));
 }
 __device__ __forceinline__ void kv4_store4(half_t* dst, float4 v) {
   *reinterpret_cast<uint2*>(dst) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
