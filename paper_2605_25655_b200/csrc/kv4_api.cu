@@ -101,6 +101,13 @@ int check_plan(int32_t rows, int32_t n_pages) {
   return THINFER_OK;
 }
 
+// Threads of the one CTA that plans: with little to look at its barriers are what takes the time.
+int plan_threads(int32_t rows, int32_t max_pages, int32_t n_pages) {
+  const int64_t entries = static_cast<int64_t>(rows) * max_pages;
+  if (n_pages > 16384 || entries > 8192) return kPlanThreads;
+  return entries <= 1024 ? 256 : 512;
+}
+
 size_t moves_bytes(int32_t most) { return 16 + static_cast<size_t>(most) * sizeof(PageMove); }
 
 int copy_pages(void* pool, const int* count, const PageMove* moves, int most_moves, int layers, int n_kv, int d, int page,
@@ -335,7 +342,7 @@ int thinfer_op_kv4_reserve(int32_t* table, const int32_t* lens, const int32_t* a
   const size_t smem = static_cast<size_t>(plan_words(n_pages)) * 8;
   rc = opt_in<kv4_reserve_kernel>(smem);
   if (rc != THINFER_OK) return rc;
-  return op_launch(kv4_reserve_kernel, dim3(1), dim3(kPlanThreads), smem, static_cast<cudaStream_t>(cuda_stream), false, t,
+  return op_launch(kv4_reserve_kernel, dim3(1), dim3(plan_threads(n_rows, max_pages, n_pages)), smem, static_cast<cudaStream_t>(cuda_stream), false, t,
                    table, add, lens_out, refused);
 }
 
@@ -371,13 +378,13 @@ int thinfer_op_kv4_fork(void* pool, int32_t n_layers, int32_t n_pages, const int
   }
   if (workspace_bytes < moves_bytes(n_rows)) return op_fail(THINFER_ECAPACITY, "kv4_fork: the workspace is too small");
   const PageTables t{table, lens, n_rows, max_pages, n_pages, page_shift_of(page_size)};
-  const size_t smem = static_cast<size_t>(plan_words(n_pages)) * 8 + nb * 2;
+  const size_t smem = static_cast<size_t>(plan_words(n_pages)) * 8 + nb * 4;
   rc = opt_in<kv4_fork_kernel>(smem);
   if (rc != THINFER_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   int* count = static_cast<int*>(workspace);
   PageMove* moves = reinterpret_cast<PageMove*>(static_cast<char*>(workspace) + 16);
-  rc = op_launch(kv4_fork_kernel, dim3(1), dim3(kPlanThreads), smem, st, false, t, source, table_out, lens_out, refused, count, moves);
+  rc = op_launch(kv4_fork_kernel, dim3(1), dim3(plan_threads(n_rows, max_pages, n_pages)), smem, st, false, t, source, table_out, lens_out, refused, count, moves);
   if (rc != THINFER_OK) return rc;
   return copy_pages(pool, count, moves, n_rows, n_layers, n_kv_heads, head_dim, page_size, n_pages, st);
 }
@@ -405,7 +412,7 @@ int thinfer_op_kv4_compact(void* pool, int32_t n_layers, int32_t n_pages, const 
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   int* count = static_cast<int*>(workspace);
   PageMove* moves = reinterpret_cast<PageMove*>(static_cast<char*>(workspace) + 16);
-  rc = op_launch(kv4_compact_kernel, dim3(1), dim3(kPlanThreads), smem, st, false, t, table_out, live_pages, count, moves);
+  rc = op_launch(kv4_compact_kernel, dim3(1), dim3(plan_threads(n_rows, max_pages, n_pages)), smem, st, false, t, table_out, live_pages, count, moves);
   if (rc != THINFER_OK) return rc;
   return copy_pages(pool, count, moves, most, n_layers, n_kv_heads, head_dim, page_size, n_pages, st);
 }

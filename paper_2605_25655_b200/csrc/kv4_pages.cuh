@@ -24,31 +24,58 @@ struct PageTables {
   int rows, max_pages, n_pages, page_shift;
 };
 
-__device__ __forceinline__ int tables_len(const PageTables& t, int r) {  // tokens of a row, within what its table can name
-  const int n = t.lens[r];
+__device__ __forceinline__ int tables_clamp(const PageTables& t, int n) {  // tokens of a row, within what its table can name
   const long long cap = static_cast<long long>(t.max_pages) << t.page_shift;
   return n < 0 ? 0 : (n > cap ? static_cast<int>(cap) : n);
 }
+__device__ __forceinline__ int tables_len(const PageTables& t, int r) { return tables_clamp(t, t.lens[r]); }
 __device__ __forceinline__ int pages_for(int tokens, int shift) {
   return static_cast<int>((static_cast<long long>(tokens) + (1 << shift) - 1) >> shift);
 }
 
-// Calls f(row, column, page) for every page in use, entries outside the pool left out.
-constexpr int kPlanSpan = 256;  // table columns of one warp task
-template <typename F>
-__device__ __forceinline__ void for_pages_in_use(const PageTables& t, F f) {
+// Calls f(row, column, tokens of the row, entry) for every entry of the tables, used or not, with live = false for those
+// behind a row's pages.  Small tables are taken as one run of entries, four per thread in flight, whose lengths and
+// numbers are read at the same time; of large ones only the live spans of each row are read, a warp per span (ALL: the
+// others are visited as well, without being read).
+constexpr int kPlanSpan = 256;           // table columns of one warp task
+constexpr int kPlanFlat = 1 << 16;       // entries up to which a table counts as small
+template <bool ALL, typename F>
+__device__ __forceinline__ void for_entries(const PageTables& t, F f) {
+  const long long entries = static_cast<long long>(t.rows) * t.max_pages;
+  if (entries <= kPlanFlat) {
+    constexpr int U = 4;
+    const int e = static_cast<int>(entries);
+    for (int i0 = threadIdx.x; i0 < e; i0 += U * blockDim.x) {
+      int p[U], n[U], r[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * blockDim.x;
+        if (i < e) {
+          r[u] = static_cast<int>(static_cast<unsigned>(i) / static_cast<unsigned>(t.max_pages));
+          p[u] = t.table[i];
+          n[u] = t.lens[r[u]];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * blockDim.x;
+        if (i >= e) break;
+        const int c = i - r[u] * t.max_pages, len = tables_clamp(t, n[u]);
+        const bool live = c < pages_for(len, t.page_shift);
+        if (ALL || live) f(r[u], c, len, p[u], live);
+      }
+    }
+    return;
+  }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   const int spans = (t.max_pages + kPlanSpan - 1) / kPlanSpan;
   const long long tasks = static_cast<long long>(t.rows) * spans;
   for (long long k = warp; k < tasks; k += warps) {
     const int r = static_cast<int>(k / spans), c0 = static_cast<int>(k - static_cast<long long>(r) * spans) * kPlanSpan;
-    const int n = pages_for(tables_len(t, r), t.page_shift);
-    const int c1 = min(n, c0 + kPlanSpan);
+    const int len = tables_len(t, r), n = pages_for(len, t.page_shift);
+    const int c1 = min(ALL ? t.max_pages : n, c0 + kPlanSpan);
     const int32_t* row = t.table + static_cast<size_t>(r) * t.max_pages;
-    for (int c = c0 + lane; c < c1; c += 32) {
-      const int p = row[c];
-      if (p >= 0 && p < t.n_pages) f(r, c, p);
-    }
+    for (int c = c0 + lane; c < c1; c += 32) f(r, c, len, c < n ? row[c] : -1, c < n);
   }
 }
 
@@ -124,7 +151,9 @@ __device__ __forceinline__ PageMap map_pages(const PageTables& t, int* mem, int*
   m.before = mem + m.words;
   for (int w = threadIdx.x; w < m.words; w += blockDim.x) m.bits[w] = 0;
   __syncthreads();
-  for_pages_in_use(t, [&](int, int, int p) { atomicOr(&m.bits[p >> 5], 1u << (p & 31)); });
+  for_entries<false>(t, [&](int, int, int, int p, bool) {
+    if (p >= 0 && p < t.n_pages) atomicOr(&m.bits[p >> 5], 1u << (p & 31));
+  });
   __syncthreads();
   const int per = (m.words + blockDim.x - 1) / blockDim.x;
   const int w0 = min(m.words, static_cast<int>(threadIdx.x) * per), w1 = min(m.words, w0 + per);
@@ -201,11 +230,13 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_fork_kernel(const PageTables
   __shared__ int buf[33];
   __shared__ int bad;
   pdl_launch_dependents();
-  int* owner = plan_mem;            // [rows] who keeps the partly filled last page of a source
-  int* fresh = plan_mem + t.rows;   // [rows] page of a row's own copy, or -1
+  int* owner = plan_mem;                  // [rows] who keeps the partly filled last page of a source
+  int* fresh = plan_mem + t.rows;         // [rows] page of a row's own copy, or -1
+  int* from = plan_mem + 2 * t.rows;      // [rows] the source
+  int* tokens = plan_mem + 3 * t.rows;    // [rows] the new length
   for (int r = threadIdx.x; r < t.rows; r += blockDim.x) owner[r] = 0x7fffffff;
   if (threadIdx.x == 0) bad = 0;
-  const PageMap m = map_pages(t, plan_mem + 2 * t.rows, buf);
+  const PageMap m = map_pages(t, plan_mem + 4 * t.rows, buf);
   for (int r = threadIdx.x; r < t.rows; r += blockDim.x) {
     const int s = source[r];
     if (s >= 0 && s < t.rows) atomicMin(&owner[s], s == r ? -1 : r);
@@ -246,6 +277,8 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_fork_kernel(const PageTables
         atomicAdd(&bad, 1);
       }
       lens_out[r] = n;
+      from[r] = s;
+      tokens[r] = n;
     }
     carry += total;
     __syncthreads();
@@ -254,19 +287,25 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_fork_kernel(const PageTables
     *refused = bad;
     *move_count = min(carry, free_pages);
   }
-  // the new tables: warps take spans of one row
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  const int spans = (t.max_pages + kPlanSpan - 1) / kPlanSpan;
-  const long long tasks = static_cast<long long>(t.rows) * spans;
-  for (long long task = warp; task < tasks; task += warps) {
-    const int r = static_cast<int>(task / spans), c0 = static_cast<int>(task - static_cast<long long>(r) * spans) * kPlanSpan;
-    const int n = lens_out[r], pages = pages_for(n, t.page_shift), s = source[r];
-    const int own_page = fresh[r];
-    const int c1 = min(t.max_pages, c0 + kPlanSpan);
-    for (int c = c0 + lane; c < c1; c += 32) {
-      int p = -1;
-      if (c < pages) p = own_page >= 0 && c == pages - 1 ? own_page : t.table[static_cast<size_t>(s) * t.max_pages + c];
-      table_out[static_cast<size_t>(r) * t.max_pages + c] = p;
+  // the new tables, entry by entry, four per thread in flight
+  const long long entries = static_cast<long long>(t.rows) * t.max_pages;
+  constexpr int U = 4;
+  for (long long i0 = threadIdx.x; i0 < entries; i0 += U * blockDim.x) {
+    int p[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long long i = i0 + static_cast<long long>(u) * blockDim.x;
+      p[u] = -1;
+      if (i < entries) {
+        const int r = (i >> 32) == 0 ? static_cast<int>(static_cast<unsigned>(i) / static_cast<unsigned>(t.max_pages)) : static_cast<int>(i / t.max_pages);
+        const int c = static_cast<int>(i - static_cast<long long>(r) * t.max_pages), pages = pages_for(tokens[r], t.page_shift);
+        if (c < pages) p[u] = fresh[r] >= 0 && c == pages - 1 ? fresh[r] : t.table[static_cast<size_t>(from[r]) * t.max_pages + c];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long long i = i0 + static_cast<long long>(u) * blockDim.x;
+      if (i < entries) table_out[i] = p[u];
     }
   }
 }
@@ -294,27 +333,16 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_compact_kernel(const PageTab
     *move_count = n_moves;
   }
   __syncthreads();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  const int spans = (t.max_pages + kPlanSpan - 1) / kPlanSpan;
-  const long long tasks = static_cast<long long>(t.rows) * spans;
-  for (long long task = warp; task < tasks; task += warps) {
-    const int r = static_cast<int>(task / spans), c0 = static_cast<int>(task - static_cast<long long>(r) * spans) * kPlanSpan;
-    const int n = tables_len(t, r), pages = pages_for(n, t.page_shift);
-    const int c1 = min(t.max_pages, c0 + kPlanSpan);
-    const size_t row = static_cast<size_t>(r) * t.max_pages;
-    for (int c = c0 + lane; c < c1; c += 32) {
-      int p = -1;
-      if (c < pages) {
-        p = t.table[row + c];
-        if (p >= m.live && p < t.n_pages) {
-          const int k = m.live_below(p) - stay;
-          atomicMax(&moves[k].tokens, min(1 << t.page_shift, n - (c << t.page_shift)));
-          p = moves[k].dst;
-        }
-      }
-      table_out[row + c] = p;
+  for_entries<true>(t, [&](int r, int c, int n, int p, bool live) {
+    if (!live) {
+      p = -1;
+    } else if (p >= m.live && p < t.n_pages) {
+      const int k = m.live_below(p) - stay;
+      atomicMax(&moves[k].tokens, min(1 << t.page_shift, n - (c << t.page_shift)));
+      p = moves[k].dst;
     }
-  }
+    table_out[static_cast<size_t>(r) * t.max_pages + c] = p;
+  });
 }
 
 // ---------------------------------------------------------------- the copies
