@@ -58,17 +58,17 @@ Kv4Cache make_cache(const void* pool, const int32_t* table, int32_t rows, int32_
 
 bool stride_ok(int64_t stride, int64_t least) { return stride >= least && stride % 8 == 0; }
 
-// Lane groups of head_dim / 8 lanes that share the rows of one token: as many as fill the device once (2048 threads an
+// Lane groups of `lanes` lanes that share the rows of one token: as many as fill the device once (2048 threads an
 // SM), one row each at most.  Twice as many cost 5 to 15 % for long prompts, sixteen times 50 to 70 %.
-int share(int64_t tokens, int64_t rows, int head_dim) {
-  const int64_t want = static_cast<int64_t>(op_sm_count()) * 2048 / (head_dim / 8);
+int share(int64_t tokens, int64_t rows, int lanes) {
+  const int64_t want = static_cast<int64_t>(op_sm_count()) * 2048 / lanes;
   const int64_t n = (want + tokens - 1) / tokens;
   return static_cast<int>(n < 1 ? 1 : n > rows ? rows : n);
 }
 
 // CTAs of 256 threads for that many groups per token: one resident wave (four per SM) at most, and at least one token's.
-int token_ctas(int64_t tokens, int chunks, int head_dim) {
-  const int64_t per_cta = 256 / (head_dim / 8), most = 4 * static_cast<int64_t>(op_sm_count());
+int token_ctas(int64_t tokens, int chunks, int lanes) {
+  const int64_t per_cta = 256 / lanes, most = 4 * static_cast<int64_t>(op_sm_count());
   const int64_t ctas = (tokens * chunks + per_cta - 1) / per_cta, least = (chunks + per_cta - 1) / per_cta;
   return static_cast<int>(ctas < most ? ctas : most > least ? most : least);
 }
@@ -114,7 +114,7 @@ int copy_pages(void* pool, const int* count, const PageMove* moves, int most_mov
                int n_pages, cudaStream_t st) {
   const size_t page_bytes = static_cast<size_t>(n_kv) * page * (d + 8);
   const long long units = static_cast<long long>(most_moves) * layers * n_kv * (page / 16);
-  const long long ctas = (units + 15) / 16, room = static_cast<long long>(op_sm_count()) * 8;   // 8 warps, two units each
+  const long long ctas = (units + 15) / 16, room = static_cast<long long>(op_sm_count()) * 32;   // 8 warps, two units each; a resident wave (8 an SM) took 3 % longer
   return op_launch(d == 128 ? kv4_copy_pages_kernel<128> : kv4_copy_pages_kernel<64>,
                    dim3(static_cast<unsigned>(ctas < room ? ctas : room)), dim3(256), 0, st, true, static_cast<uint8_t*>(pool),
                    count, moves, layers, n_kv, page_shift_of(page), page_bytes, page_bytes * static_cast<size_t>(n_pages));
@@ -201,7 +201,7 @@ int thinfer_op_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int6
   a.n_kv = n_kv_heads;
   a.half = rotary_dim / 2;
   a.eps = eps;
-  a.chunks = share(tokens, static_cast<int64_t>(n_q_heads) + n_kv_heads, head_dim);
+  a.chunks = share(tokens, static_cast<int64_t>(n_q_heads) + n_kv_heads, head_dim / 8);
   const int64_t groups = static_cast<int64_t>(tokens) * a.chunks, per_cta = 256 / (head_dim / 8);
   const int64_t ctas = (groups + per_cta - 1) / per_cta;
   if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "qk_norm_rope: too many tokens");
@@ -234,12 +234,12 @@ int thinfer_op_kv4_append(void* pool, int32_t n_pages, const int32_t* table, int
   a.rows = rows;
   a.positions = positions;
   a.tokens = tokens;
-  a.chunks = share(tokens, 2 * static_cast<int64_t>(n_kv_heads), head_dim);
+  a.chunks = share(tokens, 2 * static_cast<int64_t>(n_kv_heads), head_dim / 16);
   a.k = static_cast<const half_t*>(k);
   a.v = static_cast<const half_t*>(v);
   a.k_stride = k_stride;
   a.v_stride = v_stride;
-  const int ctas = token_ctas(tokens, a.chunks, head_dim);
+  const int ctas = token_ctas(tokens, a.chunks, head_dim / 16);
   return op_launch(head_dim == 128 ? kv4_append_kernel<128> : kv4_append_kernel<64>, dim3(static_cast<unsigned>(ctas)),
                    dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), false, a);
 }
@@ -260,12 +260,12 @@ int thinfer_op_kv4_read(const void* pool, int32_t n_pages, const int32_t* table,
   a.rows = rows;
   a.positions = positions;
   a.tokens = tokens;
-  a.chunks = share(tokens, 2 * static_cast<int64_t>(n_kv_heads), head_dim);
+  a.chunks = share(tokens, 2 * static_cast<int64_t>(n_kv_heads), head_dim / 16);
   a.k_out = static_cast<half_t*>(k_out);
   a.v_out = static_cast<half_t*>(v_out);
   a.k_stride = a.v_stride = token_stride;
   a.k_head = a.v_head = head_stride;
-  const int ctas = token_ctas(tokens, a.chunks, head_dim);
+  const int ctas = token_ctas(tokens, a.chunks, head_dim / 16);
   return op_launch(head_dim == 128 ? kv4_read_kernel<128> : kv4_read_kernel<64>, dim3(static_cast<unsigned>(ctas)),
                    dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), false, a);
 }

@@ -1,8 +1,9 @@
-// Writing tokens into the 4-bit paged cache and reading them back.  Both are bound by memory: D / 8 lanes hold one
-// row (token, head, K or V) with one 16-byte access each, the row's extremes come from shuffles, and the codes leave
-// as one 32-bit word per lane.  A lane group looks its token's page up once and walks rows of that token, several in
-// flight at a time; how many groups share a token is set so that the device is full once, and each group goes on to
-// further tokens.
+// Writing tokens into the 4-bit paged cache and reading them back.  Both are bound by memory: D / 16 lanes hold one
+// row (token, head, K or V), 16 values each - with 8 values a lane the work that a row needs whatever its length took as
+// long as the memory (51 against 2x us for 6800 tokens of 32 heads) - the row's extremes come from shuffles of packed
+// 16-bit pairs, and the codes leave as 32-bit words (K) or as the halves that belong to the token (V).  A lane group looks
+// its token's page up once and walks rows of that token, several in flight at a time; how many groups share a token is
+// set so that the device is full once, and each group goes on to further tokens.
 #pragma once
 #include "kv4_layout.cuh"
 
@@ -61,22 +62,10 @@ struct Kv4Walk {
   }
 };
 
-constexpr int kKv4RowsInFlight = 4;
+constexpr int kKv4RowsInFlight = 2;     // of an append; a read's rows are a quarter as large
 
-__device__ __forceinline__ half2_t low_pair(half2_t a, half2_t b) {
-  half2_t d;
-  d.x = a.x;
-  d.y = b.x;
-  return d;
-}
-__device__ __forceinline__ half2_t high_pair(half2_t a, half2_t b) {
-  half2_t d;
-  d.x = a.y;
-  d.y = b.y;
-  return d;
-}
-// Largest of packed pairs, a NaN if there is one.
 __device__ __forceinline__ half2_t max2_nan(half2_t a, half2_t b) { return __hmax2_nan(a, b); }
+__device__ __forceinline__ half2_t min2_nan(half2_t a, half2_t b) { return __hmin2_nan(a, b); }
 
 // x / 15, correctly rounded: a product with the rounded reciprocal and one correction by the exact residual (Markstein's
 // division theorem).
@@ -118,25 +107,35 @@ __device__ __forceinline__ int kv4_first_v(int chunk, int chunks, int n_kv) {
 
 template <int D, bool V>
 __device__ __forceinline__ void kv4_append_rows(const Kv4TokensArgs& a, const Kv4Spot& s, const half_t* src, int first, unsigned mask, int sub) {
-  constexpr int LPR = D / 8, U = kKv4RowsInFlight;
+  constexpr int LPR = D / 16, U = kKv4RowsInFlight;
   const int n = a.c.n_kv, page = 1 << a.c.page_shift, step = a.chunks;
   uint8_t* const params = s.page + page * D + (V ? page * 4 : 0) + s.slot * 4;
-  uint8_t* const codes = s.page + (V ? page * (D / 2) + (s.slot >> 1) * D + sub * 8 + (s.slot & 1) * 2 : s.slot * (D / 2) + sub * 4);
-  src += sub * 8;
+  uint8_t* const codes = s.page + (V ? page * (D / 2) + (s.slot >> 1) * D + sub * 16 + (s.slot & 1) * 2 : s.slot * (D / 2) + sub * 8);
+  src += sub * 16;
   for (int h0 = first; h0 < n; h0 += U * step) {
-    uint4 raw[U];
+    uint4 raw[U][2];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (h0 + u * step < n) raw[u] = *reinterpret_cast<const uint4*>(src + (h0 + u * step) * D);
+      if (h0 + u * step < n) {
+        const uint4* p = reinterpret_cast<const uint4*>(src + (h0 + u * step) * D);
+        raw[u][0] = p[0];
+        raw[u][1] = p[1];
+      }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int h = h0 + u * step;
       if (h >= n) break;
-      // largest value and largest negated value of the row, as a pair: both are exact in 16 bits
-      const half2_t* x2 = reinterpret_cast<const half2_t*>(&raw[u]);
-      const half2_t up = max2_nan(max2_nan(x2[0], x2[1]), max2_nan(x2[2], x2[3]));
-      const half2_t down = max2_nan(max2_nan(__hneg2(x2[0]), __hneg2(x2[1])), max2_nan(__hneg2(x2[2]), __hneg2(x2[3])));
-      half2_t ends = max2_nan(low_pair(up, down), high_pair(up, down));
+      // extremes of the row, exact in 16 bits: largest value and largest negated value as one pair
+      const half2_t* x2 = reinterpret_cast<const half2_t*>(raw[u]);
+      half2_t up = x2[0], down = x2[0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) {
+        up = max2_nan(up, x2[j]);
+        down = min2_nan(down, x2[j]);
+      }
+      half2_t ends;
+      ends.x = __hmax_nan(up.x, up.y);
+      ends.y = __hneg(__hmin_nan(down.x, down.y));
 #pragma unroll
       for (int o = LPR / 2; o > 0; o >>= 1) {
         const uint32_t other = __shfl_xor_sync(mask, *reinterpret_cast<const uint32_t*>(&ends), o);
@@ -145,16 +144,23 @@ __device__ __forceinline__ void kv4_append_rows(const Kv4TokensArgs& a, const Kv
       const float2 hl = h2_to_f2(ends);
       const float hi = hl.x, lo = -hl.y, probe = (hi - lo) * 0.f;   // probe: NaN as soon as one value is NaN or infinite
       const float scale = h_to_f(f_to_h(by_15(hi - lo)));
-      float x[8];
-      unpack8(raw[u], x);
-      const uint32_t word = kv4_codes(x, lo, scale);
+      uint32_t word[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float x[8];
+        unpack8(raw[u][j], x);
+        word[j] = kv4_codes(x, lo, scale);
+      }
       const int at = h * a.c.block_bytes;
       if (sub == 0) *reinterpret_cast<uint32_t*>(params + at) = kv4_pack_params(scale + probe, lo + probe);
       if (!V) {
-        *reinterpret_cast<uint32_t*>(codes + at) = word;
-      } else {  // two groups of four dimensions, 16 bits each, in the halves that belong to this token of the pair
-        *reinterpret_cast<uint16_t*>(codes + at) = static_cast<uint16_t>(word);
-        *reinterpret_cast<uint16_t*>(codes + at + 4) = static_cast<uint16_t>(word >> 16);
+        *reinterpret_cast<uint2*>(codes + at) = make_uint2(word[0], word[1]);
+      } else {  // groups of four dimensions, 16 bits each, in the halves that belong to this token of the pair
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          *reinterpret_cast<uint16_t*>(codes + at + 8 * j) = static_cast<uint16_t>(word[j]);
+          *reinterpret_cast<uint16_t*>(codes + at + 8 * j + 4) = static_cast<uint16_t>(word[j] >> 16);
+        }
       }
     }
   }
@@ -162,9 +168,9 @@ __device__ __forceinline__ void kv4_append_rows(const Kv4TokensArgs& a, const Kv
 
 template <int D>
 __global__ void __launch_bounds__(256, 4) kv4_append_kernel(const Kv4TokensArgs a) {
-  constexpr int LPR = D / 8;
+  constexpr int LPR = D / 16;
   const int lane = threadIdx.x & 31, sub = lane % LPR;
-  const unsigned mask = (LPR == 16 ? 0xffffu : 0xffu) << (lane & ~(LPR - 1));
+  const unsigned mask = ((1u << LPR) - 1u) << (lane & ~(LPR - 1));
   const long long group = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) / LPR;
   const long long first = group / a.chunks, step = static_cast<long long>(gridDim.x) * blockDim.x / LPR / a.chunks;
   const int chunk = static_cast<int>(group - first * a.chunks), first_v = kv4_first_v(chunk, a.chunks, a.c.n_kv);
@@ -179,25 +185,27 @@ __global__ void __launch_bounds__(256, 4) kv4_append_kernel(const Kv4TokensArgs 
 
 template <int D, bool V>
 __device__ __forceinline__ void kv4_read_rows(const Kv4TokensArgs& a, const Kv4Spot& s, half_t* dst, long long head_stride, int first, int sub) {
-  constexpr int U = 2 * kKv4RowsInFlight;   // rows are a quarter as large here
+  constexpr int U = 2 * kKv4RowsInFlight;
   const int n = a.c.n_kv, page = 1 << a.c.page_shift, step = a.chunks;
   const uint8_t* const params = s.page + page * D + (V ? page * 4 : 0) + s.slot * 4;
-  const uint8_t* const codes = s.page + (V ? page * (D / 2) + (s.slot >> 1) * D + sub * 8 : s.slot * (D / 2) + sub * 4);
-  dst += sub * 8;
+  const uint8_t* const codes = s.page + (V ? page * (D / 2) + (s.slot >> 1) * D + sub * 16 : s.slot * (D / 2) + sub * 8);
+  dst += sub * 16;
   for (int h0 = first; h0 < n; h0 += U * step) {
-    uint32_t word[U], par[U];
+    uint2 word[U];
+    uint32_t par[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int at = (h0 + u * step) * a.c.block_bytes;
-      word[u] = 0;
+      word[u] = make_uint2(0, 0);
       par[u] = 0x7fff7fffu;                            // no page there: NaN
       if (s.page != nullptr && h0 + u * step < n) {
         par[u] = *reinterpret_cast<const uint32_t*>(params + at);
         if (!V) {
-          word[u] = *reinterpret_cast<const uint32_t*>(codes + at);
-        } else {  // both tokens of the pair: 8 bytes, this token's halves
-          const uint2 w = *reinterpret_cast<const uint2*>(codes + at);
-          word[u] = __byte_perm(w.x, w.y, s.slot & 1 ? 0x7632 : 0x5410);
+          word[u] = *reinterpret_cast<const uint2*>(codes + at);
+        } else {  // both tokens of the pair: 16 bytes, this token's halves
+          const uint4 w = *reinterpret_cast<const uint4*>(codes + at);
+          const int halves = s.slot & 1 ? 0x7632 : 0x5410;
+          word[u] = make_uint2(__byte_perm(w.x, w.y, halves), __byte_perm(w.z, w.w, halves));
         }
       }
     }
@@ -207,23 +215,28 @@ __device__ __forceinline__ void kv4_read_rows(const Kv4TokensArgs& a, const Kv4S
       if (h >= n) break;
       const float2 p = kv4_unpack_params(par[u]);
       // two codes at a time as the low mantissa bits of FP16 numbers: code * 2^-24, or 2^-20 from the high nibbles
-      float x[8];
       const float s0 = p.x * 0x1p24f, s1 = p.x * 0x1p20f;
+      uint4* out = reinterpret_cast<uint4*>(dst + h * head_stride);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t b = (j & 2 ? word[u] >> 8 : word[u]) & (j & 1 ? 0x00f000f0u : 0x000f000fu);
-        const float2 c = __half22float2(*reinterpret_cast<const __half2*>(&b));
-        x[j] = fmaf(j & 1 ? s1 : s0, c.x, p.y);
-        x[j + 4] = fmaf(j & 1 ? s1 : s0, c.y, p.y);
+      for (int g = 0; g < 2; ++g) {
+        const uint32_t w = g ? word[u].y : word[u].x;
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t b = (j & 2 ? w >> 8 : w) & (j & 1 ? 0x00f000f0u : 0x000f000fu);
+          const float2 c = __half22float2(*reinterpret_cast<const __half2*>(&b));
+          x[j] = fmaf(j & 1 ? s1 : s0, c.x, p.y);
+          x[j + 4] = fmaf(j & 1 ? s1 : s0, c.y, p.y);
+        }
+        out[g] = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
       }
-      *reinterpret_cast<uint4*>(dst + h * head_stride) = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
     }
   }
 }
 
 template <int D>
 __global__ void __launch_bounds__(256, 4) kv4_read_kernel(const Kv4TokensArgs a) {
-  constexpr int LPR = D / 8;
+  constexpr int LPR = D / 16;
   const int sub = (threadIdx.x & 31) % LPR;
   const long long group = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) / LPR;
   const long long first = group / a.chunks, step = static_cast<long long>(gridDim.x) * blockDim.x / LPR / a.chunks;
