@@ -66,9 +66,9 @@ int share(int64_t tokens, int64_t rows, int lanes) {
   return static_cast<int>(n < 1 ? 1 : n > rows ? rows : n);
 }
 
-// CTAs of 256 threads for that many groups per token: one resident wave (four per SM) at most, and at least one token's.
+// CTAs of 256 threads for that many groups per token: one resident wave (three per SM) at most, and at least one token's.
 int token_ctas(int64_t tokens, int chunks, int lanes) {
-  const int64_t per_cta = 256 / lanes, most = 4 * static_cast<int64_t>(op_sm_count());
+  const int64_t per_cta = 256 / lanes, most = 3 * static_cast<int64_t>(op_sm_count());
   const int64_t ctas = (tokens * chunks + per_cta - 1) / per_cta, least = (chunks + per_cta - 1) / per_cta;
   return static_cast<int>(ctas < most ? ctas : most > least ? most : least);
 }

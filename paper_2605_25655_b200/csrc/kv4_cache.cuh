@@ -1,6 +1,6 @@
 // Writing tokens into the 4-bit paged cache and reading them back.  Both are bound by memory: D / 16 lanes hold one
 // row (token, head, K or V), 16 values each - with 8 values a lane the work that a row needs whatever its length took as
-// long as the memory (51 against 2x us for 6800 tokens of 32 heads) - the row's extremes come from shuffles of packed
+// long as the memory (52 against 41 us to write, 32 against 28 us to read 6800 tokens of 32 heads) - the row's extremes come from shuffles of packed
 // 16-bit pairs, and the codes leave as 32-bit words (K) or as the halves that belong to the token (V).  A lane group looks
 // its token's page up once and walks rows of that token, several in flight at a time; how many groups share a token is
 // set so that the device is full once, and each group goes on to further tokens.
@@ -110,16 +110,16 @@ __device__ __forceinline__ void kv4_append_rows(const Kv4TokensArgs& a, const Kv
   constexpr int LPR = D / 16, U = kKv4RowsInFlight;
   const int n = a.c.n_kv, page = 1 << a.c.page_shift, step = a.chunks;
   uint8_t* const params = s.page + page * D + (V ? page * 4 : 0) + s.slot * 4;
-  uint8_t* const codes = s.page + (V ? page * (D / 2) + (s.slot >> 1) * D + sub * 16 + (s.slot & 1) * 2 : s.slot * (D / 2) + sub * 8);
-  src += sub * 16;
+  uint8_t* const codes = s.page + (V ? page * (D / 2) + (s.slot >> 1) * D + sub * 8 + (s.slot & 1) * 2 : s.slot * (D / 2) + sub * 4);
+  src += sub * 8;                      // values 8 sub .. 8 sub + 7 of each half of the row: accesses of a group lie side by side
   for (int h0 = first; h0 < n; h0 += U * step) {
     uint4 raw[U][2];
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (h0 + u * step < n) {
-        const uint4* p = reinterpret_cast<const uint4*>(src + (h0 + u * step) * D);
-        raw[u][0] = p[0];
-        raw[u][1] = p[1];
+        const half_t* p = src + (h0 + u * step) * D;
+        raw[u][0] = *reinterpret_cast<const uint4*>(p);
+        raw[u][1] = *reinterpret_cast<const uint4*>(p + D / 2);
       }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -154,12 +154,13 @@ __device__ __forceinline__ void kv4_append_rows(const Kv4TokensArgs& a, const Kv
       const int at = h * a.c.block_bytes;
       if (sub == 0) *reinterpret_cast<uint32_t*>(params + at) = kv4_pack_params(scale + probe, lo + probe);
       if (!V) {
-        *reinterpret_cast<uint2*>(codes + at) = make_uint2(word[0], word[1]);
+        *reinterpret_cast<uint32_t*>(codes + at) = word[0];
+        *reinterpret_cast<uint32_t*>(codes + at + D / 4) = word[1];
       } else {  // groups of four dimensions, 16 bits each, in the halves that belong to this token of the pair
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          *reinterpret_cast<uint16_t*>(codes + at + 8 * j) = static_cast<uint16_t>(word[j]);
-          *reinterpret_cast<uint16_t*>(codes + at + 8 * j + 4) = static_cast<uint16_t>(word[j] >> 16);
+          *reinterpret_cast<uint16_t*>(codes + at + j * (D / 2)) = static_cast<uint16_t>(word[j]);
+          *reinterpret_cast<uint16_t*>(codes + at + j * (D / 2) + 4) = static_cast<uint16_t>(word[j] >> 16);
         }
       }
     }
@@ -167,7 +168,7 @@ __device__ __forceinline__ void kv4_append_rows(const Kv4TokensArgs& a, const Kv
 }
 
 template <int D>
-__global__ void __launch_bounds__(256, 4) kv4_append_kernel(const Kv4TokensArgs a) {
+__global__ void __launch_bounds__(256, 3) kv4_append_kernel(const Kv4TokensArgs a) {
   constexpr int LPR = D / 16;
   const int lane = threadIdx.x & 31, sub = lane % LPR;
   const unsigned mask = ((1u << LPR) - 1u) << (lane & ~(LPR - 1));
@@ -185,11 +186,11 @@ __global__ void __launch_bounds__(256, 4) kv4_append_kernel(const Kv4TokensArgs 
 
 template <int D, bool V>
 __device__ __forceinline__ void kv4_read_rows(const Kv4TokensArgs& a, const Kv4Spot& s, half_t* dst, long long head_stride, int first, int sub) {
-  constexpr int U = 2 * kKv4RowsInFlight;
+  constexpr int U = 4 * kKv4RowsInFlight;
   const int n = a.c.n_kv, page = 1 << a.c.page_shift, step = a.chunks;
   const uint8_t* const params = s.page + page * D + (V ? page * 4 : 0) + s.slot * 4;
-  const uint8_t* const codes = s.page + (V ? page * (D / 2) + (s.slot >> 1) * D + sub * 16 : s.slot * (D / 2) + sub * 8);
-  dst += sub * 16;
+  const uint8_t* const codes = s.page + (V ? page * (D / 2) + (s.slot >> 1) * D + sub * 8 : s.slot * (D / 2) + sub * 4);
+  dst += sub * 8;
   for (int h0 = first; h0 < n; h0 += U * step) {
     uint2 word[U];
     uint32_t par[U];
@@ -201,11 +202,11 @@ __device__ __forceinline__ void kv4_read_rows(const Kv4TokensArgs& a, const Kv4S
       if (s.page != nullptr && h0 + u * step < n) {
         par[u] = *reinterpret_cast<const uint32_t*>(params + at);
         if (!V) {
-          word[u] = *reinterpret_cast<const uint2*>(codes + at);
-        } else {  // both tokens of the pair: 16 bytes, this token's halves
-          const uint4 w = *reinterpret_cast<const uint4*>(codes + at);
+          word[u] = make_uint2(*reinterpret_cast<const uint32_t*>(codes + at), *reinterpret_cast<const uint32_t*>(codes + at + D / 4));
+        } else {  // both tokens of the pair, this token's halves
+          const uint2 x = *reinterpret_cast<const uint2*>(codes + at), y = *reinterpret_cast<const uint2*>(codes + at + D / 2);
           const int halves = s.slot & 1 ? 0x7632 : 0x5410;
-          word[u] = make_uint2(__byte_perm(w.x, w.y, halves), __byte_perm(w.z, w.w, halves));
+          word[u] = make_uint2(__byte_perm(x.x, x.y, halves), __byte_perm(y.x, y.y, halves));
         }
       }
     }
@@ -216,7 +217,7 @@ __device__ __forceinline__ void kv4_read_rows(const Kv4TokensArgs& a, const Kv4S
       const float2 p = kv4_unpack_params(par[u]);
       // two codes at a time as the low mantissa bits of FP16 numbers: code * 2^-24, or 2^-20 from the high nibbles
       const float s0 = p.x * 0x1p24f, s1 = p.x * 0x1p20f;
-      uint4* out = reinterpret_cast<uint4*>(dst + h * head_stride);
+      half_t* out = dst + h * head_stride;
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
         const uint32_t w = g ? word[u].y : word[u].x;
@@ -228,14 +229,14 @@ __device__ __forceinline__ void kv4_read_rows(const Kv4TokensArgs& a, const Kv4S
           x[j] = fmaf(j & 1 ? s1 : s0, c.x, p.y);
           x[j + 4] = fmaf(j & 1 ? s1 : s0, c.y, p.y);
         }
-        out[g] = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
+        *reinterpret_cast<uint4*>(out + g * (D / 2)) = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
       }
     }
   }
 }
 
 template <int D>
-__global__ void __launch_bounds__(256, 4) kv4_read_kernel(const Kv4TokensArgs a) {
+__global__ void __launch_bounds__(256, 3) kv4_read_kernel(const Kv4TokensArgs a) {
   constexpr int LPR = D / 16;
   const int sub = (threadIdx.x & 31) % LPR;
   const long long group = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) / LPR;
