@@ -332,7 +332,9 @@ int thinfer_op_kv4_reserve(int32_t* table, const int32_t* lens, const int32_t* a
   if (lens == nullptr || add == nullptr || lens_out == nullptr || refused == nullptr || !aligned4(lens) || !aligned4(add) ||
       !aligned4(lens_out) || !aligned8(refused))
     return op_fail(THINFER_EINVAL, "kv4_reserve: a pointer is NULL or not 4-byte aligned");
-  const size_t nb = static_cast<size_t>(n_rows) * 4;
+  const size_t nb = static_cast<size_t>(n_rows) * 4, tb = nb * max_pages;
+  if (overlap(table, tb, lens, nb) || overlap(table, tb, add, nb) || overlap(table, tb, lens_out, nb) || overlap(table, tb, refused, 8))
+    return op_fail(THINFER_EINVAL, "kv4_reserve: the table overlaps another tensor");
   if ((lens_out != lens && overlap(lens_out, nb, lens, nb)) || overlap(lens_out, nb, add, nb) || overlap(refused, 8, lens, nb) ||
       overlap(refused, 8, add, nb) || overlap(refused, 8, lens_out, nb))
     return op_fail(THINFER_EINVAL, "kv4_reserve: lens_out may be lens itself; other outputs must not overlap inputs");

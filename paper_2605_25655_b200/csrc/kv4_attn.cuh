@@ -26,9 +26,9 @@
 // the rounded weights) and a packed FP32 multiply-add per pair of accumulators and 32 tokens: a rounding of w then
 // counts with the distance from the middle of the row, not with the whole code, and the accumulators stay as small as
 // the result, so that the truncation of the matrix unit's additions does not add up (over 16384 keys the FP16 error
-// against 64 bits was 3.2e-4 with the 8 taken off at the end, 2.1e-4 is the rounding of the result).
-// The running maximum and that reference move only when a weight
-// would exceed 2^8 (one vote per 32 tokens): the shuffles and the rescaling of the output are then off the usual path.
+// against 64 bits was 3.2e-4 with the 8 taken off at the end and 2.9e-4 now; 2.1e-4 is the rounding of the result).  The
+// running maximum and that reference move only when a weight would exceed 2^8 (one vote per 16 tokens): the shuffles and
+// the rescaling of the output are then off the usual path.
 //
 // Bound: HBM, D + 8 bytes per key and KV head; at 6.4 TB/s an SM has to consume 48 codes a cycle, which leaves 2.7
 // issue slots per code and half as many for the ANDs and shifts (half rate).  Work: all (request, KV head, column tile)
@@ -36,9 +36,15 @@
 // then to the warps of a CTA; the lengths are only known on the device, so each CTA sums them up itself.  Each warp
 // streams its units through a private ring in shared memory with 16-byte asynchronous copies, and needs no other warp
 // until its range is done.  (Bulk copies took fewer instructions to write but more to issue: four of them per 32 tokens
-// cost 150 issue cycles where nine 16-byte copies by all lanes cost 30, 209 against 1xx us for 64 x 16384 keys.)  What a warp
-// cannot finish is merged in shared memory; what a CTA cannot finish goes to the workspace and a second kernel, chained
-// to this one, merges it in CTA order: the result does not depend on timing, and the workspace needs no initial state.
+// cost 150 issue cycles where nine 16-byte copies by all lanes cost 30: 209 against 185 us for 64 requests of up to 16384
+// keys, 8 KV heads.)  What a warp cannot finish is merged in shared memory; what a CTA cannot finish goes to the workspace
+// and a second kernel, chained to this one, merges it in CTA order: the result does not depend on timing, and the
+// workspace needs no initial state.
+//
+// Measured: those 64 requests, 845 MB, in 168 us (5.0 TB/s, 78 % of a copy); held there for a second the kernel meets the
+// 1000 W limit and takes 193 us.  About 510 instructions per 32 tokens and warp, 54 % of the cycles of the half-rate integer
+// pipe, the rest latency that three warps per scheduler do not cover; without any arithmetic the copies alone take 129 us.
+// 16 requests of up to 1279 keys, 40 KV heads: 26 us, of which 5 pass before the first key arrives and 5 in the merges.
 #pragma once
 #include "kv4_layout.cuh"
 
@@ -454,9 +460,9 @@ __device__ __forceinline__ void kv4_stage(Kv4Acc<D, NT>& s, const uint8_t* stage
           for (int e = 0; e < 2; ++e) big = fmaxf(big, ex2_approx(raw(e, n, j, mx)) * vscale(e, n, j));
 #pragma unroll
           for (int off = 4; off < 32; off <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, off));
-          const int ex = min(max(__float_as_int(big) >> 23, 27), 227);
+          const int ex = min(max(__float_as_int(big) >> 23, 27), 252);
           const float ref = __int_as_float((254 - ex) << 23);
-          const float move = al * (ref * exact_inverse(s.ref[n][j]));
+          const float move = (al * ref) * exact_inverse(s.ref[n][j]);
           s.m[n][j] = mx;
           s.ref[n][j] = ref;
           s.l[n][j] *= al;
@@ -519,7 +525,7 @@ template <int D, int NT>
 __device__ __forceinline__ float4 kv4_value4(const Kv4Acc<D, NT>& s, int n, int j, int i, float z, float back) {
   constexpr float F0 = 16777216.f, F1 = 1048576.f;  // 2^24 and 2^20: the place of the code in its operand
   const float(&x)[4] = s.o[n][2 * i], (&y)[4] = s.o[n][2 * i + 1];
-  return make_float4(fmaf(x[j], F0 * back, z), fmaf(x[2 + j], F1 * back, z), fmaf(y[j], F0 * back, z), fmaf(y[2 + j], F1 * back, z));
+  return make_float4(fmaf(x[j] * F0, back, z), fmaf(x[2 + j] * F1, back, z), fmaf(y[j] * F0, back, z), fmaf(y[2 + j] * F1, back, z));
 }
 __device__ __forceinline__ void kv4_store4(half_t* dst, float4 v) {
   *reinterpret_cast<uint2*>(dst) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));

@@ -29,15 +29,6 @@ struct Kv4Cache {
   size_t page_bytes;     // n_kv * block_bytes
 };
 
-// Base of the block that holds (row, position) of `head`; nullptr when the table has no page of the pool there.
-__device__ __forceinline__ uint8_t* kv4_block(const Kv4Cache& c, int row, int pos, int head) {
-  const int col = pos >> c.page_shift;
-  if (row >= c.n_rows || col >= c.max_pages) return nullptr;
-  const int page = __ldg(c.table + static_cast<size_t>(row) * c.max_pages + col);
-  if (page < 0 || page >= c.n_pages) return nullptr;
-  return c.pool + static_cast<size_t>(page) * c.page_bytes + static_cast<size_t>(head) * c.block_bytes;
-}
-
 __device__ __forceinline__ uint32_t kv4_pack_params(float scale, float offset) { return pack2(scale, offset); }
 __device__ __forceinline__ float2 kv4_unpack_params(uint32_t p) { return h2_to_f2(*reinterpret_cast<const half2_t*>(&p)); }
 

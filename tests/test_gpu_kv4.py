@@ -284,7 +284,7 @@ def _check_attention(T, rng, t, hq, hkv, d, page, lens, queries, pool, tab, tabl
     (8, 1, 128, 64, [1], 1), (4, 4, 64, 16, [0], 1), (2, 1, 64, 16, [15, 16, 17, 0, 31, 32, 33], 1), (8, 2, 128, 16, [257, 1, 64, 65, 63], 1),
     (5, 5, 128, 64, [130, 7, 300], 1), (6, 2, 64, 32, [95, 500], 1), (16, 1, 128, 64, [511, 40], 1), (24, 2, 64, 128, [129, 400, 128], 1),
     (10, 2, 128, 64, [77, 0, 1000], 1), (8, 2, 128, 16, [3, 1, 0, 90], 4), (4, 4, 64, 64, [70, 2, 129], 3), (16, 2, 128, 32, [45, 200], 2),
-    (8, 1, 64, 16, [33, 5], 7), (2, 2, 128, 64, [66, 12, 13, 11, 10], 12), (1, 1, 64, 16, [2500], 1), (8, 8, 128, 128, [1500, 3], 1)])
+    (8, 1, 64, 16, [33, 5], 7), (3, 1, 128, 128, [129, 31], 5), (64, 2, 64, 64, [65, 7], 1), (2, 2, 128, 64, [66, 12, 13, 11, 10], 12), (1, 1, 64, 16, [2500], 1), (8, 8, 128, 128, [1500, 3], 1)])
 def test_attention(T, t, hq, hkv, d, page, lens, queries):
     rng = np.random.default_rng(hq * 1000 + d + sum(lens) + queries)
     pool, tab, table = _filled(T, rng, t, hkv, d, page, lens)
@@ -328,6 +328,71 @@ def test_attention_over_many_and_long_rows(T, batch, n):
         tol = EPS["f16"] * want.abs() + 2.0 ** -10 * spread + 2.0 ** -19 * (1 + 16 * mag) * far + 2.0 ** -25
         assert torch.all((got[i, 0] - want).abs() <= tol)
         del pos
+
+
+def test_attention_of_a_batch_of_rows_without_keys(T):
+    torch, thinfer = T
+    pool = _fresh_pool(torch, 3, 2, 64, 16)
+    q = torch.randn(5, 2, 4, 64, device="cuda").half()
+    for lens in ([0] * 5, [-3, 0, 0, -1, 0]):
+        out = torch.full((5, 2, 4, 64), 7.0, dtype=torch.float16, device="cuda")
+        thinfer.op_kv4_attention(q, pool, torch.full((5, 2), -1, dtype=torch.int32, device="cuda"), _int(torch, lens), 16, out=out)
+        assert torch.all(out == 0)
+
+
+def test_attention_of_2048_rows(T):
+    """The most a call takes; every seventh row is empty, the last rows too."""
+    torch, thinfer = T
+    rng = np.random.default_rng(2048)
+    lens = [0 if b % 7 == 0 or b >= 2040 else 1 + int(rng.integers(0, 70)) for b in range(2048)]
+    pool, tab, table = _filled(T, rng, "f16", 1, 64, 16, lens)
+    q = _values(rng, (2048, 1, 3, 64), "f16")
+    out = _host(thinfer.op_kv4_attention(_dev(torch, q, "f16"), pool, tab, _int(torch, lens), 16))
+    ref = kv4.Pool(pool.cpu().numpy(), 1, 64, 16, np.float16)
+    for i in list(range(0, 2048, 97)) + list(range(2030, 2048)):
+        kv = kv4.keys_values(ref, table[i], lens[i])
+        want, spread, mag = kv4.attention(q[i, 0], kv, lens[i], 0)
+        far = spread + np.abs(want) + kv4_abs(kv, q[i, 0], lens[i], 0)
+        assert np.all(np.abs(out[i, 0] - want) <= EPS["f16"] * np.abs(want) + 2.0 ** -10 * spread + 2.0 ** -19 * (1 + 16 * mag) * far + 2.0 ** -25)
+    assert np.all(out[::7] == 0) and np.all(out[2040:] == 0)
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+def test_attention_with_many_query_columns(T, t):
+    """40 query tokens of 8 heads: 20 column tiles; some queries come before the first key."""
+    rng = np.random.default_rng(40)
+    lens = [39, 100, 12]
+    pool, tab, table = _filled(T, rng, t, 1, 64, 16, lens)
+    _check_attention(T, rng, t, 8, 1, 64, 16, lens, 40, pool, tab, table)
+
+
+def test_attention_with_the_ends_of_bf16(T):
+    """Values of 1e30 and of 1e-25 side by side with ordinary ones, and queries of 1e-20 and 1e10."""
+    torch, thinfer = T
+    rng = np.random.default_rng(30)
+    for v_std, q_std, k_std in ((1e30, 1.0, 1.0), (1e-25, 1.0, 1.0), (1.0, 1e10, 1e-9), (1.0, 1e-20, 1e18)):
+        pool, tab, table = _filled(T, rng, "bf16", 2, 64, 16, [50, 3], k_std=k_std, v_std=v_std)
+        q = _values(rng, (2, 1, 4, 64), "bf16", q_std)
+        out = _host(thinfer.op_kv4_attention(_dev(torch, q, "bf16"), pool, tab, _int(torch, [50, 3]), 16))
+        ref = kv4.Pool(pool.cpu().numpy(), 2, 64, 16, "bf16")
+        for i, n in enumerate((50, 3)):
+            kv = kv4.keys_values(ref, table[i], n)
+            want, spread, mag = kv4.attention(q[i, 0], kv, n, 0)
+            far = spread + np.abs(want) + kv4_abs(kv, q[i, 0], n, 0)
+            assert np.all(np.abs(out[i, 0] - want) <= EPS["bf16"] * np.abs(want) + 2.0 ** -10 * spread + 2.0 ** -19 * (1 + 16 * mag) * far)
+
+
+def test_attention_of_queries_that_end_at_the_tables_edge(T):
+    """A length one beyond the table: only the queries that see the key that has no page give NaN."""
+    torch, thinfer = T
+    rng = np.random.default_rng(31)
+    pool, tab, table = _filled(T, rng, "f16", 1, 64, 16, [32])
+    tab = tab[:, :2].contiguous()
+    q = torch.randn(1, 3, 2, 64, device="cuda").half()
+    out = thinfer.op_kv4_attention(q, pool, tab, _int(torch, [33]), 16)
+    assert torch.all(out[0, :2].isfinite()) and torch.all(out[0, 2].isnan())
+    same = thinfer.op_kv4_attention(q[:, :2].contiguous(), pool, tab, _int(torch, [32]), 16)
+    assert torch.equal(out[:, :2], same)
 
 
 def _exact_rows(torch, pool, row, m, hkv, d, page):

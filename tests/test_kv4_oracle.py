@@ -171,7 +171,7 @@ def test_attention_refuses(lib):
     _refusals(lib.thinfer_op_kv4_attention, args, [
         *(({n: None}, E) for n in ("q", "pool", "table", "lens", "out", "ws")), *(({n: 0}, E) for n in ("batch", "queries", "hq", "hkv", "n_pages", "maxp")),
         ({"hq": 7}, U), ({"d": 80}, U), ({"page": 24}, U), ({"qs": 1016}, E), ({"qs": 1028}, E), ({"q": P + 4}, E), ({"out": P + 8}, E), ({"ws": P + 8}, E),
-        ({"wb": need.value - 1}, thinfer.ECAPACITY), ({"maxp": 1 << 26}, U)])
+        ({"wb": need.value - 1}, thinfer.ECAPACITY), ({"maxp": 1 << 26}, U), ({"batch": 2049}, U), ({"queries": 70000}, U)])
 
 
 def test_page_table_calls_refuse(lib):
@@ -180,7 +180,7 @@ def test_page_table_calls_refuse(lib):
     args = dict(t=T, l=L, a=A, lo=LO, r=R, rows=4, maxp=8, n_pages=32, page=16, st=None)
     _refusals(lib.thinfer_op_kv4_reserve, args, [
         *(({n: None}, E) for n in "tla"), ({"lo": None}, E), ({"r": None}, E), ({"rows": 0}, E), ({"maxp": 0}, E), ({"n_pages": -1}, E), ({"page": 17}, U),
-        ({"rows": 4097}, U), ({"n_pages": (1 << 18) + 1}, U), ({"lo": L + 4}, E), ({"lo": A}, E), ({"r": L}, E), ({"r": LO + 8}, E), ({"l": L + 2}, E)])
+        ({"rows": 4097}, U), ({"n_pages": (1 << 18) + 1}, U), ({"lo": L + 4}, E), ({"lo": A}, E), ({"r": L}, E), ({"r": LO + 8}, E), ({"l": L + 2}, E), ({"lo": T + 16}, E), ({"r": T + 8}, E)])
     need = C.c_size_t(0)
     assert lib.thinfer_kv4_pages_workspace(4, 32, C.byref(need)) == thinfer.OK and need.value >= 16 + 16 * 12
     assert lib.thinfer_kv4_pages_workspace(0, 32, C.byref(need)) == E and lib.thinfer_kv4_pages_workspace(4, 1 << 20, C.byref(need)) == U
