@@ -116,7 +116,7 @@ int copy_pages(void* pool, const int* count, const PageMove* moves, int most_mov
   const long long units = static_cast<long long>(most_moves) * layers * n_kv * (page / 16);
   const long long ctas = (units + 15) / 16, room = static_cast<long long>(op_sm_count()) * 32;   // 8 warps, two units each; a resident wave (8 an SM) took 3 % longer
   return op_launch(d == 128 ? kv4_copy_pages_kernel<128> : kv4_copy_pages_kernel<64>,
-                   dim3(static_cast<unsigned>(ctas < room ? ctas : room)), dim3(256), 0, st, true, static_cast<uint8_t*>(pool),
+                   dim3(static_cast<unsigned>(ctas < room ? ctas : room)), dim3(256), 0, st, static_cast<uint8_t*>(pool),
                    count, moves, layers, n_kv, page_shift_of(page), page_bytes, page_bytes * static_cast<size_t>(n_pages));
 }
 
@@ -145,8 +145,8 @@ template <int D, int NT>
 int launch_attention(const Kv4AttnArgs& a, int grid, cudaStream_t st) {
   const size_t smem = kv4_warps<NT>() * kv4_warp_bytes<D, NT>() + kv4_plan_bytes(a.batch);
   int rc = opt_in<kv4_attn_kernel<D, NT>>(smem);
-  if (rc == THINFER_OK) rc = op_launch(kv4_attn_kernel<D, NT>, dim3(grid), dim3(kv4_warps<NT>() * 32), smem, st, false, a);
-  if (rc == THINFER_OK) rc = op_launch(kv4_attn_join_kernel<D, NT>, dim3(grid), dim3(NT * 256), 0, st, true, a);
+  if (rc == THINFER_OK) rc = op_launch(kv4_attn_kernel<D, NT>, dim3(grid), dim3(kv4_warps<NT>() * 32), smem, st, a);
+  if (rc == THINFER_OK) rc = op_launch(kv4_attn_join_kernel<D, NT>, dim3(grid), dim3(NT * 256), 0, st, a);
   return rc;
 }
 
@@ -207,7 +207,7 @@ int thinfer_op_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int6
   if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "qk_norm_rope: too many tokens");
   auto kernel = head_dim == 128 ? (halves ? qk_norm_rope_kernel<128, true> : qk_norm_rope_kernel<128, false>)
                                 : (halves ? qk_norm_rope_kernel<64, true> : qk_norm_rope_kernel<64, false>);
-  return op_launch(kernel, dim3(static_cast<unsigned>(ctas)), dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), false, a);
+  return op_launch(kernel, dim3(static_cast<unsigned>(ctas)), dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), a);
 }
 
 int thinfer_kv4_page_bytes(int32_t n_kv_heads, int32_t head_dim, int32_t page_size, size_t* bytes) {
@@ -241,7 +241,7 @@ int thinfer_op_kv4_append(void* pool, int32_t n_pages, const int32_t* table, int
   a.v_stride = v_stride;
   const int ctas = token_ctas(tokens, a.chunks, head_dim / 16);
   return op_launch(head_dim == 128 ? kv4_append_kernel<128> : kv4_append_kernel<64>, dim3(static_cast<unsigned>(ctas)),
-                   dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), false, a);
+                   dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), a);
 }
 
 int thinfer_op_kv4_read(const void* pool, int32_t n_pages, const int32_t* table, int32_t n_rows, int32_t max_pages,
@@ -267,7 +267,7 @@ int thinfer_op_kv4_read(const void* pool, int32_t n_pages, const int32_t* table,
   a.k_head = a.v_head = head_stride;
   const int ctas = token_ctas(tokens, a.chunks, head_dim / 16);
   return op_launch(head_dim == 128 ? kv4_read_kernel<128> : kv4_read_kernel<64>, dim3(static_cast<unsigned>(ctas)),
-                   dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), false, a);
+                   dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), a);
 }
 
 int thinfer_kv4_attention_workspace(int32_t batch, int32_t queries, int32_t n_q_heads, int32_t n_kv_heads,
@@ -344,7 +344,7 @@ int thinfer_op_kv4_reserve(int32_t* table, const int32_t* lens, const int32_t* a
   const size_t smem = static_cast<size_t>(plan_words(n_pages)) * 8;
   rc = opt_in<kv4_reserve_kernel>(smem);
   if (rc != THINFER_OK) return rc;
-  return op_launch(kv4_reserve_kernel, dim3(1), dim3(plan_threads(n_rows, max_pages, n_pages)), smem, static_cast<cudaStream_t>(cuda_stream), false, t,
+  return op_launch(kv4_reserve_kernel, dim3(1), dim3(plan_threads(n_rows, max_pages, n_pages)), smem, static_cast<cudaStream_t>(cuda_stream), t,
                    table, add, lens_out, refused);
 }
 
@@ -386,7 +386,7 @@ int thinfer_op_kv4_fork(void* pool, int32_t n_layers, int32_t n_pages, const int
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   int* count = static_cast<int*>(workspace);
   PageMove* moves = reinterpret_cast<PageMove*>(static_cast<char*>(workspace) + 16);
-  rc = op_launch(kv4_fork_kernel, dim3(1), dim3(plan_threads(n_rows, max_pages, n_pages)), smem, st, false, t, source, table_out, lens_out, refused, count, moves);
+  rc = op_launch(kv4_fork_kernel, dim3(1), dim3(plan_threads(n_rows, max_pages, n_pages)), smem, st, t, source, table_out, lens_out, refused, count, moves);
   if (rc != THINFER_OK) return rc;
   return copy_pages(pool, count, moves, n_rows, n_layers, n_kv_heads, head_dim, page_size, n_pages, st);
 }
@@ -414,7 +414,7 @@ int thinfer_op_kv4_compact(void* pool, int32_t n_layers, int32_t n_pages, const 
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   int* count = static_cast<int*>(workspace);
   PageMove* moves = reinterpret_cast<PageMove*>(static_cast<char*>(workspace) + 16);
-  rc = op_launch(kv4_compact_kernel, dim3(1), dim3(plan_threads(n_rows, max_pages, n_pages)), smem, st, false, t, table_out, live_pages, count, moves);
+  rc = op_launch(kv4_compact_kernel, dim3(1), dim3(plan_threads(n_rows, max_pages, n_pages)), smem, st, t, table_out, live_pages, count, moves);
   if (rc != THINFER_OK) return rc;
   return copy_pages(pool, count, moves, most, n_layers, n_kv_heads, head_dim, page_size, n_pages, st);
 }

@@ -109,7 +109,7 @@ __host__ __device__ constexpr int kv4_warp_bytes() {
 // behind the last key of every query.
 __device__ __forceinline__ int kv4_len(const Kv4AttnArgs& a, int b) {
   const long long cap = min((static_cast<long long>(a.c.max_pages) << a.c.page_shift) + kKv4Unit + a.queries, 0x7fffffc0ll);
-  const int n = __ldg(a.lens + b);
+  const int n = a.lens[b];
   return n < 0 ? 0 : static_cast<int>(min(static_cast<long long>(n), cap));
 }
 // a / b of numbers that are not negative; nearly always both fit 32 bits, where a division costs a fifth
@@ -552,6 +552,7 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
   if (threadIdx.x < 2 * CW) pieces[threadIdx.x].pair = -1;
+  pdl_wait();
   if (threadIdx.x == 0) a.splits[blockIdx.x].last = -1;
   const Kv4Plan plan = kv4_plan(a, kv4_mem + CW * WARP_BYTES, warp_sums);
   // requests without keys: zeros, dealt out over the CTAs
@@ -587,7 +588,7 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
   const int par_from = P * D + (lane & 8 ? P * 4 : 0) + (lane & 3) * 16;
   auto load_ids = [&](int base) {
     const int col = base + lane;
-    return col < a.c.max_pages && (static_cast<long long>(col) << shift) < f_pl.len ? __ldg(f_row + col) : -1;
+    return col < a.c.max_pages && (static_cast<long long>(col) << shift) < f_pl.len ? f_row[col] : -1;
   };
   auto request = [&]() {               // one stage, if there is one left
     if (f_u < w_units) {
@@ -787,8 +788,23 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
 template <int D, int NT>
 __global__ void __launch_bounds__(NT * 256) kv4_attn_join_kernel(const Kv4AttnArgs a) {
   constexpr int NC = NT * 8, PART = kv4_partial_floats<D, NT>(), V = D / 32;
+  pdl_launch_dependents();
   pdl_wait();
   const int first = blockIdx.x, col = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // 32 pieces at a time: lane i reads the maximum and sum of piece i, then all lanes add up the outputs, whose loads do not
+  // wait for one another.  Piece 1 of the first CTA, piece 0 of the others.
+  auto piece = [&](int i) { return a.parts + (static_cast<size_t>(i) * 2 + (i == first ? 1 : 0)) * PART; };
+  auto max_and_sum = [&](int i0) {
+    return i0 + lane < static_cast<int>(gridDim.x) ? *reinterpret_cast<const float2*>(piece(i0 + lane) + NC * D + 2 * col) : make_float2(0.f, 0.f);
+  };
+  // most pairs end in the next CTA: the first pieces are read along with the word that says whether there is a pair at all
+  constexpr int EARLY = 2;
+  float early[EARLY][V];
+  float2 ml = max_and_sum(first);
+#pragma unroll
+  for (int i = 0; i < EARLY; ++i)
+#pragma unroll
+    for (int e = 0; e < V; ++e) early[i][e] = first + i < static_cast<int>(gridDim.x) ? piece(first + i)[col * D + e * 32 + lane] : 0.f;
   const Kv4Split sp = a.splits[first];
   if (sp.last < 0) return;
   const int out_col = sp.col0 + col;
@@ -796,21 +812,29 @@ __global__ void __launch_bounds__(NT * 256) kv4_attn_join_kernel(const Kv4AttnAr
   float m = kKv4Low, l = 0.f, o[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) o[e] = 0.f;
-  // 32 pieces at a time: lane i reads the maximum and sum of piece i, then all lanes add up the outputs, whose loads do not
-  // wait for one another.  Piece 1 of the first CTA, piece 0 of the others.
   for (int i0 = first; i0 <= sp.last; i0 += 32) {
     const int n = min(32, sp.last - i0 + 1);
-    auto piece = [&](int i) { return a.parts + (static_cast<size_t>(i0 + i) * 2 + (i0 + i == first ? 1 : 0)) * PART; };
-    const float2 ml = lane < n ? *reinterpret_cast<const float2*>(piece(lane) + NC * D + 2 * col) : make_float2(kKv4Low, 0.f);
+    if (i0 != first) ml = max_and_sum(i0);
+    if (lane >= n) ml = make_float2(kKv4Low, 0.f);
     const float mn = fmaxf(m, warp_max(ml.x)), f0 = ex2_approx(m - mn), f = ex2_approx(ml.x - mn);
     m = mn;
     l = fmaf(l, f0, warp_sum(ml.y * f));
 #pragma unroll
     for (int e = 0; e < V; ++e) o[e] *= f0;
+    int i = 0;
+    if (i0 == first) {                 // the pair ends in a later CTA: there are at least two pieces
+      static_assert(EARLY == 2, "pieces that every pair here has");
+#pragma unroll
+      for (; i < EARLY; ++i) {
+        const float g = __shfl_sync(0xffffffffu, f, i);
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = fmaf(early[i][e], g, o[e]);
+      }
+    }
 #pragma unroll 8
-    for (int i = 0; i < n; ++i) {
+    for (; i < n; ++i) {
       const float g = __shfl_sync(0xffffffffu, f, i);
-      const float* q = piece(i) + col * D + lane;
+      const float* q = piece(i0 + i) + col * D + lane;
 #pragma unroll
       for (int e = 0; e < V; ++e) o[e] = fmaf(q[e * 32], g, o[e]);
     }

@@ -34,12 +34,12 @@ struct Kv4Walk {
   long long token, step;
   int row1, pos1, row2, pos2, page1;   // of the next token, of the one after it; page of the next
   __device__ __forceinline__ void look(long long t, int& row, int& pos) const {
-    row = t < a.tokens ? __ldg(a.rows + t) : -1;
-    pos = t < a.tokens ? __ldg(a.positions + t) : -1;
+    row = t < a.tokens ? a.rows[t] : -1;
+    pos = t < a.tokens ? a.positions[t] : -1;
   }
   __device__ __forceinline__ int page_of(int row, int pos) const {
     if (row < 0 || pos < 0 || row >= a.c.n_rows || (pos >> a.c.page_shift) >= a.c.max_pages) return -1;
-    return __ldg(a.c.table + static_cast<size_t>(row) * a.c.max_pages + (pos >> a.c.page_shift));
+    return a.c.table[static_cast<size_t>(row) * a.c.max_pages + (pos >> a.c.page_shift)];
   }
   __device__ __forceinline__ Kv4Walk(const Kv4TokensArgs& args, long long first, long long step_) : a(args), token(first - step_), step(step_) {
     look(first, row1, pos1);
@@ -170,12 +170,14 @@ __device__ __forceinline__ void kv4_append_rows(const Kv4TokensArgs& a, const Kv
 template <int D>
 __global__ void __launch_bounds__(256, 3) kv4_append_kernel(const Kv4TokensArgs a) {
   constexpr int LPR = D / 16;
+  pdl_launch_dependents();
   const int lane = threadIdx.x & 31, sub = lane % LPR;
   const unsigned mask = ((1u << LPR) - 1u) << (lane & ~(LPR - 1));
   const long long group = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) / LPR;
   const long long first = group / a.chunks, step = static_cast<long long>(gridDim.x) * blockDim.x / LPR / a.chunks;
   const int chunk = static_cast<int>(group - first * a.chunks), first_v = kv4_first_v(chunk, a.chunks, a.c.n_kv);
   if (first >= step) return;
+  pdl_wait();
   Kv4Walk walk(a, first, step);
   for (Kv4Spot s; walk.next(s);) {
     if (s.page == nullptr) continue;  // the same for the group, and shuffles stay inside it
@@ -238,11 +240,13 @@ __device__ __forceinline__ void kv4_read_rows(const Kv4TokensArgs& a, const Kv4S
 template <int D>
 __global__ void __launch_bounds__(256, 3) kv4_read_kernel(const Kv4TokensArgs a) {
   constexpr int LPR = D / 16;
+  pdl_launch_dependents();
   const int sub = (threadIdx.x & 31) % LPR;
   const long long group = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) / LPR;
   const long long first = group / a.chunks, step = static_cast<long long>(gridDim.x) * blockDim.x / LPR / a.chunks;
   const int chunk = static_cast<int>(group - first * a.chunks), first_v = kv4_first_v(chunk, a.chunks, a.c.n_kv);
   if (first >= step) return;
+  pdl_wait();
   Kv4Walk walk(a, first, step);
   for (Kv4Spot s; walk.next(s);) {
     if (s.skip) continue;

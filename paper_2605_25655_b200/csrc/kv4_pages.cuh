@@ -176,6 +176,8 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_reserve_kernel(const PageTab
   extern __shared__ int plan_mem[];
   __shared__ int buf[33];
   __shared__ int wanted, bad;
+  pdl_launch_dependents();
+  pdl_wait();
   if (threadIdx.x == 0) wanted = bad = 0;
   __syncthreads();
   auto need_of = [&](int r, int* first, long long* after) {
@@ -234,6 +236,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_fork_kernel(const PageTables
   int* fresh = plan_mem + t.rows;         // [rows] page of a row's own copy, or -1
   int* from = plan_mem + 2 * t.rows;      // [rows] the source
   int* tokens = plan_mem + 3 * t.rows;    // [rows] the new length
+  pdl_wait();
   for (int r = threadIdx.x; r < t.rows; r += blockDim.x) owner[r] = 0x7fffffff;
   if (threadIdx.x == 0) bad = 0;
   const PageMap m = map_pages(t, plan_mem + 4 * t.rows, buf);
@@ -317,6 +320,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_compact_kernel(const PageTab
   extern __shared__ int plan_mem[];
   __shared__ int buf[33];
   pdl_launch_dependents();
+  pdl_wait();
   const PageMap m = map_pages(t, plan_mem, buf);
   const int stay = m.live_below(m.live), n_moves = m.live - stay;
   // moves in the order of their sources
@@ -353,6 +357,7 @@ __global__ void __launch_bounds__(256) kv4_copy_pages_kernel(uint8_t* pool, cons
                                                              int layers, int n_kv, int page_shift, size_t page_bytes,
                                                              size_t layer_bytes) {
   constexpr int R = D / 64, U = 2;     // rows of 32 pieces of each kind of codes
+  pdl_launch_dependents();
   pdl_wait();
   const int lane = threadIdx.x & 31, page = 1 << page_shift, group_shift = page_shift - 4;
   const long long warps = static_cast<long long>(gridDim.x) * (blockDim.x >> 5);

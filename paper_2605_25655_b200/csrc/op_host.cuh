@@ -26,10 +26,12 @@ inline int op_fail(int code, const char* fmt, ...) {
 // SM count of the current device (asked once per device).
 int op_sm_count();
 
-// One launch.  chained: the kernel may start while its predecessor in the stream is still running and waits for it
-// on the device (programmatic dependent launch).
+// One launch, chained to its predecessor in the stream by programmatic dependent launch: the kernel may be scheduled while
+// the predecessor is still running and waits for it (pdl_wait) before it touches anything in memory.
+// Kernels launched this way read what earlier kernels may write with ordinary loads, never through the read-only path:
+// the data need not be final when the kernel starts.
 template <typename... KArgs, typename... Args>
-int op_launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, bool chained, Args&&... args) {
+int op_launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
   cudaLaunchConfig_t lc{};
   lc.gridDim = grid;
   lc.blockDim = block;
@@ -37,12 +39,9 @@ int op_launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cuda
   lc.stream = st;
   cudaLaunchAttribute attr[1];
   lc.attrs = attr;
-  lc.numAttrs = 0;
-  if (chained) {
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    lc.numAttrs = 1;
-  }
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  lc.numAttrs = 1;
   const cudaError_t e = cudaLaunchKernelEx(&lc, kernel, static_cast<KArgs>(args)...);
   if (e != cudaSuccess) return op_fail(THINFER_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
   return THINFER_OK;

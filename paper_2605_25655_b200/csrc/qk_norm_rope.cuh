@@ -34,13 +34,15 @@ template <int D, bool HALVES>
 __global__ void __launch_bounds__(256, 4) qk_norm_rope_kernel(const QkNormRopeArgs a) {
   constexpr int LPR = D / 8;        // lanes per row
   constexpr int U = 2;
+  pdl_launch_dependents();
   const int lane = threadIdx.x & 31, sub = lane % LPR;
   const unsigned group_mask = (LPR == 16 ? 0xffffu : 0xffu) << (lane & ~(LPR - 1));
   const long long group = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) / LPR;
   const long long token = group / a.chunks;
   const int chunk = static_cast<int>(group - token * a.chunks);
   const int heads = a.n_q + a.n_kv;
-  const int pos = token < a.tokens ? __ldg(a.positions + token) : -1;
+  pdl_wait();
+  const int pos = token < a.tokens ? a.positions[token] : -1;
   if (pos < 0) return;              // the same for the group, and shuffles stay inside it
   // this lane's values: two runs of four.  Halves: values j .. j + 3 of both halves, or eight behind the rotated ones
   const int j0 = 4 * sub;
@@ -52,7 +54,7 @@ __global__ void __launch_bounds__(256, 4) qk_norm_rope_kernel(const QkNormRopeAr
     cs[i] = 1.f;
     sn[i] = 0.f;
     if (rotated) {
-      const double t = static_cast<double>(pos) * __ldg(a.turns + j0 + i);
+      const double t = static_cast<double>(pos) * a.turns[j0 + i];
       sincospif(2.f * static_cast<float>(t - rint(t)), &sn[i], &cs[i]);
     }
   }
