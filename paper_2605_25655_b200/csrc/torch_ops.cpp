@@ -6,6 +6,8 @@
 // allocations and twenty foreign-function arguments cost more in the interpreter (10 to 17 us) than the kernels take.
 #include <Python.h>
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -78,7 +80,10 @@ struct On {
     if (c10::cuda::current_device() != device.index()) guard.set_device(device);
     stream = c10::cuda::getCurrentCUDAStream(device.index()).stream();
   }
-  at::TensorOptions options(at::ScalarType t) const { return at::TensorOptions().dtype(t).device(device); }
+  // A new contiguous tensor of this device, straight from its allocator.
+  at::Tensor empty(at::IntArrayRef shape, at::ScalarType type) const { return at::detail::empty_cuda(shape, type, device, c10::nullopt); }
+  // Memory for the length of a call: given back to the stream's pool when it returns, as a tensor's would be.
+  c10::DataPtr scratch(size_t bytes) const { return c10::cuda::CUDACachingAllocator::get()->allocate(bytes); }
 };
 
 const Api& api_of(at::ScalarType t) {
@@ -154,8 +159,8 @@ PyObject* qk_norm_rope(PyObject* const* a) {
   const int64_t n = q.size(0), hq = q.size(1), d = q.size(2), hkv = k.size(1);
   if (k.size(0) != n || k.size(2) != d) refuse("q and k must agree in tokens and head_dim");
   if (turns.dim() != 1) refuse("turns: FP64 [rotary_dim / 2]");
-  const at::Tensor q_out = given_or(a[8], "q_out", [&] { return at::empty({n, hq, d}, on.options(type)); });
-  const at::Tensor k_out = given_or(a[9], "k_out", [&] { return at::empty({n, hkv, d}, on.options(type)); });
+  const at::Tensor q_out = given_or(a[8], "q_out", [&] { return on.empty({n, hq, d}, type); });
+  const at::Tensor k_out = given_or(a[9], "k_out", [&] { return on.empty({n, hkv, d}, type); });
   same_shape(q_out, q, "q_out: the shape of q");
   same_shape(k_out, k, "k_out: the shape of k");
   const int64_t qos = token_stride(q_out, "q_out", type, on), kos = token_stride(k_out, "k_out", type, on);
@@ -173,8 +178,8 @@ PyObject* reserve(PyObject* const* a) {
   const On on(table);
   const int32_t* tab = table_of(table, on);
   const int64_t rows = table.size(0);
-  const at::Tensor lens_out = given_or(a[5], "lens_out", [&] { return at::empty({rows}, on.options(at::kInt)); });
-  const at::Tensor refused = given_or(a[6], "refused", [&] { return at::empty({1}, on.options(at::kLong)); });
+  const at::Tensor lens_out = given_or(a[5], "lens_out", [&] { return on.empty({rows}, at::kInt); });
+  const at::Tensor refused = given_or(a[6], "refused", [&] { return on.empty({1}, at::kLong); });
   check(g_api[0], g_api[0].reserve(const_cast<int32_t*>(tab), static_cast<const int32_t*>(plain(lens, "lens", on, {rows})),
                                    static_cast<const int32_t*>(plain(add, "add", on, {rows})),
                                    static_cast<int32_t*>(plain(lens_out, "lens_out", on, {rows})),
@@ -210,8 +215,8 @@ PyObject* read(PyObject* const* a) {
   const int64_t page = number(a[4], "page_size"), d = number(a[5], "head_dim"), hkv = pool_heads(pool, 2, page, d, on), n = positions.numel();
   const at::ScalarType type = PyObject_IsTrue(a[6]) == 1 ? at::kBFloat16 : at::kHalf;
   const Api& api = api_of(type);
-  const at::Tensor k_out = given_or(a[7], "k_out", [&] { return at::empty({n, hkv, d}, on.options(type)); });
-  const at::Tensor v_out = given_or(a[8], "v_out", [&] { return at::empty_strided({n, hkv, d}, k_out.strides(), on.options(type)); });
+  const at::Tensor k_out = given_or(a[7], "k_out", [&] { return on.empty({n, hkv, d}, type); });
+  const at::Tensor v_out = given_or(a[8], "v_out", [&] { return at::empty_strided({n, hkv, d}, k_out.strides(), k_out.options()); });
   const int64_t shape[3] = {n, hkv, d};
   for (const at::Tensor* t : {&k_out, &v_out})
     if (!t->sizes().equals(shape) || t->scalar_type() != type || t->device() != on.device || !t->strides().equals(k_out.strides()))
@@ -239,23 +244,29 @@ PyObject* attention(PyObject* const* a) {
   const int64_t hkv = pool_heads(pool, 2, page, d, on);
   const int32_t* tab = table_of(table, on);
   if (table.size(0) != b) refuse("table: one row per request");
-  const at::Tensor out = given_or(a[5], "out", [&] { return at::empty({b, n, hq, d}, on.options(type)); });
-  const at::Tensor ws = given_or(a[6], "workspace", [&] {
-    size_t need = 0;
-    check(api, api.attention_workspace(small(b, "batch"), small(n, "queries"), small(hq, "heads"), small(hkv, "heads"), small(d, "head_dim"), &need));
-    return at::empty({static_cast<int64_t>(need)}, on.options(at::kByte));
-  });
+  const at::Tensor out = given_or(a[5], "out", [&] { return on.empty({b, n, hq, d}, type); });
+  c10::DataPtr own;
+  void* ws = nullptr;
+  size_t ws_bytes = 0;
+  if (a[6] == Py_None) {
+    check(api, api.attention_workspace(small(b, "batch"), small(n, "queries"), small(hq, "heads"), small(hkv, "heads"), small(d, "head_dim"), &ws_bytes));
+    own = on.scratch(ws_bytes);
+    ws = own.get();
+  } else {
+    const at::Tensor& given = tensor(a[6], "workspace");
+    ws_bytes = static_cast<size_t>(given.numel());
+    ws = plain(given, "workspace", on, {given.numel()}, at::kByte);
+  }
   check(api, api.attention(q.data_ptr(), qs, pool.data_ptr(), small(pool.size(0), "pages"), tab, small(table.size(1), "max_pages"),
                            static_cast<const int32_t*>(plain(lens, "lens", on, {b})), plain(out, "out", on, {b, n, hq, d}, type), small(b, "batch"),
                            small(n, "queries"), small(hq, "heads"), small(hkv, "heads"), small(d, "head_dim"), small(page, "page_size"),
-                           plain(ws, "workspace", on, {ws.numel()}, at::kByte), static_cast<size_t>(ws.numel()), on.stream));
+                           ws, ws_bytes, on.stream));
   return wrap(out);
 }
 
-at::Tensor pages_workspace(int64_t rows, int64_t n_pages, const On& on) {
-  size_t need = 0;
-  check(g_api[0], g_api[0].pages_workspace(small(rows, "rows"), small(n_pages, "pages"), &need));
-  return at::empty({static_cast<int64_t>(need)}, on.options(at::kByte));
+c10::DataPtr pages_workspace(int64_t rows, int64_t n_pages, const On& on, size_t* bytes) {
+  check(g_api[0], g_api[0].pages_workspace(small(rows, "rows"), small(n_pages, "pages"), bytes));
+  return on.scratch(*bytes);
 }
 
 // pool, table, lens, source, page_size, head_dim, table_out, lens_out, refused
@@ -265,16 +276,17 @@ PyObject* fork(PyObject* const* a) {
   const int64_t page = number(a[4], "page_size"), d = number(a[5], "head_dim"), hkv = pool_heads(pool, 3, page, d, on);
   const int32_t* tab = table_of(table, on);
   const int64_t rows = table.size(0), width = table.size(1);
-  const at::Tensor table_out = given_or(a[6], "table_out", [&] { return at::empty({rows, width}, on.options(at::kInt)); });
-  const at::Tensor lens_out = given_or(a[7], "lens_out", [&] { return at::empty({rows}, on.options(at::kInt)); });
-  const at::Tensor refused = given_or(a[8], "refused", [&] { return at::empty({1}, on.options(at::kLong)); });
-  const at::Tensor ws = pages_workspace(rows, pool.size(1), on);
+  const at::Tensor table_out = given_or(a[6], "table_out", [&] { return on.empty({rows, width}, at::kInt); });
+  const at::Tensor lens_out = given_or(a[7], "lens_out", [&] { return on.empty({rows}, at::kInt); });
+  const at::Tensor refused = given_or(a[8], "refused", [&] { return on.empty({1}, at::kLong); });
+  size_t ws_bytes = 0;
+  const c10::DataPtr ws = pages_workspace(rows, pool.size(1), on, &ws_bytes);
   check(g_api[0], g_api[0].fork(pool.data_ptr(), small(pool.size(0), "layers"), small(pool.size(1), "pages"), tab,
                                 static_cast<const int32_t*>(plain(lens, "lens", on, {rows})), static_cast<const int32_t*>(plain(source, "source", on, {rows})),
                                 static_cast<int32_t*>(plain(table_out, "table_out", on, {rows, width})),
                                 static_cast<int32_t*>(plain(lens_out, "lens_out", on, {rows})),
                                 static_cast<int64_t*>(plain(refused, "refused", on, {1}, at::kLong)), small(rows, "rows"), small(width, "max_pages"),
-                                small(hkv, "heads"), small(d, "head_dim"), small(page, "page_size"), ws.data_ptr(), static_cast<size_t>(ws.numel()), on.stream));
+                                small(hkv, "heads"), small(d, "head_dim"), small(page, "page_size"), ws.get(), ws_bytes, on.stream));
   return pack({table_out, lens_out, refused});
 }
 
@@ -285,14 +297,15 @@ PyObject* compact(PyObject* const* a) {
   const int64_t page = number(a[3], "page_size"), d = number(a[4], "head_dim"), hkv = pool_heads(pool, 3, page, d, on);
   const int32_t* tab = table_of(table, on);
   const int64_t rows = table.size(0), width = table.size(1);
-  const at::Tensor table_out = given_or(a[5], "table_out", [&] { return at::empty({rows, width}, on.options(at::kInt)); });
-  const at::Tensor live = given_or(a[6], "live", [&] { return at::empty({1}, on.options(at::kLong)); });
-  const at::Tensor ws = pages_workspace(rows, pool.size(1), on);
+  const at::Tensor table_out = given_or(a[5], "table_out", [&] { return on.empty({rows, width}, at::kInt); });
+  const at::Tensor live = given_or(a[6], "live", [&] { return on.empty({1}, at::kLong); });
+  size_t ws_bytes = 0;
+  const c10::DataPtr ws = pages_workspace(rows, pool.size(1), on, &ws_bytes);
   check(g_api[0], g_api[0].compact(pool.data_ptr(), small(pool.size(0), "layers"), small(pool.size(1), "pages"), tab,
                                    static_cast<const int32_t*>(plain(lens, "lens", on, {rows})),
                                    static_cast<int32_t*>(plain(table_out, "table_out", on, {rows, width})),
                                    static_cast<int64_t*>(plain(live, "live", on, {1}, at::kLong)), small(rows, "rows"), small(width, "max_pages"),
-                                   small(hkv, "heads"), small(d, "head_dim"), small(page, "page_size"), ws.data_ptr(), static_cast<size_t>(ws.numel()),
+                                   small(hkv, "heads"), small(d, "head_dim"), small(page, "page_size"), ws.get(), ws_bytes,
                                    on.stream));
   return pack({table_out, live});
 }
