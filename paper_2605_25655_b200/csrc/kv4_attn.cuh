@@ -41,7 +41,7 @@
 // and a second kernel, chained to this one, merges it in CTA order: the result does not depend on timing, and the
 // workspace needs no initial state.
 //
-// Measured: those 64 requests, 845 MB, in 164 us (5.2 TB/s, 80 % of a copy); held there for a second the kernel meets the
+// Measured: those 64 requests, 845 MB, in 162 us (5.2 TB/s, 81 % of a copy); held there for a second the kernel meets the
 // 1000 W limit and takes 190 us.  About 510 instructions per 32 tokens and warp, 54 % of the cycles of the half-rate integer
 // pipe, the rest latency that three warps per scheduler do not cover; without any arithmetic the copies alone take 129 us.
 // 16 requests of up to 1279 keys, 40 KV heads: 26 us, of which 5 pass before the first key arrives and 5 in the merges.
@@ -437,7 +437,7 @@ __device__ __forceinline__ void kv4_stage(Kv4Acc<D, NT>& s, const uint8_t* stage
     float top = 0.f;
     auto weights = [&]() {
       top = 0.f;
-      if constexpr (!MASKED) {   // both columns at once in packed FP32: 164 instead of 168 us
+      if constexpr (!MASKED) {   // both columns at once in packed FP32: 4 of 168 us
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const uint64_t qf = f32x2(s.qf[n][0], s.qf[n][1]), qs = f32x2(s.qs[n][0], s.qs[n][1]);
@@ -556,6 +556,13 @@ __device__ __forceinline__ float4 kv4_value4(const Kv4Acc<D, NT>& s, int n, int 
 __device__ __forceinline__ void kv4_store4(half_t* dst, float4 v) {
   *reinterpret_cast<uint2*>(dst) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
 }
+// Where 16 bytes of a column of an unfinished piece lie in shared memory: permuted so that the 8 lanes (two rows r, four
+// column pairs) that store together meet different banks.
+template <int D>
+__device__ __forceinline__ int kv4_piece_at(int col, int p) {  // p: 16-byte part of the column's D floats
+  const int c = (col >> 1) & 3;
+  return col * D + ((p ^ (D == 128 ? c : (c & 1) | (c & 2) << 1)) << 2);
+}
 // First output element of a column.
 template <int D>
 __device__ __forceinline__ half_t* kv4_out(const Kv4AttnArgs& a, int b, int hk, int col) {
@@ -576,7 +583,7 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
   __shared__ long long warp_sums[CW];
   __shared__ Kv4Piece pieces[2 * CW];       // unfinished pieces, 2 w: head, 2 w + 1: tail of warp w
   pdl_launch_dependents();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (threadIdx.x < 2 * CW) pieces[threadIdx.x].pair = -1;
   pdl_wait();
   if (threadIdx.x == 0) a.splits[blockIdx.x].last = -1;
@@ -703,6 +710,9 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
       slot = slot + 1 == NS ? 0 : slot + 1;
     }
     // ---- the segment's result: sums over the lanes that hold other tokens of the same columns
+    int here;
+    asm volatile("mov.u32 %0, %%laneid;" : "=r"(here));   // opaque: addresses kept for this in the loop above cost it 5 of 162 us
+    const int r = here >> 2, c = here & 3;
     const bool head = pl.unit > 0, whole = !head && n_units == pl.units;
     // the piece that ends the range takes the ring, which nobody fills any more
     float* part = reinterpret_cast<float*>(mine + (head ? WARP_BYTES - PART * 4 : 0));
@@ -733,7 +743,7 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
         } else {
 #pragma unroll
           for (int i = 0; i < W; ++i)
-            *reinterpret_cast<float4*>(part + col * D + r * (D / 8) + 4 * i) = kv4_value4<D, NT>(s, n, j, i, z, back);
+            *reinterpret_cast<float4*>(part + kv4_piece_at<D>(col, r * W + i)) = kv4_value4<D, NT>(s, n, j, i, z, back);
           if (r == 0) *reinterpret_cast<float2*>(part + NC * D + 2 * col) = make_float2(s.m[n][j], l);
         }
       }
@@ -742,70 +752,88 @@ __global__ void __launch_bounds__(kv4_warps<NT>() * 32, 1) kv4_attn_kernel(const
   }
   __syncthreads();
 
-  // ---- unfinished pieces, pair by pair: a warp takes some columns of a pair at a time (two in a pass where 16 lanes cover
-  // one).  Lane i knows piece i.
-  constexpr int PASS = 128 / D;
-  const int TASKS = (min(NC, a.cols) + PASS - 1) / PASS;   // only the last tile of several has fewer columns
+  // ---- unfinished pieces.  Lane i knows piece i; a task is GROUP columns of one pair, dealt over the warps.  A warp adds up
+  // CHAINS columns beside each other (each of them two where 16 lanes cover one): a task is all latency.
+  constexpr int CHAINS = 2, PASS = 128 / D, GROUP = CHAINS * PASS;
   static_assert(2 * CW <= 32, "a lane for every piece");
+  static_assert(NC % GROUP == 0, "whole tasks");
+  const int tasks = (min(NC, a.cols) + GROUP - 1) / GROUP;   // only the last tile of several has fewer columns
   const long long my_pair = lane < 2 * CW ? pieces[lane].pair : -1;
+  const unsigned my_members = __match_any_sync(0xffffffffu, my_pair);
+  const bool leads = my_pair >= 0 && __ffs(my_members) - 1 == lane;
+  const unsigned leaders = __ballot_sync(0xffffffffu, leads);
+  const int my_rank = __popc(leaders & ((1u << lane) - 1));
   const float* const my_part = reinterpret_cast<const float*>(kv4_mem + (lane >> 1) * WARP_BYTES + ((lane & 1) ? 0 : WARP_BYTES - PART * 4));
-  int task = -warp;                      // the warp's next task among those of the pairs so far
-  for (unsigned left = __ballot_sync(0xffffffffu, my_pair >= 0); left != 0;) {
-    const int k = __ffs(left) - 1;
-    const long long pair = __shfl_sync(0xffffffffu, my_pair, k);
-    const unsigned members = __ballot_sync(0xffffffffu, my_pair == pair);
-    left &= ~members;
-    task += TASKS;
-    if (task <= 0) continue;
+  for (int task = warp; task < __popc(leaders) * tasks; task += CW) {
+    const int rank = task / tasks, col0 = (task - rank * tasks) * GROUP;
+    const int k = __ffs(__ballot_sync(0xffffffffu, leads && my_rank == rank)) - 1;   // the pair's first piece
+    const unsigned members = __shfl_sync(0xffffffffu, my_members, k);
     const Kv4Piece pc = pieces[k];
-    const bool done = pair >= c_beg && pair + pc.units <= c_beg + c_units;
-    float* ws = a.parts + (static_cast<size_t>(blockIdx.x) * 2 + (pair < c_beg ? 0 : 1)) * PART;
-    if (!done && pair >= c_beg && task == TASKS && lane == 0)
-      a.splits[blockIdx.x] = Kv4Split{pc.b, pc.hk, pc.col0, static_cast<int>(kv4_cta_of(total, ctas, pair + pc.units - 1))};
     const bool member = (members >> lane) & 1u;
-    for (; task > 0; task -= CW) {
-      const int first_col = (TASKS - task) * PASS;
-      float top[PASS], l[PASS], f[PASS];   // of the pass's columns; f: this lane's piece
+    float top[GROUP], l[GROUP], f[GROUP];   // of the task's columns; f: this lane's piece
 #pragma unroll
-      for (int i = 0; i < PASS; ++i) {
-        const float2 ml = member ? *reinterpret_cast<const float2*>(my_part + NC * D + 2 * (first_col + i)) : make_float2(kKv4Low, 0.f);
-        top[i] = warp_max(ml.x);
-        f[i] = ex2_approx(ml.x - top[i]);
-        l[i] = warp_sum(ml.y * f[i]);
-      }
-      const int mine_col = PASS == 1 ? 0 : lane >> 4, col = first_col + mine_col, d = (lane * 4) % D;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (unsigned rest = members; rest != 0;) {   // four pieces at a time
-        float g[4];
-        float4 x[4];
+    for (int i = 0; i < GROUP; ++i) {
+      const float2 ml = member ? *reinterpret_cast<const float2*>(my_part + NC * D + 2 * (col0 + i)) : make_float2(kKv4Low, 0.f);
+      top[i] = ml.x;
+      l[i] = ml.y;
+    }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const bool more = rest != 0;
-          const int i = more ? __ffs(rest) - 1 : k;  // behind the last piece: a piece of the pair again, with weight 0
-          rest &= rest - 1;
-          g[q] = __shfl_sync(0xffffffffu, f[0], i);
+    for (int i = 0; i < GROUP; ++i) {
+      const float m = top[i];
+      top[i] = warp_max(m);
+      f[i] = ex2_approx(m - top[i]);
+      l[i] = warp_sum(l[i] * f[i]);
+    }
+    const int mine_col = PASS == 1 ? 0 : lane >> 4, d = (lane * 4) % D;
+    float4 v[CHAINS];
+#pragma unroll
+    for (int h = 0; h < CHAINS; ++h) v[h] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (unsigned rest = members; rest != 0;) {   // four pieces at a time
+      float g[4][CHAINS];
+      float4 x[4][CHAINS];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const bool more = rest != 0;
+        const int i = more ? __ffs(rest) - 1 : k;  // behind the last piece: a piece of the pair again, with weight 0
+        rest &= rest - 1;
+        const float* part = reinterpret_cast<const float*>(kv4_mem + (i >> 1) * WARP_BYTES + ((i & 1) ? 0 : WARP_BYTES - PART * 4));
+#pragma unroll
+        for (int h = 0; h < CHAINS; ++h) {
+          g[q][h] = __shfl_sync(0xffffffffu, f[h * PASS], i);
           if (PASS == 2) {
-            const float g1 = __shfl_sync(0xffffffffu, f[PASS - 1], i);
-            g[q] = mine_col ? g1 : g[q];
+            const float g1 = __shfl_sync(0xffffffffu, f[h * PASS + PASS - 1], i);
+            g[q][h] = mine_col ? g1 : g[q][h];
           }
-          if (!more) g[q] = 0.f;
-          x[q] = *reinterpret_cast<const float4*>(kv4_mem + (i >> 1) * WARP_BYTES + ((i & 1) ? 0 : WARP_BYTES - PART * 4) + (col * D + d) * 4);
+          if (!more) g[q][h] = 0.f;
+          x[q][h] = *reinterpret_cast<const float4*>(part + kv4_piece_at<D>(col0 + h * PASS + mine_col, d >> 2));
         }
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          v = make_float4(fmaf(x[q].x, g[q], v.x), fmaf(x[q].y, g[q], v.y), fmaf(x[q].z, g[q], v.z), fmaf(x[q].w, g[q], v.w));
       }
-      const float sum = PASS == 2 && mine_col ? l[PASS - 1] : l[0], largest = PASS == 2 && mine_col ? top[PASS - 1] : top[0];
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int h = 0; h < CHAINS; ++h)
+          v[h] = make_float4(fmaf(x[q][h].x, g[q][h], v[h].x), fmaf(x[q][h].y, g[q][h], v[h].y), fmaf(x[q][h].z, g[q][h], v[h].z),
+                             fmaf(x[q][h].w, g[q][h], v[h].w));
+    }
+    const bool done = pc.pair >= c_beg && pc.pair + pc.units <= c_beg + c_units;
+    float* ws = a.parts + (static_cast<size_t>(blockIdx.x) * 2 + (pc.pair < c_beg ? 0 : 1)) * PART;
+#pragma unroll
+    for (int h = 0; h < CHAINS; ++h) {
+      const int col = col0 + h * PASS + mine_col;
+      const float sum = PASS == 2 && mine_col ? l[h * PASS + PASS - 1] : l[h * PASS];
+      const float largest = PASS == 2 && mine_col ? top[h * PASS + PASS - 1] : top[h * PASS];
       if (done) {
         if (pc.col0 + col < a.cols) {
           const float inv = sum == 0.f ? 0.f : 1.f / sum;
-          kv4_store4(kv4_out<D>(a, pc.b, pc.hk, pc.col0 + col) + d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+          kv4_store4(kv4_out<D>(a, pc.b, pc.hk, pc.col0 + col) + d, make_float4(v[h].x * inv, v[h].y * inv, v[h].z * inv, v[h].w * inv));
         }
       } else {
-        *reinterpret_cast<float4*>(ws + col * D + d) = v;
+        *reinterpret_cast<float4*>(ws + col * D + d) = v[h];
         if (d == 0) *reinterpret_cast<float2*>(ws + NC * D + 2 * col) = make_float2(largest, sum);
       }
     }
+    if (!done && pc.pair >= c_beg && col0 == 0 && lane == 0)
+      a.splits[blockIdx.x] = Kv4Split{pc.b, pc.hk, pc.col0, static_cast<int>(kv4_cta_of(total, ctas, pc.pair + pc.units - 1))};
   }
 }
 
@@ -820,17 +848,19 @@ __global__ void __launch_bounds__(NT * 256) kv4_attn_join_kernel(const Kv4AttnAr
   // 32 pieces at a time: lane i reads the maximum and sum of piece i, then all lanes add up the outputs, whose loads do not
   // wait for one another.  Piece 1 of the first CTA, piece 0 of the others.
   auto piece = [&](int i) { return a.parts + (static_cast<size_t>(i) * 2 + (i == first ? 1 : 0)) * PART; };
+  struct alignas(4 * V) Wide {
+    float v[V];
+  };
+  auto values = [&](int i) { return reinterpret_cast<const Wide*>(piece(i) + col * D)[lane]; };
   auto max_and_sum = [&](int i0) {
     return i0 + lane < static_cast<int>(gridDim.x) ? *reinterpret_cast<const float2*>(piece(i0 + lane) + NC * D + 2 * col) : make_float2(0.f, 0.f);
   };
   // most pairs end in the next CTA: the first pieces are read along with the word that says whether there is a pair at all
   constexpr int EARLY = 2;
-  float early[EARLY][V];
+  Wide early[EARLY];
   float2 ml = max_and_sum(first);
 #pragma unroll
-  for (int i = 0; i < EARLY; ++i)
-#pragma unroll
-    for (int e = 0; e < V; ++e) early[i][e] = first + i < static_cast<int>(gridDim.x) ? piece(first + i)[col * D + e * 32 + lane] : 0.f;
+  for (int i = 0; i < EARLY; ++i) early[i] = first + i < static_cast<int>(gridDim.x) ? values(first + i) : Wide{};
   const Kv4Split sp = a.splits[first];
   if (sp.last < 0) return;
   const int out_col = sp.col0 + col;
@@ -854,21 +884,21 @@ __global__ void __launch_bounds__(NT * 256) kv4_attn_join_kernel(const Kv4AttnAr
       for (; i < EARLY; ++i) {
         const float g = __shfl_sync(0xffffffffu, f, i);
 #pragma unroll
-        for (int e = 0; e < V; ++e) o[e] = fmaf(early[i][e], g, o[e]);
+        for (int e = 0; e < V; ++e) o[e] = fmaf(early[i].v[e], g, o[e]);
       }
     }
-#pragma unroll 8
+#pragma unroll 16
     for (; i < n; ++i) {
       const float g = __shfl_sync(0xffffffffu, f, i);
-      const float* q = piece(i0 + i) + col * D + lane;
+      const Wide x = values(i0 + i);
 #pragma unroll
-      for (int e = 0; e < V; ++e) o[e] = fmaf(q[e * 32], g, o[e]);
+      for (int e = 0; e < V; ++e) o[e] = fmaf(x.v[e], g, o[e]);
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  half_t* dst = kv4_out<D>(a, sp.b, sp.hk, out_col);
-#pragma unroll
-  for (int e = 0; e < V; ++e) dst[e * 32 + lane] = f_to_h(o[e] * inv);
+  uint32_t* dst = reinterpret_cast<uint32_t*>(kv4_out<D>(a, sp.b, sp.hk, out_col)) + lane * (V / 2);
+  if constexpr (V == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv));
+  else *dst = pack2(o[0] * inv, o[1] * inv);
 }
 
 }  // namespace thinfer

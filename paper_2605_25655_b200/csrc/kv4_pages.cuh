@@ -171,7 +171,7 @@ __device__ __forceinline__ PageMap map_pages(const PageTables& t, int* mem, int*
 // ---------------------------------------------------------------- reserve
 // Rows in ascending order take the lowest free pages for `add` more tokens each; a row whose pages, with those of the
 // rows before it, do not fit the pool or its table keeps its length and is counted in *refused.
-// Bounded by the latency of one CTA's dependent steps (1.8 us when no row opens a page, 3.6 us for the 12 rows of a prompt
+// Bounded by the latency of one CTA's dependent steps (1.8 us when no row opens a page, 3.6 us for the 8 rows of a prompt
 // batch).  The new pages are dealt over all threads: with a warp per row, 8 rows of 256 new pages took 26 us, now 7.
 __global__ void __launch_bounds__(kPlanThreads) kv4_reserve_kernel(const PageTables t, int32_t* table, const int32_t* add,
                                                                    int32_t* lens_out, int64_t* refused) {
