@@ -2,12 +2,11 @@
 // values each: with 8 values a lane the work that a row needs whatever its length took as long as the memory (52 against
 // 41 us to write, 32 against 28 us to read 6800 tokens of 32 heads).  The row's extremes come from shuffles of packed 16-bit
 // pairs, and the codes leave as 32-bit words (K) or as the halves that belong to the token (V).  A lane group looks its
-// token's page up once and walks rows of that token, several in flight at a time; how many groups share a token is set so
-// that the device is full once, and each group goes on to further tokens.
+// token's page up once, walks rows of that token, several in flight at a time, and goes on to further tokens.
 //
-// Measured at those tokens: writing 38 us (145 MB, 3.8 TB/s; about two thirds of the issue slots are busy, and more loads in
-// flight cost warps: 73 us against 69 for the whole call sequence with rows requested one ahead, 76 two ahead), reading 27
-// us (145 MB, 5.3 TB/s, waits for its loads).  At one token per request both are one chain of three loads: 2 us.
+// Measured at those tokens: writing 36 us (145 MB, 4.0 TB/s; the SMs are busy in 59 % of their issue slots, and more loads in
+// flight cost warps: 73 us against 69 for reserve, append and read with rows requested one ahead, 76 two ahead), reading 28
+// us (145 MB, 5.2 TB/s, waits for its loads).  At one token per request both are one chain of three loads: 2 us.
 #pragma once
 #include "kv4_layout.cuh"
 
@@ -66,6 +65,7 @@ struct Kv4Walk {
   }
 };
 
+constexpr int kKv4CtasPerSm = 3;        // of 256 threads
 constexpr int kKv4RowsInFlight = 2;     // of an append; a read's rows are a quarter as large
 
 __device__ __forceinline__ half2_t max2_nan(half2_t a, half2_t b) { return __hmax2_nan(a, b); }
@@ -181,7 +181,7 @@ __device__ __forceinline__ void kv4_append_rows(const Kv4TokensArgs& a, const Kv
 }
 
 template <int D>
-__global__ void __launch_bounds__(256, 3) kv4_append_kernel(const Kv4TokensArgs a) {
+__global__ void __launch_bounds__(256, kKv4CtasPerSm) kv4_append_kernel(const Kv4TokensArgs a) {
   constexpr int LPR = D / 16;
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, sub = lane % LPR;
@@ -251,7 +251,7 @@ __device__ __forceinline__ void kv4_read_rows(const Kv4TokensArgs& a, const Kv4S
 }
 
 template <int D>
-__global__ void __launch_bounds__(256, 3) kv4_read_kernel(const Kv4TokensArgs a) {
+__global__ void __launch_bounds__(256, kKv4CtasPerSm) kv4_read_kernel(const Kv4TokensArgs a) {
   constexpr int LPR = D / 16;
   pdl_launch_dependents();
   const int sub = (threadIdx.x & 31) % LPR;
