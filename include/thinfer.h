@@ -402,7 +402,8 @@ int thinfer_op_kv4_read(const void* pool, int32_t n_pages, const int32_t* table,
  * lens[b] - (queries - 1 - i) (one query: all of them).  A query that sees no key gives 0.  q FP16 [batch * queries]
  * tokens of n_q_heads * head_dim values, q_stride elements apart, already rotated; out FP16 [batch][queries][n_q_heads
  * * head_dim].  n_q_heads a multiple of n_kv_heads; batch <= 2048.  workspace: thinfer_kv4_attention_workspace bytes, 16-byte
- * aligned; its contents mean nothing between calls, but calls that may overlap on the device need their own. */
+ * aligned; its contents mean nothing between calls, but calls that may overlap on the device need their own.  out and
+ * workspace must not overlap q, table, lens or each other. */
 int thinfer_kv4_attention_workspace(int32_t batch, int32_t queries, int32_t n_q_heads, int32_t n_kv_heads,
                                     int32_t head_dim, size_t* bytes);
 int thinfer_op_kv4_attention(const void* q, int64_t q_stride, const void* pool, int32_t n_pages, const int32_t* table,

@@ -93,6 +93,15 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return x < y + nb && y < x + na;
 }
 
+// n rows of wa (wb) bytes, sa (sb) bytes apart; with different strides any overlap of the whole ranges counts.
+bool rows_overlap(const void* a, int64_t sa, int64_t wa, const void* b, int64_t sb, int64_t wb, int64_t n) {
+  if (!overlap(a, static_cast<size_t>((n - 1) * sa + wa), b, static_cast<size_t>((n - 1) * sb + wb))) return false;
+  if (sa != sb || n == 1) return true;
+  const int64_t apart = static_cast<int64_t>(reinterpret_cast<uintptr_t>(a)) - static_cast<int64_t>(reinterpret_cast<uintptr_t>(b));
+  const int64_t at = (apart % sa + sa) % sa;   // where a's row begins behind the beginning of one of b's
+  return at < wb || at + wa > sa;
+}
+
 // Opts a kernel in to more than 48 KB of dynamic shared memory: a property of the kernel on a device, asked for once for
 // each new maximum.
 template <auto Kernel>
@@ -198,6 +207,14 @@ int thinfer_op_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int6
   if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(q_gain) || !aligned16(k_gain) ||
       !aligned4(positions) || (reinterpret_cast<uintptr_t>(turns) & 7u) != 0)
     return op_fail(THINFER_EINVAL, "qk_norm_rope: a pointer is not aligned");
+  auto meet = [&](const void* x, int64_t sx, int64_t wx, const void* y, int64_t sy, int64_t wy) {
+    return rows_overlap(x, sx * 2, wx * 2, y, sy * 2, wy * 2, tokens);
+  };
+  if (((q_out != q || q_out_stride != q_stride) && meet(q_out, q_out_stride, q_row, q, q_stride, q_row)) ||
+      ((k_out != k || k_out_stride != k_stride) && meet(k_out, k_out_stride, k_row, k, k_stride, k_row)) ||
+      meet(q_out, q_out_stride, q_row, k, k_stride, k_row) || meet(k_out, k_out_stride, k_row, q, q_stride, q_row) ||
+      meet(q_out, q_out_stride, q_row, k_out, k_out_stride, k_row))
+    return op_fail(THINFER_EINVAL, "qk_norm_rope: an output overlaps an input that it does not replace, or the other output");
   QkNormRopeArgs a{};
   a.q = static_cast<const half_t*>(q);
   a.k = static_cast<const half_t*>(k);
@@ -311,6 +328,13 @@ int thinfer_op_kv4_attention(const void* q, int64_t q_stride, const void* pool, 
     return op_fail(THINFER_EINVAL, "kv4_attention: a pointer or the token stride is not aligned, or the stride is below heads * head_dim");
   if (workspace_bytes < p.split_bytes + p.part_bytes)
     return op_fail(THINFER_ECAPACITY, "kv4_attention: the workspace has %zu bytes of %zu", workspace_bytes, p.split_bytes + p.part_bytes);
+  const size_t out_bytes = static_cast<size_t>(batch) * queries * n_q_heads * head_dim * 2, ws_bytes = p.split_bytes + p.part_bytes;
+  const size_t q_bytes = ((static_cast<size_t>(batch) * queries - 1) * q_stride + static_cast<size_t>(n_q_heads) * head_dim) * 2;
+  const size_t tab_bytes = static_cast<size_t>(batch) * max_pages * 4, len_bytes = static_cast<size_t>(batch) * 4;
+  if (overlap(out, out_bytes, workspace, ws_bytes) || overlap(out, out_bytes, q, q_bytes) || overlap(out, out_bytes, table, tab_bytes) ||
+      overlap(out, out_bytes, lens, len_bytes) || overlap(workspace, ws_bytes, q, q_bytes) || overlap(workspace, ws_bytes, table, tab_bytes) ||
+      overlap(workspace, ws_bytes, lens, len_bytes))
+    return op_fail(THINFER_EINVAL, "kv4_attention: the output or the workspace overlaps an input, or they overlap each other");
   Kv4AttnArgs a{};
   a.c = make_cache(pool, table, batch, max_pages, n_pages, n_kv_heads, head_dim, page_size);
   a.lens = lens;

@@ -145,6 +145,13 @@ def test_qk_norm_rope_refuses(lib):
         *(({n: 0}, E) for n in ("tokens", "hq", "hkv", "d")), ({"d": 96}, U), ({"rot": 136}, U), ({"rot": 24}, U), ({"rot": -16}, E),
         ({"halves": 2}, E), ({"eps": -1.0}, E), ({"eps": float("nan")}, E), ({"qs": 504}, E), ({"ks": 260}, E), ({"kos": 128}, E), ({"q": P + 8}, E),
         ({"ko": P + 2}, E), ({"turns": P + 4}, E), ({"pos": P + 2}, E)])
+    # outputs over inputs that they do not replace, row by row: slices of one projection output do not overlap
+    F, N = 1 << 24, 1 << 26
+    args.update(q=F, qs=1024, k=F + 1024, ks=1024, qo=N, qos=512, ko=2 * N, kos=256, tokens=3)
+    _refusals(lib.thinfer_op_qk_norm_rope, args, [
+        ({"qo": F, "qos": 512}, E), ({"qo": F + 16, "qos": 1024}, E), ({"qo": F + 1024, "qos": 1024}, E), ({"ko": F, "kos": 1024}, E),
+        ({"ko": F + 1040, "kos": 1024}, E), ({"ko": N + 512, "kos": 256}, E), ({"qo": F, "qos": 1024, "ko": F, "kos": 1024}, E),
+        ({"qo": F + 1536, "qos": 1024}, E)])
 
 
 def test_append_and_read_refuse(lib):
@@ -172,6 +179,12 @@ def test_attention_refuses(lib):
         *(({n: None}, E) for n in ("q", "pool", "table", "lens", "out", "ws")), *(({n: 0}, E) for n in ("batch", "queries", "hq", "hkv", "n_pages", "maxp")),
         ({"hq": 7}, U), ({"d": 80}, U), ({"page": 24}, U), ({"qs": 1016}, E), ({"qs": 1028}, E), ({"q": P + 4}, E), ({"out": P + 8}, E), ({"ws": P + 8}, E),
         ({"wb": need.value - 1}, thinfer.ECAPACITY), ({"maxp": 1 << 26}, U), ({"batch": 2049}, U), ({"queries": 70000}, U)])
+    # an output or a workspace that overlaps an input, or each other
+    q, table, lens, out, ws = ((1 << 24) * i for i in range(1, 6))
+    args.update(q=q, table=table, lens=lens, out=out, ws=ws)
+    _refusals(lib.thinfer_op_kv4_attention, args, [
+        ({"out": q}, E), ({"out": q + 2048}, E), ({"out": q - 4080}, E), ({"out": table}, E), ({"lens": out + 16}, E), ({"ws": out}, E), ({"ws": q}, E),
+        ({"ws": table}, E), ({"ws": lens}, E)])
 
 
 def test_page_table_calls_refuse(lib):
