@@ -186,6 +186,41 @@ def test_largest_values_and_tiny_ranges(T):
     assert np.array_equal(pool.cpu().numpy(), ref.data)
 
 
+@pytest.mark.parametrize("t,tokens,hkv,d,page", [("f16", 900, 40, 128, 64), ("bf16", 4100, 8, 128, 16), ("bf16", 9001, 1, 128, 128),
+                                                 ("f16", 2500, 24, 64, 32), ("bf16", 7000, 6, 64, 16), ("f16", 333, 33, 128, 16)])
+def test_many_tokens_in_one_call_and_in_small_ones(T, t, tokens, hkv, d, page):
+    """How the rows of a call are shared out depends on its size; the bytes and values do not."""
+    torch, thinfer = T
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    width, rows_n = -(-tokens // 5 // page) + 2, 5
+    n_pages = rows_n * width
+    tab = torch.randperm(n_pages, generator=g, device="cuda").to(torch.int32).view(rows_n, width)
+    rows = (torch.arange(tokens, device="cuda") % rows_n).to(torch.int32)
+    pos = (torch.arange(tokens, device="cuda") // rows_n + 3).to(torch.int32)
+    rows[::17], pos[5::23] = -1, -4                                       # padding
+    k, v = (torch.randn(tokens, hkv, d, generator=g, device="cuda").to(_tt(torch, t)) for _ in range(2))
+    one, many = _fresh_pool(torch, n_pages, hkv, d, page), _fresh_pool(torch, n_pages, hkv, d, page)
+    thinfer.op_kv4_append(one, tab, k, v, rows, pos, page)
+    for i in range(0, tokens, 61):
+        s = slice(i, i + 61)
+        thinfer.op_kv4_append(many, tab, k[s], v[s], rows[s], pos[s], page)
+    assert torch.equal(one, many)
+    out = [torch.full_like(k, 7.0) for _ in range(4)]
+    thinfer.op_kv4_read(one, tab, rows, pos, page, d, k.dtype, k_out=out[0], v_out=out[1])
+    for i in range(0, tokens, 61):
+        s = slice(i, i + 61)
+        thinfer.op_kv4_read(one, tab, rows[s], pos[s], page, d, k.dtype, k_out=out[2][s], v_out=out[3][s])
+    assert torch.equal(out[0], out[2]) and torch.equal(out[1], out[3])
+    skip = (rows < 0) | (pos < 0)
+    assert torch.all(out[0][skip] == 7.0)
+    # half a step is span / 30; the rounding of the scale moves the step by EPS of itself, 15 of them by EPS of the span; the
+    # value read is rounded once
+    for x, y in ((k, out[0]), (v, out[1])):
+        x, y = x[~skip].double(), y[~skip].double()
+        span = x.amax(-1, keepdim=True) - x.amin(-1, keepdim=True)
+        assert torch.all((x - y).abs() <= span * (1 / 30 + 2 * EPS[t]) + y.abs() * EPS[t])
+
+
 def test_a_block_far_into_a_large_pool(T):
     """Byte offsets beyond 2^32."""
     torch, thinfer = T
