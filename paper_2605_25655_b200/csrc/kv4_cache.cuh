@@ -230,8 +230,9 @@ __device__ __forceinline__ void kv4_read_rows(const Kv4TokensArgs& a, const Kv4S
       const int h = h0 + u * step;
       if (h >= n) break;
       const float2 p = kv4_unpack_params(par[u]);
-      // two codes at a time as the low mantissa bits of FP16 numbers: code * 2^-24, or 2^-20 from the high nibbles
-      const float s0 = p.x * 0x1p24f, s1 = p.x * 0x1p20f;
+      // two codes at a time as the low mantissa bits of FP16 numbers: code * 2^-24, or 2^-20 from the high nibbles.  The power
+      // of two goes to the code, where it is exact: 2^24 times the scale of a BF16 row may be beyond FP32
+      const uint64_t scale = f32x2(p.x, p.x), offset = f32x2(p.y, p.y);
       half_t* out = dst + h * head_stride;
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
@@ -241,8 +242,10 @@ __device__ __forceinline__ void kv4_read_rows(const Kv4TokensArgs& a, const Kv4S
         for (int j = 0; j < 4; ++j) {
           const uint32_t b = (j & 2 ? w >> 8 : w) & (j & 1 ? 0x00f000f0u : 0x000f000fu);
           const float2 c = __half22float2(*reinterpret_cast<const __half2*>(&b));
-          x[j] = fmaf(j & 1 ? s1 : s0, c.x, p.y);
-          x[j + 4] = fmaf(j & 1 ? s1 : s0, c.y, p.y);
+          const uint64_t up = j & 1 ? f32x2(0x1p20f, 0x1p20f) : f32x2(0x1p24f, 0x1p24f);
+          const float2 y = f32x2_unpack(fma_f32x2(scale, mul_f32x2(f32x2(c.x, c.y), up), offset));
+          x[j] = y.x;
+          x[j + 4] = y.y;
         }
         *reinterpret_cast<uint4*>(out + g * (D / 2)) = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
       }
