@@ -58,6 +58,9 @@ __host__ __device__ constexpr int kv4_warps() {
   return NT == 1 ? 12 : 8;
 }
 constexpr float kKv4Low = -1e30f;    // running maximum before the first key
+// Scores are put together without a factor of 2^12 in the BF16 build and multiplied by it last: with the 2^24 of the codes in
+// one factor, a query of 2^116 and more made that factor infinite however small the keys were.  FP16 has no such numbers.
+constexpr float kKv4Last = kStorageType == 1 ? 0x1p12f : 1.f;
 
 // What a CTA leaves for the second kernel about the pair that begins in it and ends in a later one.
 struct Kv4Split {
@@ -273,7 +276,7 @@ template <int D, int NT>
 struct Kv4Acc {
   float o[NT][D / 16][4];
   float m[NT][2], l[NT][2], z[NT][2], ref[NT][2];  // maximum, sum of p, sum of p times row middle, reference of w
-  float qf[NT][2], qs[NT][2];                      // scale of the code product, scaled sum of the query
+  float qf[NT][2], qs[NT][2];                      // scale of the code product, scaled sum of the query; over kKv4Last
   int lim[NT][2];                                  // keys a column sees
   uint32_t q[NT][D / 16][2];                       // B operand
 
@@ -331,17 +334,15 @@ __device__ __forceinline__ void kv4_load_queries(const Kv4AttnArgs& a, Kv4Acc<D,
     }
     float top = 0.f, sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8 * W; ++e) {
-      top = fmaxf(top, fabsf(x[e]));
-      sum += x[e];
-    }
+    for (int e = 0; e < 8 * W; ++e) top = fmaxf(top, fabsf(x[e]));
 #pragma unroll
-    for (int off = 1; off < 4; off <<= 1) {
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-      sum += __shfl_xor_sync(0xffffffffu, sum, off);
-    }
+    for (int off = 1; off < 4; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
     const int ex = min(max(__float_as_int(top) >> 23, 13), 253);
     const float up = __int_as_float((266 - ex) << 23), down = __int_as_float((ex - 12) << 23);
+#pragma unroll
+    for (int e = 0; e < 8 * W; ++e) sum = fmaf(x[e], up, sum);      // of the scaled values: the sum of large ones may pass FP32
+#pragma unroll
+    for (int off = 1; off < 4; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       const float* y = x + 8 * w;
@@ -350,7 +351,7 @@ __device__ __forceinline__ void kv4_load_queries(const Kv4AttnArgs& a, Kv4Acc<D,
       s.q[n][2 * w + 1][0] = pack_f16(y[2] * up, y[6] * up);
       s.q[n][2 * w + 1][1] = pack_f16(y[3] * up * 0.0625f, y[7] * up * 0.0625f);
     }
-    const float qf = 16777216.f * down * a.scale_log2, qs = sum * a.scale_log2;
+    const float qf = (16777216.f / kKv4Last) * down * a.scale_log2, qs = sum * 0x1p-24f * qf;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       s.qf[n][j] = __shfl_sync(0xffffffffu, qf, 8 * c + 4 * j);
@@ -418,7 +419,8 @@ __device__ __forceinline__ void kv4_stage(Kv4Acc<D, NT>& s, const uint8_t* stage
     }
     auto seen = [&](int e, int n, int j) { return !MASKED || t0 + 16 * b + tr + 2 * e < s.lim[n][j]; };
     auto raw = [&](int e, int n, int j, float minus) {   // score - minus, log2 units
-      float x = fmaf(kp[e].x, sc[n][2 * e + j] * s.qf[n][j], fmaf(kp[e].y, s.qs[n][j], -minus));
+      float x = kStorageType == 1 ? fmaf(fmaf(kp[e].x * s.qf[n][j], sc[n][2 * e + j], kp[e].y * s.qs[n][j]), kKv4Last, -minus)
+                                  : fmaf(kp[e].x, sc[n][2 * e + j] * s.qf[n][j], fmaf(kp[e].y, s.qs[n][j], -minus));
       if (MASKED) {
         if ((bad >> b) & 1u) x = __int_as_float(0x7fffffff);
         if (!seen(e, n, j)) x = -INFINITY;
@@ -440,7 +442,9 @@ __device__ __forceinline__ void kv4_stage(Kv4Acc<D, NT>& s, const uint8_t* stage
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const uint64_t kx = f32x2(kp[e].x, kp[e].x), ky = f32x2(kp[e].y, kp[e].y), vx = f32x2(vp[e].x, vp[e].x);
-            const float2 x = f32x2_unpack(fma_f32x2(kx, mul_f32x2(f32x2(sc[n][2 * e], sc[n][2 * e + 1]), qf), fma_f32x2(ky, qs, less)));
+            const uint64_t codes = f32x2(sc[n][2 * e], sc[n][2 * e + 1]);
+            const float2 x = f32x2_unpack(kStorageType == 1 ? fma_f32x2(fma_f32x2(mul_f32x2(kx, qf), codes, mul_f32x2(ky, qs)), f32x2(kKv4Last, kKv4Last), less)
+                                                            : fma_f32x2(kx, mul_f32x2(codes, qf), fma_f32x2(ky, qs, less)));
             const float x0 = ex2_approx(x.x), x1 = ex2_approx(x.y);
             const float2 y = f32x2_unpack(mul_f32x2(mul_f32x2(f32x2(x0, x1), ref), vx));
             p[n][2 * e] = x0;

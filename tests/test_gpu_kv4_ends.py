@@ -66,3 +66,32 @@ def test_read_of_rows_with_large_scales(T, d, page):
         assert np.all(np.isfinite(want))
         # one FP32 rounding (2^-24) before the stored one
         assert np.all(np.abs(_host(got[which]) - want) <= EPS["bf16"] * np.abs(want) * 1.001)
+
+
+# ------------------------------------------------------------------ attention
+def _attend(T, rng, q, k, v, queries=1, page=16, with_mag=True):
+    """BF16 attention of one request whose last tokens are q [queries][hq][d], against the float64 definition over the
+    stored bytes; the tolerance of test_gpu_kv4.test_attention (without the part for scores where they decide by far)."""
+    torch, thinfer = T
+    n, hkv, d = k.shape
+    q, k, v = (kv4.round_to(x, "bf16") for x in (q, k, v))
+    pool, table, _, _, ref = _one_row(torch, thinfer, k, v, "bf16", page)
+    got = _host(thinfer.op_kv4_attention(_dev(torch, q[None], "bf16"), pool, _int(torch, table), _int(torch, [n]), page))[0]
+    kv = kv4.keys_values(ref, table[0], n)
+    assert np.all(np.isfinite(kv))
+    for i in range(queries):
+        want, spread, mag = kv4.attention(q[i], kv, n, queries - 1 - i)
+        far = spread + np.abs(want) + kv4.attention(q[i], (kv[0], np.abs(kv[1])), n, queries - 1 - i)[0]
+        tol = EPS["bf16"] * np.abs(want) + 2.0 ** -10 * spread + (2.0 ** -19 * (1 + 16 * mag) * far if with_mag else 0)
+        assert np.all(np.isfinite(got[i])) and np.all(np.abs(got[i] - want) <= tol), (i, np.max(np.abs(got[i] - want) / tol))
+
+
+@pytest.mark.parametrize("n,hq,hkv,d,queries", [(1, 2, 1, 64, 1), (50, 4, 2, 64, 1), (70, 4, 1, 128, 5), (700, 2, 1, 128, 1)])
+def test_attention_of_queries_near_the_largest_value(T, n, hq, hkv, d, queries):
+    """Queries on either side of 2^116 (8.3e34) and up to 1.5e38 over small keys: scores of ordinary size."""
+    rng = np.random.default_rng(n)
+    for q_size, k_size in ((5e34, 1e-34), (1e35, 1e-34), (1e37, 1e-36), (4e37, 1e-37), (1e-33, 1e33), (1e-37, 1e37)):
+        q = np.clip(rng.standard_normal((queries, hq, d)), -3.5, 3.5) * q_size
+        _attend(T, rng, q, rng.standard_normal((n, hkv, d)) * k_size / 4, rng.standard_normal((n, hkv, d)), queries)
+    same = 1.5e38 * (1 - 0.2 * rng.random((queries, hq, d)))      # of one sign: their sum is beyond FP32
+    _attend(T, rng, same, (rng.standard_normal((n, hkv, d)) + 3) * 1e-38 / 4, rng.standard_normal((n, hkv, d)), queries)
