@@ -57,7 +57,7 @@ template <int NT>
 __host__ __device__ constexpr int kv4_warps() {
   return NT == 1 ? 12 : 8;
 }
-constexpr float kKv4Low = -1e30f;    // running maximum before the first key
+constexpr float kKv4Low = -3.402823466e38f;   // running maximum before the first key: no finite score lies below it
 // Scores are put together without a factor of 2^12 in the BF16 build and multiplied by it last: with the 2^24 of the codes in
 // one factor, a query of 2^116 and more made that factor infinite however small the keys were.  FP16 has no such numbers.
 constexpr float kKv4Last = kStorageType == 1 ? 0x1p12f : 1.f;

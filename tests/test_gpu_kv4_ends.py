@@ -95,3 +95,15 @@ def test_attention_of_queries_near_the_largest_value(T, n, hq, hkv, d, queries):
         _attend(T, rng, q, rng.standard_normal((n, hkv, d)) * k_size / 4, rng.standard_normal((n, hkv, d)), queries)
     same = 1.5e38 * (1 - 0.2 * rng.random((queries, hq, d)))      # of one sign: their sum is beyond FP32
     _attend(T, rng, same, (rng.standard_normal((n, hkv, d)) + 3) * 1e-38 / 4, rng.standard_normal((n, hkv, d)), queries)
+
+
+@pytest.mark.parametrize("n,hq,hkv,d,queries", [(1, 2, 1, 64, 1), (3, 4, 2, 64, 1), (40, 4, 1, 128, 4), (700, 2, 1, 128, 1)])
+def test_attention_where_every_score_is_far_below_zero(T, n, hq, hkv, d, queries):
+    """Scores of -1e32 to -2e38.  Keys grow smaller towards the last one, in steps of 5 % of its size, far more than the values
+    of a key differ: the last key that a query sees takes all the weight."""
+    rng = np.random.default_rng(n + d)
+    for q_size, k_size in ((1e16, 1e16), (1e18, 1e18), (-1e20, -1e16), (5e18, 1e19)):
+        q = q_size * (1 + 0.1 * rng.random((queries, hq, d)))
+        far = np.minimum(np.arange(n)[::-1], 20)[:, None, None]
+        k = -k_size / 8 * (1 + 0.05 * far) * (1 + 0.005 * rng.random((n, hkv, d)))
+        _attend(T, rng, q, k, rng.standard_normal((n, hkv, d)), queries, with_mag=False)
