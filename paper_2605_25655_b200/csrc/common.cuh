@@ -127,6 +127,17 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
+// Sums towards zero and upwards: of numbers that are not negative, they differ where a sum is not exact.
+__device__ __forceinline__ uint64_t add_rz_f32x2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rz.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t add_rp_f32x2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rp.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 
 // ------------------------------------------------------------------ timing
 __device__ __forceinline__ uint64_t global_ns() {

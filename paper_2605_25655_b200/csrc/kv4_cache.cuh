@@ -4,7 +4,7 @@
 // pairs, and the codes leave as 32-bit words (K) or as the halves that belong to the token (V).  A lane group looks its
 // token's page up once, walks rows of that token, several in flight at a time, and goes on to further tokens.
 //
-// Measured at those tokens: writing 36 us (145 MB, 4.0 TB/s; the SMs are busy in 59 % of their issue slots, and more loads in
+// Measured at those tokens: writing 39 us (145 MB, 3.7 TB/s; the SMs are busy in some 60 % of their issue slots, and more loads in
 // flight cost warps: 73 us against 69 for reserve, append and read with rows requested one ahead, 76 two ahead), reading 28
 // us (145 MB, 5.2 TB/s, waits for its loads).  At one token per request both are one chain of three loads: 2 us.
 #pragma once
@@ -78,20 +78,31 @@ __device__ __forceinline__ float by_15(float x) {
   return fmaf(fmaf(-15.f, q, x), 1.f / 15.f, q);
 }
 
+// x + less, not negative, two at a time: exact, or the neighbour of the exact sum with an odd last bit.
+__device__ __forceinline__ uint64_t kv4_less(uint64_t x, uint64_t less) {
+  return add_rz_f32x2(x, less) | (add_rp_f32x2(x, less) & 0x0000000100000001ull);
+}
+
 // Codes of eight values of a row with the given offset and scale, four bits each.  The quotient (x - offset) / scale is a
 // product with a reciprocal and one correction by the residual, so that a quotient half way between two codes (common:
-// 16-bit values lie on a grid) comes out as exactly that and the addition of 1.5 * 2^23 rounds it to the even code.  Two
-// values at a time in packed FP32 (38 instead of 40 us).  A scale too small for a reciprocal is left to a division.
+// 16-bit values lie on a grid) comes out as exactly that and the addition of 1.5 * 2^23 rounds it to the even code.  A
+// quotient beside such a point must not land on it: where x - offset takes more than 24 bits (a value far smaller than the
+// offset, or the other way round), the difference is rounded to the neighbour with an odd last bit.  A half step is a
+// multiple of scale / 2 with at most 16 bits, so neither an odd difference of 24 bits nor its quotient, rounded once more,
+// is one, and both lie on the side of it on which the exact difference lies: the codes are the exact quotient's.  (That is
+// three instructions more for two values, 39 instead of 36 us; done only in rows that have such values, which takes their
+// smallest size, 41.)  Two values at a time in packed FP32 (38 instead of 40 us).  A scale too small for a reciprocal is left to a division.
 __device__ __forceinline__ uint32_t kv4_codes(const float (&x)[8], float lo, float scale) {
   uint32_t word = 0;
+  const uint64_t less = f32x2(-lo, -lo);
   // a normal scale is within 2^-8 of (max - min) / 15, so that no code can pass 15
   const float smallest = kStorageType == 1 ? 0x1p-100f : 0x1p-14f;
   if (scale >= smallest && scale < 0x1p100f) {
     constexpr float M = 12582912.f;
     const float r = __fdividef(1.f, scale);
-    const uint64_t inv = f32x2(r, r), less = f32x2(-lo, -lo), neg = f32x2(-scale, -scale), magic = f32x2(M, M), back = f32x2(-M, -M);
+    const uint64_t inv = f32x2(r, r), neg = f32x2(-scale, -scale), magic = f32x2(M, M), back = f32x2(-M, -M);
     auto whole = [&](float a, float b) {   // M + code of two values
-      const uint64_t d = add_f32x2(f32x2(a, b), less), q = mul_f32x2(d, inv);
+      const uint64_t d = kv4_less(f32x2(a, b), less), q = mul_f32x2(d, inv);
       return add_f32x2(fma_f32x2(fma_f32x2(q, neg, d), inv, q), magic);
     };
     // pairs of values 4 apart, so that the codes of two neighbours meet in the low byte of M + code + 16 * next code
@@ -107,7 +118,8 @@ __device__ __forceinline__ uint32_t kv4_codes(const float (&x)[8], float lo, flo
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float q = scale > 0.f ? fminf(rintf(__fdiv_rn(x[j] - lo, scale)), 15.f) : 0.f;
+    const float d = __int_as_float(__float_as_int(__fadd_rz(x[j], -lo)) | (__float_as_int(__fadd_ru(x[j], -lo)) & 1));
+    const float q = scale > 0.f ? fminf(rintf(__fdiv_rn(d, scale)), 15.f) : 0.f;
     word |= static_cast<uint32_t>(q) << (4 * j);
   }
   return word;

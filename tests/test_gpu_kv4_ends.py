@@ -107,3 +107,55 @@ def test_attention_where_every_score_is_far_below_zero(T, n, hq, hkv, d, queries
         far = np.minimum(np.arange(n)[::-1], 20)[:, None, None]
         k = -k_size / 8 * (1 + 0.05 * far) * (1 + 0.005 * rng.random((n, hkv, d)))
         _attend(T, rng, q, k, rng.standard_normal((n, hkv, d)), queries, with_mag=False)
+
+
+# ------------------------------------------------------------------ append
+def _written_bytes_are_the_definitions(T, x, t, page=16):
+    """Appends x [tokens][d] as K and, in reverse order, as V of one head; every byte against the float64 definition."""
+    torch, thinfer = T
+    n, d = x.shape
+    pages = -(-n // page)
+    pool = torch.zeros(pages, page * (d + 8), dtype=torch.uint8, device="cuda")
+    ref = kv4.Pool(pool.cpu().numpy(), 1, d, page, DT[t])
+    k, v = x[:, None], x[::-1][:, None]
+    tab, rows, pos = _int(torch, [list(range(pages))]), _int(torch, [0] * n), _int(torch, list(range(n)))
+    thinfer.op_kv4_append(pool, tab, _dev(torch, k, t), _dev(torch, v, t), rows, pos, page)
+    for i in range(n):
+        ref.write(i // page, i % page, 0, 0, k[i, 0])
+        ref.write(i // page, i % page, 0, 1, v[i, 0])
+    got = pool.cpu().numpy()
+    bad = np.argwhere(got != ref.data)
+    assert len(bad) == 0, (len(bad), bad[:3], got[got != ref.data][:3], ref.data[got != ref.data][:3])
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_codes_of_rows_of_wide_spread(T, t, d):
+    """Rows whose values differ by many powers of two: x - offset takes more bits than FP32 has."""
+    rng = np.random.default_rng(d)
+    rows = []
+    for sigma in (1.0, 3.0, 6.0):
+        x = rng.choice([-1.0, 1.0], (1200, d)) * np.exp(sigma * rng.standard_normal((1200, d)))
+        x /= np.maximum(1, np.abs(x).max(-1, keepdims=True) / 30000.0)        # inside FP16
+        rows.append(x)
+    _written_bytes_are_the_definitions(T, kv4.round_to(np.concatenate(rows), DT[t]), t)
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+def test_codes_beside_the_middle_of_two(T, t):
+    """Rows from -7.5 m to 7.5 m and from 0 to 15 m, of scale m, with values that are 0 or tiny or a half step with both signs of
+    tiny beside it: as far from the half step as the type can say."""
+    rows = []
+    tiny = [0.0] + [s * 2.0 ** -e for e in range(2, 25) for s in (1, -1)]
+    for m in (1.0, 0.125, 64.0, 2.0 ** -8):
+        x = np.resize(np.array(tiny), 64) * m
+        x[0], x[1] = -7.5 * m, 7.5 * m
+        rows.append(x)
+        x = np.resize(np.concatenate([np.arange(0.5, 15), np.abs(tiny)]), 64) * m
+        x[0], x[1] = 15 * m, 0.0
+        rows.append(x)
+        rows.append(np.where(np.arange(64) % 9 == 0, 0.0, rows[-1]) - 2.0 ** -20)   # the offset is the tiny one
+        x = np.resize((np.arange(0.5, 15)[:, None] * (1 + np.array([0, 1, -1, 2, -2]) * 2.0 ** -9)).ravel(), 64) * m
+        x[0], x[1] = 15 * m, 0.0
+        rows.append(x)
+    _written_bytes_are_the_definitions(T, kv4.round_to(np.array(rows), DT[t]), t)
