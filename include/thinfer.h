@@ -364,8 +364,8 @@ int thinfer_op_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int6
  *   V codes  [page_size/2][head_dim/4][2][2] token pair, group of four dimensions, token of the pair, bytes as for K
  *   K params [page_size][2], V params [page_size][2]: FP16 scale, offset of the token's row
  * A row x (one token, one head, K or V) is stored with offset = min x, scale = (max x - min x) / 15 rounded to FP16,
- * code = (x - offset) / scale rounded to nearest, ties to even, and is read as offset + scale * code.  A row with a NaN
- * or an infinity (or whose range overflows the storage type) is read as NaN.
+ * code = (x - offset) / scale rounded to nearest, ties to even, and is read as offset + scale * code (rounded to FP16:
+ * beyond the type's largest value that is infinity).  A row with a NaN or an infinity is read as NaN.
  * table: int32 [n_rows][max_pages]; position p of row r lies on page table[r][p / page_size], slot p % page_size.  The
  * same table serves all layers.  lens: int32 [n_rows], tokens of each row (negative: none).  A page is in use when a row names it
  * among its first ceil(len / page_size) entries; several rows may name one page (fork).  Nothing else records who

@@ -91,7 +91,8 @@ __device__ __forceinline__ uint64_t kv4_less(uint64_t x, uint64_t less) {
 // multiple of scale / 2 with at most 16 bits, so neither an odd difference of 24 bits nor its quotient, rounded once more,
 // is one, and both lie on the side of it on which the exact difference lies: the codes are the exact quotient's.  (That is
 // three instructions more for two values, 39 instead of 36 us; done only in rows that have such values, which takes their
-// smallest size, 41.)  Two values at a time in packed FP32 (38 instead of 40 us).  A scale too small for a reciprocal is left to a division.
+// smallest size, 41.)  Two values at a time in packed FP32 (38 instead of 40 us).  A scale too small or too large for a
+// reciprocal is left to a division, of halves (exact for 16-bit values), whose difference is inside FP32.
 __device__ __forceinline__ uint32_t kv4_codes(const float (&x)[8], float lo, float scale) {
   uint32_t word = 0;
   const uint64_t less = f32x2(-lo, -lo);
@@ -118,8 +119,8 @@ __device__ __forceinline__ uint32_t kv4_codes(const float (&x)[8], float lo, flo
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float d = __int_as_float(__float_as_int(__fadd_rz(x[j], -lo)) | (__float_as_int(__fadd_ru(x[j], -lo)) & 1));
-    const float q = scale > 0.f ? fminf(rintf(__fdiv_rn(d, scale)), 15.f) : 0.f;
+    const float d = __int_as_float(__float_as_int(__fmaf_rz(0.5f, x[j], -0.5f * lo)) | (__float_as_int(__fmaf_ru(0.5f, x[j], -0.5f * lo)) & 1));
+    const float q = scale > 0.f ? fminf(rintf(__fdiv_rn(d, 0.5f * scale)), 15.f) : 0.f;
     word |= static_cast<uint32_t>(q) << (4 * j);
   }
   return word;
@@ -167,8 +168,10 @@ __device__ __forceinline__ void kv4_append_rows(const Kv4TokensArgs& a, const Kv
         ends = max2_nan(ends, *reinterpret_cast<const half2_t*>(&other));
       }
       const float2 hl = h2_to_f2(ends);
-      const float hi = hl.x, lo = -hl.y, probe = (hi - lo) * 0.f;   // probe: NaN as soon as one value is NaN or infinite
-      const float scale = h_to_f(f_to_h(by_15(hi - lo)));
+      // of halves in the BF16 build, whose rows may span more than FP32's largest value, though not more than twice that
+      constexpr float H = kStorageType == 1 ? 0.5f : 1.f;
+      const float lo = -hl.y, span = H * hl.x - H * lo, probe = span * 0.f;   // probe: NaN as soon as one value is NaN or infinite
+      const float scale = h_to_f(f_to_h(by_15(span) * (1.f / H)));
       uint32_t word[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {

@@ -11,7 +11,8 @@
 //
 // Quantisation of a row x of D values: offset = min x (exact in 16 bits), scale = (max x - min x) / 15 rounded to the
 // storage type, code = (x - offset) / scale rounded to nearest, ties to even, at most 15; scale 0 gives code 0.  A row
-// that holds a NaN or an infinity gets NaN params, so that everything that reads it sees NaN.  The rounding of the
+// that holds a NaN or an infinity gets NaN params, so that everything that reads it sees NaN; a finite row is stored as it
+// is, over the whole range of the type (at whose end a value read back may round to infinity).  The rounding of the
 // scale to 16 bits costs at most half a unit of its last place times 15 at the top of the row: 15 * 2^-12 of a step in
 // FP16 and 15 * 2^-9 in BF16, small against the half step of the code itself.
 #pragma once

@@ -159,3 +159,31 @@ def test_codes_beside_the_middle_of_two(T, t):
         x[0], x[1] = 15 * m, 0.0
         rows.append(x)
     _written_bytes_are_the_definitions(T, kv4.round_to(np.array(rows), DT[t]), t)
+
+
+def test_rows_that_span_more_than_the_largest_value(T):
+    """BF16 rows from -3.3e38 to 3.3e38: max - min is beyond FP32, scale and codes are not."""
+    torch, thinfer = T
+    rng = np.random.default_rng(8)
+    x = rng.uniform(-1, 1, (40, 64)) * np.array([1.6e38, 1.75e38, 2.5e38, 3.35e38])[np.arange(40) % 4][:, None]
+    x[::3] *= 10.0 ** rng.integers(-50, 1, (14, 64))
+    x[:, 0], x[:, 1] = -np.abs(x).max(-1) * 0.99, np.abs(x).max(-1)
+    x = kv4.round_to(x, "bf16")
+    assert np.all(np.isfinite(x)) and np.sum(x[:, 1] - x[:, 0] > 3.5e38) == 15
+    _written_bytes_are_the_definitions(T, x, "bf16")
+    pool, table, rows, pos, ref = _one_row(torch, thinfer, x[:, None], x[:, None], "bf16", 16)
+    want = kv4.round_to(np.stack([ref.read(table[0][i // 16], i % 16, 0, 0) for i in range(40)]), "bf16")
+    for got in thinfer.op_kv4_read(pool, _int(torch, table), rows, pos, 16, 64, torch.bfloat16):
+        got = _host(got)[:, 0]
+        near = np.isfinite(want)
+        assert near.mean() > 0.9 and np.array_equal(got[~near], want[~near])
+        assert np.all(np.abs(got - want)[near] <= 2 * EPS["bf16"] * np.abs(want)[near] * 1.001)     # FP32's rounding beside a tie
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+def test_codes_of_rows_of_tiny_values(T, t):
+    """Rows whose scale is subnormal, or so small that it rounds to 0."""
+    rng = np.random.default_rng(9)
+    sizes = 2.0 ** -np.arange(8, 25) if t == "f16" else 2.0 ** -np.arange(96, 134)
+    x = rng.standard_normal((4 * len(sizes), 64)) * np.repeat(sizes, 4)[:, None]
+    _written_bytes_are_the_definitions(T, kv4.round_to(x, DT[t]), t)
