@@ -102,13 +102,12 @@ bool rows_overlap(const void* a, int64_t sa, int64_t wa, const void* b, int64_t 
   return at < wb || at + wa > sa;
 }
 
-// Opts a kernel in to more than 48 KB of dynamic shared memory: a property of the kernel on a device, asked for once for
-// each new maximum.
+// Opts a kernel in to its dynamic shared memory: a property of the kernel on a device, asked for once for each new maximum.
+// What a kernel may have without being asked depends on its static shared memory too, so that small sizes ask as well.
 template <auto Kernel>
 int opt_in(size_t bytes) {
   constexpr int kDevices = 64;
   static std::atomic<int> reserved[kDevices];
-  if (bytes <= 48 * 1024) return THINFER_OK;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return op_fail(THINFER_ECUDA, "no current CUDA device");
   const int want = static_cast<int>(bytes);

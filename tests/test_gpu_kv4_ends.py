@@ -187,3 +187,45 @@ def test_codes_of_rows_of_tiny_values(T, t):
     sizes = 2.0 ** -np.arange(8, 25) if t == "f16" else 2.0 ** -np.arange(96, 134)
     x = rng.standard_normal((4 * len(sizes), 64)) * np.repeat(sizes, 4)[:, None]
     _written_bytes_are_the_definitions(T, kv4.round_to(x, DT[t]), t)
+
+
+# ------------------------------------------------------------------ page tables
+_POOL_SIZES = """
+import sys
+sys.path.insert(0, {root!r})
+import torch
+from paper_2605_25655_b200 import thinfer
+i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+for call, sizes in (("reserve", {reserve}), ("fork", {fork}), ("compact", {compact})):
+    for n in sizes:
+        tab, lens = i32([[n - 1, -1], [n - 2, -1]]), i32([16, 5])
+        if call == "reserve":
+            out, refused = thinfer.op_kv4_reserve(tab, lens, i32([16, 0]), n, 16)
+            ok = tab.tolist() == [[n - 1, 0], [n - 2, -1]] and out.tolist() == [32, 5]
+            out, refused = thinfer.op_kv4_reserve(tab, lens, i32([0, 1]), n, 16)
+            ok = ok and out.tolist() == [16, 6] and refused.item() == 0
+        else:
+            pool = torch.zeros(1, n, 16 * 72, dtype=torch.uint8, device="cuda")
+            pool[0, n - 2] = 7
+            if call == "fork":
+                t, l, bad = thinfer.op_kv4_fork(pool, tab[1:], lens[1:], i32([0]), 16, 64)
+                ok = t.tolist() == [[n - 2, -1]] and l.tolist() == [5] and bad.item() == 0
+            else:
+                t, live = thinfer.op_kv4_compact(pool, tab, lens, 16, 64)
+                ok = t.tolist() == [[1, -1], [0, -1]] and live.item() == 2 and bool((pool[0, 0] == 7).all())
+        assert ok, (call, n)
+print("all right")
+"""
+
+
+def test_page_calls_of_pools_of_every_size_in_a_fresh_process(T):
+    """Pools whose bitmap is just below 48 KB, or goes above it with what a kernel holds of its own: nothing has been asked of
+    the device before, as the tests of a larger pool in this process have."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = _POOL_SIZES.format(root=root, reserve=[40, 146000, 146896, 146912, 160000, 196608, 196640, 1 << 18],
+                              fork=[196480, 196512, 196544, 196576, 196608], compact=[195000, 196096, 196576, 196608, 196640])
+    got = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert got.returncode == 0 and "all right" in got.stdout, got.stdout[-500:] + got.stderr[-1500:]
