@@ -1,7 +1,6 @@
 // C entry points (include/thinfer.h) of the per-head norm with rotation and of the 4-bit paged cache.  Every call
 // checks its arguments on the host, enqueues its kernels on the given stream and returns; no call allocates, waits or
 // keeps anything for the next.
-#include <atomic>
 #include <cmath>
 
 #include "kv4_attn.cuh"
@@ -102,19 +101,12 @@ bool rows_overlap(const void* a, int64_t sa, int64_t wa, const void* b, int64_t 
   return at < wb || at + wa > sa;
 }
 
-// Opts a kernel in to its dynamic shared memory: a property of the kernel on a device, asked for once for each new maximum.
-// What a kernel may have without being asked depends on its static shared memory too, so that small sizes ask as well.
+// Opts a kernel in to its dynamic shared memory, small sizes too: what it may have without being asked depends on its static
+// shared memory.
 template <auto Kernel>
 int opt_in(size_t bytes) {
-  constexpr int kDevices = 64;
-  static std::atomic<int> reserved[kDevices];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return op_fail(THINFER_ECUDA, "no current CUDA device");
-  const int want = static_cast<int>(bytes);
-  if (dev >= 0 && dev < kDevices && reserved[dev].load(std::memory_order_relaxed) >= want) return THINFER_OK;
-  if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, want) != cudaSuccess)
-    return op_fail(THINFER_ECUDA, "cannot reserve %zu bytes of shared memory", bytes);
-  if (dev >= 0 && dev < kDevices) reserved[dev].store(want, std::memory_order_relaxed);
+  static SmemOptIn opt;
+  if (!opt.ensure(Kernel, static_cast<int>(bytes))) return op_fail(THINFER_ECUDA, "cannot reserve %zu bytes of shared memory", bytes);
   return THINFER_OK;
 }
 

@@ -7,6 +7,7 @@
 #include <cstdio>
 
 #include "../../include/thinfer.h"
+#include "smem_opt_in.cuh"
 
 namespace thinfer {
 
@@ -22,6 +23,19 @@ inline int op_fail(int code, const char* fmt, ...) {
   op_set_error(buf);
   return code;
 }
+
+// The opt-in of one kernel to dynamic shared memory (a function-local static per kernel instantiation), on each device that
+// it is launched on.
+struct SmemOptIn {
+  static constexpr int kMaxDevices = SmemAllowance::kMaxDevices;
+  SmemAllowance allowance;
+  template <typename K>
+  bool ensure(K kernel, int bytes) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) dev = -1;
+    return allowance.ensure(dev, bytes, [&](int n) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, n) == cudaSuccess; });
+  }
+};
 
 // SM count of the current device (asked once per device).
 int op_sm_count();

@@ -346,28 +346,6 @@ struct Launcher {
   }
 };
 
-template <typename K>
-bool opt_in_smem(K kernel, int bytes) {
-  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
-}
-
-// The opt-in above is a per-device property of a kernel.  One of these (a function-local static per kernel
-// instantiation) remembers what has been reserved on which device, so that a process that drives several GPUs
-// opts in on each of them and a launch pays one cudaGetDevice instead of a driver call.
-struct SmemOptIn {
-  static constexpr int kMaxDevices = 64;
-  int reserved[kMaxDevices] = {};
-  template <typename K>
-  bool ensure(K kernel, int bytes) {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return opt_in_smem(kernel, bytes);
-    if (bytes <= reserved[dev]) return true;
-    if (!opt_in_smem(kernel, bytes)) return false;
-    reserved[dev] = bytes;
-    return true;
-  }
-};
-
 // SM count of the current device for the context-free operator entry points (asked once per device)
 int current_sm_count() {
   static int cached[SmemOptIn::kMaxDevices] = {};
