@@ -2,6 +2,7 @@
 // checks its arguments on the host, enqueues its kernels on the given stream and returns; no call allocates, waits or
 // keeps anything for the next.
 #include <cmath>
+#include <initializer_list>
 
 #include "kv4_attn.cuh"
 #include "kv4_cache.cuh"
@@ -55,7 +56,7 @@ Kv4Cache make_cache(const void* pool, const int32_t* table, int32_t rows, int32_
   return c;
 }
 
-bool stride_ok(int64_t stride, int64_t least) { return stride >= least && stride % 8 == 0; }
+bool stride_ok(int64_t stride, int64_t least) { return stride >= least && stride % 8 == 0 && stride <= (int64_t{1} << 40); }
 
 // Lane groups of `lanes` lanes that share the rows of one token: as many as fill the device once (2048 threads an
 // SM), one row each at most.  Twice as many cost 5 to 15 % for long prompts, sixteen times 50 to 70 %.
@@ -92,6 +93,11 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return x < y + nb && y < x + na;
 }
 
+size_t pool_bytes(int32_t n_pages, int32_t n_kv, int32_t head_dim, int32_t page_size) {   // of one layer
+  return static_cast<size_t>(n_pages) * n_kv * page_size * (head_dim + 8);
+}
+size_t table_bytes(int32_t rows, int32_t max_pages) { return static_cast<size_t>(rows) * max_pages * 4; }
+
 // n rows of wa (wb) bytes, sa (sb) bytes apart; with different strides any overlap of the whole ranges counts.
 bool rows_overlap(const void* a, int64_t sa, int64_t wa, const void* b, int64_t sb, int64_t wb, int64_t n) {
   if (!overlap(a, static_cast<size_t>((n - 1) * sa + wa), b, static_cast<size_t>((n - 1) * sb + wb))) return false;
@@ -99,6 +105,32 @@ bool rows_overlap(const void* a, int64_t sa, int64_t wa, const void* b, int64_t 
   const int64_t apart = static_cast<int64_t>(reinterpret_cast<uintptr_t>(a)) - static_cast<int64_t>(reinterpret_cast<uintptr_t>(b));
   const int64_t at = (apart % sa + sa) % sa;   // where a's row begins behind the beginning of one of b's
   return at < wb || at + wa > sa;
+}
+
+struct Span {
+  const void* at;
+  size_t bytes;
+};
+bool meet(std::initializer_list<Span> a, std::initializer_list<Span> b) {
+  for (const Span& x : a)
+    for (const Span& y : b)
+      if (overlap(x.at, x.bytes, y.at, y.bytes)) return true;
+  return false;
+}
+
+// Blocks of d elements at i * ts + h * hs (i < n, h < heads; ts >= d): whether one of them shares an element with one of the
+// same blocks `apart` elements further on; own: the same ones, each against the others.
+bool blocks_meet(bool own, int64_t apart, int64_t ts, int64_t hs, int64_t n, int64_t heads, int64_t d) {
+  for (int64_t dh = 1 - heads; dh < heads; ++dh) {
+    const int64_t base = apart + dh * hs;
+    // the smallest di with base + di * ts >= 0: only for that one and the one before it can the sum lie within d of 0
+    const int64_t low = base >= 0 ? -(base / ts) : (-base + ts - 1) / ts;
+    for (int64_t di = low - 1; di <= low; ++di) {
+      const int64_t at = base + di * ts;
+      if (di > -n && di < n && at > -d && at < d && !(own && dh == 0 && di == 0)) return true;
+    }
+  }
+  return false;
 }
 
 // Opts a kernel in to its dynamic shared memory, small sizes too: what it may have without being asked depends on its static
@@ -278,12 +310,23 @@ int thinfer_op_kv4_read(const void* pool, int32_t n_pages, const int32_t* table,
   if (!stride_ok(token_stride, head_dim) || !stride_ok(head_stride, head_dim) || !aligned16(k_out) || !aligned16(v_out) ||
       !aligned4(rows) || !aligned4(positions))
     return op_fail(THINFER_EINVAL, "kv4_read: a pointer or a stride is not aligned, or a stride is below head_dim");
+  const int64_t d = head_dim, across = (n_kv_heads - 1) * head_stride + d, along = (tokens - 1) * token_stride + d;
+  const size_t out_bytes = static_cast<size_t>(along + across - d) * 2, list_bytes = static_cast<size_t>(tokens) * 4;
+  // one of the two usual orders, or looked at block by block
+  if (token_stride < across && head_stride < along && blocks_meet(true, 0, token_stride, head_stride, tokens, n_kv_heads, d))
+    return op_fail(THINFER_EINVAL, "kv4_read: with these strides rows of an output overlap each other");
+  const int64_t apart = (reinterpret_cast<intptr_t>(v_out) - reinterpret_cast<intptr_t>(k_out)) / 2;
+  if (overlap(k_out, out_bytes, v_out, out_bytes) && blocks_meet(false, apart, token_stride, head_stride, tokens, n_kv_heads, d))
+    return op_fail(THINFER_EINVAL, "kv4_read: k_out and v_out overlap");
+  if (meet({{k_out, out_bytes}, {v_out, out_bytes}}, {{pool, pool_bytes(n_pages, n_kv_heads, head_dim, page_size)}, {table, table_bytes(n_rows, max_pages)},
+                                                      {rows, list_bytes}, {positions, list_bytes}}))
+    return op_fail(THINFER_EINVAL, "kv4_read: an output overlaps the pool, the table, rows or positions");
   Kv4TokensArgs a{};
   a.c = make_cache(pool, table, n_rows, max_pages, n_pages, n_kv_heads, head_dim, page_size);
   a.rows = rows;
   a.positions = positions;
   a.tokens = tokens;
-    a.chunks = share_rows(tokens, 2 * static_cast<int64_t>(n_kv_heads), head_dim / 16, 1);
+  a.chunks = share_rows(tokens, 2 * static_cast<int64_t>(n_kv_heads), head_dim / 16, 1);
   a.k_out = static_cast<half_t*>(k_out);
   a.v_out = static_cast<half_t*>(v_out);
   a.k_stride = a.v_stride = token_stride;

@@ -229,3 +229,39 @@ def test_page_calls_of_pools_of_every_size_in_a_fresh_process(T):
                               fork=[196480, 196512, 196544, 196576, 196608], compact=[195000, 196096, 196576, 196608, 196640])
     got = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
     assert got.returncode == 0 and "all right" in got.stdout, got.stdout[-500:] + got.stderr[-1500:]
+
+
+def test_read_into_every_layout_that_does_not_overlap(T):
+    """Strides and distances of the outputs at random: refused exactly where two rows share an element (counted here element by
+    element), and elsewhere the same values."""
+    import ctypes as C
+    torch, thinfer = T
+    rng = np.random.default_rng(12)
+    d, page, most = 64, 16, 6
+    x = kv4.round_to(rng.standard_normal((most, 5, d)), np.float16)
+    seen = {True: 0, False: 0}
+    buf = torch.zeros(1 << 17, dtype=torch.float16, device="cuda")
+    for trial in range(400):
+        n, hkv = int(rng.integers(1, most + 1)), int(rng.integers(1, 6))
+        pool, table, rows, pos, _ = _one_row(torch, thinfer, x[:n, :hkv], -x[:n, :hkv], "f16", page)
+        if trial % 4 == 0:                                   # K and V side by side in a token, or in a head
+            ts, hs, apart = [(2 * hkv * d, d, hkv * d), (2 * hkv * d, 2 * d, d)][trial // 4 % 2]
+        else:
+            ts, hs = (int(d + 8 * rng.integers(0, 40)) if rng.random() < 0.5 else d * int(rng.integers(1, 8)) for _ in range(2))
+            apart = int(rng.integers(-200, 200)) * 8 if rng.random() < 0.7 else int(rng.integers(-8, 8)) * d
+        at = (1 << 16) + np.arange(d) + ts * np.arange(n)[:, None, None] + hs * np.arange(hkv)[:, None]
+        want = np.concatenate([at.ravel(), at.ravel() + apart])
+        clash = len(np.unique(want)) < len(want)
+        seen[clash] += 1
+        buf.fill_(7.0)
+        tab = _int(torch, table)
+        rc = thinfer.lib().thinfer_op_kv4_read(C.c_void_p(pool.data_ptr()), pool.shape[0], C.c_void_p(tab.data_ptr()), 1, tab.shape[1],
+                                               C.c_void_p(buf.data_ptr() + (2 << 16)), C.c_void_p(buf.data_ptr() + (2 << 16) + 2 * apart), ts, hs,
+                                               C.c_void_p(rows.data_ptr()), C.c_void_p(pos.data_ptr()), n, hkv, d, page,
+                                               C.c_void_p(torch.cuda.current_stream().cuda_stream))
+        assert rc == (thinfer.EINVAL if clash else thinfer.OK), (n, hkv, ts, hs, apart)
+        if not clash:
+            k, v = thinfer.op_kv4_read(pool, tab, rows, pos, page, d, torch.float16)
+            assert torch.equal(buf[torch.from_numpy(at)], k) and torch.equal(buf[torch.from_numpy(at + apart)], v)
+            assert torch.sum(buf == 7.0).item() >= len(buf) - len(want)
+    assert min(seen.values()) > 100, seen

@@ -1,0 +1,32 @@
+"""Calls of the 4-bit paged cache and of the norm with rotation that write over what they read, or twice to one place, are
+refused on the host, before anything is enqueued (no GPU needed)."""
+import pytest
+
+from paper_2605_25655_b200 import _build, thinfer
+
+E, U = thinfer.EINVAL, thinfer.EUNSUPPORTED
+# addresses that are never used: every call below is refused.  Far enough apart that nothing here reaches the next one
+A = [(1 << 30) * (i + 1) for i in range(16)]
+
+
+@pytest.fixture(scope="module")
+def lib():
+    _build.build()
+    return thinfer.lib()
+
+
+def _refused(fn, args, cases, code=E):
+    for change in cases:
+        assert set(change) <= set(args)
+        assert fn(*(change.get(n, v) for n, v in args.items())) == code, change
+        assert thinfer.lib().thinfer_last_error(None)
+
+
+def test_read_refuses_outputs_that_meet(lib):
+    args = dict(pool=A[0], n_pages=4, table=A[1], n_rows=2, maxp=3, ko=A[2], vo=A[3], ts=256, hs=128, rows=A[4], pos=A[5], tokens=5, hkv=2, d=128,
+                page=64, st=None)
+    pool_end = A[0] + 4 * 2 * 64 * 136
+    _refused(lib.thinfer_op_kv4_read, args, [
+        {"vo": A[2]}, {"vo": A[2] + 256}, {"vo": A[2] - 512 * 4}, {"vo": A[2] + 16}, {"ts": 128}, {"ts": 192}, {"ts": 128, "hs": 512}, {"ts": 256, "hs": 512},
+        {"ts": 256, "hs": 328}, {"ts": 384, "vo": A[2] + 2 * 136}, {"ts": 128, "hs": 640, "vo": A[2] + 2 * 5 * 128},
+        {"ko": A[0]}, {"vo": pool_end - 16}, {"ko": A[0] - 16}, {"vo": A[1]}, {"table": A[2] + 64}, {"rows": A[2] + 1024}, {"pos": A[3]}])
