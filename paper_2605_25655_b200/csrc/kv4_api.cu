@@ -96,6 +96,7 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
 size_t pool_bytes(int32_t n_pages, int32_t n_kv, int32_t head_dim, int32_t page_size) {   // of one layer
   return static_cast<size_t>(n_pages) * n_kv * page_size * (head_dim + 8);
 }
+size_t rows_bytes(int64_t n, int64_t stride, int64_t row) { return static_cast<size_t>((n - 1) * stride + row) * 2; }   // from first to last element
 size_t table_bytes(int32_t rows, int32_t max_pages) { return static_cast<size_t>(rows) * max_pages * 4; }
 
 // n rows of wa (wb) bytes, sa (sb) bytes apart; with different strides any overlap of the whole ranges counts.
@@ -284,6 +285,10 @@ int thinfer_op_kv4_append(void* pool, int32_t n_pages, const int32_t* table, int
   const int64_t row = static_cast<int64_t>(n_kv_heads) * head_dim;
   if (!stride_ok(k_stride, row) || !stride_ok(v_stride, row) || !aligned16(k) || !aligned16(v) || !aligned4(rows) || !aligned4(positions))
     return op_fail(THINFER_EINVAL, "kv4_append: a pointer or a token stride is not aligned, or a stride is below heads * head_dim");
+  const size_t list_bytes = static_cast<size_t>(tokens) * 4;
+  if (meet({{pool, pool_bytes(n_pages, n_kv_heads, head_dim, page_size)}},
+           {{k, rows_bytes(tokens, k_stride, row)}, {v, rows_bytes(tokens, v_stride, row)}, {table, table_bytes(n_rows, max_pages)}, {rows, list_bytes}, {positions, list_bytes}}))
+    return op_fail(THINFER_EINVAL, "kv4_append: the pool overlaps what is written into it, the table, rows or positions");
   Kv4TokensArgs a{};
   a.c = make_cache(pool, table, n_rows, max_pages, n_pages, n_kv_heads, head_dim, page_size);
   a.rows = rows;

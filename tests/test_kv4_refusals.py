@@ -30,3 +30,12 @@ def test_read_refuses_outputs_that_meet(lib):
         {"vo": A[2]}, {"vo": A[2] + 256}, {"vo": A[2] - 512 * 4}, {"vo": A[2] + 16}, {"ts": 128}, {"ts": 192}, {"ts": 128, "hs": 512}, {"ts": 256, "hs": 512},
         {"ts": 256, "hs": 328}, {"ts": 384, "vo": A[2] + 2 * 136}, {"ts": 128, "hs": 640, "vo": A[2] + 2 * 5 * 128},
         {"ko": A[0]}, {"vo": pool_end - 16}, {"ko": A[0] - 16}, {"vo": A[1]}, {"table": A[2] + 64}, {"rows": A[2] + 1024}, {"pos": A[3]}])
+
+
+def test_append_refuses_a_pool_over_its_inputs(lib):
+    args = dict(pool=A[0], n_pages=4, table=A[1], n_rows=2, maxp=3, k=A[2], ks=256, v=A[3], vs=512, rows=A[4], pos=A[5], tokens=5, hkv=2, d=128,
+                page=64, st=None)
+    n = 4 * 2 * 64 * 136
+    _refused(lib.thinfer_op_kv4_append, args, [
+        {"k": A[0]}, {"v": A[0] + n - 16}, {"k": A[0] - (4 * 256 + 240) * 2}, {"v": A[0] - (4 * 512 + 240) * 2}, {"table": A[0]}, {"table": A[0] - 20},
+        {"rows": A[0] + 64}, {"pos": A[0] - 16}])
