@@ -457,6 +457,9 @@ int thinfer_op_kv4_fork(void* pool, int32_t n_layers, int32_t n_pages, const int
       if (overlap(outs[o], out_b[o], outs[p], out_b[p])) return op_fail(THINFER_EINVAL, "kv4_fork: two outputs overlap");
   }
   if (workspace_bytes < moves_bytes(n_rows)) return op_fail(THINFER_ECAPACITY, "kv4_fork: the workspace is too small");
+  const Span all_pages{pool, pool_bytes(n_pages, n_kv_heads, head_dim, page_size) * n_layers}, ws{workspace, moves_bytes(n_rows)};
+  if (meet({all_pages, ws}, {{table, tb}, {lens, nb}, {source, nb}, {table_out, tb}, {lens_out, nb}, {refused, 8}}) || meet({all_pages}, {ws}))
+    return op_fail(THINFER_EINVAL, "kv4_fork: the pool or the workspace overlaps another tensor");
   const PageTables t{table, lens, n_rows, max_pages, n_pages, page_shift_of(page_size)};
   const size_t smem = static_cast<size_t>(plan_words(n_pages)) * 8 + nb * 4;
   rc = opt_in<kv4_fork_kernel>(smem);
@@ -485,6 +488,9 @@ int thinfer_op_kv4_compact(void* pool, int32_t n_layers, int32_t n_pages, const 
     return op_fail(THINFER_EINVAL, "kv4_compact: an output overlaps another tensor");
   const int most = n_pages / 2 > 0 ? n_pages / 2 : 1;
   if (workspace_bytes < moves_bytes(n_pages / 2)) return op_fail(THINFER_ECAPACITY, "kv4_compact: the workspace is too small");
+  const Span all_pages{pool, pool_bytes(n_pages, n_kv_heads, head_dim, page_size) * n_layers}, ws{workspace, moves_bytes(n_pages / 2)};
+  if (meet({all_pages, ws}, {{table, tb}, {lens, nb}, {table_out, tb}, {live_pages, 8}}) || meet({all_pages}, {ws}))
+    return op_fail(THINFER_EINVAL, "kv4_compact: the pool or the workspace overlaps another tensor");
   const PageTables t{table, lens, n_rows, max_pages, n_pages, page_shift_of(page_size)};
   const size_t smem = static_cast<size_t>(plan_words(n_pages)) * 8;
   rc = opt_in<kv4_compact_kernel>(smem);

@@ -39,3 +39,16 @@ def test_append_refuses_a_pool_over_its_inputs(lib):
     _refused(lib.thinfer_op_kv4_append, args, [
         {"k": A[0]}, {"v": A[0] + n - 16}, {"k": A[0] - (4 * 256 + 240) * 2}, {"v": A[0] - (4 * 512 + 240) * 2}, {"table": A[0]}, {"table": A[0] - 20},
         {"rows": A[0] + 64}, {"pos": A[0] - 16}])
+
+
+def test_fork_and_compact_refuse_a_pool_or_workspace_over_another_tensor(lib):
+    n = 2 * 32 * 2 * 16 * 72                            # bytes of the pool
+    args = dict(pool=A[0], layers=2, n_pages=32, t=A[1], l=A[2], s=A[3], to=A[4], lo=A[5], r=A[6], rows=4, maxp=8, hkv=2, d=64, page=16, ws=A[7],
+                wb=1 << 12, st=None)
+    _refused(lib.thinfer_op_kv4_fork, args, [
+        *({x: A[0] + n - 16} for x in ("t", "l", "s", "to", "lo", "r", "ws")), *({x: A[7] + 16} for x in ("t", "l", "s", "to", "lo", "r")),
+        {"ws": A[0] - 16}, {"pool": A[1] - n + 16}, {"pool": A[6]}])
+    args = dict(pool=A[0], layers=2, n_pages=32, t=A[1], l=A[2], to=A[4], live=A[6], rows=4, maxp=8, hkv=2, d=64, page=16, ws=A[7], wb=1 << 12, st=None)
+    _refused(lib.thinfer_op_kv4_compact, args, [
+        *({x: A[0] + n - 16} for x in ("t", "l", "to", "live", "ws")), *({x: A[7] + 16} for x in ("t", "l", "to", "live")), {"ws": A[0] - 16},
+        {"pool": A[4] - n + 16}, {"pool": A[6]}])
