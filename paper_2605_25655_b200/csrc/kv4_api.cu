@@ -372,7 +372,8 @@ int thinfer_op_kv4_attention(const void* q, int64_t q_stride, const void* pool, 
   const size_t tab_bytes = static_cast<size_t>(batch) * max_pages * 4, len_bytes = static_cast<size_t>(batch) * 4;
   if (overlap(out, out_bytes, workspace, ws_bytes) || overlap(out, out_bytes, q, q_bytes) || overlap(out, out_bytes, table, tab_bytes) ||
       overlap(out, out_bytes, lens, len_bytes) || overlap(workspace, ws_bytes, q, q_bytes) || overlap(workspace, ws_bytes, table, tab_bytes) ||
-      overlap(workspace, ws_bytes, lens, len_bytes))
+      overlap(workspace, ws_bytes, lens, len_bytes) ||
+      meet({{pool, pool_bytes(n_pages, n_kv_heads, head_dim, page_size)}}, {{out, out_bytes}, {workspace, ws_bytes}}))
     return op_fail(THINFER_EINVAL, "kv4_attention: the output or the workspace overlaps an input, or they overlap each other");
   Kv4AttnArgs a{};
   a.c = make_cache(pool, table, batch, max_pages, n_pages, n_kv_heads, head_dim, page_size);

@@ -52,3 +52,10 @@ def test_fork_and_compact_refuse_a_pool_or_workspace_over_another_tensor(lib):
     _refused(lib.thinfer_op_kv4_compact, args, [
         *({x: A[0] + n - 16} for x in ("t", "l", "to", "live", "ws")), *({x: A[7] + 16} for x in ("t", "l", "to", "live")), {"ws": A[0] - 16},
         {"pool": A[4] - n + 16}, {"pool": A[6]}])
+
+
+def test_attention_refuses_outputs_over_the_pool(lib):
+    args = dict(q=A[0], qs=1024, pool=A[1], n_pages=4, table=A[2], maxp=3, lens=A[3], out=A[4], batch=2, queries=1, hq=8, hkv=2, d=128, page=64, ws=A[5],
+                wb=1 << 24, st=None)
+    n = 4 * 2 * 64 * 136
+    _refused(lib.thinfer_op_kv4_attention, args, [{"out": A[1]}, {"out": A[1] + n - 16}, {"out": A[1] - 16}, {"ws": A[1] + 16}, {"ws": A[1] - 64}])
