@@ -119,6 +119,14 @@ bool meet(std::initializer_list<Span> a, std::initializer_list<Span> b) {
   return false;
 }
 
+// n rows of `wide` bytes, `stride` bytes apart, and one block of memory, which may lie between them.
+bool rows_meet(const void* first, int64_t stride, int64_t wide, int64_t n, const Span& block) {
+  if (block.bytes == 0) return false;
+  const int64_t at = reinterpret_cast<intptr_t>(block.at) - reinterpret_cast<intptr_t>(first);
+  const int64_t i = at < wide ? 0 : (at - wide) / stride + 1;   // the first row that ends behind the block's beginning
+  return i < n && i * stride < at + static_cast<int64_t>(block.bytes);
+}
+
 // Blocks of d elements at i * ts + h * hs (i < n, h < heads; ts >= d): whether one of them shares an element with one of the
 // same blocks `apart` elements further on; own: the same ones, each against the others.
 bool blocks_meet(bool own, int64_t apart, int64_t ts, int64_t hs, int64_t n, int64_t heads, int64_t d) {
@@ -239,6 +247,10 @@ int thinfer_op_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int6
       meet(q_out, q_out_stride, q_row, k, k_stride, k_row) || meet(k_out, k_out_stride, k_row, q, q_stride, q_row) ||
       meet(q_out, q_out_stride, q_row, k_out, k_out_stride, k_row))
     return op_fail(THINFER_EINVAL, "qk_norm_rope: an output overlaps an input that it does not replace, or the other output");
+  const size_t gain_bytes = static_cast<size_t>(head_dim) * 2;
+  for (const Span& in : {Span{q_gain, gain_bytes}, Span{k_gain, gain_bytes}, Span{turns, static_cast<size_t>(rotary_dim) * 4}, Span{positions, static_cast<size_t>(tokens) * 4}})
+    if (rows_meet(q_out, q_out_stride * 2, q_row * 2, tokens, in) || rows_meet(k_out, k_out_stride * 2, k_row * 2, tokens, in))
+      return op_fail(THINFER_EINVAL, "qk_norm_rope: an output overlaps gains, turns or positions");
   QkNormRopeArgs a{};
   a.q = static_cast<const half_t*>(q);
   a.k = static_cast<const half_t*>(k);

@@ -265,3 +265,19 @@ def test_read_into_every_layout_that_does_not_overlap(T):
             assert torch.equal(buf[torch.from_numpy(at)], k) and torch.equal(buf[torch.from_numpy(at + apart)], v)
             assert torch.sum(buf == 7.0).item() >= len(buf) - len(want)
     assert min(seen.values()) > 100, seen
+
+
+def test_norm_with_small_tensors_between_the_rows_of_an_output(T):
+    """Gains, turns and positions in the gaps of a strided output are no overlap."""
+    torch, thinfer = T
+    g = torch.Generator(device="cuda").manual_seed(3)
+    buf = torch.zeros(4, 1024, dtype=torch.float16, device="cuda")       # rows of 4 x 64 values for q_out, then gaps
+    q, k = (torch.randn(4, h, 64, generator=g, device="cuda").half() for h in (4, 1))
+    qg, kg, turns = torch.randn(64, generator=g, device="cuda").half(), torch.randn(64, generator=g, device="cuda").half(), thinfer.rope_turns(1e4, 64)
+    pos = _int(torch, [3, 0, 700, 12])
+    want = thinfer.op_qk_norm_rope(q, k, qg, kg, 1e-6, turns, pos)
+    in_gap = [buf[0, 256:320], buf[1, 256:320], buf[2, 256:384].view(torch.float64), buf[0, 512:520].view(torch.int32)]
+    for dst, src in zip(in_gap, (qg, kg, turns, pos)):
+        dst.copy_(src)
+    got = thinfer.op_qk_norm_rope(q, k, in_gap[0], in_gap[1], 1e-6, in_gap[2], in_gap[3], q_out=buf[:, :256].unflatten(1, (4, 64)))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

@@ -59,3 +59,12 @@ def test_attention_refuses_outputs_over_the_pool(lib):
                 wb=1 << 24, st=None)
     n = 4 * 2 * 64 * 136
     _refused(lib.thinfer_op_kv4_attention, args, [{"out": A[1]}, {"out": A[1] + n - 16}, {"out": A[1] - 16}, {"ws": A[1] + 16}, {"ws": A[1] - 64}])
+
+
+def test_norm_refuses_outputs_over_gains_turns_and_positions(lib):
+    args = dict(q=A[0], qs=1024, k=A[1], ks=256, qo=A[2], qos=1024, ko=A[3], kos=512, qg=A[4], kg=A[5], turns=A[6], pos=A[7], tokens=3, hq=4, hkv=2, d=128,
+                rot=128, halves=0, eps=1e-6, st=None)
+    q_row, k_row = 4 * 128 * 2, 2 * 128 * 2
+    _refused(lib.thinfer_op_qk_norm_rope, args, [
+        {"qg": A[2]}, {"kg": A[2] + 2048 + q_row - 16}, {"turns": A[2] + 2 * 2048 - 16}, {"pos": A[2] - 8}, {"pos": A[2] + 2 * 2048 + q_row - 4},
+        {"qg": A[3] + 1024}, {"kg": A[3] - 240}, {"turns": A[3] + k_row - 8}, {"pos": A[3] + 2 * 1024 + k_row - 8}])
