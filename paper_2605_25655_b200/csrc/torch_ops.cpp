@@ -47,6 +47,22 @@ void check(const Api& api, int rc) {
   }
 }
 
+// Makes one call of the library without the interpreter lock: a full launch queue makes it wait, and the process's other
+// threads go on meanwhile, as they do around a foreign function.  The arguments are ready before the lock is given up.
+struct Unlocked {
+  PyThreadState* state = PyEval_SaveThread();
+  ~Unlocked() { PyEval_RestoreThread(state); }
+};
+template <typename F, typename... A>
+void call(const Api& api, F f, A... a) {
+  int rc;
+  {
+    const Unlocked now;
+    rc = f(a...);
+  }
+  check(api, rc);
+}
+
 std::string describe(const at::Tensor& t) {
   std::string s = std::string(c10::toString(t.scalar_type())) + " [";
   for (int64_t i = 0; i < t.dim(); ++i) s += (i ? ", " : "") + std::to_string(t.size(i));
@@ -164,11 +180,11 @@ PyObject* qk_norm_rope(PyObject* const* a) {
   same_shape(q_out, q, "q_out: the shape of q");
   same_shape(k_out, k, "k_out: the shape of k");
   const int64_t qos = token_stride(q_out, "q_out", type, on), kos = token_stride(k_out, "k_out", type, on);
-  check(api, api.qk_norm_rope(q.data_ptr(), qs, k.data_ptr(), ks, q_out.data_ptr(), qos, k_out.data_ptr(), kos, plain(gq, "q_gain", on, {d}, type),
+  call(api, api.qk_norm_rope, q.data_ptr(), qs, k.data_ptr(), ks, q_out.data_ptr(), qos, k_out.data_ptr(), kos, plain(gq, "q_gain", on, {d}, type),
                               plain(gk, "k_gain", on, {d}, type), static_cast<const double*>(plain(turns, "turns", on, turns.sizes(), at::kDouble)),
                               static_cast<const int32_t*>(plain(positions, "positions", on, {n})), small(n, "tokens"), small(hq, "heads"),
                               small(hkv, "heads"), small(d, "head_dim"), small(2 * turns.size(0), "rotary_dim"), PyObject_IsTrue(a[7]) == 1,
-                              static_cast<float>(eps), on.stream));
+                              static_cast<float>(eps), on.stream);
   return pack({q_out, k_out});
 }
 
@@ -180,12 +196,12 @@ PyObject* reserve(PyObject* const* a) {
   const int64_t rows = table.size(0);
   const at::Tensor lens_out = given_or(a[5], "lens_out", [&] { return on.empty({rows}, at::kInt); });
   const at::Tensor refused = given_or(a[6], "refused", [&] { return on.empty({1}, at::kLong); });
-  check(g_api[0], g_api[0].reserve(const_cast<int32_t*>(tab), static_cast<const int32_t*>(plain(lens, "lens", on, {rows})),
+  call(g_api[0], g_api[0].reserve, const_cast<int32_t*>(tab), static_cast<const int32_t*>(plain(lens, "lens", on, {rows})),
                                    static_cast<const int32_t*>(plain(add, "add", on, {rows})),
                                    static_cast<int32_t*>(plain(lens_out, "lens_out", on, {rows})),
                                    static_cast<int64_t*>(plain(refused, "refused", on, {1}, at::kLong)), small(rows, "rows"),
                                    small(table.size(1), "max_pages"), small(number(a[3], "n_pages"), "n_pages"),
-                                   small(number(a[4], "page_size"), "page_size"), on.stream));
+                                   small(number(a[4], "page_size"), "page_size"), on.stream);
   return pack({lens_out, refused});
 }
 
@@ -201,10 +217,10 @@ PyObject* append(PyObject* const* a) {
   same_shape(k, v, "k and v must have one shape");
   const int64_t n = k.size(0), hkv = k.size(1), d = k.size(2);
   if (pool_heads(pool, 2, page, d, on) != hkv) refuse("the pool's pages are for another number of heads");
-  check(api, api.append(pool.data_ptr(), small(pool.size(0), "pages"), table_of(table, on), small(table.size(0), "rows"), small(table.size(1), "max_pages"),
+  call(api, api.append, pool.data_ptr(), small(pool.size(0), "pages"), table_of(table, on), small(table.size(0), "rows"), small(table.size(1), "max_pages"),
                         k.data_ptr(), ks, v.data_ptr(), vs, static_cast<const int32_t*>(plain(rows, "rows", on, {n})),
                         static_cast<const int32_t*>(plain(positions, "positions", on, {n})), small(n, "tokens"), small(hkv, "heads"),
-                        small(d, "head_dim"), small(page, "page_size"), on.stream));
+                        small(d, "head_dim"), small(page, "page_size"), on.stream);
   Py_RETURN_NONE;
 }
 
@@ -222,10 +238,10 @@ PyObject* read(PyObject* const* a) {
     if (!t->sizes().equals(shape) || t->scalar_type() != type || t->device() != on.device || !t->strides().equals(k_out.strides()))
       refuse("k_out, v_out: [tokens, heads, head_dim] of one type, device and strides");
   if (k_out.stride(2) != 1) refuse("k_out, v_out: the values of a head must be contiguous");
-  check(api, api.read(pool.data_ptr(), small(pool.size(0), "pages"), table_of(table, on), small(table.size(0), "rows"), small(table.size(1), "max_pages"),
+  call(api, api.read, pool.data_ptr(), small(pool.size(0), "pages"), table_of(table, on), small(table.size(0), "rows"), small(table.size(1), "max_pages"),
                       k_out.data_ptr(), v_out.data_ptr(), k_out.stride(0), k_out.stride(1), static_cast<const int32_t*>(plain(rows, "rows", on, {n})),
                       static_cast<const int32_t*>(plain(positions, "positions", on, {n})), small(n, "tokens"), small(hkv, "heads"),
-                      small(d, "head_dim"), small(page, "page_size"), on.stream));
+                      small(d, "head_dim"), small(page, "page_size"), on.stream);
   return pack({k_out, v_out});
 }
 
@@ -257,10 +273,10 @@ PyObject* attention(PyObject* const* a) {
     ws_bytes = static_cast<size_t>(given.numel());
     ws = plain(given, "workspace", on, {given.numel()}, at::kByte);
   }
-  check(api, api.attention(q.data_ptr(), qs, pool.data_ptr(), small(pool.size(0), "pages"), tab, small(table.size(1), "max_pages"),
+  call(api, api.attention, q.data_ptr(), qs, pool.data_ptr(), small(pool.size(0), "pages"), tab, small(table.size(1), "max_pages"),
                            static_cast<const int32_t*>(plain(lens, "lens", on, {b})), plain(out, "out", on, {b, n, hq, d}, type), small(b, "batch"),
                            small(n, "queries"), small(hq, "heads"), small(hkv, "heads"), small(d, "head_dim"), small(page, "page_size"),
-                           ws, ws_bytes, on.stream));
+                           ws, ws_bytes, on.stream);
   return wrap(out);
 }
 
@@ -281,12 +297,12 @@ PyObject* fork(PyObject* const* a) {
   const at::Tensor refused = given_or(a[8], "refused", [&] { return on.empty({1}, at::kLong); });
   size_t ws_bytes = 0;
   const c10::DataPtr ws = pages_workspace(rows, pool.size(1), on, &ws_bytes);
-  check(g_api[0], g_api[0].fork(pool.data_ptr(), small(pool.size(0), "layers"), small(pool.size(1), "pages"), tab,
+  call(g_api[0], g_api[0].fork, pool.data_ptr(), small(pool.size(0), "layers"), small(pool.size(1), "pages"), tab,
                                 static_cast<const int32_t*>(plain(lens, "lens", on, {rows})), static_cast<const int32_t*>(plain(source, "source", on, {rows})),
                                 static_cast<int32_t*>(plain(table_out, "table_out", on, {rows, width})),
                                 static_cast<int32_t*>(plain(lens_out, "lens_out", on, {rows})),
                                 static_cast<int64_t*>(plain(refused, "refused", on, {1}, at::kLong)), small(rows, "rows"), small(width, "max_pages"),
-                                small(hkv, "heads"), small(d, "head_dim"), small(page, "page_size"), ws.get(), ws_bytes, on.stream));
+                                small(hkv, "heads"), small(d, "head_dim"), small(page, "page_size"), ws.get(), ws_bytes, on.stream);
   return pack({table_out, lens_out, refused});
 }
 
@@ -301,12 +317,12 @@ PyObject* compact(PyObject* const* a) {
   const at::Tensor live = given_or(a[6], "live", [&] { return on.empty({1}, at::kLong); });
   size_t ws_bytes = 0;
   const c10::DataPtr ws = pages_workspace(rows, pool.size(1), on, &ws_bytes);
-  check(g_api[0], g_api[0].compact(pool.data_ptr(), small(pool.size(0), "layers"), small(pool.size(1), "pages"), tab,
+  call(g_api[0], g_api[0].compact, pool.data_ptr(), small(pool.size(0), "layers"), small(pool.size(1), "pages"), tab,
                                    static_cast<const int32_t*>(plain(lens, "lens", on, {rows})),
                                    static_cast<int32_t*>(plain(table_out, "table_out", on, {rows, width})),
                                    static_cast<int64_t*>(plain(live, "live", on, {1}, at::kLong)), small(rows, "rows"), small(width, "max_pages"),
                                    small(hkv, "heads"), small(d, "head_dim"), small(page, "page_size"), ws.get(), ws_bytes,
-                                   on.stream));
+                                   on.stream);
   return pack({table_out, live});
 }
 

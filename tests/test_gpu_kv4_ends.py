@@ -281,3 +281,47 @@ def test_norm_with_small_tensors_between_the_rows_of_an_output(T):
         dst.copy_(src)
     got = thinfer.op_qk_norm_rope(q, k, in_gap[0], in_gap[1], 1e-6, in_gap[2], in_gap[3], q_out=buf[:, :256].unflatten(1, (4, 64)))
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+# ------------------------------------------------------------------ calls from Python
+def test_other_threads_go_on_while_a_call_waits(T, tmp_path):
+    """A call that has to wait in the driver (here: an entry point that sleeps half a second) does not hold the interpreter."""
+    import ctypes as C
+    import subprocess
+    import threading
+    import time
+    torch, thinfer = T
+    (tmp_path / "slow.c").write_text("#include <unistd.h>\nint slow(void) { usleep(500000); return 0; }\n")
+    subprocess.run(["gcc", "-shared", "-fPIC", str(tmp_path / "slow.c"), "-o", str(tmp_path / "slow.so")], check=True, timeout=120)
+    slow = C.cast(C.CDLL(str(tmp_path / "slow.so")).slow, C.c_void_p).value
+    ops = thinfer._load_fast()
+    real = [[C.cast(getattr(thinfer.lib(s), n), C.c_void_p).value for n in thinfer._FAST_NAMES] for s in ("f16", "bf16")]
+    quick = ("thinfer_kv4_attention_workspace", "thinfer_kv4_pages_workspace", "thinfer_last_error")
+    z = _int(torch, [0])
+    pool, kv = torch.zeros(1, 16 * 72, dtype=torch.uint8, device="cuda"), torch.zeros(1, 1, 64, dtype=torch.float16, device="cuda")
+    gain, turns = kv[0, 0], thinfer.rope_turns(1e4, 64)
+    calls = (lambda: thinfer.op_qk_norm_rope(kv, kv, gain, gain, 1e-6, turns, z), lambda: thinfer.op_kv4_reserve(z.view(1, 1), z, z, 1, 16),
+             lambda: thinfer.op_kv4_append(pool, z.view(1, 1), kv, kv, z, z, 16), lambda: thinfer.op_kv4_read(pool, z.view(1, 1), z, z, 16, 64, kv.dtype),
+             lambda: thinfer.op_kv4_attention(kv.view(1, 1, 1, 64), pool, z.view(1, 1), z, 16),
+             lambda: thinfer.op_kv4_fork(pool[None], z.view(1, 1), z, z, 16, 64), lambda: thinfer.op_kv4_compact(pool[None], z.view(1, 1), z, 16, 64))
+    ops.bind(thinfer.ThinferError, *([a if n in quick else slow for a, n in zip(r, thinfer._FAST_NAMES)] for r in real))
+    try:
+        for call in calls:
+            turns_taken, stop = [0], threading.Event()
+
+            def other():
+                while not stop.is_set():
+                    time.sleep(0.01)
+                    turns_taken[0] += 1
+            t = threading.Thread(target=other)
+            t.start()
+            begun, before = time.monotonic(), turns_taken[0]
+            call()
+            during, took = turns_taken[0] - before, time.monotonic() - begun
+            stop.set()
+            t.join()
+            assert took > 0.4 and during >= 10, (took, during)
+    finally:
+        ops.bind(thinfer.ThinferError, *real)
+    _, refused = thinfer.op_kv4_reserve(_int(torch, [[-1]]), z, _int(torch, [1]), 1, 16)      # the library's own again
+    assert refused.item() == 0
