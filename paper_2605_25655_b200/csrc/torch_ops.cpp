@@ -81,6 +81,14 @@ int64_t number(PyObject* o, const char* name) {
   }
   return v;
 }
+bool truth(PyObject* o, const char* name) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) {
+    PyErr_Clear();
+    refuse(std::string(name) + ": a truth value is wanted");
+  }
+  return v == 1;
+}
 int32_t small(int64_t v, const char* name) {
   if (v < INT32_MIN || v > INT32_MAX) refuse(std::string(name) + " = " + std::to_string(v) + " does not fit 32 bits");
   return static_cast<int32_t>(v);
@@ -183,7 +191,7 @@ PyObject* qk_norm_rope(PyObject* const* a) {
   call(api, api.qk_norm_rope, q.data_ptr(), qs, k.data_ptr(), ks, q_out.data_ptr(), qos, k_out.data_ptr(), kos, plain(gq, "q_gain", on, {d}, type),
                               plain(gk, "k_gain", on, {d}, type), static_cast<const double*>(plain(turns, "turns", on, turns.sizes(), at::kDouble)),
                               static_cast<const int32_t*>(plain(positions, "positions", on, {n})), small(n, "tokens"), small(hq, "heads"),
-                              small(hkv, "heads"), small(d, "head_dim"), small(2 * turns.size(0), "rotary_dim"), PyObject_IsTrue(a[7]) == 1,
+                              small(hkv, "heads"), small(d, "head_dim"), small(2 * turns.size(0), "rotary_dim"), truth(a[7], "halves"),
                               static_cast<float>(eps), on.stream);
   return pack({q_out, k_out});
 }
@@ -229,7 +237,7 @@ PyObject* read(PyObject* const* a) {
   const at::Tensor &pool = tensor(a[0], "pool"), &table = tensor(a[1], "table"), &rows = tensor(a[2], "rows"), &positions = tensor(a[3], "positions");
   const On on(pool);
   const int64_t page = number(a[4], "page_size"), d = number(a[5], "head_dim"), hkv = pool_heads(pool, 2, page, d, on), n = positions.numel();
-  const at::ScalarType type = PyObject_IsTrue(a[6]) == 1 ? at::kBFloat16 : at::kHalf;
+  const at::ScalarType type = truth(a[6], "bf16") ? at::kBFloat16 : at::kHalf;
   const Api& api = api_of(type);
   const at::Tensor k_out = given_or(a[7], "k_out", [&] { return on.empty({n, hkv, d}, type); });
   const at::Tensor v_out = given_or(a[8], "v_out", [&] { return at::empty_strided({n, hkv, d}, k_out.strides(), k_out.options()); });

@@ -325,3 +325,12 @@ def test_other_threads_go_on_while_a_call_waits(T, tmp_path):
         ops.bind(thinfer.ThinferError, *real)
     _, refused = thinfer.op_kv4_reserve(_int(torch, [[-1]]), z, _int(torch, [1]), 1, 16)      # the library's own again
     assert refused.item() == 0
+
+
+def test_a_truth_value_that_is_none_is_refused(T):
+    torch, thinfer = T
+    z, kv = _int(torch, [0]), torch.zeros(1, 1, 64, dtype=torch.float16, device="cuda")
+    for bad in (np.zeros(2), torch.zeros(2)):
+        with pytest.raises(thinfer.ThinferError) as e:
+            thinfer.op_qk_norm_rope(kv, kv, kv[0, 0], kv[0, 0], 1e-6, thinfer.rope_turns(1e4, 64), z, halves=bad)
+        assert e.value.code == thinfer.EINVAL and "halves" in str(e.value)
