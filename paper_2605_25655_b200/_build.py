@@ -2,6 +2,7 @@
 _ops.so with the host compiler."""
 from __future__ import annotations
 
+import importlib.metadata
 import os
 import shutil
 import subprocess
@@ -35,6 +36,14 @@ def sources():
         os.path.join(os.path.dirname(HERE), "include", "thinfer.h")]
 
 
+def _torch_version():
+    """Version of the installed torch (without importing it), None without one."""
+    try:
+        return importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:
+        return None
+
+
 def _ops_is_stale() -> bool:
     deps = (OPS_SRC, os.path.join(os.path.dirname(HERE), "include", "thinfer.h"))
     return not os.path.exists(OPS) or any(os.path.getmtime(s) > os.path.getmtime(OPS) for s in deps)
@@ -52,7 +61,7 @@ def _ops_command():
 
 def is_stale(lib: str = None) -> bool:
     libs = [lib] if lib else [v[0] for v in VARIANTS]
-    if lib is None and _ops_is_stale():
+    if lib is None and _torch_version() is not None and _ops_is_stale():
         return True
     for l in libs:
         if not os.path.exists(l):
@@ -64,24 +73,30 @@ def is_stale(lib: str = None) -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compiles every .cu of csrc/ into one shared library per storage type and torch_ops.cpp into _ops.so (the
-    compilations run side by side); returns the path of the FP16 library."""
+    """Compiles every .cu of csrc/ into one shared library per storage type and, where torch is installed, torch_ops.cpp
+    into _ops.so (the compilations run side by side, and each leaves its result whatever becomes of the others); returns
+    the path of the FP16 library."""
     cus = [s for s in sources() if s.endswith(".cu")]
     extra = os.environ.get("THINFER_NVCC_EXTRA", "").split()
-    procs = []
+    procs, failed = [], []
     for lib, defs in VARIANTS:
         if not force and not is_stale(lib):
             continue
         cmd = [_nvcc()] + NVCC_FLAGS + defs + extra + (["-Xptxas", "-v"] if verbose else []) + ["-o", lib] + cus
         procs.append((lib, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-    if force or _ops_is_stale():
-        procs.append((OPS, subprocess.Popen(_ops_command(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    if _torch_version() is not None and (force or _ops_is_stale()):   # without torch there is nothing to marshal
+        try:
+            procs.append((OPS, subprocess.Popen(_ops_command(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+        except (OSError, ImportError) as e:                            # the libraries do not depend on it
+            failed.append(f"the compiler cannot be run for {os.path.basename(OPS)}:\n{e}")
     for lib, p in procs:
         out, _ = p.communicate()
         if p.returncode != 0:
-            raise RuntimeError(f"the compiler failed for {os.path.basename(lib)}:\n" + out)
-        if verbose:
+            failed.append(f"the compiler failed for {os.path.basename(lib)}:\n" + out)
+        elif verbose:
             print(out)
+    if failed:
+        raise RuntimeError("\n".join(failed))
     return LIB
 
 
