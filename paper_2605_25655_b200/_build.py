@@ -14,6 +14,7 @@ LIB = os.path.join(HERE, "libthinfer.so")            # IEEE FP16 storage
 LIB_BF16 = os.path.join(HERE, "libthinfer_bf16.so")  # BF16 storage: the same sources with -DTHINFER_BF16
 VARIANTS = ((LIB, []), (LIB_BF16, ["-DTHINFER_BF16"]))
 OPS = os.path.join(HERE, "_ops.so")                  # Python module: torch tensors -> the C entry points
+OPS_TORCH = OPS + ".torch"                           # the version of torch it was compiled for
 OPS_SRC = os.path.join(CSRC, "torch_ops.cpp")
 
 NVCC_FLAGS = [
@@ -46,7 +47,16 @@ def _torch_version():
 
 def _ops_is_stale() -> bool:
     deps = (OPS_SRC, os.path.join(os.path.dirname(HERE), "include", "thinfer.h"))
-    return not os.path.exists(OPS) or any(os.path.getmtime(s) > os.path.getmtime(OPS) for s in deps)
+    return not os.path.exists(OPS) or any(os.path.getmtime(s) > os.path.getmtime(OPS) for s in deps) or _ops_torch() != _torch_version()
+
+
+def _ops_torch():
+    """Version of torch that _ops.so was compiled for: it fits no other."""
+    try:
+        with open(OPS_TORCH) as f:
+            return f.read().strip()
+    except OSError:
+        return None
 
 
 def _ops_command():
@@ -91,6 +101,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
             failed.append(f"the compiler cannot be run for {os.path.basename(OPS)}:\n{e}")
     for lib, p in procs:
         out, _ = p.communicate()
+        if p.returncode == 0 and lib == OPS:
+            with open(OPS_TORCH, "w") as f:
+                f.write(_torch_version() + "\n")
         if p.returncode != 0:
             failed.append(f"the compiler failed for {os.path.basename(lib)}:\n" + out)
         elif verbose:

@@ -409,6 +409,11 @@ def _load_fast():
     global _fast
     if _fast is None:
         import torch  # noqa: F401  (its libraries come first)
+        from . import _build
+        built_for, here = _build._ops_torch(), _build._torch_version()
+        if built_for not in (None, here):
+            raise ThinferError(ECUDA, f"_ops.so was built for torch {built_for}, this is {here}: build it again with "
+                                      "`python -m paper_2605_25655_b200._build`")
         try:
             from . import _ops
         except ImportError as e:

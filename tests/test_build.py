@@ -11,6 +11,7 @@ def fakes(monkeypatch, tmp_path):
     """Targets in a scratch folder and a Popen that writes its target, or fails for the names in `broken`."""
     for name in ("LIB", "LIB_BF16", "OPS"):
         monkeypatch.setattr(_build, name, str(tmp_path / os.path.basename(getattr(_build, name))))
+    monkeypatch.setattr(_build, "OPS_TORCH", str(tmp_path / "version"), raising=False)
     monkeypatch.setattr(_build, "VARIANTS", ((_build.LIB, []), (_build.LIB_BF16, ["-DTHINFER_BF16"])))
     monkeypatch.setattr(_build, "_nvcc", lambda: "nvcc")
     state = {"broken": set(), "missing": set(), "run": []}
@@ -60,3 +61,25 @@ def test_every_failure_is_told(fakes):
     with pytest.raises(RuntimeError) as e:
         _build.build()
     assert "libthinfer.so" in str(e.value) and "_ops.so" in str(e.value) and os.path.exists(_build.LIB_BF16)
+
+
+def test_another_torch_makes_the_module_stale(fakes, monkeypatch):
+    monkeypatch.setattr(_build, "_torch_version", lambda: "1.2.3")
+    _build.build()
+    assert not _build.is_stale() and fakes["run"] == BOTH + ["_ops.so"]
+    monkeypatch.setattr(_build, "_torch_version", lambda: "1.2.4")
+    assert _build.is_stale()
+    _build.build()
+    assert fakes["run"] == BOTH + ["_ops.so"] * 2 and not _build.is_stale()
+
+
+def test_a_module_for_another_torch_is_not_loaded(monkeypatch, tmp_path):
+    from paper_2605_25655_b200 import thinfer
+    _build.build()
+    note = tmp_path / "version"
+    note.write_text("0.0.1\n")
+    monkeypatch.setattr(_build, "OPS_TORCH", str(note), raising=False)
+    monkeypatch.setattr(thinfer, "_fast", None)
+    with pytest.raises(thinfer.ThinferError) as e:
+        thinfer._load_fast()
+    assert "0.0.1" in str(e.value)
