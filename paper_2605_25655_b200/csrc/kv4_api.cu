@@ -269,6 +269,7 @@ int thinfer_op_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int6
   a.n_kv = n_kv_heads;
   a.half = rotary_dim / 2;
   a.eps = eps;
+  a.least = eps < 0x1p-80f ? 0x1p-100f : 0.f;   // beside a larger eps nothing is lost below 2^-100
   a.chunks = share(tokens, static_cast<int64_t>(n_q_heads) + n_kv_heads, head_dim / 8);
   const int64_t groups = static_cast<int64_t>(tokens) * a.chunks, per_cta = 256 / (head_dim / 8);
   const int64_t ctas = (groups + per_cta - 1) / per_cta;

@@ -334,3 +334,49 @@ def test_a_truth_value_that_is_none_is_refused(T):
         with pytest.raises(thinfer.ThinferError) as e:
             thinfer.op_qk_norm_rope(kv, kv, kv[0, 0], kv[0, 0], 1e-6, thinfer.rope_turns(1e4, 64), z, halves=bad)
         assert e.value.code == thinfer.EINVAL and "halves" in str(e.value)
+
+
+# ------------------------------------------------------------------ norm with rotation
+@pytest.mark.parametrize("d,rot,halves", [(64, 64, False), (128, 64, True)])
+def test_norm_of_rows_whose_squares_leave_fp32(T, d, rot, halves):
+    """BF16 rows of 1e16 to 3e38, and of 1e-16 to 1e-38 with an eps of 0 or small beside their squares."""
+    torch, thinfer = T
+    rng = np.random.default_rng(d)
+    sizes = np.array([1e16, 1e18, 1e19, 3e20, 1e30, 1e37, 9e37, 1.0, 1e-12, 1e-16, 1e-19, 1e-22, 1e-30, 1e-36])
+    n = len(sizes)
+    x = kv4.round_to(np.clip(rng.standard_normal((n, 3, d)), -3.5, 3.5) * sizes[:, None, None], "bf16")
+    gain = kv4.round_to(1 + 0.1 * rng.standard_normal(d), "bf16")
+    turns = 10000.0 ** (-2 * np.arange(rot // 2) / rot) / (2 * np.pi)
+    pos = rng.integers(0, 5000, n)
+    for eps in (0.0, 1e-40, 1e-30, 1e-24, 1e-6):
+        got = thinfer.op_qk_norm_rope(_dev(torch, x[:, :2], "bf16"), _dev(torch, x[:, 2:], "bf16"), _dev(torch, gain, "bf16"), _dev(torch, gain, "bf16"), eps,
+                                      torch.tensor(turns, device="cuda"), _int(torch, pos.tolist()), halves=halves)
+        # eps is FP32 in the call
+        want = kv4.qk_norm_rope(x, gain, float(np.float32(eps)), turns, pos, halves)
+        got = np.concatenate([_host(g) for g in got], 1)
+        big = np.max(np.abs(want), axis=-1, keepdims=True)
+        # as in test_norm_and_rotation; results below the smallest normal number are on BF16's grid of 2^-133
+        assert np.all(np.abs(got - want) <= EPS["bf16"] * np.abs(want) + 2.0 ** -18 * big + 2.0 ** -133), eps
+
+
+def test_norm_of_many_rows_with_such_rows_among_them(T):
+    """Lane groups that walk several heads of a token; gains so large that a finished row looks like one of those rows, in place
+    too."""
+    torch, thinfer = T
+    g = torch.Generator(device="cuda").manual_seed(7)
+    n, hq, hkv, d = 2400, 30, 10, 128
+    x = torch.randn(n, hq + hkv, d, generator=g, device="cuda", dtype=torch.float64)
+    x *= torch.where(torch.rand(n, hq + hkv, 1, generator=g, device="cuda") < 0.1, 1e25, 1.0)
+    x = x.bfloat16()
+    gain = (1e20 * (1 + 0.1 * torch.randn(d, generator=g, device="cuda", dtype=torch.float64))).bfloat16()
+    turns, pos = thinfer.rope_turns(1e4, d), torch.randint(0, 4000, (n,), generator=g, device="cuda").to(torch.int32)
+    y = x.double()
+    y = y / torch.sqrt(y.square().mean(-1, keepdim=True) + float(np.float32(1e-6))) * gain.double()
+    angle = 2 * np.pi * torch.remainder(pos.double()[:, None] * turns, 1.0)[:, None]
+    a, b = y[..., 0::2], y[..., 1::2]
+    want = torch.stack([a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()], -1).flatten(-2)
+    q, k = thinfer.op_qk_norm_rope(x[:, :hq], x[:, hq:], gain, gain, 1e-6, turns, pos)
+    tol = EPS["bf16"] * want.abs() + 2.0 ** -18 * want.abs().amax(-1, keepdim=True)
+    assert torch.all((torch.cat([q, k], 1).double() - want).abs() <= tol)
+    thinfer.op_qk_norm_rope(x[:, :hq], x[:, hq:], gain, gain, 1e-6, turns, pos, q_out=x[:, :hq], k_out=x[:, hq:])
+    assert torch.equal(x, torch.cat([q, k], 1))
