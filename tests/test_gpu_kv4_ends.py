@@ -380,3 +380,104 @@ def test_norm_of_many_rows_with_such_rows_among_them(T):
     assert torch.all((torch.cat([q, k], 1).double() - want).abs() <= tol)
     thinfer.op_qk_norm_rope(x[:, :hq], x[:, hq:], gain, gain, 1e-6, turns, pos, q_out=x[:, :hq], k_out=x[:, hq:])
     assert torch.equal(x, torch.cat([q, k], 1))
+
+
+# ------------------------------------------------------------------ the same bits every time
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("hq,hkv,d,page,lens,queries", [
+    (8, 8, 128, 64, [1500, 3, 0, 700], 1), (16, 4, 64, 16, [9000, 1, 4000], 1), (64, 8, 128, 16, [2100, 1999, 4001], 4), (40, 40, 128, 64, [640, 1279, 1000], 1),
+    (2, 1, 64, 32, [33000], 1)])
+def test_attention_repeats_itself_bit_by_bit(T, t, hq, hkv, d, page, lens, queries):
+    """Pairs that are cut across warps and CTAs are merged in a fixed order: twenty calls, some of them beside other work, give
+    the same bits, NaN and all."""
+    torch, thinfer = T
+    g = torch.Generator(device="cuda").manual_seed(hq + d)
+    width = max(-(-n // page) for n in lens) + 1
+    n_pages = len(lens) * width
+    pool = torch.randint(0, 256, (n_pages, hkv * page * (d + 8)), dtype=torch.uint8, device="cuda", generator=g)
+    params = torch.rand(n_pages, hkv, 2 * page, 2, generator=g, device="cuda") * 0.2 + 0.2
+    params[..., 1] *= -7
+    pool.view(n_pages, hkv, -1)[..., page * d:] = params.to(_tt(torch, t)).view(torch.uint8).reshape(n_pages, hkv, -1)
+    table = torch.randperm(n_pages, generator=g, device="cuda").to(torch.int32).view(len(lens), width)
+    q = torch.randn(len(lens), queries, hq, d, generator=g, device="cuda").to(_tt(torch, t))
+    q[-1, 0, 0, 0] = float("nan")                           # one query column that is NaN throughout
+    lens, side = _int(torch, lens), torch.cuda.Stream()
+    first = thinfer.op_kv4_attention(q, pool, table, lens, page)
+    assert first[-1, 0, 0].isnan().all() and first.isfinite().sum() == first.numel() - d
+    busy = torch.randn(2048, 2048, device="cuda")
+    side.wait_stream(torch.cuda.current_stream())
+    for i in range(20):
+        if i % 3 == 1:
+            with torch.cuda.stream(side):
+                busy = busy @ busy * 1e-3                   # takes SMs, so that CTAs begin at other times
+        again = thinfer.op_kv4_attention(q, pool, table, lens, page)
+        assert torch.equal(again.view(torch.int16), first.view(torch.int16)), i
+    torch.cuda.synchronize()
+
+
+def test_attention_with_the_callers_workspace(T):
+    """One workspace for calls in a row, full of NaN at first, of the least size and of a larger one; a smaller one is refused."""
+    import ctypes as C
+    torch, thinfer = T
+    rng = np.random.default_rng(4)
+    x = kv4.round_to(rng.standard_normal((700, 2, 64)), np.float16)
+    pool, table, _, _, _ = _one_row(torch, thinfer, x, x[::-1], "f16", 16)
+    tab, lens = _int(torch, table), _int(torch, [700])
+    need = C.c_size_t(0)
+    assert thinfer.lib().thinfer_kv4_attention_workspace(1, 3, 8, 2, 64, C.byref(need)) == thinfer.OK
+    for extra in (0, 4096):
+        ws = torch.full((need.value + extra,), 255, dtype=torch.uint8, device="cuda")
+        for _ in range(3):
+            q = torch.randn(1, 3, 8, 64, device="cuda").half()
+            assert torch.equal(thinfer.op_kv4_attention(q, pool, tab, lens, 16, workspace=ws), thinfer.op_kv4_attention(q, pool, tab, lens, 16))
+        assert torch.all(ws[need.value:] == 255)
+    with pytest.raises(thinfer.ThinferError) as e:
+        thinfer.op_kv4_attention(q, pool, tab, lens, 16, workspace=ws[:need.value - 1])
+    assert e.value.code == thinfer.ECAPACITY
+
+
+@pytest.mark.parametrize("n", [1, 50, 700])
+def test_attention_of_large_values(T, n):
+    """V rows of 1e31 to 1e34, and K rows of scales on either side of 2^104 under queries as small."""
+    rng = np.random.default_rng(n)
+    for q_size, k_size, v_size in ((1.0, 1.0, 1e31), (1.0, 1.0, 1e33), (1.0, 1.0, 1e34), (1e-31, 1e31, 1e32), (1e-33, 1e33, 1e33)):
+        _attend(T, rng, rng.standard_normal((1, 4, 64)) * q_size, rng.standard_normal((n, 2, 64)) * k_size, rng.standard_normal((n, 2, 64)) * v_size)
+
+
+# ------------------------------------------------------------------ tables of more than 65536 entries
+def _long_tables(rng, rows, width, n_pages, page, fill):
+    counts = rng.multinomial(int(n_pages * fill), [1 / rows] * rows).clip(0, width)
+    lens = [int(max(0, c * page - rng.integers(0, page))) if c else 0 for c in counts]
+    ids, table, at = rng.permutation(n_pages), [], 0
+    for c in counts:
+        table.append([int(i) for i in ids[at:at + c]] + [int(i) for i in rng.integers(-3, n_pages, width - c)])    # stale entries behind
+        at += c
+    return table, lens
+
+
+@pytest.mark.parametrize("rows,width,n_pages,page,fill", [(64, 2048, 7000, 16, 0.7), (3, 30000, 9000, 16, 0.6), (4096, 17, 9000, 32, 0.8), (300, 257, 7000, 128, 0.95)])
+def test_page_calls_over_long_tables(T, rows, width, n_pages, page, fill):
+    torch, thinfer = T
+    assert rows * width > 65536
+    rng = np.random.default_rng(rows)
+    table, lens = _long_tables(rng, rows, width, n_pages, page, fill)
+    t_in, l_in = _int(torch, table), _int(torch, lens)
+    add = [int(x) for x in rng.integers(-2, 3 * page, rows)]
+    want = kv4.reserve(table, lens, add, n_pages, page)
+    tab = t_in.clone()
+    out, refused = thinfer.op_kv4_reserve(tab, l_in, _int(torch, add), n_pages, page)
+    assert tab.tolist() == want[0] and out.tolist() == want[1] and refused.item() == want[2]
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    start = torch.randint(0, 256, (1, n_pages, page * 72), dtype=torch.uint8, device="cuda", generator=g)
+    # the oracle's fork looks through all rows for every row: take few distinct sources where there are many rows
+    source = [int(x) for x in (rng.integers(-1, rows, rows) if rows <= 300 else np.repeat(rng.integers(-1, rows, 16), rows // 16))]
+    tab, l, refused, moves = kv4.fork(table, lens, source, n_pages, page)
+    pool = start.clone()
+    t_out, l_out, bad = thinfer.op_kv4_fork(pool, t_in, l_in, _int(torch, source), page, 64)
+    assert t_out.tolist() == tab and l_out.tolist() == l and bad.item() == refused
+    assert np.array_equal(pool.cpu().numpy(), kv4.copied(start.cpu().numpy(), moves, 1, 64, page))
+    tab, live, moves = kv4.compact(table, lens, n_pages, page)
+    pool = start.clone()
+    t_out, count = thinfer.op_kv4_compact(pool, t_in, l_in, page, 64)
+    assert t_out.tolist() == tab and count.item() == live and t_in.tolist() == table
+    assert np.array_equal(pool.cpu().numpy(), kv4.copied(start.cpu().numpy(), moves, 1, 64, page))
