@@ -333,8 +333,12 @@ int thinfer_op_rmsnorm(const void* x, const void* gain, void* y, int32_t rows, i
  * memory of the current device, every call only enqueues kernels on
  * cuda_stream, allocates nothing and keeps nothing for the next call, and can
  * be captured into a CUDA graph; a replayed graph follows the tables, lengths
- * and positions it finds on the device at that time.  The text of a refusal is
- * in thinfer_last_error(NULL).
+ * and positions it finds on the device at that time.  Calls may come from
+ * several threads at once.  A call with nothing to do (no tokens, rows or
+ * requests) is refused with THINFER_EINVAL like any other size that is not
+ * positive: leave it out.  Outputs and workspaces must not overlap what the
+ * call reads, nor each other, unless it is said that they may.  The text of a
+ * refusal is in thinfer_last_error(NULL), for the calling thread.
  * ------------------------------------------------------------------------ */
 
 /* turns[j] = base^(-2j/rotary_dim) / (2 pi), j < rotary_dim / 2: revolutions per position of each rotated pair, as
@@ -348,7 +352,7 @@ int thinfer_rope_turns(float base, int32_t rotary_dim, double* host_out);
  * halves 0: pairs are neighbours (2j, 2j+1), the framework's order; 1: pairs are (j, j + rotary_dim/2).
  *   q FP16 [tokens][n_q_heads * head_dim], k FP16 [tokens][n_kv_heads * head_dim]; the strides count elements between
  *   tokens, so that both may lie inside one fused projection output.  q_out / k_out: the same layout, may be q / k
- *   themselves (same stride), must not overlap them otherwise.  q_gain, k_gain FP16 [head_dim].  turns FP64
+ *   themselves (same stride), must not overlap them otherwise, nor the gains, turns or positions.  q_gain, k_gain FP16 [head_dim].  turns FP64
  *   [rotary_dim / 2].  positions int32 [tokens]; the outputs of a token with a negative position are left as they were.
  * head_dim 64 or 128; rotary_dim a multiple of 16 up to head_dim (0: norm only); strides multiples of 8; pointers
  * 16-byte aligned. */
@@ -391,7 +395,8 @@ int thinfer_op_kv4_append(void* pool, int32_t n_pages, const int32_t* table, int
 
 /* Reads tokens of one layer back: FP16 values at k_out / v_out + i * token_stride + head * head_stride (elements) for
  * token i = (rows[i], positions[i]); with head_stride = T * head_dim and token_stride = head_dim this is the layout
- * thinfer_op_attention_prefill reads.  A token with a negative row or position is left as it was. */
+ * thinfer_op_attention_prefill reads.  A token with a negative row or position is left as it was.  Any strides do that give
+ * every row of k_out and v_out elements of its own. */
 int thinfer_op_kv4_read(const void* pool, int32_t n_pages, const int32_t* table, int32_t n_rows, int32_t max_pages,
                         void* k_out, void* v_out, int64_t token_stride, int64_t head_stride, const int32_t* rows,
                         const int32_t* positions, int32_t tokens, int32_t n_kv_heads, int32_t head_dim,
@@ -399,7 +404,8 @@ int thinfer_op_kv4_read(const void* pool, int32_t n_pages, const int32_t* table,
 
 /* Attention of the last `queries` tokens of every request over the cache of one layer (Eq. 6): request b is row b of
  * table with lens[b] keys, its query tokens among them; query i attends the keys before position
- * lens[b] - (queries - 1 - i) (one query: all of them).  A query that sees no key gives 0.  q FP16 [batch * queries]
+ * lens[b] - (queries - 1 - i) (one query: all of them).  A query that sees no key gives 0.  Scores, and the sums over the
+ * keys of values times weights of up to 2^8, are FP32: numbers beyond its range come out as infinity or NaN.  q FP16 [batch * queries]
  * tokens of n_q_heads * head_dim values, q_stride elements apart, already rotated; out FP16 [batch][queries][n_q_heads
  * * head_dim].  n_q_heads a multiple of n_kv_heads; batch <= 2048.  workspace: thinfer_kv4_attention_workspace bytes, 16-byte
  * aligned; its contents mean nothing between calls, but calls that may overlap on the device need their own.  out and

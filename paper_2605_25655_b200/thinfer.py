@@ -398,6 +398,7 @@ def op_argmax(logits, stream=None):
 
 # ------------------------------------- per-head norm + rotation, 4-bit paged cache
 # These run once per layer and decode step: their checks, allocations and calls are in csrc/torch_ops.cpp (_ops.so).
+# A call with no tokens, rows or requests is refused: leave it out.
 _FAST_NAMES = ("thinfer_op_qk_norm_rope", "thinfer_op_kv4_reserve", "thinfer_op_kv4_append", "thinfer_op_kv4_read",
                "thinfer_kv4_attention_workspace", "thinfer_op_kv4_attention", "thinfer_kv4_pages_workspace", "thinfer_op_kv4_fork",
                "thinfer_op_kv4_compact", "thinfer_last_error")
@@ -442,7 +443,9 @@ def rope_turns(base, rotary_dim, device="cuda:0"):
 def op_qk_norm_rope(q, k, q_gain, k_gain, eps, turns, positions, halves=False, q_out=None, k_out=None, stream=None):
     """Per-head RMSNorm and rotation of q [tokens, n_q_heads, d] and k [tokens, n_kv_heads, d] (token strides as they
     come, e.g. slices of a fused projection output); turns from rope_turns (its length sets the rotated dimensions);
-    positions int32 [tokens], negative: left as they were.  Returns (q_out, k_out); they may be q and k themselves."""
+    positions int32 [tokens], negative: that token's rows of q_out and k_out are not written (they keep what a given output
+    held; in outputs that the call allocates they are uninitialised memory).  Returns (q_out, k_out); they may be q and k
+    themselves."""
     if stream is not None:
         with _on(stream, q):
             return op_qk_norm_rope(q, k, q_gain, k_gain, eps, turns, positions, halves, q_out, k_out)
@@ -476,7 +479,8 @@ def op_kv4_append(pool, table, k, v, rows, positions, page_size, stream=None):
 
 def op_kv4_read(pool, table, rows, positions, page_size, head_dim, dtype, k_out=None, v_out=None, stream=None):
     """Values of tokens (rows[i], positions[i]) of one layer: (k, v) [tokens, n_kv_heads, d] of `dtype` (the type the
-    pool was written with).  k_out / v_out: two tensors of that shape with equal strides (e.g. transposed views)."""
+    pool was written with).  k_out / v_out: two tensors of that shape with equal strides (e.g. transposed views).  Tokens with
+    a negative row or position are not written: uninitialised memory in outputs that the call allocates."""
     import torch
     if stream is not None:
         with _on(stream, pool):

@@ -481,3 +481,19 @@ def test_page_calls_over_long_tables(T, rows, width, n_pages, page, fill):
     t_out, count = thinfer.op_kv4_compact(pool, t_in, l_in, page, 64)
     assert t_out.tolist() == tab and count.item() == live and t_in.tolist() == table
     assert np.array_equal(pool.cpu().numpy(), kv4.copied(start.cpu().numpy(), moves, 1, 64, page))
+
+
+def test_calls_with_nothing_to_do_are_refused(T):
+    torch, thinfer = T
+    pool = torch.zeros(2, 16 * 72, dtype=torch.uint8, device="cuda")
+    kv, z, none = torch.zeros(0, 1, 64, dtype=torch.float16, device="cuda"), _int(torch, [0]), torch.zeros(0, dtype=torch.int32, device="cuda")
+    gain, tab, no_rows = torch.ones(64, dtype=torch.float16, device="cuda"), _int(torch, [[0]]), torch.zeros(0, 1, dtype=torch.int32, device="cuda")
+    for call in (lambda: thinfer.op_qk_norm_rope(kv, kv, gain, gain, 1e-6, thinfer.rope_turns(1e4, 64), none),
+                 lambda: thinfer.op_kv4_append(pool, tab, kv, kv, none, none, 16), lambda: thinfer.op_kv4_read(pool, tab, none, none, 16, 64, kv.dtype),
+                 lambda: thinfer.op_kv4_attention(kv.view(0, 1, 1, 64), pool, no_rows, none, 16), lambda: thinfer.op_kv4_reserve(no_rows, none, none, 2, 16),
+                 lambda: thinfer.op_kv4_fork(pool[None], no_rows, none, none, 16, 64), lambda: thinfer.op_kv4_compact(pool[None], no_rows, none, 16, 64),
+                 lambda: thinfer.op_kv4_reserve(torch.zeros(1, 0, dtype=torch.int32, device="cuda"), z, z, 2, 16),
+                 lambda: thinfer.op_kv4_append(pool[:0], tab, kv, kv, none, none, 16)):
+        with pytest.raises(thinfer.ThinferError) as e:
+            call()
+        assert e.value.code == thinfer.EINVAL
