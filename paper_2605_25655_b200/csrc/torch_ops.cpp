@@ -243,11 +243,13 @@ PyObject* read(PyObject* const* a) {
   const at::Tensor v_out = given_or(a[8], "v_out", [&] { return at::empty_strided({n, hkv, d}, k_out.strides(), k_out.options()); });
   const int64_t shape[3] = {n, hkv, d};
   for (const at::Tensor* t : {&k_out, &v_out})
-    if (!t->sizes().equals(shape) || t->scalar_type() != type || t->device() != on.device || !t->strides().equals(k_out.strides()))
-      refuse("k_out, v_out: [tokens, heads, head_dim] of one type, device and strides");
-  if (k_out.stride(2) != 1) refuse("k_out, v_out: the values of a head must be contiguous");
+    if (!t->sizes().equals(shape) || t->scalar_type() != type || t->device() != on.device || (d > 1 && t->stride(2) != 1) ||
+        (n > 1 && t->stride(0) != k_out.stride(0)) || (hkv > 1 && t->stride(1) != k_out.stride(1)))
+      refuse("k_out, v_out: [tokens, heads, head_dim] of one type, device and strides, the values of a head contiguous");
+  // the stride of a dimension of one says nothing
+  const int64_t hs = hkv > 1 ? k_out.stride(1) : d, ts = n > 1 ? k_out.stride(0) : hkv * d;
   call(api, api.read, pool.data_ptr(), small(pool.size(0), "pages"), table_of(table, on), small(table.size(0), "rows"), small(table.size(1), "max_pages"),
-                      k_out.data_ptr(), v_out.data_ptr(), k_out.stride(0), k_out.stride(1), static_cast<const int32_t*>(plain(rows, "rows", on, {n})),
+                      k_out.data_ptr(), v_out.data_ptr(), ts, hs, static_cast<const int32_t*>(plain(rows, "rows", on, {n})),
                       static_cast<const int32_t*>(plain(positions, "positions", on, {n})), small(n, "tokens"), small(hkv, "heads"),
                       small(d, "head_dim"), small(page, "page_size"), on.stream);
   return pack({k_out, v_out});

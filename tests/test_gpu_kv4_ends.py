@@ -497,3 +497,17 @@ def test_calls_with_nothing_to_do_are_refused(T):
         with pytest.raises(thinfer.ThinferError) as e:
             call()
         assert e.value.code == thinfer.EINVAL
+
+
+@pytest.mark.parametrize("n,hkv", [(1, 3), (4, 1), (1, 1)])
+def test_read_into_outputs_whose_strides_differ_where_there_is_one(T, n, hkv):
+    torch, thinfer = T
+    x = kv4.round_to(np.random.default_rng(n).standard_normal((n, hkv, 64)), np.float16)
+    pool, table, rows, pos, _ = _one_row(torch, thinfer, x, -x, "f16", 16)
+    want = thinfer.op_kv4_read(pool, _int(torch, table), rows, pos, 16, 64, torch.float16)
+    k = torch.empty_strided((n, hkv, 64), (64 * hkv if n > 1 else 3, 64 if hkv > 1 else 0, 1), dtype=torch.float16, device="cuda")
+    v = torch.empty_strided((n, hkv, 64), (64 * hkv if n > 1 else 4096, 64 if hkv > 1 else 8, 1), dtype=torch.float16, device="cuda")
+    thinfer.op_kv4_read(pool, _int(torch, table), rows, pos, 16, 64, torch.float16, k_out=k, v_out=v)
+    assert torch.equal(k, want[0]) and torch.equal(v, want[1])
+    with pytest.raises(thinfer.ThinferError):
+        thinfer.op_kv4_read(pool, _int(torch, table), rows, pos, 16, 64, torch.float16, k_out=k, v_out=torch.empty(n, hkv, 128, dtype=k.dtype, device="cuda")[..., ::2])
