@@ -44,6 +44,7 @@ __device__ __forceinline__ int qk_norm_rope_rows(const QkNormRopeArgs& a, int fr
   const long long group = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) / LPR;
   const long long token = group / a.chunks;
   const int chunk = static_cast<int>(group - token * a.chunks);
+  if (!SCALED) pdl_wait();             // behind what needs no memory
   const int pos = token < a.tokens ? a.positions[token] : -1;
   if (pos < 0) return -1;              // the same for the group, and shuffles stay inside it
   // this lane's values: two runs of four.  Halves: values j .. j + 3 of both halves, or eight behind the rotated ones
@@ -144,7 +145,6 @@ __device__ __noinline__ void qk_norm_rope_far_rows(const QkNormRopeArgs& a, int 
 template <int D, bool HALVES>
 __global__ void __launch_bounds__(256, 4) qk_norm_rope_kernel(const __grid_constant__ QkNormRopeArgs a) {
   pdl_launch_dependents();
-  pdl_wait();
   const int from = qk_norm_rope_rows<D, HALVES, false>(a, 0);
   if (kStorageType == 1 && from >= 0) qk_norm_rope_far_rows<D, HALVES>(a, from);
 }
