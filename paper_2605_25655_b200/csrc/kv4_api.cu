@@ -56,7 +56,10 @@ Kv4Cache make_cache(const void* pool, const int32_t* table, int32_t rows, int32_
   return c;
 }
 
-bool stride_ok(int64_t stride, int64_t least) { return stride >= least && stride % 8 == 0 && stride <= (int64_t{1} << 40); }
+// n rows `stride` elements apart: in order, aligned, and within 2^50 elements, so that no product here leaves 64 bits.
+bool stride_ok(int64_t stride, int64_t least, int64_t n) {
+  return stride >= least && stride % 8 == 0 && (n <= 1 || stride <= (int64_t{1} << 50) / n);
+}
 
 // Lane groups of `lanes` lanes that share the rows of one token: as many as fill the device once (2048 threads an
 // SM), one row each at most.  Twice as many cost 5 to 15 % for long prompts, sixteen times 50 to 70 %.
@@ -234,7 +237,8 @@ int thinfer_op_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int6
   if (halves != 0 && halves != 1) return op_fail(THINFER_EINVAL, "halves must be 0 or 1");
   if (n_q_heads > 65536 || n_kv_heads > 65536) return op_fail(THINFER_EUNSUPPORTED, "more than 65536 heads");
   const int64_t q_row = static_cast<int64_t>(n_q_heads) * head_dim, k_row = static_cast<int64_t>(n_kv_heads) * head_dim;
-  if (!stride_ok(q_stride, q_row) || !stride_ok(q_out_stride, q_row) || !stride_ok(k_stride, k_row) || !stride_ok(k_out_stride, k_row))
+  if (!stride_ok(q_stride, q_row, tokens) || !stride_ok(q_out_stride, q_row, tokens) || !stride_ok(k_stride, k_row, tokens) ||
+      !stride_ok(k_out_stride, k_row, tokens))
     return op_fail(THINFER_EINVAL, "qk_norm_rope: a token stride is below heads * head_dim or no multiple of 8");
   if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(q_gain) || !aligned16(k_gain) ||
       !aligned4(positions) || (reinterpret_cast<uintptr_t>(turns) & 7u) != 0)
@@ -296,7 +300,7 @@ int thinfer_op_kv4_append(void* pool, int32_t n_pages, const int32_t* table, int
   if (k == nullptr || v == nullptr || rows == nullptr || positions == nullptr || tokens <= 0)
     return op_fail(THINFER_EINVAL, "kv4_append: NULL pointer or no tokens");
   const int64_t row = static_cast<int64_t>(n_kv_heads) * head_dim;
-  if (!stride_ok(k_stride, row) || !stride_ok(v_stride, row) || !aligned16(k) || !aligned16(v) || !aligned4(rows) || !aligned4(positions))
+  if (!stride_ok(k_stride, row, tokens) || !stride_ok(v_stride, row, tokens) || !aligned16(k) || !aligned16(v) || !aligned4(rows) || !aligned4(positions))
     return op_fail(THINFER_EINVAL, "kv4_append: a pointer or a token stride is not aligned, or a stride is below heads * head_dim");
   const size_t list_bytes = static_cast<size_t>(tokens) * 4;
   if (meet({{pool, pool_bytes(n_pages, n_kv_heads, head_dim, page_size)}},
@@ -325,7 +329,7 @@ int thinfer_op_kv4_read(const void* pool, int32_t n_pages, const int32_t* table,
   if (rc != THINFER_OK) return rc;
   if (k_out == nullptr || v_out == nullptr || rows == nullptr || positions == nullptr || tokens <= 0)
     return op_fail(THINFER_EINVAL, "kv4_read: NULL pointer or no tokens");
-  if (!stride_ok(token_stride, head_dim) || !stride_ok(head_stride, head_dim) || !aligned16(k_out) || !aligned16(v_out) ||
+  if (!stride_ok(token_stride, head_dim, tokens) || !stride_ok(head_stride, head_dim, n_kv_heads) || !aligned16(k_out) || !aligned16(v_out) ||
       !aligned4(rows) || !aligned4(positions))
     return op_fail(THINFER_EINVAL, "kv4_read: a pointer or a stride is not aligned, or a stride is below head_dim");
   const int64_t d = head_dim, across = (n_kv_heads - 1) * head_stride + d, along = (tokens - 1) * token_stride + d;
@@ -376,7 +380,7 @@ int thinfer_op_kv4_attention(const void* q, int64_t q_stride, const void* pool, 
   AttnPlan p;
   rc = plan_attention(batch, queries, n_q_heads, n_kv_heads, head_dim, &p);
   if (rc != THINFER_OK) return rc;
-  if (!stride_ok(q_stride, static_cast<int64_t>(n_q_heads) * head_dim) || !aligned16(q) || !aligned16(out) || !aligned4(lens) || !aligned16(workspace))
+  if (!stride_ok(q_stride, static_cast<int64_t>(n_q_heads) * head_dim, static_cast<int64_t>(batch) * queries) || !aligned16(q) || !aligned16(out) || !aligned4(lens) || !aligned16(workspace))
     return op_fail(THINFER_EINVAL, "kv4_attention: a pointer or the token stride is not aligned, or the stride is below heads * head_dim");
   if (workspace_bytes < p.split_bytes + p.part_bytes)
     return op_fail(THINFER_ECAPACITY, "kv4_attention: the workspace has %zu bytes of %zu", workspace_bytes, p.split_bytes + p.part_bytes);

@@ -68,3 +68,19 @@ def test_norm_refuses_outputs_over_gains_turns_and_positions(lib):
     _refused(lib.thinfer_op_qk_norm_rope, args, [
         {"qg": A[2]}, {"kg": A[2] + 2048 + q_row - 16}, {"turns": A[2] + 2 * 2048 - 16}, {"pos": A[2] - 8}, {"pos": A[2] + 2 * 2048 + q_row - 4},
         {"qg": A[3] + 1024}, {"kg": A[3] - 240}, {"turns": A[3] + k_row - 8}, {"pos": A[3] + 2 * 1024 + k_row - 8}])
+
+
+def test_strides_beyond_any_memory_are_refused(lib):
+    big = 1 << 62
+    args = dict(pool=A[0], n_pages=4, table=A[1], n_rows=2, maxp=3, ko=A[2], vo=A[3], ts=256, hs=128, rows=A[4], pos=A[5], tokens=5, hkv=2, d=128,
+                page=64, st=None)
+    _refused(lib.thinfer_op_kv4_read, args, [{"ts": big}, {"hs": big}, {"ts": 1 << 40, "tokens": (1 << 31) - 1}])
+    args = dict(pool=A[0], n_pages=4, table=A[1], n_rows=2, maxp=3, k=A[2], ks=256, v=A[3], vs=512, rows=A[4], pos=A[5], tokens=5, hkv=2, d=128,
+                page=64, st=None)
+    _refused(lib.thinfer_op_kv4_append, args, [{"ks": big}, {"vs": big}, {"vs": 1 << 40, "tokens": (1 << 31) - 1}])
+    args = dict(q=A[0], qs=1024, k=A[1], ks=256, qo=A[2], qos=1024, ko=A[3], kos=512, qg=A[4], kg=A[5], turns=A[6], pos=A[7], tokens=3, hq=4, hkv=2, d=128,
+                rot=128, halves=0, eps=1e-6, st=None)
+    _refused(lib.thinfer_op_qk_norm_rope, args, [{"qs": big}, {"ks": big}, {"qos": big}, {"kos": big}])
+    args = dict(q=A[0], qs=1024, pool=A[1], n_pages=4, table=A[2], maxp=3, lens=A[3], out=A[4], batch=2, queries=1, hq=8, hkv=2, d=128, page=64, ws=A[5],
+                wb=1 << 24, st=None)
+    _refused(lib.thinfer_op_kv4_attention, args, [{"qs": big}])
