@@ -287,7 +287,7 @@ struct Kv4Acc {
       for (int j = 0; j < 2; ++j) {
         m[n][j] = kKv4Low;
         l[n][j] = z[n][j] = 0.f;
-        ref[n][j] = __int_as_float(227 << 23);  // 2^100: the first weight sets it
+        ref[n][j] = __int_as_float(245 << 23);  // 2^118: the first weight sets it
       }
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
@@ -485,7 +485,8 @@ __device__ __forceinline__ void kv4_stage(Kv4Acc<D, NT>& s, const uint8_t* stage
           for (int e = 0; e < 2; ++e) big = fmaxf(big, ex2_approx(raw(e, n, j, mx)) * vscale(e, n, j));
 #pragma unroll
           for (int off = 4; off < 32; off <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, off));
-          const int ex = min(max(__float_as_int(big) >> 23, 27), 252);
+          // at most 2^118: scales down to BF16's smallest leave weights inside FP16, and p * ref (p <= 2^8) inside FP32
+          const int ex = min(max(__float_as_int(big) >> 23, 9), 252);
           const float ref = __int_as_float((254 - ex) << 23);
           const float move = (al * ref) * exact_inverse(s.ref[n][j]);
           s.m[n][j] = mx;

@@ -511,3 +511,13 @@ def test_read_into_outputs_whose_strides_differ_where_there_is_one(T, n, hkv):
     assert torch.equal(k, want[0]) and torch.equal(v, want[1])
     with pytest.raises(thinfer.ThinferError):
         thinfer.op_kv4_read(pool, _int(torch, table), rows, pos, 16, 64, torch.float16, k_out=k, v_out=torch.empty(n, hkv, 128, dtype=k.dtype, device="cuda")[..., ::2])
+
+
+@pytest.mark.parametrize("n", [1, 50, 700])
+def test_attention_of_tiny_values(T, n):
+    """V rows of 1e-28 to 1e-36, some of them constant (scale 0)."""
+    rng = np.random.default_rng(n + 1)
+    for v_size in (1e-28, 1e-31, 1e-33, 1e-35, 1e-36):
+        v = rng.standard_normal((n, 2, 64)) * v_size
+        v[::3, 0] = v[::3, 0, :1]
+        _attend(T, rng, rng.standard_normal((1, 4, 64)), rng.standard_normal((n, 2, 64)), v)
