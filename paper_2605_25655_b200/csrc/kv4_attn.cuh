@@ -41,8 +41,8 @@
 // and a second kernel, chained to this one, merges it in CTA order: the result does not depend on timing, and the
 // workspace needs no initial state.
 //
-// Measured: those 64 requests, 845 MB, in 162 us (5.2 TB/s, 81 % of a copy; BF16 174); held there for a second the kernel meets the
-// 1000 W limit and takes 190 us.  About 510 instructions per 32 tokens and warp, 54 % of the cycles of the half-rate integer
+// Measured: those 64 requests, 845 MB, in 189 us a call when calls follow one another (4.5 TB/s, 70 % of a copy: the kernel meets the
+// 1000 W limit), and in 161 us (BF16 173) in short replayed runs, before it does.  About 510 instructions per 32 tokens and warp, 54 % of the cycles of the half-rate integer
 // pipe, the rest latency that three warps per scheduler do not cover; without any arithmetic the copies alone take 129 us.
 // 16 requests of up to 1279 keys, 40 KV heads: 26 us, of which 3 pass before the first key arrives and 5 behind the last.
 #pragma once

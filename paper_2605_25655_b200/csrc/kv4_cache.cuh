@@ -78,6 +78,10 @@ __device__ __forceinline__ float by_15(float x) {
   return fmaf(fmaf(-15.f, q, x), 1.f / 15.f, q);
 }
 
+// a + b, not negative: exact, or the neighbour of the exact sum with an odd last bit.
+__device__ __forceinline__ float odd_sum(float a, float b) {
+  return __int_as_float(__float_as_int(__fadd_rz(a, b)) | (__float_as_int(__fadd_ru(a, b)) & 1));
+}
 // x + less, not negative, two at a time: exact, or the neighbour of the exact sum with an odd last bit.
 __device__ __forceinline__ uint64_t kv4_less(uint64_t x, uint64_t less) {
   return add_rz_f32x2(x, less) | (add_rp_f32x2(x, less) & 0x0000000100000001ull);
@@ -168,9 +172,12 @@ __device__ __forceinline__ void kv4_append_rows(const Kv4TokensArgs& a, const Kv
         ends = max2_nan(ends, *reinterpret_cast<const half2_t*>(&other));
       }
       const float2 hl = h2_to_f2(ends);
-      // of halves in the BF16 build, whose rows may span more than FP32's largest value, though not more than twice that
+      // The span has to keep on which side of a tie of its fifteenth it lies: where FP16 ends take more than 24 bits, with an odd
+      // last bit, as above (BF16 ends so far apart are too far from any tie).  A BF16 row may span more than FP32's largest value,
+      // though not more than twice that: halves there.
       constexpr float H = kStorageType == 1 ? 0.5f : 1.f;
-      const float lo = -hl.y, span = H * hl.x - H * lo, probe = span * 0.f;   // probe: NaN as soon as one value is NaN or infinite
+      const float hi = hl.x, lo = -hl.y;
+      const float span = kStorageType == 1 ? H * hi - H * lo : odd_sum(hi, -lo), probe = span * 0.f;   // probe: NaN as soon as one value is NaN or infinite
       const float scale = h_to_f(f_to_h(by_15(span) * (1.f / H)));
       uint32_t word[2];
 #pragma unroll

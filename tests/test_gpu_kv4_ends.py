@@ -521,3 +521,24 @@ def test_attention_of_tiny_values(T, n):
         v = rng.standard_normal((n, 2, 64)) * v_size
         v[::3, 0] = v[::3, 0, :1]
         _attend(T, rng, rng.standard_normal((1, 4, 64)), rng.standard_normal((n, 2, 64)), v)
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+def test_scales_beside_the_middle_of_two(T, t):
+    """Rows whose max - min is 15 times the middle of two values of the type, or just beside that: by less than FP32 can tell."""
+    rng = np.random.default_rng(15)
+    bits, rows = {"f16": 11, "bf16": 8}[t], []
+    while len(rows) < 600:
+        e = int(rng.integers(-6, 3)) if t == "f16" else int(rng.integers(-40, 40))
+        far = 15.0 * (2 * int(rng.integers(2 ** (bits - 1), 2 ** bits)) + 1) * 2.0 ** e       # 15 times a middle
+        high = float(kv4.round_to(far, DT[t]))
+        low = -(far - high)
+        if not 0 < abs(high) < 65504 or low >= 0:
+            continue
+        low = float(kv4.round_to(low, DT[t]))
+        step = 2.0 ** (np.floor(np.log2(-low)) - bits + 1)
+        low += step * int(rng.integers(-2, 3))                                                # 0: on the middle itself
+        x = rng.uniform(low, high, 64)
+        x[0], x[1] = high, low
+        rows.append(x)
+    _written_bytes_are_the_definitions(T, kv4.round_to(np.array(rows), DT[t]), t)
