@@ -380,8 +380,9 @@ int thinfer_kv4_page_bytes(int32_t n_kv_heads, int32_t head_dim, int32_t page_si
 
 /* Makes room for add[r] more tokens of every row (negative: none): rows in ascending order take the lowest free pages,
  * their numbers are written into table, lens_out[r] = lens[r] + add[r].  A row whose pages, together with those asked
- * for by the rows before it, exceed the free pages, or that would not fit max_pages, keeps its length and table;
- * *refused (int64) counts those rows.  lens_out may be lens.  n_rows <= 4096, n_pages <= 262144. */
+ * for by the rows before it (refused ones among them), exceed the free pages, or that would not fit max_pages, keeps its
+ * length and table; *refused (int64) counts those rows.  Their new tokens have no place: entries behind a row's pages may
+ * name pages that others own by now, so leave those tokens out of the append (a row whose length did not grow: rows[i] = -1).  lens_out may be lens.  n_rows <= 4096, n_pages <= 262144. */
 int thinfer_op_kv4_reserve(int32_t* table, const int32_t* lens, const int32_t* add, int32_t* lens_out, int64_t* refused,
                            int32_t n_rows, int32_t max_pages, int32_t n_pages, int32_t page_size, void* cuda_stream);
 

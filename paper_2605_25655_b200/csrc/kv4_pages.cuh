@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_reserve_kernel(const PageTab
   if (threadIdx.x == 0) wanted = bad = 0;
   __syncthreads();
   auto need_of = [&](int r, int* first, long long* after) {
-    const int n = tables_len(t, r), a = max(add[r], 0);
+    const int n = max(t.lens[r], 0), a = max(add[r], 0);   // a length beyond the table asks for what it says, and is refused
     *first = pages_for(n, t.page_shift);
     *after = static_cast<long long>(n) + a;
     return static_cast<int>(((*after + (1 << t.page_shift) - 1) >> t.page_shift) - *first);

@@ -542,3 +542,14 @@ def test_scales_beside_the_middle_of_two(T, t):
         x[0], x[1] = high, low
         rows.append(x)
     _written_bytes_are_the_definitions(T, kv4.round_to(np.array(rows), DT[t]), t)
+
+
+def test_reserve_behind_a_row_whose_length_is_beyond_its_table(T):
+    """It is refused, and the rows behind it get the pages that its length, as it stands, leaves them."""
+    torch, thinfer = T
+    for lens, add in (([33, 5, 16], [10, 20, 1]), ([33, 5, 16], [20, 20, 1]), ([48, 0, 0], [0, 3, 4]), ([47, 1, 1], [2, 40, 20])):
+        table = [[7, 8], [9, -1], [3, -1]]
+        want = kv4.reserve(table, lens, add, 10, 16)
+        tab = _int(torch, table)
+        out, refused = thinfer.op_kv4_reserve(tab, _int(torch, lens), _int(torch, add), 10, 16)
+        assert tab.tolist() == want[0] and out.tolist() == want[1] and refused.item() == want[2], (lens, add)
