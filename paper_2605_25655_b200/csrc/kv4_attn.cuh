@@ -334,15 +334,17 @@ __device__ __forceinline__ void kv4_load_queries(const Kv4AttnArgs& a, Kv4Acc<D,
     }
     float top = 0.f, sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8 * W; ++e) top = fmaxf(top, fabsf(x[e]));
+    for (int e = 0; e < 8 * W; ++e) {
+      top = fmaxf(top, fabsf(x[e]));
+      sum = fmaf(x[e], 1.f / kKv4Last, sum);   // the sum of large values of one sign may pass FP32
+    }
 #pragma unroll
-    for (int off = 1; off < 4; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    for (int off = 1; off < 4; off <<= 1) {
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+      sum += __shfl_xor_sync(0xffffffffu, sum, off);
+    }
     const int ex = min(max(__float_as_int(top) >> 23, 13), 253);
     const float up = __int_as_float((266 - ex) << 23), down = __int_as_float((ex - 12) << 23);
-#pragma unroll
-    for (int e = 0; e < 8 * W; ++e) sum = fmaf(x[e], up, sum);      // of the scaled values: the sum of large ones may pass FP32
-#pragma unroll
-    for (int off = 1; off < 4; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       const float* y = x + 8 * w;
@@ -351,7 +353,7 @@ __device__ __forceinline__ void kv4_load_queries(const Kv4AttnArgs& a, Kv4Acc<D,
       s.q[n][2 * w + 1][0] = pack_f16(y[2] * up, y[6] * up);
       s.q[n][2 * w + 1][1] = pack_f16(y[3] * up * 0.0625f, y[7] * up * 0.0625f);
     }
-    const float qf = (16777216.f / kKv4Last) * down * a.scale_log2, qs = sum * 0x1p-24f * qf;
+    const float qf = (16777216.f / kKv4Last) * down * a.scale_log2, qs = sum * a.scale_log2;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       s.qf[n][j] = __shfl_sync(0xffffffffu, qf, 8 * c + 4 * j);
