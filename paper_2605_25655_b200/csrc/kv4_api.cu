@@ -73,8 +73,8 @@ int share(int64_t tokens, int64_t rows, int lanes) {
 // `at_once` times, that; otherwise a power of two, so that the groups of a warp are on neighbouring heads of one token: at
 // most 8 rows each (append of 7000 tokens of 32 heads, 32 / 16 / 8 / 4 rows: 21, 15, 11, 12 us), and more groups while the
 // device is not full.  Against as many groups as 2048 threads an SM hold: appends of 6800 tokens of 32 heads 36 instead of
-// 38 us, of 17000 from L2 20 instead of 39; reads of 5000 tokens of 8 heads 7 instead of 9, of 6800 of 32 heads 28 against 27.  (Appends measured before their codes were
-// made exact, which adds 7 % on either side.)
+// 38 us, of 17000 from L2 20 instead of 39 (before their codes were made exact, which adds 7 % on either side); reads of 5000
+// tokens of 8 heads 7 instead of 9, of 6800 of 32 heads 28 against 27.
 int share_rows(int64_t tokens, int64_t rows, int lanes, int at_once) {
   const int64_t slots = static_cast<int64_t>(op_sm_count()) * (kKv4CtasPerSm * 256 / lanes);
   if (tokens * rows <= slots * at_once) return static_cast<int>(rows);

@@ -553,3 +553,48 @@ def test_reserve_behind_a_row_whose_length_is_beyond_its_table(T):
         tab = _int(torch, table)
         out, refused = thinfer.op_kv4_reserve(tab, _int(torch, lens), _int(torch, add), 10, 16)
         assert tab.tolist() == want[0] and out.tolist() == want[1] and refused.item() == want[2], (lens, add)
+
+
+def test_calls_from_several_threads(T):
+    """Four threads, each with its own stream, sizes, results and refusals."""
+    import threading
+    torch, thinfer = T
+    rng = np.random.default_rng(3)
+    jobs = []
+    for i in range(4):
+        n, t = (900, 33, 2500, 300)[i], ("f16", "bf16")[i % 2]
+        k, v = (kv4.round_to(rng.standard_normal((n, 2, 64)), DT[t]) for _ in range(2))
+        pool, table, rows, pos, _ = _one_row(torch, thinfer, k, v, t, 16)
+        q = torch.from_numpy(rng.standard_normal((1, 1, 8, 64))).to(_tt(torch, t)).cuda()
+        tab, lens = _int(torch, table), _int(torch, [n])
+        jobs.append((pool, tab, rows, pos, _dev(torch, k, t), _dev(torch, v, t), q, lens, thinfer.op_kv4_attention(q, pool, tab, lens, 16)))
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        pool, tab, rows, pos, k, v, q, lens, want = jobs[i]
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for j in range(60):
+                    mine = torch.full_like(pool, 255)
+                    thinfer.op_kv4_append(mine, tab, k, v, rows, pos, 16)
+                    out = thinfer.op_kv4_attention(q, mine, tab, lens, 16)
+                    _, refused = thinfer.op_kv4_reserve(tab.clone(), lens, lens * 0, 1000 + 50 * i, 16)
+                    try:
+                        thinfer.op_kv4_attention(q, mine, tab, lens, 17 + i)
+                        wrong.append((i, j, "not refused"))
+                    except thinfer.ThinferError as e:
+                        if f"multiple of {(17 + i) * 72} bytes" not in str(e):
+                            wrong.append((i, j, str(e)))
+                    torch.cuda.current_stream().synchronize()
+                    if not (torch.equal(mine, pool) and torch.equal(out, want) and refused.item() == 0):
+                        wrong.append((i, j))
+        except Exception as e:  # noqa: BLE001  (told by the test)
+            wrong.append((i, repr(e)))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for x in threads:
+        x.start()
+    for x in threads:
+        x.join()
+    assert not wrong, wrong[:3]
