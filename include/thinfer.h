@@ -440,6 +440,65 @@ int thinfer_op_kv4_compact(void* pool, int32_t n_layers, int32_t n_pages, const 
                            int32_t n_kv_heads, int32_t head_dim, int32_t page_size, void* workspace,
                            size_t workspace_bytes, void* cuda_stream);
 
+/* ------------------------------------------------------------------------ *
+ * Weights in 4 bits, and several tokens out of one pass over them (no
+ * counterpart in the paper: a decode step is bound by its weights' bytes,
+ * Section 3.2.2; a quarter of them, and drafted tokens verified together, are
+ * what makes a step's tokens cheaper).  Context-free, as the operators above:
+ * device pointers, nothing allocated or kept, captured calls follow the tensors
+ * as they are at replay, several threads at once, empty calls refused, outputs
+ * must not overlap what the call reads unless it is said that they may.
+ * ------------------------------------------------------------------------ */
+
+/* Packed weights of a matrix [n_out][k] in groups of `group` columns (32, 64 or 128; k a multiple of 8, the last group may
+ * be shorter).  Per row and group: lo = min(0, smallest), hi = max(0, largest), scale = (hi - lo) / 15 rounded to the storage
+ * type, zero = -lo / scale and code = zero + w / scale, the quotients rounded to nearest, ties to even, and the results cut to 0 .. 15;
+ * a code is read as scale * (code - zero).  A group whose scale is 0 is read as zeros, one with a NaN or an infinity as NaN.
+ * Rows come in tiles of 16, columns in blocks of 128, the last ones padded with zero bytes; row 8i + g of a tile, column
+ * 32q + 8t + 4s + 2b + e of a block, P = 128 / group:
+ *   codes   [tile][block][q / 2][g][t][q % 2][s][e][b]   byte: code of row g (low four bits), of row 8 + g (high four bits)
+ *   scales  [tile][block][g][P][i]                       FP16
+ *   zeros   [tile][block][g][P]                          byte as for the codes
+ * one region behind the other; 16-byte aligned.  Weights that were quantised elsewhere to whole zero points may be laid out
+ * like that too. */
+int thinfer_w4_bytes(int32_t n_out, int32_t k, int32_t group, size_t* bytes);
+
+/* Quantises w FP16 [n_out][k], rows w_stride elements apart (a multiple of 8), into `packed`. */
+int thinfer_op_w4_quantize(const void* w, int64_t w_stride, void* packed, int32_t n_out, int32_t k, int32_t group, void* cuda_stream);
+
+/* Reads packed weights back as FP16 [n_out][k], rows w_stride elements apart (a multiple of 8): scale * (code - zero),
+ * rounded once (beyond the type's largest value that is infinity).  For prompts, whose products run on thinfer_op_linear. */
+int thinfer_op_w4_read(const void* packed, void* w, int64_t w_stride, int32_t n_out, int32_t k, int32_t group, void* cuda_stream);
+
+/* y[rows, n_out] = x[rows, k] * (packed weights)^T for 1 .. 64 rows: FP32 sums of exact products, group by group, FP16 out
+ * (out_fp32 == 0) or FP32 out.  x: rows x_stride elements apart (a multiple of 8), 16-byte aligned; y: rows y_stride
+ * elements apart.  The sums have to stay inside FP32; beyond it they come out as infinity or NaN.  Equal calls give equal
+ * bits. */
+int thinfer_op_w4_linear(const void* x, int64_t x_stride, const void* packed, void* y, int64_t y_stride, int32_t rows, int32_t n_out,
+                         int32_t k, int32_t group, int32_t out_fp32, void* cuda_stream);
+
+/* Probabilities of FP32 logits [rows][vocab], rows logit_stride elements apart: exp((l - max) / T) over their sum, FP32, rows
+ * prob_stride elements apart; probs may be the logits themselves (same stride).  temperature: FP32 [rows], NULL: 1 for
+ * all.  A row whose temperature is not positive (NaN too) gets 1 at the lowest index of its largest logit and 0 elsewhere.  A logit of -inf has
+ * probability 0; a row that has no other gives zeros; one with a NaN (or with +inf, where T > 0) gives NaN. */
+int thinfer_op_token_probs(const float* logits, int64_t logit_stride, const float* temperature, float* probs, int64_t prob_stride,
+                           int32_t rows, int32_t vocab, void* cuda_stream);
+
+/* Which drafted tokens stay, and the token behind them.  p FP32 [batch][n_drafts + 1][vocab]: the target's probabilities at
+ * the position of each draft and behind the last; q FP32 [batch][n_drafts][vocab]: those that the drafts were drawn from,
+ * NULL: the drafts are certain (drafted without probabilities); batch and row strides in elements, the values of a row
+ * contiguous.  drafts int32 [batch][n_drafts]; counts int32 [batch]: how many of them a request has (NULL: all; above
+ * n_drafts: all; negative: the request is padding, its outputs are left as they were); uniforms FP32 [batch][n_drafts + 1], in [0, 1).
+ * With count drafts, draft i stays if all before it do and uniforms[i] * q[i][draft] < p[i][draft].  At the first that does not,
+ * say a, one token is drawn from max(p[a] - q[a], 0) - from p[a] where that is 0 everywhere -, behind count drafts that all
+ * stay, from p[count]: the lowest v whose sum over the vocabulary up to v exceeds uniforms[n_drafts] times the whole sum, in FP64.
+ * tokens int32 [batch][n_drafts + 1]: the drafts that stay, the drawn token, then -1; accepted int32 [batch]: how many
+ * stay.  n_drafts = 0 draws from p alone.  A draft outside 0 .. vocab - 1 does not stay.  NaN and negative values of what is
+ * drawn from count as 0; where it is 0 everywhere the drawn token is -1. */
+int thinfer_op_verify_drafts(const float* p, int64_t p_batch_stride, int64_t p_row_stride, const float* q, int64_t q_batch_stride,
+                             int64_t q_row_stride, const int32_t* drafts, const float* uniforms, const int32_t* counts, int32_t* tokens,
+                             int32_t* accepted, int32_t batch, int32_t n_drafts, int32_t vocab, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -2,7 +2,6 @@
 // checks its arguments on the host, enqueues its kernels on the given stream and returns; no call allocates, waits or
 // keeps anything for the next.
 #include <cmath>
-#include <initializer_list>
 
 #include "kv4_attn.cuh"
 #include "kv4_cache.cuh"
@@ -92,44 +91,11 @@ int token_ctas(int64_t tokens, int chunks, int lanes, int waves) {
   return static_cast<int>(ctas < most ? ctas : most > least ? most : least);
 }
 
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + nb && y < x + na;
-}
-
 size_t pool_bytes(int32_t n_pages, int32_t n_kv, int32_t head_dim, int32_t page_size) {   // of one layer
   return static_cast<size_t>(n_pages) * n_kv * page_size * (head_dim + 8);
 }
 size_t rows_bytes(int64_t n, int64_t stride, int64_t row) { return static_cast<size_t>((n - 1) * stride + row) * 2; }   // from first to last element
 size_t table_bytes(int32_t rows, int32_t max_pages) { return static_cast<size_t>(rows) * max_pages * 4; }
-
-// n rows of wa (wb) bytes, sa (sb) bytes apart; with different strides any overlap of the whole ranges counts.
-bool rows_overlap(const void* a, int64_t sa, int64_t wa, const void* b, int64_t sb, int64_t wb, int64_t n) {
-  if (!overlap(a, static_cast<size_t>((n - 1) * sa + wa), b, static_cast<size_t>((n - 1) * sb + wb))) return false;
-  if (sa != sb || n == 1) return true;
-  const int64_t apart = static_cast<int64_t>(reinterpret_cast<uintptr_t>(a)) - static_cast<int64_t>(reinterpret_cast<uintptr_t>(b));
-  const int64_t at = (apart % sa + sa) % sa;   // where a's row begins behind the beginning of one of b's
-  return at < wb || at + wa > sa;
-}
-
-struct Span {
-  const void* at;
-  size_t bytes;
-};
-bool meet(std::initializer_list<Span> a, std::initializer_list<Span> b) {
-  for (const Span& x : a)
-    for (const Span& y : b)
-      if (overlap(x.at, x.bytes, y.at, y.bytes)) return true;
-  return false;
-}
-
-// n rows of `wide` bytes, `stride` bytes apart, and one block of memory, which may lie between them.
-bool rows_meet(const void* first, int64_t stride, int64_t wide, int64_t n, const Span& block) {
-  if (block.bytes == 0) return false;
-  const int64_t at = reinterpret_cast<intptr_t>(block.at) - reinterpret_cast<intptr_t>(first);
-  const int64_t i = at < wide ? 0 : (at - wide) / stride + 1;   // the first row that ends behind the block's beginning
-  return i < n && i * stride < at + static_cast<int64_t>(block.bytes);
-}
 
 // Blocks of d elements at i * ts + h * hs (i < n, h < heads; ts >= d): whether one of them shares an element with one of the
 // same blocks `apart` elements further on; own: the same ones, each against the others.
@@ -144,15 +110,6 @@ bool blocks_meet(bool own, int64_t apart, int64_t ts, int64_t hs, int64_t n, int
     }
   }
   return false;
-}
-
-// Opts a kernel in to its dynamic shared memory, small sizes too: what it may have without being asked depends on its static
-// shared memory.
-template <auto Kernel>
-int opt_in(size_t bytes) {
-  static SmemOptIn opt;
-  if (!opt.ensure(Kernel, static_cast<int>(bytes))) return op_fail(THINFER_ECUDA, "cannot reserve %zu bytes of shared memory", bytes);
-  return THINFER_OK;
 }
 
 int check_plan(int32_t rows, int32_t n_pages) {

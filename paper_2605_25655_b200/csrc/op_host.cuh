@@ -5,6 +5,7 @@
 
 #include <cstdarg>
 #include <cstdio>
+#include <initializer_list>
 
 #include "../../include/thinfer.h"
 #include "smem_opt_in.cuh"
@@ -64,5 +65,48 @@ int op_launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cuda
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
 inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+
+// n rows of wa (wb) bytes, sa (sb) bytes apart; with different strides any overlap of the whole ranges counts.
+inline bool rows_overlap(const void* a, int64_t sa, int64_t wa, const void* b, int64_t sb, int64_t wb, int64_t n) {
+  if (!overlap(a, static_cast<size_t>((n - 1) * sa + wa), b, static_cast<size_t>((n - 1) * sb + wb))) return false;
+  if (sa != sb || n == 1) return true;
+  const int64_t apart = static_cast<int64_t>(reinterpret_cast<uintptr_t>(a)) - static_cast<int64_t>(reinterpret_cast<uintptr_t>(b));
+  const int64_t at = (apart % sa + sa) % sa;   // where a's row begins behind the beginning of one of b's
+  return at < wb || at + wa > sa;
+}
+
+struct Span {
+  const void* at;
+  size_t bytes;
+};
+inline bool meet(std::initializer_list<Span> a, std::initializer_list<Span> b) {
+  for (const Span& x : a)
+    for (const Span& y : b)
+      if (overlap(x.at, x.bytes, y.at, y.bytes)) return true;
+  return false;
+}
+
+// n rows of `wide` bytes, `stride` bytes apart, and one block of memory, which may lie between them.
+inline bool rows_meet(const void* first, int64_t stride, int64_t wide, int64_t n, const Span& block) {
+  if (block.bytes == 0) return false;
+  const int64_t at = reinterpret_cast<intptr_t>(block.at) - reinterpret_cast<intptr_t>(first);
+  const int64_t i = at < wide ? 0 : (at - wide) / stride + 1;   // the first row that ends behind the block's beginning
+  return i < n && i * stride < at + static_cast<int64_t>(block.bytes);
+}
+
+// Opts a kernel in to its dynamic shared memory, small sizes too: what it may have without being asked depends on its static
+// shared memory.  Internal to each source file: a static of a function with external linkage is one object for the whole
+// process, also where it loads the builds of both storage types, whose kernels bear the same names.
+template <auto Kernel>
+static int opt_in(size_t bytes) {
+  static SmemOptIn opt;
+  if (!opt.ensure(Kernel, static_cast<int>(bytes))) return op_fail(THINFER_ECUDA, "cannot reserve %zu bytes of shared memory", bytes);
+  return THINFER_OK;
+}
 
 }  // namespace thinfer

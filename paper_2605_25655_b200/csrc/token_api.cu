@@ -1,0 +1,77 @@
+// C entry points (include/thinfer.h) of what chooses tokens: probabilities of logits, verification of drafts.  Every call
+// checks its arguments on the host, enqueues its kernel on the given stream and returns; no call allocates, waits or keeps
+// anything for the next.
+#include "op_host.cuh"
+#include "token_choice.cuh"
+
+using namespace thinfer;
+
+namespace {
+
+constexpr int64_t kFar = int64_t{1} << 50;   // elements: no product below leaves 64 bits
+
+bool stride_ok(int64_t stride, int64_t least, int64_t n) { return stride >= least && (n <= 1 || stride <= kFar / n); }
+
+}  // namespace
+
+extern "C" {
+
+int thinfer_op_token_probs(const float* logits, int64_t logit_stride, const float* temperature, float* probs, int64_t prob_stride,
+                           int32_t rows, int32_t vocab, void* cuda_stream) {
+  if (logits == nullptr || probs == nullptr || rows <= 0 || vocab <= 0) return op_fail(THINFER_EINVAL, "token_probs: NULL pointer, or a size that is not positive");
+  if (!stride_ok(logit_stride, vocab, rows) || !stride_ok(prob_stride, vocab, rows) || !aligned4(logits) || !aligned4(probs) || !aligned4(temperature))
+    return op_fail(THINFER_EINVAL, "token_probs: a pointer is not aligned, or a row stride is below vocab");
+  const int64_t wide = static_cast<int64_t>(vocab) * 4;
+  if ((probs != logits || prob_stride != logit_stride) && rows_overlap(probs, prob_stride * 4, wide, logits, logit_stride * 4, wide, rows))
+    return op_fail(THINFER_EINVAL, "token_probs: the output overlaps the logits without being them");
+  if (temperature != nullptr && rows_meet(probs, prob_stride * 4, wide, rows, {temperature, static_cast<size_t>(rows) * 4}))
+    return op_fail(THINFER_EINVAL, "token_probs: the output overlaps the temperatures");
+  TokenProbsArgs a{};
+  a.logits = logits;
+  a.out = probs;
+  a.temperature = temperature;
+  a.stride = logit_stride;
+  a.out_stride = prob_stride;
+  a.vocab = vocab;
+  return op_launch(token_probs_kernel, dim3(static_cast<unsigned>(rows)), dim3(512), 0, static_cast<cudaStream_t>(cuda_stream), a);
+}
+
+int thinfer_op_verify_drafts(const float* p, int64_t p_batch_stride, int64_t p_row_stride, const float* q, int64_t q_batch_stride,
+                             int64_t q_row_stride, const int32_t* drafts, const float* uniforms, const int32_t* counts, int32_t* tokens,
+                             int32_t* accepted, int32_t batch, int32_t n_drafts, int32_t vocab, void* cuda_stream) {
+  if (p == nullptr || uniforms == nullptr || tokens == nullptr || accepted == nullptr || (drafts == nullptr && n_drafts > 0))
+    return op_fail(THINFER_EINVAL, "verify_drafts: NULL pointer");
+  if (batch <= 0 || n_drafts < 0 || vocab <= 0) return op_fail(THINFER_EINVAL, "verify_drafts: batch or vocab is not positive, or n_drafts is negative");
+  if (n_drafts > 65535) return op_fail(THINFER_EUNSUPPORTED, "verify_drafts: %d drafts > 65535", n_drafts);
+  if (n_drafts == 0) q = nullptr;
+  const int64_t n = n_drafts, b = batch;
+  if (p_batch_stride < 0 || p_row_stride < 0 || p_batch_stride > kFar / b || p_row_stride > kFar / (n + 1) ||
+      (q != nullptr && (q_batch_stride < 0 || q_row_stride < 0 || q_batch_stride > kFar / b || q_row_stride > kFar / n)))
+    return op_fail(THINFER_EINVAL, "verify_drafts: a stride is negative, or beyond any memory");
+  for (const void* x : {static_cast<const void*>(p), static_cast<const void*>(q), static_cast<const void*>(drafts), static_cast<const void*>(uniforms),
+                        static_cast<const void*>(counts), static_cast<const void*>(tokens), static_cast<const void*>(accepted)})
+    if (!aligned4(x)) return op_fail(THINFER_EINVAL, "verify_drafts: a pointer is not 4-byte aligned");
+  auto all = [&](const void* x, int64_t sb, int64_t sr, int64_t r) { return Span{x, x ? static_cast<size_t>((b - 1) * sb + (r - 1) * sr + vocab) * 4 : 0}; };
+  const Span out{tokens, static_cast<size_t>(b * (n + 1)) * 4}, kept{accepted, static_cast<size_t>(b) * 4};
+  for (const Span& in : {all(p, p_batch_stride, p_row_stride, n + 1), all(q, q_batch_stride, q_row_stride, n), Span{drafts, static_cast<size_t>(b * n) * 4},
+                         Span{uniforms, static_cast<size_t>(b * (n + 1)) * 4}, Span{counts, counts ? static_cast<size_t>(b) * 4 : 0}})
+    if (in.bytes != 0 && meet({out, kept}, {in})) return op_fail(THINFER_EINVAL, "verify_drafts: an output overlaps an input");
+  if (meet({out}, {kept})) return op_fail(THINFER_EINVAL, "verify_drafts: tokens and accepted overlap");
+  VerifyDraftsArgs a{};
+  a.p = p;
+  a.q = q;
+  a.p_batch = p_batch_stride;
+  a.p_row = p_row_stride;
+  a.q_batch = q_batch_stride;
+  a.q_row = q_row_stride;
+  a.tokens = drafts;
+  a.counts = counts;
+  a.uniforms = uniforms;
+  a.out = tokens;
+  a.accepted = accepted;
+  a.drafts = n_drafts;
+  a.vocab = vocab;
+  return op_launch(verify_drafts_kernel, dim3(static_cast<unsigned>(batch)), dim3(512), 0, static_cast<cudaStream_t>(cuda_stream), a);
+}
+
+}  // extern "C"

@@ -1,4 +1,5 @@
-// Argument marshalling of the per-layer operators (per-head norm with rotation, 4-bit paged cache) for torch tensors:
+// Argument marshalling of the per-layer operators (per-head norm with rotation, 4-bit paged cache, 4-bit weights) and of
+// those that choose tokens, for torch tensors:
 // checks types, shapes and strides, allocates what the caller did not pass, and calls the C entry points of
 // include/thinfer.h on the tensors' device and its current stream.  No arithmetic happens here.
 //
@@ -31,6 +32,12 @@ struct Api {
   decltype(&thinfer_kv4_pages_workspace) pages_workspace = nullptr;
   decltype(&thinfer_op_kv4_fork) fork = nullptr;
   decltype(&thinfer_op_kv4_compact) compact = nullptr;
+  decltype(&thinfer_w4_bytes) w4_bytes = nullptr;
+  decltype(&thinfer_op_w4_quantize) w4_quantize = nullptr;
+  decltype(&thinfer_op_w4_read) w4_read = nullptr;
+  decltype(&thinfer_op_w4_linear) w4_linear = nullptr;
+  decltype(&thinfer_op_token_probs) token_probs = nullptr;
+  decltype(&thinfer_op_verify_drafts) verify_drafts = nullptr;
   decltype(&thinfer_last_error) last_error = nullptr;
 };
 Api g_api[2];   // FP16 build, BF16 build
@@ -336,6 +343,116 @@ PyObject* compact(PyObject* const* a) {
   return pack({table_out, live});
 }
 
+// Elements between the rows of [rows, columns] whose columns lie side by side; a stride of a single row says nothing.
+int64_t row_stride(const at::Tensor& t, const char* name, at::ScalarType type, const On& on) {
+  if (t.dim() != 2 || t.scalar_type() != type || t.device() != on.device)
+    refuse(std::string(name) + ": a " + c10::toString(type) + " tensor [rows, columns] on " + on.device.str() + ", not " + describe(t));
+  if (t.size(0) == 0 || t.size(1) == 0 || (t.size(1) != 1 && t.stride(1) != 1))
+    refuse(std::string(name) + ": the columns of a row must be contiguous, and there must be some");
+  return t.size(0) > 1 ? t.stride(0) : t.size(1);
+}
+
+void* packed_weights(const at::Tensor& t, const Api& api, int64_t n, int64_t k, int64_t group, const On& on) {
+  size_t bytes = 0;
+  check(api, api.w4_bytes(small(n, "n_out"), small(k, "k"), small(group, "group"), &bytes));
+  return plain(t, "packed", on, {static_cast<int64_t>(bytes)}, at::kByte);
+}
+
+// w, group, packed
+PyObject* w4_quantize(PyObject* const* a) {
+  const at::Tensor& w = tensor(a[0], "w");
+  const On on(w);
+  const Api& api = api_of(w.scalar_type());
+  const int64_t ws = row_stride(w, "w", w.scalar_type(), on), n = w.size(0), k = w.size(1), group = number(a[1], "group");
+  size_t bytes = 0;
+  check(api, api.w4_bytes(small(n, "n_out"), small(k, "k"), small(group, "group"), &bytes));
+  const at::Tensor packed = given_or(a[2], "packed", [&] { return on.empty({static_cast<int64_t>(bytes)}, at::kByte); });
+  call(api, api.w4_quantize, w.data_ptr(), ws, packed_weights(packed, api, n, k, group, on), small(n, "n_out"), small(k, "k"), small(group, "group"), on.stream);
+  return wrap(packed);
+}
+
+// packed, n_out, k, group, bf16 (truth value), out
+PyObject* w4_read(PyObject* const* a) {
+  const at::Tensor& packed = tensor(a[0], "packed");
+  const On on(packed);
+  const int64_t n = number(a[1], "n_out"), k = number(a[2], "k"), group = number(a[3], "group");
+  const at::ScalarType type = truth(a[4], "bf16") ? at::kBFloat16 : at::kHalf;
+  const Api& api = api_of(type);
+  const void* in = packed_weights(packed, api, n, k, group, on);
+  const at::Tensor out = given_or(a[5], "out", [&] { return on.empty({n, k}, type); });
+  const int64_t os = row_stride(out, "out", type, on);
+  if (out.size(0) != n || out.size(1) != k) refuse("out: [n_out, k]");
+  call(api, api.w4_read, in, out.data_ptr(), os, small(n, "n_out"), small(k, "k"), small(group, "group"), on.stream);
+  return wrap(out);
+}
+
+// x, packed, n_out, group, out_fp32, out
+PyObject* w4_linear(PyObject* const* a) {
+  const at::Tensor &x = tensor(a[0], "x"), &packed = tensor(a[1], "packed");
+  const On on(x);
+  const at::ScalarType type = x.scalar_type();
+  const Api& api = api_of(type);
+  const int64_t xs = row_stride(x, "x", type, on), rows = x.size(0), k = x.size(1), n = number(a[2], "n_out"), group = number(a[3], "group");
+  const void* weights = packed_weights(packed, api, n, k, group, on);
+  bool fp32 = truth(a[4], "out_fp32");
+  const at::Tensor out = given_or(a[5], "out", [&] { return on.empty({rows, n}, fp32 ? at::kFloat : type); });
+  if (a[5] != Py_None) fp32 = out.scalar_type() == at::kFloat;
+  const int64_t os = row_stride(out, "out", fp32 ? at::kFloat : type, on);
+  if (out.size(0) != rows || out.size(1) != n) refuse("out: [rows, n_out]");
+  call(api, api.w4_linear, x.data_ptr(), xs, weights, out.data_ptr(), os, small(rows, "rows"), small(n, "n_out"), small(k, "k"), small(group, "group"),
+                           fp32 ? 1 : 0, on.stream);
+  return wrap(out);
+}
+
+// logits, temperature, out
+PyObject* token_probs(PyObject* const* a) {
+  const at::Tensor& logits = tensor(a[0], "logits");
+  const On on(logits);
+  const int64_t ls = row_stride(logits, "logits", at::kFloat, on), rows = logits.size(0), vocab = logits.size(1);
+  const float* temperature = a[1] == Py_None ? nullptr : static_cast<const float*>(plain(tensor(a[1], "temperature"), "temperature", on, {rows}, at::kFloat));
+  const at::Tensor out = given_or(a[2], "out", [&] { return on.empty({rows, vocab}, at::kFloat); });
+  same_shape(out, logits, "out: the shape of the logits");
+  const int64_t os = row_stride(out, "out", at::kFloat, on);
+  call(g_api[0], g_api[0].token_probs, static_cast<const float*>(logits.data_ptr()), ls, temperature, static_cast<float*>(out.data_ptr()), os, small(rows, "rows"),
+                                       small(vocab, "vocab"), on.stream);
+  return wrap(out);
+}
+
+// [batch, rows, vocab] whose values of a row lie side by side
+const float* distributions(const at::Tensor& t, const char* name, int64_t batch, int64_t rows, int64_t vocab, const On& on) {
+  if (t.dim() != 3 || t.scalar_type() != at::kFloat || t.device() != on.device || t.size(0) != batch || t.size(1) != rows || t.size(2) != vocab ||
+      (vocab > 1 && t.stride(2) != 1))
+    refuse(std::string(name) + ": a Float tensor [" + std::to_string(batch) + ", " + std::to_string(rows) + ", " + std::to_string(vocab) +
+           "] with contiguous rows on " + on.device.str() + ", not " + describe(t));
+  return static_cast<const float*>(t.data_ptr());
+}
+
+// p, q, drafts, uniforms, counts, tokens, accepted
+PyObject* verify_drafts(PyObject* const* a) {
+  const at::Tensor &p = tensor(a[0], "p"), &drafts = tensor(a[2], "drafts"), &uniforms = tensor(a[3], "uniforms");
+  const On on(p);
+  if (p.dim() != 3 || p.numel() == 0) refuse("p: [batch, drafts + 1, vocab], with something in it");
+  const int64_t b = p.size(0), n = p.size(1) - 1, v = p.size(2);
+  const float *pp = distributions(p, "p", b, n + 1, v, on), *qp = nullptr;
+  int64_t qb = 0, qr = 0;
+  if (a[1] != Py_None && n > 0) {
+    const at::Tensor& q = tensor(a[1], "q");
+    qp = distributions(q, "q", b, n, v, on);
+    qb = b > 1 ? q.stride(0) : 0;
+    qr = n > 1 ? q.stride(1) : 0;
+  }
+  const int32_t* counts = a[4] == Py_None ? nullptr : static_cast<const int32_t*>(plain(tensor(a[4], "counts"), "counts", on, {b}));
+  const at::Tensor tokens = given_or(a[5], "tokens", [&] { return on.empty({b, n + 1}, at::kInt); });
+  const at::Tensor accepted = given_or(a[6], "accepted", [&] { return on.empty({b}, at::kInt); });
+  call(g_api[0], g_api[0].verify_drafts, pp, b > 1 ? p.stride(0) : 0, n > 0 ? p.stride(1) : 0, qp, qb, qr,
+                                         static_cast<const int32_t*>(plain(drafts, "drafts", on, {b, n})),
+                                         static_cast<const float*>(plain(uniforms, "uniforms", on, {b, n + 1}, at::kFloat)), counts,
+                                         static_cast<int32_t*>(plain(tokens, "tokens", on, {b, n + 1})),
+                                         static_cast<int32_t*>(plain(accepted, "accepted", on, {b})), small(b, "batch"), small(n, "drafts"),
+                                         small(v, "vocab"), on.stream);
+  return pack({tokens, accepted});
+}
+
 // No C++ exception passes this frame: a refusal becomes ThinferError(code, text), what torch throws becomes torch's error.
 template <PyObject* (*F)(PyObject* const*), Py_ssize_t N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -362,12 +479,13 @@ PyObject* bind(PyObject*, PyObject* args) {
   PyObject *error, *tables[2];
   if (!PyArg_ParseTuple(args, "OOO", &error, &tables[0], &tables[1])) return nullptr;
   for (int s = 0; s < 2; ++s) {
-    void* at[10];
-    if (PySequence_Size(tables[s]) != 10) {
-      PyErr_SetString(PyExc_TypeError, "ten addresses");
+    constexpr int kCount = 16;
+    void* at[kCount];
+    if (PySequence_Size(tables[s]) != kCount) {
+      PyErr_Format(PyExc_TypeError, "%d addresses", kCount);
       return nullptr;
     }
-    for (int i = 0; i < 10; ++i) {
+    for (int i = 0; i < kCount; ++i) {
       PyObject* o = PySequence_GetItem(tables[s], i);
       at[i] = o ? PyLong_AsVoidPtr(o) : nullptr;
       Py_XDECREF(o);
@@ -386,7 +504,13 @@ PyObject* bind(PyObject*, PyObject* args) {
     p.pages_workspace = reinterpret_cast<decltype(p.pages_workspace)>(at[6]);
     p.fork = reinterpret_cast<decltype(p.fork)>(at[7]);
     p.compact = reinterpret_cast<decltype(p.compact)>(at[8]);
-    p.last_error = reinterpret_cast<decltype(p.last_error)>(at[9]);
+    p.w4_bytes = reinterpret_cast<decltype(p.w4_bytes)>(at[9]);
+    p.w4_quantize = reinterpret_cast<decltype(p.w4_quantize)>(at[10]);
+    p.w4_read = reinterpret_cast<decltype(p.w4_read)>(at[11]);
+    p.w4_linear = reinterpret_cast<decltype(p.w4_linear)>(at[12]);
+    p.token_probs = reinterpret_cast<decltype(p.token_probs)>(at[13]);
+    p.verify_drafts = reinterpret_cast<decltype(p.verify_drafts)>(at[14]);
+    p.last_error = reinterpret_cast<decltype(p.last_error)>(at[15]);
   }
   Py_INCREF(error);
   Py_XDECREF(g_error);
@@ -396,7 +520,8 @@ PyObject* bind(PyObject*, PyObject* args) {
 
 #define ENTRY(f, n) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<f, n>)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {ENTRY(qk_norm_rope, 10), ENTRY(reserve, 7), ENTRY(append, 7), ENTRY(read, 9), ENTRY(attention, 7),
-                          ENTRY(fork, 9), ENTRY(compact, 7), {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                          ENTRY(fork, 9), ENTRY(compact, 7), ENTRY(w4_quantize, 3), ENTRY(w4_read, 6), ENTRY(w4_linear, 6),
+                          ENTRY(token_probs, 3), ENTRY(verify_drafts, 7), {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_ops", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

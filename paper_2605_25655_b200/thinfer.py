@@ -31,6 +31,8 @@ EXPORTS = (
     "thinfer_rope_turns", "thinfer_op_qk_norm_rope", "thinfer_kv4_page_bytes", "thinfer_op_kv4_reserve",
     "thinfer_op_kv4_append", "thinfer_op_kv4_read", "thinfer_kv4_attention_workspace", "thinfer_op_kv4_attention",
     "thinfer_kv4_pages_workspace", "thinfer_op_kv4_fork", "thinfer_op_kv4_compact",
+    "thinfer_w4_bytes", "thinfer_op_w4_quantize", "thinfer_op_w4_read", "thinfer_op_w4_linear", "thinfer_op_token_probs",
+    "thinfer_op_verify_drafts",
 )
 
 
@@ -126,6 +128,12 @@ def lib(storage="f16"):
     L.thinfer_kv4_pages_workspace.argtypes = [i32, i32, szp]
     L.thinfer_op_kv4_fork.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, C.c_size_t, vp]
     L.thinfer_op_kv4_compact.argtypes = [vp, i32, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, C.c_size_t, vp]
+    L.thinfer_w4_bytes.argtypes = [i32, i32, i32, szp]
+    L.thinfer_op_w4_quantize.argtypes = [vp, i64, vp, i32, i32, i32, vp]
+    L.thinfer_op_w4_read.argtypes = [vp, vp, i64, i32, i32, i32, vp]
+    L.thinfer_op_w4_linear.argtypes = [vp, i64, vp, vp, i64, i32, i32, i32, i32, i32, vp]
+    L.thinfer_op_token_probs.argtypes = [vp, i64, vp, vp, i64, i32, i32, vp]
+    L.thinfer_op_verify_drafts.argtypes = [vp, i64, i64, vp, i64, i64, vp, vp, vp, vp, vp, i32, i32, i32, vp]
     _libs[storage] = L
     return L
 
@@ -397,11 +405,12 @@ def op_argmax(logits, stream=None):
 
 
 # ------------------------------------- per-head norm + rotation, 4-bit paged cache
-# These run once per layer and decode step: their checks, allocations and calls are in csrc/torch_ops.cpp (_ops.so).
+# These, and the operators on 4-bit weights and drafted tokens, run once per layer or decode step: their checks, allocations and calls are in csrc/torch_ops.cpp (_ops.so).
 # A call with no tokens, rows or requests is refused: leave it out.
 _FAST_NAMES = ("thinfer_op_qk_norm_rope", "thinfer_op_kv4_reserve", "thinfer_op_kv4_append", "thinfer_op_kv4_read",
                "thinfer_kv4_attention_workspace", "thinfer_op_kv4_attention", "thinfer_kv4_pages_workspace", "thinfer_op_kv4_fork",
-               "thinfer_op_kv4_compact", "thinfer_last_error")
+               "thinfer_op_kv4_compact", "thinfer_w4_bytes", "thinfer_op_w4_quantize", "thinfer_op_w4_read", "thinfer_op_w4_linear",
+               "thinfer_op_token_probs", "thinfer_op_verify_drafts", "thinfer_last_error")
 _fast = None
 
 
@@ -517,6 +526,64 @@ def op_kv4_compact(pool, table, lens, page_size, head_dim, table_out=None, live=
         with _on(stream, pool):
             return op_kv4_compact(pool, table, lens, page_size, head_dim, table_out, live)
     return (_fast or _load_fast()).compact(pool, table, lens, page_size, head_dim, table_out, live)
+
+
+# ------------------------------------- weights in 4 bits, drafted tokens
+def w4_bytes(n_out, k, group):
+    """Bytes of packed 4-bit weights [n_out, k] with a scale and a zero point per row and `group` columns."""
+    n = C.c_size_t(0)
+    _check(lib().thinfer_w4_bytes(n_out, k, group, C.byref(n)))
+    return n.value
+
+
+def op_w4_quantize(w, group, packed=None, stream=None):
+    """Quantises w [n_out, k] (rows may be strided) to 4 bits; returns the packed weights, uint8 [w4_bytes(n_out, k, group)]."""
+    if stream is not None:
+        with _on(stream, w):
+            return op_w4_quantize(w, group, packed)
+    return (_fast or _load_fast()).w4_quantize(w, group, packed)
+
+
+def op_w4_read(packed, n_out, k, group, dtype, out=None, stream=None):
+    """The values of packed weights, [n_out, k] of `dtype` (the type that they were quantised from), e.g. for the products of
+    a prompt with op_linear."""
+    import torch
+    if stream is not None:
+        with _on(stream, packed):
+            return op_w4_read(packed, n_out, k, group, dtype, out)
+    if dtype is not torch.float16 and dtype is not torch.bfloat16:
+        raise ThinferError(EUNSUPPORTED, f"storage type {dtype}: the library is built for float16 and bfloat16")
+    return (_fast or _load_fast()).w4_read(packed, n_out, k, group, dtype is torch.bfloat16, out)
+
+
+def op_w4_linear(x, packed, n_out, group, out_fp32=False, out=None, stream=None):
+    """x [rows, k] (1 .. 64 rows, which may be strided) times packed weights: [rows, n_out], of x's type or FP32.  out: a
+    tensor of that shape whose rows may be strided; its type decides."""
+    if stream is not None:
+        with _on(stream, x):
+            return op_w4_linear(x, packed, n_out, group, out_fp32, out)
+    return (_fast or _load_fast()).w4_linear(x, packed, n_out, group, out_fp32, out)
+
+
+def op_token_probs(logits, temperature=None, out=None, stream=None):
+    """Probabilities of FP32 logits [rows, vocab]: softmax(logits / temperature), temperature FP32 [rows] (None: 1; a row's that
+    is not positive: all of it on the lowest index of the largest logit).  out: FP32 of that shape, may be the logits."""
+    if stream is not None:
+        with _on(stream, logits):
+            return op_token_probs(logits, temperature, out)
+    return (_fast or _load_fast()).token_probs(logits, temperature, out)
+
+
+def op_verify_drafts(p, q, drafts, uniforms, counts=None, tokens=None, accepted=None, stream=None):
+    """Which drafted tokens stay: p FP32 [batch, n + 1, vocab], the target's probabilities; q FP32 [batch, n, vocab], those the
+    drafts were drawn from (None: drafted without probabilities); drafts int32 [batch, n]; uniforms FP32 [batch, n + 1] in [0, 1),
+    the last for the token that is drawn; counts int32 [batch]: drafts of each request (None: n; negative: padding, its rows
+    of the outputs are not written).  Returns (tokens int32 [batch, n + 1]: the drafts that stay, the drawn token, -1 behind
+    it; accepted int32 [batch]: how many stay).  With n = 0 a sampler."""
+    if stream is not None:
+        with _on(stream, p):
+            return op_verify_drafts(p, q, drafts, uniforms, counts, tokens, accepted)
+    return (_fast or _load_fast()).verify_drafts(p, q, drafts, uniforms, counts, tokens, accepted)
 
 
 def to_device_layers(np_layers, device="cuda:0"):
