@@ -45,21 +45,30 @@ int op_sm_count();
 // the predecessor is still running and waits for it (pdl_wait) before it touches anything in memory.
 // Kernels launched this way read what earlier kernels may write with ordinary loads, never through the read-only path:
 // the data need not be final when the kernel starts.
+// cluster: CTAs of a thread-block cluster, side by side along x.
 template <typename... KArgs, typename... Args>
-int op_launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
+int op_launch_clusters(void (*kernel)(KArgs...), unsigned cluster, dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
   cudaLaunchConfig_t lc{};
   lc.gridDim = grid;
   lc.blockDim = block;
   lc.dynamicSmemBytes = smem;
   lc.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   lc.attrs = attr;
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  lc.numAttrs = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  lc.numAttrs = cluster > 1 ? 2 : 1;
   const cudaError_t e = cudaLaunchKernelEx(&lc, kernel, static_cast<KArgs>(args)...);
   if (e != cudaSuccess) return op_fail(THINFER_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
   return THINFER_OK;
+}
+
+template <typename... KArgs, typename... Args>
+int op_launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
+  return op_launch_clusters(kernel, 1, grid, block, smem, st, static_cast<Args&&>(args)...);
 }
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

@@ -1,5 +1,7 @@
 // C entry points (include/thinfer.h) of the weights in 4 bits with group scales.  Every call checks its arguments on the
 // host, enqueues its kernel on the given stream and returns; no call allocates, waits or keeps anything for the next.
+#include <atomic>
+
 #include "op_host.cuh"
 #include "w4_linear.cuh"
 #include "w4_weights.cuh"
@@ -29,10 +31,84 @@ unsigned unit_ctas(const W4View& v, int waves) {
   return static_cast<unsigned>(ctas < most ? ctas : most);
 }
 
+constexpr size_t kLinearSmem = 220 * 1024, kLinearTokens = 128 * 1024;   // of a CTA; of that for the tokens
+
+// How many clusters of 2^log2 CTAs, one CTA per SM, the current device runs at once (asked once per device).
+int active_clusters(int log2, int* count) {
+  static std::atomic<int> known[SmemOptIn::kMaxDevices][4];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return op_fail(THINFER_ECUDA, "no current device");
+  const bool keep = dev >= 0 && dev < SmemOptIn::kMaxDevices;
+  *count = keep ? known[dev][log2].load(std::memory_order_relaxed) : 0;
+  if (*count > 0) return THINFER_OK;
+  const int rc = opt_in<w4_linear_kernel<1, 1, 128>>(kLinearSmem);
+  if (rc != THINFER_OK) return rc;
+  cudaLaunchConfig_t lc{};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 1u << log2;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  lc.gridDim = dim3(static_cast<unsigned>(op_sm_count()) << log2);
+  lc.blockDim = dim3(kW4Warps * 32);
+  lc.dynamicSmemBytes = kLinearSmem;
+  lc.attrs = attr;
+  lc.numAttrs = 1;
+  const cudaError_t e = cudaOccupancyMaxActiveClusters(count, w4_linear_kernel<1, 1, 128>, &lc);
+  if (e != cudaSuccess) return op_fail(THINFER_ECUDA, "cannot ask for the number of clusters: %s", cudaGetErrorString(e));
+  if (*count < 1) *count = 1;
+  if (keep) known[dev][log2].store(*count, std::memory_order_relaxed);
+  return THINFER_OK;
+}
+
+struct LinearPlan {
+  int cluster, clusters, blocks_at_once, groups_at_once;
+  size_t smem;
+};
+
+// Cluster size by the bytes that the busiest CTA moves: weights, its share of the tokens (from L2, at half price), and what a
+// round of sums at the end costs in bytes that could have been read meanwhile.
+int plan_linear(int tiles, int blocks, int rows, int nt, int r, int token_tiles, LinearPlan* best) {
+  const int64_t groups = (tiles + r - 1) / r, per_block = static_cast<int64_t>(nt) * 2048, per_group = static_cast<int64_t>(r) * nt * 512;
+  int64_t least = INT64_MAX;
+  for (int log2 = 0; log2 <= 3; ++log2) {
+    const int64_t ctas = 1 << log2;
+    if (ctas > blocks) break;
+    int active = 0;
+    const int rc = active_clusters(log2, &active);
+    if (rc != THINFER_OK) return rc;
+    int64_t clusters = active / token_tiles;
+    clusters = clusters < 1 ? 1 : clusters > groups ? groups : clusters;
+    const int64_t slice = (blocks + ctas - 1) / ctas, most = kLinearTokens / per_block, phases = (slice + most - 1) / most, held = (slice + phases - 1) / phases;
+    const int64_t per = (groups + clusters - 1) / clusters, room = (static_cast<int64_t>(kLinearSmem) - held * per_block) / per_group - (kW4Warps - 1);
+    const int64_t batches = (per + room - 1) / room, batch = (per + batches - 1) / batches;
+    const int64_t cost = per * slice * r * 1064 + (phases > 1 ? batches : 1) * slice * (rows < 8 * nt ? rows : 8 * nt) * 128 + (batches - 1) * 40000 + log2 * 2000;
+    if (cost >= least) continue;
+    least = cost;
+    best->cluster = static_cast<int>(ctas);
+    best->clusters = static_cast<int>(clusters);
+    best->blocks_at_once = static_cast<int>(held);
+    best->groups_at_once = static_cast<int>(batch);
+    best->smem = static_cast<size_t>(held * per_block + (batch + kW4Warps - 1) * per_group);
+  }
+  return THINFER_OK;
+}
+
+template <int NT, int R, int G>
+int launch_linear(W4LinearArgs& a, cudaStream_t st) {
+  const int token_tiles = (a.rows + 8 * NT - 1) / (8 * NT);
+  LinearPlan p{};
+  int rc = plan_linear(static_cast<int>(a.v.tiles), static_cast<int>(a.v.blocks), a.rows, NT, R, token_tiles, &p);
+  if (rc == THINFER_OK) rc = opt_in<w4_linear_kernel<NT, R, G>>(kLinearSmem);
+  if (rc != THINFER_OK) return rc;
+  a.blocks_at_once = p.blocks_at_once;
+  a.groups_at_once = p.groups_at_once;
+  return op_launch_clusters(w4_linear_kernel<NT, R, G>, static_cast<unsigned>(p.cluster), dim3(static_cast<unsigned>(p.cluster * p.clusters), static_cast<unsigned>(token_tiles)),
+                            dim3(kW4Warps * 32), p.smem, st, a);
+}
 template <int G>
-int launch_linear(const W4LinearArgs& a, bool fp32, cudaStream_t st) {
-  const dim3 grid(static_cast<unsigned>((a.v.tiles + 3) / 4), static_cast<unsigned>((a.rows + 7) / 8));
-  return op_launch(fp32 ? w4_linear_kernel<G, true> : w4_linear_kernel<G, false>, grid, dim3(128), 0, st, a);
+int launch_linear(W4LinearArgs& a, cudaStream_t st) {
+  if (a.rows <= 8) return launch_linear<1, 1, G>(a, st);
+  return a.rows <= 16 ? launch_linear<2, 2, G>(a, st) : launch_linear<4, 2, G>(a, st);
 }
 
 }  // namespace
@@ -106,9 +182,10 @@ int thinfer_op_w4_linear(const void* x, int64_t x_stride, const void* packed, vo
   a.rows = rows;
   a.n = n_out;
   a.k = k;
+  a.fp32 = out_fp32;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (group == 128) return launch_linear<128>(a, out_fp32 != 0, st);
-  return group == 64 ? launch_linear<64>(a, out_fp32 != 0, st) : launch_linear<32>(a, out_fp32 != 0, st);
+  if (group == 128) return launch_linear<128>(a, st);
+  return group == 64 ? launch_linear<64>(a, st) : launch_linear<32>(a, st);
 }
 
 }  // extern "C"
