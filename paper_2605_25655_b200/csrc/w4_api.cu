@@ -31,7 +31,7 @@ unsigned unit_ctas(const W4View& v, int waves) {
   return static_cast<unsigned>(ctas < most ? ctas : most);
 }
 
-constexpr size_t kLinearSmem = 220 * 1024, kLinearTokens = 128 * 1024;   // of a CTA; of that for the tokens
+constexpr int64_t kLinearSmem = 226 * 1024, kLinearTokens = 96 * 1024;   // of a CTA; of that for the tokens, at most
 
 // How many clusters of 2^log2 CTAs, one CTA per SM, the current device runs at once (asked once per device).
 int active_clusters(int log2, int* count) {
@@ -41,7 +41,7 @@ int active_clusters(int log2, int* count) {
   const bool keep = dev >= 0 && dev < SmemOptIn::kMaxDevices;
   *count = keep ? known[dev][log2].load(std::memory_order_relaxed) : 0;
   if (*count > 0) return THINFER_OK;
-  const int rc = opt_in<w4_linear_kernel<1, 1, 128>>(kLinearSmem);
+  const int rc = opt_in<w4_linear_kernel<1, 2, 128>>(kLinearSmem);
   if (rc != THINFER_OK) return rc;
   cudaLaunchConfig_t lc{};
   cudaLaunchAttribute attr[1];
@@ -53,7 +53,7 @@ int active_clusters(int log2, int* count) {
   lc.dynamicSmemBytes = kLinearSmem;
   lc.attrs = attr;
   lc.numAttrs = 1;
-  const cudaError_t e = cudaOccupancyMaxActiveClusters(count, w4_linear_kernel<1, 1, 128>, &lc);
+  const cudaError_t e = cudaOccupancyMaxActiveClusters(count, w4_linear_kernel<1, 2, 128>, &lc);
   if (e != cudaSuccess) return op_fail(THINFER_ECUDA, "cannot ask for the number of clusters: %s", cudaGetErrorString(e));
   if (*count < 1) *count = 1;
   if (keep) known[dev][log2].store(*count, std::memory_order_relaxed);
@@ -67,8 +67,10 @@ struct LinearPlan {
 
 // Cluster size by the bytes that the busiest CTA moves: weights, its share of the tokens (from L2, at half price), and what a
 // round of sums at the end costs in bytes that could have been read meanwhile.
-int plan_linear(int tiles, int blocks, int rows, int nt, int r, int token_tiles, LinearPlan* best) {
+int plan_linear(int tiles, int blocks, int rows, int nt, int r, int stage, int token_tiles, LinearPlan* best) {
   const int64_t groups = (tiles + r - 1) / r, per_block = static_cast<int64_t>(nt) * 2048, per_group = static_cast<int64_t>(r) * nt * 512;
+  const int64_t ring = static_cast<int64_t>(kW4Warps) * (kW4Ahead + 1) * stage, left = kLinearSmem - ring - (kW4Warps + 7) * per_group;
+  const int64_t most = (left < kLinearTokens ? left : kLinearTokens) / per_block;   // blocks, beside slots for 8 row groups
   int64_t least = INT64_MAX;
   for (int log2 = 0; log2 <= 3; ++log2) {
     const int64_t ctas = 1 << log2;
@@ -78,8 +80,8 @@ int plan_linear(int tiles, int blocks, int rows, int nt, int r, int token_tiles,
     if (rc != THINFER_OK) return rc;
     int64_t clusters = active / token_tiles;
     clusters = clusters < 1 ? 1 : clusters > groups ? groups : clusters;
-    const int64_t slice = (blocks + ctas - 1) / ctas, most = kLinearTokens / per_block, phases = (slice + most - 1) / most, held = (slice + phases - 1) / phases;
-    const int64_t per = (groups + clusters - 1) / clusters, room = (static_cast<int64_t>(kLinearSmem) - held * per_block) / per_group - (kW4Warps - 1);
+    const int64_t slice = (blocks + ctas - 1) / ctas, phases = (slice + most - 1) / most, held = (slice + phases - 1) / phases;
+    const int64_t per = (groups + clusters - 1) / clusters, room = (kLinearSmem - ring - held * per_block) / per_group - (kW4Warps - 1);
     const int64_t batches = (per + room - 1) / room, batch = (per + batches - 1) / batches;
     const int64_t cost = per * slice * r * 1064 + (phases > 1 ? batches : 1) * slice * (rows < 8 * nt ? rows : 8 * nt) * 128 + (batches - 1) * 40000 + log2 * 2000;
     if (cost >= least) continue;
@@ -88,7 +90,7 @@ int plan_linear(int tiles, int blocks, int rows, int nt, int r, int token_tiles,
     best->clusters = static_cast<int>(clusters);
     best->blocks_at_once = static_cast<int>(held);
     best->groups_at_once = static_cast<int>(batch);
-    best->smem = static_cast<size_t>(held * per_block + (batch + kW4Warps - 1) * per_group);
+    best->smem = static_cast<size_t>(ring + held * per_block + (batch + kW4Warps - 1) * per_group);
   }
   return THINFER_OK;
 }
@@ -97,7 +99,7 @@ template <int NT, int R, int G>
 int launch_linear(W4LinearArgs& a, cudaStream_t st) {
   const int token_tiles = (a.rows + 8 * NT - 1) / (8 * NT);
   LinearPlan p{};
-  int rc = plan_linear(static_cast<int>(a.v.tiles), static_cast<int>(a.v.blocks), a.rows, NT, R, token_tiles, &p);
+  int rc = plan_linear(static_cast<int>(a.v.tiles), static_cast<int>(a.v.blocks), a.rows, NT, R, W4Stage<R, 128 / G>::kBytes, token_tiles, &p);
   if (rc == THINFER_OK) rc = opt_in<w4_linear_kernel<NT, R, G>>(kLinearSmem);
   if (rc != THINFER_OK) return rc;
   a.blocks_at_once = p.blocks_at_once;
@@ -107,8 +109,8 @@ int launch_linear(W4LinearArgs& a, cudaStream_t st) {
 }
 template <int G>
 int launch_linear(W4LinearArgs& a, cudaStream_t st) {
-  if (a.rows <= 8) return launch_linear<1, 1, G>(a, st);
-  return a.rows <= 16 ? launch_linear<2, 2, G>(a, st) : launch_linear<4, 2, G>(a, st);
+  if (a.rows <= 8) return launch_linear<1, 2, G>(a, st);
+  return a.rows <= 16 ? launch_linear<2, 2, G>(a, st) : launch_linear<4, 1, G>(a, st);
 }
 
 }  // namespace

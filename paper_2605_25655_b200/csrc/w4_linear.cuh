@@ -16,6 +16,7 @@
 namespace thinfer {
 
 constexpr int kW4Warps = 16;
+constexpr int kW4Ahead = 2;   // units that are on their way while one is multiplied
 
 struct W4LinearArgs {
   W4View v;
@@ -44,7 +45,7 @@ __device__ __forceinline__ float4 w4_cluster_load(uint32_t addr, uint32_t rank) 
   uint32_t at;
   float4 v;
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
-  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
   return v;
 }
 
@@ -64,16 +65,44 @@ __device__ __forceinline__ void w4_store(const W4LinearArgs& a, long long row, l
     static_cast<half_t*>(a.y)[row * a.y_stride + out] = f_to_h(v);
 }
 
-// The codes and parameters of one block of R tiles, as lane 4 g + t holds them: scale and zero of group t % P.
-template <int R>
-struct W4Unit {
-  uint4 codes[R][2];
-  uint32_t scale[R], zero[R];
+__device__ __forceinline__ void w4_mma_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {   // d = a * b
+  asm("mma.sync.aligned.m16n8k16.row.col.f32." THINFER_MMA_SYNC_TYPES ".f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+
+// Item i of the slots of row groups from `tile` on, group by group: rows g and 8 + g of a tile, tokens 2 t and 2 t + 1.
+__device__ __forceinline__ void w4_output(const W4LinearArgs& a, int i, int per_group, int nt, int tile, int first_token, int r, const float4& v) {
+  const int group = i / per_group, part = i - group * per_group;
+  const long long out = (static_cast<long long>(tile) + group * r + part / (nt * 32)) * 16 + part % 32 / 4;
+  const long long token = first_token + part / 32 % nt * 8 + part % 4 * 2;
+  w4_store(a, token, out, v.x);
+  w4_store(a, token + 1, out, v.y);
+  w4_store(a, token, out + 8, v.z);
+  w4_store(a, token + 1, out + 8, v.w);
+}
+
+// What a warp multiplies at a time: one block of R tiles, with their scales and zeros behind the codes.
+template <int R, int P>
+struct W4Stage {
+  static constexpr int kScales = R * 1024, kZeros = kScales + R * P * 32, kBytes = (kZeros + R * P * 8 + 15) / 16 * 16;
 };
 
+__device__ __forceinline__ void w4_copy16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void w4_copy8(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void w4_copies_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void w4_copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// sum += scale * (a block of R tiles times its tokens x).
 template <int NT, int R, int P>
-__device__ __forceinline__ void w4_multiply(const W4Unit<R>& unit, const uint4* x, float (&sum)[R][NT][4]) {
+__device__ __forceinline__ void w4_multiply(const uint8_t* stage, const uint4* x, float (&sum)[R][NT][4]) {
   const int lane = threadIdx.x & 31;
+  uint4 codes[R][2];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) codes[i][h] = reinterpret_cast<const uint4*>(stage)[i * 64 + h * 32 + lane];
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     W4Zero z[R];
@@ -81,11 +110,9 @@ __device__ __forceinline__ void w4_multiply(const W4Unit<R>& unit, const uint4* 
     float d[R][NT][4];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      const uint32_t s = P == 1 ? unit.scale[i] : __shfl_sync(0xffffffffu, unit.scale[i], (lane & 28) + p);
-      z[i] = w4_zero<true>(P == 1 ? unit.zero[i] : __shfl_sync(0xffffffffu, unit.zero[i], (lane & 28) + p));
-      scale[i] = h2_to_f2(*reinterpret_cast<const half2_t*>(&s));
-#pragma unroll
-      for (int j = 0; j < NT; ++j) d[i][j][0] = d[i][j][1] = d[i][j][2] = d[i][j][3] = 0.f;
+      const int at = (i * 8 + (lane >> 2)) * P + p;
+      z[i] = w4_zero<true>(stage[W4Stage<R, P>::kZeros + at]);
+      scale[i] = h2_to_f2(reinterpret_cast<const half2_t*>(stage + W4Stage<R, P>::kScales)[at]);
     }
 #pragma unroll
     for (int q = p * 4 / P; q < (p + 1) * 4 / P; ++q) {
@@ -95,10 +122,15 @@ __device__ __forceinline__ void w4_multiply(const W4Unit<R>& unit, const uint4* 
 #pragma unroll
       for (int i = 0; i < R; ++i) {
         uint32_t r[4];
-        w4_unpack<true>(q % 2 ? unit.codes[i][q / 2].z : unit.codes[i][q / 2].x, z[i], r);
+        w4_unpack<true>(q % 2 ? codes[i][q / 2].z : codes[i][q / 2].x, z[i], r);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) w4_mma(d[i][j], r, token[j].x, token[j].y);
-        w4_unpack<true>(q % 2 ? unit.codes[i][q / 2].w : unit.codes[i][q / 2].y, z[i], r);
+        for (int j = 0; j < NT; ++j) {
+          if (q == p * 4 / P)
+            w4_mma_first(d[i][j], r, token[j].x, token[j].y);
+          else
+            w4_mma(d[i][j], r, token[j].x, token[j].y);
+        }
+        w4_unpack<true>(q % 2 ? codes[i][q / 2].w : codes[i][q / 2].y, z[i], r);
 #pragma unroll
         for (int j = 0; j < NT; ++j) w4_mma(d[i][j], r, token[j].z, token[j].w);
       }
@@ -115,10 +147,79 @@ __device__ __forceinline__ void w4_multiply(const W4Unit<R>& unit, const uint4* 
   }
 }
 
+// The units of one warp on their way into its ring: one block of R tiles after the other along a row group, then the next
+// group's.  Every lane keeps the address of what it copies itself, so that a unit costs a few additions.
+template <int R, int P>
+struct W4Feed {
+  static constexpr int kPieces = 5 * P * R;       // of 8 bytes: 4 P of scales and P of zeros for each tile
+  const W4LinearArgs& a;
+  uint32_t ring, to;
+  int left, step, steps, here, block, tile;       // units, step of the group, steps of a group and how many of them exist, the first one's block
+  const uint8_t* codes;
+  const uint8_t* params[(kPieces + 31) / 32];
+  long long second;                               // from the first tile's codes to the second's
+
+  __device__ __forceinline__ void begin_group() {
+    const int lane = threadIdx.x & 31;
+    const long long blocks = a.v.blocks;
+    // behind the last tile the last one is read again; what comes of it is not kept
+    const int more = R > 1 && tile + 1 < a.v.tiles ? 1 : 0;
+    const long long at = tile * blocks + block;
+    codes = a.v.codes + at * 1024 + lane * 16;
+    second = more * blocks * 1024;
+#pragma unroll
+    for (int h = 0; h < (kPieces + 31) / 32; ++h) {
+      const int piece = lane + 32 * h, i = piece >= 5 * P ? 1 : 0, j = piece - i * 5 * P;
+      const long long mine = at + i * more * blocks;
+      params[h] = j < 4 * P ? a.v.scales + mine * (32 * P) + j * 8 : a.v.zeros + mine * (8 * P) + (j - 4 * P) * 8;
+    }
+  }
+  __device__ __forceinline__ W4Feed(const W4LinearArgs& args, uint32_t ring_, int u0, int u1, int steps_, int here_, int block_, int first_tile)
+      : a(args), ring(ring_), to(ring_), left(u1 - u0), step(u0 % steps_), steps(steps_), here(here_), block(block_), tile(first_tile + u0 / steps_ * R) {
+    begin_group();
+    codes += step * 1024;
+#pragma unroll
+    for (int h = 0; h < (kPieces + 31) / 32; ++h) params[h] += step * stride(h);
+  }
+  __device__ __forceinline__ static int stride(int h) {
+    const int piece = (threadIdx.x & 31) + 32 * h;
+    return (piece >= 5 * P ? piece - 5 * P : piece) < 4 * P ? 32 * P : 8 * P;
+  }
+  __device__ __forceinline__ void next() {
+    const int lane = threadIdx.x & 31;
+    if (left > 0) {
+      if (step < here) {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) w4_copy16(to + i * 1024 + h * 512 + lane * 16, codes + i * second + h * 512);
+#pragma unroll
+        for (int h = 0; h < (kPieces + 31) / 32; ++h) {
+          const int piece = lane + 32 * h, i = piece >= 5 * P ? 1 : 0, j = piece - i * 5 * P;
+          const int dst = j < 4 * P ? W4Stage<R, P>::kScales + i * P * 32 + j * 8 : W4Stage<R, P>::kZeros + i * P * 8 + (j - 4 * P) * 8;
+          if (piece < kPieces) w4_copy8(to + dst, params[h]);
+        }
+      }
+      --left;
+      if (++step == steps) {
+        step = 0;
+        tile += R;
+        if (left > 0) begin_group();
+      } else {
+        codes += 1024;
+#pragma unroll
+        for (int h = 0; h < (kPieces + 31) / 32; ++h) params[h] += stride(h);
+      }
+      to = to == ring + kW4Ahead * W4Stage<R, P>::kBytes ? ring : to + W4Stage<R, P>::kBytes;
+    }
+    w4_copies_done();
+  }
+};
+
 // NT: tiles of 8 tokens; R: tiles of 16 weight rows that a warp multiplies with what it reads of the tokens; G: columns of a group.
 template <int NT, int R, int G>
 __global__ void __launch_bounds__(kW4Warps * 32, 1) w4_linear_kernel(const __grid_constant__ W4LinearArgs a) {
-  constexpr int P = 128 / G, kAhead = R == 1 ? 4 : 2;
+  constexpr int P = 128 / G, kStage = W4Stage<R, P>::kBytes, kGroup = R * NT * 32;
   extern __shared__ uint4 smem[];
   pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -131,49 +232,20 @@ __global__ void __launch_bounds__(kW4Warps * 32, 1) w4_linear_kernel(const __gri
   const int slice = static_cast<int>(static_cast<long long>(blocks) * (rank + 1) / ctas) - block0;
   const long long groups = (tiles + R - 1) / R;
   const int group0 = static_cast<int>(groups * cluster / clusters), group1 = static_cast<int>(groups * (cluster + 1) / clusters);
-  uint4* x_s = smem;                                        // [block][q][token tile][lane]
-  uint4* slots = smem + a.blocks_at_once * (4 * NT * 32);   // [row group + warp][tile][token tile][lane]
   const int held = a.blocks_at_once;
-  const int at_p = lane / 4 * P + lane % P;                 // this lane's parameters of a block
+  uint4* x_s = smem;                                        // [block][q][token tile][lane]
+  uint4* slots = smem + held * (4 * NT * 32);               // [row group + warp][tile][token tile][lane]
+  const uint8_t* ring = reinterpret_cast<const uint8_t*>(slots + (a.groups_at_once + kW4Warps - 1) * kGroup) + warp * (kW4Ahead + 1) * kStage;
   pdl_wait();
 
   for (int from = group0; from < group1; from += a.groups_at_once) {
     const int batch = min(a.groups_at_once, group1 - from);
-    // a run of the (row group, block) units, block by block
+    // a run of the (row group, block) units
     const int units = batch * held, u0 = static_cast<int>(static_cast<long long>(units) * warp / kW4Warps), u1 = static_cast<int>(static_cast<long long>(units) * (warp + 1) / kW4Warps);
     for (int phase = 0; phase * held < slice || phase == 0; ++phase) {
       const int here = min(held, slice - phase * held);     // blocks of this phase; the rest of `held` is skipped
-      W4Unit<R> ring[kAhead];
-      int next_group = u0 / held, next_block = u0 - next_group * held, next = u0;
-      auto load = [&](W4Unit<R>& unit) {
-        if (next >= u1) return;
-        if (next_block < here) {
-#pragma unroll
-          for (int i = 0; i < R; ++i) {
-            const int tile = (from + next_group) * R + i;
-            if (R > 1 && tile >= tiles) {
-              unit.codes[i][0] = unit.codes[i][1] = make_uint4(0, 0, 0, 0);
-              unit.scale[i] = unit.zero[i] = 0;
-              continue;
-            }
-            const long long at = static_cast<long long>(tile) * blocks + block0 + phase * held + next_block;
-            const uint4* codes = reinterpret_cast<const uint4*>(a.v.codes) + at * 64 + lane;
-            unit.codes[i][0] = ld_stream(codes);
-            unit.codes[i][1] = ld_stream(codes + 32);
-            unit.scale[i] = reinterpret_cast<const uint32_t*>(a.v.scales)[at * (8 * P) + at_p];
-            unit.zero[i] = a.v.zeros[at * (8 * P) + at_p];
-          }
-        }
-        ++next;
-        if (++next_block == held) {
-          next_block = 0;
-          ++next_group;
-        }
-      };
-#pragma unroll
-      for (int d = 0; d < kAhead; ++d) load(ring[d]);
-      // the tokens of this slice's blocks
-      if (from == group0 || held < slice) {
+      const bool tokens = from == group0 || held < slice;   // to be fetched for this phase
+      if (tokens) {
         __syncthreads();                                    // nobody reads those of the phase before any more
         for (int i = tid; i < 8 * NT * 16 * here; i += kW4Warps * 32) {
           const int row = i / (16 * here), piece = i - row * (16 * here), col = (block0 + phase * held) * 128 + piece * 8;
@@ -182,60 +254,79 @@ __global__ void __launch_bounds__(kW4Warps * 32, 1) w4_linear_kernel(const __gri
           uint4* dst = x_s + ((piece >> 2) * NT + (row >> 3)) * 32 + (row & 7) * 4 + (piece & 3);
           asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
         }
-        asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
+        w4_copies_done();
+      }
+      W4Feed<R, P> feed(a, smem_u32(ring), u0, u1, held, here, block0 + phase * held, from * R);
+#pragma unroll
+      for (int d = 0; d < kW4Ahead; ++d) feed.next();
+      if (tokens) {
+        w4_copies_wait<kW4Ahead>();
         __syncthreads();
       }
       float sum[R][NT][4] = {};
-      int group = u0 / held, block = u0 - group * held;
-      for (int u = u0; u < u1; u += kAhead) {
+      int group = u0 / held, step = u0 - group * held;
+      const uint8_t* stage = ring;
+      for (int u = u0; u < u1; ++u) {
+        w4_copies_wait<kW4Ahead - 1>();
+        __syncwarp();                                       // all lanes' copies of this unit are there, and all have read the last one
+        feed.next();
+        if (step < here) w4_multiply<NT, R, P>(stage, x_s + step * (4 * NT * 32), sum);
+        stage = stage == ring + kW4Ahead * kStage ? ring : stage + kStage;
+        if (++step == held || u + 1 == u1) {                // the last unit of a row group, or of this warp
+          float4* slot = reinterpret_cast<float4*>(slots) + (group + warp) * kGroup + lane;
 #pragma unroll
-        for (int d = 0; d < kAhead; ++d) {
-          if (u + d < u1) {
-            if (block < here) w4_multiply<NT, R, P>(ring[d], x_s + block * (4 * NT * 32), sum);
-            load(ring[d]);
-            if (++block == held || u + d + 1 == u1) {       // the last unit of a row group, or of this warp
-              float4* slot = reinterpret_cast<float4*>(slots) + (group + warp) * (R * NT * 32) + lane;
+          for (int i = 0; i < R; ++i)
 #pragma unroll
-              for (int i = 0; i < R; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                  float4& to = slot[(i * NT + j) * 32];
-                  float4 v = make_float4(sum[i][j][0], sum[i][j][1], sum[i][j][2], sum[i][j][3]);
-                  if (phase > 0) v.x += to.x, v.y += to.y, v.z += to.z, v.w += to.w;
-                  to = v;
-                  sum[i][j][0] = sum[i][j][1] = sum[i][j][2] = sum[i][j][3] = 0.f;
-                }
-              if (block == held) {
-                block = 0;
-                ++group;
-              }
+            for (int j = 0; j < NT; ++j) {
+              float4& to = slot[(i * NT + j) * 32];
+              float4 v = make_float4(sum[i][j][0], sum[i][j][1], sum[i][j][2], sum[i][j][3]);
+              if (phase > 0) v.x += to.x, v.y += to.y, v.z += to.z, v.w += to.w;
+              to = v;
+              sum[i][j][0] = sum[i][j][1] = sum[i][j][2] = sum[i][j][3] = 0.f;
             }
-          }
+          step = 0;
+          ++group;
         }
       }
     }
-    // the cluster adds up what its CTAs' warps have for each row group
-    w4_cluster_sync();
-    const uint32_t slots_at = smem_u32(slots);
-    for (int i = rank * (kW4Warps * 32) + tid; i < batch * (R * NT * 32); i += ctas * (kW4Warps * 32)) {
-      const int group = i / (R * NT * 32), part = i - group * (R * NT * 32);
-      // warp w begins at unit w * units / 16: the ones that hold the group's first and last unit
-      const int w0 = (kW4Warps * (group * held + 1) - 1) / units, w1 = (kW4Warps * ((group + 1) * held) - 1) / units;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int c = 0; c < ctas; ++c)
-        for (int w = w0; w <= w1; ++w) {
-          if (w * units / kW4Warps == (w + 1) * units / kW4Warps) continue;   // it had none
-          const float4 p = w4_cluster_load(slots_at + static_cast<uint32_t>((group + w) * (R * NT * 32) + part) * 16, c);
-          v.x += p.x, v.y += p.y, v.z += p.z, v.w += p.w;
-        }
-      const long long out = (static_cast<long long>(from + group) * R + part / (NT * 32)) * 16 + part % 32 / 4;
-      const long long token = first_token + part / 32 % NT * 8 + part % 4 * 2;
-      w4_store(a, token, out, v.x);
-      w4_store(a, token + 1, out, v.y);
-      w4_store(a, token, out + 8, v.z);
-      w4_store(a, token + 1, out + 8, v.w);
+    __syncthreads();
+    // what the warps of this CTA have for each row group, in the order of the warps.  Warp w begins at unit w * units / 16: w0
+    // holds a group's first unit, w1 its last; the sum goes to w0's slot.
+    const int items = batch * kGroup;
+    for (int i = tid; i < items; i += kW4Warps * 32) {
+      const int group = i / kGroup, w0 = (kW4Warps * (group * held + 1) - 1) / units, w1 = (kW4Warps * ((group + 1) * held) - 1) / units;
+      float4* slot = reinterpret_cast<float4*>(slots) + w0 * kGroup + i;
+      float4 v = *slot;
+      for (int w = w0 + 1; w <= w1; ++w) {
+        if (w * units / kW4Warps == (w + 1) * units / kW4Warps) continue;   // it had none
+        const float4 p = slot[(w - w0) * kGroup];
+        v.x += p.x, v.y += p.y, v.z += p.z, v.w += p.w;
+      }
+      if (ctas == 1)
+        w4_output(a, i, kGroup, NT, from * R, first_token, R, v);
+      else
+        *slot = v;
     }
-    w4_cluster_sync();                                      // the slots are read, by the other CTAs too
+    if (ctas > 1) {
+      w4_cluster_sync();
+      const uint32_t slots_at = smem_u32(slots);
+      for (int i = rank * (kW4Warps * 32) + tid; i < items; i += ctas * (kW4Warps * 32)) {
+        const int w0 = (kW4Warps * (i / kGroup * held + 1) - 1) / units;
+        const uint32_t at = slots_at + static_cast<uint32_t>(w0 * kGroup + i) * 16;
+        float4 p[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+          if (c < ctas) p[c] = w4_cluster_load(at, c);
+        float4 v = p[0];
+#pragma unroll
+        for (int c = 1; c < 8; ++c)
+          if (c < ctas) v.x += p[c].x, v.y += p[c].y, v.z += p[c].z, v.w += p[c].w;
+        w4_output(a, i, kGroup, NT, from * R, first_token, R, v);
+      }
+      w4_cluster_sync();                                    // the slots are read, by the other CTAs too
+    } else {
+      __syncthreads();
+    }
   }
 }
 
