@@ -10,6 +10,23 @@ namespace {
 
 constexpr int64_t kFar = int64_t{1} << 50;   // elements: no product below leaves 64 bits
 
+// Clusters of CTAs for rows of `slots` 16-byte slots: as many CTAs as fill the device, at least as many as hold a row with
+// `most` slots a thread, at most 8.
+struct RowPlan {
+  unsigned ctas, threads;
+  int slots;   // a thread
+};
+RowPlan plan_rows(int64_t rows, int64_t slots, int most) {
+  RowPlan p{1, 512, 1};
+  const int64_t sms = op_sm_count();
+  while (p.ctas < 8 && (slots > static_cast<int64_t>(p.ctas) * 512 * most || (rows * p.ctas < sms && slots > p.ctas * 256))) p.ctas *= 2;
+  const int64_t slice = (slots + p.ctas - 1) / p.ctas;
+  while (p.slots < most && slice > 512 * static_cast<int64_t>(p.slots)) p.slots *= 2;
+  const int64_t each = (slice + p.slots - 1) / p.slots;
+  p.threads = each >= 512 ? 512 : static_cast<unsigned>((each + 31) / 32 * 32);
+  return p;
+}
+
 bool stride_ok(int64_t stride, int64_t least, int64_t n) { return stride >= least && (n <= 1 || stride <= kFar / n); }
 
 }  // namespace
@@ -33,7 +50,14 @@ int thinfer_op_token_probs(const float* logits, int64_t logit_stride, const floa
   a.stride = logit_stride;
   a.out_stride = prob_stride;
   a.vocab = vocab;
-  return op_launch(token_probs_kernel, dim3(static_cast<unsigned>(rows)), dim3(512), 0, static_cast<cudaStream_t>(cuda_stream), a);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const int64_t slots = (static_cast<int64_t>(vocab) + 6) / 4;   // wherever a row begins
+  if (slots > 8 * 512 * 16) return op_launch(token_probs_long_kernel, dim3(static_cast<unsigned>(rows)), dim3(512), 0, st, a);
+  const RowPlan plan = plan_rows(rows, slots, 16);
+  const int64_t ctas = static_cast<int64_t>(rows) * plan.ctas;
+  if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "token_probs: too many rows");
+  auto kernel = plan.slots == 1 ? token_probs_kernel<1> : plan.slots == 2 ? token_probs_kernel<2> : plan.slots == 4 ? token_probs_kernel<4> : plan.slots == 8 ? token_probs_kernel<8> : token_probs_kernel<16>;
+  return op_launch_clusters(kernel, plan.ctas, dim3(static_cast<unsigned>(ctas)), dim3(plan.threads), 0, st, a);
 }
 
 int thinfer_op_verify_drafts(const float* p, int64_t p_batch_stride, int64_t p_row_stride, const float* q, int64_t q_batch_stride,
@@ -71,7 +95,11 @@ int thinfer_op_verify_drafts(const float* p, int64_t p_batch_stride, int64_t p_r
   a.accepted = accepted;
   a.drafts = n_drafts;
   a.vocab = vocab;
-  return op_launch(verify_drafts_kernel, dim3(static_cast<unsigned>(batch)), dim3(512), 0, static_cast<cudaStream_t>(cuda_stream), a);
+  const RowPlan plan = plan_rows(batch, (static_cast<int64_t>(vocab) + 6) / 4, 8);
+  const int64_t ctas = static_cast<int64_t>(batch) * plan.ctas;
+  if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "verify_drafts: too many requests");
+  auto kernel = plan.slots == 1 ? verify_drafts_kernel<1> : plan.slots == 2 ? verify_drafts_kernel<2> : plan.slots == 4 ? verify_drafts_kernel<4> : verify_drafts_kernel<8>;
+  return op_launch_clusters(kernel, plan.ctas, dim3(static_cast<unsigned>(ctas)), dim3(plan.threads), 0, static_cast<cudaStream_t>(cuda_stream), a);
 }
 
 }  // extern "C"

@@ -35,6 +35,7 @@ struct Api {
   decltype(&thinfer_w4_bytes) w4_bytes = nullptr;
   decltype(&thinfer_op_w4_quantize) w4_quantize = nullptr;
   decltype(&thinfer_op_w4_read) w4_read = nullptr;
+  decltype(&thinfer_w4_linear_workspace) w4_linear_workspace = nullptr;
   decltype(&thinfer_op_w4_linear) w4_linear = nullptr;
   decltype(&thinfer_op_token_probs) token_probs = nullptr;
   decltype(&thinfer_op_verify_drafts) verify_drafts = nullptr;
@@ -386,7 +387,7 @@ PyObject* w4_read(PyObject* const* a) {
   return wrap(out);
 }
 
-// x, packed, n_out, group, out_fp32, out
+// x, packed, n_out, group, out_fp32, out, workspace
 PyObject* w4_linear(PyObject* const* a) {
   const at::Tensor &x = tensor(a[0], "x"), &packed = tensor(a[1], "packed");
   const On on(x);
@@ -399,8 +400,20 @@ PyObject* w4_linear(PyObject* const* a) {
   if (a[5] != Py_None) fp32 = out.scalar_type() == at::kFloat;
   const int64_t os = row_stride(out, "out", fp32 ? at::kFloat : type, on);
   if (out.size(0) != rows || out.size(1) != n) refuse("out: [rows, n_out]");
+  c10::DataPtr own;
+  void* ws = nullptr;
+  size_t ws_bytes = 0;
+  if (a[6] == Py_None) {
+    check(api, api.w4_linear_workspace(small(rows, "rows"), small(n, "n_out"), small(k, "k"), small(group, "group"), &ws_bytes));
+    if (ws_bytes > 0) own = on.scratch(ws_bytes);
+    ws = own.get();
+  } else {
+    const at::Tensor& given = tensor(a[6], "workspace");
+    ws_bytes = static_cast<size_t>(given.numel());
+    ws = plain(given, "workspace", on, {given.numel()}, at::kByte);
+  }
   call(api, api.w4_linear, x.data_ptr(), xs, weights, out.data_ptr(), os, small(rows, "rows"), small(n, "n_out"), small(k, "k"), small(group, "group"),
-                           fp32 ? 1 : 0, on.stream);
+                           fp32 ? 1 : 0, ws, ws_bytes, on.stream);
   return wrap(out);
 }
 
@@ -479,7 +492,7 @@ PyObject* bind(PyObject*, PyObject* args) {
   PyObject *error, *tables[2];
   if (!PyArg_ParseTuple(args, "OOO", &error, &tables[0], &tables[1])) return nullptr;
   for (int s = 0; s < 2; ++s) {
-    constexpr int kCount = 16;
+    constexpr int kCount = 17;
     void* at[kCount];
     if (PySequence_Size(tables[s]) != kCount) {
       PyErr_Format(PyExc_TypeError, "%d addresses", kCount);
@@ -507,10 +520,11 @@ PyObject* bind(PyObject*, PyObject* args) {
     p.w4_bytes = reinterpret_cast<decltype(p.w4_bytes)>(at[9]);
     p.w4_quantize = reinterpret_cast<decltype(p.w4_quantize)>(at[10]);
     p.w4_read = reinterpret_cast<decltype(p.w4_read)>(at[11]);
-    p.w4_linear = reinterpret_cast<decltype(p.w4_linear)>(at[12]);
-    p.token_probs = reinterpret_cast<decltype(p.token_probs)>(at[13]);
-    p.verify_drafts = reinterpret_cast<decltype(p.verify_drafts)>(at[14]);
-    p.last_error = reinterpret_cast<decltype(p.last_error)>(at[15]);
+    p.w4_linear_workspace = reinterpret_cast<decltype(p.w4_linear_workspace)>(at[12]);
+    p.w4_linear = reinterpret_cast<decltype(p.w4_linear)>(at[13]);
+    p.token_probs = reinterpret_cast<decltype(p.token_probs)>(at[14]);
+    p.verify_drafts = reinterpret_cast<decltype(p.verify_drafts)>(at[15]);
+    p.last_error = reinterpret_cast<decltype(p.last_error)>(at[16]);
   }
   Py_INCREF(error);
   Py_XDECREF(g_error);
@@ -520,7 +534,7 @@ PyObject* bind(PyObject*, PyObject* args) {
 
 #define ENTRY(f, n) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<f, n>)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {ENTRY(qk_norm_rope, 10), ENTRY(reserve, 7), ENTRY(append, 7), ENTRY(read, 9), ENTRY(attention, 7),
-                          ENTRY(fork, 9), ENTRY(compact, 7), ENTRY(w4_quantize, 3), ENTRY(w4_read, 6), ENTRY(w4_linear, 6),
+                          ENTRY(fork, 9), ENTRY(compact, 7), ENTRY(w4_quantize, 3), ENTRY(w4_read, 6), ENTRY(w4_linear, 7),
                           ENTRY(token_probs, 3), ENTRY(verify_drafts, 7), {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_ops", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

@@ -4,6 +4,7 @@
 
 #include "op_host.cuh"
 #include "w4_linear.cuh"
+#include "w4_linear_tc.cuh"
 #include "w4_weights.cuh"
 
 using namespace thinfer;
@@ -107,10 +108,49 @@ int launch_linear(W4LinearArgs& a, cudaStream_t st) {
   return op_launch_clusters(w4_linear_kernel<NT, R, G>, static_cast<unsigned>(p.cluster), dim3(static_cast<unsigned>(p.cluster * p.clusters), static_cast<unsigned>(token_tiles)),
                             dim3(kW4Warps * 32), p.smem, st, a);
 }
+// Rows beyond which the tensor-memory kernel takes over.
+#ifdef W4_DEV
+#include <cstdlib>
+int most_mma_rows() { return getenv("W4_MMA") ? atoi(getenv("W4_MMA")) : 16; }
+#else
+constexpr int most_mma_rows() { return 16; }
+#endif
+
+struct TcPlan {
+  long long row_tiles, units;
+  int ctas;
+  size_t part_bytes;
+};
+template <int N>
+TcPlan plan_tc(int64_t tiles, int64_t blocks) {
+  constexpr int W = w4_tc_groups<N>();
+  TcPlan p{};
+  p.row_tiles = (tiles + 8 * W - 1) / (8 * W);
+  p.units = p.row_tiles * blocks;
+  const int sms = op_sm_count();
+  p.ctas = p.units < sms ? static_cast<int>(p.units) : sms;
+  p.part_bytes = static_cast<size_t>(p.ctas) * 2 * N * W * 128 * 4;
+  return p;
+}
+TcPlan plan_tc_rows(int rows, int64_t tiles, int64_t blocks) { return rows <= 16 ? plan_tc<16>(tiles, blocks) : rows <= 32 ? plan_tc<32>(tiles, blocks) : plan_tc<64>(tiles, blocks); }
+
+size_t linear_workspace(int32_t rows, int32_t n_out, int32_t k) { return rows <= most_mma_rows() ? 0 : plan_tc_rows(rows, w4_tiles(n_out), w4_blocks(k)).part_bytes; }
+
+template <int N, int G>
+int launch_tc(const W4LinearArgs& a, void* workspace, cudaStream_t st) {
+  constexpr int P = 128 / G, kSmem = w4_tc_smem<N, P>(), kTile = w4_tc_groups<N>() * 128;
+  const TcPlan p = plan_tc<N>(a.v.tiles, a.v.blocks);
+  const W4TcArgs args{a, static_cast<float*>(workspace), p.row_tiles};
+  int rc = opt_in<w4_linear_tc_kernel<N, P>>(kSmem);
+  if (rc == THINFER_OK) rc = op_launch(w4_linear_tc_kernel<N, P>, dim3(static_cast<unsigned>(p.ctas)), dim3(w4_tc_groups<N>() * 128), kSmem, st, args);
+  if (rc != THINFER_OK || (p.units % p.ctas == 0 && p.units / p.ctas % a.v.blocks == 0)) return rc;   // every CTA has whole row tiles
+  return op_launch(w4_linear_join_kernel<N>, dim3(static_cast<unsigned>(p.row_tiles * kTile / 256 + (kTile % 256 != 0)), static_cast<unsigned>(a.rows)), dim3(256), 0, st, args, p.ctas);
+}
+
 template <int G>
-int launch_linear(W4LinearArgs& a, cudaStream_t st) {
-  if (a.rows <= 8) return launch_linear<1, 2, G>(a, st);
-  return a.rows <= 16 ? launch_linear<2, 2, G>(a, st) : launch_linear<4, 1, G>(a, st);
+int launch_linear(W4LinearArgs& a, void* workspace, cudaStream_t st) {
+  if (a.rows <= most_mma_rows()) return a.rows <= 8 ? launch_linear<1, 2, G>(a, st) : launch_linear<2, 2, G>(a, st);
+  return a.rows <= 16 ? launch_tc<16, G>(a, workspace, st) : a.rows <= 32 ? launch_tc<32, G>(a, workspace, st) : launch_tc<64, G>(a, workspace, st);
 }
 
 }  // namespace
@@ -161,8 +201,17 @@ int thinfer_op_w4_read(const void* packed, void* w, int64_t w_stride, int32_t n_
   return op_launch(kernel, dim3(unit_ctas(a.v, 4)), dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), a);
 }
 
+int thinfer_w4_linear_workspace(int32_t rows, int32_t n_out, int32_t k, int32_t group, size_t* bytes) {
+  const int rc = check_shape(n_out, k, group);
+  if (rc != THINFER_OK) return rc;
+  if (bytes == nullptr || rows <= 0) return op_fail(THINFER_EINVAL, "w4_linear: no rows, or bytes is NULL");
+  if (rows > kMaxRows) return op_fail(THINFER_EUNSUPPORTED, "w4_linear: %d rows > %d: read the weights back and multiply those", rows, kMaxRows);
+  *bytes = linear_workspace(rows, n_out, k);
+  return THINFER_OK;
+}
+
 int thinfer_op_w4_linear(const void* x, int64_t x_stride, const void* packed, void* y, int64_t y_stride, int32_t rows, int32_t n_out,
-                         int32_t k, int32_t group, int32_t out_fp32, void* cuda_stream) {
+                         int32_t k, int32_t group, int32_t out_fp32, void* workspace, size_t workspace_bytes, void* cuda_stream) {
   const int rc = check_shape(n_out, k, group);
   if (rc != THINFER_OK) return rc;
   if (x == nullptr || packed == nullptr || y == nullptr || rows <= 0) return op_fail(THINFER_EINVAL, "w4_linear: NULL pointer, or no rows");
@@ -175,6 +224,15 @@ int thinfer_op_w4_linear(const void* x, int64_t x_stride, const void* packed, vo
   if (rows_overlap(y, y_stride * size, n_out * size, x, x_stride * 2, static_cast<int64_t>(k) * 2, rows) ||
       rows_meet(y, y_stride * size, n_out * size, rows, {packed, w4_packed_bytes(n_out, k, group)}))
     return op_fail(THINFER_EINVAL, "w4_linear: the output overlaps an input");
+  const size_t need = linear_workspace(rows, n_out, k);
+  if (need > 0) {
+    if (workspace == nullptr || !aligned16(workspace)) return op_fail(THINFER_EINVAL, "w4_linear: the workspace is NULL or not 16-byte aligned");
+    if (workspace_bytes < need) return op_fail(THINFER_ECAPACITY, "w4_linear: the workspace has %zu bytes of %zu", workspace_bytes, need);
+    const Span ws{workspace, need};
+    if (rows_meet(y, y_stride * size, n_out * size, rows, ws) || rows_meet(x, x_stride * 2, static_cast<int64_t>(k) * 2, rows, ws) ||
+        meet({ws}, {{packed, w4_packed_bytes(n_out, k, group)}}))
+      return op_fail(THINFER_EINVAL, "w4_linear: the workspace overlaps another tensor");
+  }
   W4LinearArgs a{};
   a.v = w4_view(const_cast<void*>(packed), n_out, k, group);
   a.x = static_cast<const half_t*>(x);
@@ -186,8 +244,8 @@ int thinfer_op_w4_linear(const void* x, int64_t x_stride, const void* packed, vo
   a.k = k;
   a.fp32 = out_fp32;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (group == 128) return launch_linear<128>(a, st);
-  return group == 64 ? launch_linear<64>(a, st) : launch_linear<32>(a, st);
+  if (group == 128) return launch_linear<128>(a, workspace, st);
+  return group == 64 ? launch_linear<64>(a, workspace, st) : launch_linear<32>(a, workspace, st);
 }
 
 }  // extern "C"

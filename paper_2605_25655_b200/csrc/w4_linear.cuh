@@ -149,7 +149,7 @@ __device__ __forceinline__ void w4_multiply(const uint8_t* stage, const uint4* x
 
 // The units of one warp on their way into its ring: one block of R tiles after the other along a row group, then the next
 // group's.  Every lane keeps the address of what it copies itself, so that a unit costs a few additions.
-template <int R, int P>
+template <int R, int P, int Ahead, int TileStep>
 struct W4Feed {
   static constexpr int kPieces = 5 * P * R;       // of 8 bytes: 4 P of scales and P of zeros for each tile
   const W4LinearArgs& a;
@@ -163,8 +163,8 @@ struct W4Feed {
     const int lane = threadIdx.x & 31;
     const long long blocks = a.v.blocks;
     // behind the last tile the last one is read again; what comes of it is not kept
-    const int more = R > 1 && tile + 1 < a.v.tiles ? 1 : 0;
-    const long long at = tile * blocks + block;
+    const int last = static_cast<int>(a.v.tiles) - 1, more = R > 1 && tile < last ? 1 : 0;
+    const long long at = min(tile, last) * blocks + block;
     codes = a.v.codes + at * 1024 + lane * 16;
     second = more * blocks * 1024;
 #pragma unroll
@@ -175,7 +175,16 @@ struct W4Feed {
     }
   }
   __device__ __forceinline__ W4Feed(const W4LinearArgs& args, uint32_t ring_, int u0, int u1, int steps_, int here_, int block_, int first_tile)
-      : a(args), ring(ring_), to(ring_), left(u1 - u0), step(u0 % steps_), steps(steps_), here(here_), block(block_), tile(first_tile + u0 / steps_ * R) {
+      : a(args), ring(ring_), to(ring_), left(u1 - u0), step(u0 % steps_), steps(steps_), here(here_), block(block_), tile(first_tile + u0 / steps_ * TileStep) {
+    begin_group();
+    codes += step * 1024;
+#pragma unroll
+    for (int h = 0; h < (kPieces + 31) / 32; ++h) params[h] += step * stride(h);
+  }
+  // Goes to unit u of (row group, block) units whose first group begins at first_tile.
+  __device__ __forceinline__ void at(long long u, int blocks, int first_tile) {
+    step = static_cast<int>(u % blocks);
+    tile = first_tile + static_cast<int>(u / blocks) * TileStep;
     begin_group();
     codes += step * 1024;
 #pragma unroll
@@ -203,14 +212,14 @@ struct W4Feed {
       --left;
       if (++step == steps) {
         step = 0;
-        tile += R;
+        tile += TileStep;
         if (left > 0) begin_group();
       } else {
         codes += 1024;
 #pragma unroll
         for (int h = 0; h < (kPieces + 31) / 32; ++h) params[h] += stride(h);
       }
-      to = to == ring + kW4Ahead * W4Stage<R, P>::kBytes ? ring : to + W4Stage<R, P>::kBytes;
+      to = to == ring + Ahead * W4Stage<R, P>::kBytes ? ring : to + W4Stage<R, P>::kBytes;
     }
     w4_copies_done();
   }
@@ -256,7 +265,7 @@ __global__ void __launch_bounds__(kW4Warps * 32, 1) w4_linear_kernel(const __gri
         }
         w4_copies_done();
       }
-      W4Feed<R, P> feed(a, smem_u32(ring), u0, u1, held, here, block0 + phase * held, from * R);
+      W4Feed<R, P, kW4Ahead, R> feed(a, smem_u32(ring), u0, u1, held, here, block0 + phase * held, from * R);
 #pragma unroll
       for (int d = 0; d < kW4Ahead; ++d) feed.next();
       if (tokens) {

@@ -31,8 +31,8 @@ EXPORTS = (
     "thinfer_rope_turns", "thinfer_op_qk_norm_rope", "thinfer_kv4_page_bytes", "thinfer_op_kv4_reserve",
     "thinfer_op_kv4_append", "thinfer_op_kv4_read", "thinfer_kv4_attention_workspace", "thinfer_op_kv4_attention",
     "thinfer_kv4_pages_workspace", "thinfer_op_kv4_fork", "thinfer_op_kv4_compact",
-    "thinfer_w4_bytes", "thinfer_op_w4_quantize", "thinfer_op_w4_read", "thinfer_op_w4_linear", "thinfer_op_token_probs",
-    "thinfer_op_verify_drafts",
+    "thinfer_w4_bytes", "thinfer_op_w4_quantize", "thinfer_op_w4_read", "thinfer_w4_linear_workspace", "thinfer_op_w4_linear",
+    "thinfer_op_token_probs", "thinfer_op_verify_drafts",
 )
 
 
@@ -131,7 +131,8 @@ def lib(storage="f16"):
     L.thinfer_w4_bytes.argtypes = [i32, i32, i32, szp]
     L.thinfer_op_w4_quantize.argtypes = [vp, i64, vp, i32, i32, i32, vp]
     L.thinfer_op_w4_read.argtypes = [vp, vp, i64, i32, i32, i32, vp]
-    L.thinfer_op_w4_linear.argtypes = [vp, i64, vp, vp, i64, i32, i32, i32, i32, i32, vp]
+    L.thinfer_w4_linear_workspace.argtypes = [i32, i32, i32, i32, szp]
+    L.thinfer_op_w4_linear.argtypes = [vp, i64, vp, vp, i64, i32, i32, i32, i32, i32, vp, C.c_size_t, vp]
     L.thinfer_op_token_probs.argtypes = [vp, i64, vp, vp, i64, i32, i32, vp]
     L.thinfer_op_verify_drafts.argtypes = [vp, i64, i64, vp, i64, i64, vp, vp, vp, vp, vp, i32, i32, i32, vp]
     _libs[storage] = L
@@ -409,8 +410,8 @@ def op_argmax(logits, stream=None):
 # A call with no tokens, rows or requests is refused: leave it out.
 _FAST_NAMES = ("thinfer_op_qk_norm_rope", "thinfer_op_kv4_reserve", "thinfer_op_kv4_append", "thinfer_op_kv4_read",
                "thinfer_kv4_attention_workspace", "thinfer_op_kv4_attention", "thinfer_kv4_pages_workspace", "thinfer_op_kv4_fork",
-               "thinfer_op_kv4_compact", "thinfer_w4_bytes", "thinfer_op_w4_quantize", "thinfer_op_w4_read", "thinfer_op_w4_linear",
-               "thinfer_op_token_probs", "thinfer_op_verify_drafts", "thinfer_last_error")
+               "thinfer_op_kv4_compact", "thinfer_w4_bytes", "thinfer_op_w4_quantize", "thinfer_op_w4_read",
+               "thinfer_w4_linear_workspace", "thinfer_op_w4_linear", "thinfer_op_token_probs", "thinfer_op_verify_drafts", "thinfer_last_error")
 _fast = None
 
 
@@ -556,13 +557,14 @@ def op_w4_read(packed, n_out, k, group, dtype, out=None, stream=None):
     return (_fast or _load_fast()).w4_read(packed, n_out, k, group, dtype is torch.bfloat16, out)
 
 
-def op_w4_linear(x, packed, n_out, group, out_fp32=False, out=None, stream=None):
+def op_w4_linear(x, packed, n_out, group, out_fp32=False, out=None, workspace=None, stream=None):
     """x [rows, k] (1 .. 64 rows, which may be strided) times packed weights: [rows, n_out], of x's type or FP32.  out: a
-    tensor of that shape whose rows may be strided; its type decides."""
+    tensor of that shape whose rows may be strided; its type decides.  workspace: uint8, at least
+    thinfer_w4_linear_workspace bytes (default: allocated for the call)."""
     if stream is not None:
         with _on(stream, x):
-            return op_w4_linear(x, packed, n_out, group, out_fp32, out)
-    return (_fast or _load_fast()).w4_linear(x, packed, n_out, group, out_fp32, out)
+            return op_w4_linear(x, packed, n_out, group, out_fp32, out, workspace)
+    return (_fast or _load_fast()).w4_linear(x, packed, n_out, group, out_fp32, out, workspace)
 
 
 def op_token_probs(logits, temperature=None, out=None, stream=None):

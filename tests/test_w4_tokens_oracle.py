@@ -110,11 +110,24 @@ def test_weights_calls_refuse(lib):
 
 def test_linear_refuses(lib):
     n = thinfer.w4_bytes(40, 264, 64)
-    args = dict(x=A[0], xs=272, packed=A[1], y=A[2], ys=40, rows=5, n=40, k=264, group=64, fp32=0, st=None)
+    args = dict(x=A[0], xs=272, packed=A[1], y=A[2], ys=40, rows=5, n=40, k=264, group=64, fp32=0, ws=None, wb=0, st=None)
     _refused(lib.thinfer_op_w4_linear, args, SHAPES + [
         *(({x: None}, E) for x in ("x", "packed", "y")), ({"rows": 0}, E), ({"rows": -2}, E), ({"rows": 65}, U), ({"fp32": 2}, E), ({"x": A[0] + 8}, E),
         ({"packed": A[1] + 4}, E), ({"y": A[2] + 1}, E), ({"y": A[2] + 2, "fp32": 1}, E), ({"xs": 256}, E), ({"xs": 268}, E), ({"ys": 39}, E), ({"xs": 1 << 60}, E),
         ({"ys": 1 << 60}, E), ({"y": A[0]}, E), ({"y": A[0] + 4 * 272 * 2 + 526}, E), ({"y": A[1] + n - 2}, E), ({"y": A[1] - 4 * 80 - 78}, E), ({"y": A[0] + 520, "ys": 272}, E)])
+
+
+def test_linear_refuses_workspaces(lib):
+    need = C.c_size_t(0)
+    for bad, code in (((0, 40, 264, 64), E), ((65, 40, 264, 64), U), ((5, 0, 264, 64), E), ((5, 40, 264, 48), U)):
+        assert lib.thinfer_w4_linear_workspace(*bad, C.byref(need)) == code
+    assert lib.thinfer_w4_linear_workspace(5, 40, 264, 64, None) == E
+    assert lib.thinfer_w4_linear_workspace(64, 40, 264, 64, C.byref(need)) == thinfer.OK and need.value > 0
+    n = thinfer.w4_bytes(40, 264, 64)
+    args = dict(x=A[0], xs=272, packed=A[1], y=A[2], ys=40, rows=64, n=40, k=264, group=64, fp32=0, ws=A[3], wb=need.value, st=None)
+    _refused(lib.thinfer_op_w4_linear, args, [
+        ({"ws": None}, E), ({"ws": A[3] + 8}, E), ({"wb": need.value - 1}, thinfer.ECAPACITY), ({"wb": 0}, thinfer.ECAPACITY), ({"ws": A[0]}, E), ({"ws": A[1] + n - 16}, E),
+        ({"ws": A[2]}, E), ({"ws": A[1] - need.value + 16}, E), ({"y": A[3] + need.value - 2}, E), ({"x": A[3] + 16}, E)])
 
 
 def test_probs_refuses(lib):
