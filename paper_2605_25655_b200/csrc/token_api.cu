@@ -10,21 +10,28 @@ namespace {
 
 constexpr int64_t kFar = int64_t{1} << 50;   // elements: no product below leaves 64 bits
 
-// Clusters of CTAs for rows of `slots` 16-byte slots: as many CTAs as fill the device, at least as many as hold a row with
-// `most` slots a thread, at most 8.
+// Clusters of up to 8 CTAs for rows of `slots` 16-byte slots, with up to `most` slots a thread: as many CTAs as hold a row, and
+// as many as the device has room for (two on an SM) while a CTA has more than 256 slots.
 struct RowPlan {
   unsigned ctas, threads;
   int slots;   // a thread
 };
 RowPlan plan_rows(int64_t rows, int64_t slots, int most) {
   RowPlan p{1, 512, 1};
-  const int64_t sms = op_sm_count();
-  while (p.ctas < 8 && (slots > static_cast<int64_t>(p.ctas) * 512 * most || (rows * p.ctas < sms && slots > p.ctas * 256))) p.ctas *= 2;
+  const int64_t room = static_cast<int64_t>(op_sm_count()) * 2;
+  while (p.ctas < 8 && (slots > static_cast<int64_t>(p.ctas) * 512 * most || (rows * p.ctas * 2 <= room && slots > p.ctas * 256))) p.ctas *= 2;
   const int64_t slice = (slots + p.ctas - 1) / p.ctas;
   while (p.slots < most && slice > 512 * static_cast<int64_t>(p.slots)) p.slots *= 2;
   const int64_t each = (slice + p.slots - 1) / p.slots;
   p.threads = each >= 512 ? 512 : static_cast<unsigned>((each + 31) / 32 * 32);
   return p;
+}
+
+template <int E>
+int launch_verify(const VerifyDraftsArgs& a, const RowPlan& plan, unsigned ctas, cudaStream_t st) {
+  const size_t smem = static_cast<size_t>(E) * plan.threads * 8;
+  const int rc = opt_in<verify_drafts_kernel<E>>(smem);
+  return rc != THINFER_OK ? rc : op_launch_clusters(verify_drafts_kernel<E>, plan.ctas, dim3(ctas), dim3(plan.threads), smem, st, a);
 }
 
 bool stride_ok(int64_t stride, int64_t least, int64_t n) { return stride >= least && (n <= 1 || stride <= kFar / n); }
@@ -52,11 +59,11 @@ int thinfer_op_token_probs(const float* logits, int64_t logit_stride, const floa
   a.vocab = vocab;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const int64_t slots = (static_cast<int64_t>(vocab) + 6) / 4;   // wherever a row begins
-  if (slots > 8 * 512 * 16) return op_launch(token_probs_long_kernel, dim3(static_cast<unsigned>(rows)), dim3(512), 0, st, a);
-  const RowPlan plan = plan_rows(rows, slots, 16);
+  if (slots > 8 * 512 * 8) return op_launch(token_probs_long_kernel, dim3(static_cast<unsigned>(rows)), dim3(512), 0, st, a);
+  const RowPlan plan = plan_rows(rows, slots, 8);
   const int64_t ctas = static_cast<int64_t>(rows) * plan.ctas;
   if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "token_probs: too many rows");
-  auto kernel = plan.slots == 1 ? token_probs_kernel<1> : plan.slots == 2 ? token_probs_kernel<2> : plan.slots == 4 ? token_probs_kernel<4> : plan.slots == 8 ? token_probs_kernel<8> : token_probs_kernel<16>;
+  auto kernel = plan.slots == 1 ? token_probs_kernel<1> : plan.slots == 2 ? token_probs_kernel<2> : plan.slots == 4 ? token_probs_kernel<4> : token_probs_kernel<8>;
   return op_launch_clusters(kernel, plan.ctas, dim3(static_cast<unsigned>(ctas)), dim3(plan.threads), 0, st, a);
 }
 
@@ -95,11 +102,17 @@ int thinfer_op_verify_drafts(const float* p, int64_t p_batch_stride, int64_t p_r
   a.accepted = accepted;
   a.drafts = n_drafts;
   a.vocab = vocab;
-  const RowPlan plan = plan_rows(batch, (static_cast<int64_t>(vocab) + 6) / 4, 8);
-  const int64_t ctas = static_cast<int64_t>(batch) * plan.ctas;
-  if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "verify_drafts: too many requests");
-  auto kernel = plan.slots == 1 ? verify_drafts_kernel<1> : plan.slots == 2 ? verify_drafts_kernel<2> : plan.slots == 4 ? verify_drafts_kernel<4> : verify_drafts_kernel<8>;
-  return op_launch_clusters(kernel, plan.ctas, dim3(static_cast<unsigned>(ctas)), dim3(plan.threads), 0, static_cast<cudaStream_t>(cuda_stream), a);
+  const RowPlan plan = plan_rows(batch, (static_cast<int64_t>(vocab) + 6) / 4, 16);
+  if (static_cast<int64_t>(batch) * plan.ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "verify_drafts: too many requests");
+  const unsigned ctas = static_cast<unsigned>(batch) * plan.ctas;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  switch (plan.slots) {
+    case 1: return launch_verify<1>(a, plan, ctas, st);
+    case 2: return launch_verify<2>(a, plan, ctas, st);
+    case 4: return launch_verify<4>(a, plan, ctas, st);
+    case 8: return launch_verify<8>(a, plan, ctas, st);
+    default: return launch_verify<16>(a, plan, ctas, st);
+  }
 }
 
 }  // extern "C"

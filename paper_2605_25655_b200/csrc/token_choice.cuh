@@ -16,20 +16,31 @@ struct TokenProbsArgs {
 };
 
 // exp(d / T) for d <= 0, with log2(e) / T = high + low: what the product loses comes back as a factor, so that the exponent
-// of a far logit is as exact as d itself.
+// of a far logit is as exact as d itself.  Weights below 2^-126 are 0.
 struct TokenHeat {
   float high, low;
 };
 __device__ __forceinline__ TokenHeat token_heat(float temperature) {
-  const double by = 1.4426950408889634 / temperature;
-  const float high = fminf(static_cast<float>(by), 3e38f);
-  return {high, by < 3e38 ? static_cast<float>(by - high) : 0.f};
+  constexpr float kLog = 1.44269504088896f, kRest = 1.92596299e-8f;   // log2(e) and what FP32 leaves of it
+  const float high = kLog / temperature;
+  if (!(high <= 3e38f)) return {3e38f, 0.f};
+  if (high < 1e-30f) return {high, 0.f};   // an infinite temperature too
+  return {high, (fmaf(-high, temperature, kLog) + kRest) / temperature};
 }
 __device__ __forceinline__ float token_weight(float d, const TokenHeat& h) {
-  const float a = d * h.high;
-  if (!(a >= -160.f)) return 0.f;   // and -inf, whatever the temperature
-  const float rest = fmaf(d, h.high, -a) + d * h.low;
-  return exp2f(a) * fmaf(rest, 0.693147180559945f, 1.f);
+  const float a = d * h.high, rest = fmaf(d, h.low, fmaf(d, h.high, -a)) * 0.693147180559945f, w = ex2_approx(a);
+  return a >= -127.f ? fmaf(w, rest, w) : 0.f;   // 0 for -inf too, whatever the temperature, and for NaN
+}
+// The larger one; NaN where there is one.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 
 __device__ __forceinline__ uint32_t token_cluster(uint32_t* rank) {   // size of this CTA's cluster
@@ -51,26 +62,29 @@ __device__ __forceinline__ uint4 cluster_read(const void* shared, uint32_t rank)
 // A row as 16-byte slots of memory, whatever its alignment: slot s holds elements 4 s - before .. + 3; those outside the row
 // are not touched.
 struct TokenRow {
-  const float* at;    // of slot 0
-  int before, count;
-  long long slots;
+  const float* at;             // of slot 0
+  int before, count, slots;
+  int first_whole, wholes;     // slots that lie inside the row
   __device__ __forceinline__ TokenRow(const float* row, int n) {
     before = static_cast<int>(reinterpret_cast<uintptr_t>(row) >> 2) & 3;
     at = row - before;
     count = n;
-    slots = (static_cast<long long>(n) + before + 3) / 4;
+    slots = static_cast<int>((static_cast<unsigned>(n) + before + 3) / 4);
+    first_whole = before > 0 ? 1 : 0;
+    wholes = static_cast<int>((static_cast<unsigned>(n) + before) / 4) - first_whole;
   }
-  __device__ __forceinline__ bool whole(long long s) const { return 4 * s >= before && 4 * s + 4 - before <= count; }
-  __device__ __forceinline__ bool has(long long s, int i) const { return 4 * s + i >= before && 4 * s + i - before < count; }
-  __device__ __forceinline__ float4 load(long long s, float fill) const {
+  __device__ __forceinline__ bool whole(int s) const { return s - first_whole >= 0 && s - first_whole < wholes; }
+  __device__ __forceinline__ bool has(int s, int i) const { return (s > 0 || i >= before) && 4ll * s + i - before < count; }
+  // of a row whose memory has this one's alignment
+  __device__ __forceinline__ float4 load(const float* from, int s, float fill) const {
     if (whole(s)) {
-      const uint4 v = ld_stream(at + 4 * s);
+      const uint4 v = ld_stream(from + 4ll * s);
       return make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
     }
-    float f[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = has(s, i) ? at[4 * s + i] : fill;
-    return make_float4(f[0], f[1], f[2], f[3]);
+    return load_parts(from, s, fill);
+  }
+  __device__ __forceinline__ float4 load_parts(const float* from, int s, float fill) const {
+    return make_float4(has(s, 0) ? from[4ll * s] : fill, has(s, 1) ? from[4ll * s + 1] : fill, has(s, 2) ? from[4ll * s + 2] : fill, has(s, 3) ? from[4ll * s + 3] : fill);
   }
 };
 
@@ -78,46 +92,46 @@ struct TokenRow {
 // own largest logit, then the CTAs exchange (largest, sum) once, and the weights leave with one factor.  Bound by memory: each
 // logit is read once and each probability written once.
 template <int E>
-__global__ void __launch_bounds__(512) token_probs_kernel(const __grid_constant__ TokenProbsArgs a) {
+__global__ void __launch_bounds__(512, 2) token_probs_kernel(const __grid_constant__ TokenProbsArgs a) {
   __shared__ float s_top[16], s_sum[16];
-  __shared__ int s_nan, s_index;
-  __shared__ uint4 s_mine;          // largest, sum, its lowest index, whether there was a NaN
+  __shared__ int s_index;
+  __shared__ uint4 s_mine;          // largest (NaN where there is one), sum, its lowest index
   pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
   uint32_t rank;
   const uint32_t ctas = token_cluster(&rank);
   const long long which = blockIdx.x / ctas;
   const TokenRow row(a.logits + which * a.stride, a.vocab);
-  const long long slice = (row.slots + ctas - 1) / ctas, from = slice * rank, to = min(row.slots, from + slice);
-  if (tid == 0) s_nan = 0, s_index = INT_MAX;
+  const int slice = (row.slots + static_cast<int>(ctas) - 1) / static_cast<int>(ctas), from = slice * static_cast<int>(rank) + tid, to = min(row.slots, from - tid + slice);
+  const int threads = blockDim.x;
+  if (tid == 0) s_index = INT_MAX;
   pdl_wait();
   const float temp = a.temperature ? a.temperature[which] : 1.f;
   const bool greedy = !(temp > 0.f);
   float4 x[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const long long s = from + e * blockDim.x + tid;
-    x[e] = s < to ? row.load(s, -INFINITY) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    const int s = from + e * threads;
+    x[e] = s < to ? row.load(row.at, s, -INFINITY) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
   }
   float top = -INFINITY;
-  bool nan = false;
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    top = fmaxf(top, fmaxf(fmaxf(x[e].x, x[e].y), fmaxf(x[e].z, x[e].w)));
-    nan |= x[e].x != x[e].x || x[e].y != x[e].y || x[e].z != x[e].z || x[e].w != x[e].w;
-  }
-  top = warp_max(top);
+  for (int e = 0; e < E; ++e) top = max_nan(max_nan(top, x[e].x, x[e].y), x[e].z, x[e].w);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
   if (lane == 0) s_top[warp] = top;
   __syncthreads();
-  if (nan) s_nan = 1;
-  for (int w = 0; w < warps; ++w) top = fmaxf(top, s_top[w]);
+  top = lane < warps ? s_top[lane] : -INFINITY;
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+  top = __shfl_sync(0xffffffffu, top, 0);
   float sum = 0.f;
   const TokenHeat heat = token_heat(greedy ? 1.f : temp);
   if (greedy) {
     int index = INT_MAX;
 #pragma unroll
     for (int e = E - 1; e >= 0; --e) {
-      const int i = static_cast<int>(4 * (from + e * blockDim.x + tid)) - row.before;
+      const int i = 4 * (from + e * threads) - row.before;
       index = x[e].x == top ? i : x[e].y == top ? i + 1 : x[e].z == top ? i + 2 : x[e].w == top ? i + 3 : index;
     }
     index = __reduce_min_sync(0xffffffffu, index);
@@ -136,61 +150,55 @@ __global__ void __launch_bounds__(512) token_probs_kernel(const __grid_constant_
   }
   __syncthreads();
   if (!greedy) {
-    sum = 0.f;
-    for (int w = 0; w < warps; ++w) sum += s_sum[w];
+    sum = lane < warps ? s_sum[lane] : 0.f;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    sum = __shfl_sync(0xffffffffu, sum, 0);
   }
-  // all CTAs' (largest, sum)
   float all_top = top, all_sum = sum;
   int first = s_index;
-  bool bad = s_nan != 0;
-  if (ctas > 1) {
-    if (tid == 0) s_mine = make_uint4(__float_as_uint(top), __float_as_uint(sum), static_cast<uint32_t>(s_index), static_cast<uint32_t>(s_nan));
+  if (ctas > 1) {                   // lane c: what CTA c has
+    if (tid == 0) s_mine = make_uint4(__float_as_uint(top), __float_as_uint(sum), static_cast<uint32_t>(s_index), 0u);
     cluster_arrive();
     cluster_wait();
-    uint4 other[8];
+    uint4 other = make_uint4(__float_as_uint(-INFINITY), 0u, INT_MAX, 0u);
+    if (lane < static_cast<int>(ctas)) other = cluster_read(&s_mine, lane);
+    __syncwarp();
+    cluster_arrive();               // this warp has read; the CTA leaves when all have
+    const float its = __uint_as_float(other.x);
+    all_top = its;
 #pragma unroll
-    for (uint32_t c = 0; c < 8; ++c)
-      if (c < ctas) other[c] = cluster_read(&s_mine, c);
-    cluster_arrive();               // this CTA has read; it leaves when all have
-    all_top = -INFINITY;
+    for (int o = 4; o > 0; o >>= 1) all_top = max_nan(all_top, __shfl_xor_sync(0xffffffffu, all_top, o));
+    all_top = __shfl_sync(0xffffffffu, all_top, 0);
+    if (greedy) {
+      first = __reduce_min_sync(0xffffffffu, its == all_top ? static_cast<int>(other.z) : INT_MAX);
+    } else {
+      all_sum = __uint_as_float(other.y) * token_weight(its - all_top, heat);
 #pragma unroll
-    for (uint32_t c = 0; c < 8; ++c)
-      if (c < ctas) {
-        all_top = fmaxf(all_top, __uint_as_float(other[c].x));
-        bad |= other[c].w != 0;
-      }
-    all_sum = 0.f;
-    first = INT_MAX;
-#pragma unroll
-    for (uint32_t c = 0; c < 8; ++c)
-      if (c < ctas) {
-        const float its = __uint_as_float(other[c].x);
-        all_sum += __uint_as_float(other[c].y) * token_weight(its - all_top, heat);
-        if (its == all_top) first = min(first, static_cast<int>(other[c].z));
-      }
+      for (int o = 4; o > 0; o >>= 1) all_sum += __shfl_xor_sync(0xffffffffu, all_sum, o);
+      all_sum = __shfl_sync(0xffffffffu, all_sum, 0);
+    }
   }
-  bad |= !greedy && all_top == INFINITY;
+  const bool bad = all_top != all_top || (!greedy && all_top == INFINITY);
   const float by = bad ? __int_as_float(0x7fffffff) : all_top == -INFINITY ? 0.f : token_weight(top - all_top, heat) / all_sum;
   if (all_top == -INFINITY) first = INT_MAX;
   float* out = a.out + which * a.out_stride - row.before;
   const bool aligned = (reinterpret_cast<uintptr_t>(out) & 15) == 0;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const long long s = from + e * blockDim.x + tid;
+    const int s = from + e * threads;
     if (s >= to) continue;
-    float p[4] = {x[e].x * by, x[e].y * by, x[e].z * by, x[e].w * by};
+    float p[4] = {x[e].x * by, x[e].y * by, x[e].z * by, x[e].w * by};   // NaN where by is
     if (greedy) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) p[i] = bad ? by : 4 * s + i - row.before == first ? 1.f : 0.f;
-    } else if (bad) {
-      p[0] = p[1] = p[2] = p[3] = by;
     }
     if (aligned && row.whole(s)) {
-      *reinterpret_cast<float4*>(out + 4 * s) = make_float4(p[0], p[1], p[2], p[3]);
+      *reinterpret_cast<float4*>(out + 4ll * s) = make_float4(p[0], p[1], p[2], p[3]);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (row.has(s, i)) out[4 * s + i] = p[i];
+        if (row.has(s, i)) out[4ll * s + i] = p[i];
     }
   }
   if (ctas > 1) cluster_wait();
@@ -259,12 +267,14 @@ struct VerifyDraftsArgs {
 __device__ __forceinline__ double block_sum(double v, double* s_warp, int warps) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  const int lane = threadIdx.x & 31;
   __syncthreads();                  // the last sums have been read
-  if ((threadIdx.x & 31) == 0) s_warp[threadIdx.x >> 5] = v;
+  if (lane == 0) s_warp[threadIdx.x >> 5] = v;
   __syncthreads();
-  v = 0;
-  for (int w = 0; w < warps; ++w) v += s_warp[w];
-  return v;
+  v = lane < warps ? s_warp[lane] : 0.0;
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return __shfl_sync(0xffffffffu, v, 0);
 }
 
 // The first part whose sum, with those before it, exceeds the target - or, where rounding or the target leave none, the last one that
@@ -298,80 +308,94 @@ __device__ __forceinline__ int pick_lane(double sum, double before, double targe
   return over ? __ffs(over) - 1 : some ? 31 - __clz(some) : 0;
 }
 
-// A cluster per request.  Every CTA works out by itself how many drafts stay; then it holds a slice of what is drawn from in
-// registers, E slots of four values a thread (of a long vocabulary: round by round), and sums it up in FP64, so that
-// the drawn token does not depend on the order of the sums.  The CTAs exchange their sums, and the one that holds the target
-// looks for the token among its steps, warps, lanes and values.
+// A cluster per request.  Every CTA works out by itself how many drafts stay; then it sums up its slice of what is drawn from in
+// FP64, so that the drawn token does not depend on the order of the sums, and leaves every thread's sum of each step of
+// four values in shared memory (of a long vocabulary: of one round of E steps).  The CTAs exchange their sums, and the one
+// that holds the target looks for the token among its steps and warps, then lanes, and reads the last four values again.
 template <int E>
-__global__ void __launch_bounds__(512, 1) verify_drafts_kernel(const __grid_constant__ VerifyDraftsArgs a) {
-  __shared__ int s_kept, s_token;
+__global__ void __launch_bounds__(512, 2) verify_drafts_kernel(const __grid_constant__ VerifyDraftsArgs a) {
+  constexpr int kBatch = E < 4 ? E : 4;
+  extern __shared__ double s_step[];   // [E][threads]
+  __shared__ int s_token;
   __shared__ double s_warp[16], s_part[E * 16];
   __shared__ __align__(16) double s_mine[2];
   pdl_launch_dependents();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5, n = a.drafts;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5, n = a.drafts;
   uint32_t rank;
   const uint32_t ctas = token_cluster(&rank);
   const long long b = blockIdx.x / ctas;
-  pdl_wait();
-  int count = a.counts ? a.counts[b] : n;
-  if (count < 0) return;            // padding, for the whole cluster
-  count = min(count, n);
-  if (tid == 0) s_kept = count;
-  __syncthreads();
   const float *p = a.p + b * a.p_batch, *q = a.q ? a.q + b * a.q_batch : nullptr, *u = a.uniforms + b * (n + 1);
   const int32_t* drafted = a.tokens + b * n;
+  pdl_wait();
+  // every warp by itself: the first of its drafts that does not stay, 32 at a time
+  int count = a.counts ? a.counts[b] : n;
   const float draw = u[n];
-  for (int i = tid; i < count; i += blockDim.x) {
-    const int t = drafted[i];
-    bool stays = t >= 0 && t < a.vocab;
-    if (stays) stays = static_cast<double>(u[i]) * (q ? q[i * a.q_row + t] : 1.f) < static_cast<double>(p[i * a.p_row + t]);
-    if (!stays) atomicMin(&s_kept, i);
+  int kept = n;
+  for (int at = 0; at < n && kept == n; at += 32) {
+    const int i = at + lane, t = i < n ? drafted[i] : 0;
+    const float chance = i < n ? u[i] : 0.f;
+    bool goes = i >= count;
+    if (i < n && (t < 0 || t >= a.vocab))
+      goes = true;
+    else if (i < n)
+      goes = goes || !(static_cast<double>(chance) * (q ? q[i * a.q_row + t] : 1.f) < static_cast<double>(p[i * a.p_row + t]));
+    const unsigned gone = __ballot_sync(0xffffffffu, i < n && goes);
+    if (gone) kept = at + __ffs(gone) - 1;
   }
-  __syncthreads();
-  const int kept = s_kept;
+  if (count < 0) return;            // padding, for the whole cluster
+  count = min(count, n);
   const TokenRow row(p + kept * a.p_row, a.vocab);
-  bool less = kept < count;         // the draft's probabilities are taken off
-  const int gone = less && !q ? drafted[kept] : -1;
-  const float* off = less && q ? q + kept * a.q_row - row.before : nullptr;   // slots as those of the target
+  // what is taken off: the draft's probabilities, in slots as those of the target, or all of a certain draft
+  const float* off = kept < count && q ? q + kept * a.q_row - row.before : nullptr;
+  int gone = -1, gone_slot = -1;    // of the certain draft: its place in its slot
+  if (kept < count && !q && drafted[kept] >= 0 && drafted[kept] < a.vocab) {
+    const long long place = static_cast<long long>(drafted[kept]) + row.before;
+    gone_slot = static_cast<int>(place / 4);
+    gone = static_cast<int>(place % 4);
+  }
   const bool off_aligned = (reinterpret_cast<uintptr_t>(off) & 15) == 0;
-  const long long slice = (row.slots + ctas - 1) / ctas, from = min(row.slots, slice * rank), to = min(row.slots, from + slice);
-  const long long step = static_cast<long long>(E) * blockDim.x;
-  float4 x[E], y[E];
-  auto load = [&](long long at) {   // slots at + e * blockDim.x + tid
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const long long s = at + e * blockDim.x + tid;
-      x[e] = s < to ? row.load(s, 0.f) : make_float4(0.f, 0.f, 0.f, 0.f);
-      y[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (s >= to || !less) continue;
-      if (off && off_aligned && row.whole(s)) {
-        const uint4 v = ld_stream(off + 4 * s);
-        y[e] = make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
-      } else if (off) {
-        float f[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = row.has(s, i) ? off[4 * s + i] : 0.f;
-        y[e] = make_float4(f[0], f[1], f[2], f[3]);
-      } else {                      // a certain draft: all of it goes
-        const long long i = static_cast<long long>(gone) + row.before - 4 * s;
-        if (i >= 0 && i < 4) (i == 0 ? x[e].x : i == 1 ? x[e].y : i == 2 ? x[e].z : x[e].w) = 0.f;
-      }
+  const int slice = (row.slots + static_cast<int>(ctas) - 1) / static_cast<int>(ctas), from = min(static_cast<long long>(row.slots), static_cast<long long>(slice) * rank);
+  const int to = min(static_cast<long long>(row.slots), static_cast<long long>(from) + slice), step = E * threads;
+  // the four values of slot s, and what is taken off them
+  auto load = [&](int s, float4& x, float4& y) {
+    x = y = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (s >= to) return;
+    x = row.load(row.at, s, 0.f);
+    if (off) y = off_aligned ? row.load(off, s, 0.f) : row.load_parts(off, s, 0.f);
+    if (s == gone_slot) {
+      x.x = gone == 0 ? 0.f : x.x;
+      x.y = gone == 1 ? 0.f : x.y;
+      x.z = gone == 2 ? 0.f : x.z;
+      x.w = gone == 3 ? 0.f : x.w;
     }
   };
-  auto rest = [](float have, float off) {
-    const double r = static_cast<double>(have) - static_cast<double>(off);
-    return r > 0 ? r : 0.0;
+  // max(have - less, 0), 0 where one is NaN: an exact difference of FP32 numbers, unless their sizes are 2^29 apart
+  auto rest = [](float have, float less) {
+    const bool more = have > less;
+    return static_cast<double>(more ? have : 0.f) - static_cast<double>(more ? less : 0.f);
   };
-  auto sum_of = [&](int e) { return (rest(x[e].x, y[e].x) + rest(x[e].y, y[e].y)) + (rest(x[e].z, y[e].z) + rest(x[e].w, y[e].w)); };
+  // the steps of one round: this thread's sum
+  auto sum_round = [&](int at) {
+    double mine = 0;
+#pragma unroll
+    for (int e0 = 0; e0 < E; e0 += kBatch) {
+      float4 x[kBatch], y[kBatch];
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e) load(at + (e0 + e) * threads + tid, x[e], y[e]);
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e) {
+        const double v = (rest(x[e].x, y[e].x) + rest(x[e].y, y[e].y)) + (rest(x[e].z, y[e].z) + rest(x[e].w, y[e].w));
+        s_step[(e0 + e) * threads + tid] = v;
+        mine += v;
+      }
+    }
+    return mine;
+  };
   int token = -1;
   bool have = false;                // this CTA draws the token
   for (int again = 0; again < 2; ++again) {
     double mine = 0;
-    for (long long at = from; at < to; at += step) {
-      load(at);
-#pragma unroll
-      for (int e = 0; e < E; ++e) mine += sum_of(e);
-    }
+    for (int at = from; at < to; at += step) mine += sum_round(at);
     mine = block_sum(mine, s_warp, warps);
     Pick cta;
     double total = mine;
@@ -379,21 +403,21 @@ __global__ void __launch_bounds__(512, 1) verify_drafts_kernel(const __grid_cons
       if (tid == 0) s_mine[0] = mine;
       cluster_arrive();
       cluster_wait();
-      double sums[8];
+      double its = 0;               // lane c: of CTA c
+      if (lane < static_cast<int>(ctas)) {
+        const uint4 v = cluster_read(s_mine, lane);
+        its = __hiloint2double(static_cast<int>(v.y), static_cast<int>(v.x));
+      }
+      __syncwarp();
+      cluster_arrive();             // this warp has read; the CTA goes on when all have
+      total = its;
 #pragma unroll
-      for (uint32_t c = 0; c < 8; ++c)
-        if (c < ctas) {
-          const uint4 v = cluster_read(s_mine, c);
-          sums[c] = __hiloint2double(static_cast<int>(v.y), static_cast<int>(v.x));
-        }
-      cluster_arrive();
-      total = 0;
-#pragma unroll
-      for (uint32_t c = 0; c < 8; ++c)
-        if (c < ctas) total += sums[c];
-#pragma unroll
-      for (uint32_t c = 0; c < 8; ++c)
-        if (c < ctas) cta.part(static_cast<int>(c), sums[c], static_cast<double>(draw) * total);
+      for (int o = 4; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+      total = __shfl_sync(0xffffffffu, total, 0);
+      double upto = 0;
+      const int who = pick_lane(its, 0.0, static_cast<double>(draw) * total, &upto);
+      cta.picked = who;
+      cta.picked_before = __shfl_sync(0xffffffffu, upto, who);
     } else {
       cta.part(0, mine, static_cast<double>(draw) * total);
     }
@@ -402,31 +426,29 @@ __global__ void __launch_bounds__(512, 1) verify_drafts_kernel(const __grid_cons
       if (have) {
         const double target = static_cast<double>(draw) * total;
         double before = cta.picked_before;
-        long long at = from;
+        int at = from;
         if (from + step < to) {     // the round, read again
           Pick round;
           round.before = before;
-          for (long long r = from; r < to; r += step) {
-            load(r);
-            double s = 0;
-#pragma unroll
-            for (int e = 0; e < E; ++e) s += sum_of(e);
-            round.part(static_cast<int>((r - from) / step), block_sum(s, s_warp, warps), target);
-          }
+          for (int r = from; r < to; r += step) round.part((r - from) / step, block_sum(sum_round(r), s_warp, warps), target);
           at = from + round.picked * step;
           before = round.picked_before;
-          load(at);
-        }
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          double s = sum_of(e);
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-          if (lane == 0) s_part[e * warps + warp] = s;
+          sum_round(at);
         }
         if (tid == 0) s_token = -1;
+        double mine_of[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) mine_of[e] = s_step[e * threads + tid];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+          for (int e = 0; e < E; ++e) mine_of[e] += __shfl_xor_sync(0xffffffffu, mine_of[e], o);
+        if (lane == 0) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) s_part[e * warps + warp] = mine_of[e];
+        }
         __syncthreads();
-        // the step and warp, by every warp: E / 2 (or 1) of the E * 16 sums a lane
+        // the step and warp, by every warp
         constexpr int kEach = (E * 16 + 31) / 32;
         double some_of[kEach], sum = 0;
 #pragma unroll
@@ -442,19 +464,19 @@ __global__ void __launch_bounds__(512, 1) verify_drafts_kernel(const __grid_cons
         for (int i = 0; i < kEach; ++i) part.part(lane * kEach + i, some_of[i], target);
         const int picked = __shfl_sync(0xffffffffu, part.picked, who);
         before = __shfl_sync(0xffffffffu, part.picked_before, who);
-        if (picked % warps == warp) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            if (e != picked / warps) continue;
-            if (lane == pick_lane(sum_of(e), before, target, &upto)) {
-              Pick value;
-              value.before = upto;
-              value.part(0, rest(x[e].x, y[e].x), target);
-              value.part(1, rest(x[e].y, y[e].y), target);
-              value.part(2, rest(x[e].z, y[e].z), target);
-              value.part(3, rest(x[e].w, y[e].w), target);
-              s_token = static_cast<int>(4 * (at + e * static_cast<long long>(blockDim.x) + tid)) + value.picked - row.before;
-            }
+        if (picked >= 0 && picked % warps == warp) {
+          const int e = picked / warps;
+          if (lane == pick_lane(s_step[e * threads + tid], before, target, &upto)) {
+            const int s = at + e * threads + tid;
+            float4 x, y;
+            load(s, x, y);
+            Pick value;
+            value.before = upto;
+            value.part(0, rest(x.x, y.x), target);
+            value.part(1, rest(x.y, y.y), target);
+            value.part(2, rest(x.z, y.z), target);
+            value.part(3, rest(x.w, y.w), target);
+            s_token = 4 * s + value.picked - row.before;
           }
         }
         __syncthreads();
@@ -464,12 +486,13 @@ __global__ void __launch_bounds__(512, 1) verify_drafts_kernel(const __grid_cons
       have = rank == 0;             // nothing to draw from
     }
     if (ctas > 1) cluster_wait();
-    if (total > 0 || !less) break;
-    less = false;                   // the target has nothing that the draft has less of: drawn from the target
+    if (total > 0 || (off == nullptr && gone_slot < 0)) break;
+    off = nullptr;                  // the target has nothing that the draft has less of: drawn from the target
+    gone_slot = -1;
   }
   if (!have) return;
   if (tid == 0) a.accepted[b] = kept;
-  for (int i = tid; i <= n; i += blockDim.x) a.out[b * (n + 1) + i] = i < kept ? drafted[i] : i == kept ? token : -1;
+  for (int i = tid; i <= n; i += threads) a.out[b * (n + 1) + i] = i < kept ? drafted[i] : i == kept ? token : -1;
 }
 
 }  // namespace thinfer
