@@ -69,7 +69,7 @@ struct LinearPlan {
 // Cluster size by the bytes that the busiest CTA moves: weights, its share of the tokens (from L2, at half price), and what a
 // round of sums at the end costs in bytes that could have been read meanwhile.
 int plan_linear(int tiles, int blocks, int rows, int nt, int r, int stage, int token_tiles, LinearPlan* best) {
-  const int64_t groups = (tiles + r - 1) / r, per_block = static_cast<int64_t>(nt) * 2048, per_group = static_cast<int64_t>(r) * nt * 512;
+  const int64_t tokens = rows < 8 * nt ? rows : 8 * nt, groups = (tiles + r - 1) / r, per_block = tokens * 256, per_group = static_cast<int64_t>(r) * nt * 512;
   const int64_t ring = static_cast<int64_t>(kW4Warps) * (kW4Ahead + 1) * stage, left = kLinearSmem - ring - (kW4Warps + 7) * per_group;
   const int64_t most = (left < kLinearTokens ? left : kLinearTokens) / per_block;   // blocks, beside slots for 8 row groups
   int64_t least = INT64_MAX;
@@ -84,7 +84,7 @@ int plan_linear(int tiles, int blocks, int rows, int nt, int r, int stage, int t
     const int64_t slice = (blocks + ctas - 1) / ctas, phases = (slice + most - 1) / most, held = (slice + phases - 1) / phases;
     const int64_t per = (groups + clusters - 1) / clusters, room = (kLinearSmem - ring - held * per_block) / per_group - (kW4Warps - 1);
     const int64_t batches = (per + room - 1) / room, batch = (per + batches - 1) / batches;
-    const int64_t cost = per * slice * r * 1064 + (phases > 1 ? batches : 1) * slice * (rows < 8 * nt ? rows : 8 * nt) * 128 + (batches - 1) * 40000 + log2 * 2000;
+    const int64_t cost = per * slice * r * 1064 + (phases > 1 ? batches : 1) * slice * tokens * 128 + (batches * phases - 1) * 40000 + log2 * 2000;
     if (cost >= least) continue;
     least = cost;
     best->cluster = static_cast<int>(ctas);

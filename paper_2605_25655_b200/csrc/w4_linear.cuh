@@ -41,6 +41,9 @@ __device__ __forceinline__ uint32_t w4_cluster_size() {
 __device__ __forceinline__ void w4_cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// Release: what this warp has read of other CTAs' memory has been read, so that they may leave.
+__device__ __forceinline__ void w4_cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void w4_cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ float4 w4_cluster_load(uint32_t addr, uint32_t rank) {
   uint32_t at;
   float4 v;
@@ -71,11 +74,11 @@ __device__ __forceinline__ void w4_mma_first(float (&d)[4], const uint32_t (&a)[
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 
-// Item i of the slots of row groups from `tile` on, group by group: rows g and 8 + g of a tile, tokens 2 t and 2 t + 1.
-__device__ __forceinline__ void w4_output(const W4LinearArgs& a, int i, int per_group, int nt, int tile, int first_token, int r, const float4& v) {
-  const int group = i / per_group, part = i - group * per_group;
-  const long long out = (static_cast<long long>(tile) + group * r + part / (nt * 32)) * 16 + part % 32 / 4;
-  const long long token = first_token + part / 32 % nt * 8 + part % 4 * 2;
+// What lane 4 g + t has summed up: weight rows out + g and out + 8 + g, tokens token + 2 t, + 1.
+__device__ __forceinline__ void w4_output(const W4LinearArgs& a, long long out, int token, const float4& v) {
+  const int lane = threadIdx.x & 31;
+  out += lane >> 2;
+  token += 2 * (lane & 3);
   w4_store(a, token, out, v.x);
   w4_store(a, token + 1, out, v.y);
   w4_store(a, token, out + 8, v.z);
@@ -94,9 +97,10 @@ __device__ __forceinline__ void w4_copies_done() { asm volatile("cp.async.commit
 template <int N>
 __device__ __forceinline__ void w4_copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// sum += scale * (a block of R tiles times its tokens x).
+// sum += scale * (a block of R tiles times its tokens).  x[j]: where this lane finds its columns of token tile j; `quarter`
+// from one 32 columns to the next.
 template <int NT, int R, int P>
-__device__ __forceinline__ void w4_multiply(const uint8_t* stage, const uint4* x, float (&sum)[R][NT][4]) {
+__device__ __forceinline__ void w4_multiply(const uint8_t* stage, const uint4* const (&x)[NT], int quarter, float (&sum)[R][NT][4]) {
   const int lane = threadIdx.x & 31;
   uint4 codes[R][2];
 #pragma unroll
@@ -118,7 +122,7 @@ __device__ __forceinline__ void w4_multiply(const uint8_t* stage, const uint4* x
     for (int q = p * 4 / P; q < (p + 1) * 4 / P; ++q) {
       uint4 token[NT];
 #pragma unroll
-      for (int j = 0; j < NT; ++j) token[j] = x[(q * NT + j) * 32 + lane];
+      for (int j = 0; j < NT; ++j) token[j] = x[j][q * quarter];
 #pragma unroll
       for (int i = 0; i < R; ++i) {
         uint32_t r[4];
@@ -242,30 +246,36 @@ __global__ void __launch_bounds__(kW4Warps * 32, 1) w4_linear_kernel(const __gri
   const long long groups = (tiles + R - 1) / R;
   const int group0 = static_cast<int>(groups * cluster / clusters), group1 = static_cast<int>(groups * (cluster + 1) / clusters);
   const int held = a.blocks_at_once;
-  uint4* x_s = smem;                                        // [block][q][token tile][lane]
-  uint4* slots = smem + held * (4 * NT * 32);               // [row group + warp][tile][token tile][lane]
+  const int rows = min(8 * NT, a.rows - first_token);       // of the tokens
+  uint4* x_s = smem;                                        // [block][q][token][t]
+  uint4* slots = smem + held * (16 * rows);                 // [row group + warp][tile][token tile][lane]
   const uint8_t* ring = reinterpret_cast<const uint8_t*>(slots + (a.groups_at_once + kW4Warps - 1) * kGroup) + warp * (kW4Ahead + 1) * kStage;
-  pdl_wait();
+  bool waited = false;
 
   for (int from = group0; from < group1; from += a.groups_at_once) {
     const int batch = min(a.groups_at_once, group1 - from);
     // a run of the (row group, block) units
-    const int units = batch * held, u0 = static_cast<int>(static_cast<long long>(units) * warp / kW4Warps), u1 = static_cast<int>(static_cast<long long>(units) * (warp + 1) / kW4Warps);
+    const int units = batch * held, u0 = units * warp / kW4Warps, u1 = units * (warp + 1) / kW4Warps;
     for (int phase = 0; phase * held < slice || phase == 0; ++phase) {
       const int here = min(held, slice - phase * held);     // blocks of this phase; the rest of `held` is skipped
       const bool tokens = from == group0 || held < slice;   // to be fetched for this phase
+      W4Feed<R, P, kW4Ahead, R> feed(a, smem_u32(ring), u0, u1, held, here, block0 + phase * held, from * R);
+      if (!waited) pdl_wait();                              // behind the index arithmetic, which takes as long as a load
+      waited = true;
       if (tokens) {
         __syncthreads();                                    // nobody reads those of the phase before any more
-        for (int i = tid; i < 8 * NT * 16 * here; i += kW4Warps * 32) {
-          const int row = i / (16 * here), piece = i - row * (16 * here), col = (block0 + phase * held) * 128 + piece * 8;
-          const bool there = first_token + row < a.rows && col < a.k;
-          const half_t* src = there ? a.x + (first_token + row) * a.x_stride + col : a.x;
-          uint4* dst = x_s + ((piece >> 2) * NT + (row >> 3)) * 32 + (row & 7) * 4 + (piece & 3);
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
+        // the products of a token that is not there go nowhere: only what lies behind the last column has to be 0
+        const int col0 = (block0 + phase * held) * 128;
+        for (int piece = tid; piece < 16 * here; piece += kW4Warps * 32) {
+          const int col = col0 + piece * 8;
+          const half_t* src = a.x + first_token * a.x_stride + col;
+          uint32_t dst = smem_u32(x_s + (piece >> 2) * rows * 4 + (piece & 3));
+#pragma unroll 4
+          for (int row = 0; row < rows; ++row, dst += 64)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(col < a.k ? src + row * a.x_stride : a.x), "r"(col < a.k ? 16 : 0) : "memory");
         }
         w4_copies_done();
       }
-      W4Feed<R, P, kW4Ahead, R> feed(a, smem_u32(ring), u0, u1, held, here, block0 + phase * held, from * R);
 #pragma unroll
       for (int d = 0; d < kW4Ahead; ++d) feed.next();
       if (tokens) {
@@ -275,11 +285,16 @@ __global__ void __launch_bounds__(kW4Warps * 32, 1) w4_linear_kernel(const __gri
       float sum[R][NT][4] = {};
       int group = u0 / held, step = u0 - group * held;
       const uint8_t* stage = ring;
+      const uint4* x[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) x[j] = x_s + step * (16 * rows) + min(8 * j + (lane >> 2), rows - 1) * 4 + (lane & 3);
       for (int u = u0; u < u1; ++u) {
         w4_copies_wait<kW4Ahead - 1>();
         __syncwarp();                                       // all lanes' copies of this unit are there, and all have read the last one
         feed.next();
-        if (step < here) w4_multiply<NT, R, P>(stage, x_s + step * (4 * NT * 32), sum);
+        if (step < here) w4_multiply<NT, R, P>(stage, x, 4 * rows, sum);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) x[j] += 16 * rows;
         stage = stage == ring + kW4Ahead * kStage ? ring : stage + kStage;
         if (++step == held || u + 1 == u1) {                // the last unit of a row group, or of this warp
           float4* slot = reinterpret_cast<float4*>(slots) + (group + warp) * kGroup + lane;
@@ -293,46 +308,58 @@ __global__ void __launch_bounds__(kW4Warps * 32, 1) w4_linear_kernel(const __gri
               to = v;
               sum[i][j][0] = sum[i][j][1] = sum[i][j][2] = sum[i][j][3] = 0.f;
             }
+#pragma unroll
+          for (int j = 0; j < NT; ++j) x[j] -= step * (16 * rows);
           step = 0;
           ++group;
         }
       }
     }
     __syncthreads();
-    // what the warps of this CTA have for each row group, in the order of the warps.  Warp w begins at unit w * units / 16: w0
-    // holds a group's first unit, w1 its last; the sum goes to w0's slot.
-    const int items = batch * kGroup;
-    for (int i = tid; i < items; i += kW4Warps * 32) {
-      const int group = i / kGroup, w0 = (kW4Warps * (group * held + 1) - 1) / units, w1 = (kW4Warps * ((group + 1) * held) - 1) / units;
-      float4* slot = reinterpret_cast<float4*>(slots) + w0 * kGroup + i;
-      float4 v = *slot;
-      for (int w = w0 + 1; w <= w1; ++w) {
-        if (w * units / kW4Warps == (w + 1) * units / kW4Warps) continue;   // it had none
-        const float4 p = slot[(w - w0) * kGroup];
-        v.x += p.x, v.y += p.y, v.z += p.z, v.w += p.w;
+    // What the warps of this CTA have for each row group, in the order of the warps: w0 holds the group's first unit, w1 its
+    // last; the sum goes to w0's slot.  Warp w begins at unit w * units / 16.
+    auto warp_of = [&](int unit) { return __popc(__ballot_sync(0xffffffffu, lane < kW4Warps && units * lane / kW4Warps <= unit)) - 1; };
+    float4* slot = reinterpret_cast<float4*>(slots) + lane;
+    for (int g = warp; g < batch; g += kW4Warps) {
+      const int w0 = warp_of(g * held), w1 = warp_of((g + 1) * held - 1);
+      float4* to = slot + (g + w0) * kGroup;
+#pragma unroll
+      for (int i = 0; i < R * NT; ++i) {
+        float4 v = to[i * 32];
+        for (int w = w0 + 1; w <= w1; ++w) {
+          if (w * units / kW4Warps == (w + 1) * units / kW4Warps) continue;   // it had none
+          const float4 p = to[(w - w0) * kGroup + i * 32];
+          v.x += p.x, v.y += p.y, v.z += p.z, v.w += p.w;
+        }
+        if (ctas == 1)
+          w4_output(a, ((from + g) * R + i / NT) * 16ll, first_token + i % NT * 8, v);
+        else
+          to[i * 32] = v;
       }
-      if (ctas == 1)
-        w4_output(a, i, kGroup, NT, from * R, first_token, R, v);
-      else
-        *slot = v;
     }
     if (ctas > 1) {
       w4_cluster_sync();
-      const uint32_t slots_at = smem_u32(slots);
-      for (int i = rank * (kW4Warps * 32) + tid; i < items; i += ctas * (kW4Warps * 32)) {
-        const int w0 = (kW4Warps * (i / kGroup * held + 1) - 1) / units;
-        const uint32_t at = slots_at + static_cast<uint32_t>(w0 * kGroup + i) * 16;
-        float4 p[8];
+      for (int g = rank * kW4Warps + warp; g < batch; g += ctas * kW4Warps) {
+        const int w0 = warp_of(g * held);
+        const uint32_t at = smem_u32(slot + (g + w0) * kGroup);
+        float4 v[R * NT];
 #pragma unroll
-        for (int c = 0; c < 8; ++c)
-          if (c < ctas) p[c] = w4_cluster_load(at, c);
-        float4 v = p[0];
+        for (int i = 0; i < R * NT; ++i) {
+          float4 p[8];
 #pragma unroll
-        for (int c = 1; c < 8; ++c)
-          if (c < ctas) v.x += p[c].x, v.y += p[c].y, v.z += p[c].z, v.w += p[c].w;
-        w4_output(a, i, kGroup, NT, from * R, first_token, R, v);
+          for (int c = 0; c < 8; ++c)
+            if (c < ctas) p[c] = w4_cluster_load(at + i * 512, c);
+          v[i] = p[0];
+#pragma unroll
+          for (int c = 1; c < 8; ++c)
+            if (c < ctas) v[i].x += p[c].x, v[i].y += p[c].y, v[i].z += p[c].z, v[i].w += p[c].w;
+        }
+        if (g + ctas * kW4Warps >= batch) w4_cluster_arrive();   // this warp's last read, ahead of its last stores
+#pragma unroll
+        for (int i = 0; i < R * NT; ++i) w4_output(a, ((from + g) * R + i / NT) * 16ll, first_token + i % NT * 8, v[i]);
       }
-      w4_cluster_sync();                                    // the slots are read, by the other CTAs too
+      if (rank * kW4Warps + warp >= batch) w4_cluster_arrive();  // it had nothing to read
+      w4_cluster_wait();                                    // the slots are read, by the other CTAs too
     } else {
       __syncthreads();
     }
