@@ -1,5 +1,6 @@
 // Host helpers of the context-free operators that live outside thinfer_api.cu: error text, launch, device queries.
 #pragma once
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -40,6 +41,9 @@ struct SmemOptIn {
 
 // SM count of the current device (asked once per device).
 int op_sm_count();
+
+// Tensor map of 32-bit words [d2][d1][d0], rows of d0 side by side, boxes [box2][1][d0], nothing swizzled, 0 outside.
+bool op_tensor_map(CUtensorMap* map, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint32_t box2);
 
 // One launch, chained to its predecessor in the stream by programmatic dependent launch: the kernel may be scheduled while
 // the predecessor is still running and waits for it (pdl_wait) before it touches anything in memory.

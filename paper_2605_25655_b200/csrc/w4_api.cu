@@ -42,7 +42,7 @@ int active_clusters(int log2, int* count) {
   const bool keep = dev >= 0 && dev < SmemOptIn::kMaxDevices;
   *count = keep ? known[dev][log2].load(std::memory_order_relaxed) : 0;
   if (*count > 0) return THINFER_OK;
-  const int rc = opt_in<w4_linear_kernel<1, 2, 128>>(kLinearSmem);
+  const int rc = opt_in<w4_linear_kernel<1, 2, 128, 16>>(kLinearSmem);
   if (rc != THINFER_OK) return rc;
   cudaLaunchConfig_t lc{};
   cudaLaunchAttribute attr[1];
@@ -50,11 +50,11 @@ int active_clusters(int log2, int* count) {
   attr[0].val.clusterDim.x = 1u << log2;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   lc.gridDim = dim3(static_cast<unsigned>(op_sm_count()) << log2);
-  lc.blockDim = dim3(kW4Warps * 32);
+  lc.blockDim = dim3(512);
   lc.dynamicSmemBytes = kLinearSmem;
   lc.attrs = attr;
   lc.numAttrs = 1;
-  const cudaError_t e = cudaOccupancyMaxActiveClusters(count, w4_linear_kernel<1, 2, 128>, &lc);
+  const cudaError_t e = cudaOccupancyMaxActiveClusters(count, w4_linear_kernel<1, 2, 128, 16>, &lc);
   if (e != cudaSuccess) return op_fail(THINFER_ECUDA, "cannot ask for the number of clusters: %s", cudaGetErrorString(e));
   if (*count < 1) *count = 1;
   if (keep) known[dev][log2].store(*count, std::memory_order_relaxed);
@@ -68,9 +68,9 @@ struct LinearPlan {
 
 // Cluster size by the bytes that the busiest CTA moves: weights, its share of the tokens (from L2, at half price), and what a
 // round of sums at the end costs in bytes that could have been read meanwhile.
-int plan_linear(int tiles, int blocks, int rows, int nt, int r, int stage, int token_tiles, LinearPlan* best) {
+int plan_linear(int tiles, int blocks, int rows, int nt, int r, int warps, int stage, int token_tiles, LinearPlan* best) {
   const int64_t tokens = rows < 8 * nt ? rows : 8 * nt, groups = (tiles + r - 1) / r, per_block = tokens * 256, per_group = static_cast<int64_t>(r) * nt * 512;
-  const int64_t ring = static_cast<int64_t>(kW4Warps) * (kW4Ahead + 1) * stage, left = kLinearSmem - ring - (kW4Warps + 7) * per_group;
+  const int64_t ring = static_cast<int64_t>(warps) * (kW4Ahead + 1) * stage, left = kLinearSmem - ring - (warps + 7) * per_group;
   const int64_t most = (left < kLinearTokens ? left : kLinearTokens) / per_block;   // blocks, beside slots for 8 row groups
   int64_t least = INT64_MAX;
   for (int log2 = 0; log2 <= 3; ++log2) {
@@ -82,7 +82,7 @@ int plan_linear(int tiles, int blocks, int rows, int nt, int r, int stage, int t
     int64_t clusters = active / token_tiles;
     clusters = clusters < 1 ? 1 : clusters > groups ? groups : clusters;
     const int64_t slice = (blocks + ctas - 1) / ctas, phases = (slice + most - 1) / most, held = (slice + phases - 1) / phases;
-    const int64_t per = (groups + clusters - 1) / clusters, room = (kLinearSmem - ring - held * per_block) / per_group - (kW4Warps - 1);
+    const int64_t per = (groups + clusters - 1) / clusters, room = (kLinearSmem - ring - held * per_block) / per_group - (warps - 1);
     const int64_t batches = (per + room - 1) / room, batch = (per + batches - 1) / batches;
     const int64_t cost = per * slice * r * 1064 + (phases > 1 ? batches : 1) * slice * tokens * 128 + (batches * phases - 1) * 40000 + log2 * 2000;
     if (cost >= least) continue;
@@ -91,65 +91,82 @@ int plan_linear(int tiles, int blocks, int rows, int nt, int r, int stage, int t
     best->clusters = static_cast<int>(clusters);
     best->blocks_at_once = static_cast<int>(held);
     best->groups_at_once = static_cast<int>(batch);
-    best->smem = static_cast<size_t>(ring + held * per_block + (batch + kW4Warps - 1) * per_group);
+    best->smem = static_cast<size_t>(ring + held * per_block + (batch + warps - 1) * per_group);
   }
   return THINFER_OK;
 }
 
-template <int NT, int R, int G>
+template <int NT, int R, int G, int Warps>
 int launch_linear(W4LinearArgs& a, cudaStream_t st) {
   const int token_tiles = (a.rows + 8 * NT - 1) / (8 * NT);
   LinearPlan p{};
-  int rc = plan_linear(static_cast<int>(a.v.tiles), static_cast<int>(a.v.blocks), a.rows, NT, R, W4Stage<R, 128 / G>::kBytes, token_tiles, &p);
-  if (rc == THINFER_OK) rc = opt_in<w4_linear_kernel<NT, R, G>>(kLinearSmem);
+  int rc = plan_linear(static_cast<int>(a.v.tiles), static_cast<int>(a.v.blocks), a.rows, NT, R, Warps, W4Stage<R, 128 / G>::kBytes, token_tiles, &p);
+  if (rc == THINFER_OK) rc = opt_in<w4_linear_kernel<NT, R, G, Warps>>(kLinearSmem);
   if (rc != THINFER_OK) return rc;
   a.blocks_at_once = p.blocks_at_once;
   a.groups_at_once = p.groups_at_once;
-  return op_launch_clusters(w4_linear_kernel<NT, R, G>, static_cast<unsigned>(p.cluster), dim3(static_cast<unsigned>(p.cluster * p.clusters), static_cast<unsigned>(token_tiles)),
-                            dim3(kW4Warps * 32), p.smem, st, a);
+  return op_launch_clusters(w4_linear_kernel<NT, R, G, Warps>, static_cast<unsigned>(p.cluster), dim3(static_cast<unsigned>(p.cluster * p.clusters), static_cast<unsigned>(token_tiles)),
+                            dim3(Warps * 32), p.smem, st, a);
 }
 // Rows beyond which the tensor-memory kernel takes over.
 #ifdef W4_DEV
 #include <cstdlib>
-int most_mma_rows() { return getenv("W4_MMA") ? atoi(getenv("W4_MMA")) : 16; }
+int most_mma_rows() { return getenv("W4_MMA") ? atoi(getenv("W4_MMA")) : 8; }
 #else
-constexpr int most_mma_rows() { return 16; }
+constexpr int most_mma_rows() { return 8; }
 #endif
 
 struct TcPlan {
-  long long row_tiles, units;
+  long long row_tiles;
   int ctas;
-  size_t part_bytes;
+  size_t token_bytes, part_bytes, arrived_bytes;
+  size_t bytes() const { return token_bytes + part_bytes + arrived_bytes; }
 };
-template <int N>
-TcPlan plan_tc(int64_t tiles, int64_t blocks) {
-  constexpr int W = w4_tc_groups<N>();
+int tc_tokens(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+TcPlan plan_tc(int n, int64_t tiles, int64_t blocks) {
   TcPlan p{};
-  p.row_tiles = (tiles + 8 * W - 1) / (8 * W);
-  p.units = p.row_tiles * blocks;
+  p.row_tiles = (tiles * 16 + kW4TcTile - 1) / kW4TcTile;
+  const int64_t units = p.row_tiles * blocks;
   const int sms = op_sm_count();
-  p.ctas = p.units < sms ? static_cast<int>(p.units) : sms;
-  p.part_bytes = static_cast<size_t>(p.ctas) * 2 * N * W * 128 * 4;
+  p.ctas = units < sms ? static_cast<int>(units) : sms;
+  p.token_bytes = static_cast<size_t>(blocks) * n * 256;
+  p.part_bytes = static_cast<size_t>(p.ctas) * 2 * n * kW4TcTile * 4;
+  p.arrived_bytes = static_cast<size_t>(p.row_tiles) * kW4TcGroups * 4;
   return p;
 }
-TcPlan plan_tc_rows(int rows, int64_t tiles, int64_t blocks) { return rows <= 16 ? plan_tc<16>(tiles, blocks) : rows <= 32 ? plan_tc<32>(tiles, blocks) : plan_tc<64>(tiles, blocks); }
-
-size_t linear_workspace(int32_t rows, int32_t n_out, int32_t k) { return rows <= most_mma_rows() ? 0 : plan_tc_rows(rows, w4_tiles(n_out), w4_blocks(k)).part_bytes; }
+size_t linear_workspace(int32_t rows, int32_t n_out, int32_t k) { return rows <= most_mma_rows() ? 0 : plan_tc(tc_tokens(rows), w4_tiles(n_out), w4_blocks(k)).bytes(); }
 
 template <int N, int G>
 int launch_tc(const W4LinearArgs& a, void* workspace, cudaStream_t st) {
-  constexpr int P = 128 / G, kSmem = w4_tc_smem<N, P>(), kTile = w4_tc_groups<N>() * 128;
-  const TcPlan p = plan_tc<N>(a.v.tiles, a.v.blocks);
-  const W4TcArgs args{a, static_cast<float*>(workspace), p.row_tiles};
+  constexpr int P = 128 / G, kSmem = W4Tc<N, P>::kSmem;
+  const TcPlan p = plan_tc(N, a.v.tiles, a.v.blocks);
+  char* ws = static_cast<char*>(workspace);
+  const W4TcArgs args{a, reinterpret_cast<uint8_t*>(ws), reinterpret_cast<float*>(ws + p.token_bytes), reinterpret_cast<int*>(ws + p.token_bytes + p.part_bytes), p.row_tiles};
+  CUtensorMap codes, scales;
+  if (!op_tensor_map(&codes, a.v.codes, 256, a.v.blocks, a.v.tiles, kW4TcGroups * 8) || !op_tensor_map(&scales, a.v.scales, 8 * P, a.v.blocks, a.v.tiles, kW4TcGroups * 8))
+    return op_fail(THINFER_ECUDA, "cuTensorMapEncodeTiled failed for packed weights");
   int rc = opt_in<w4_linear_tc_kernel<N, P>>(kSmem);
-  if (rc == THINFER_OK) rc = op_launch(w4_linear_tc_kernel<N, P>, dim3(static_cast<unsigned>(p.ctas)), dim3(w4_tc_groups<N>() * 128), kSmem, st, args);
-  if (rc != THINFER_OK || (p.units % p.ctas == 0 && p.units / p.ctas % a.v.blocks == 0)) return rc;   // every CTA has whole row tiles
-  return op_launch(w4_linear_join_kernel<N>, dim3(static_cast<unsigned>(p.row_tiles * kTile / 256 + (kTile % 256 != 0)), static_cast<unsigned>(a.rows)), dim3(256), 0, st, args, p.ctas);
+  if (rc == THINFER_OK) rc = op_launch(w4_tokens_kernel<N>, dim3(static_cast<unsigned>((a.v.blocks * N * 16 + 255) / 256)), dim3(256), 0, st, args);
+  if (rc == THINFER_OK) rc = op_launch(w4_linear_tc_kernel<N, P>, dim3(static_cast<unsigned>(p.ctas)), dim3(kW4TcTile + 128), kSmem, st, args, codes, scales);
+  return rc;
 }
 
 template <int G>
 int launch_linear(W4LinearArgs& a, void* workspace, cudaStream_t st) {
-  if (a.rows <= most_mma_rows()) return a.rows <= 8 ? launch_linear<1, 2, G>(a, st) : launch_linear<2, 2, G>(a, st);
+#ifdef W4_DEV
+  const int v = getenv("W4_V") ? atoi(getenv("W4_V")) : 0;
+  if (v == 1) return launch_linear<1, 2, G, 16>(a, st);
+  if (v == 2) return launch_linear<1, 4, G, 8>(a, st);
+  if (v == 3) return launch_linear<2, 2, G, 16>(a, st);
+  if (v == 4) return launch_linear<2, 4, G, 8>(a, st);
+  if (v == 5) return launch_linear<2, 2, G, 8>(a, st);
+  if (v == 6) return launch_linear<4, 2, G, 8>(a, st);
+  if (v == 7) return launch_linear<4, 4, G, 8>(a, st);
+  if (v == 8) return launch_linear<3, 4, G, 8>(a, st);
+  if (v == 9) return launch_linear<3, 2, G, 8>(a, st);
+  if (v == 10) return launch_linear<2, 2, G, 12>(a, st);
+#endif
+  if (a.rows <= most_mma_rows()) return a.rows <= 8 ? launch_linear<1, 2, G, 16>(a, st) : launch_linear<2, 2, G, 16>(a, st);
   return a.rows <= 16 ? launch_tc<16, G>(a, workspace, st) : a.rows <= 32 ? launch_tc<32, G>(a, workspace, st) : launch_tc<64, G>(a, workspace, st);
 }
 

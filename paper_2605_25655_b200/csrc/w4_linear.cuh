@@ -15,7 +15,6 @@
 
 namespace thinfer {
 
-constexpr int kW4Warps = 16;
 constexpr int kW4Ahead = 2;   // units that are on their way while one is multiplied
 
 struct W4LinearArgs {
@@ -161,20 +160,21 @@ struct W4Feed {
   int left, step, steps, here, block, tile;       // units, step of the group, steps of a group and how many of them exist, the first one's block
   const uint8_t* codes;
   const uint8_t* params[(kPieces + 31) / 32];
-  long long second;                               // from the first tile's codes to the second's
+  long long apart[R];                             // from the first tile's codes to the others'
 
   __device__ __forceinline__ void begin_group() {
     const int lane = threadIdx.x & 31;
     const long long blocks = a.v.blocks;
     // behind the last tile the last one is read again; what comes of it is not kept
-    const int last = static_cast<int>(a.v.tiles) - 1, more = R > 1 && tile < last ? 1 : 0;
-    const long long at = min(tile, last) * blocks + block;
+    const int last = static_cast<int>(a.v.tiles) - 1, first = min(tile, last);
+    const long long at = first * blocks + block;
     codes = a.v.codes + at * 1024 + lane * 16;
-    second = more * blocks * 1024;
+#pragma unroll
+    for (int i = 0; i < R; ++i) apart[i] = (min(tile + i, last) - first) * blocks * 1024;
 #pragma unroll
     for (int h = 0; h < (kPieces + 31) / 32; ++h) {
-      const int piece = lane + 32 * h, i = piece >= 5 * P ? 1 : 0, j = piece - i * 5 * P;
-      const long long mine = at + i * more * blocks;
+      const int piece = lane + 32 * h, i = piece / (5 * P), j = piece - i * 5 * P;
+      const long long mine = at + (min(tile + i, last) - first) * blocks;
       params[h] = j < 4 * P ? a.v.scales + mine * (32 * P) + j * 8 : a.v.zeros + mine * (8 * P) + (j - 4 * P) * 8;
     }
   }
@@ -196,7 +196,7 @@ struct W4Feed {
   }
   __device__ __forceinline__ static int stride(int h) {
     const int piece = (threadIdx.x & 31) + 32 * h;
-    return (piece >= 5 * P ? piece - 5 * P : piece) < 4 * P ? 32 * P : 8 * P;
+    return piece % (5 * P) < 4 * P ? 32 * P : 8 * P;
   }
   __device__ __forceinline__ void next() {
     const int lane = threadIdx.x & 31;
@@ -205,10 +205,10 @@ struct W4Feed {
 #pragma unroll
         for (int i = 0; i < R; ++i)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) w4_copy16(to + i * 1024 + h * 512 + lane * 16, codes + i * second + h * 512);
+          for (int h = 0; h < 2; ++h) w4_copy16(to + i * 1024 + h * 512 + lane * 16, codes + apart[i] + h * 512);
 #pragma unroll
         for (int h = 0; h < (kPieces + 31) / 32; ++h) {
-          const int piece = lane + 32 * h, i = piece >= 5 * P ? 1 : 0, j = piece - i * 5 * P;
+          const int piece = lane + 32 * h, i = piece / (5 * P), j = piece - i * 5 * P;
           const int dst = j < 4 * P ? W4Stage<R, P>::kScales + i * P * 32 + j * 8 : W4Stage<R, P>::kZeros + i * P * 8 + (j - 4 * P) * 8;
           if (piece < kPieces) w4_copy8(to + dst, params[h]);
         }
@@ -230,8 +230,9 @@ struct W4Feed {
 };
 
 // NT: tiles of 8 tokens; R: tiles of 16 weight rows that a warp multiplies with what it reads of the tokens; G: columns of a group.
-template <int NT, int R, int G>
-__global__ void __launch_bounds__(kW4Warps * 32, 1) w4_linear_kernel(const __grid_constant__ W4LinearArgs a) {
+// Warps: a CTA's.
+template <int NT, int R, int G, int Warps>
+__global__ void __launch_bounds__(Warps * 32, 1) w4_linear_kernel(const __grid_constant__ W4LinearArgs a) {
   constexpr int P = 128 / G, kStage = W4Stage<R, P>::kBytes, kGroup = R * NT * 32;
   extern __shared__ uint4 smem[];
   pdl_launch_dependents();
@@ -249,13 +250,13 @@ __global__ void __launch_bounds__(kW4Warps * 32, 1) w4_linear_kernel(const __gri
   const int rows = min(8 * NT, a.rows - first_token);       // of the tokens
   uint4* x_s = smem;                                        // [block][q][token][t]
   uint4* slots = smem + held * (16 * rows);                 // [row group + warp][tile][token tile][lane]
-  const uint8_t* ring = reinterpret_cast<const uint8_t*>(slots + (a.groups_at_once + kW4Warps - 1) * kGroup) + warp * (kW4Ahead + 1) * kStage;
+  const uint8_t* ring = reinterpret_cast<const uint8_t*>(slots + (a.groups_at_once + Warps - 1) * kGroup) + warp * (kW4Ahead + 1) * kStage;
   bool waited = false;
 
   for (int from = group0; from < group1; from += a.groups_at_once) {
     const int batch = min(a.groups_at_once, group1 - from);
     // a run of the (row group, block) units
-    const int units = batch * held, u0 = units * warp / kW4Warps, u1 = units * (warp + 1) / kW4Warps;
+    const int units = batch * held, u0 = units * warp / Warps, u1 = units * (warp + 1) / Warps;
     for (int phase = 0; phase * held < slice || phase == 0; ++phase) {
       const int here = min(held, slice - phase * held);     // blocks of this phase; the rest of `held` is skipped
       const bool tokens = from == group0 || held < slice;   // to be fetched for this phase
@@ -266,7 +267,7 @@ __global__ void __launch_bounds__(kW4Warps * 32, 1) w4_linear_kernel(const __gri
         __syncthreads();                                    // nobody reads those of the phase before any more
         // the products of a token that is not there go nowhere: only what lies behind the last column has to be 0
         const int col0 = (block0 + phase * held) * 128;
-        for (int piece = tid; piece < 16 * here; piece += kW4Warps * 32) {
+        for (int piece = tid; piece < 16 * here; piece += Warps * 32) {
           const int col = col0 + piece * 8;
           const half_t* src = a.x + first_token * a.x_stride + col;
           uint32_t dst = smem_u32(x_s + (piece >> 2) * rows * 4 + (piece & 3));
@@ -318,16 +319,16 @@ __global__ void __launch_bounds__(kW4Warps * 32, 1) w4_linear_kernel(const __gri
     __syncthreads();
     // What the warps of this CTA have for each row group, in the order of the warps: w0 holds the group's first unit, w1 its
     // last; the sum goes to w0's slot.  Warp w begins at unit w * units / 16.
-    auto warp_of = [&](int unit) { return __popc(__ballot_sync(0xffffffffu, lane < kW4Warps && units * lane / kW4Warps <= unit)) - 1; };
+    auto warp_of = [&](int unit) { return __popc(__ballot_sync(0xffffffffu, lane < Warps && units * lane / Warps <= unit)) - 1; };
     float4* slot = reinterpret_cast<float4*>(slots) + lane;
-    for (int g = warp; g < batch; g += kW4Warps) {
+    for (int g = warp; g < batch; g += Warps) {
       const int w0 = warp_of(g * held), w1 = warp_of((g + 1) * held - 1);
       float4* to = slot + (g + w0) * kGroup;
 #pragma unroll
       for (int i = 0; i < R * NT; ++i) {
         float4 v = to[i * 32];
         for (int w = w0 + 1; w <= w1; ++w) {
-          if (w * units / kW4Warps == (w + 1) * units / kW4Warps) continue;   // it had none
+          if (w * units / Warps == (w + 1) * units / Warps) continue;   // it had none
           const float4 p = to[(w - w0) * kGroup + i * 32];
           v.x += p.x, v.y += p.y, v.z += p.z, v.w += p.w;
         }
@@ -339,7 +340,7 @@ __global__ void __launch_bounds__(kW4Warps * 32, 1) w4_linear_kernel(const __gri
     }
     if (ctas > 1) {
       w4_cluster_sync();
-      for (int g = rank * kW4Warps + warp; g < batch; g += ctas * kW4Warps) {
+      for (int g = rank * Warps + warp; g < batch; g += ctas * Warps) {
         const int w0 = warp_of(g * held);
         const uint32_t at = smem_u32(slot + (g + w0) * kGroup);
         float4 v[R * NT];
@@ -354,11 +355,11 @@ __global__ void __launch_bounds__(kW4Warps * 32, 1) w4_linear_kernel(const __gri
           for (int c = 1; c < 8; ++c)
             if (c < ctas) v[i].x += p[c].x, v[i].y += p[c].y, v[i].z += p[c].z, v[i].w += p[c].w;
         }
-        if (g + ctas * kW4Warps >= batch) w4_cluster_arrive();   // this warp's last read, ahead of its last stores
+        if (g + ctas * Warps >= batch) w4_cluster_arrive();   // this warp's last read, ahead of its last stores
 #pragma unroll
         for (int i = 0; i < R * NT; ++i) w4_output(a, ((from + g) * R + i / NT) * 16ll, first_token + i % NT * 8, v[i]);
       }
-      if (rank * kW4Warps + warp >= batch) w4_cluster_arrive();  // it had nothing to read
+      if (rank * Warps + warp >= batch) w4_cluster_arrive();  // it had nothing to read
       w4_cluster_wait();                                    // the slots are read, by the other CTAs too
     } else {
       __syncthreads();

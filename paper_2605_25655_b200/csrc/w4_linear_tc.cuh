@@ -1,42 +1,53 @@
-// The products of w4_linear.cuh for more tokens, on the 5th-generation tensor cores: with 17 rows and more, mma.sync would take
-// longer than the weights' bytes (16 weight rows by 8 tokens by 16 columns take two cycles of an SM; 64 rows 273 us as a
-// simple kernel, 117 us as in w4_linear.cuh, for 19 us of bytes).
+// The products of w4_linear.cuh for more tokens, on the 5th-generation tensor cores: with mma.sync, 16 weight rows by 8 tokens by 16
+// columns take two cycles of an SM, which is more than their bytes take from 24 tokens on, and the fragments of the tokens
+// cost registers and issue slots before that.
 //
 // Weights are the A operand, in tensor memory: 128 rows by a block of 128 columns per warpgroup, each warp turning the codes of
 // its two tiles into the storage type (exact differences code - zero) and storing them with the 16 x 256 bit shape, whose lanes are
-// those of the layout in w4_weights.cuh.  Tokens are the B operand, in shared memory with 128-byte swizzle, copied in pieces of 4
-// columns, in the order that the layout has the columns in.  The products of a group of columns
-// go to columns of tensor memory of their own, from which every thread scales and adds up one weight row by N tokens in FP32.
+// those of the layout in w4_weights.cuh.  Tokens are the B operand, in shared memory with 128-byte swizzle.  A first, small kernel lays
+// them out block by block as they stand there, their columns in the order that the weights have.  The products of a group
+// of columns go to columns of tensor memory of their own, from which every thread scales and adds up one weight row by N
+// tokens in FP32.
 //
-// A CTA holds W warpgroups, each with its own 128 rows, so that what is read of the tokens serves 128 W rows.  The (rows,
-// block) units of the whole matrix are dealt out to one CTA per SM in equal contiguous runs; rows that belong to one CTA are stored, the
-// others' partial sums go to the workspace and are added up by a second kernel in the order of the CTAs.
+// A CTA per SM: W warpgroups that unpack, each with its own 128 rows; a warp that feeds codes, scales and tokens of one block
+// after the other to a ring (three copies a block); and a warp for each warpgroup that issues its tensor instructions (as a
+// part of the unpacking warps that took a third of their time).  While the tensor cores multiply a block, its warpgroup unpacks
+// the next.  The (rows, block) units of the whole matrix are dealt out to the CTAs in equal contiguous runs; rows that belong to one
+// CTA are stored, the others' partial sums go to the workspace, and the warpgroup that comes last adds them up in the
+// order of the CTAs.
 #pragma once
 #include "w4_linear.cuh"
 
 namespace thinfer {
 
-constexpr int kW4TcAhead = 3, kW4TokenStages = 6;   // units on their way; blocks of tokens, which come one unit earlier
+constexpr int kW4TcGroups = 3;                        // W
+constexpr int kW4TcTile = kW4TcGroups * 128;          // weight rows of a CTA
+constexpr int kW4TcColumns = 512 / kW4TcGroups / 32 * 32;   // of tensor memory, for a warpgroup
 
 struct W4TcArgs {
   W4LinearArgs a;
+  uint8_t* tokens;       // [block][N * 256 bytes]
   float* parts;          // [CTA][first segment of its run, last one][token][row of the CTA's tile]
-  long long row_tiles;   // of 128 W rows
+  int* arrived;          // [row tile][warpgroup]
+  long long row_tiles;
 };
 
-template <int N>
-constexpr int w4_tc_groups() { return N == 64 ? 3 : 4; }   // warpgroups, by the registers and tensor memory that N tokens take
 template <int N, int P>
-constexpr int w4_tc_round() {   // groups of columns whose sums tensor memory holds at a time
-  constexpr int room = (512 / w4_tc_groups<N>() / 32 * 32 - 64) / N;
-  return P < room ? P : room;
-}
-template <int N, int P>
-constexpr int w4_tc_smem() { return 1024 + kW4TokenStages * N * 256 + w4_tc_groups<N>() * 4 * (kW4TcAhead + 1) * W4Stage<2, P>::kBytes; }
+struct W4Tc {
+  // Tensor memory of a warpgroup: weights, twice where there is room beside the sums of one group, and the sums of as many groups
+  // as fit (the others follow in further rounds).
+  static constexpr int kA = N < 64 ? 2 : 1, kSums = kA * 64, kRoom = (kW4TcColumns - kSums) / N;
+  static constexpr int kRound = P <= kRoom ? P : kRoom >= 2 ? 2 : 1, kRounds = P / kRound;
+  static constexpr int kCodes = kW4TcGroups * 8192, kScales = kW4TcGroups * 8 * 32 * P, kTokens = N * 256;
+  static constexpr int kBytes = kCodes + kTokens + kScales, kStage = (kBytes + 1023) / 1024 * 1024;
+  static constexpr int kFit = 224 * 1024 / kStage, kStages = kFit < 8 ? kFit : 8;
+  static constexpr int kSmem = 1024 + kStages * kStage;
+  static_assert(P % kRound == 0 && kSums + kRound * N <= kW4TcColumns, "the sums of a round");
+};
 
 // A run of units: CTA c of `ctas` begins at unit c * units / ctas.
 __host__ __device__ __forceinline__ long long w4_run(long long c, long long units, long long ctas) { return c * units / ctas; }
-__device__ __forceinline__ long long w4_run_of(long long unit, long long units, long long ctas) { return (ctas * (unit + 1) - 1) / units; }
+__device__ __forceinline__ int w4_run_of(long long unit, long long units, long long ctas) { return static_cast<int>((ctas * (unit + 1) - 1) / units); }
 
 // 16 lanes by 64 columns of tensor memory: r[4 i ..] of lane 4 g + t are columns 8 i + 2 t, + 1 of lane g, then of lane 8 + g.
 __device__ __forceinline__ void tmem_st_16x64(uint32_t taddr, const uint32_t (&r)[32]) {
@@ -50,26 +61,65 @@ __device__ __forceinline__ void tmem_st_16x64(uint32_t taddr, const uint32_t (&r
       "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(one));
+  return one != 0;
+}
+__device__ __forceinline__ void w4_bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+
+// The tokens, block by block as shared memory holds them: 64 columns in 128 bytes of a row of N, twice, the 16-byte units of
+// row r at unit ^ (r % 8).  Position 16 s' + 4 t + 2 b + e of half c is column 64 c + 32 (s' / 2) + 8 t + 4 (s' % 2) + 2 b + e of the block.
+// Clears what the CTAs count their arrivals in.
+template <int N>
+__global__ void __launch_bounds__(256) w4_tokens_kernel(const __grid_constant__ W4TcArgs args) {
+  pdl_wait();
+  pdl_launch_dependents();   // behind the wait: what the next kernel reads before its own wait is final
+  const W4LinearArgs& a = args.a;
+  const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+  for (long long c = i; c < args.row_tiles * kW4TcGroups; c += static_cast<long long>(gridDim.x) * 256) args.arrived[c] = 0;
+  const long long block = i / (N * 16);
+  if (block < a.v.blocks) {
+    const int at = static_cast<int>(i % (N * 16)), half = at / (N * 8), row = at / 8 % N, unit = at % 8, from = unit ^ (row & 7);
+    const long long col = block * 128 + half * 64 + from / 4 * 32 + (from & 1) * 16 + (from / 2 & 1) * 4;
+    uint2 lo = make_uint2(0, 0), hi = lo;
+    if (row < a.rows) {
+      const half_t* x = a.x + row * a.x_stride + col;
+      if (col < a.k) lo = *reinterpret_cast<const uint2*>(x);
+      if (col + 8 < a.k) hi = *reinterpret_cast<const uint2*>(x + 8);
+    }
+    reinterpret_cast<uint4*>(args.tokens)[i] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+  }
+  fence_proxy_async_all();
+}
 
 template <int N, int P>
-__global__ void __launch_bounds__(w4_tc_groups<N>() * 128, 1) w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args) {
-  constexpr int W = w4_tc_groups<N>(), kRound = w4_tc_round<N, P>(), kRounds = P / kRound, kColumns = 512 / W / 32 * 32;
-  constexpr int kStage = W4Stage<2, P>::kBytes, kTokens = N * 256, kTile = W * 128;
+__global__ void __launch_bounds__(kW4TcGroups * 128 + 128, 1)
+w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant__ CUtensorMap codes_map, const __grid_constant__ CUtensorMap scales_map) {
+  using T = W4Tc<N, P>;
+  constexpr int W = kW4TcGroups;
   constexpr uint32_t kIdesc = idesc_f16(128, N, 0, 0);
-  static_assert(P % kRound == 0 && 64 + kRound * N <= kColumns, "groups per round");
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t token_full[kW4TokenStages], token_empty[kW4TokenStages], done[W];
+  __shared__ __align__(8) uint64_t full[T::kStages], empty[T::kStages], a_full[W], d_free[W], done[W];
   __shared__ uint32_t tmem_holder;
-  __shared__ volatile int dead;    // a wait has run out: nothing is waited for any more, and the results are NaN
+  __shared__ int last_one[W];
+  __shared__ volatile int dead;    // a wait has run out: whom it happened to waits no more, and the results are NaN
   const W4LinearArgs& a = args.a;
-  uint8_t* tokens = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  uint8_t* ring = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   if (tid == 0) {
-    for (int i = 0; i < kW4TokenStages; ++i) {
-      mbar_init(&token_full[i], 4 * W);
-      mbar_init(&token_empty[i], W);
+    for (int i = 0; i < T::kStages; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 4 * W + W);   // the warps that unpack, and the products that read the tokens
     }
-    for (int i = 0; i < W; ++i) mbar_init(&done[i], 1);
+    for (int i = 0; i < W; ++i) {
+      mbar_init(&a_full[i], 4);
+      mbar_init(&d_free[i], 4);
+      mbar_init(&done[i], 1);
+    }
     dead = 0;
     fence_barrier_init();
   }
@@ -79,197 +129,252 @@ __global__ void __launch_bounds__(w4_tc_groups<N>() * 128, 1) w4_linear_tc_kerne
   tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_holder);
   pdl_launch_dependents();   // behind the allocation: a successor must not take the tensor memory first and then wait for this kernel
-  pdl_wait();
   const int blocks = static_cast<int>(a.v.blocks);
   const long long units = args.row_tiles * blocks, ctas = gridDim.x, cta = blockIdx.x;
   const long long u0 = w4_run(cta, units, ctas);
   const int count = static_cast<int>(w4_run(cta + 1, units, ctas) - u0);
-  const int first_block = static_cast<int>(u0 % blocks);
+  const int first_tile = static_cast<int>(u0 / blocks), first_block = static_cast<int>(u0 % blocks);
+  bool alive = true;
   auto wait = [&](uint64_t* bar, uint32_t parity) {
-    if (dead) return false;
-    if (mbar_wait(bar, parity, nullptr)) return true;
-    dead = 1;
-    return false;
+    if (alive && !mbar_wait(bar, parity, nullptr)) {
+      alive = false;
+      dead = 1;
+    }
+    return alive;
   };
 
-  const int wg = warp >> 2;
-  const uint8_t* ring = tokens + kW4TokenStages * kTokens + warp * (kW4TcAhead + 1) * kStage;
-  const uint32_t mine = tmem + wg * kColumns + (static_cast<uint32_t>((warp & 3) * 32) << 16);   // this warp's lanes
-  W4Feed<2, P, kW4TcAhead, 8 * W> feed(a, smem_u32(ring), 0, count, blocks, blocks, 0, 0);
-  feed.at(u0, blocks, 2 * warp);
-  // tokens warp, warp + 4 W, ...: 32 pieces of 4 columns
-  const int token_unit = (((lane >> 3) & 1) * 2 + (lane & 1)) * 2 + ((lane >> 2) & 1);
-  const uint32_t token_to = smem_u32(tokens) + (lane >> 4) * (N * 128) + ((lane >> 1) & 1) * 8;
-  int token_block = first_block;
-  auto copy_tokens = [&](int i) {
-    if (i >= count) return;
-    const int at = i % kW4TokenStages;
-    if (i >= kW4TokenStages) wait(&token_empty[at], (i / kW4TokenStages - 1) & 1);
-    const int col = token_block * 128 + 4 * lane;
-#pragma unroll
-    for (int row = warp; row < N; row += 4 * W) {
-      const bool there = row < a.rows && col < a.k;
-      asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(token_to + at * kTokens + row * 128 + ((token_unit ^ (row & 7)) << 4)),
-                   "l"(there ? a.x + row * a.x_stride + col : a.x), "r"(there ? 8 : 0)
-                   : "memory");
-    }
-    if (++token_block == blocks) token_block = 0;
-  };
-  copy_tokens(0);
-#pragma unroll
-  for (int d = 0; d < kW4TcAhead; ++d) {
-    copy_tokens(d + 1);
-    feed.next();
-  }
-  float acc[N];
-#pragma unroll
-  for (int j = 0; j < N; ++j) acc[j] = 0.f;
-  float scale[P] = {};
-  uint32_t rounds = 0;            // of this warpgroup so far
-  long long row_tile = u0 / blocks;
-  int block = first_block, begun = first_block;
-  const uint8_t* stage = ring;
-  // adds the sums of the groups of the last round to this thread's row
-  auto collect = [&](int first) {
-    const bool ok = __all_sync(0xffffffffu, wait(&done[wg], (rounds - 1) & 1));
-    tc_fence_after();
-    if (ok) {
-#pragma unroll
-      for (int p = 0; p < kRound; ++p)
-#pragma unroll
-        for (int j = 0; j < N; j += 16) {
-          uint32_t d[16];
-          tmem_ld16(mine + 64 + p * N + j, d);
-          tmem_ld_wait();
-#pragma unroll
-          for (int c = 0; c < 16; ++c) acc[j + c] = fmaf(scale[first + p], __uint_as_float(d[c]), acc[j + c]);
-        }
-    }
-    tc_fence_before();
-  };
-  // what this CTA has of a row tile, from block `begun` to block `last`
-  auto flush = [&](int last) {
-    const int row = wg * 128 + (warp & 3) * 32 + lane;
-    if (begun == 0 && last == blocks - 1) {
-#pragma unroll
-      for (int j = 0; j < N; ++j) w4_store(a, j, row_tile * kTile + row, dead ? __int_as_float(0x7fffffff) : acc[j]);
-    } else {
-      const bool first = row_tile * blocks + begun == u0;
-      float* part = args.parts + ((cta * 2 + (first ? 0 : 1)) * N) * kTile + row;
-#pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (j < a.rows) part[j * kTile] = dead ? __int_as_float(0x7fffffff) : acc[j];
-    }
-#pragma unroll
-    for (int j = 0; j < N; ++j) acc[j] = 0.f;
-  };
-  for (int i = 0; i < count; ++i) {
-    w4_copies_wait<kW4TcAhead - 1>();
-    fence_proxy_async_smem();                             // the tokens are read by the tensor cores
-    __syncwarp();
+  if (warp == 4 * W) {
+    // The feeder.  Codes and scales were final before the kernel in front of this one let it start; the tokens are its work.
     if (lane == 0) {
-      if (i == 0) mbar_arrive(&token_full[0]);
-      mbar_arrive(&token_full[(i + 1) % kW4TokenStages]);
-    }
-    uint4 codes[2][2];
-    uint32_t zeros[2][P];
-    float next_scale[P];
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) codes[c][h] = reinterpret_cast<const uint4*>(stage)[c * 64 + h * 32 + lane];
-#pragma unroll
-      for (int p = 0; p < P; ++p) zeros[c][p] = stage[W4Stage<2, P>::kZeros + (c * 8 + (lane >> 2)) * P + p];
-    }
-#pragma unroll
-    for (int p = 0; p < P; ++p)   // of this thread's row: tile lane / 16, row lane % 16
-      next_scale[p] = h_to_f(reinterpret_cast<const half_t*>(stage + W4Stage<2, P>::kScales)[(((lane >> 4) * 8 + (lane & 7)) * P + p) * 2 + ((lane >> 3) & 1)]);
-    stage = stage == ring + kW4TcAhead * kStage ? ring : stage + kStage;
-    copy_tokens(i + kW4TcAhead + 1);
-    feed.next();
-    uint32_t r[32];
-    auto unpack = [&](int c) {
-#pragma unroll
-      for (int w = 0; w < 8; ++w) {   // step w: columns 16 w .. of the block as they lie
-        const uint4& from = codes[c][w / 4];
-        uint32_t v[4];
-        w4_unpack<true>(w % 4 == 0 ? from.x : w % 4 == 1 ? from.y : w % 4 == 2 ? from.z : from.w, w4_zero<true>(zeros[c][w * P / 8]), v);
-        r[4 * w] = v[0];
-        r[4 * w + 1] = v[2];
-        r[4 * w + 2] = v[1];
-        r[4 * w + 3] = v[3];
+      fence_proxy_async_all();
+      int tile = first_tile, block = first_block, token_block = first_block;
+      int issued = count;
+      bool waited = false;
+      auto tokens = [&](int i) {
+        w4_bulk_load(ring + i % T::kStages * T::kStage + T::kCodes, args.tokens + static_cast<long long>(token_block) * T::kTokens, T::kTokens, &full[i % T::kStages]);
+        if (++token_block == blocks) token_block = 0;
+      };
+      for (int i = 0; i < count; ++i) {
+        const int s = i % T::kStages;
+        if (i >= T::kStages) {
+          if (!waited) {             // the ring is full: now the tokens of what is in it
+            waited = true;
+            pdl_wait();
+            fence_proxy_async_all();
+            for (int j = 0; j < i; ++j) tokens(j);
+          }
+          if (!wait(&empty[s], (i / T::kStages - 1) & 1)) {
+            issued = i;
+            break;
+          }
+        }
+        uint8_t* stage = ring + s * T::kStage;
+        mbar_expect_tx(&full[s], T::kBytes);
+        tma_load_3d(stage, &codes_map, &full[s], 0, block, tile * 8 * W);
+        tma_load_3d(stage + T::kCodes + T::kTokens, &scales_map, &full[s], 0, block, tile * 8 * W);
+        if (waited) tokens(i);
+        if (++block == blocks) {
+          block = 0;
+          ++tile;
+        }
       }
-    };
-    unpack(0);
-    if (i > 0) {
-      collect(P - kRound);
-      if (block == 0) {
-        flush(blocks - 1);
-        ++row_tile;
-        begun = 0;
+      if (!waited) {
+        pdl_wait();
+        fence_proxy_async_all();
+        for (int j = 0; j < count; ++j) tokens(j);
       }
+      // nothing of its own is under way when it leaves
+      for (int i = issued > T::kStages ? issued - T::kStages : 0; i < issued; ++i) mbar_wait(&full[i % T::kStages], (i / T::kStages) & 1, nullptr);
     }
-    tmem_st_16x64(mine, r);
-    unpack(1);
-    tmem_st_16x64(mine + (16u << 16), r);
-    tmem_st_wait();
-    tc_fence_before();
+  } else if (warp > 4 * W) {
+    // the products of warpgroup wg
+    const int wg = warp - 4 * W - 1;
+    const uint32_t columns = tmem + wg * kW4TcColumns;
+    const uint64_t first = smem_desc_sw128(smem_u32(ring + T::kCodes), 16, 1024);
+    uint32_t frees = 0;
+    for (int i = 0; i < count; ++i) {
+      const int s = i % T::kStages;
+      bool ok = wait(&full[s], (i / T::kStages) & 1);
+      ok = wait(&a_full[wg], i & 1) && ok;
+      const uint64_t b = first + static_cast<uint64_t>(s * (T::kStage >> 4));
 #pragma unroll
-    for (int p = 0; p < P; ++p) scale[p] = next_scale[p];
-#pragma unroll
-    for (int round = 0; round < kRounds; ++round) {
-      asm volatile("bar.sync %0, 128;" ::"r"(wg + 1) : "memory");
-      if ((warp & 3) == 0 && lane == 0) {
-        const int at = i % kW4TokenStages;
-        bool ok = round > 0 || wait(&token_full[at], (i / kW4TokenStages) & 1);
+      for (int round = 0; round < T::kRounds; ++round) {
+        if (round > 0) ok = wait(&d_free[wg], frees++ & 1) && ok;
         tc_fence_after();
-        if (ok && !dead) {
-          const uint64_t b = smem_desc_sw128(smem_u32(tokens + at * kTokens), 16, 1024);
+        if (ok && elect_one()) {
 #pragma unroll
-          for (int p = 0; p < kRound; ++p)
+          for (int p = 0; p < T::kRound; ++p)
 #pragma unroll
             for (int w = 0; w < 8 / P; ++w) {
-              const int s = (round * kRound + p) * (8 / P) + w;
-              tc_mma_f16_ts(tmem + wg * kColumns + 64 + p * N, tmem + wg * kColumns + s * 8, b + (s / 4) * (N * 128 >> 4) + (s % 4) * 2, kIdesc, w > 0);
+              const int st = (round * T::kRound + p) * (8 / P) + w;
+              tc_mma_f16_ts(columns + T::kSums + p * N, columns + (T::kA == 2 ? (i & 1) * 64 : 0) + st * 8, b + (st / 4) * (N * 128 >> 4) + (st % 4) * 2, kIdesc, w > 0);
             }
           tc_commit(&done[wg]);
-          if (round == kRounds - 1) tc_commit(&token_empty[at]);
+          if (round == T::kRounds - 1) tc_commit(&empty[s]);
+        }
+        __syncwarp();
+      }
+    }
+  } else {
+    const int wg = warp >> 2;
+    const uint32_t mine = tmem + wg * kW4TcColumns + (static_cast<uint32_t>((warp & 3) * 32) << 16);   // this warp's lanes
+    float acc[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) acc[j] = 0.f;
+    float scale[P] = {};
+    uint32_t rounds = 0;            // of this warpgroup so far
+    int row_tile = first_tile, block = first_block, begun = first_block;
+    // the zero points, two units ahead: the bytes of P groups of row g of both tiles
+    const int last_tile = static_cast<int>(a.v.tiles) - 1;
+    int zero_tile = first_tile * 8 * W + 2 * warp, zero_block = first_block;
+    const uint8_t* zero_at[2];
+    auto zeros_of_tile = [&] {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) zero_at[c] = a.v.zeros + ((static_cast<long long>(min(zero_tile + c, last_tile)) * blocks + zero_block) * 8 + (lane >> 2)) * P;
+    };
+    zeros_of_tile();
+    auto zeros = [&](uint32_t (&z)[2]) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        z[c] = P == 4 ? *reinterpret_cast<const uint32_t*>(zero_at[c]) : P == 2 ? *reinterpret_cast<const uint16_t*>(zero_at[c]) : *zero_at[c];
+        zero_at[c] += 8 * P;
+      }
+      if (++zero_block == blocks) {
+        zero_block = 0;
+        zero_tile += 8 * W;
+        zeros_of_tile();
+      }
+    };
+    uint32_t z0[2], z1[2];
+    zeros(z0);
+    zeros(z1);
+    // adds the sums of the groups of the last round to this thread's row
+    auto collect = [&](int first) {
+      const bool ok = __all_sync(0xffffffffu, wait(&done[wg], rounds++ & 1));
+      tc_fence_after();
+      if (ok) {
+#pragma unroll
+        for (int p = 0; p < T::kRound; ++p) {
+          uint32_t d[N / 16][16];
+#pragma unroll
+          for (int j = 0; j < N / 16; ++j) tmem_ld16(mine + T::kSums + p * N + 16 * j, d[j]);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < N; ++j) acc[j] = fmaf(scale[first + p], __uint_as_float(d[j / 16][j % 16]), acc[j]);
         }
       }
+      tc_fence_before();
+    };
+    // what this CTA has of a row tile, from block `begun` to block `last`
+    auto flush = [&](int last) {
+      const int row = wg * 128 + (warp & 3) * 32 + lane;
+      const long long out = static_cast<long long>(row_tile) * kW4TcTile + row;
+      if (begun == 0 && last == blocks - 1) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) w4_store(a, j, out, dead ? __int_as_float(0x7fffffff) : acc[j]);
+      } else {
+        const long long unit = static_cast<long long>(row_tile) * blocks;
+        float* part = args.parts + ((cta * 2 + (unit + begun == u0 ? 0 : 1)) * N) * kW4TcTile + row;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (j < a.rows) part[j * kW4TcTile] = dead ? __int_as_float(0x7fffffff) : acc[j];
+        const int c0 = w4_run_of(unit, units, ctas), c1 = w4_run_of(unit + blocks - 1, units, ctas);
+        pdl_wait();                 // the counter has been cleared
+        __threadfence();
+        asm volatile("bar.sync %0, 128;" ::"r"(wg + 1) : "memory");
+        if ((warp & 3) == 0 && lane == 0) last_one[wg] = atomicAdd(&args.arrived[row_tile * W + wg], 1) == c1 - c0;
+        asm volatile("bar.sync %0, 128;" ::"r"(wg + 1) : "memory");
+        if (last_one[wg]) {
+          __threadfence();
+          const int slot = w4_run(c0, units, ctas) >= unit ? 0 : 1;
+          const float* from = args.parts + static_cast<long long>(c0) * 2 * N * kW4TcTile + row;
+#pragma unroll
+          for (int j = 0; j < N; ++j) acc[j] = j < a.rows ? __ldcg(from + (slot * N + j) * kW4TcTile) : 0.f;
+          for (int c = 1; c <= c1 - c0; ++c) {
+            from += 2 * N * kW4TcTile;
+#pragma unroll
+            for (int j = 0; j < N; ++j) acc[j] += j < a.rows ? __ldcg(from + j * kW4TcTile) : 0.f;
+          }
+#pragma unroll
+          for (int j = 0; j < N; ++j) w4_store(a, j, out, acc[j]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j) acc[j] = 0.f;
+    };
+    for (int i = 0; i < count; ++i) {
+      const int s = i % T::kStages;
+      const uint8_t* stage = ring + s * T::kStage;
+      wait(&full[s], (i / T::kStages) & 1);
+      uint4 codes[2][2];
+      float next_scale[P];
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) codes[c][h] = reinterpret_cast<const uint4*>(stage)[(2 * warp + c) * 64 + h * 32 + lane];
+#pragma unroll
+      for (int p = 0; p < P; ++p)   // of this thread's row: tile lane / 16, row lane % 16
+        next_scale[p] = h_to_f(reinterpret_cast<const half_t*>(stage + T::kCodes + T::kTokens)[(((2 * warp + (lane >> 4)) * 8 + (lane & 7)) * P + p) * 2 + ((lane >> 3) & 1)]);
+      uint32_t r[2][32];
+      auto unpack = [&](int c) {
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {   // step w: columns 16 w .. of the block as they lie
+          const uint4& from = codes[c][w / 4];
+          uint32_t v[4];
+          w4_unpack<true>(w % 4 == 0 ? from.x : w % 4 == 1 ? from.y : w % 4 == 2 ? from.z : from.w, w4_zero<true>(z0[c] >> (8 * (w * P / 8)) & 255u), v);
+          r[c][4 * w] = v[0];
+          r[c][4 * w + 1] = v[2];
+          r[c][4 * w + 2] = v[1];
+          r[c][4 * w + 3] = v[3];
+        }
+      };
+      auto collect_last = [&] {
+        if (i == 0) return;
+        collect(P - T::kRound);
+        if (block == 0) {
+          flush(blocks - 1);
+          ++row_tile;
+          begun = 0;
+        }
+      };
+      // Into the weights that the products of the last block do not read, while they are under way; or, where there is room for
+      // one block only, behind them.
+      const uint32_t to = mine + (T::kA == 2 ? (i & 1) * 64 : 0);
+      unpack(0);
+      if (T::kA == 1) collect_last();
+      tmem_st_16x64(to, r[0]);
+      unpack(1);
+      tmem_st_16x64(to + (16u << 16), r[1]);
       __syncwarp();
-      ++rounds;
-      if (round < kRounds - 1) collect(round * kRound);
+      if (lane == 0) mbar_arrive(&empty[s]);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) z0[c] = z1[c];
+      zeros(z1);
+      if (T::kA == 2) collect_last();
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&a_full[wg]);
+#pragma unroll
+      for (int p = 0; p < P; ++p) scale[p] = next_scale[p];
+#pragma unroll
+      for (int round = 0; round < T::kRounds - 1; ++round) {
+        collect(round * T::kRound);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&d_free[wg]);
+      }
+      if (++block == blocks) block = 0;
     }
-    if (++block == blocks) block = 0;
+    if (count > 0) {
+      collect(P - T::kRound);
+      flush(block == 0 ? blocks - 1 : block - 1);
+    }
   }
-  if (count > 0) {
-    collect(P - kRound);
-    flush(block == 0 ? blocks - 1 : block - 1);
-  }
-  w4_copies_wait<0>();
+  __syncwarp();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   if (warp == 1) tmem_dealloc(tmem, 512);
-}
-
-// Adds up the partial sums of row tiles that several CTAs have: one thread per weight row and token.
-template <int N>
-__global__ void __launch_bounds__(256) w4_linear_join_kernel(const __grid_constant__ W4TcArgs args, int ctas) {
-  constexpr int kTile = w4_tc_groups<N>() * 128;
-  pdl_launch_dependents();
-  const W4LinearArgs& a = args.a;
-  const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x, row_tile = i / kTile;
-  const int row = static_cast<int>(i % kTile), token = blockIdx.y;
-  const long long blocks = a.v.blocks, units = args.row_tiles * blocks;
-  pdl_wait();
-  if (row_tile >= args.row_tiles) return;
-  const long long c0 = w4_run_of(row_tile * blocks, units, ctas), c1 = w4_run_of(row_tile * blocks + blocks - 1, units, ctas);
-  if (c0 == c1) return;
-  const long long slot = w4_run(c0, units, ctas) >= row_tile * blocks ? 0 : 1;
-  float v = args.parts[((c0 * 2 + slot) * N + token) * kTile + row];
-  for (long long c = c0 + 1; c <= c1; ++c) v += args.parts[(c * 2 * N + token) * kTile + row];
-  w4_store(a, token, row_tile * kTile + row, v);
 }
 
 }  // namespace thinfer
