@@ -12,9 +12,8 @@
 // A CTA per SM: W warpgroups that unpack, each with its own 128 rows; a warp that feeds codes, scales and tokens of one block
 // after the other to a ring (three copies a block); and a warp for each warpgroup that issues its tensor instructions (as a
 // part of the unpacking warps that took a third of their time).  While the tensor cores multiply a block, its warpgroup unpacks
-// the next.  The (rows, block) units of the whole matrix are dealt out to the CTAs in equal contiguous runs; rows that belong to one
-// CTA are stored, the others' partial sums go to the workspace, and the warpgroup that comes last adds them up in the
-// order of the CTAs.
+// the next.  The (rows, block) units of the whole matrix are dealt out to the CTAs in equal contiguous runs; their partial
+// sums go to the workspace, and the warpgroup that comes last adds up those of its rows in the order of the CTAs.
 #pragma once
 #include "w4_linear.cuh"
 
@@ -34,9 +33,9 @@ struct W4TcArgs {
 
 template <int N, int P>
 struct W4Tc {
-  // Tensor memory of a warpgroup: weights, twice where there is room beside the sums of one group, and the sums of as many groups
-  // as fit (the others follow in further rounds).
-  static constexpr int kA = N < 64 ? 2 : 1, kSums = kA * 64, kRoom = (kW4TcColumns - kSums) / N;
+  // Tensor memory of a warpgroup: weights, twice where there is room beside the sums of all groups of a block, and the sums of as
+  // many groups as fit (the others follow in further rounds).
+  static constexpr int kA = P * N <= 32 ? 2 : 1, kSums = kA * 64, kRoom = (kW4TcColumns - kSums) / N;
   static constexpr int kRound = P <= kRoom ? P : kRoom >= 2 ? 2 : 1, kRounds = P / kRound;
   static constexpr int kCodes = kW4TcGroups * 8192, kScales = kW4TcGroups * 8 * 32 * P, kTokens = N * 256;
   static constexpr int kBytes = kCodes + kTokens + kScales, kStage = (kBytes + 1023) / 1024 * 1024;
@@ -265,42 +264,50 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
       }
       tc_fence_before();
     };
-    // what this CTA has of a row tile, from block `begun` to block `last`
-    auto flush = [&](int last) {
+    // What this CTA has of a row tile from block `begun` on, and the result where nothing is missing.  All of it goes by way of
+    // the workspace, in short code: it runs once or twice, and the instructions of 64 tokens' stores side by side took longer
+    // to fetch (up to 40 us) than the sums to read.
+    auto flush = [&] {
       const int row = wg * 128 + (warp & 3) * 32 + lane;
-      const long long out = static_cast<long long>(row_tile) * kW4TcTile + row;
-      if (begun == 0 && last == blocks - 1) {
+      const long long unit = static_cast<long long>(row_tile) * blocks;
+      const int c0 = w4_run_of(unit, units, ctas), c1 = w4_run_of(unit + blocks - 1, units, ctas);
+      float* part = args.parts + ((cta * 2 + (unit + begun == u0 ? 0 : 1)) * N) * kW4TcTile + row;
+      const bool lost = dead;
 #pragma unroll
-        for (int j = 0; j < N; ++j) w4_store(a, j, out, dead ? __int_as_float(0x7fffffff) : acc[j]);
-      } else {
-        const long long unit = static_cast<long long>(row_tile) * blocks;
-        float* part = args.parts + ((cta * 2 + (unit + begun == u0 ? 0 : 1)) * N) * kW4TcTile + row;
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-          if (j < a.rows) part[j * kW4TcTile] = dead ? __int_as_float(0x7fffffff) : acc[j];
-        const int c0 = w4_run_of(unit, units, ctas), c1 = w4_run_of(unit + blocks - 1, units, ctas);
+      for (int j = 0; j < N; ++j) {
+        if (j < a.rows) part[j * kW4TcTile] = lost ? __int_as_float(0x7fffffff) : acc[j];
+        acc[j] = 0.f;
+      }
+      if (c1 > c0) {
         pdl_wait();                 // the counter has been cleared
         __threadfence();
         asm volatile("bar.sync %0, 128;" ::"r"(wg + 1) : "memory");
         if ((warp & 3) == 0 && lane == 0) last_one[wg] = atomicAdd(&args.arrived[row_tile * W + wg], 1) == c1 - c0;
         asm volatile("bar.sync %0, 128;" ::"r"(wg + 1) : "memory");
-        if (last_one[wg]) {
-          __threadfence();
-          const int slot = w4_run(c0, units, ctas) >= unit ? 0 : 1;
-          const float* from = args.parts + static_cast<long long>(c0) * 2 * N * kW4TcTile + row;
-#pragma unroll
-          for (int j = 0; j < N; ++j) acc[j] = j < a.rows ? __ldcg(from + (slot * N + j) * kW4TcTile) : 0.f;
-          for (int c = 1; c <= c1 - c0; ++c) {
-            from += 2 * N * kW4TcTile;
-#pragma unroll
-            for (int j = 0; j < N; ++j) acc[j] += j < a.rows ? __ldcg(from + j * kW4TcTile) : 0.f;
-          }
-#pragma unroll
-          for (int j = 0; j < N; ++j) w4_store(a, j, out, acc[j]);
-        }
+        if (!last_one[wg]) return;
+        __threadfence();
       }
+      const long long out = static_cast<long long>(row_tile) * kW4TcTile + row;
+      const float* from = args.parts + ((static_cast<long long>(c0) * 2 + (w4_run(c0, units, ctas) >= unit ? 0 : 1)) * N) * kW4TcTile + row;
+      const float* more = args.parts + (static_cast<long long>(c0 + 1) * 2 * N) * kW4TcTile + row;
+#pragma unroll 1
+      for (int j0 = 0; j0 < a.rows; j0 += 8) {
+        float v[8];
 #pragma unroll
-      for (int j = 0; j < N; ++j) acc[j] = 0.f;
+        for (int j = 0; j < 8; ++j) v[j] = j0 + j < a.rows ? __ldcg(from + (j0 + j) * kW4TcTile) : 0.f;
+#pragma unroll 1
+        for (int c = c0; c < c1; c += 2) {
+          float x[2][8];
+#pragma unroll
+          for (int o = 0; o < 2; ++o)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[o][j] = c + o < c1 && j0 + j < a.rows ? __ldcg(more + (static_cast<long long>(c + o - c0) * 2 * N + j0 + j) * kW4TcTile) : 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = (v[j] + x[0][j]) + x[1][j];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w4_store(a, j0 + j, out, v[j]);
+      }
     };
     for (int i = 0; i < count; ++i) {
       const int s = i % T::kStages;
@@ -332,7 +339,7 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
         if (i == 0) return;
         collect(P - T::kRound);
         if (block == 0) {
-          flush(blocks - 1);
+          flush();
           ++row_tile;
           begun = 0;
         }
@@ -367,7 +374,7 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
     }
     if (count > 0) {
       collect(P - T::kRound);
-      flush(block == 0 ? blocks - 1 : block - 1);
+      flush();
     }
   }
   __syncwarp();
