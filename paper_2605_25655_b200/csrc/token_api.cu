@@ -21,17 +21,10 @@ RowPlan plan_rows(int64_t rows, int64_t slots, int most) {
   const int64_t room = static_cast<int64_t>(op_sm_count()) * 2;
   while (p.ctas < 8 && (slots > static_cast<int64_t>(p.ctas) * 512 * most || (rows * p.ctas * 2 <= room && slots > p.ctas * 256))) p.ctas *= 2;
   const int64_t slice = (slots + p.ctas - 1) / p.ctas;
-  while (p.slots < most && slice > 512 * static_cast<int64_t>(p.slots)) p.slots *= 2;
+  p.slots = static_cast<int>((slice + 511) / 512 < most ? (slice + 511) / 512 : most);
   const int64_t each = (slice + p.slots - 1) / p.slots;
   p.threads = each >= 512 ? 512 : static_cast<unsigned>((each + 31) / 32 * 32);
   return p;
-}
-
-template <int E>
-int launch_verify(const VerifyDraftsArgs& a, const RowPlan& plan, unsigned ctas, cudaStream_t st) {
-  const size_t smem = static_cast<size_t>(E) * plan.threads * 8;
-  const int rc = opt_in<verify_drafts_kernel<E>>(smem);
-  return rc != THINFER_OK ? rc : op_launch_clusters(verify_drafts_kernel<E>, plan.ctas, dim3(ctas), dim3(plan.threads), smem, st, a);
 }
 
 bool stride_ok(int64_t stride, int64_t least, int64_t n) { return stride >= least && (n <= 1 || stride <= kFar / n); }
@@ -59,12 +52,15 @@ int thinfer_op_token_probs(const float* logits, int64_t logit_stride, const floa
   a.vocab = vocab;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const int64_t slots = (static_cast<int64_t>(vocab) + 6) / 4;   // wherever a row begins
-  if (slots > 8 * 512 * 8) return op_launch(token_probs_long_kernel, dim3(static_cast<unsigned>(rows)), dim3(512), 0, st, a);
-  const RowPlan plan = plan_rows(rows, slots, 8);
+  constexpr int kMost = 27;                                      // slots a thread: 216 KB
+  if (slots > 8 * 512 * kMost) return op_launch(token_probs_long_kernel, dim3(static_cast<unsigned>(rows)), dim3(512), 0, st, a);
+  const RowPlan plan = plan_rows(rows, slots, slots > 8 * 512 * 8 ? kMost : 8);
   const int64_t ctas = static_cast<int64_t>(rows) * plan.ctas;
   if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "token_probs: too many rows");
-  auto kernel = plan.slots == 1 ? token_probs_kernel<1> : plan.slots == 2 ? token_probs_kernel<2> : plan.slots == 4 ? token_probs_kernel<4> : token_probs_kernel<8>;
-  return op_launch_clusters(kernel, plan.ctas, dim3(static_cast<unsigned>(ctas)), dim3(plan.threads), 0, st, a);
+  const size_t smem = static_cast<size_t>(plan.slots) * plan.threads * 16;
+  const int rc = opt_in<token_probs_kernel>(smem);
+  if (rc != THINFER_OK) return rc;
+  return op_launch_clusters(token_probs_kernel, plan.ctas, dim3(static_cast<unsigned>(ctas)), dim3(plan.threads), smem, st, a);
 }
 
 int thinfer_op_verify_drafts(const float* p, int64_t p_batch_stride, int64_t p_row_stride, const float* q, int64_t q_batch_stride,
@@ -102,17 +98,14 @@ int thinfer_op_verify_drafts(const float* p, int64_t p_batch_stride, int64_t p_r
   a.accepted = accepted;
   a.drafts = n_drafts;
   a.vocab = vocab;
-  const RowPlan plan = plan_rows(batch, (static_cast<int64_t>(vocab) + 6) / 4, 16);
-  if (static_cast<int64_t>(batch) * plan.ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "verify_drafts: too many requests");
-  const unsigned ctas = static_cast<unsigned>(batch) * plan.ctas;
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  switch (plan.slots) {
-    case 1: return launch_verify<1>(a, plan, ctas, st);
-    case 2: return launch_verify<2>(a, plan, ctas, st);
-    case 4: return launch_verify<4>(a, plan, ctas, st);
-    case 8: return launch_verify<8>(a, plan, ctas, st);
-    default: return launch_verify<16>(a, plan, ctas, st);
-  }
+  const RowPlan plan = plan_rows(batch, (static_cast<int64_t>(vocab) + 6) / 4, kVerifySteps);
+  const int64_t ctas = static_cast<int64_t>(batch) * plan.ctas;
+  if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "verify_drafts: too many requests");
+  a.steps = plan.slots;
+  const size_t smem = static_cast<size_t>(plan.slots) * plan.threads * 8;
+  const int rc = opt_in<verify_drafts_kernel>(smem);
+  if (rc != THINFER_OK) return rc;
+  return op_launch_clusters(verify_drafts_kernel, plan.ctas, dim3(static_cast<unsigned>(ctas)), dim3(plan.threads), smem, static_cast<cudaStream_t>(cuda_stream), a);
 }
 
 }  // extern "C"

@@ -74,49 +74,71 @@ struct TokenRow {
     wholes = static_cast<int>((static_cast<unsigned>(n) + before) / 4) - first_whole;
   }
   __device__ __forceinline__ bool whole(int s) const { return s - first_whole >= 0 && s - first_whole < wholes; }
-  __device__ __forceinline__ bool has(int s, int i) const { return (s > 0 || i >= before) && 4ll * s + i - before < count; }
-  // of a row whose memory has this one's alignment
-  __device__ __forceinline__ float4 load(const float* from, int s, float fill) const {
-    if (whole(s)) {
-      const uint4 v = ld_stream(from + 4ll * s);
-      return make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
-    }
-    return load_parts(from, s, fill);
-  }
-  __device__ __forceinline__ float4 load_parts(const float* from, int s, float fill) const {
-    return make_float4(has(s, 0) ? from[4ll * s] : fill, has(s, 1) ? from[4ll * s + 1] : fill, has(s, 2) ? from[4ll * s + 2] : fill, has(s, 3) ? from[4ll * s + 3] : fill);
-  }
 };
 
-// A cluster holds one row in registers: E slots of four logits a thread.  Every CTA brings its slice down to weights against its
-// own largest logit, then the CTAs exchange (largest, sum) once, and the weights leave with one factor.  Bound by memory: each
-// logit is read once and each probability written once.
-template <int E>
-__global__ void __launch_bounds__(512, 2) token_probs_kernel(const __grid_constant__ TokenProbsArgs a) {
+// The ends of a row, apart from the code that every slot takes.
+__device__ __noinline__ float4 token_load_end(const float* from, int s, int before, int count, float fill) {
+  float f[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const long long place = 4ll * s + i - before;
+    f[i] = place >= 0 && place < count ? from[4ll * s + i] : fill;
+  }
+  return make_float4(f[0], f[1], f[2], f[3]);
+}
+__device__ __noinline__ void token_store_end(float* to, int s, int before, int count, float4 v) {
+  const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const long long place = 4ll * s + i - before;
+    if (place >= 0 && place < count) to[4ll * s + i] = f[i];
+  }
+}
+// Slot s of a row with the places of `row`; aligned: its memory has their alignment too.
+__device__ __forceinline__ float4 token_load(const TokenRow& row, const float* from, bool aligned, int s, float fill) {
+  if (!row.whole(s)) return token_load_end(from, s, row.before, row.count, fill);
+  if (!aligned) return make_float4(from[4ll * s], from[4ll * s + 1], from[4ll * s + 2], from[4ll * s + 3]);
+  const uint4 v = ld_stream(from + 4ll * s);
+  return make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
+}
+
+// A cluster holds one row in shared memory: `steps` slots of four logits a thread, which nobody else touches.  Every CTA brings its
+// slice down to weights against its own largest logit, then the CTAs exchange (largest, sum) once, and the weights leave
+// with one factor.  Bound by memory: each logit is read once and each probability written once.  A slice of 64 KB leaves
+// room for three CTAs on an SM, one of which reads while another computes and a third one writes (two with the slice in registers: 84 us
+// instead of MEASURED_PROBS for 320 x 128000).
+__global__ void __launch_bounds__(512, 3) token_probs_kernel(const __grid_constant__ TokenProbsArgs a) {
+  extern __shared__ float4 s_x[];   // [steps][threads]
   __shared__ float s_top[16], s_sum[16];
   __shared__ int s_index;
   __shared__ uint4 s_mine;          // largest (NaN where there is one), sum, its lowest index
   pdl_launch_dependents();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
   uint32_t rank;
   const uint32_t ctas = token_cluster(&rank);
   const long long which = blockIdx.x / ctas;
   const TokenRow row(a.logits + which * a.stride, a.vocab);
   const int slice = (row.slots + static_cast<int>(ctas) - 1) / static_cast<int>(ctas), from = slice * static_cast<int>(rank) + tid, to = min(row.slots, from - tid + slice);
-  const int threads = blockDim.x;
+  const int mine = to > from ? (to - from + threads - 1) / threads : 0;   // this thread's slots
+  float4* x = s_x + tid;
   if (tid == 0) s_index = INT_MAX;
   pdl_wait();
+  for (int e = 0, s = from; e < mine; ++e, s += threads) {
+    if (row.whole(s))
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(x + e * threads)), "l"(row.at + 4ll * s) : "memory");
+    else
+      x[e * threads] = token_load_end(row.at, s, row.before, row.count, -INFINITY);
+  }
   const float temp = a.temperature ? a.temperature[which] : 1.f;
   const bool greedy = !(temp > 0.f);
-  float4 x[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const int s = from + e * threads;
-    x[e] = s < to ? row.load(row.at, s, -INFINITY) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-  }
+  const TokenHeat heat = token_heat(greedy ? 1.f : temp);
+  asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
   float top = -INFINITY;
-#pragma unroll
-  for (int e = 0; e < E; ++e) top = max_nan(max_nan(top, x[e].x, x[e].y), x[e].z, x[e].w);
+#pragma unroll 4
+  for (int e = 0; e < mine; ++e) {
+    const float4 v = x[e * threads];
+    top = max_nan(max_nan(top, v.x, v.y), v.z, v.w);
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
   if (lane == 0) s_top[warp] = top;
@@ -126,24 +148,25 @@ __global__ void __launch_bounds__(512, 2) token_probs_kernel(const __grid_consta
   for (int o = 8; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
   top = __shfl_sync(0xffffffffu, top, 0);
   float sum = 0.f;
-  const TokenHeat heat = token_heat(greedy ? 1.f : temp);
   if (greedy) {
     int index = INT_MAX;
-#pragma unroll
-    for (int e = E - 1; e >= 0; --e) {
+    for (int e = mine - 1; e >= 0; --e) {
+      const float4 v = x[e * threads];
       const int i = 4 * (from + e * threads) - row.before;
-      index = x[e].x == top ? i : x[e].y == top ? i + 1 : x[e].z == top ? i + 2 : x[e].w == top ? i + 3 : index;
+      index = v.x == top ? i : v.y == top ? i + 1 : v.z == top ? i + 2 : v.w == top ? i + 3 : index;
     }
     index = __reduce_min_sync(0xffffffffu, index);
     if (lane == 0 && index != INT_MAX) atomicMin(&s_index, index);
   } else {
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      x[e].x = token_weight(x[e].x - top, heat);
-      x[e].y = token_weight(x[e].y - top, heat);
-      x[e].z = token_weight(x[e].z - top, heat);
-      x[e].w = token_weight(x[e].w - top, heat);
-      sum += (x[e].x + x[e].y) + (x[e].z + x[e].w);
+#pragma unroll 2
+    for (int e = 0; e < mine; ++e) {
+      float4 v = x[e * threads];
+      v.x = token_weight(v.x - top, heat);
+      v.y = token_weight(v.y - top, heat);
+      v.z = token_weight(v.z - top, heat);
+      v.w = token_weight(v.w - top, heat);
+      sum += (v.x + v.y) + (v.z + v.w);
+      x[e * threads] = v;
     }
     sum = warp_sum(sum);
     if (lane == 0) s_sum[warp] = sum;
@@ -184,21 +207,23 @@ __global__ void __launch_bounds__(512, 2) token_probs_kernel(const __grid_consta
   if (all_top == -INFINITY) first = INT_MAX;
   float* out = a.out + which * a.out_stride - row.before;
   const bool aligned = (reinterpret_cast<uintptr_t>(out) & 15) == 0;
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
+#pragma unroll 2
+  for (int e = 0; e < mine; ++e) {
     const int s = from + e * threads;
-    if (s >= to) continue;
-    float p[4] = {x[e].x * by, x[e].y * by, x[e].z * by, x[e].w * by};   // NaN where by is
+    float4 v = x[e * threads];
     if (greedy) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) p[i] = bad ? by : 4 * s + i - row.before == first ? 1.f : 0.f;
-    }
-    if (aligned && row.whole(s)) {
-      *reinterpret_cast<float4*>(out + 4ll * s) = make_float4(p[0], p[1], p[2], p[3]);
+      const int i = first - (4 * s - row.before);
+      v = make_float4(i == 0 ? 1.f : 0.f, i == 1 ? 1.f : 0.f, i == 2 ? 1.f : 0.f, i == 3 ? 1.f : 0.f);
+      if (bad) v.x = v.y = v.z = v.w = by;
     } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (row.has(s, i)) out[4ll * s + i] = p[i];
+      v.x *= by, v.y *= by, v.z *= by, v.w *= by;   // NaN where by is
+    }
+    if (!row.whole(s)) {
+      token_store_end(out, s, row.before, row.count, v);
+    } else if (aligned) {
+      *reinterpret_cast<float4*>(out + 4ll * s) = v;
+    } else {
+      out[4ll * s] = v.x, out[4ll * s + 1] = v.y, out[4ll * s + 2] = v.z, out[4ll * s + 3] = v.w;
     }
   }
   if (ctas > 1) cluster_wait();
@@ -261,6 +286,7 @@ struct VerifyDraftsArgs {
   const float* uniforms;            // [batch][drafts + 1]
   int32_t *out, *accepted;          // [batch][drafts + 1], [batch]
   int drafts, vocab;
+  int steps;                        // of four values a thread in one round
 };
 
 // The sums of a block's threads, in every thread; order: lanes, then warps.
@@ -310,17 +336,16 @@ __device__ __forceinline__ int pick_lane(double sum, double before, double targe
 
 // A cluster per request.  Every CTA works out by itself how many drafts stay; then it sums up its slice of what is drawn from in
 // FP64, so that the drawn token does not depend on the order of the sums, and leaves every thread's sum of each step of
-// four values in shared memory (of a long vocabulary: of one round of E steps).  The CTAs exchange their sums, and the one
+// four values in shared memory (of a long vocabulary: of one round of 16 steps).  The CTAs exchange their sums, and the one
 // that holds the target looks for the token among its steps and warps, then lanes, and reads the last four values again.
-template <int E>
+constexpr int kVerifySteps = 16;
 __global__ void __launch_bounds__(512, 2) verify_drafts_kernel(const __grid_constant__ VerifyDraftsArgs a) {
-  constexpr int kBatch = E < 4 ? E : 4;
-  extern __shared__ double s_step[];   // [E][threads]
+  extern __shared__ double s_step[];   // [steps][threads]
   __shared__ int s_token;
-  __shared__ double s_warp[16], s_part[E * 16];
+  __shared__ double s_warp[16], s_part[kVerifySteps];
   __shared__ __align__(16) double s_mine[2];
   pdl_launch_dependents();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5, n = a.drafts;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5, n = a.drafts, steps = a.steps;
   uint32_t rank;
   const uint32_t ctas = token_cluster(&rank);
   const long long b = blockIdx.x / ctas;
@@ -355,13 +380,13 @@ __global__ void __launch_bounds__(512, 2) verify_drafts_kernel(const __grid_cons
   }
   const bool off_aligned = (reinterpret_cast<uintptr_t>(off) & 15) == 0;
   const int slice = (row.slots + static_cast<int>(ctas) - 1) / static_cast<int>(ctas), from = min(static_cast<long long>(row.slots), static_cast<long long>(slice) * rank);
-  const int to = min(static_cast<long long>(row.slots), static_cast<long long>(from) + slice), step = E * threads;
+  const int to = min(static_cast<long long>(row.slots), static_cast<long long>(from) + slice), step = steps * threads;
   // the four values of slot s, and what is taken off them
   auto load = [&](int s, float4& x, float4& y) {
     x = y = make_float4(0.f, 0.f, 0.f, 0.f);
     if (s >= to) return;
-    x = row.load(row.at, s, 0.f);
-    if (off) y = off_aligned ? row.load(off, s, 0.f) : row.load_parts(off, s, 0.f);
+    x = token_load(row, row.at, true, s, 0.f);
+    if (off) y = token_load(row, off, off_aligned, s, 0.f);
     if (s == gone_slot) {
       x.x = gone == 0 ? 0.f : x.x;
       x.y = gone == 1 ? 0.f : x.y;
@@ -374,16 +399,17 @@ __global__ void __launch_bounds__(512, 2) verify_drafts_kernel(const __grid_cons
     const bool more = have > less;
     return static_cast<double>(more ? have : 0.f) - static_cast<double>(more ? less : 0.f);
   };
-  // the steps of one round: this thread's sum
+  // the steps of one round: this thread's sum.  One walk over short code: every CTA fetches its instructions anew.
   auto sum_round = [&](int at) {
     double mine = 0;
+#pragma unroll 1
+    for (int e0 = 0; e0 < steps; e0 += 4) {
+      float4 x[4], y[4];
 #pragma unroll
-    for (int e0 = 0; e0 < E; e0 += kBatch) {
-      float4 x[kBatch], y[kBatch];
+      for (int e = 0; e < 4; ++e) load(e0 + e < steps ? at + (e0 + e) * threads + tid : to, x[e], y[e]);
 #pragma unroll
-      for (int e = 0; e < kBatch; ++e) load(at + (e0 + e) * threads + tid, x[e], y[e]);
-#pragma unroll
-      for (int e = 0; e < kBatch; ++e) {
+      for (int e = 0; e < 4; ++e) {
+        if (e0 + e >= steps) break;
         const double v = (rest(x[e].x, y[e].x) + rest(x[e].y, y[e].y)) + (rest(x[e].z, y[e].z) + rest(x[e].w, y[e].w));
         s_step[(e0 + e) * threads + tid] = v;
         mine += v;
@@ -435,39 +461,29 @@ __global__ void __launch_bounds__(512, 2) verify_drafts_kernel(const __grid_cons
           before = round.picked_before;
           sum_round(at);
         }
+        // the step: warp w sums up steps w, w + warps, ...
         if (tid == 0) s_token = -1;
-        double mine_of[E];
+        for (int e = warp; e < steps; e += warps) {
+          double v = 0;
+#pragma unroll 4
+          for (int i = lane; i < threads; i += 32) v += s_step[e * threads + i];
 #pragma unroll
-        for (int e = 0; e < E; ++e) mine_of[e] = s_step[e * threads + tid];
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-          for (int e = 0; e < E; ++e) mine_of[e] += __shfl_xor_sync(0xffffffffu, mine_of[e], o);
-        if (lane == 0) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) s_part[e * warps + warp] = mine_of[e];
+          for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+          if (lane == 0) s_part[e] = v;
         }
         __syncthreads();
-        // the step and warp, by every warp
-        constexpr int kEach = (E * 16 + 31) / 32;
-        double some_of[kEach], sum = 0;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-          some_of[i] = lane * kEach + i < E * warps ? s_part[lane * kEach + i] : 0.0;
-          sum += some_of[i];
-        }
-        double upto = 0;
-        const int who = pick_lane(sum, before, target, &upto);
-        Pick part;
-        part.before = upto;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) part.part(lane * kEach + i, some_of[i], target);
-        const int picked = __shfl_sync(0xffffffffu, part.picked, who);
-        before = __shfl_sync(0xffffffffu, part.picked_before, who);
-        if (picked >= 0 && picked % warps == warp) {
-          const int e = picked / warps;
-          if (lane == pick_lane(s_step[e * threads + tid], before, target, &upto)) {
-            const int s = at + e * threads + tid;
+        if (warp == 0) {            // the step, the warp's worth of threads, the thread, its value
+          double upto = 0;
+          const int e = pick_lane(lane < steps ? s_part[lane] : 0.0, before, target, &upto);
+          before = __shfl_sync(0xffffffffu, upto, e);
+          double v = 0;
+#pragma unroll 4
+          for (int i = 0; i < warps; ++i) v += s_step[e * threads + lane * warps + i];
+          const int part = pick_lane(v, before, target, &upto);
+          before = __shfl_sync(0xffffffffu, upto, part);
+          const int place = pick_lane(lane < warps ? s_step[e * threads + part * warps + lane] : 0.0, before, target, &upto);
+          if (lane == place) {
+            const int s = at + e * threads + part * warps + place;
             float4 x, y;
             load(s, x, y);
             Pick value;

@@ -111,9 +111,9 @@ int launch_linear(W4LinearArgs& a, cudaStream_t st) {
 // Rows beyond which the tensor-memory kernel takes over.
 #ifdef W4_DEV
 #include <cstdlib>
-int most_mma_rows() { return getenv("W4_MMA") ? atoi(getenv("W4_MMA")) : 8; }
+int most_mma_rows() { return getenv("W4_MMA") ? atoi(getenv("W4_MMA")) : 16; }
 #else
-constexpr int most_mma_rows() { return 8; }
+constexpr int most_mma_rows() { return 16; }
 #endif
 
 struct TcPlan {
@@ -153,20 +153,7 @@ int launch_tc(const W4LinearArgs& a, void* workspace, cudaStream_t st) {
 
 template <int G>
 int launch_linear(W4LinearArgs& a, void* workspace, cudaStream_t st) {
-#ifdef W4_DEV
-  const int v = getenv("W4_V") ? atoi(getenv("W4_V")) : 0;
-  if (v == 1) return launch_linear<1, 2, G, 16>(a, st);
-  if (v == 2) return launch_linear<1, 4, G, 8>(a, st);
-  if (v == 3) return launch_linear<2, 2, G, 16>(a, st);
-  if (v == 4) return launch_linear<2, 4, G, 8>(a, st);
-  if (v == 5) return launch_linear<2, 2, G, 8>(a, st);
-  if (v == 6) return launch_linear<4, 2, G, 8>(a, st);
-  if (v == 7) return launch_linear<4, 4, G, 8>(a, st);
-  if (v == 8) return launch_linear<3, 4, G, 8>(a, st);
-  if (v == 9) return launch_linear<3, 2, G, 8>(a, st);
-  if (v == 10) return launch_linear<2, 2, G, 12>(a, st);
-#endif
-  if (a.rows <= most_mma_rows()) return a.rows <= 8 ? launch_linear<1, 2, G, 16>(a, st) : launch_linear<2, 2, G, 16>(a, st);
+  if (a.rows <= most_mma_rows()) return a.rows <= 8 ? launch_linear<1, 2, G, 16>(a, st) : launch_linear<2, 2, G, 12>(a, st);
   return a.rows <= 16 ? launch_tc<16, G>(a, workspace, st) : a.rows <= 32 ? launch_tc<32, G>(a, workspace, st) : launch_tc<64, G>(a, workspace, st);
 }
 

@@ -291,22 +291,22 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
       const float* from = args.parts + ((static_cast<long long>(c0) * 2 + (w4_run(c0, units, ctas) >= unit ? 0 : 1)) * N) * kW4TcTile + row;
       const float* more = args.parts + (static_cast<long long>(c0 + 1) * 2 * N) * kW4TcTile + row;
 #pragma unroll 1
-      for (int j0 = 0; j0 < a.rows; j0 += 8) {
-        float v[8];
+      for (int j0 = 0; j0 < a.rows; j0 += 16) {
+        float v[16];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j0 + j < a.rows ? __ldcg(from + (j0 + j) * kW4TcTile) : 0.f;
+        for (int j = 0; j < 16; ++j) v[j] = j0 + j < a.rows ? __ldcg(from + (j0 + j) * kW4TcTile) : 0.f;
 #pragma unroll 1
-        for (int c = c0; c < c1; c += 2) {
-          float x[2][8];
+        for (int c = c0; c < c1; c += 2) {   // mostly once: its loads do not wait for the first
+          float x[2][16];
 #pragma unroll
           for (int o = 0; o < 2; ++o)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[o][j] = c + o < c1 && j0 + j < a.rows ? __ldcg(more + (static_cast<long long>(c + o - c0) * 2 * N + j0 + j) * kW4TcTile) : 0.f;
+            for (int j = 0; j < 16; ++j) x[o][j] = c + o < c1 && j0 + j < a.rows ? __ldcg(more + (static_cast<long long>(c + o - c0) * 2 * N + j0 + j) * kW4TcTile) : 0.f;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = (v[j] + x[0][j]) + x[1][j];
+          for (int j = 0; j < 16; ++j) v[j] = (v[j] + x[0][j]) + x[1][j];
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w4_store(a, j0 + j, out, v[j]);
+        for (int j = 0; j < 16; ++j) w4_store(a, j0 + j, out, v[j]);
       }
     };
     for (int i = 0; i < count; ++i) {
