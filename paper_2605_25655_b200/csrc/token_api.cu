@@ -10,20 +10,20 @@ namespace {
 
 constexpr int64_t kFar = int64_t{1} << 50;   // elements: no product below leaves 64 bits
 
-// Clusters of up to 8 CTAs for rows of `slots` 16-byte slots, with up to `most` slots a thread: as many CTAs as hold a row, and
-// as many as the device has room for (two on an SM) while a CTA has more than 256 slots.
+// Clusters of up to 8 CTAs for rows of `slots` 16-byte slots, with up to `most` slots in a CTA's slice: as many CTAs as hold a row,
+// and as many as the device has room for (two on an SM) while a CTA has more than 256 slots.
 struct RowPlan {
   unsigned ctas, threads;
-  int slots;   // a thread
+  int each;   // slots of a thread
 };
-RowPlan plan_rows(int64_t rows, int64_t slots, int most) {
-  RowPlan p{1, 512, 1};
+RowPlan plan_rows(int64_t rows, int64_t slots, int64_t most, int64_t threads) {
+  RowPlan p{1, 0, 1};
   const int64_t room = static_cast<int64_t>(op_sm_count()) * 2;
-  while (p.ctas < 8 && (slots > static_cast<int64_t>(p.ctas) * 512 * most || (rows * p.ctas * 2 <= room && slots > p.ctas * 256))) p.ctas *= 2;
-  const int64_t slice = (slots + p.ctas - 1) / p.ctas;
-  p.slots = static_cast<int>((slice + 511) / 512 < most ? (slice + 511) / 512 : most);
-  const int64_t each = (slice + p.slots - 1) / p.slots;
-  p.threads = each >= 512 ? 512 : static_cast<unsigned>((each + 31) / 32 * 32);
+  while (p.ctas < 8 && (slots > p.ctas * most || (rows * p.ctas * 2 <= room && slots > p.ctas * 256))) p.ctas *= 2;
+  int64_t slice = (slots + p.ctas - 1) / p.ctas;
+  if (slice > most) slice = most;
+  p.each = static_cast<int>((slice + threads - 1) / threads);
+  p.threads = static_cast<unsigned>(((slice + p.each - 1) / p.each + 31) / 32 * 32);
   return p;
 }
 
@@ -52,12 +52,13 @@ int thinfer_op_token_probs(const float* logits, int64_t logit_stride, const floa
   a.vocab = vocab;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const int64_t slots = (static_cast<int64_t>(vocab) + 6) / 4;   // wherever a row begins
-  constexpr int kMost = 27;                                      // slots a thread: 216 KB
-  if (slots > 8 * 512 * kMost) return op_launch(token_probs_long_kernel, dim3(static_cast<unsigned>(rows)), dim3(512), 0, st, a);
-  const RowPlan plan = plan_rows(rows, slots, slots > 8 * 512 * 8 ? kMost : 8);
+  constexpr int64_t kUsual = 4096, kMost = 27 * 512;             // of a slice: 64 and 216 KB
+  if (slots > 8 * kMost) return op_launch(token_probs_long_kernel, dim3(static_cast<unsigned>(rows)), dim3(512), 0, st, a);
+  // 16 slots a thread where a device full of such slices has fewer threads to set up (MEASURED), else 512 threads for latency
+  const RowPlan plan = plan_rows(rows, slots, slots > 8 * kUsual ? kMost : kUsual, rows * slots > 1 << 19 ? 256 : 512);
   const int64_t ctas = static_cast<int64_t>(rows) * plan.ctas;
   if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "token_probs: too many rows");
-  const size_t smem = static_cast<size_t>(plan.slots) * plan.threads * 16;
+  const size_t smem = static_cast<size_t>(plan.each) * plan.threads * 16;
   const int rc = opt_in<token_probs_kernel>(smem);
   if (rc != THINFER_OK) return rc;
   return op_launch_clusters(token_probs_kernel, plan.ctas, dim3(static_cast<unsigned>(ctas)), dim3(plan.threads), smem, st, a);
@@ -98,11 +99,11 @@ int thinfer_op_verify_drafts(const float* p, int64_t p_batch_stride, int64_t p_r
   a.accepted = accepted;
   a.drafts = n_drafts;
   a.vocab = vocab;
-  const RowPlan plan = plan_rows(batch, (static_cast<int64_t>(vocab) + 6) / 4, kVerifySteps);
+  const RowPlan plan = plan_rows(batch, (static_cast<int64_t>(vocab) + 6) / 4, kVerifySteps * 512, 512);
   const int64_t ctas = static_cast<int64_t>(batch) * plan.ctas;
   if (ctas > 0x7fffffff) return op_fail(THINFER_EUNSUPPORTED, "verify_drafts: too many requests");
-  a.steps = plan.slots;
-  const size_t smem = static_cast<size_t>(plan.slots) * plan.threads * 8;
+  a.steps = plan.each;
+  const size_t smem = static_cast<size_t>(plan.each) * plan.threads * 8;
   const int rc = opt_in<verify_drafts_kernel>(smem);
   if (rc != THINFER_OK) return rc;
   return op_launch_clusters(verify_drafts_kernel, plan.ctas, dim3(static_cast<unsigned>(ctas)), dim3(plan.threads), smem, static_cast<cudaStream_t>(cuda_stream), a);

@@ -16,20 +16,29 @@ struct TokenProbsArgs {
 };
 
 // exp(d / T) for d <= 0, with log2(e) / T = high + low: what the product loses comes back as a factor, so that the exponent
-// of a far logit is as exact as d itself.  Weights below 2^-126 are 0.
+// of a far logit is as exact as d itself.  Weights below 2^-126 are 0, those of -inf and NaN too.  Temperatures above 10^30 count as that.
 struct TokenHeat {
-  float high, low;
+  float high, low, rest, least;   // rest = low * ln 2; least: where the exponent is -200
 };
 __device__ __forceinline__ TokenHeat token_heat(float temperature) {
   constexpr float kLog = 1.44269504088896f, kRest = 1.92596299e-8f;   // log2(e) and what FP32 leaves of it
-  const float high = kLog / temperature;
-  if (!(high <= 3e38f)) return {3e38f, 0.f};
-  if (high < 1e-30f) return {high, 0.f};   // an infinite temperature too
-  return {high, (fmaf(-high, temperature, kLog) + kRest) / temperature};
+  const float high = fminf(fmaxf(kLog / temperature, 1e-30f), 3e38f);
+  const float low = temperature > 1e-37f && temperature < 1e30f ? (fmaf(-high, temperature, kLog) + kRest) / temperature : 0.f;
+  return {high, low, low * 0.693147180559945f, -200.f / high};
 }
 __device__ __forceinline__ float token_weight(float d, const TokenHeat& h) {
-  const float a = d * h.high, rest = fmaf(d, h.low, fmaf(d, h.high, -a)) * 0.693147180559945f, w = ex2_approx(a);
-  return a >= -127.f ? fmaf(w, rest, w) : 0.f;   // 0 for -inf too, whatever the temperature, and for NaN
+  d = fmaxf(d, h.least);
+  const float a = d * h.high, rest = fmaf(fmaf(d, h.high, -a), 0.693147180559945f, d * h.rest), w = ex2_approx(a);
+  return fmaf(w, rest, w);
+}
+// Two at a time.
+__device__ __forceinline__ uint64_t token_weights(float x, float y, float top, const TokenHeat& h) {
+  const uint64_t d = f32x2(fmaxf(x - top, h.least), fmaxf(y - top, h.least)), high = f32x2(h.high, h.high), a = mul_f32x2(d, high);
+  const float2 e = f32x2_unpack(a);
+  const uint64_t less = fma_f32x2(d, high, f32x2(-e.x, -e.y));
+  const uint64_t rest = fma_f32x2(less, f32x2(0.693147180559945f, 0.693147180559945f), mul_f32x2(d, f32x2(h.rest, h.rest)));
+  const uint64_t w = f32x2(ex2_approx(e.x), ex2_approx(e.y));
+  return fma_f32x2(w, rest, w);
 }
 // The larger one; NaN where there is one.
 __device__ __forceinline__ float max_nan(float a, float b) {
@@ -158,16 +167,16 @@ __global__ void __launch_bounds__(512, 3) token_probs_kernel(const __grid_consta
     index = __reduce_min_sync(0xffffffffu, index);
     if (lane == 0 && index != INT_MAX) atomicMin(&s_index, index);
   } else {
+    uint64_t sums = f32x2(0.f, 0.f);
 #pragma unroll 2
     for (int e = 0; e < mine; ++e) {
       float4 v = x[e * threads];
-      v.x = token_weight(v.x - top, heat);
-      v.y = token_weight(v.y - top, heat);
-      v.z = token_weight(v.z - top, heat);
-      v.w = token_weight(v.w - top, heat);
-      sum += (v.x + v.y) + (v.z + v.w);
-      x[e * threads] = v;
+      const uint64_t lo = token_weights(v.x, v.y, top, heat), hi = token_weights(v.z, v.w, top, heat);
+      sums = add_f32x2(sums, add_f32x2(lo, hi));
+      *reinterpret_cast<ulonglong2*>(x + e * threads) = make_ulonglong2(lo, hi);
     }
+    const float2 both = f32x2_unpack(sums);
+    sum = both.x + both.y;
     sum = warp_sum(sum);
     if (lane == 0) s_sum[warp] = sum;
   }
@@ -460,6 +469,7 @@ __global__ void __launch_bounds__(512, 2) verify_drafts_kernel(const __grid_cons
           at = from + round.picked * step;
           before = round.picked_before;
           sum_round(at);
+          __syncthreads();
         }
         // the step: warp w sums up steps w, w + warps, ...
         if (tid == 0) s_token = -1;
