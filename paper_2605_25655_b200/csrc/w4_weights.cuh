@@ -106,33 +106,57 @@ __device__ __forceinline__ half_t w4_round(double x) {
 }
 
 // Scale and zero point of a group with these extremes (high >= 0, low = -min >= 0, NaN if one of its values is).
-// The exact (high + low) / 15 decides: FP64 holds the sum of two FP16 numbers, and where it rounds that of two BF16
-// numbers or the quotient, what is rounded away is far smaller than the distance to the middle of two 16-bit numbers.
 struct W4Scale {
   half_t scale;
   float scaled, inverse, zero;   // scale * by; what a weight * by is multiplied by; the zero point
   float by;                      // 2^100 for BF16 scales whose inverse leaves FP32
+  bool plain;                    // by is 1, and no weight comes out below -zero
 };
-__device__ __forceinline__ W4Scale w4_scale(half2_t extremes) {
-  const float2 e = h2_to_f2(extremes);
+
+// (high + low) / 15 in the storage type, rounded once: sum and quotient are rounded to odd in FP32, which keeps on which side
+// of the middle of two 16-bit numbers the exact quotient is.  What FP32 cannot hold on the way goes through FP64, where
+// the sum of two FP16 numbers is exact and what is rounded away of BF16 numbers is far smaller than the distance to a middle.
+__device__ __forceinline__ half_t w4_fifteenth(float high, float low) {
+  const float range = high + low;
+  if (kStorageType == 1 && !(range >= 0x1p-90f && range <= 0x1p120f)) return w4_round((static_cast<double>(high) + static_cast<double>(low)) / 15.0);
+  float sum = __fadd_rz(high, low);
+  if (sum != __fadd_ru(high, low)) sum = __uint_as_float(__float_as_uint(sum) | 1u);
+  constexpr float kInverse = 1.f / 15.f;
+  float q = sum * kInverse;
+  q = fmaf(fmaf(-15.f, q, sum), kInverse, q);
+  const float left = fmaf(-15.f, q, sum);   // exact
+  uint32_t bits = __float_as_uint(q);
+  if (left < 0.f) --bits;
+  if (left != 0.f) bits |= 1u;
+  return f_to_h(__uint_as_float(bits));
+}
+
+__device__ __forceinline__ W4Scale w4_scale(float high, float low) {
   W4Scale s{};
   s.by = 1.f;
-  const float range = e.x + e.y;
-  if (!(e.x <= 3.4e38f && e.y <= 3.4e38f)) {   // a NaN or an infinity: the group reads as NaN
+  s.plain = true;
+  s.scale = f_to_h(0.f);
+  if (!(high <= 3.4e38f && low <= 3.4e38f)) {   // a NaN or an infinity: the group reads as NaN
     s.scale = f_to_h(__int_as_float(0x7fffffff));
+    s.plain = false;
     return s;
   }
-  if (range == 0.f) {
-    s.scale = f_to_h(0.f);
-    return s;
-  }
-  s.scale = w4_round((static_cast<double>(e.x) + static_cast<double>(e.y)) / 15.0);
+  if (high == 0.f && low == 0.f) return s;
+  s.scale = w4_fifteenth(high, low);
   s.scaled = h_to_f(s.scale);
-  if (s.scaled == 0.f) return s;
-  if (kStorageType == 1 && s.scaled < 0x1p-100f) s.by = 0x1p100f;
+  if (s.scaled == 0.f) {
+    s.plain = false;
+    return s;
+  }
+  if (kStorageType == 1 && s.scaled < 0x1p-100f) {
+    s.by = 0x1p100f;
+    s.plain = false;
+  }
   s.scaled *= s.by;
-  s.inverse = 1.f / s.scaled;
-  s.zero = fminf(rintf(e.y * s.by / s.scaled), 15.f);
+  s.inverse = __frcp_rn(s.scaled);
+  const float w = low * s.by, q = w * s.inverse, zero = rintf(fmaf(fmaf(-s.scaled, q, w), s.inverse, q));
+  s.zero = fminf(zero, 15.f);
+  s.plain = s.plain && zero <= 15.f;
   return s;
 }
 
@@ -144,8 +168,22 @@ __device__ __forceinline__ uint32_t w4_code(float w, const W4Scale& s) {
   const float q = w * s.inverse, r = fmaf(fmaf(-s.scaled, q, w), s.inverse, q);
   return __float_as_uint(fminf(fmaxf(r, -s.zero), 15.f - s.zero) + 12582912.f);
 }
+// The same for two weights of a plain group: with zero = rint(low / scale) none comes out below -zero.
+struct W4Plain {
+  uint64_t inverse, scaled;   // twice; -scaled
+  float most;
+};
+__device__ __forceinline__ uint2 w4_codes(half2_t w, const W4Plain& s) {
+  const float2 f = h2_to_f2(w);
+  const uint64_t x = f32x2(f.x, f.y), q = mul_f32x2(x, s.inverse);
+  const float2 r = f32x2_unpack(fma_f32x2(fma_f32x2(s.scaled, q, x), s.inverse, q));
+  const float2 c = f32x2_unpack(add_f32x2(f32x2(fminf(r.x, s.most), fminf(r.y, s.most)), f32x2(12582912.f, 12582912.f)));
+  return make_uint2(__float_as_uint(c.x), __float_as_uint(c.y));
+}
 
-// One warp per tile and block, 8 loads of 16 bytes in flight per lane: rows g and 8 + g, columns 32 q + 8 t ..
+// One warp per tile and block, 8 loads of 16 bytes in flight per lane: rows g and 8 + g, columns 32 q + 8 t ..  Bound by memory
+// with groups of 128 columns.  A word's eight codes are summed up as they come (the word so far times 16 plus the next),
+// and what 1.5 * 2^23 and the zero points add comes off once a word.
 template <int G>
 __global__ void __launch_bounds__(256) w4_quantize_kernel(const __grid_constant__ W4QuantizeArgs a) {
   constexpr int P = 128 / G;
@@ -164,62 +202,116 @@ __global__ void __launch_bounds__(256) w4_quantize_kernel(const __grid_constant_
       for (int q = 0; q < 4; ++q)
         raw[i][q] = row < a.n && col + 32 * q < a.k ? ld_stream(a.w + row * a.stride + col + 32 * q) : make_uint4(0, 0, 0, 0);
     }
-    W4Scale s[2][P];
+    // (largest, largest negated) of every group, in all four lanes of its rows
+    half2_t ends[2][P];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int p = 0; p < P; ++p) {
-        half2_t high = f2_to_h2(0.f, 0.f), low = high;   // largest values, largest negated values
+        half2_t high = f2_to_h2(0.f, 0.f), low = high;
 #pragma unroll
         for (int q = p * 4 / P; q < (p + 1) * 4 / P; ++q) {
           const half2_t* h = reinterpret_cast<const half2_t*>(&raw[i][q]);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             high = __hmax2_nan(high, h[j]);
-            low = __hmax2_nan(low, __hneg2(h[j]));
+            low = __hmin2_nan(low, h[j]);
           }
         }
-        // (largest, largest negated)
+        low = __hneg2(low);
         half2_t both = __hmax2_nan(w4_pair<0x5410>(high, low), w4_pair<0x7632>(high, low));
 #pragma unroll
         for (int o = 1; o <= 2; o <<= 1) {
           const uint32_t other = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<uint32_t*>(&both), o);
           both = __hmax2_nan(both, *reinterpret_cast<const half2_t*>(&other));
         }
-        s[i][p] = w4_scale(both);
+        ends[i][p] = both;
       }
+    // lane t works out the parameters of group t % P of both rows
+    W4Scale own[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      half2_t mine = ends[i][0];
+#pragma unroll
+      for (int p = 1; p < P; ++p) mine = t % P == p ? ends[i][p] : mine;
+      const float2 e = h2_to_f2(mine);
+      own[i] = w4_scale(e.x, e.y);
     }
+    const long long at = (u * 8 + g) * P + t;
+    if (t < P) {
+      reinterpret_cast<half2_t*>(a.v.scales)[at] = half2_t(own[0].scale, own[1].scale);
+      a.v.zeros[at] = static_cast<uint8_t>(static_cast<uint32_t>(own[0].zero) | static_cast<uint32_t>(own[1].zero) << 4);
+    }
+    const bool plain = __all_sync(0xffffffffu, own[0].plain && own[1].plain);
+    auto of = [&](float v, int p) { return P == 1 ? v : __shfl_sync(0xffffffffu, v, (lane & 28) + p); };
+    constexpr uint32_t kMagic = 0x4b400000u * 0x11111111u;
     uint32_t words[8];
+    if (plain) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+      for (int p = 0; p < P; ++p) {
+        W4Plain s[2];
+        float zero[2];
 #pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        // nibble 4 e + 2 b + i, highest first: sums of whole numbers shifted by four; the constants come off at the end
-        uint32_t w = 0;
+        for (int i = 0; i < 2; ++i) {
+          const float scaled = of(own[i].scaled, p), inverse = of(own[i].inverse, p);
+          zero[i] = of(own[i].zero, p);
+          s[i] = {f32x2(inverse, inverse), f32x2(-scaled, -scaled), 15.f - zero[i]};
+        }
+        const uint32_t less = static_cast<uint32_t>(zero[0]) * 0x01010101u + static_cast<uint32_t>(zero[1]) * 0x10101010u - kMagic;
 #pragma unroll
-        for (int e = 1; e >= 0; --e)
+        for (int q = p * 4 / P; q < (p + 1) * 4 / P; ++q)
 #pragma unroll
-          for (int b = 1; b >= 0; --b)
+          for (int st = 0; st < 2; ++st) {
+            uint2 c[2][2];           // [b][i]
 #pragma unroll
-            for (int i = 1; i >= 0; --i) {
-              const half2_t h = reinterpret_cast<const half2_t*>(&raw[i][q])[2 * st + b];
-              const float2 f = h2_to_f2(h);
-              const W4Scale& sc = s[i][q * P / 4];
-              w = (w << 4) + w4_code(e ? f.y : f.x, sc) - 0x4b400000u + static_cast<uint32_t>(sc.zero);
-            }
-        words[2 * q + st] = col + 32 * q < a.k ? w : 0u;
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) c[b][i] = w4_codes(reinterpret_cast<const half2_t*>(&raw[i][q])[2 * st + b], s[i]);
+            uint32_t w = c[1][1].y;   // nibble 4 e + 2 b + i, highest first
+            w = w * 16u + c[1][0].y;
+            w = w * 16u + c[0][1].y;
+            w = w * 16u + c[0][0].y;
+            w = w * 16u + c[1][1].x;
+            w = w * 16u + c[1][0].x;
+            w = w * 16u + c[0][1].x;
+            w = w * 16u + c[0][0].x;
+            words[2 * q + st] = w + less;
+          }
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        W4Scale s[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          s[i].scaled = of(own[i].scaled, q * P / 4);
+          s[i].inverse = of(own[i].inverse, q * P / 4);
+          s[i].zero = of(own[i].zero, q * P / 4);
+          s[i].by = of(own[i].by, q * P / 4);
+        }
+#pragma unroll 1
+        for (int st = 0; st < 2; ++st) {
+          uint32_t w = 0;
+#pragma unroll
+          for (int n = 7; n >= 0; --n) {   // nibble 4 e + 2 b + i
+            const uint4& from = raw[n & 1][q];
+            const uint32_t pair = st == 0 ? (n & 2 ? from.y : from.x) : (n & 2 ? from.w : from.z);
+            const float2 f = h2_to_f2(*reinterpret_cast<const half2_t*>(&pair));
+            w = w * 16u + w4_code(n & 4 ? f.y : f.x, s[n & 1]) - 0x4b400000u + static_cast<uint32_t>(s[n & 1].zero);
+          }
+          if (st == 0)
+            words[2 * q] = w;
+          else
+            words[2 * q + 1] = w;
+        }
       }
     }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (col + 32 * q >= a.k) words[2 * q] = words[2 * q + 1] = 0;
     uint4* out = reinterpret_cast<uint4*>(a.v.codes + u * 1024) + lane;
     out[0] = make_uint4(words[0], words[1], words[2], words[3]);
     out[32] = make_uint4(words[4], words[5], words[6], words[7]);
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      if (t != p) continue;
-      const long long at = (u * 8 + g) * P + p;
-      reinterpret_cast<half2_t*>(a.v.scales)[at] = half2_t(s[0][p].scale, s[1][p].scale);
-      a.v.zeros[at] = static_cast<uint8_t>(static_cast<uint32_t>(s[0][p].zero) | static_cast<uint32_t>(s[1][p].zero) << 4);
-    }
   }
 }
 
