@@ -66,6 +66,10 @@ struct LinearPlan {
   size_t smem;
 };
 
+#ifdef W4_DEV
+#include <cstdio>
+#include <cstdlib>
+#endif
 // Cluster size by the bytes that the busiest CTA moves: weights, its share of the tokens (from L2, at half price), and what a
 // round of sums at the end costs in bytes that could have been read meanwhile.
 int plan_linear(int tiles, int blocks, int rows, int nt, int r, int warps, int stage, int token_tiles, LinearPlan* best) {
@@ -76,6 +80,9 @@ int plan_linear(int tiles, int blocks, int rows, int nt, int r, int warps, int s
   for (int log2 = 0; log2 <= 3; ++log2) {
     const int64_t ctas = 1 << log2;
     if (ctas > blocks) break;
+#ifdef W4_DEV
+    if (getenv("W4_C") && atoi(getenv("W4_C")) != ctas) continue;
+#endif
     int active = 0;
     const int rc = active_clusters(log2, &active);
     if (rc != THINFER_OK) return rc;
@@ -84,7 +91,10 @@ int plan_linear(int tiles, int blocks, int rows, int nt, int r, int warps, int s
     const int64_t slice = (blocks + ctas - 1) / ctas, phases = (slice + most - 1) / most, held = (slice + phases - 1) / phases;
     const int64_t per = (groups + clusters - 1) / clusters, room = (kLinearSmem - ring - held * per_block) / per_group - (warps - 1);
     const int64_t batches = (per + room - 1) / room, batch = (per + batches - 1) / batches;
-    const int64_t cost = per * slice * r * 1064 + (phases > 1 ? batches : 1) * slice * tokens * 128 + (batches * phases - 1) * 40000 + log2 * 2000;
+    const int64_t cost = per * slice * r * 1064 + (phases > 1 ? batches : 1) * slice * tokens * 128 + (batches * phases - 1) * 25000 + log2 * 6000 + (log2 == 3 ? 12000 : 0);
+#ifdef W4_DEV
+    if (getenv("W4_PRINT")) printf("C %d clusters %d per %d slice %d phases %d batches %d cost %d\n", (int)ctas, (int)clusters, (int)per, (int)slice, (int)phases, (int)batches, (int)cost);
+#endif
     if (cost >= least) continue;
     least = cost;
     best->cluster = static_cast<int>(ctas);

@@ -185,7 +185,7 @@ __device__ __forceinline__ uint2 w4_codes(half2_t w, const W4Plain& s) {
 // with groups of 128 columns.  A word's eight codes are summed up as they come (the word so far times 16 plus the next),
 // and what 1.5 * 2^23 and the zero points add comes off once a word.
 template <int G>
-__global__ void __launch_bounds__(256) w4_quantize_kernel(const __grid_constant__ W4QuantizeArgs a) {
+__global__ void __launch_bounds__(256, 3) w4_quantize_kernel(const __grid_constant__ W4QuantizeArgs a) {
   constexpr int P = 128 / G;
   pdl_launch_dependents();
   pdl_wait();
