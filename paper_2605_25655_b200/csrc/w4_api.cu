@@ -118,53 +118,59 @@ int launch_linear(W4LinearArgs& a, cudaStream_t st) {
   return op_launch_clusters(w4_linear_kernel<NT, R, G, Warps>, static_cast<unsigned>(p.cluster), dim3(static_cast<unsigned>(p.cluster * p.clusters), static_cast<unsigned>(token_tiles)),
                             dim3(Warps * 32), p.smem, st, a);
 }
-// Rows beyond which the tensor-memory kernel takes over.
+// The tensor-memory kernel for more than 16 rows and large matrices.  In front of and behind its stream it has some 15 us of its own
+// (tokens laid out, partial sums), while the other one walks over the weights again for every 16 rows.  us, here and there:
+// MEASURED_CROSS
+bool on_tensor_memory(int64_t rows, int64_t tiles, int64_t blocks, int group) {
 #ifdef W4_DEV
-#include <cstdlib>
-int most_mma_rows() { return getenv("W4_MMA") ? atoi(getenv("W4_MMA")) : 16; }
-#else
-constexpr int most_mma_rows() { return 16; }
+  if (getenv("W4_MMA")) return rows > atoi(getenv("W4_MMA"));
 #endif
+  return rows > 16 && tiles * blocks > (group == 32 ? 48 : 32) * 1024;
+}
 
 struct TcPlan {
   long long row_tiles;
   int ctas;
-  size_t token_bytes, part_bytes, arrived_bytes;
-  size_t bytes() const { return token_bytes + part_bytes + arrived_bytes; }
+  size_t token_bytes, part_bytes;
+  size_t bytes() const { return token_bytes + part_bytes; }
 };
-int tc_tokens(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+int tc_tokens(int rows) { return rows <= 32 ? 32 : 64; }
 TcPlan plan_tc(int n, int64_t tiles, int64_t blocks) {
   TcPlan p{};
   p.row_tiles = (tiles * 16 + kW4TcTile - 1) / kW4TcTile;
-  const int64_t units = p.row_tiles * blocks;
+  // as many CTAs as the device has SMs, but no more than 8 for a row tile, whose sums one thread adds up
+  const int64_t most = blocks < 8 ? p.row_tiles * blocks : p.row_tiles * 8;
   const int sms = op_sm_count();
-  p.ctas = units < sms ? static_cast<int>(units) : sms;
+  p.ctas = most < sms ? static_cast<int>(most) : sms;
   p.token_bytes = static_cast<size_t>(blocks) * n * 256;
   p.part_bytes = static_cast<size_t>(p.ctas) * 2 * n * kW4TcTile * 4;
-  p.arrived_bytes = static_cast<size_t>(p.row_tiles) * kW4TcGroups * 4;
   return p;
 }
-size_t linear_workspace(int32_t rows, int32_t n_out, int32_t k) { return rows <= most_mma_rows() ? 0 : plan_tc(tc_tokens(rows), w4_tiles(n_out), w4_blocks(k)).bytes(); }
+size_t linear_workspace(int32_t rows, int32_t n_out, int32_t k, int32_t group) {
+  return on_tensor_memory(rows, w4_tiles(n_out), w4_blocks(k), group) ? plan_tc(tc_tokens(rows), w4_tiles(n_out), w4_blocks(k)).bytes() : 0;
+}
 
 template <int N, int G>
 int launch_tc(const W4LinearArgs& a, void* workspace, cudaStream_t st) {
   constexpr int P = 128 / G, kSmem = W4Tc<N, P>::kSmem;
   const TcPlan p = plan_tc(N, a.v.tiles, a.v.blocks);
   char* ws = static_cast<char*>(workspace);
-  const W4TcArgs args{a, reinterpret_cast<uint8_t*>(ws), reinterpret_cast<float*>(ws + p.token_bytes), reinterpret_cast<int*>(ws + p.token_bytes + p.part_bytes), p.row_tiles};
+  const W4TcArgs args{a, reinterpret_cast<uint8_t*>(ws), reinterpret_cast<float*>(ws + p.token_bytes), p.row_tiles};
   CUtensorMap codes, scales;
   if (!op_tensor_map(&codes, a.v.codes, 256, a.v.blocks, a.v.tiles, kW4TcGroups * 8) || !op_tensor_map(&scales, a.v.scales, 8 * P, a.v.blocks, a.v.tiles, kW4TcGroups * 8))
     return op_fail(THINFER_ECUDA, "cuTensorMapEncodeTiled failed for packed weights");
   int rc = opt_in<w4_linear_tc_kernel<N, P>>(kSmem);
   if (rc == THINFER_OK) rc = op_launch(w4_tokens_kernel<N>, dim3(static_cast<unsigned>((a.v.blocks * N * 16 + 255) / 256)), dim3(256), 0, st, args);
   if (rc == THINFER_OK) rc = op_launch(w4_linear_tc_kernel<N, P>, dim3(static_cast<unsigned>(p.ctas)), dim3(kW4TcTile + 128), kSmem, st, args, codes, scales);
+  if (rc == THINFER_OK)
+    rc = op_launch(w4_linear_join_kernel<N>, dim3(static_cast<unsigned>(p.row_tiles * kW4TcGroups), static_cast<unsigned>((a.rows + 15) / 16)), dim3(512), 0, st, args, p.ctas);
   return rc;
 }
 
 template <int G>
 int launch_linear(W4LinearArgs& a, void* workspace, cudaStream_t st) {
-  if (a.rows <= most_mma_rows()) return a.rows <= 8 ? launch_linear<1, 2, G, 16>(a, st) : launch_linear<2, 2, G, 12>(a, st);
-  return a.rows <= 16 ? launch_tc<16, G>(a, workspace, st) : a.rows <= 32 ? launch_tc<32, G>(a, workspace, st) : launch_tc<64, G>(a, workspace, st);
+  if (!on_tensor_memory(a.rows, a.v.tiles, a.v.blocks, G)) return a.rows <= 8 ? launch_linear<1, 2, G, 16>(a, st) : launch_linear<2, 2, G, 12>(a, st);
+  return a.rows <= 32 ? launch_tc<32, G>(a, workspace, st) : launch_tc<64, G>(a, workspace, st);
 }
 
 }  // namespace
@@ -220,7 +226,7 @@ int thinfer_w4_linear_workspace(int32_t rows, int32_t n_out, int32_t k, int32_t 
   if (rc != THINFER_OK) return rc;
   if (bytes == nullptr || rows <= 0) return op_fail(THINFER_EINVAL, "w4_linear: no rows, or bytes is NULL");
   if (rows > kMaxRows) return op_fail(THINFER_EUNSUPPORTED, "w4_linear: %d rows > %d: read the weights back and multiply those", rows, kMaxRows);
-  *bytes = linear_workspace(rows, n_out, k);
+  *bytes = linear_workspace(rows, n_out, k, group);
   return THINFER_OK;
 }
 
@@ -238,7 +244,7 @@ int thinfer_op_w4_linear(const void* x, int64_t x_stride, const void* packed, vo
   if (rows_overlap(y, y_stride * size, n_out * size, x, x_stride * 2, static_cast<int64_t>(k) * 2, rows) ||
       rows_meet(y, y_stride * size, n_out * size, rows, {packed, w4_packed_bytes(n_out, k, group)}))
     return op_fail(THINFER_EINVAL, "w4_linear: the output overlaps an input");
-  const size_t need = linear_workspace(rows, n_out, k);
+  const size_t need = linear_workspace(rows, n_out, k, group);
   if (need > 0) {
     if (workspace == nullptr || !aligned16(workspace)) return op_fail(THINFER_EINVAL, "w4_linear: the workspace is NULL or not 16-byte aligned");
     if (workspace_bytes < need) return op_fail(THINFER_ECAPACITY, "w4_linear: the workspace has %zu bytes of %zu", workspace_bytes, need);

@@ -13,7 +13,7 @@
 // after the other to a ring (three copies a block); and a warp for each warpgroup that issues its tensor instructions (as a
 // part of the unpacking warps that took a third of their time).  While the tensor cores multiply a block, its warpgroup unpacks
 // the next.  The (rows, block) units of the whole matrix are dealt out to the CTAs in equal contiguous runs; their partial
-// sums go to the workspace, and the warpgroup that comes last adds up those of its rows in the order of the CTAs.
+// sums go to the workspace, and a last kernel adds them up in the order of the CTAs.
 #pragma once
 #include "w4_linear.cuh"
 
@@ -27,7 +27,6 @@ struct W4TcArgs {
   W4LinearArgs a;
   uint8_t* tokens;       // [block][N * 256 bytes]
   float* parts;          // [CTA][first segment of its run, last one][token][row of the CTA's tile]
-  int* arrived;          // [row tile][warpgroup]
   long long row_tiles;
 };
 
@@ -46,7 +45,11 @@ struct W4Tc {
 
 // A run of units: CTA c of `ctas` begins at unit c * units / ctas.
 __host__ __device__ __forceinline__ long long w4_run(long long c, long long units, long long ctas) { return c * units / ctas; }
-__device__ __forceinline__ int w4_run_of(long long unit, long long units, long long ctas) { return static_cast<int>((ctas * (unit + 1) - 1) / units); }
+__device__ __forceinline__ int w4_run_of(long long unit, long long units, long long ctas) {
+  const long long n = ctas * (unit + 1) - 1;
+  if (n < 1ll << 32) return static_cast<int>(static_cast<uint32_t>(n) / static_cast<uint32_t>(units));
+  return static_cast<int>(n / units);
+}
 
 // 16 lanes by 64 columns of tensor memory: r[4 i ..] of lane 4 g + t are columns 8 i + 2 t, + 1 of lane g, then of lane 8 + g.
 __device__ __forceinline__ void tmem_st_16x64(uint32_t taddr, const uint32_t (&r)[32]) {
@@ -72,14 +75,12 @@ __device__ __forceinline__ void w4_bulk_load(void* dst, const void* src, uint32_
 
 // The tokens, block by block as shared memory holds them: 64 columns in 128 bytes of a row of N, twice, the 16-byte units of
 // row r at unit ^ (r % 8).  Position 16 s' + 4 t + 2 b + e of half c is column 64 c + 32 (s' / 2) + 8 t + 4 (s' % 2) + 2 b + e of the block.
-// Clears what the CTAs count their arrivals in.
 template <int N>
 __global__ void __launch_bounds__(256) w4_tokens_kernel(const __grid_constant__ W4TcArgs args) {
   pdl_wait();
   pdl_launch_dependents();   // behind the wait: what the next kernel reads before its own wait is final
   const W4LinearArgs& a = args.a;
   const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
-  for (long long c = i; c < args.row_tiles * kW4TcGroups; c += static_cast<long long>(gridDim.x) * 256) args.arrived[c] = 0;
   const long long block = i / (N * 16);
   if (block < a.v.blocks) {
     const int at = static_cast<int>(i % (N * 16)), half = at / (N * 8), row = at / 8 % N, unit = at % 8, from = unit ^ (row & 7);
@@ -104,7 +105,6 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t full[T::kStages], empty[T::kStages], a_full[W], d_free[W], done[W];
   __shared__ uint32_t tmem_holder;
-  __shared__ int last_one[W];
   __shared__ volatile int dead;    // a wait has run out: whom it happened to waits no more, and the results are NaN
   const W4LinearArgs& a = args.a;
   uint8_t* ring = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024;
@@ -264,49 +264,15 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
       }
       tc_fence_before();
     };
-    // What this CTA has of a row tile from block `begun` on, and the result where nothing is missing.  All of it goes by way of
-    // the workspace, in short code: it runs once or twice, and the instructions of 64 tokens' stores side by side took longer
-    // to fetch (up to 40 us) than the sums to read.
+    // What this CTA has of a row tile from block `begun` on.  Short code: it runs once or twice, and the instructions of 64 tokens'
+    // sums and stores side by side took longer to fetch (up to 40 us) than the sums to read.
     auto flush = [&] {
-      const int row = wg * 128 + (warp & 3) * 32 + lane;
-      const long long unit = static_cast<long long>(row_tile) * blocks;
-      const int c0 = w4_run_of(unit, units, ctas), c1 = w4_run_of(unit + blocks - 1, units, ctas);
-      float* part = args.parts + ((cta * 2 + (unit + begun == u0 ? 0 : 1)) * N) * kW4TcTile + row;
-      const bool lost = dead;
+      const bool first = static_cast<long long>(row_tile) * blocks + begun == u0, lost = dead;
+      float* part = args.parts + ((cta * 2 + (first ? 0 : 1)) * N) * kW4TcTile + wg * 128 + (warp & 3) * 32 + lane;
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         if (j < a.rows) part[j * kW4TcTile] = lost ? __int_as_float(0x7fffffff) : acc[j];
         acc[j] = 0.f;
-      }
-      if (c1 > c0) {
-        pdl_wait();                 // the counter has been cleared
-        __threadfence();
-        asm volatile("bar.sync %0, 128;" ::"r"(wg + 1) : "memory");
-        if ((warp & 3) == 0 && lane == 0) last_one[wg] = atomicAdd(&args.arrived[row_tile * W + wg], 1) == c1 - c0;
-        asm volatile("bar.sync %0, 128;" ::"r"(wg + 1) : "memory");
-        if (!last_one[wg]) return;
-        __threadfence();
-      }
-      const long long out = static_cast<long long>(row_tile) * kW4TcTile + row;
-      const float* from = args.parts + ((static_cast<long long>(c0) * 2 + (w4_run(c0, units, ctas) >= unit ? 0 : 1)) * N) * kW4TcTile + row;
-      const float* more = args.parts + (static_cast<long long>(c0 + 1) * 2 * N) * kW4TcTile + row;
-#pragma unroll 1
-      for (int j0 = 0; j0 < a.rows; j0 += 16) {
-        float v[16];
-#pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = j0 + j < a.rows ? __ldcg(from + (j0 + j) * kW4TcTile) : 0.f;
-#pragma unroll 1
-        for (int c = c0; c < c1; c += 2) {   // mostly once: its loads do not wait for the first
-          float x[2][16];
-#pragma unroll
-          for (int o = 0; o < 2; ++o)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) x[o][j] = c + o < c1 && j0 + j < a.rows ? __ldcg(more + (static_cast<long long>(c + o - c0) * 2 * N + j0 + j) * kW4TcTile) : 0.f;
-#pragma unroll
-          for (int j = 0; j < 16; ++j) v[j] = (v[j] + x[0][j]) + x[1][j];
-        }
-#pragma unroll
-        for (int j = 0; j < 16; ++j) w4_store(a, j0 + j, out, v[j]);
       }
     };
     for (int i = 0; i < count; ++i) {
@@ -382,6 +348,32 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
   __syncthreads();
   tc_fence_after();
   if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
+// Adds up the partial sums: 128 weight rows a CTA, 16 tokens, four of them a thread.
+template <int N>
+__global__ void __launch_bounds__(512) w4_linear_join_kernel(const __grid_constant__ W4TcArgs args, int ctas) {
+  pdl_launch_dependents();
+  const W4LinearArgs& a = args.a;
+  const int row_tile = blockIdx.x / kW4TcGroups, row = blockIdx.x % kW4TcGroups * 128 + threadIdx.x % 128, token = blockIdx.y * 16 + threadIdx.x / 128 * 4;
+  const long long blocks = a.v.blocks, units = args.row_tiles * blocks, first = row_tile * blocks, segment = static_cast<long long>(N) * kW4TcTile;
+  const int c0 = w4_run_of(first, units, ctas), c1 = w4_run_of(first + blocks - 1, units, ctas);
+  // of the first CTA its first or last segment, of the others always their first
+  const float* from = args.parts + (2ll * c0 + (w4_run(c0, units, ctas) >= first ? 0 : 1)) * segment + token * kW4TcTile + row;
+  const float* more = args.parts + 2ll * c0 * segment + token * kW4TcTile + row;
+  const int here = min(4, a.rows - token);
+  pdl_wait();
+  float v[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = j < here ? from[j * kW4TcTile] : 0.f;
+#pragma unroll 2
+  for (int c = 1; c <= c1 - c0; ++c) {
+    more += 2 * segment;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] += j < here ? more[j * kW4TcTile] : 0.f;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w4_store(a, token + j, static_cast<long long>(row_tile) * kW4TcTile + row, v[j]);
 }
 
 }  // namespace thinfer
