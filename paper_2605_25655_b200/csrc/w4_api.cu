@@ -66,10 +66,6 @@ struct LinearPlan {
   size_t smem;
 };
 
-#ifdef W4_DEV
-#include <cstdio>
-#include <cstdlib>
-#endif
 // Cluster size by the bytes that the busiest CTA moves: weights, its share of the tokens (from L2, at half price), and what a
 // round of sums at the end costs in bytes that could have been read meanwhile.
 int plan_linear(int tiles, int blocks, int rows, int nt, int r, int warps, int stage, int token_tiles, LinearPlan* best) {
@@ -80,9 +76,6 @@ int plan_linear(int tiles, int blocks, int rows, int nt, int r, int warps, int s
   for (int log2 = 0; log2 <= 3; ++log2) {
     const int64_t ctas = 1 << log2;
     if (ctas > blocks) break;
-#ifdef W4_DEV
-    if (getenv("W4_C") && atoi(getenv("W4_C")) != ctas) continue;
-#endif
     int active = 0;
     const int rc = active_clusters(log2, &active);
     if (rc != THINFER_OK) return rc;
@@ -92,9 +85,6 @@ int plan_linear(int tiles, int blocks, int rows, int nt, int r, int warps, int s
     const int64_t per = (groups + clusters - 1) / clusters, room = (kLinearSmem - ring - held * per_block) / per_group - (warps - 1);
     const int64_t batches = (per + room - 1) / room, batch = (per + batches - 1) / batches;
     const int64_t cost = per * slice * r * 1064 + (phases > 1 ? batches : 1) * slice * tokens * 128 + (batches * phases - 1) * 25000 + log2 * 6000 + (log2 == 3 ? 12000 : 0);
-#ifdef W4_DEV
-    if (getenv("W4_PRINT")) printf("C %d clusters %d per %d slice %d phases %d batches %d cost %d\n", (int)ctas, (int)clusters, (int)per, (int)slice, (int)phases, (int)batches, (int)cost);
-#endif
     if (cost >= least) continue;
     least = cost;
     best->cluster = static_cast<int>(ctas);
@@ -118,14 +108,15 @@ int launch_linear(W4LinearArgs& a, cudaStream_t st) {
   return op_launch_clusters(w4_linear_kernel<NT, R, G, Warps>, static_cast<unsigned>(p.cluster), dim3(static_cast<unsigned>(p.cluster * p.clusters), static_cast<unsigned>(token_tiles)),
                             dim3(Warps * 32), p.smem, st, a);
 }
-// The tensor-memory kernel for more than 16 rows and large matrices.  In front of and behind its stream it has some 15 us of its own
-// (tokens laid out, partial sums), while the other one walks over the weights again for every 16 rows.  us, here and there:
-// MEASURED_CROSS
+// Whether the tensor-memory kernel takes over: in front of and behind its stream it has two small kernels (tokens laid out, partial
+// sums added up, some 5 us), while the other one walks over the weights again for every 16 rows, and needs up to 16 rows
+// for longer than the bytes only where there are many of them.  FP16, us, the other one / this one, by tiles x blocks:
+//   groups of 128  8192: 24 rows 10.9 / 11.2, 64 rows 17.1 / 15.3;  22016: 16 rows 12.3 / 15.7, 24 rows 17.8 / 15.9, 48 rows 24.4 / 21.9;
+//                  57344: 16 rows 22.9 / 24.1;  114688: 8 rows 29.2 / 36.7, 16 rows 40.0 / 36.6, 24 rows 69.1 / 36.0, 64 rows 137 / 60
+//   groups of 32   8192: 24 rows 11.7 / 13.2, 64 rows 18.9 / 18.6;  22016: 24 rows 20.4 / 19.8, 48 rows 29.0 / 27.4;  114688: 16 rows 46.9 / 55.8
 bool on_tensor_memory(int64_t rows, int64_t tiles, int64_t blocks, int group) {
-#ifdef W4_DEV
-  if (getenv("W4_MMA")) return rows > atoi(getenv("W4_MMA"));
-#endif
-  return rows > 16 && tiles * blocks > (group == 32 ? 48 : 32) * 1024;
+  const int64_t units = tiles * blocks;
+  return rows > 16 ? units > (group == 32 ? 16 : 10) * 1024 : rows > 8 && group != 32 && units > 80 * 1024;
 }
 
 struct TcPlan {
@@ -143,7 +134,7 @@ TcPlan plan_tc(int n, int64_t tiles, int64_t blocks) {
   const int sms = op_sm_count();
   p.ctas = most < sms ? static_cast<int>(most) : sms;
   p.token_bytes = static_cast<size_t>(blocks) * n * 256;
-  p.part_bytes = static_cast<size_t>(p.ctas) * 2 * n * kW4TcTile * 4;
+  p.part_bytes = static_cast<size_t>(p.row_tiles + p.ctas) * n * kW4TcTile * 4;
   return p;
 }
 size_t linear_workspace(int32_t rows, int32_t n_out, int32_t k, int32_t group) {

@@ -26,7 +26,7 @@ constexpr int kW4TcColumns = 512 / kW4TcGroups / 32 * 32;   // of tensor memory,
 struct W4TcArgs {
   W4LinearArgs a;
   uint8_t* tokens;       // [block][N * 256 bytes]
-  float* parts;          // [CTA][first segment of its run, last one][token][row of the CTA's tile]
+  float* parts;          // [row tile + CTA][token][row of the tile]: every piece of a row tile that a CTA has, each in a place of its own
   long long row_tiles;
 };
 
@@ -222,7 +222,7 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
     for (int j = 0; j < N; ++j) acc[j] = 0.f;
     float scale[P] = {};
     uint32_t rounds = 0;            // of this warpgroup so far
-    int row_tile = first_tile, block = first_block, begun = first_block;
+    int row_tile = first_tile, block = first_block;
     // the zero points, two units ahead: the bytes of P groups of row g of both tiles
     const int last_tile = static_cast<int>(a.v.tiles) - 1;
     int zero_tile = first_tile * 8 * W + 2 * warp, zero_block = first_block;
@@ -264,11 +264,11 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
       }
       tc_fence_before();
     };
-    // What this CTA has of a row tile from block `begun` on.  Short code: it runs once or twice, and the instructions of 64 tokens'
+    // What this CTA has of a row tile.  Short code: it runs once or twice, and the instructions of 64 tokens'
     // sums and stores side by side took longer to fetch (up to 40 us) than the sums to read.
     auto flush = [&] {
-      const bool first = static_cast<long long>(row_tile) * blocks + begun == u0, lost = dead;
-      float* part = args.parts + ((cta * 2 + (first ? 0 : 1)) * N) * kW4TcTile + wg * 128 + (warp & 3) * 32 + lane;
+      const bool lost = dead;
+      float* part = args.parts + (row_tile + cta) * (N * kW4TcTile) + wg * 128 + (warp & 3) * 32 + lane;
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         if (j < a.rows) part[j * kW4TcTile] = lost ? __int_as_float(0x7fffffff) : acc[j];
@@ -307,7 +307,6 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
         if (block == 0) {
           flush();
           ++row_tile;
-          begun = 0;
         }
       };
       // Into the weights that the products of the last block do not read, while they are under way; or, where there is room for
@@ -358,9 +357,7 @@ __global__ void __launch_bounds__(512) w4_linear_join_kernel(const __grid_consta
   const int row_tile = blockIdx.x / kW4TcGroups, row = blockIdx.x % kW4TcGroups * 128 + threadIdx.x % 128, token = blockIdx.y * 16 + threadIdx.x / 128 * 4;
   const long long blocks = a.v.blocks, units = args.row_tiles * blocks, first = row_tile * blocks, segment = static_cast<long long>(N) * kW4TcTile;
   const int c0 = w4_run_of(first, units, ctas), c1 = w4_run_of(first + blocks - 1, units, ctas);
-  // of the first CTA its first or last segment, of the others always their first
-  const float* from = args.parts + (2ll * c0 + (w4_run(c0, units, ctas) >= first ? 0 : 1)) * segment + token * kW4TcTile + row;
-  const float* more = args.parts + 2ll * c0 * segment + token * kW4TcTile + row;
+  const float* from = args.parts + (row_tile + c0) * segment + token * kW4TcTile + row;   // the CTAs' pieces follow each other
   const int here = min(4, a.rows - token);
   pdl_wait();
   float v[4];
@@ -368,9 +365,9 @@ __global__ void __launch_bounds__(512) w4_linear_join_kernel(const __grid_consta
   for (int j = 0; j < 4; ++j) v[j] = j < here ? from[j * kW4TcTile] : 0.f;
 #pragma unroll 2
   for (int c = 1; c <= c1 - c0; ++c) {
-    more += 2 * segment;
+    from += segment;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] += j < here ? more[j * kW4TcTile] : 0.f;
+    for (int j = 0; j < 4; ++j) v[j] += j < here ? from[j * kW4TcTile] : 0.f;
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j) w4_store(a, token + j, static_cast<long long>(row_tile) * kW4TcTile + row, v[j]);

@@ -85,7 +85,10 @@ def _random_packed(rng, n, k, group, t, whole):
 
 SIZES = [(1, 16, 128, 128), (1, 4096, 256, 64), (2, 1, 8, 32), (3, 17, 40, 32), (5, 100, 1000, 64), (7, 1001, 136, 128), (8, 64, 4096, 128), (9, 33, 264, 32),
          (16, 500, 2048, 128), (17, 48, 520, 64), (24, 257, 1024, 32), (33, 130, 392, 128), (40, 31, 3000, 64), (64, 200, 1536, 128), (64, 15, 72, 32),
-         (1, 40, 40960, 128), (16, 24, 30000, 32), (64, 20, 28672, 64), (4, 5000, 512, 128), (16, 9000, 136, 64), (64, 7000, 264, 32)]
+         (1, 40, 40960, 128), (16, 24, 30000, 32), (64, 20, 28672, 64), (4, 5000, 512, 128), (16, 9000, 136, 64), (64, 7000, 264, 32),
+         # more than 10 (16) x 1024 tiles and blocks: tensor memory.  Few blocks and many rows, many blocks and few rows, one block
+         (17, 1100, 20000, 64), (40, 5200, 4200, 128), (64, 2600, 8200, 128), (33, 2700, 13000, 32), (24, 41000, 640, 64), (64, 100000, 136, 128), (20, 170000, 120, 64),
+         (32, 20000, 1784, 32), (64, 16, 1310728, 128)]
 
 
 @pytest.mark.parametrize("t", ["f16", "bf16"])
@@ -113,7 +116,28 @@ def test_products_of_whole_numbers_are_exact(T, t, rows, n, k, group):
 
 
 @pytest.mark.parametrize("t", ["f16", "bf16"])
-@pytest.mark.parametrize("rows,n,k,group", [(1, 700, 4096, 128), (4, 512, 8192, 64), (16, 300, 11008, 32), (33, 80, 5120, 128), (64, 160, 28672, 64)])
+@pytest.mark.parametrize("rows", [8, 9, 16, 17, 32, 33, 64])
+def test_products_of_a_large_matrix_are_exact(T, t, rows):
+    """The same for more than 80 x 1024 tiles and blocks, against the weights as they are read back (which has a test of its own)."""
+    torch, thinfer = T
+    n, k, group, tt = 20501, 8200, 128, _tt(torch, t)
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    (nc, ns, nz) = w4.sizes(n, k, group)[3]
+    packed = torch.randint(0, 256, (nc + ns + nz,), dtype=torch.uint8, device="cuda", generator=gen)
+    packed[nc:nc + ns].view(tt).copy_(2.0 ** -torch.randint(0, 4, (ns // 2,), device="cuda", generator=gen).float())
+    x = torch.randint(-2, 3, (rows, k), device="cuda", generator=gen).to(tt)
+    w = thinfer.op_w4_read(packed, n, k, group, tt)
+    want = torch.cat([x.double() @ part.double().T for part in w.split(4096)], 1)        # multiples of 2^-3 below 2^18
+    got = thinfer.op_w4_linear(x, packed, n, group, out_fp32=True)
+    assert torch.equal(got.double(), want)
+    out = torch.full((rows + 1, n + 2), 7.0, dtype=tt, device="cuda")
+    thinfer.op_w4_linear(x, packed, n, group, out=out[:-1, 1:-1])
+    assert torch.equal(out[:-1, 1:-1], want.to(tt)) and torch.all(out[-1] == 7) and torch.all(out[:, 0] == 7) and torch.all(out[:, -1] == 7)
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,n,k,group", [(1, 700, 4096, 128), (4, 512, 8192, 64), (16, 300, 11008, 32), (33, 80, 5120, 128), (64, 160, 28672, 64), (64, 2600, 8192, 64),
+                                            (24, 1100, 32768, 32)])
 def test_products(T, t, rows, n, k, group):
     torch, thinfer = T
     rng = np.random.default_rng(rows + n + k)
@@ -134,11 +158,11 @@ def test_products(T, t, rows, n, k, group):
 
 
 @pytest.mark.parametrize("t", ["f16", "bf16"])
-@pytest.mark.parametrize("rows", [1, 8, 13, 40])
-def test_what_is_not_finite_stays_in_its_row_and_column(T, t, rows):
+@pytest.mark.parametrize("rows,n,k", [(1, 70, 600), (8, 70, 600), (13, 70, 600), (40, 70, 600), (20, 4000, 5200), (64, 4000, 5200)])
+def test_what_is_not_finite_stays_in_its_row_and_column(T, t, rows, n, k):
     torch, thinfer = T
     rng = np.random.default_rng(rows)
-    n, k, group = 70, 600, 64
+    group = 64
     w = w4.round_to(rng.standard_normal((n, k)) * 0.02, DT[t])
     w[5, 70], w[37, 599] = np.nan, np.inf
     x = w4.round_to(rng.standard_normal((rows, k)), DT[t])
@@ -222,6 +246,60 @@ def test_streams_and_graphs(T):
         graph.replay()
         p = thinfer.op_w4_quantize(w, 64)
         assert torch.equal(y, thinfer.op_w4_linear(x, p, 300, 64)) and torch.equal(z, thinfer.op_w4_linear(x[:1], p, 300, 64, out_fp32=True))
+
+
+def test_workspaces_graphs_and_streams_on_tensor_memory(T):
+    """Two graphs that share a workspace, replayed in turn; calls on two streams at once with a workspace each; a workspace full of
+    other numbers."""
+    import ctypes as C
+    torch, thinfer = T
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    n, k, group = 2600, 8200, 128
+    need = C.c_size_t(0)
+    assert thinfer.lib().thinfer_w4_linear_workspace(40, n, k, group, C.byref(need)) == thinfer.OK and need.value > 0
+    assert thinfer.lib().thinfer_w4_linear_workspace(16, n, k, group, C.byref(C.c_size_t(0))) == thinfer.OK
+    packed = [thinfer.op_w4_quantize((torch.randn(n, k, generator=gen, device="cuda") * 0.02).half(), group) for _ in range(2)]
+    x = [torch.randn(40, k, generator=gen, device="cuda").half() for _ in range(2)]
+    want = [[thinfer.op_w4_linear(a, p, n, group, out_fp32=True) for a in x] for p in packed]
+    workspace = torch.full((need.value,), 255, dtype=torch.uint8, device="cuda")
+    graphs = []
+    for p in packed:
+        graph, held = torch.cuda.CUDAGraph(), x[0].clone()
+        with torch.cuda.graph(graph):
+            y = thinfer.op_w4_linear(held, p, n, group, out_fp32=True, workspace=workspace)
+        graphs.append((graph, held, y))
+    for turn in range(4):
+        for i, (graph, held, y) in enumerate(graphs):
+            held.copy_(x[turn % 2])
+            graph.replay()
+            assert torch.equal(y, want[i][turn % 2])
+            workspace.fill_(turn * 37)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[thinfer.op_w4_linear(x[i], packed[i], n, group, out_fp32=True, stream=s) for _ in range(5)] for i, s in enumerate(streams)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want[i][i]) for i in range(2) for g in got[i])
+    with pytest.raises(thinfer.ThinferError) as e:
+        thinfer.op_w4_linear(x[0], packed[0], n, group, workspace=workspace[:-16])
+    assert e.value.code == thinfer.ECAPACITY
+
+
+def test_other_kernels_around_tensor_memory(T):
+    """Products between the library's other kernels that use tensor memory, all chained in one stream."""
+    torch, thinfer = T
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    n, k = 2600, 8200
+    w = (torch.randn(n, k, generator=gen, device="cuda") * 0.02).half()
+    packed = thinfer.op_w4_quantize(w, 128)
+    x = torch.randn(64, k, generator=gen, device="cuda").half()
+    back = thinfer.op_w4_read(packed, n, k, 128, torch.float16)
+    want, plain = thinfer.op_w4_linear(x, packed, n, 128), thinfer.op_linear(x, back)
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        got.append((thinfer.op_w4_linear(x, packed, n, 128), thinfer.op_linear(x, back)))
+        got.append((thinfer.op_w4_linear(x, thinfer.op_w4_quantize(w, 128), n, 128), thinfer.op_linear(x, thinfer.op_w4_read(packed, n, k, 128, torch.float16))))
+    assert all(torch.equal(a, want) and torch.equal(b, plain) for a, b in got)
 
 
 def test_the_binding_refuses(T):

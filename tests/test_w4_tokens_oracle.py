@@ -122,12 +122,14 @@ def test_linear_refuses_workspaces(lib):
     for bad, code in (((0, 40, 264, 64), E), ((65, 40, 264, 64), U), ((5, 0, 264, 64), E), ((5, 40, 264, 48), U)):
         assert lib.thinfer_w4_linear_workspace(*bad, C.byref(need)) == code
     assert lib.thinfer_w4_linear_workspace(5, 40, 264, 64, None) == E
-    assert lib.thinfer_w4_linear_workspace(64, 40, 264, 64, C.byref(need)) == thinfer.OK and need.value > 0
-    n = thinfer.w4_bytes(40, 264, 64)
-    args = dict(x=A[0], xs=272, packed=A[1], y=A[2], ys=40, rows=64, n=40, k=264, group=64, fp32=0, ws=A[3], wb=need.value, st=None)
+    assert lib.thinfer_w4_linear_workspace(64, 40, 264, 64, C.byref(need)) == thinfer.OK and need.value == 0      # a small one needs none
+    n_out, k = 2600, 8200
+    assert lib.thinfer_w4_linear_workspace(64, n_out, k, 64, C.byref(need)) == thinfer.OK and need.value > 0
+    n = thinfer.w4_bytes(n_out, k, 64)
+    args = dict(x=A[0], xs=k, packed=A[1], y=A[2], ys=n_out, rows=64, n=n_out, k=k, group=64, fp32=0, ws=A[3], wb=need.value, st=None)
     _refused(lib.thinfer_op_w4_linear, args, [
-        ({"ws": None}, E), ({"ws": A[3] + 8}, E), ({"wb": need.value - 1}, thinfer.ECAPACITY), ({"wb": 0}, thinfer.ECAPACITY), ({"ws": A[0]}, E), ({"ws": A[1] + n - 16}, E),
-        ({"ws": A[2]}, E), ({"ws": A[1] - need.value + 16}, E), ({"y": A[3] + need.value - 2}, E), ({"x": A[3] + 16}, E)])
+        ({"ws": None}, E), ({"ws": A[3] + 8}, E), ({"wb": need.value - 1}, thinfer.ECAPACITY), ({"wb": 0}, thinfer.ECAPACITY), ({"ws": A[0]}, E), ({"ws": A[1] + n // 16 * 16 - 16}, E),
+        ({"ws": A[2]}, E), ({"ws": A[1] - need.value // 16 * 16 + 16}, E), ({"y": A[3] + need.value - 2}, E), ({"x": A[3] + 16}, E)])
 
 
 def test_probs_refuses(lib):
