@@ -108,15 +108,17 @@ int launch_linear(W4LinearArgs& a, cudaStream_t st) {
   return op_launch_clusters(w4_linear_kernel<NT, R, G, Warps>, static_cast<unsigned>(p.cluster), dim3(static_cast<unsigned>(p.cluster * p.clusters), static_cast<unsigned>(token_tiles)),
                             dim3(Warps * 32), p.smem, st, a);
 }
+
 // Whether the tensor-memory kernel takes over: in front of and behind its stream it has two small kernels (tokens laid out, partial
 // sums added up, some 5 us), while the other one walks over the weights again for every 16 rows, and needs up to 16 rows
 // for longer than the bytes only where there are many of them.  FP16, us, the other one / this one, by tiles x blocks:
-//   groups of 128  8192: 24 rows 10.9 / 11.2, 64 rows 17.1 / 15.3;  22016: 16 rows 12.3 / 15.7, 24 rows 17.8 / 15.9, 48 rows 24.4 / 21.9;
-//                  57344: 16 rows 22.9 / 24.1;  114688: 8 rows 29.2 / 36.7, 16 rows 40.0 / 36.6, 24 rows 69.1 / 36.0, 64 rows 137 / 60
-//   groups of 32   8192: 24 rows 11.7 / 13.2, 64 rows 18.9 / 18.6;  22016: 24 rows 20.4 / 19.8, 48 rows 29.0 / 27.4;  114688: 16 rows 46.9 / 55.8
+//   groups of 128  8192: 24 rows 11.0 / 11.2, 33 rows 13.5 / 12.0, 64 rows 17.2 / 13.5;  22016: 16 rows 12.4 / 15.6, 24 rows 18.0 / 16.2;
+//                  57344: 16 rows 24.2 / 24.1;  114688: 8 rows 29.2 / 36.7, 16 rows 40.2 / 35.7, 24 rows 69.1 / 36.2, 64 rows 137 / 47
+//   groups of 64   8192: 24 rows 10.9 / 12.4, 33 rows 13.7 / 12.5;  22016: 24 rows 18.5 / 18.0;  114688: 16 rows 42.0 / 44.5
+//   groups of 32   8192: 24 rows 11.8 / 11.8, 33 rows 15.0 / 14.5, 64 rows 19.1 / 16.3;  22016: 24 rows 20.6 / 18.1;  114688: 16 rows 47.1 / 50.9
 bool on_tensor_memory(int64_t rows, int64_t tiles, int64_t blocks, int group) {
   const int64_t units = tiles * blocks;
-  return rows > 16 ? units > (group == 32 ? 16 : 10) * 1024 : rows > 8 && group != 32 && units > 80 * 1024;
+  return rows > 16 ? units > (rows > 32 ? 7 : 10) * 1024 : rows > 8 && group == 128 && units > 80 * 1024;
 }
 
 struct TcPlan {
@@ -126,35 +128,36 @@ struct TcPlan {
   size_t bytes() const { return token_bytes + part_bytes; }
 };
 int tc_tokens(int rows) { return rows <= 32 ? 32 : 64; }
-TcPlan plan_tc(int n, int64_t tiles, int64_t blocks) {
+TcPlan plan_tc(int n, int group, int64_t tiles, int64_t blocks) {
+  const int64_t tile = w4_tc_groups(n, group) * 128;
   TcPlan p{};
-  p.row_tiles = (tiles * 16 + kW4TcTile - 1) / kW4TcTile;
+  p.row_tiles = (tiles * 16 + tile - 1) / tile;
   // as many CTAs as the device has SMs, but no more than 8 for a row tile, whose sums one thread adds up
   const int64_t most = blocks < 8 ? p.row_tiles * blocks : p.row_tiles * 8;
   const int sms = op_sm_count();
   p.ctas = most < sms ? static_cast<int>(most) : sms;
   p.token_bytes = static_cast<size_t>(blocks) * n * 256;
-  p.part_bytes = static_cast<size_t>(p.row_tiles + p.ctas) * n * kW4TcTile * 4;
+  p.part_bytes = static_cast<size_t>(p.row_tiles + p.ctas) * n * tile * 4;
   return p;
 }
 size_t linear_workspace(int32_t rows, int32_t n_out, int32_t k, int32_t group) {
-  return on_tensor_memory(rows, w4_tiles(n_out), w4_blocks(k), group) ? plan_tc(tc_tokens(rows), w4_tiles(n_out), w4_blocks(k)).bytes() : 0;
+  return on_tensor_memory(rows, w4_tiles(n_out), w4_blocks(k), group) ? plan_tc(tc_tokens(rows), group, w4_tiles(n_out), w4_blocks(k)).bytes() : 0;
 }
 
 template <int N, int G>
 int launch_tc(const W4LinearArgs& a, void* workspace, cudaStream_t st) {
-  constexpr int P = 128 / G, kSmem = W4Tc<N, P>::kSmem;
-  const TcPlan p = plan_tc(N, a.v.tiles, a.v.blocks);
+  constexpr int P = 128 / G, W = W4Tc<N, P>::W, kSmem = W4Tc<N, P>::kSmem;
+  const TcPlan p = plan_tc(N, G, a.v.tiles, a.v.blocks);
   char* ws = static_cast<char*>(workspace);
   const W4TcArgs args{a, reinterpret_cast<uint8_t*>(ws), reinterpret_cast<float*>(ws + p.token_bytes), p.row_tiles};
   CUtensorMap codes, scales;
-  if (!op_tensor_map(&codes, a.v.codes, 256, a.v.blocks, a.v.tiles, kW4TcGroups * 8) || !op_tensor_map(&scales, a.v.scales, 8 * P, a.v.blocks, a.v.tiles, kW4TcGroups * 8))
+  if (!op_tensor_map(&codes, a.v.codes, 256, a.v.blocks, a.v.tiles, W * 8) || !op_tensor_map(&scales, a.v.scales, 8 * P, a.v.blocks, a.v.tiles, W * 8))
     return op_fail(THINFER_ECUDA, "cuTensorMapEncodeTiled failed for packed weights");
   int rc = opt_in<w4_linear_tc_kernel<N, P>>(kSmem);
   if (rc == THINFER_OK) rc = op_launch(w4_tokens_kernel<N>, dim3(static_cast<unsigned>((a.v.blocks * N * 16 + 255) / 256)), dim3(256), 0, st, args);
-  if (rc == THINFER_OK) rc = op_launch(w4_linear_tc_kernel<N, P>, dim3(static_cast<unsigned>(p.ctas)), dim3(kW4TcTile + 128), kSmem, st, args, codes, scales);
+  if (rc == THINFER_OK) rc = op_launch(w4_linear_tc_kernel<N, P>, dim3(static_cast<unsigned>(p.ctas)), dim3(W4Tc<N, P>::kThreads), kSmem, st, args, codes, scales);
   if (rc == THINFER_OK)
-    rc = op_launch(w4_linear_join_kernel<N>, dim3(static_cast<unsigned>(p.row_tiles * kW4TcGroups), static_cast<unsigned>((a.rows + 15) / 16)), dim3(512), 0, st, args, p.ctas);
+    rc = op_launch(w4_linear_join_kernel<N, W>, dim3(static_cast<unsigned>(p.row_tiles * W), static_cast<unsigned>((a.rows + 15) / 16)), dim3(512), 0, st, args, p.ctas);
   return rc;
 }
 

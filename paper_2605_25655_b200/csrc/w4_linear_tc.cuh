@@ -14,14 +14,19 @@
 // part of the unpacking warps that took a third of their time).  While the tensor cores multiply a block, its warpgroup unpacks
 // the next.  The (rows, block) units of the whole matrix are dealt out to the CTAs in equal contiguous runs; their partial
 // sums go to the workspace, and a last kernel adds them up in the order of the CTAs.
+//
+// 64 x 28672 x 8192 in groups of 128 (127 MB): 47 us in FP16, 50 in BF16, of which 5 are the two small kernels; 32 rows 36 and 39.  A
+// copy would take 19, the products 18.  Bound by the unpacking: two or three warps for each of a SM's quarters do not cover its
+// dependences, and their registers (tokens' sums, codes, 64 unpacked words) leave room for no more.
 #pragma once
 #include "w4_linear.cuh"
 
 namespace thinfer {
 
-constexpr int kW4TcGroups = 3;                        // W
-constexpr int kW4TcTile = kW4TcGroups * 128;          // weight rows of a CTA
-constexpr int kW4TcColumns = 512 / kW4TcGroups / 32 * 32;   // of tensor memory, for a warpgroup
+// W: two warpgroups with 168 registers a thread, or three with 128 - where those are enough and the sums of 128 rows have room beside
+// the weights.  28672 x 8192, us, two / three: 64 rows 47.2 / 59.5 in groups of 128, 80 / 88 of 32; 32 rows 43.8 / 36.4 in groups of
+// 128, 45.3 / 46.2 of 64, 51.3 / 58.8 of 32.
+constexpr int w4_tc_groups(int n, int group) { return n == 64 || group < 128 ? 2 : 3; }
 
 struct W4TcArgs {
   W4LinearArgs a;
@@ -32,15 +37,18 @@ struct W4TcArgs {
 
 template <int N, int P>
 struct W4Tc {
-  // Tensor memory of a warpgroup: weights, twice where there is room beside the sums of all groups of a block, and the sums of as
-  // many groups as fit (the others follow in further rounds).
-  static constexpr int kA = P * N <= 32 ? 2 : 1, kSums = kA * 64, kRoom = (kW4TcColumns - kSums) / N;
+  static constexpr int W = w4_tc_groups(N, 128 / P), kTile = W * 128, kThreads = (4 * W + 1 + W) * 32;   // kTile: weight rows of a CTA
+  static constexpr int kColumns = 512 / W / 32 * 32;                                          // of tensor memory, for a warpgroup
+  // Tensor memory of a warpgroup: the weights of one or two blocks, and the sums of one or two blocks, or of as many groups of
+  // a block as fit (the others follow in further rounds).
+  static constexpr int kA = P * N <= kColumns - 128 ? 2 : 1, kSums = kA * 64, kRoom = (kColumns - kSums) / N;
   static constexpr int kRound = P <= kRoom ? P : kRoom >= 2 ? 2 : 1, kRounds = P / kRound;
-  static constexpr int kCodes = kW4TcGroups * 8192, kScales = kW4TcGroups * 8 * 32 * P, kTokens = N * 256;
+  static constexpr int kD = kRounds == 1 && kA == 2 && 2 * P * N <= kColumns - kSums ? 2 : 1;
+  static constexpr int kCodes = W * 8192, kScales = W * 8 * 32 * P, kTokens = N * 256;
   static constexpr int kBytes = kCodes + kTokens + kScales, kStage = (kBytes + 1023) / 1024 * 1024;
   static constexpr int kFit = 224 * 1024 / kStage, kStages = kFit < 8 ? kFit : 8;
   static constexpr int kSmem = 1024 + kStages * kStage;
-  static_assert(P % kRound == 0 && kSums + kRound * N <= kW4TcColumns, "the sums of a round");
+  static_assert(P % kRound == 0 && kSums + kD * kRound * N <= kColumns, "the sums of a round");
 };
 
 // A run of units: CTA c of `ctas` begins at unit c * units / ctas.
@@ -97,13 +105,13 @@ __global__ void __launch_bounds__(256) w4_tokens_kernel(const __grid_constant__ 
 }
 
 template <int N, int P>
-__global__ void __launch_bounds__(kW4TcGroups * 128 + 128, 1)
+__global__ void __launch_bounds__(W4Tc<N, P>::kThreads, 1)
 w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant__ CUtensorMap codes_map, const __grid_constant__ CUtensorMap scales_map) {
   using T = W4Tc<N, P>;
-  constexpr int W = kW4TcGroups;
+  constexpr int W = T::W;
   constexpr uint32_t kIdesc = idesc_f16(128, N, 0, 0);
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t full[T::kStages], empty[T::kStages], a_full[W], d_free[W], done[W];
+  __shared__ __align__(8) uint64_t full[T::kStages], empty[T::kStages], a_full[W][2], d_free[W], done[W][2];
   __shared__ uint32_t tmem_holder;
   __shared__ volatile int dead;    // a wait has run out: whom it happened to waits no more, and the results are NaN
   const W4LinearArgs& a = args.a;
@@ -115,9 +123,11 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
       mbar_init(&empty[i], 4 * W + W);   // the warps that unpack, and the products that read the tokens
     }
     for (int i = 0; i < W; ++i) {
-      mbar_init(&a_full[i], 4);
       mbar_init(&d_free[i], 4);
-      mbar_init(&done[i], 1);
+      for (int j = 0; j < 2; ++j) {      // of even and odd units: with two sums the warps may be a unit ahead of who waits
+        mbar_init(&a_full[i][j], 4);
+        mbar_init(&done[i][j], 1);
+      }
     }
     dead = 0;
     fence_barrier_init();
@@ -188,17 +198,18 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
   } else if (warp > 4 * W) {
     // the products of warpgroup wg
     const int wg = warp - 4 * W - 1;
-    const uint32_t columns = tmem + wg * kW4TcColumns;
+    const uint32_t columns = tmem + wg * T::kColumns;
     const uint64_t first = smem_desc_sw128(smem_u32(ring + T::kCodes), 16, 1024);
     uint32_t frees = 0;
     for (int i = 0; i < count; ++i) {
       const int s = i % T::kStages;
       bool ok = wait(&full[s], (i / T::kStages) & 1);
-      ok = wait(&a_full[wg], i & 1) && ok;
+      ok = wait(&a_full[wg][i & 1], (i >> 1) & 1) && ok;
       const uint64_t b = first + static_cast<uint64_t>(s * (T::kStage >> 4));
 #pragma unroll
       for (int round = 0; round < T::kRounds; ++round) {
         if (round > 0) ok = wait(&d_free[wg], frees++ & 1) && ok;
+        ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
         if (ok && elect_one()) {
 #pragma unroll
@@ -206,9 +217,9 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
 #pragma unroll
             for (int w = 0; w < 8 / P; ++w) {
               const int st = (round * T::kRound + p) * (8 / P) + w;
-              tc_mma_f16_ts(columns + T::kSums + p * N, columns + (T::kA == 2 ? (i & 1) * 64 : 0) + st * 8, b + (st / 4) * (N * 128 >> 4) + (st % 4) * 2, kIdesc, w > 0);
+              tc_mma_f16_ts(columns + T::kSums + (T::kD == 2 ? (i & 1) * (P * N) : 0) + p * N, columns + (T::kA == 2 ? (i & 1) * 64 : 0) + st * 8, b + (st / 4) * (N * 128 >> 4) + (st % 4) * 2, kIdesc, w > 0);
             }
-          tc_commit(&done[wg]);
+          tc_commit(&done[wg][T::kRounds == 1 ? i & 1 : 0]);
           if (round == T::kRounds - 1) tc_commit(&empty[s]);
         }
         __syncwarp();
@@ -216,7 +227,7 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
     }
   } else {
     const int wg = warp >> 2;
-    const uint32_t mine = tmem + wg * kW4TcColumns + (static_cast<uint32_t>((warp & 3) * 32) << 16);   // this warp's lanes
+    const uint32_t mine = tmem + wg * T::kColumns + (static_cast<uint32_t>((warp & 3) * 32) << 16);   // this warp's lanes
     float acc[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) acc[j] = 0.f;
@@ -248,15 +259,15 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
     zeros(z0);
     zeros(z1);
     // adds the sums of the groups of the last round to this thread's row
-    auto collect = [&](int first) {
-      const bool ok = __all_sync(0xffffffffu, wait(&done[wg], rounds++ & 1));
+    auto collect = [&](int first, int i) {   // i: the unit, counted from the run's beginning
+      const bool ok = __all_sync(0xffffffffu, T::kRounds == 1 ? wait(&done[wg][i & 1], (i >> 1) & 1) : wait(&done[wg][0], rounds++ & 1));
       tc_fence_after();
       if (ok) {
 #pragma unroll
         for (int p = 0; p < T::kRound; ++p) {
           uint32_t d[N / 16][16];
 #pragma unroll
-          for (int j = 0; j < N / 16; ++j) tmem_ld16(mine + T::kSums + p * N + 16 * j, d[j]);
+          for (int j = 0; j < N / 16; ++j) tmem_ld16(mine + T::kSums + (T::kD == 2 ? (i & 1) * (P * N) : 0) + p * N + 16 * j, d[j]);
           tmem_ld_wait();
 #pragma unroll
           for (int j = 0; j < N; ++j) acc[j] = fmaf(scale[first + p], __uint_as_float(d[j / 16][j % 16]), acc[j]);
@@ -268,10 +279,10 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
     // sums and stores side by side took longer to fetch (up to 40 us) than the sums to read.
     auto flush = [&] {
       const bool lost = dead;
-      float* part = args.parts + (row_tile + cta) * (N * kW4TcTile) + wg * 128 + (warp & 3) * 32 + lane;
+      float* part = args.parts + (row_tile + cta) * (N * T::kTile) + wg * 128 + (warp & 3) * 32 + lane;
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        if (j < a.rows) part[j * kW4TcTile] = lost ? __int_as_float(0x7fffffff) : acc[j];
+        if (j < a.rows) part[j * T::kTile] = lost ? __int_as_float(0x7fffffff) : acc[j];
         acc[j] = 0.f;
       }
     };
@@ -303,14 +314,15 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
       };
       auto collect_last = [&] {
         if (i == 0) return;
-        collect(P - T::kRound);
+        collect(P - T::kRound, i - 1);
         if (block == 0) {
           flush();
           ++row_tile;
         }
       };
       // Into the weights that the products of the last block do not read, while they are under way; or, where there is room for
-      // one block only, behind them.
+      // one block only, behind them.  With room for the sums of two blocks those of the last one are read when the products of this
+      // one are on their way.
       const uint32_t to = mine + (T::kA == 2 ? (i & 1) * 64 : 0);
       unpack(0);
       if (T::kA == 1) collect_last();
@@ -322,23 +334,24 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
 #pragma unroll
       for (int c = 0; c < 2; ++c) z0[c] = z1[c];
       zeros(z1);
-      if (T::kA == 2) collect_last();
+      if (T::kA == 2 && T::kD == 1) collect_last();
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&a_full[wg]);
+      if (lane == 0) mbar_arrive(&a_full[wg][i & 1]);
+      if (T::kD == 2) collect_last();
 #pragma unroll
       for (int p = 0; p < P; ++p) scale[p] = next_scale[p];
 #pragma unroll
       for (int round = 0; round < T::kRounds - 1; ++round) {
-        collect(round * T::kRound);
+        collect(round * T::kRound, i);
         __syncwarp();
         if (lane == 0) mbar_arrive(&d_free[wg]);
       }
       if (++block == blocks) block = 0;
     }
     if (count > 0) {
-      collect(P - T::kRound);
+      collect(P - T::kRound, count - 1);
       flush();
     }
   }
@@ -350,27 +363,28 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
 }
 
 // Adds up the partial sums: 128 weight rows a CTA, 16 tokens, four of them a thread.
-template <int N>
+template <int N, int W>
 __global__ void __launch_bounds__(512) w4_linear_join_kernel(const __grid_constant__ W4TcArgs args, int ctas) {
   pdl_launch_dependents();
+  constexpr int kTile = W * 128;
   const W4LinearArgs& a = args.a;
-  const int row_tile = blockIdx.x / kW4TcGroups, row = blockIdx.x % kW4TcGroups * 128 + threadIdx.x % 128, token = blockIdx.y * 16 + threadIdx.x / 128 * 4;
-  const long long blocks = a.v.blocks, units = args.row_tiles * blocks, first = row_tile * blocks, segment = static_cast<long long>(N) * kW4TcTile;
+  const int row_tile = blockIdx.x / W, row = blockIdx.x % W * 128 + threadIdx.x % 128, token = blockIdx.y * 16 + threadIdx.x / 128 * 4;
+  const long long blocks = a.v.blocks, units = args.row_tiles * blocks, first = row_tile * blocks, segment = static_cast<long long>(N) * kTile;
   const int c0 = w4_run_of(first, units, ctas), c1 = w4_run_of(first + blocks - 1, units, ctas);
-  const float* from = args.parts + (row_tile + c0) * segment + token * kW4TcTile + row;   // the CTAs' pieces follow each other
+  const float* from = args.parts + (row_tile + c0) * segment + token * kTile + row;   // the CTAs' pieces follow each other
   const int here = min(4, a.rows - token);
   pdl_wait();
   float v[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) v[j] = j < here ? from[j * kW4TcTile] : 0.f;
+  for (int j = 0; j < 4; ++j) v[j] = j < here ? from[j * kTile] : 0.f;
 #pragma unroll 2
   for (int c = 1; c <= c1 - c0; ++c) {
     from += segment;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] += j < here ? from[j * kW4TcTile] : 0.f;
+    for (int j = 0; j < 4; ++j) v[j] += j < here ? from[j * kTile] : 0.f;
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) w4_store(a, token + j, static_cast<long long>(row_tile) * kW4TcTile + row, v[j]);
+  for (int j = 0; j < 4; ++j) w4_store(a, token + j, static_cast<long long>(row_tile) * kTile + row, v[j]);
 }
 
 }  // namespace thinfer
