@@ -270,7 +270,17 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
           for (int j = 0; j < N / 16; ++j) tmem_ld16(mine + T::kSums + (T::kD == 2 ? (i & 1) * (P * N) : 0) + p * N + 16 * j, d[j]);
           tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < N; ++j) acc[j] = fmaf(scale[first + p], __uint_as_float(d[j / 16][j % 16]), acc[j]);
+          for (int j = 0; j < N; j += 2) {
+            const float by = scale[first + p], x = __uint_as_float(d[j / 16][j % 16]), y = __uint_as_float(d[j / 16][j % 16 + 1]);
+            if (N == 32) {   // two at a time: 54 instead of 56 us for 24 x 32000 x 8192 in groups of 32; with 64 tokens' registers 84 instead of 80
+              const float2 v = f32x2_unpack(fma_f32x2(f32x2(by, by), f32x2(x, y), f32x2(acc[j], acc[j + 1])));
+              acc[j] = v.x;
+              acc[j + 1] = v.y;
+            } else {
+              acc[j] = fmaf(by, x, acc[j]);
+              acc[j + 1] = fmaf(by, y, acc[j + 1]);
+            }
+          }
         }
       }
       tc_fence_before();
