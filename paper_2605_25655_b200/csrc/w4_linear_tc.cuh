@@ -10,12 +10,13 @@
 // tokens in FP32.
 //
 // A CTA per SM: W warpgroups that unpack, each with its own 128 rows; a warp that feeds codes, scales and tokens of one block
-// after the other to a ring (three copies a block); and a warp for each warpgroup that issues its tensor instructions (as a
+// after the other to a ring (three copies a block, and the zeros by its lanes: loaded by those who unpack, two blocks ahead, they
+// cost 5 % more); and a warp for each warpgroup that issues its tensor instructions (as a
 // part of the unpacking warps that took a third of their time).  While the tensor cores multiply a block, its warpgroup unpacks
 // the next.  The (rows, block) units of the whole matrix are dealt out to the CTAs in equal contiguous runs; their partial
 // sums go to the workspace, and a last kernel adds them up in the order of the CTAs.
 //
-// 64 x 28672 x 8192 in groups of 128 (127 MB): 47 us in FP16, 50 in BF16, of which 5 are the two small kernels; 32 rows 36 and 39.  A
+// 64 x 28672 x 8192 in groups of 128 (127 MB): 46 us in FP16, 47 in BF16, of which 7 are the two small kernels; 32 rows 35 and 38.  A
 // copy would take 19, the products 18.  Bound by the unpacking: two or three warps for each of a SM's quarters do not cover its
 // dependences, and their registers (tokens' sums, codes, 64 unpacked words) leave room for no more.
 #pragma once
@@ -45,7 +46,7 @@ struct W4Tc {
   static constexpr int kRound = P <= kRoom ? P : kRoom >= 2 ? 2 : 1, kRounds = P / kRound;
   static constexpr int kD = kRounds == 1 && kA == 2 && 2 * P * N <= kColumns - kSums ? 2 : 1;
   static constexpr int kCodes = W * 8192, kScales = W * 8 * 32 * P, kTokens = N * 256;
-  static constexpr int kBytes = kCodes + kTokens + kScales, kStage = (kBytes + 1023) / 1024 * 1024;
+  static constexpr int kBytes = kCodes + kTokens + kScales, kZeros = W * 8 * 8 * P, kStage = (kBytes + kZeros + 1023) / 1024 * 1024;
   static constexpr int kFit = 224 * 1024 / kStage, kStages = kFit < 8 ? kFit : 8;
   static constexpr int kSmem = 1024 + kStages * kStage;
   static_assert(P % kRound == 0 && kSums + kD * kRound * N <= kColumns, "the sums of a round");
@@ -119,7 +120,7 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   if (tid == 0) {
     for (int i = 0; i < T::kStages; ++i) {
-      mbar_init(&full[i], 1);
+      mbar_init(&full[i], 1 + 32);       // the copies, and what each lane of the feeder has copied itself
       mbar_init(&empty[i], 4 * W + W);   // the warps that unpack, and the products that read the tokens
     }
     for (int i = 0; i < W; ++i) {
@@ -154,47 +155,58 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
 
   if (warp == 4 * W) {
     // The feeder.  Codes and scales were final before the kernel in front of this one let it start; the tokens are its work.
-    if (lane == 0) {
-      fence_proxy_async_all();
-      int tile = first_tile, block = first_block, token_block = first_block;
-      int issued = count;
-      bool waited = false;
-      auto tokens = [&](int i) {
+    fence_proxy_async_all();
+    int tile = first_tile, block = first_block, token_block = first_block;
+    int issued = count;
+    bool waited = false;
+    auto tokens = [&](int i) {
+      if (lane == 0)
         w4_bulk_load(ring + i % T::kStages * T::kStage + T::kCodes, args.tokens + static_cast<long long>(token_block) * T::kTokens, T::kTokens, &full[i % T::kStages]);
-        if (++token_block == blocks) token_block = 0;
-      };
-      for (int i = 0; i < count; ++i) {
-        const int s = i % T::kStages;
-        if (i >= T::kStages) {
-          if (!waited) {             // the ring is full: now the tokens of what is in it
-            waited = true;
-            pdl_wait();
-            fence_proxy_async_all();
-            for (int j = 0; j < i; ++j) tokens(j);
-          }
-          if (!wait(&empty[s], (i / T::kStages - 1) & 1)) {
-            issued = i;
-            break;
-          }
+      if (++token_block == blocks) token_block = 0;
+    };
+    auto tokens_are_there = [&] {
+      pdl_wait();
+      fence_proxy_async_all();
+    };
+    for (int i = 0; i < count; ++i) {
+      const int s = i % T::kStages;
+      if (i >= T::kStages) {
+        if (!waited) {             // the ring is full: now the tokens of what is in it
+          waited = true;
+          tokens_are_there();
+          for (int j = 0; j < i; ++j) tokens(j);
         }
-        uint8_t* stage = ring + s * T::kStage;
+        if (!__all_sync(0xffffffffu, wait(&empty[s], (i / T::kStages - 1) & 1))) {
+          issued = i;
+          break;
+        }
+      }
+      uint8_t* stage = ring + s * T::kStage;
+      if (lane == 0) {
         mbar_expect_tx(&full[s], T::kBytes);
         tma_load_3d(stage, &codes_map, &full[s], 0, block, tile * 8 * W);
         tma_load_3d(stage + T::kCodes + T::kTokens, &scales_map, &full[s], 0, block, tile * 8 * W);
-        if (waited) tokens(i);
-        if (++block == blocks) {
-          block = 0;
-          ++tile;
-        }
       }
-      if (!waited) {
-        pdl_wait();
-        fence_proxy_async_all();
-        for (int j = 0; j < count; ++j) tokens(j);
+      if (lane < 8 * W) {          // the zeros of a tile: up to 32 bytes, which need not be a tensor copy's 16
+        const uint8_t* from = a.v.zeros + (min(tile * 8 * W + lane, static_cast<int>(a.v.tiles) - 1) * static_cast<long long>(blocks) + block) * (8 * P);
+        const uint32_t to = smem_u32(stage + T::kBytes + lane * (8 * P));
+        if (P == 1) w4_copy8(to, from);
+        if (P >= 2) w4_copy16(to, from);
+        if (P == 4) w4_copy16(to + 16, from + 16);
       }
-      // nothing of its own is under way when it leaves
-      for (int i = issued > T::kStages ? issued - T::kStages : 0; i < issued; ++i) mbar_wait(&full[i % T::kStages], (i / T::kStages) & 1, nullptr);
+      asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&full[s])) : "memory");
+      if (waited) tokens(i);
+      if (++block == blocks) {
+        block = 0;
+        ++tile;
+      }
     }
+    if (!waited) {
+      tokens_are_there();
+      for (int j = 0; j < count; ++j) tokens(j);
+    }
+    // nothing of its own is under way when it leaves
+    for (int i = issued > T::kStages ? issued - T::kStages : 0; i < issued; ++i) mbar_wait(&full[i % T::kStages], (i / T::kStages) & 1, nullptr);
   } else if (warp > 4 * W) {
     // the products of warpgroup wg
     const int wg = warp - 4 * W - 1;
@@ -234,30 +246,6 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
     float scale[P] = {};
     uint32_t rounds = 0;            // of this warpgroup so far
     int row_tile = first_tile, block = first_block;
-    // the zero points, two units ahead: the bytes of P groups of row g of both tiles
-    const int last_tile = static_cast<int>(a.v.tiles) - 1;
-    int zero_tile = first_tile * 8 * W + 2 * warp, zero_block = first_block;
-    const uint8_t* zero_at[2];
-    auto zeros_of_tile = [&] {
-#pragma unroll
-      for (int c = 0; c < 2; ++c) zero_at[c] = a.v.zeros + ((static_cast<long long>(min(zero_tile + c, last_tile)) * blocks + zero_block) * 8 + (lane >> 2)) * P;
-    };
-    zeros_of_tile();
-    auto zeros = [&](uint32_t (&z)[2]) {
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        z[c] = P == 4 ? *reinterpret_cast<const uint32_t*>(zero_at[c]) : P == 2 ? *reinterpret_cast<const uint16_t*>(zero_at[c]) : *zero_at[c];
-        zero_at[c] += 8 * P;
-      }
-      if (++zero_block == blocks) {
-        zero_block = 0;
-        zero_tile += 8 * W;
-        zeros_of_tile();
-      }
-    };
-    uint32_t z0[2], z1[2];
-    zeros(z0);
-    zeros(z1);
     // adds the sums of the groups of the last round to this thread's row
     auto collect = [&](int first, int i) {   // i: the unit, counted from the run's beginning
       const bool ok = __all_sync(0xffffffffu, T::kRounds == 1 ? wait(&done[wg][i & 1], (i >> 1) & 1) : wait(&done[wg][0], rounds++ & 1));
@@ -309,13 +297,19 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
 #pragma unroll
       for (int p = 0; p < P; ++p)   // of this thread's row: tile lane / 16, row lane % 16
         next_scale[p] = h_to_f(reinterpret_cast<const half_t*>(stage + T::kCodes + T::kTokens)[(((2 * warp + (lane >> 4)) * 8 + (lane & 7)) * P + p) * 2 + ((lane >> 3) & 1)]);
+      uint32_t zero[2];             // the bytes of P groups of row g of both tiles
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const uint8_t* z = stage + T::kBytes + ((2 * warp + c) * 8 + (lane >> 2)) * P;
+        zero[c] = P == 4 ? *reinterpret_cast<const uint32_t*>(z) : P == 2 ? *reinterpret_cast<const uint16_t*>(z) : *z;
+      }
       uint32_t r[2][32];
       auto unpack = [&](int c) {
 #pragma unroll
         for (int w = 0; w < 8; ++w) {   // step w: columns 16 w .. of the block as they lie
           const uint4& from = codes[c][w / 4];
           uint32_t v[4];
-          w4_unpack<true>(w % 4 == 0 ? from.x : w % 4 == 1 ? from.y : w % 4 == 2 ? from.z : from.w, w4_zero<true>(z0[c] >> (8 * (w * P / 8)) & 255u), v);
+          w4_unpack<true>(w % 4 == 0 ? from.x : w % 4 == 1 ? from.y : w % 4 == 2 ? from.z : from.w, w4_zero<true>(zero[c] >> (8 * (w * P / 8)) & 255u), v);
           r[c][4 * w] = v[0];
           r[c][4 * w + 1] = v[2];
           r[c][4 * w + 2] = v[1];
@@ -341,9 +335,6 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
       tmem_st_16x64(to + (16u << 16), r[1]);
       __syncwarp();
       if (lane == 0) mbar_arrive(&empty[s]);
-#pragma unroll
-      for (int c = 0; c < 2; ++c) z0[c] = z1[c];
-      zeros(z1);
       if (T::kA == 2 && T::kD == 1) collect_last();
       tmem_st_wait();
       tc_fence_before();
