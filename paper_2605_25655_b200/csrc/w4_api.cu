@@ -112,13 +112,13 @@ int launch_linear(W4LinearArgs& a, cudaStream_t st) {
 // Whether the tensor-memory kernel takes over: in front of and behind its stream it has two small kernels (tokens laid out, partial
 // sums added up, some 5 us), while the other one walks over the weights again for every 16 rows, and needs up to 16 rows
 // for longer than the bytes only where there are many of them.  FP16, us, the other one / this one, by tiles x blocks:
-//   groups of 128  8192: 24 rows 11.0 / 11.2, 33 rows 13.5 / 12.0, 64 rows 17.2 / 13.5;  22016: 16 rows 12.4 / 15.6, 24 rows 18.0 / 16.2;
-//                  57344: 16 rows 24.2 / 24.1;  114688: 8 rows 29.2 / 36.7, 16 rows 40.2 / 35.7, 24 rows 69.1 / 36.2, 64 rows 137 / 47
-//   groups of 64   8192: 24 rows 10.9 / 12.4, 33 rows 13.7 / 12.5;  22016: 24 rows 18.5 / 18.0;  114688: 16 rows 42.0 / 44.5
-//   groups of 32   8192: 24 rows 11.8 / 11.8, 33 rows 15.0 / 14.5, 64 rows 19.1 / 16.3;  22016: 24 rows 20.6 / 18.1;  114688: 16 rows 47.1 / 50.9
+//   groups of 128  8192: 24 rows 11.0 / 11.0, 33 rows 13.5 / 12.0, 64 rows 17.2 / 13.7;  22016: 16 rows 12.4 / 15.2, 24 rows 18.0 / 15.7;
+//                  57344: 16 rows 24.2 / 23.4;  114688: 8 rows 29.2 / 33.0, 16 rows 40.2 / 34.0, 24 rows 69.1 / 34.3, 64 rows 137 / 46
+//   groups of 64   8192: 24 rows 10.9 / 10.8, 33 rows 13.7 / 12.5;  22016: 24 rows 18.5 / 15.1;  114688: 16 rows 42.0 / 40.8
+//   groups of 32   8192: 24 rows 11.8 / 11.6, 33 rows 15.0 / 14.7, 64 rows 19.1 / 16.3;  22016: 24 rows 20.6 / 16.6;  114688: 16 rows 47.1 / 47.1
 bool on_tensor_memory(int64_t rows, int64_t tiles, int64_t blocks, int group) {
   const int64_t units = tiles * blocks;
-  return rows > 16 ? units > (rows > 32 ? 7 : 10) * 1024 : rows > 8 && group == 128 && units > 80 * 1024;
+  return rows > 16 ? units > (rows > 32 ? 7 : 10) * 1024 : rows > 8 && group > 32 && units > 80 * 1024;
 }
 
 struct TcPlan {

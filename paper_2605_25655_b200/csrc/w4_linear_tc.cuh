@@ -26,7 +26,7 @@ namespace thinfer {
 
 // W: two warpgroups with 168 registers a thread, or three with 128 - where those are enough and the sums of 128 rows have room beside
 // the weights.  28672 x 8192, us, two / three: 64 rows 47.2 / 59.5 in groups of 128, 80 / 88 of 32; 32 rows 43.8 / 36.4 in groups of
-// 128, 45.3 / 46.2 of 64, 51.3 / 58.8 of 32.
+// 128, 45.3 / 46.2 of 64, 51.3 / 58.8 of 32 (before the zeros came through the ring).
 constexpr int w4_tc_groups(int n, int group) { return n == 64 || group < 128 ? 2 : 3; }
 
 struct W4TcArgs {

@@ -76,6 +76,24 @@ def test_verification_of_very_long_vocabularies(T, vocab):
     assert tokens.tolist() == want and [t[1] for t in want] == places
 
 
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,group", [(9, 32), (9, 64), (16, 64), (23, 32), (32, 64), (41, 64), (64, 32)])
+def test_products_of_a_large_matrix_in_small_groups(T, t, rows, group):
+    """Small whole numbers, more than 80 x 1024 tiles and blocks: nothing may be off, in any token row or behind the last one."""
+    torch, thinfer = T
+    n, k, tt = 20501, 8200, {"f16": torch.float16, "bf16": torch.bfloat16}[t]
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    w = torch.randint(-7, 8, (n, k), device="cuda", generator=gen).to(tt)
+    w[:, ::8], w[:, 1::8] = -7, 8                     # every group spans 15: codes are the numbers themselves
+    packed = thinfer.op_w4_quantize(w, group)
+    assert torch.equal(thinfer.op_w4_read(packed, n, k, group, tt), w)
+    x = torch.randint(-2, 3, (rows, k), device="cuda", generator=gen).to(tt)
+    want = torch.cat([x.double() @ part.double().T for part in w.split(4096)], 1)         # whole numbers below 2^18
+    out = torch.full((rows + 1, n + 2), 7.0, dtype=torch.float32, device="cuda")
+    thinfer.op_w4_linear(x, packed, n, group, out=out[:-1, 1:-1])
+    assert torch.equal(out[:-1, 1:-1].double(), want) and torch.all(out[-1] == 7) and torch.all(out[:, 0] == 7) and torch.all(out[:, -1] == 7)
+
+
 def test_first_calls_inside_a_capture():
     """A process that captures the very first call of each kind, and replays them on other numbers."""
     import os
