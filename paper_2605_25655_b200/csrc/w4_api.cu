@@ -157,7 +157,7 @@ int launch_tc(const W4LinearArgs& a, void* workspace, cudaStream_t st) {
   if (rc == THINFER_OK) rc = op_launch(w4_tokens_kernel<N>, dim3(static_cast<unsigned>((a.v.blocks * N * 16 + 255) / 256)), dim3(256), 0, st, args);
   if (rc == THINFER_OK) rc = op_launch(w4_linear_tc_kernel<N, P>, dim3(static_cast<unsigned>(p.ctas)), dim3(W4Tc<N, P>::kThreads), kSmem, st, args, codes, scales);
   if (rc == THINFER_OK)
-    rc = op_launch(w4_linear_join_kernel<N, W>, dim3(static_cast<unsigned>(p.row_tiles * W), static_cast<unsigned>((a.rows + 15) / 16)), dim3(512), 0, st, args, p.ctas);
+    rc = op_launch(w4_linear_join_kernel<N, W>, dim3(static_cast<unsigned>(p.row_tiles * W), static_cast<unsigned>((a.rows + N / 2 - 1) / (N / 2))), dim3(512), 0, st, args, p.ctas);
   return rc;
 }
 
