@@ -87,7 +87,9 @@ __device__ __forceinline__ void w4_bulk_load(void* dst, const void* src, uint32_
 template <int N>
 __global__ void __launch_bounds__(256) w4_tokens_kernel(const __grid_constant__ W4TcArgs args) {
   pdl_wait();
-  pdl_launch_dependents();   // behind the wait: what the next kernel reads before its own wait is final
+  // Behind the wait: the next kernel takes an SM's shared and tensor memory for itself, and its warps wait for the feeder's copies for a
+  // limited time, which must not pass behind a long predecessor of this one.
+  pdl_launch_dependents();
   const W4LinearArgs& a = args.a;
   const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
   const long long block = i / (N * 16);
@@ -154,38 +156,23 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
   };
 
   if (warp == 4 * W) {
-    // The feeder.  Codes and scales were final before the kernel in front of this one let it start; the tokens are its work.
+    // The feeder.  Nothing is read ahead of this wait: the packed weights may have been written by the kernel in front of the call.
+    pdl_wait();
     fence_proxy_async_all();
-    int tile = first_tile, block = first_block, token_block = first_block;
+    int tile = first_tile, block = first_block;
     int issued = count;
-    bool waited = false;
-    auto tokens = [&](int i) {
-      if (lane == 0)
-        w4_bulk_load(ring + i % T::kStages * T::kStage + T::kCodes, args.tokens + static_cast<long long>(token_block) * T::kTokens, T::kTokens, &full[i % T::kStages]);
-      if (++token_block == blocks) token_block = 0;
-    };
-    auto tokens_are_there = [&] {
-      pdl_wait();
-      fence_proxy_async_all();
-    };
     for (int i = 0; i < count; ++i) {
       const int s = i % T::kStages;
-      if (i >= T::kStages) {
-        if (!waited) {             // the ring is full: now the tokens of what is in it
-          waited = true;
-          tokens_are_there();
-          for (int j = 0; j < i; ++j) tokens(j);
-        }
-        if (!__all_sync(0xffffffffu, wait(&empty[s], (i / T::kStages - 1) & 1))) {
-          issued = i;
-          break;
-        }
+      if (i >= T::kStages && !__all_sync(0xffffffffu, wait(&empty[s], (i / T::kStages - 1) & 1))) {
+        issued = i;
+        break;
       }
       uint8_t* stage = ring + s * T::kStage;
       if (lane == 0) {
         mbar_expect_tx(&full[s], T::kBytes);
         tma_load_3d(stage, &codes_map, &full[s], 0, block, tile * 8 * W);
         tma_load_3d(stage + T::kCodes + T::kTokens, &scales_map, &full[s], 0, block, tile * 8 * W);
+        w4_bulk_load(stage + T::kCodes, args.tokens + static_cast<long long>(block) * T::kTokens, T::kTokens, &full[s]);
       }
       if (lane < 8 * W) {          // the zeros of a tile: up to 32 bytes, which need not be a tensor copy's 16
         const uint8_t* from = a.v.zeros + (min(tile * 8 * W + lane, static_cast<int>(a.v.tiles) - 1) * static_cast<long long>(blocks) + block) * (8 * P);
@@ -195,15 +182,10 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
         if (P == 4) w4_copy16(to + 16, from + 16);
       }
       asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&full[s])) : "memory");
-      if (waited) tokens(i);
       if (++block == blocks) {
         block = 0;
         ++tile;
       }
-    }
-    if (!waited) {
-      tokens_are_there();
-      for (int j = 0; j < count; ++j) tokens(j);
     }
     // nothing of its own is under way when it leaves
     for (int i = issued > T::kStages ? issued - T::kStages : 0; i < issued; ++i) mbar_wait(&full[i % T::kStages], (i / T::kStages) & 1, nullptr);
