@@ -325,10 +325,11 @@ struct W4ReadArgs {
 
 __device__ __forceinline__ half2_t w4_times(uint32_t x, half2_t s) { return __hmul2(*reinterpret_cast<half2_t*>(&x), s); }
 
+// Lets no later kernel start before it has ended: what it writes may be the weights of a model, and the kernels of a decode step read
+// those ahead of their wait.
 template <int G>
 __global__ void __launch_bounds__(256) w4_read_kernel(const __grid_constant__ W4ReadArgs a) {
   constexpr int P = 128 / G;
-  pdl_launch_dependents();
   pdl_wait();
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const long long units = a.v.tiles * a.v.blocks, step = static_cast<long long>(gridDim.x) * 8;

@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import tokens as tk
+from paper_2605_25655_b200 import synth
 
 pytestmark = pytest.mark.gpu
 INF, NAN = np.inf, np.nan
@@ -40,3 +41,45 @@ def test_weights_quantised_anew_between_products(T, t, rows, group):
         thinfer.op_w4_quantize(w[i % 2], group, packed=packed)
         got.append(thinfer.op_w4_linear(x, packed, n, group, out_fp32=True))
     assert all(torch.equal(y.double(), want[i % 2]) for i, y in enumerate(got))
+
+
+@pytest.mark.parametrize("mode", [0, 1, 2])
+@pytest.mark.parametrize("between", ["nothing", "probabilities"])
+def test_a_models_weights_read_back_in_front_of_a_step(T, mode, between):
+    """4-bit weights read back into the tensors of a model, directly in front of each decode step or with another call between them:
+    the same bits as with a pause behind the call."""
+    torch, thinfer = T
+    shape = synth.Shape(hidden=1024, n_q_heads=8, n_kv_heads=8, head_dim=128, ffn=2816, n_layers=1)
+    layers = thinfer.to_device_layers([synth.layer_weights(shape, 0)])
+    names = [n for n, w in layers[0].items() if w.dim() == 2]
+    packed = [{n: thinfer.op_w4_quantize(layers[0][n] * by, 64) for n in names} for by in (1.0, -0.75)]
+    x = torch.from_numpy(synth.hidden_states(shape, 0, (2, 24))).cuda()
+    logits = torch.randn(64, 5000, device="cuda")
+
+    def run(pause):
+        ctx = thinfer.Context(shape, layers, max_batch=2, max_seq=32)
+        ctx.set_launch_mode(mode)
+        out = [ctx.prefill(x[:, :8].contiguous())]
+        steps = [x[:, 8 + i].contiguous() for i in range(16)]
+        for i, step in enumerate(steps):
+            for n in reversed(names):
+                w = layers[0][n]
+                thinfer.op_w4_read(packed[i % 2][n], w.shape[0], w.shape[1], 64, torch.float16, out=w)
+            if between == "probabilities":
+                thinfer.op_token_probs(logits)
+            if pause:
+                torch.cuda.synchronize()
+            out.append(ctx.decode_step(step))
+            if pause:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        assert ctx.status() == 0
+        ctx.close()
+        return out
+    for w, p in ((layers[0][n], packed[1][n]) for n in names):
+        thinfer.op_w4_read(p, w.shape[0], w.shape[1], 64, torch.float16, out=w)
+    want = run(True)
+    assert torch.equal(layers[0][names[0]], thinfer.op_w4_read(packed[1][names[0]], *layers[0][names[0]].shape, 64, torch.float16))
+    assert not torch.equal(want[-1], want[-2])
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(run(False), want))
