@@ -67,7 +67,6 @@ __device__ __forceinline__ void w4_mma(float (&d)[4], const uint32_t (&a)[4], ui
 
 __device__ __forceinline__ void w4_store(const W4LinearArgs& a, long long row, long long out, float v) {
   if (row >= a.rows || out >= a.n) return;
-  v *= kW4SumsBy;
   if (a.fp32)
     static_cast<float*>(a.y)[row * a.y_stride + out] = v;
   else
@@ -105,8 +104,8 @@ __device__ __forceinline__ void w4_copies_wait() { asm volatile("cp.async.wait_g
 
 // sum += scale * (a block of R tiles times its tokens).  x[j]: where this lane finds its columns of token tile j; `quarter`
 // from one 32 columns to the next.
-template <int NT, int R, int P>
-__device__ __forceinline__ void w4_multiply(const uint8_t* stage, const uint4* const (&x)[NT], int quarter, float (&sum)[R][NT][4]) {
+template <int NT, int R, int P, bool FAR>
+__device__ __forceinline__ void w4_multiply(const uint8_t* stage, const uint32_t (&scales)[R][P], const uint4* const (&x)[NT], int quarter, float (&sum)[R][NT][4]) {
   const int lane = threadIdx.x & 31;
   uint4 codes[R][2];
 #pragma unroll
@@ -122,7 +121,8 @@ __device__ __forceinline__ void w4_multiply(const uint8_t* stage, const uint4* c
     for (int i = 0; i < R; ++i) {
       const int at = (i * 8 + (lane >> 2)) * P + p;
       z[i] = w4_zero<true>(stage[W4Stage<R, P>::kZeros + at]);
-      scale[i] = h2_to_f2(reinterpret_cast<const half2_t*>(stage + W4Stage<R, P>::kScales)[at]);
+      scale[i] = h2_to_f2(*reinterpret_cast<const half2_t*>(&scales[i][p]));
+      if (!FAR && kW4SumsBy != 1.f) scale[i].x *= kW4SumsBy, scale[i].y *= kW4SumsBy;
     }
 #pragma unroll
     for (int q = p * 4 / P; q < (p + 1) * 4 / P; ++q) {
@@ -145,6 +145,18 @@ __device__ __forceinline__ void w4_multiply(const uint8_t* stage, const uint4* c
         for (int j = 0; j < NT; ++j) w4_mma(d[i][j], r, token[j].z, token[j].w);
       }
     }
+    if (FAR)
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const bool x_far = w4_far(scale[i].x), y_far = w4_far(scale[i].y);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          d[i][j][0] *= x_far ? kW4SumsBy : 1.f, d[i][j][1] *= x_far ? kW4SumsBy : 1.f;
+          d[i][j][2] *= y_far ? kW4SumsBy : 1.f, d[i][j][3] *= y_far ? kW4SumsBy : 1.f;
+        }
+        scale[i].x *= x_far ? 1.f : kW4SumsBy;
+        scale[i].y *= y_far ? 1.f : kW4SumsBy;
+      }
 #pragma unroll
     for (int i = 0; i < R; ++i)
 #pragma unroll
@@ -155,6 +167,23 @@ __device__ __forceinline__ void w4_multiply(const uint8_t* stage, const uint4* c
         sum[i][j][3] = fmaf(scale[i].y, d[i][j][3], sum[i][j][3]);
       }
   }
+}
+
+template <int NT, int R, int P>
+__device__ __forceinline__ void w4_multiply(const uint8_t* stage, const uint4* const (&x)[NT], int quarter, float (&sum)[R][NT][4]) {
+  uint32_t scales[R][P];
+  bool far = false;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      scales[i][p] = reinterpret_cast<const uint32_t*>(stage + W4Stage<R, P>::kScales)[(i * 8 + (threadIdx.x & 31) / 4) * P + p];
+      far |= w4_far(scales[i][p]);
+    }
+  if (kW4SumsBy != 1.f && __any_sync(0xffffffffu, far))   // one way for the whole block: in between, a branch would keep the instructions of two groups apart
+    w4_multiply<NT, R, P, true>(stage, scales, x, quarter, sum);
+  else
+    w4_multiply<NT, R, P, false>(stage, scales, x, quarter, sum);
 }
 
 // The units of one warp on their way into its ring: one block of R tiles after the other along a row group, then the next

@@ -235,13 +235,28 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
       if (ok) {
 #pragma unroll
         for (int p = 0; p < T::kRound; ++p) {
+          const uint32_t from = mine + T::kSums + (T::kD == 2 ? (i & 1) * (P * N) : 0) + p * N;
+          const bool far = w4_far(scale[first + p]);
+          const float by = scale[first + p] * (far ? 1.f : kW4SumsBy);
+          if (kW4SumsBy != 1.f && __any_sync(0xffffffffu, far)) {   // few sums at a time: registers are short, and hardly any weights are that large
+            const float other = far ? kW4SumsBy : 1.f;
+#pragma unroll
+            for (int j = 0; j < N; j += 16) {
+              uint32_t d[16];
+              tmem_ld16(from + j, d);
+              tmem_ld_wait();
+#pragma unroll
+              for (int e = 0; e < 16; ++e) acc[j + e] = fmaf(by, __uint_as_float(d[e]) * other, acc[j + e]);
+            }
+            continue;
+          }
           uint32_t d[N / 16][16];
 #pragma unroll
-          for (int j = 0; j < N / 16; ++j) tmem_ld16(mine + T::kSums + (T::kD == 2 ? (i & 1) * (P * N) : 0) + p * N + 16 * j, d[j]);
+          for (int j = 0; j < N / 16; ++j) tmem_ld16(from + 16 * j, d[j]);
           tmem_ld_wait();
 #pragma unroll
           for (int j = 0; j < N; j += 2) {
-            const float by = scale[first + p], x = __uint_as_float(d[j / 16][j % 16]), y = __uint_as_float(d[j / 16][j % 16 + 1]);
+            const float x = __uint_as_float(d[j / 16][j % 16]), y = __uint_as_float(d[j / 16][j % 16 + 1]);
             if (N == 32) {   // two at a time: 54 instead of 56 us for 24 x 32000 x 8192 in groups of 32; with 64 tokens' registers 84 instead of 80
               const float2 v = f32x2_unpack(fma_f32x2(f32x2(by, by), f32x2(x, y), f32x2(acc[j], acc[j + 1])));
               acc[j] = v.x;

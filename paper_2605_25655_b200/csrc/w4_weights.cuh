@@ -38,7 +38,8 @@ inline size_t w4_packed_bytes(int n, int k, int group) {
 // c - zero of the 8 codes of one word as pairs of the storage type, exactly: r[0], r[2] of row g, r[1], r[3] of row 8 + g.
 // FP16: 0x6400 | c is 1024 + c; 0x6400 | 16 c is 1024 + 16 c, of which one multiply-add makes c - zero, so that only every
 // other pair needs a shift.  BF16 has seven bits behind the point: 0x4300 | c is 128 + c.  For sums (SUMS) the BF16 build makes
-// 2^-12 of that, at no cost: a token value times up to 15, 128 of them added up, could leave FP32, which a 4096th cannot.
+// 2^-12 of that, at no cost: a token value times up to 15, 128 of them added up, could leave FP32, which a 4096th cannot.  At the
+// other end nothing is lost: the smallest token, 2^-133, times 2^-12 is a multiple of FP32's smallest number.
 struct W4Zero {
   uint32_t lo, hi;   // of row g and of row 8 + g
 };
@@ -52,7 +53,7 @@ __device__ __forceinline__ uint32_t w4_sub(uint32_t a, uint32_t b) {
   return *reinterpret_cast<const uint32_t*>(&d);
 }
 #ifdef THINFER_BF16
-constexpr float kW4SumsBy = 4096.f;   // what sums of the differences are multiplied by
+constexpr float kW4SumsBy = 4096.f;   // what sums of the differences are multiplied by as the scale is applied
 template <bool SUMS>
 __device__ __forceinline__ W4Zero w4_zero(uint32_t both) {   // the byte of two zeros
   constexpr uint32_t kOne = SUMS ? 0x3d003d00u : 0x43004300u;
@@ -81,6 +82,11 @@ __device__ __forceinline__ void w4_unpack(uint32_t w, const W4Zero& z, uint32_t 
   }
 }
 #endif
+
+// Whether a scale times kW4SumsBy could leave FP32 (from 2^97; of a pair of 16-bit scales: one of them).  Then the group's sums are
+// multiplied instead: where that leaves FP32 so does their product with the scale.
+__device__ __forceinline__ bool w4_far(float scale) { return kW4SumsBy != 1.f && fabsf(scale) >= 0x1p97f; }
+__device__ __forceinline__ bool w4_far(uint32_t scales) { return kW4SumsBy != 1.f && (((scales & 0x70007000u) + 0x10001000u) & 0x80008000u) != 0; }
 
 // Two 16-bit numbers out of two pairs, chosen as __byte_perm chooses bytes.
 template <int Which>

@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import tokens as tk
+from oracle import w4
 from paper_2605_25655_b200 import synth
 
 pytestmark = pytest.mark.gpu
@@ -83,3 +84,51 @@ def test_a_models_weights_read_back_in_front_of_a_step(T, mode, between):
     assert not torch.equal(want[-1], want[-2])
     for _ in range(3):
         assert all(torch.equal(a, b) for a, b in zip(run(False), want))
+
+
+# ------------------------------------------------------------------ numbers at the ends of their types
+def _whole(rng, rows, n, k, group, t, scale, token):
+    """Packed weights with scales of 2^scale, tokens that are whole numbers times 2^token, and their products, which are exact in
+    FP64: whole numbers below 2^19 times a power of two."""
+    dt = {"float16": np.float16, "bfloat16": "bf16"}[t]
+    codes, zeros = rng.integers(0, 16, (n, k)), rng.integers(0, 16, (n, -(-k // group)))
+    of = np.arange(k) // group
+    x = rng.integers(-3, 4, (rows, k)).astype(np.float64)
+    want = (x @ (codes - zeros[:, of]).T.astype(np.float64)) * 2.0 ** (token + scale)
+    return w4.pack(codes, np.full(zeros.shape, 2.0 ** scale), zeros, group, dt), x * 2.0 ** token, want
+
+
+@pytest.mark.parametrize("t,scale,token", [("float16", -24, -24), ("float16", -14, -24), ("float16", 14, 13), ("bfloat16", -10, -133), ("bfloat16", 0, -126), ("bfloat16", -133, 0), ("bfloat16", -3, -117),
+                                           ("bfloat16", 100, -130), ("bfloat16", 125, -133), ("bfloat16", 127, -60), ("bfloat16", -100, 120), ("bfloat16", -133, 126), ("bfloat16", 3, 100)])
+@pytest.mark.parametrize("rows,n,k,group", [(1, 70, 600, 128), (8, 33, 392, 32), (16, 40, 1000, 64), (17, 2600, 8200, 128), (64, 2600, 8200, 128), (32, 2700, 8200, 32), (64, 2600, 8200, 64)])
+def test_products_over_the_range_of_the_type(T, t, scale, token, rows, n, k, group):
+    """Tokens and scales down to the smallest number of their type and up to the largest.  The results are whole numbers below 2^19
+    times 2^-143 and more, multiples of FP32's smallest number 2^-149, and so are all sums on the way: nothing may be off."""
+    torch, thinfer = T
+    rng = np.random.default_rng(rows + k)
+    packed, x, want = _whole(rng, rows, n, k, group, t, scale, token)
+    x, packed = torch.from_numpy(x).to(getattr(torch, t)).cuda(), torch.from_numpy(packed).cuda()
+    got = thinfer.op_w4_linear(x, packed, n, group, out_fp32=True)
+    assert np.array_equal(got.double().cpu().numpy(), want)
+    assert torch.equal(thinfer.op_w4_linear(x, packed, n, group), torch.from_numpy(want).cuda().to(getattr(torch, t)))
+
+
+@pytest.mark.parametrize("rows,n,k,group", [(3, 70, 600, 128), (12, 33, 392, 32), (20, 2600, 8200, 128), (64, 2600, 8200, 32)])
+def test_very_large_scales_beside_small_ones(T, rows, n, k, group):
+    """BF16: weight rows with scales near the type's end and rows with small ones, in turn of 3 and 5.  Tokens of 2^-60 leave the
+    former exact, and of the latter, which are multiples of 2^-160, each group's sum is rounded to a multiple of 2^-149 (sums of
+    those are exact); tokens of 2^120 leave FP32 in the former rows only."""
+    torch, thinfer = T
+    rng = np.random.default_rng(rows)
+    codes, zeros = rng.integers(0, 16, (n, k)), rng.integers(0, 16, (n, -(-k // group)))
+    large = np.arange(n) % 8 < 3
+    scale = np.where(large, 2.0 ** 127, 2.0 ** -100)[:, None]
+    packed = torch.from_numpy(w4.pack(codes, np.broadcast_to(scale, zeros.shape), zeros, group, "bf16")).cuda()
+    x = rng.integers(1, 4, (rows, k)).astype(np.float64)
+    whole = x @ (codes - zeros[:, np.arange(k) // group]).T.astype(np.float64)        # below 2^19
+    for token in (-60, 120):
+        got = thinfer.op_w4_linear(torch.from_numpy(x * 2.0 ** token).bfloat16().cuda(), packed, n, group, out_fp32=True).double().cpu().numpy()
+        want = whole * scale.T * 2.0 ** token
+        fine = np.broadcast_to(~large, want.shape) if token > 0 else np.ones(want.shape, bool)
+        tol = np.where(large | (token > 0), 0.0, -(-k // group) * 2.0 ** -150)
+        assert np.all(np.abs(got - want)[fine] <= np.broadcast_to(tol, want.shape)[fine]) and not np.any(np.isfinite(got[~fine]) & (whole[~fine] != 0))
