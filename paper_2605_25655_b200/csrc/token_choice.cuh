@@ -239,9 +239,12 @@ __global__ void __launch_bounds__(512, 3) token_probs_kernel(const __grid_consta
   if (ctas > 1) cluster_wait();
 }
 
-// Rows that no cluster holds: one CTA a row, which reads it three times, the second and third time from L2.
+// Rows that no cluster holds: one CTA a row, which reads it three times, the second and third time from L2.  A thread has more than 800
+// weights there: eight at a time are added up in FP32, what comes of them in FP64 (a running sum in FP32 would drift by
+// 2^-24 for every second weight of one size).
 __global__ void __launch_bounds__(512) token_probs_long_kernel(const __grid_constant__ TokenProbsArgs a) {
-  __shared__ float s_top[16], s_sum[16];
+  __shared__ float s_top[16];
+  __shared__ double s_sum[16];
   __shared__ int s_nan, s_index;
   pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -265,7 +268,7 @@ __global__ void __launch_bounds__(512) token_probs_long_kernel(const __grid_cons
   for (int w = 0; w < 16; ++w) top = fmaxf(top, s_top[w]);
   const bool greedy = !(temp > 0.f);
   const TokenHeat heat = token_heat(greedy ? 1.f : temp);
-  float sum = 0.f;
+  double sum = 0;
   if (greedy) {
     int index = INT_MAX;
 #pragma unroll 8
@@ -273,16 +276,21 @@ __global__ void __launch_bounds__(512) token_probs_long_kernel(const __grid_cons
       if (x[i] == top) index = min(index, static_cast<int>(i));
     if (index != INT_MAX) atomicMin(&s_index, index);
   } else {
-#pragma unroll 8
-    for (long long i = tid; i < a.vocab; i += 512) sum += token_weight(x[i] - top, heat);
+    for (long long i = tid; i < a.vocab; i += 8 * 512) {
+      float w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = i + 512 * e < a.vocab ? token_weight(x[i + 512 * e] - top, heat) : 0.f;
+      sum += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+    }
   }
-  sum = warp_sum(sum);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) s_sum[warp] = sum;
   __syncthreads();
-  sum = 0.f;
+  sum = 0;
   for (int w = 0; w < 16; ++w) sum += s_sum[w];
   const bool bad = s_nan != 0 || (!greedy && top == INFINITY), none = top == -INFINITY;
-  const float by = 1.f / sum;
+  const float by = static_cast<float>(1.0 / sum);
 #pragma unroll 8
   for (long long i = tid; i < a.vocab; i += 512)
     out[i] = bad ? __int_as_float(0x7fffffff) : none ? 0.f : greedy ? (i == s_index ? 1.f : 0.f) : token_weight(x[i] - top, heat) * by;

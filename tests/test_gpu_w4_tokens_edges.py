@@ -132,3 +132,19 @@ def test_very_large_scales_beside_small_ones(T, rows, n, k, group):
         fine = np.broadcast_to(~large, want.shape) if token > 0 else np.ones(want.shape, bool)
         tol = np.where(large | (token > 0), 0.0, -(-k // group) * 2.0 ** -150)
         assert np.all(np.abs(got - want)[fine] <= np.broadcast_to(tol, want.shape)[fine]) and not np.any(np.isfinite(got[~fine]) & (whole[~fine] != 0))
+
+
+@pytest.mark.parametrize("vocab", [442367, 1000003, 3000001])
+def test_sums_of_long_rows_do_not_drift(T, vocab):
+    """Weights of one size, whose running sum in 32 bits would be rounded to the same side again and again.  Eight weights at a
+    time are added up in FP32 (three roundings), the rest in FP64; a weight and the last product are off by 2^-24 for the
+    distance d / T and for twenty roundings."""
+    torch, thinfer = T
+    weights = np.array([0.45, 0.3, 0.9, 0.7, 1 / 3])
+    temp = np.array([1, 0.5, 2, 1, 1], np.float32)
+    x = np.tile((np.log(weights) * temp).astype(np.float32)[:, None], (1, vocab))
+    x[:, 17] = 0
+    want = tk.probs(x, temp)
+    got = thinfer.op_token_probs(torch.from_numpy(x).cuda(), torch.from_numpy(temp).cuda()).double().cpu().numpy()
+    tol = 2.0 ** -24 * (np.abs(x) / temp[:, None] + 23) * want
+    assert np.all(np.abs(got - want) <= tol)
