@@ -482,7 +482,8 @@ int thinfer_op_w4_linear(const void* x, int64_t x_stride, const void* packed, vo
 /* Probabilities of FP32 logits [rows][vocab], rows logit_stride elements apart: exp((l - max) / T) over their sum, FP32, rows
  * prob_stride elements apart; probs may be the logits themselves (same stride).  temperature: FP32 [rows], NULL: 1 for
  * all.  A row whose temperature is not positive (NaN too) gets 1 at the lowest index of its largest logit and 0 elsewhere.  A logit of -inf has
- * probability 0; a row that has no other gives zeros; one with a NaN (or with +inf, where T > 0) gives NaN. */
+ * probability 0; a row that has no other gives zeros; one with a NaN (or with +inf, where T > 0) gives NaN.  Temperatures between
+ * 0 and 2^-126 count as 2^-126; a logit whose exp((l - max) / T) is below 2^-126 may get 0. */
 int thinfer_op_token_probs(const float* logits, int64_t logit_stride, const float* temperature, float* probs, int64_t prob_stride,
                            int32_t rows, int32_t vocab, void* cuda_stream);
 

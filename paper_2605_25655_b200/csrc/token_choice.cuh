@@ -15,25 +15,28 @@ struct TokenProbsArgs {
   int vocab;
 };
 
-// exp(d / T) for d <= 0, with log2(e) / T = high + low: what the product loses comes back as a factor, so that the exponent
-// of a far logit is as exact as d itself.  Weights below 2^-126 are 0, those of -inf and NaN too.  Temperatures above 10^30 count as that.
+// exp(d / T) for the distance d <= 0 from the largest logit, with log2(e) / T = high + low: what the product loses comes back as a
+// factor, so that the exponent of a far logit is as exact as d itself.  Weights below 2^-126 are 0, those of -inf and NaN too.
+// Beyond T = 2^64 logits and T are taken 2^-80 times, so that no distance leaves FP32 that T would bring back; there an infinite T
+// may stand for 10^30, which makes every weight of a finite logit 1.  Temperatures below 2^-126 count as that.
 struct TokenHeat {
-  float high, low, rest, least;   // rest = low * ln 2; least: where the exponent is -200
+  float by, high, rest, least;   // by: what logits are multiplied by; rest = low * ln 2; least: where the exponent is -200
 };
 __device__ __forceinline__ TokenHeat token_heat(float temperature) {
   constexpr float kLog = 1.44269504088896f, kRest = 1.92596299e-8f;   // log2(e) and what FP32 leaves of it
-  const float high = fminf(fmaxf(kLog / temperature, 1e-30f), 3e38f);
-  const float low = temperature > 1e-37f && temperature < 1e30f ? (fmaf(-high, temperature, kLog) + kRest) / temperature : 0.f;
-  return {high, low, low * 0.693147180559945f, -200.f / high};
+  const float by = temperature > 0x1p64f ? 0x1p-80f : 1.f, t = fminf(fmaxf(temperature, 0x1p-126f) * by, 1e30f);
+  const float high = kLog / t, low = (fmaf(-high, t, kLog) + kRest) / t;
+  return {by, high, low * 0.693147180559945f, -200.f / high};
 }
-__device__ __forceinline__ float token_weight(float d, const TokenHeat& h) {
-  d = fmaxf(d, h.least);
+// The weight of logit x; top: the largest one times by.
+__device__ __forceinline__ float token_weight(float x, float top, const TokenHeat& h) {
+  const float d = fmaxf(fmaf(x, h.by, -top), h.least);
   const float a = d * h.high, rest = fmaf(fmaf(d, h.high, -a), 0.693147180559945f, d * h.rest), w = ex2_approx(a);
   return fmaf(w, rest, w);
 }
 // Two at a time.
 __device__ __forceinline__ uint64_t token_weights(float x, float y, float top, const TokenHeat& h) {
-  const uint64_t d = f32x2(fmaxf(x - top, h.least), fmaxf(y - top, h.least)), high = f32x2(h.high, h.high), a = mul_f32x2(d, high);
+  const uint64_t d = f32x2(fmaxf(fmaf(x, h.by, -top), h.least), fmaxf(fmaf(y, h.by, -top), h.least)), high = f32x2(h.high, h.high), a = mul_f32x2(d, high);
   const float2 e = f32x2_unpack(a);
   const uint64_t less = fma_f32x2(d, high, f32x2(-e.x, -e.y));
   const uint64_t rest = fma_f32x2(less, f32x2(0.693147180559945f, 0.693147180559945f), mul_f32x2(d, f32x2(h.rest, h.rest)));
@@ -169,10 +172,11 @@ __global__ void __launch_bounds__(512, 3) token_probs_kernel(const __grid_consta
     if (lane == 0 && index != INT_MAX) atomicMin(&s_index, index);
   } else {
     uint64_t sums = f32x2(0.f, 0.f);
+    const float its_top = top * heat.by;
 #pragma unroll 2
     for (int e = 0; e < mine; ++e) {
       float4 v = x[e * threads];
-      const uint64_t lo = token_weights(v.x, v.y, top, heat), hi = token_weights(v.z, v.w, top, heat);
+      const uint64_t lo = token_weights(v.x, v.y, its_top, heat), hi = token_weights(v.z, v.w, its_top, heat);
       sums = add_f32x2(sums, add_f32x2(lo, hi));
       *reinterpret_cast<ulonglong2*>(x + e * threads) = make_ulonglong2(lo, hi);
     }
@@ -206,14 +210,14 @@ __global__ void __launch_bounds__(512, 3) token_probs_kernel(const __grid_consta
     if (greedy) {
       first = __reduce_min_sync(0xffffffffu, its == all_top ? static_cast<int>(other.z) : INT_MAX);
     } else {
-      all_sum = __uint_as_float(other.y) * token_weight(its - all_top, heat);
+      all_sum = __uint_as_float(other.y) * token_weight(its, all_top * heat.by, heat);
 #pragma unroll
       for (int o = 4; o > 0; o >>= 1) all_sum += __shfl_xor_sync(0xffffffffu, all_sum, o);
       all_sum = __shfl_sync(0xffffffffu, all_sum, 0);
     }
   }
   const bool bad = all_top != all_top || (!greedy && all_top == INFINITY);
-  const float by = bad ? __int_as_float(0x7fffffff) : all_top == -INFINITY ? 0.f : token_weight(top - all_top, heat) / all_sum;
+  const float by = bad ? __int_as_float(0x7fffffff) : all_top == -INFINITY ? 0.f : token_weight(top, all_top * heat.by, heat) / all_sum;
   if (all_top == -INFINITY) first = INT_MAX;
   float* out = a.out + which * a.out_stride - row.before;
   const bool aligned = (reinterpret_cast<uintptr_t>(out) & 15) == 0;
@@ -268,6 +272,7 @@ __global__ void __launch_bounds__(512) token_probs_long_kernel(const __grid_cons
   for (int w = 0; w < 16; ++w) top = fmaxf(top, s_top[w]);
   const bool greedy = !(temp > 0.f);
   const TokenHeat heat = token_heat(greedy ? 1.f : temp);
+  const float its_top = top * heat.by;
   double sum = 0;
   if (greedy) {
     int index = INT_MAX;
@@ -279,7 +284,7 @@ __global__ void __launch_bounds__(512) token_probs_long_kernel(const __grid_cons
     for (long long i = tid; i < a.vocab; i += 8 * 512) {
       float w[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = i + 512 * e < a.vocab ? token_weight(x[i + 512 * e] - top, heat) : 0.f;
+      for (int e = 0; e < 8; ++e) w[e] = i + 512 * e < a.vocab ? token_weight(x[i + 512 * e], its_top, heat) : 0.f;
       sum += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
     }
   }
@@ -293,7 +298,7 @@ __global__ void __launch_bounds__(512) token_probs_long_kernel(const __grid_cons
   const float by = static_cast<float>(1.0 / sum);
 #pragma unroll 8
   for (long long i = tid; i < a.vocab; i += 512)
-    out[i] = bad ? __int_as_float(0x7fffffff) : none ? 0.f : greedy ? (i == s_index ? 1.f : 0.f) : token_weight(x[i] - top, heat) * by;
+    out[i] = bad ? __int_as_float(0x7fffffff) : none ? 0.f : greedy ? (i == s_index ? 1.f : 0.f) : token_weight(x[i], its_top, heat) * by;
 }
 
 // ------------------------------------------------------------------ verification

@@ -148,3 +148,25 @@ def test_sums_of_long_rows_do_not_drift(T, vocab):
     got = thinfer.op_token_probs(torch.from_numpy(x).cuda(), torch.from_numpy(temp).cuda()).double().cpu().numpy()
     tol = 2.0 ** -24 * (np.abs(x) / temp[:, None] + 23) * want
     assert np.all(np.abs(got - want) <= tol)
+
+
+@pytest.mark.parametrize("vocab", [6, 3001, 150001, 450001])
+def test_temperatures_over_their_range(T, vocab):
+    """Logits and temperatures of any size: only the quotient d / T decides.  The distance d is rounded once; twenty roundings
+    more, and the additions of a thread's weights, as for usual temperatures."""
+    torch, thinfer = T
+    top = np.float32(3.4e38)
+    temp = np.array([3e38, 3e38, 1e38, 2e30, 1.5e30, 1e31, 2.0 ** 64, 2.0 ** 65, 1e25, INF, INF, 3e38, 1e-38, 2.0 ** -126, 2.0 ** -120], np.float32)
+    size = np.array([3.4e38, 1e30, 3.4e38, 1e31, 1e30, 3.4e38, 1e20, 1e20, 1e25, 3.4e38, 1.0, 5.0, 2.0 ** -125, 2.0 ** -126, 2.0 ** -119])
+    rng = np.random.default_rng(vocab)
+    x = np.clip(rng.uniform(-1, 1, (len(temp), vocab)) * size[:, None], -top, top).astype(np.float32)
+    x[:, 1], x[:, -1] = size, -size                   # the far ends
+    x[:, 2] = -INF                                    # a masked token keeps its 0 at any temperature
+    x[:2, 3] = -top
+    with np.errstate(over="ignore"):
+        want = tk.probs(x, temp)
+    far = np.where(np.isneginf(x), 0, x.astype(np.float64).max(1, keepdims=True) - x) / np.maximum(temp, 2.0 ** -126).astype(np.float64)[:, None]
+    want[12] = tk.probs(x[12:13], np.array([2.0 ** -126]))[0]      # smaller ones count as the smallest normal number
+    got = thinfer.op_token_probs(torch.from_numpy(x).cuda(), torch.from_numpy(temp).cuda()).double().cpu().numpy()
+    tol = 2.0 ** -24 * (far + 20 + min(vocab / 256, 90)) * want + 2.0 ** -126
+    assert np.all(got[:, 2] == 0) and np.all(np.abs(got - want) <= tol), [(i, np.abs(got[i] - want[i]).max(), want[i].max()) for i in range(len(temp)) if np.any(np.abs(got[i] - want[i]) > tol[i])]
