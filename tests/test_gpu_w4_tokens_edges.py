@@ -170,3 +170,84 @@ def test_temperatures_over_their_range(T, vocab):
     got = thinfer.op_token_probs(torch.from_numpy(x).cuda(), torch.from_numpy(temp).cuda()).double().cpu().numpy()
     tol = 2.0 ** -24 * (far + 20 + min(vocab / 256, 90)) * want + 2.0 ** -126
     assert np.all(got[:, 2] == 0) and np.all(np.abs(got - want) <= tol), [(i, np.abs(got[i] - want[i]).max(), want[i].max()) for i in range(len(temp)) if np.any(np.abs(got[i] - want[i]) > tol[i])]
+
+
+# ------------------------------------------------------------------ requests that differ, threads
+@pytest.mark.parametrize("batch,n,vocab", [(1, 3, 33), (40, 4, 1000), (9, 2, 100003), (70, 7, 515), (3, 600, 40)])
+def test_certain_drafts_of_ragged_counts(T, batch, n, vocab):
+    """Drafts without probabilities, each request with a count of its own: padding, none, some, all, more than there are; most drafts
+    stay, so that many requests keep all of their count and draw from the row behind it, of which nothing is taken off."""
+    torch, thinfer = T
+    rng = np.random.default_rng(batch + n + vocab)
+    w = rng.random((batch, n + 1, vocab)) ** 8
+    p = (w / w.sum(-1, keepdims=True)).astype(np.float32)
+    drafts = rng.integers(0, vocab, (batch, n)).astype(np.int32)
+    u = np.minimum(rng.random((batch, n + 1)), 1 - 2.0 ** -24).astype(np.float32)
+    u[:, :n] = np.take_along_axis(p[:, :n], drafts[..., None], 2)[..., 0] * rng.choice([0.5, 2.0], (batch, n), p=[0.9, 0.1]).astype(np.float32)
+    counts = (np.arange(batch) % (n + 4) - 1 if n < 20 else np.array([-1, 300, n + 2])).astype(np.int32)
+    want, kept = tk.verify(p, None, drafts, u, counts)
+    assert batch < 9 or any(0 < c < n and k == c for c, k in zip(counts, kept))
+    tokens = torch.full((batch, n + 1), -77, dtype=torch.int32, device="cuda")
+    accepted = torch.full((batch,), -77, dtype=torch.int32, device="cuda")
+    cuda = [torch.from_numpy(a).cuda() for a in (p, drafts, u, counts)]
+    thinfer.op_verify_drafts(cuda[0], None, cuda[1], cuda[2], cuda[3], tokens, accepted)
+    for b in range(batch):
+        assert (tokens[b].tolist(), int(accepted[b])) == (([-77] * (n + 1), -77) if want[b] is None else (want[b], kept[b])), b
+
+
+def test_threads_finish_their_rounds(T):
+    """Products on both kernels, probabilities and verification from four threads on streams of their own; every thread counts the
+    rounds that it has compared, and none is left behind."""
+    import threading
+    torch, thinfer = T
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    inputs = []
+    for i in range(4):
+        t = (torch.float16, torch.bfloat16)[i % 2]
+        packed = thinfer.op_w4_quantize((torch.randn(2600 + 16 * i, 8200, generator=gen, device="cuda") * 0.02).to(t), 128)
+        inputs.append((packed, 2600 + 16 * i, torch.randn(64, 8200, generator=gen, device="cuda").to(t), torch.randint(0, 2600, (16, 3), generator=gen, device="cuda").int(),
+                       torch.rand(16, 4, generator=gen, device="cuda")))
+
+    def run(packed, n, x, drafts, u):
+        y = thinfer.op_w4_linear(x, packed, n, 128, out_fp32=True)
+        p = thinfer.op_token_probs(y).view(16, 4, n)
+        return [y, thinfer.op_w4_linear(x[:8], packed, n, 128), p, *thinfer.op_verify_drafts(p, None, drafts, u)]
+    want = [run(*i) for i in inputs]
+    torch.cuda.synchronize()
+    rounds, equal = [0] * 4, [0] * 4
+
+    def thread(i):
+        torch.cuda.set_device(0)
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(20):
+                got = run(*inputs[i])
+                stream.synchronize()
+                rounds[i] += 1
+                equal[i] += all(torch.equal(a, b) for a, b in zip(got, want[i]))
+    threads = [threading.Thread(target=thread, args=(i,), daemon=True) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(120)
+    assert not any(t.is_alive() for t in threads) and rounds == equal == [20] * 4
+
+
+@pytest.mark.parametrize("rows,vocab", [(40, 131069), (40, 131070), (40, 151936), (36, 221184), (40, 256000)])
+def test_many_rows_of_long_vocabularies(T, rows, vocab):
+    """Clusters of every size and slice, rows at every alignment.  At most 108 weights are added up by a thread, half of them
+    in each of two sums, and twenty roundings more."""
+    torch, thinfer = T
+    rng = np.random.default_rng(vocab)
+    x = (rng.standard_normal((rows, vocab)) * 4).astype(np.float32)
+    temp = rng.uniform(0.5, 1.5, rows).astype(np.float32)
+    temp[::7] = 0
+    x[3, vocab - 1] = x[3].max() + 1
+    wide = torch.full((rows, vocab + 1), 99.0, device="cuda")
+    wide[:, 1:] = torch.from_numpy(x).cuda()
+    want = tk.probs(x, temp)
+    far = (x.max(1, keepdims=True).astype(np.float64) - x) / np.where(temp > 0, temp, 1)[:, None]
+    got = thinfer.op_token_probs(wide[:, 1:], torch.from_numpy(temp).cuda())
+    assert np.all(np.abs(got.double().cpu().numpy() - want) <= 2.0 ** -24 * (far + 54 + 20) * want + 2.0 ** -126)
+    thinfer.op_token_probs(wide[:, 1:], torch.from_numpy(temp).cuda(), out=wide[:, 1:])
+    assert torch.equal(wide[:, 1:], got) and torch.all(wide[:, 0] == 99)
