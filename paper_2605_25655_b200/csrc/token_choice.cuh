@@ -516,7 +516,7 @@ __global__ void __launch_bounds__(512, 2) verify_drafts_kernel(const __grid_cons
             value.part(1, rest(x.y, y.y), target);
             value.part(2, rest(x.z, y.z), target);
             value.part(3, rest(x.w, y.w), target);
-            s_token = 4 * s + value.picked - row.before;
+            s_token = static_cast<int>(4ll * s + value.picked - row.before);
           }
         }
         __syncthreads();

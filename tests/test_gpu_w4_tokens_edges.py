@@ -251,3 +251,39 @@ def test_many_rows_of_long_vocabularies(T, rows, vocab):
     assert np.all(np.abs(got.double().cpu().numpy() - want) <= 2.0 ** -24 * (far + 54 + 20) * want + 2.0 ** -126)
     thinfer.op_token_probs(wide[:, 1:], torch.from_numpy(temp).cuda(), out=wide[:, 1:])
     assert torch.equal(wide[:, 1:], got) and torch.all(wide[:, 0] == 99)
+
+
+def test_the_longest_vocabulary(T):
+    """2^31 - 1 tokens in a row that begins three numbers behind a 16-byte boundary, so that its last ones are numbers 2^31 and more
+    of their walk: drawn, drafted, the largest logit, and its probability."""
+    torch, thinfer = T
+    vocab = 2 ** 31 - 1
+    row = torch.zeros(vocab + 5, device="cuda")
+    assert row.data_ptr() % 16 == 0
+    p = row[3:3 + vocab].view(1, 1, vocab)
+    empty = torch.zeros(1, 0, dtype=torch.int32, device="cuda")
+    for places, u, token in (((vocab - 1,), 0.5, vocab - 1), ((vocab - 3, vocab - 2), 0.25, vocab - 3), ((5, vocab - 2), 0.75, vocab - 2), ((0, vocab - 1), 0.25, 0)):
+        for place in places:
+            p[0, 0, place] = 0.5
+        tokens, accepted = thinfer.op_verify_drafts(p, None, empty, torch.full((1, 1), u, device="cuda"))
+        assert tokens.tolist() == [[token]] and accepted.tolist() == [0]
+        for place in places:
+            p[0, 0, place] = 0
+    draft = torch.tensor([[vocab - 1]], dtype=torch.int32, device="cuda")
+    two = p.expand(1, 2, vocab)
+    p[0, 0, vocab - 1], p[0, 0, vocab - 2] = 0.25, 0.75
+    for u, want in ((0.2, [[vocab - 1, vocab - 2]]), (0.3, [[vocab - 2, -1]])):
+        assert thinfer.op_verify_drafts(two, None, draft, torch.tensor([[u, 0.5]], device="cuda"))[0].tolist() == want
+    logits = p[0]
+    logits.zero_()
+    logits[0, vocab - 1] = 20
+    thinfer.op_token_probs(logits, torch.zeros(1, device="cuda"), out=logits)
+    assert logits[0, vocab - 1] == 1 and logits[0, :vocab - 1].max() == 0
+    logits[0, vocab - 1] = 20
+    thinfer.op_token_probs(logits, out=logits)
+    far = np.exp(-20.0)
+    one = 1 / (1 + far * (vocab - 1))
+    last, least, most = (float(v) for v in (logits[0, vocab - 1], logits[0, :vocab - 1].min(), logits[0, :vocab - 1].max()))
+    tol = 2.0 ** -24 * (20 + 23)                      # the distance, twenty roundings, three more of the sums
+    assert abs(last - one) <= tol * one and least == most and abs(most - far * one) <= tol * far * one
+    assert torch.all(row[:3] == 0) and torch.all(row[3 + vocab:] == 0)
