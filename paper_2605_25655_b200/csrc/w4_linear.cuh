@@ -188,7 +188,7 @@ __device__ __forceinline__ void w4_multiply(const uint8_t* stage, const uint4* c
 
 // The units of one warp on their way into its ring: one block of R tiles after the other along a row group, then the next
 // group's.  Every lane keeps the address of what it copies itself, so that a unit costs a few additions.
-template <int R, int P, int Ahead, int TileStep>
+template <int R, int P>
 struct W4Feed {
   static constexpr int kPieces = 5 * P * R;       // of 8 bytes: 4 P of scales and P of zeros for each tile
   const W4LinearArgs& a;
@@ -215,16 +215,7 @@ struct W4Feed {
     }
   }
   __device__ __forceinline__ W4Feed(const W4LinearArgs& args, uint32_t ring_, int u0, int u1, int steps_, int here_, int block_, int first_tile)
-      : a(args), ring(ring_), to(ring_), left(u1 - u0), step(u0 % steps_), steps(steps_), here(here_), block(block_), tile(first_tile + u0 / steps_ * TileStep) {
-    begin_group();
-    codes += step * 1024;
-#pragma unroll
-    for (int h = 0; h < (kPieces + 31) / 32; ++h) params[h] += step * stride(h);
-  }
-  // Goes to unit u of (row group, block) units whose first group begins at first_tile.
-  __device__ __forceinline__ void at(long long u, int blocks, int first_tile) {
-    step = static_cast<int>(u % blocks);
-    tile = first_tile + static_cast<int>(u / blocks) * TileStep;
+      : a(args), ring(ring_), to(ring_), left(u1 - u0), step(u0 % steps_), steps(steps_), here(here_), block(block_), tile(first_tile + u0 / steps_ * R) {
     begin_group();
     codes += step * 1024;
 #pragma unroll
@@ -252,14 +243,14 @@ struct W4Feed {
       --left;
       if (++step == steps) {
         step = 0;
-        tile += TileStep;
+        tile += R;
         if (left > 0) begin_group();
       } else {
         codes += 1024;
 #pragma unroll
         for (int h = 0; h < (kPieces + 31) / 32; ++h) params[h] += stride(h);
       }
-      to = to == ring + Ahead * W4Stage<R, P>::kBytes ? ring : to + W4Stage<R, P>::kBytes;
+      to = to == ring + kW4Ahead * W4Stage<R, P>::kBytes ? ring : to + W4Stage<R, P>::kBytes;
     }
     w4_copies_done();
   }
@@ -296,7 +287,7 @@ __global__ void __launch_bounds__(Warps * 32, 1) w4_linear_kernel(const __grid_c
     for (int phase = 0; phase * held < slice || phase == 0; ++phase) {
       const int here = min(held, slice - phase * held);     // blocks of this phase; the rest of `held` is skipped
       const bool tokens = from == group0 || held < slice;   // to be fetched for this phase
-      W4Feed<R, P, kW4Ahead, R> feed(a, smem_u32(ring), u0, u1, held, here, block0 + phase * held, from * R);
+      W4Feed<R, P> feed(a, smem_u32(ring), u0, u1, held, here, block0 + phase * held, from * R);
       if (!waited) pdl_wait();                              // behind the index arithmetic, which takes as long as a load
       waited = true;
       if (tokens) {
