@@ -467,14 +467,16 @@ int thinfer_w4_bytes(int32_t n_out, int32_t k, int32_t group, size_t* bytes);
 int thinfer_op_w4_quantize(const void* w, int64_t w_stride, void* packed, int32_t n_out, int32_t k, int32_t group, void* cuda_stream);
 
 /* Reads packed weights back as FP16 [n_out][k], rows w_stride elements apart (a multiple of 8): scale * (code - zero),
- * rounded once (beyond the type's largest value that is infinity).  For prompts, whose products run on thinfer_op_linear. */
+ * rounded once (beyond the type's largest value that is infinity).  For prompts, whose products run on thinfer_op_linear.  w may be
+ * weights of a context: a step behind the call reads them as the call leaves them. */
 int thinfer_op_w4_read(const void* packed, void* w, int64_t w_stride, int32_t n_out, int32_t k, int32_t group, void* cuda_stream);
 
 /* y[rows, n_out] = x[rows, k] * (packed weights)^T for 1 .. 64 rows: FP32 sums of exact products, group by group, FP16 out
  * (out_fp32 == 0) or FP32 out.  x: rows x_stride elements apart (a multiple of 8), 16-byte aligned; y: rows y_stride
  * elements apart.  The sums have to stay inside FP32; beyond it they come out as infinity or NaN.  Equal calls give equal
- * bits.  The waits inside the device are bounded; results whose wait has run out are NaN.  workspace: thinfer_w4_linear_workspace bytes, 16-byte aligned (0 bytes, NULL: none is needed); its contents mean
- * nothing between calls, but calls that may overlap on the device need their own, and it must not overlap another tensor. */
+ * bits.  The waits inside the device are bounded; results whose wait has run out are NaN, and the call reports nothing else of it.
+ * workspace: thinfer_w4_linear_workspace bytes, 16-byte aligned (0 bytes, NULL: none is needed); its contents mean nothing
+ * between calls, but calls that may overlap on the device need their own, and it must not overlap another tensor. */
 int thinfer_w4_linear_workspace(int32_t rows, int32_t n_out, int32_t k, int32_t group, size_t* bytes);
 int thinfer_op_w4_linear(const void* x, int64_t x_stride, const void* packed, void* y, int64_t y_stride, int32_t rows, int32_t n_out,
                          int32_t k, int32_t group, int32_t out_fp32, void* workspace, size_t workspace_bytes, void* cuda_stream);

@@ -111,11 +111,12 @@ int launch_linear(W4LinearArgs& a, cudaStream_t st) {
 
 // Whether the tensor-memory kernel takes over: in front of and behind its stream it has two small kernels (tokens laid out, partial
 // sums added up, some 5 us), while the other one walks over the weights again for every 16 rows, and needs up to 16 rows
-// for longer than the bytes only where there are many of them.  FP16, us, the other one / this one, by tiles x blocks:
-//   groups of 128  8192: 24 rows 11.0 / 11.0, 33 rows 13.5 / 12.0, 64 rows 17.2 / 13.7;  22016: 16 rows 12.4 / 15.2, 24 rows 18.0 / 15.7;
-//                  57344: 16 rows 24.2 / 23.4;  114688: 8 rows 29.2 / 33.0, 16 rows 40.2 / 34.0, 24 rows 69.1 / 34.3, 64 rows 137 / 46
-//   groups of 64   8192: 24 rows 10.9 / 10.8, 33 rows 13.7 / 12.5;  22016: 24 rows 18.5 / 15.1;  114688: 16 rows 42.0 / 40.8
-//   groups of 32   8192: 24 rows 11.8 / 11.6, 33 rows 15.0 / 14.7, 64 rows 19.1 / 16.3;  22016: 24 rows 20.6 / 16.6;  114688: 16 rows 47.1 / 47.1
+// for longer than the bytes only where there are many of them.  FP16, us, the other one / this one, by tiles x blocks (a call
+// of these varies by up to 5 %):
+//   groups of 128  8192: 24 rows 10.6 / 10.9, 33 rows 13.2 / 12.7, 64 rows 16.5 / 14.5;  22016: 16 rows 12.7 / 15.4, 24 rows 17.3 / 15.7;
+//                  57344: 16 rows 22.4 / 21.6;  114688: 8 rows 29.8 / 32.2, 16 rows 39.0 / 33.3, 24 rows 66.5 / 34.4, 64 rows 131 / 46
+//   groups of 64   8192: 24 rows 10.8 / 12.2, 33 rows 13.7 / 13.9;  22016: 16 rows 13.0 / 15.6, 24 rows 18.5 / 15.7;  114688: 16 rows 42.5 / 40.4
+//   groups of 32   8192: 24 rows 11.6 / 11.7, 33 rows 14.6 / 15.4, 64 rows 18.7 / 17.2;  22016: 24 rows 20.1 / 17.0;  114688: 16 rows 46.6 / 46.0
 bool on_tensor_memory(int64_t rows, int64_t tiles, int64_t blocks, int group) {
   const int64_t units = tiles * blocks;
   return rows > 16 ? units > (rows > 32 ? 7 : 10) * 1024 : rows > 8 && group > 32 && units > 80 * 1024;
@@ -132,7 +133,8 @@ TcPlan plan_tc(int n, int group, int64_t tiles, int64_t blocks) {
   const int64_t tile = w4_tc_groups(n, group) * 128;
   TcPlan p{};
   p.row_tiles = (tiles * 16 + tile - 1) / tile;
-  // as many CTAs as the device has SMs, but no more than 8 for a row tile, whose sums one thread adds up
+  // as many CTAs as the device has SMs, but no more than 8 a row tile, whose sums one thread adds up (runs do not begin with a tile:
+  // up to 9 CTAs may have a piece of it)
   const int64_t most = blocks < 8 ? p.row_tiles * blocks : p.row_tiles * 8;
   const int sms = op_sm_count();
   p.ctas = most < sms ? static_cast<int>(most) : sms;

@@ -5,8 +5,8 @@
 // 8 tokens, 16 columns) multiplies them with the tokens without any rounding; its FP32 sums are scaled group by group.
 //
 // Bound by the weights' bytes: every warp brings its own into a ring of shared memory, two units of 2 KB ahead of the one that it
-// multiplies, 64 KB under way per SM (loads into registers instead stopped each warp at its newest load, 42 us against 29
-// for 4 x 28672 x 8192).  The device is divided into clusters of 1 to 8 CTAs, one CTA of 16 or 12 warps per SM.  A cluster owns a
+// multiplies, 64 KB (with two token tiles 48) under way per SM (loads into registers instead stopped each warp at its newest load, 42 us
+// against 29 for 4 x 28672 x 8192).  The device is divided into clusters of 1 to 8 CTAs, one CTA of 16 (12) warps per SM.  A cluster owns a
 // run of weight rows, and each of its CTAs a slice of the columns, whose tokens it keeps in shared memory in the order of
 // the lanes that read them.  Inside a CTA the (32 rows, 128 columns) units are dealt out to the warps in equal contiguous
 // runs; what a warp has summed up for its rows goes to a slot of shared memory, and at the end the cluster adds up the
@@ -14,7 +14,8 @@
 //
 // 4 x 28672 x 8192 in groups of 128 (122 MB): 29 us alone in a graph, 65 % of a copy's rate; the stream itself takes 20 us (6.0
 // TB/s), the rest is the launch, the tokens (1.2 us), the sums in the CTA and the cluster (2.5 us).  1 x 4096 x 4096: 5.9 us.
-// 16 x 28672 x 8192: 40 us; the matrix instructions take 28 of 68 cycles a unit, dependences between few warps the rest.
+// 16 x 28672 x 8192: 39 us; the matrix instructions take 28 of 68 cycles a unit, dependences between few warps the rest.  BF16, whose
+// scales take the factor of the differences off: 44 us.  In groups of 32 up to 12 bytes a thread are spilled.
 // Tried: FP16 codes as subnormal numbers with the zero points taken off sums of the tokens (half of the unpacking: no
 // change for 8 tokens, 46 instead of 41 us for 16); four tiles a warp and 8 warps (32 and 47 us); one tile and 16 warps.
 #pragma once
@@ -345,7 +346,7 @@ __global__ void __launch_bounds__(Warps * 32, 1) w4_linear_kernel(const __grid_c
     }
     __syncthreads();
     // What the warps of this CTA have for each row group, in the order of the warps: w0 holds the group's first unit, w1 its
-    // last; the sum goes to w0's slot.  Warp w begins at unit w * units / 16.
+    // last; the sum goes to w0's slot.  Warp w begins at unit w * units / Warps.
     auto warp_of = [&](int unit) { return __popc(__ballot_sync(0xffffffffu, lane < Warps && units * lane / Warps <= unit)) - 1; };
     float4* slot = reinterpret_cast<float4*>(slots) + lane;
     for (int g = warp; g < batch; g += Warps) {

@@ -16,7 +16,7 @@
 // the next.  The (rows, block) units of the whole matrix are dealt out to the CTAs in equal contiguous runs; their partial
 // sums go to the workspace, and a last kernel adds them up in the order of the CTAs.
 //
-// 64 x 28672 x 8192 in groups of 128 (127 MB): 46 us in FP16, 47 in BF16, of which 7 are the two small kernels; 32 rows 35 and 38.  A
+// 64 x 28672 x 8192 in groups of 128 (127 MB): 45 us in FP16, 47 in BF16, of which 7 are the two small kernels; 32 rows 34 and 37.  A
 // copy would take 19, the products 18.  Bound by the unpacking: two or three warps for each of a SM's quarters do not cover its
 // dependences, and their registers (tokens' sums, codes, 64 unpacked words) leave room for no more.
 #pragma once
@@ -25,8 +25,8 @@
 namespace thinfer {
 
 // W: two warpgroups with 168 registers a thread, or three with 128 - where those are enough and the sums of 128 rows have room beside
-// the weights.  28672 x 8192, us, two / three: 64 rows 47.2 / 59.5 in groups of 128, 80 / 88 of 32; 32 rows 43.8 / 36.4 in groups of
-// 128, 45.3 / 46.2 of 64, 51.3 / 58.8 of 32 (before the zeros came through the ring).
+// the weights.  28672 x 8192 in FP16, us, two / three: 64 rows 44.7 / 45.0 in groups of 128, 54.6 / 64.2 of 64, 77.8 / 84.1 of 32; 32 rows
+// 38.7 / 34.3 in groups of 128, 41.2 / 41.0 of 64, 48.1 / 57.0 of 32 (BF16 the same way).
 constexpr int w4_tc_groups(int n, int group) { return n == 64 || group < 128 ? 2 : 3; }
 
 struct W4TcArgs {
@@ -270,8 +270,7 @@ w4_linear_tc_kernel(const __grid_constant__ W4TcArgs args, const __grid_constant
       }
       tc_fence_before();
     };
-    // What this CTA has of a row tile.  Short code: it runs once or twice, and the instructions of 64 tokens'
-    // sums and stores side by side took longer to fetch (up to 40 us) than the sums to read.
+    // What this CTA has of a row tile, to a place of its own: nobody else's piece is read or waited for here.
     auto flush = [&] {
       const bool lost = dead;
       float* part = args.parts + (row_tile + cta) * (N * T::kTile) + wg * 128 + (warp & 3) * 32 + lane;

@@ -406,7 +406,8 @@ def op_argmax(logits, stream=None):
 
 
 # ------------------------------------- per-head norm + rotation, 4-bit paged cache
-# These, and the operators on 4-bit weights and drafted tokens, run once per layer or decode step: their checks, allocations and calls are in csrc/torch_ops.cpp (_ops.so).
+# These, and the operators on 4-bit weights and drafted tokens, run once per layer or decode step: their checks, allocations
+# and calls are in csrc/torch_ops.cpp (_ops.so).
 # A call with no tokens, rows or requests is refused: leave it out.
 _FAST_NAMES = ("thinfer_op_qk_norm_rope", "thinfer_op_kv4_reserve", "thinfer_op_kv4_append", "thinfer_op_kv4_read",
                "thinfer_kv4_attention_workspace", "thinfer_op_kv4_attention", "thinfer_kv4_pages_workspace", "thinfer_op_kv4_fork",
